@@ -90,6 +90,10 @@ extern "C" {
                              paper names regression as the method's other use,
                              Section 5) */
 
+#define PMLP_GATED 4      /* pmlp_create_block flags: a second input projection V1 that */
+#define PMLP_NORM 8       /* the activations multiply; a layer norm over each model's
+                             hidden units */
+
 typedef struct pmlp* pmlp_t;
 
 /* Create a packed model of M MLPs with F inputs and O outputs each.
@@ -162,6 +166,51 @@ int pmlp_set_params_deep(pmlp_t h, const float* W1_host, const float* W12_host,
 /* N2 (second-layer units) and K (entries of all W12 blocks) of a
  * two-hidden-layer pack; PMLP_ESTATE for a one-layer handle. */
 int pmlp_info_deep(pmlp_t h, int64_t* N2, int64_t* K);
+
+/* A pack of M one-hidden-layer MLPs whose hidden layer is a feed-forward block
+ * (one of the flags at least; PMLP_MSE adds the regression head):
+ *   PMLP_GATED  H = act_m(X W1^T) * (X V1^T), two projections of the input, one
+ *               of them through the model's activation (without: H = act_m(X W1^T));
+ *   PMLP_NORM   every model's hidden vector is normalised over its own h_m units,
+ *               per sample: T = gain * (H - mu) / sqrt(var + 1e-5) + shift, var the
+ *               mean square of H - mu (without: T = H).  The norm of a model of one
+ *               unit is its shift.
+ * and logits[b,m,o] = sum_{n in model m} T[b,n] W2[o,n].  Parameters
+ * (pmlp_get_params_block): W1 and V1 [N, F], W2 [O, N], gain and shift [N].
+ * Initial values: W1 and W2 as pmlp_create, V1 as W1 with tag 6, gain 1, shift 0.
+ * The products are fp32 (PMLP_FP32 of pmlp_set_precision); where operands or
+ * hidden values are not finite the logits and gradients of their samples (their
+ * models) may be NaN where another order of summation gives infinity.
+ * Such a handle takes pmlp_forward, pmlp_train_step[_lr|_mse], pmlp_losses,
+ * pmlp_nonfinite, pmlp_info, pmlp_set_stream, profiling and the _block calls below;
+ * the other calls, the bf16 modes, biases and feature masks return PMLP_ESTATE.
+ * Workspaces that a larger batch replaces are kept until pmlp_destroy, so that
+ * graphs captured with them stay valid; a capture that would have to grow them
+ * returns PMLP_ESTATE (call once with that batch size first).  Calls and graph
+ * replays of one handle share its workspace: keep them in order.
+ * Arguments as for pmlp_create. */
+int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* hidden_sizes,
+                      const int32_t* act_ids, uint64_t seed, int32_t flags);
+
+/* Gradients of sum_m L_m of a block pack on one batch without an update (device,
+ * fp32): dW1_dev and dV1_dev [N, F], dW2_dev [O, N], dgain_dev and dshift_dev [N].
+ * Buffers of what the pack does not have are ignored.  Records the batch losses.
+ * The _mse call is that of a PMLP_MSE handle (targets Y_dev [B, O]).  PMLP_ESTATE
+ * for other handles. */
+int pmlp_gradients_block(pmlp_t h, const float* X_dev, const int32_t* y_dev, int32_t B,
+                         float* dW1_dev, float* dV1_dev, float* dW2_dev, float* dgain_dev,
+                         float* dshift_dev);
+int pmlp_gradients_block_mse(pmlp_t h, const float* X_dev, const float* Y_dev, int32_t B,
+                             float* dW1_dev, float* dV1_dev, float* dW2_dev, float* dgain_dev,
+                             float* dshift_dev);
+
+/* Parameters of a block pack to / from host memory in the layout above (any
+ * pointer may be null; one that the pack does not have returns PMLP_EINVAL).
+ * Synchronous. */
+int pmlp_get_params_block(pmlp_t h, float* W1_host, float* V1_host, float* W2_host,
+                          float* gain_host, float* shift_host);
+int pmlp_set_params_block(pmlp_t h, const float* W1_host, const float* V1_host,
+                          const float* W2_host, const float* gain_host, const float* shift_host);
 
 /* Free the handle and every device buffer it owns (synchronises its
  * stream first).  A null handle is accepted. */

@@ -29,7 +29,8 @@ __all__ = [
     "pmlp_set_feature_mask", "pmlp_get_models", "pmlp_create_deep", "pmlp_gradients_deep",
     "pmlp_get_params_deep", "pmlp_set_params_deep", "pmlp_info_deep", "pmlp_kernel_variant",
     "PMLP_ARITH_NONE", "PMLP_ARITH_FP32", "PMLP_ARITH_X3", "PMLP_ARITH_BF16", "PackedMLP",
-    "DeepPackedMLP",
+    "DeepPackedMLP", "PMLP_GATED", "PMLP_NORM", "pmlp_create_block", "pmlp_gradients_block",
+    "pmlp_gradients_block_mse", "pmlp_get_params_block", "pmlp_set_params_block", "BlockPackedMLP",
 ]
 
 PMLP_OK = 0
@@ -42,6 +43,8 @@ PMLP_BF16_GEMM = 1
 PMLP_BF16_STORE = 2
 PMLP_BIAS = 1
 PMLP_MSE = 2
+PMLP_GATED = 4
+PMLP_NORM = 8
 PMLP_NUM_KERNELS = 11
 
 ACT_IDS = {
@@ -106,6 +109,11 @@ def load_library():
         "pmlp_get_params_deep": [P, P, P, P],
         "pmlp_set_params_deep": [P, P, P, P],
         "pmlp_info_deep": [P, C.POINTER(i64), C.POINTER(i64)],
+        "pmlp_create_block": [C.POINTER(P), i32, i32, i32, P, P, u64, i32],
+        "pmlp_gradients_block": [P, P, P, i32, P, P, P, P, P],
+        "pmlp_gradients_block_mse": [P, P, P, i32, P, P, P, P, P],
+        "pmlp_get_params_block": [P, P, P, P, P, P],
+        "pmlp_set_params_block": [P, P, P, P, P, P],
         "pmlp_kernel_variant": [P, i32, C.POINTER(C.c_char_p), C.POINTER(i32)],
     }
     for name, args in sig.items():
@@ -335,6 +343,57 @@ def pmlp_set_params_deep(h: int, W1=None, W12=None, W2=None) -> None:
         arrs.append(c)
     _check(load_library().pmlp_set_params_deep(h, *[None if c is None else c.ctypes.data
                                                     for c in arrs]), "pmlp_set_params_deep")
+
+
+def pmlp_create_block(F: int, O: int, hidden_sizes: Sequence[int], act_ids: Sequence[int],
+                      seed: int, flags: int) -> int:
+    hs = _host(hidden_sizes, np.int32)
+    ac = _host(act_ids, np.int32)
+    if hs.shape != ac.shape or hs.ndim != 1:
+        raise ValueError("hidden_sizes and act_ids must be 1-D of equal length")
+    h = C.c_void_p()
+    _check(load_library().pmlp_create_block(C.byref(h), int(F), int(O), int(hs.size),
+                                            hs.ctypes.data, ac.ctypes.data,
+                                            int(seed) & 0xFFFFFFFFFFFFFFFF, int(flags)),
+           "pmlp_create_block")
+    return h.value
+
+
+def pmlp_gradients_block(h: int, X, y, B: int, dW1, dV1, dW2, dgain, dshift) -> None:
+    _check(load_library().pmlp_gradients_block(h, _ptr(X), _ptr(y), int(B), _ptr(dW1), _ptr(dV1),
+                                               _ptr(dW2), _ptr(dgain), _ptr(dshift)),
+           "pmlp_gradients_block")
+
+
+def pmlp_gradients_block_mse(h: int, X, Y, B: int, dW1, dV1, dW2, dgain, dshift) -> None:
+    _check(load_library().pmlp_gradients_block_mse(h, _ptr(X), _ptr(Y), int(B), _ptr(dW1),
+                                                   _ptr(dV1), _ptr(dW2), _ptr(dgain),
+                                                   _ptr(dshift)), "pmlp_gradients_block_mse")
+
+
+def _block_shapes(h: int):
+    N, _, F, O = pmlp_info(h)
+    return {"W1": (N, F), "V1": (N, F), "W2": (O, N), "gain": (N,), "shift": (N,)}
+
+
+def pmlp_get_params_block(h: int, names: Sequence[str]) -> Tuple[np.ndarray, ...]:
+    """The named parameters (of W1, V1, W2, gain, shift), in that order."""
+    shapes = _block_shapes(h)
+    got = {k: np.empty(shapes[k], np.float32) for k in names}
+    _check(load_library().pmlp_get_params_block(h, *[got[k].ctypes.data if k in got else None
+                                                     for k in shapes]), "pmlp_get_params_block")
+    return tuple(got[k] for k in names)
+
+
+def pmlp_set_params_block(h: int, W1=None, V1=None, W2=None, gain=None, shift=None) -> None:
+    arrs = []
+    for a, (what, shape) in zip((W1, V1, W2, gain, shift), _block_shapes(h).items()):
+        c = None if a is None else _host(a, np.float32)
+        if c is not None and c.shape != shape:
+            raise ValueError("%s must be %s" % (what, shape))
+        arrs.append(c)
+    _check(load_library().pmlp_set_params_block(h, *[None if c is None else c.ctypes.data
+                                                     for c in arrs]), "pmlp_set_params_block")
 
 
 def pmlp_set_feature_mask(h: int, mask: Optional[np.ndarray]) -> None:
@@ -589,3 +648,50 @@ class DeepPackedMLP(PackedMLP):
 
     def set_params(self, W1=None, W12=None, W2=None) -> None:
         pmlp_set_params_deep(self.handle, W1, W12, W2)
+
+
+class BlockPackedMLP(PackedMLP):
+    """M independent MLPs whose hidden layer is a feed-forward block: gated
+    (act(X W1^T) * (X V1^T)), with a layer norm over each model's hidden units
+    (gain, shift), or both.  Takes the forward, train_step (one rate, or per-model
+    rates for the "ce" head), losses and nonfinite_count calls of PackedMLP;
+    gradients and parameters are those of `param_names`."""
+
+    def __init__(self, F: int, O: int, hidden_sizes: Sequence[int], act_ids: Sequence[int],
+                 seed: int = 0, gated: bool = True, norm: bool = False, head: str = "ce"):
+        import torch
+        if head not in ("ce", "mse"):
+            raise ValueError("head must be 'ce' or 'mse'")
+        self._torch = torch
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.biases = False
+        self.head = head
+        self.gated, self.norm = bool(gated), bool(norm)
+        self.handle = pmlp_create_block(F, O, hidden_sizes, act_ids, seed,
+                                        (PMLP_GATED if gated else 0) | (PMLP_NORM if norm else 0)
+                                        | (PMLP_MSE if head == "mse" else 0))
+        self.N, self.M, self.F, self.O = pmlp_info(self.handle)
+        self.hidden_sizes = _host(hidden_sizes, np.int32)
+        self.act_ids = _host(act_ids, np.int32)
+        self.param_names = (("W1",) + (("V1",) if gated else ()) + ("W2",)
+                            + (("gain", "shift") if norm else ()))
+
+    def gradients(self, X, y):
+        """The gradients of param_names, in that order."""
+        B = self._x(X)
+        self._y(y, B)
+        t = self._torch
+        shapes = {"W1": (self.N, self.F), "V1": (self.N, self.F), "W2": (self.O, self.N),
+                  "gain": (self.N,), "shift": (self.N,)}
+        d = {k: t.empty(shapes[k], dtype=t.float32, device=self.device) for k in self.param_names}
+        self._stream()
+        call = pmlp_gradients_block_mse if self.head == "mse" else pmlp_gradients_block
+        call(self.handle, X, y, B, *[d.get(k) for k in shapes])
+        return tuple(d[k] for k in self.param_names)
+
+    def get_params(self) -> Tuple[np.ndarray, ...]:
+        """param_names, in that order."""
+        return pmlp_get_params_block(self.handle, self.param_names)
+
+    def set_params(self, W1=None, V1=None, W2=None, gain=None, shift=None) -> None:
+        pmlp_set_params_block(self.handle, W1, V1, W2, gain, shift)

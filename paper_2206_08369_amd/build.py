@@ -20,7 +20,7 @@ LIB = os.path.join(PKG, "libpmlp.so")
 SOURCES = [("k_lds.hip", [])]
 SOURCES += [("k_fwd_s.hip", ["-DPMLP_FWD_BP=%d" % bp]) for bp in (256, 128, 64, 32, 16)]
 SOURCES += [(s, []) for s in ("k_gemm_bf16.hip", "k_m3.hip", "k_misc.hip", "k_gemm.hip", "k_deep.hip",
-                              "api.hip")]
+                              "k_block.hip", "api.hip")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

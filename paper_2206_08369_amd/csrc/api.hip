@@ -3,6 +3,7 @@
 // declared and documented in include/pmlp.h.
 
 #include "pmlp.h"
+#include "block.h"
 #include "pmlp_internal.h"
 
 #include <algorithm>
@@ -99,6 +100,23 @@ struct PmlpDeep {
   float* Zt2 = nullptr;       // [N2pad][Bp]
 };
 
+// The gate and the norm of a pack made by pmlp_create_block (W1 is then the
+// first half of one allocation whose second half, if gated, is V1).
+struct PmlpBlock {
+  bool gated = false, norm = false;
+  float* V1 = nullptr;     // [Npad][F4], inside W1's allocation
+  float* gain = nullptr;   // [Npad]
+  float* shift = nullptr;  // [Npad]
+  BlkPiece* d_pieces = nullptr;
+  int32_t* d_poff = nullptr;  // [M+1]
+  int32_t npieces = 0;
+  // Workspace.  A captured graph keeps the addresses it was captured with, so a
+  // buffer that a larger batch replaces lives until the handle goes.
+  unsigned char* ws = nullptr;
+  size_t cap = 0;
+  std::vector<unsigned char*> retired;
+};
+
 // How a batch class (a padded batch size up to 256) divides the pack for
 // k_fwd_s: groups of whole models, widest first, for passes of one batch and
 // of many.  Made by the first forward pass that needs it.
@@ -155,6 +173,7 @@ struct pmlp {
   unsigned short* W1b = nullptr;  // [Npad][bf16_ld(F4)] bf16 of W1 (operand of Z = X W1^T)
   bool w1b_valid = false;         // W1b equals bf16(W1)
   PmlpDeep* deep = nullptr;     // second hidden layer (pmlp_create_deep), or null
+  PmlpBlock* block = nullptr;   // gate and norm (pmlp_create_block), or null
   float* stage = nullptr;       // rows on their way to or from the host (copy_rows)
   size_t cap_stage = 0;         // floats, at most kStageFloats
   uint32_t* d_fmask = nullptr;  // per-model feature masks [M][fmw] (null: none)
@@ -226,6 +245,16 @@ void release(pmlp* h) {
     dfree(d->Zt2);
     delete d;
     h->deep = nullptr;
+  }
+  if (PmlpBlock* k = h->block) {
+    dfree(k->gain);
+    dfree(k->shift);
+    dfree(k->d_pieces);
+    dfree(k->d_poff);
+    dfree(k->ws);
+    for (unsigned char*& p : k->retired) dfree(p);
+    delete k;
+    h->block = nullptr;
   }
   h->w1b_valid = false;
   h->capBp = 0;
@@ -474,8 +503,12 @@ int check_handle(pmlp* h) {
   return PMLP_OK;
 }
 
-// Calls that a pack with two hidden layers does not provide.
+// Calls that a pack with two hidden layers, or with a gate or a norm, does not
+// provide.
 int one_layer_only(pmlp* h, const char* what) {
+  if (h->block)
+    return fail(PMLP_ESTATE, std::string(what) + " is not provided for a block pack (see "
+                                                 "pmlp_create_block)");
   if (h->deep)
     return fail(PMLP_ESTATE, std::string(what) + " is not provided for a pack with two hidden "
                                                  "layers");
@@ -1277,6 +1310,275 @@ int forward_logits(pmlp* h, const float* X, int32_t B, int32_t Bp, float* out) {
   });
 }
 
+// ---- block packs ---------------------------------------------------------------
+
+// Pieces of the forward's sums: whole models up to `cap` units (tile_cap: a small
+// pack still gives a few thousand waves), equal parts of wider ones.
+void block_pieces(const std::vector<int32_t>& hs, int64_t cap, std::vector<BlkPiece>& pieces,
+                  std::vector<int32_t>& poff) {
+  int64_t n = 0;
+  for (size_t m = 0; m < hs.size(); ++m) {
+    poff.push_back((int32_t)pieces.size());
+    const int32_t k = div_up(hs[m], cap), len = div_up(hs[m], k);
+    for (int32_t at = 0; at < hs[m]; at += len)
+      pieces.push_back(BlkPiece{n + at, std::min(len, hs[m] - at), (int32_t)m});
+    n += hs[m];
+  }
+  poff.push_back((int32_t)pieces.size());
+}
+
+BlkPack block_pack(const pmlp* h) {
+  const PmlpBlock* k = h->block;
+  BlkPack p{};
+  p.W1 = h->W1;
+  p.V1 = k->V1;
+  p.W2 = h->W2;
+  p.gain = k->gain;
+  p.shift = k->shift;
+  p.ldw = h->Npad;
+  p.N = h->N;
+  p.M = h->M;
+  p.O = h->O;
+  p.F = h->F;
+  p.F4 = h->F4;
+  p.seg_off = h->d_seg_off;
+  p.mid = h->d_mid;
+  p.actn = h->d_actn;
+  p.pieces = k->d_pieces;
+  p.poff = k->d_poff;
+  p.npieces = k->npieces;
+  return p;
+}
+
+// Parts of the block workspace, each 256-byte aligned, by their sizes in floats.
+struct Carver {
+  size_t bytes = 0;
+  size_t take(size_t floats) {
+    const size_t at = bytes;
+    bytes += align256(floats * sizeof(float));
+    return at;
+  }
+};
+
+int ensure_block_ws(pmlp* h, size_t bytes) {
+  PmlpBlock* k = h->block;
+  if (bytes <= k->cap) return PMLP_OK;
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  PMLP_HIP(hipStreamIsCapturing(h->stream, &st));
+  if (st != hipStreamCaptureStatusNone)
+    return fail(PMLP_ESTATE, "under graph capture a block pack needs an earlier call of this kind "
+                             "and batch size");
+  size_t want = bytes;
+  if (bytes < (size_t)64 << 20)  // few small buffers on the way to a large batch
+    for (want = (size_t)1 << 16; want < bytes;) want <<= 1;
+  unsigned char* p = nullptr;
+  if (hipMalloc(&p, want) != hipSuccess) {
+    (void)hipGetLastError();
+    return fail(PMLP_ENOMEM, "block workspace allocation failed (" + std::to_string(want >> 20) +
+                                 " MiB)");
+  }
+  try {
+    if (k->ws) k->retired.push_back(k->ws);
+  } catch (const std::bad_alloc&) {
+    dfree(p);
+    return fail(PMLP_ENOMEM, "host allocation failed");
+  }
+  k->ws = p;
+  k->cap = want;
+  return PMLP_OK;
+}
+
+// Zt (and Ut after it) = W1 (V1) Xp^T: one product over both halves of W1's
+// allocation.  The rows between N and Npad are zero.
+int block_product(pmlp* h, const float* Xp, float* Zt, int32_t Bp) {
+  const int64_t rows = h->block->gated ? h->Npad + h->N : h->N;
+  if (h->lds_kernels && fwd_lds_supported(Bp, h->F4)) {
+    FwdLdsArgs f{};
+    f.W1 = h->W1;
+    f.Xp = Xp;
+    f.Zt = Zt;
+    f.N = rows;
+    f.Bp = Bp;
+    f.K = h->F4;
+    return run(h, KID_GEMM_FWD, [&] { return launch_fwd_lds(f, h->stream); });
+  }
+  if (h->lds_kernels) {
+    GemmBfArgs g{};
+    g.P = h->W1;
+    g.ldp = g.kp = h->F4;
+    g.NP = rows;
+    g.Qf = Xp;
+    g.ldq = h->F4;
+    g.NQ = Bp;
+    g.K = h->F4;
+    g.out = Zt;
+    g.ldo = g.ncols = Bp;
+    return run(h, KID_GEMM_FWD, [&] { return launch_gemm_bf16(g, EPI_STORE, h->stream); });
+  }
+  GemmArgs g{};
+  g.P = h->W1;
+  g.ldp = h->F4;
+  g.NP = rows;
+  g.Q = Xp;
+  g.ldq = h->F4;
+  g.NQ = Bp;
+  g.K = h->F4;
+  g.out = Zt;
+  g.ldo = g.ncols = Bp;
+  return run(h, KID_GEMM_FWD, [&] { return launch_gemm(g, EPI_STORE, h->stream); });
+}
+
+// dW = dZ^T X stored into dW [N][F], or W -= lr dW where that is null.
+int block_weight_grad(pmlp* h, const float* dZt, const float* Xt, int32_t Bp, float* W, float* dW,
+                      float lr, const float* lrm) {
+  if (h->lds_kernels) {
+    GemmBfArgs g{};
+    g.P = dZt;
+    g.ldp = g.kp = Bp;
+    g.NP = h->N;
+    g.Qf = Xt;
+    g.ldq = Bp;
+    g.NQ = h->F4;
+    g.K = Bp;
+    g.out = dW ? dW : W;
+    g.ldo = dW ? h->F : h->F4;
+    g.ncols = h->F;
+    g.lr = lr;
+    g.lrm = lrm;
+    g.mid = h->d_mid;
+    g.bcol = -1;
+    return run(h, KID_GEMM_BWD,
+               [&] { return launch_gemm_bf16(g, dW ? EPI_GRAD : EPI_SGD, h->stream); });
+  }
+  GemmArgs g{};
+  g.P = dZt;
+  g.ldp = Bp;
+  g.NP = h->N;
+  g.Q = Xt;
+  g.ldq = Bp;
+  g.NQ = h->F4;
+  g.K = Bp;
+  g.out = dW ? dW : W;
+  g.ldo = dW ? h->F : h->F4;
+  g.ncols = h->F;
+  g.lr = lr;
+  g.lrm = lrm;
+  g.mid = h->d_mid;
+  g.bcol = -1;
+  return run(h, KID_GEMM_BWD, [&] { return launch_gemm(g, dW ? EPI_GRAD : EPI_SGD, h->stream); });
+}
+
+constexpr size_t kBlockSlice = (size_t)1 << 30;  // bytes of Z that a forward pass stores at once
+
+// Forward pass of a block pack.  A forward pass that stores its pre-activations
+// takes its samples in slices of at most kBlockSlice bytes of them (or 256 samples).
+int forward_block(pmlp* h, const float* X, int32_t B, float* out) {
+  const PmlpBlock* k = h->block;
+  const BlkPack p = block_pack(h);
+  const size_t rows = (size_t)h->Npad * (k->gated ? 2 : 1);
+  int32_t slice = B;
+  if ((size_t)pad_batch(B) * rows * sizeof(float) > kBlockSlice) {
+    const size_t fit = kBlockSlice / (rows * sizeof(float)) / 256 * 256;
+    slice = (int32_t)std::min<size_t>(std::max<size_t>(fit, 256), (size_t)B);
+  }
+  const int64_t sb = (int64_t)h->M * h->O, nout = (int64_t)B * sb;
+  // Logits over X itself go through the workspace: a slice would write over the
+  // samples of the next.
+  const uintptr_t x0 = (uintptr_t)X, x1 = x0 + (size_t)B * h->F * sizeof(float);
+  const uintptr_t l0 = (uintptr_t)out, l1 = l0 + (size_t)nout * sizeof(float);
+  const bool over = x0 < l1 && l0 < x1;
+  const int32_t Bp = pad_batch(slice);
+  Carver c;
+  const size_t oXp = c.take((size_t)Bp * h->F4), oXt = c.take((size_t)Bp * h->F4);
+  const size_t oZ = c.take(rows * Bp), oP = c.take((size_t)k->npieces * blk_planes(p) * Bp);
+  const size_t oL = over ? c.take((size_t)nout) : 0;
+  if (int rc = ensure_block_ws(h, c.bytes)) return rc;
+  float *Xp = (float*)(k->ws + oXp), *Xt = (float*)(k->ws + oXt), *Zt = (float*)(k->ws + oZ),
+        *part = (float*)(k->ws + oP), *dst = over ? (float*)(k->ws + oL) : out;
+  for (int32_t b0 = 0; b0 < B; b0 += slice) {
+    const int32_t n = std::min(slice, B - b0), np = pad_batch(n);
+    if (int rc = run(h, KID_PACK_X, [&] {
+          return launch_pack_x(X + (int64_t)b0 * h->F, n, h->F, np, h->F4, -1, Xp, Xt, nullptr, 0,
+                               h->stream);
+        }))
+      return rc;
+    if (int rc = block_product(h, Xp, Zt, np)) return rc;
+    if (int rc = run(h, KID_M3_FWD, [&] {
+          return launch_blk_fwd(p, Zt, k->gated ? Zt + h->Npad * np : nullptr, np, part, h->stream);
+        }))
+      return rc;
+    if (int rc = run(h, KID_CE, [&] {
+          return launch_blk_out(p, part, np, n, dst + b0 * sb, h->O, sb, h->stream);
+        }))
+      return rc;
+  }
+  if (!over) return PMLP_OK;
+  return run(h, KID_AUX, [&] { return launch_copy_rows(out, 1, dst, 1, nout, 1, h->stream); });
+}
+
+// Gradients of a block pack's parameters, as pmlp_gradients_block takes them
+// (all null: the SGD update).
+struct BlockGrads {
+  float *dW1, *dV1, *dW2, *dgain, *dshift;
+};
+
+int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_t B, float lr,
+               const float* lrm, const BlockGrads& d) {
+  const PmlpBlock* k = h->block;
+  const BlkPack p = block_pack(h);
+  const int32_t Bp = pad_batch(B);
+  if (int rc = use_device(h)) return rc;
+  const size_t rows = (size_t)h->Npad * (k->gated ? 2 : 1), mb = (size_t)h->M * Bp;
+  Carver c;
+  const size_t oXp = c.take((size_t)Bp * h->F4), oXt = c.take((size_t)Bp * h->F4);
+  const size_t oG = c.take(mb * h->O), oR = c.take(k->norm ? mb * 4 : 0),
+               oS = c.take(k->norm ? (size_t)h->M * h->O : 0);
+  const size_t oP = c.take((size_t)k->npieces * blk_planes(p) * Bp), oZ = c.take(rows * Bp);
+  if (int rc = ensure_block_ws(h, c.bytes)) return rc;
+  auto at = [&](size_t o) { return (float*)(k->ws + o); };
+  float* const Zt = at(oZ);
+  float* const Ut = k->gated ? Zt + h->Npad * Bp : nullptr;
+  if (int rc = run(h, KID_PACK_X, [&] {
+        return launch_pack_x(X, B, h->F, Bp, h->F4, -1, at(oXp), at(oXt), nullptr, 0, h->stream);
+      }))
+    return rc;
+  if (int rc = block_product(h, at(oXp), Zt, Bp)) return rc;
+  if (int rc = run(h, KID_M3_FWD,
+                   [&] { return launch_blk_fwd(p, Zt, Ut, Bp, at(oP), h->stream); }))
+    return rc;
+  const BlkLoss l{y, Y, B, at(oG), at(oR), at(oS), h->loss, h->flag, d.dW1 ? nullptr : lrm};
+  if (int rc = run(h, KID_CE, [&] { return launch_blk_loss(p, at(oP), Bp, l, h->stream); }))
+    return rc;
+  const BlkGrads g{d.dW2, d.dgain, d.dshift, lr, lrm};
+  if (int rc = run(h, KID_M3_BWD, [&] {
+        return launch_blk_bwd(p, Zt, Ut, Bp, at(oG), at(oR), at(oS), g, h->stream);
+      }))
+    return rc;
+  if (int rc = block_weight_grad(h, Zt, at(oXt), Bp, h->W1, d.dW1, lr, lrm)) return rc;
+  if (k->gated)
+    if (int rc = block_weight_grad(h, Ut, at(oXt), Bp, k->V1, d.dV1, lr, lrm)) return rc;
+  h->have_loss = true;
+  return PMLP_OK;
+}
+
+int check_block(pmlp* h) {
+  if (int rc = check_handle(h)) return rc;
+  if (!h->block)
+    return fail(PMLP_ESTATE, "the handle has no gate and no norm (see pmlp_create_block)");
+  return PMLP_OK;
+}
+
+// The gradient buffers of what the handle has, none of the others.
+int block_grads(pmlp* h, float* dW1, float* dV1, float* dW2, float* dgain, float* dshift,
+                BlockGrads* out) {
+  const PmlpBlock* k = h->block;
+  if (!dW1 || !dW2 || (k->gated && !dV1) || (k->norm && (!dgain || !dshift)))
+    return fail(PMLP_EINVAL, "null gradient buffer");
+  *out = BlockGrads{dW1, k->gated ? dV1 : nullptr, dW2, k->norm ? dgain : nullptr,
+                    k->norm ? dshift : nullptr};
+  return PMLP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1441,6 +1743,7 @@ int pmlp_forward(pmlp_t h, const float* X_dev, int32_t B, float* logits_dev) {
   const int32_t Bp = pad_batch(B);
   const int64_t nout = (int64_t)B * h->M * h->O;
   if (int rc = use_device(h)) return rc;
+  if (h->block) return forward_block(h, X_dev, B, logits_dev);
   // Logits over X itself go through the workspace: k_fwd_s and the batch copy
   // read X while they write (clear) logits.
   const uintptr_t x0 = (uintptr_t)X_dev, x1 = x0 + (size_t)B * h->F * sizeof(float);
@@ -1470,6 +1773,7 @@ int pmlp_train_step(pmlp_t h, const float* X_dev, const int32_t* y_dev, int32_t 
   if (!y_dev) return fail(PMLP_EINVAL, "null labels");
   if (!std::isfinite(lr)) return fail(PMLP_EINVAL, "learning rate is not finite");
   if (h->deep) return step_deep(h, X_dev, y_dev, B, lr, nullptr, nullptr, nullptr);
+  if (h->block) return step_block(h, X_dev, y_dev, nullptr, B, lr, nullptr, BlockGrads{});
   return step(h, X_dev, y_dev, B, lr, nullptr, nullptr, nullptr);
 }
 
@@ -1503,17 +1807,19 @@ int pmlp_train_step_noalloc(pmlp_t h, const float* X_dev, const int32_t* y_dev, 
 int pmlp_train_step_lr(pmlp_t h, const float* X_dev, const int32_t* y_dev, int32_t B,
                        const float* lr_dev) {
   if (int rc = check_batch(h, X_dev, B)) return rc;
-  if (int rc = one_layer_only(h, "pmlp_train_step_lr")) return rc;
+  if (!h->block)
+    if (int rc = one_layer_only(h, "pmlp_train_step_lr")) return rc;
   if (h->mse) return fail(PMLP_ESTATE, "a regression handle trains with pmlp_train_step_mse");
   if (!y_dev) return fail(PMLP_EINVAL, "null labels");
   if (!lr_dev) return fail(PMLP_EINVAL, "null per-model learning rates");
+  if (h->block) return step_block(h, X_dev, y_dev, nullptr, B, 0.f, lr_dev, BlockGrads{});
   return step(h, X_dev, y_dev, B, 0.f, lr_dev, nullptr, nullptr);
 }
 
 int pmlp_gradients(pmlp_t h, const float* X_dev, const int32_t* y_dev, int32_t B,
                    float* dW1_dev, float* dW2_dev) {
   if (int rc = check_batch(h, X_dev, B)) return rc;
-  if (int rc = one_layer_only(h, "pmlp_gradients (use pmlp_gradients_deep)")) return rc;
+  if (int rc = one_layer_only(h, "pmlp_gradients (use pmlp_gradients_deep or pmlp_gradients_block)")) return rc;
   if (h->mse) return fail(PMLP_ESTATE, "a regression handle uses pmlp_gradients_mse");
   if (!y_dev || !dW1_dev || !dW2_dev) return fail(PMLP_EINVAL, "null labels or gradient buffer");
   return step(h, X_dev, y_dev, B, 0.f, nullptr, dW1_dev, dW2_dev);
@@ -1521,10 +1827,12 @@ int pmlp_gradients(pmlp_t h, const float* X_dev, const int32_t* y_dev, int32_t B
 
 int pmlp_train_step_mse(pmlp_t h, const float* X_dev, const float* Y_dev, int32_t B, float lr) {
   if (int rc = check_batch(h, X_dev, B)) return rc;
-  if (int rc = one_layer_only(h, "pmlp_train_step_mse")) return rc;
+  if (!h->block)
+    if (int rc = one_layer_only(h, "pmlp_train_step_mse")) return rc;
   if (!h->mse) return fail(PMLP_ESTATE, "the handle was created without PMLP_MSE");
   if (!Y_dev) return fail(PMLP_EINVAL, "null targets");
   if (!std::isfinite(lr)) return fail(PMLP_EINVAL, "learning rate is not finite");
+  if (h->block) return step_block(h, X_dev, nullptr, Y_dev, B, lr, nullptr, BlockGrads{});
   return step(h, X_dev, Y_dev, B, lr, nullptr, nullptr, nullptr);
 }
 
@@ -1611,7 +1919,7 @@ int pmlp_losses(pmlp_t h, float* out_host) {
 
 int pmlp_get_params(pmlp_t h, float* W1_host, float* W2_host) {
   if (int rc = check_handle(h)) return rc;
-  if (int rc = one_layer_only(h, "pmlp_get_params (use pmlp_get_params_deep)")) return rc;
+  if (int rc = one_layer_only(h, "pmlp_get_params (use pmlp_get_params_deep or pmlp_get_params_block)")) return rc;
   if (int rc = use_device(h)) return rc;
   PMLP_HIP(hipStreamSynchronize(h->stream));
   if (W1_host)
@@ -1623,7 +1931,7 @@ int pmlp_get_params(pmlp_t h, float* W1_host, float* W2_host) {
 
 int pmlp_set_params(pmlp_t h, const float* W1_host, const float* W2_host) {
   if (int rc = check_handle(h)) return rc;
-  if (int rc = one_layer_only(h, "pmlp_set_params (use pmlp_set_params_deep)")) return rc;
+  if (int rc = one_layer_only(h, "pmlp_set_params (use pmlp_set_params_deep or pmlp_set_params_block)")) return rc;
   if (int rc = use_device(h)) return rc;
   PMLP_HIP(hipStreamSynchronize(h->stream));
   if (W1_host) h->w1b_valid = false;
@@ -1885,6 +2193,138 @@ int pmlp_create_deep(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t
   }
   *out = h;
   return PMLP_OK;
+}
+
+int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* hidden_sizes,
+                      const int32_t* act_ids, uint64_t seed, int32_t flags) {
+  if (!out) return fail(PMLP_EINVAL, "null output handle pointer");
+  *out = nullptr;
+  if (flags & ~(PMLP_GATED | PMLP_NORM | PMLP_MSE)) return fail(PMLP_EINVAL, "unknown flags");
+  if (!(flags & (PMLP_GATED | PMLP_NORM)))
+    return fail(PMLP_EINVAL, "a block pack has a gate, a norm or both (pmlp_create_ex makes packs "
+                             "without)");
+  pmlp_t h = nullptr;  // checks the rest
+  if (int rc = pmlp_create_ex(&h, F, O, M, hidden_sizes, act_ids, seed, flags & PMLP_MSE)) return rc;
+  PmlpBlock* k = new (std::nothrow) PmlpBlock();
+  if (!k) {
+    pmlp_destroy(h);
+    return fail(PMLP_ENOMEM, "host allocation failed");
+  }
+  h->block = k;
+  k->gated = (flags & PMLP_GATED) != 0;
+  k->norm = (flags & PMLP_NORM) != 0;
+  std::vector<BlkPiece> pieces;
+  std::vector<int32_t> poff;
+  try {
+    block_pieces(h->hs, tile_cap(h->N), pieces, poff);
+  } catch (const std::bad_alloc&) {
+    pmlp_destroy(h);
+    return fail(PMLP_ENOMEM, "host allocation failed");
+  }
+  k->npieces = (int32_t)pieces.size();
+  const size_t half = (size_t)h->Npad * h->F4, units = (size_t)h->Npad * sizeof(float);
+  float* W = nullptr;
+  if ((k->gated && hipMalloc(&W, (2 * half + 64) * sizeof(float)) != hipSuccess) ||
+      (k->norm && (hipMalloc(&k->gain, units) != hipSuccess ||
+                   hipMalloc(&k->shift, units) != hipSuccess)) ||
+      hipMalloc(&k->d_pieces, pieces.size() * sizeof(BlkPiece)) != hipSuccess ||
+      hipMalloc(&k->d_poff, poff.size() * sizeof(int32_t)) != hipSuccess) {
+    (void)hipGetLastError();
+    dfree(W);
+    pmlp_destroy(h);
+    return fail(PMLP_ENOMEM, "device allocation failed for the block parameters");
+  }
+  auto setup = [&]() -> int {
+    if (k->gated) {
+      PMLP_HIP(hipMemset(W, 0, (2 * half + 64) * sizeof(float)));
+      PMLP_HIP(hipMemcpy(W, h->W1, half * sizeof(float), hipMemcpyDeviceToDevice));
+      std::swap(W, h->W1);
+      k->V1 = h->W1 + half;
+    }
+    if (k->norm) {
+      PMLP_HIP(hipMemset(k->gain, 0, units));
+      PMLP_HIP(hipMemset(k->shift, 0, units));
+    }
+    PMLP_HIP(hipMemcpy(k->d_pieces, pieces.data(), pieces.size() * sizeof(BlkPiece),
+                       hipMemcpyHostToDevice));
+    PMLP_HIP(hipMemcpy(k->d_poff, poff.data(), poff.size() * sizeof(int32_t),
+                       hipMemcpyHostToDevice));
+    PMLP_HIP(launch_blk_init(k->V1, h->N, F, h->F4, (float)(1.0 / std::sqrt((double)F)),
+                             splitmix64_host(seed), k->gain, k->shift, nullptr));
+    PMLP_HIP(hipStreamSynchronize(nullptr));
+    return PMLP_OK;
+  };
+  const int rc = setup();
+  dfree(W);
+  if (rc) {
+    pmlp_destroy(h);
+    return rc;
+  }
+  *out = h;
+  return PMLP_OK;
+}
+
+int pmlp_gradients_block(pmlp_t h, const float* X_dev, const int32_t* y_dev, int32_t B,
+                         float* dW1_dev, float* dV1_dev, float* dW2_dev, float* dgain_dev,
+                         float* dshift_dev) {
+  if (int rc = check_batch(h, X_dev, B)) return rc;
+  if (int rc = check_block(h)) return rc;
+  if (h->mse) return fail(PMLP_ESTATE, "a regression handle uses pmlp_gradients_block_mse");
+  if (!y_dev) return fail(PMLP_EINVAL, "null labels");
+  BlockGrads d;
+  if (int rc = block_grads(h, dW1_dev, dV1_dev, dW2_dev, dgain_dev, dshift_dev, &d)) return rc;
+  return step_block(h, X_dev, y_dev, nullptr, B, 0.f, nullptr, d);
+}
+
+int pmlp_gradients_block_mse(pmlp_t h, const float* X_dev, const float* Y_dev, int32_t B,
+                             float* dW1_dev, float* dV1_dev, float* dW2_dev, float* dgain_dev,
+                             float* dshift_dev) {
+  if (int rc = check_batch(h, X_dev, B)) return rc;
+  if (int rc = check_block(h)) return rc;
+  if (!h->mse) return fail(PMLP_ESTATE, "the handle was created without PMLP_MSE");
+  if (!Y_dev) return fail(PMLP_EINVAL, "null targets");
+  BlockGrads d;
+  if (int rc = block_grads(h, dW1_dev, dV1_dev, dW2_dev, dgain_dev, dshift_dev, &d)) return rc;
+  return step_block(h, X_dev, nullptr, Y_dev, B, 0.f, nullptr, d);
+}
+
+namespace {
+
+// The parameters of a block pack, to the host or from it.
+int copy_block(pmlp* h, float* W1, float* V1, float* W2, float* gain, float* shift, bool to_host) {
+  if (int rc = check_block(h)) return rc;
+  const PmlpBlock* k = h->block;
+  if ((V1 && !k->gated) || ((gain || shift) && !k->norm))
+    return fail(PMLP_EINVAL, V1 && !k->gated ? "the pack has no gate (V1)"
+                                             : "the pack has no norm (gain, shift)");
+  if (int rc = use_device(h)) return rc;
+  PMLP_HIP(hipStreamSynchronize(h->stream));
+  const int64_t N = h->N;
+  if (W1)
+    if (int rc = copy_rows(h, h->W1, h->F4, W1, h->F, N, to_host)) return rc;
+  if (V1)
+    if (int rc = copy_rows(h, k->V1, h->F4, V1, h->F, N, to_host)) return rc;
+  if (W2)
+    if (int rc = copy_rows(h, h->W2, h->Npad, W2, N, h->O, to_host)) return rc;
+  if (gain)
+    if (int rc = copy_rows(h, k->gain, N, gain, N, 1, to_host)) return rc;
+  if (shift)
+    if (int rc = copy_rows(h, k->shift, N, shift, N, 1, to_host)) return rc;
+  return PMLP_OK;
+}
+
+}  // namespace
+
+int pmlp_get_params_block(pmlp_t h, float* W1_host, float* V1_host, float* W2_host,
+                          float* gain_host, float* shift_host) {
+  return copy_block(h, W1_host, V1_host, W2_host, gain_host, shift_host, true);
+}
+
+int pmlp_set_params_block(pmlp_t h, const float* W1_host, const float* V1_host,
+                          const float* W2_host, const float* gain_host, const float* shift_host) {
+  return copy_block(h, const_cast<float*>(W1_host), const_cast<float*>(V1_host),
+                    const_cast<float*>(W2_host), const_cast<float*>(gain_host),
+                    const_cast<float*>(shift_host), false);
 }
 
 int pmlp_gradients_deep(pmlp_t h, const float* X_dev, const int32_t* y_dev, int32_t B,

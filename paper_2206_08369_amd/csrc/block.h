@@ -1,0 +1,89 @@
+// Block packs (pmlp_create_block): a gated hidden layer, a layer norm over each
+// model's hidden units, or both.  Declarations shared by the host library and
+// the kernels of k_block*.hip.
+#pragma once
+
+#include "pmlp_internal.h"
+
+namespace pmlpk {
+
+constexpr float kNormEps = 1e-5f;
+
+// Consecutive hidden units of one model: what one wave (workgroup) of the
+// forward sums.  Models wider than the plan's cap have several pieces, which the
+// output kernels merge in order.
+struct BlkPiece {
+  int64_t n0;
+  int32_t len, m;
+};
+static_assert(sizeof(BlkPiece) == 16, "BlkPiece layout");
+
+// The pack as the block kernels see it.
+struct BlkPack {
+  const float* W1;      // [Npad][F4]
+  const float* V1;      // [Npad][F4], or null (no gate)
+  float* W2;            // [O][ldw]
+  float* gain;          // [Npad], or null (no norm)
+  float* shift;         // [Npad]
+  int64_t ldw;          // = Npad
+  int64_t N;
+  int32_t M, O, F, F4;
+  const int64_t* seg_off;  // [M+1]
+  const int32_t* mid;      // [Npad]
+  const int32_t* actn;     // [Npad]
+  const BlkPiece* pieces;  // in unit order
+  const int32_t* poff;     // [M+1] first piece of each model
+  int32_t npieces;
+};
+
+// Per piece and sample, planar: part[(piece * PQ + q) * Bp + b], q < O the sums
+// S_o over the piece's units, and with a norm the mean and the sum of squared
+// deviations of its hidden values after them.
+inline int32_t blk_planes(const BlkPack& p) { return p.O + (p.gain ? 2 : 0); }
+
+// Z (and U) stored batch-minor: Zt [Npad][Bp], Ut [Npad][Bp] (null: no gate).
+hipError_t launch_blk_fwd(const BlkPack& p, const float* Zt, const float* Ut, int32_t Bp,
+                          float* part, hipStream_t s);
+
+// Logits out[b sb + m sm + o] of B samples from the pieces' sums.
+hipError_t launch_blk_out(const BlkPack& p, const float* part, int32_t Bp, int32_t B, float* out,
+                          int64_t sm, int64_t sb, hipStream_t s);
+
+// Losses and what the backward reads, from the pieces' sums:
+//   G [M][Bp][O]  dLoss/dlogits (0 past the batch)
+//   R [M][Bp][4]  with a norm: mu, r, a1, a2 (see k_blk_bwd)
+//   Gs [M][O]     with a norm: sum_b G
+// y: labels int32 [B], or Y float [B][O] for the regression head; flags as
+// launch_ce.
+struct BlkLoss {
+  const int32_t* y;
+  const float* Y;
+  int32_t B;
+  float* G;
+  float* R;
+  float* Gs;
+  float* loss;
+  int32_t* flag;
+  const float* lrm;
+};
+hipError_t launch_blk_loss(const BlkPack& p, const float* part, int32_t Bp, const BlkLoss& l,
+                           hipStream_t s);
+
+// Gradients of the output weights, gains and shifts (stored, or applied with
+// the rate lr or lrm[m] where dW2 is null).
+struct BlkGrads {
+  float* dW2;     // [O][N]
+  float* dgain;   // [N]
+  float* dshift;  // [N]
+  float lr;
+  const float* lrm;
+};
+// dZ over Zt and dU over Ut, in place.
+hipError_t launch_blk_bwd(const BlkPack& p, float* Zt, float* Ut, int32_t Bp, const float* G,
+                          const float* R, const float* Gs, const BlkGrads& g, hipStream_t s);
+
+// V1 (tag 6, like W1), gain 1, shift 0 (either may be null).
+hipError_t launch_blk_init(float* V1, int64_t N, int32_t F, int32_t F4, float bound, uint64_t key,
+                           float* gain, float* shift, hipStream_t s);
+
+}  // namespace pmlpk

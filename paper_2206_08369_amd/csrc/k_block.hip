@@ -1,0 +1,482 @@
+// Block packs: the gated hidden layer and the layer norm of packed MLPs, on
+// pre-activations that are stored (any shape), and the output and loss kernels
+// that every path shares.
+//
+// Model m's hidden values are H = act_m(X W1^T), or, gated, act_m(X W1^T) *
+// (X V1^T).  With a norm the output weights see g Hh + s, Hh = (H - mu) r over
+// the model's own h units, r = (var + eps)^-1/2.  As the output product is
+// linear, its sums and the norm's statistics come from one pass over the units:
+//   S_o = sum_n H_n g_n W2[o,n],  C_o = sum_n g_n W2[o,n],  D_o = sum_n s_n W2[o,n]
+//   P_o = r (S_o - mu C_o),       logits_o = P_o + D_o
+// and the two means over the units that the norm's gradient needs come from the
+// outputs' gradients G, with no pass of their own:
+//   dN_n = sum_o G_o W2[o,n]                      (gradient of g Hh + s)
+//   dH_n = r (g_n dN_n - a1 - Hh_n a2)
+//   a1 = 1/h sum_n g_n dN_n = 1/h sum_o G_o C_o,  a2 = 1/h sum_n g_n dN_n Hh_n = 1/h sum_o G_o P_o.
+// With T_o = sum_b G_o Hh_n the parameters' gradients are
+//   dW2[o,n] = g_n T_o + s_n sum_b G_o,  dg_n = sum_o W2[o,n] T_o,  ds_n = sum_o W2[o,n] sum_b G_o.
+// The statistics are running means and sums of squared deviations (Welford's
+// update; two sets merge by Chan, Golub and LeVeque's formula), all in fp32: a sum
+// of squares minus a squared mean would lose the variance of a layer whose mean is
+// large.  S_o - mu C_o cancels no worse than H - mu does.
+
+#include "block.h"
+#include "device_common.h"
+
+namespace pmlpk {
+
+namespace {
+
+constexpr int kFU = 4;  // units per lane group whose loads are in flight
+
+// (n, mean, M2) of the union of two sets
+__device__ __forceinline__ void merge_stats(float& n, float& mean, float& m2, float nb, float meanb,
+                                            float m2b) {
+  const float t = n + nb;
+  const float f = t > 0.f ? nb / t : 0.f;
+  const float d = meanb - mean;
+  mean = fmaf(d, f, mean);
+  m2 += m2b + d * d * n * f;
+  n = t;
+}
+
+// One wave per (piece, block of 4 LG samples).  Lane l takes four samples and
+// every NG-th unit (LG = lanes per unit, NG = 64 / LG), as k_m3_fwd.  Bound by
+// reading Z and U once.
+template <int OM, bool GATED, bool NORM>
+__global__ __launch_bounds__(kBlock) void k_blk_fwd(BlkPack p, const float* __restrict__ Zt,
+                                                    const float* __restrict__ Ut, int Bp, int LG,
+                                                    int nbblk, float* __restrict__ part) {
+  const int lane = threadIdx.x & 63;
+  const int64_t wv = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int pc = (int)(wv / nbblk), blk = (int)(wv - (int64_t)pc * nbblk);
+  if (pc >= p.npieces) return;
+  const BlkPiece q = p.pieces[pc];
+  const int NG = 64 / LG, g = lane / LG;
+  const int b = 4 * (blk * LG + lane - g * LG);
+  const bool valid = b < Bp;
+  const int bl = valid ? b : Bp - 4;
+  const int a = p.actn[q.n0];
+  float S[4][OM];
+  float mean[4] = {0.f, 0.f, 0.f, 0.f}, m2[4] = {0.f, 0.f, 0.f, 0.f}, cnt = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int o = 0; o < OM; ++o) S[i][o] = 0.f;
+  for (int u0 = g; u0 < q.len; u0 += kFU * NG) {
+    f32x4 z[kFU], v[kFU];
+    float w[kFU][OM];
+#pragma unroll
+    for (int u = 0; u < kFU; ++u) {  // (past the piece: its last unit, not used)
+      const int k = u0 + u * NG < q.len ? u0 + u * NG : q.len - 1;
+      const int64_t n = q.n0 + k;
+      z[u] = *(const f32x4*)(Zt + n * Bp + bl);
+      if (GATED) v[u] = *(const f32x4*)(Ut + n * Bp + bl);
+      const float gn = NORM ? p.gain[n] : 1.f;
+#pragma unroll
+      for (int o = 0; o < OM; ++o) w[u][o] = o < p.O ? p.W2[(int64_t)o * p.ldw + n] * gn : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < kFU; ++u) {
+      if (u0 + u * NG >= q.len) break;
+      cnt += 1.f;
+      const float rc = NORM ? 1.f / cnt : 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float h = act_fwd(a, z[u][i]);
+        if (GATED) h *= v[u][i];
+        if (NORM) {
+          const float d = h - mean[i];
+          mean[i] = fmaf(d, rc, mean[i]);
+          m2[i] = fmaf(d, h - mean[i], m2[i]);
+        }
+#pragma unroll
+        for (int o = 0; o < OM; ++o) S[i][o] = fmaf(h, w[u][o], S[i][o]);
+      }
+    }
+  }
+  for (int s = LG; s < 64; s <<= 1) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int o = 0; o < OM; ++o) S[i][o] += __shfl_xor(S[i][o], s);
+    if (NORM) {
+      const float nb = __shfl_xor(cnt, s);
+      float n = cnt;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float mb = __shfl_xor(mean[i], s), qb = __shfl_xor(m2[i], s);
+        n = cnt;
+        merge_stats(n, mean[i], m2[i], nb, mb, qb);
+      }
+      cnt = n;
+    }
+  }
+  if (g != 0 || !valid) return;
+  float* dst = part + (int64_t)pc * (p.O + (NORM ? 2 : 0)) * Bp + b;
+#pragma unroll
+  for (int o = 0; o < OM; ++o)
+    if (o < p.O) *(f32x4*)(dst + (int64_t)o * Bp) = f32x4{S[0][o], S[1][o], S[2][o], S[3][o]};
+  if (NORM) {
+    *(f32x4*)(dst + (int64_t)p.O * Bp) = f32x4{mean[0], mean[1], mean[2], mean[3]};
+    *(f32x4*)(dst + (int64_t)(p.O + 1) * Bp) = f32x4{m2[0], m2[1], m2[2], m2[3]};
+  }
+}
+
+// C_o and D_o of model m, summed by the 64 lanes of a wave.
+template <int OM>
+__device__ __forceinline__ void norm_consts(const BlkPack& p, int m, int lane, float (&C)[OM],
+                                            float (&D)[OM]) {
+#pragma unroll
+  for (int o = 0; o < OM; ++o) C[o] = D[o] = 0.f;
+  for (int64_t n = p.seg_off[m] + lane; n < p.seg_off[m + 1]; n += 64) {
+    const float gn = p.gain[n], sn = p.shift[n];
+#pragma unroll
+    for (int o = 0; o < OM; ++o) {
+      const float w = o < p.O ? p.W2[(int64_t)o * p.ldw + n] : 0.f;
+      C[o] = fmaf(gn, w, C[o]);
+      D[o] = fmaf(sn, w, D[o]);
+    }
+  }
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1)
+#pragma unroll
+    for (int o = 0; o < OM; ++o) {
+      C[o] += __shfl_xor(C[o], s);
+      D[o] += __shfl_xor(D[o], s);
+    }
+}
+
+// The sums of model m and sample b over its pieces: with a norm P_o and the
+// statistics (mu, r), else the logits.  r = 0 for a model of one unit, whose norm
+// is constant, so that its gradient is exactly zero.
+template <int OM, bool NORM>
+__device__ __forceinline__ void merge_pieces(const BlkPack& p, const float* __restrict__ part, int m,
+                                             int Bp, int b, const float (&C)[OM], float (&P)[OM],
+                                             float* mu, float* r) {
+  float n = 0.f, mean = 0.f, m2 = 0.f;
+#pragma unroll
+  for (int o = 0; o < OM; ++o) P[o] = 0.f;
+  const int k1 = p.poff[m + 1];
+  for (int k = p.poff[m]; k < k1; ++k) {
+    const float* src = part + (int64_t)k * (p.O + (NORM ? 2 : 0)) * Bp + b;
+#pragma unroll
+    for (int o = 0; o < OM; ++o)
+      if (o < p.O) P[o] += src[(int64_t)o * Bp];
+    if (NORM)
+      merge_stats(n, mean, m2, (float)p.pieces[k].len, src[(int64_t)p.O * Bp],
+                  src[(int64_t)(p.O + 1) * Bp]);
+  }
+  if (NORM) {
+    const float rr = n > 1.f ? 1.f / sqrtf(m2 / n + kNormEps) : 0.f;
+#pragma unroll
+    for (int o = 0; o < OM; ++o) P[o] = rr * (P[o] - mean * C[o]);
+    *mu = mean;
+    *r = rr;
+  }
+}
+
+constexpr int kOutSamples = 1024;  // samples of a model per wave, at most
+
+template <int OM, bool NORM>
+__global__ __launch_bounds__(kBlock) void k_blk_out(BlkPack p, const float* __restrict__ part,
+                                                    int Bp, int B, int nblk, float* __restrict__ out,
+                                                    int64_t sm, int64_t sb) {
+  const int lane = threadIdx.x & 63;
+  const int64_t wv = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int m = (int)(wv / nblk);
+  if (m >= p.M) return;
+  const int b0 = (int)(wv - (int64_t)m * nblk) * kOutSamples;
+  float C[OM], D[OM];
+  if (NORM) norm_consts<OM>(p, m, lane, C, D);
+  for (int b = b0 + lane; b < B && b < b0 + kOutSamples; b += 64) {
+    float P[OM], mu, r;
+    merge_pieces<OM, NORM>(p, part, m, Bp, b, C, P, &mu, &r);
+#pragma unroll
+    for (int o = 0; o < OM; ++o)
+      if (o < p.O) out[(int64_t)b * sb + (int64_t)m * sm + o] = NORM ? P[o] + D[o] : P[o];
+  }
+}
+
+// One workgroup per model, its threads over the samples.
+template <int OM, bool NORM>
+__global__ __launch_bounds__(1024) void k_blk_loss(BlkPack p, const float* __restrict__ part, int Bp,
+                                                   BlkLoss l, float scale) {
+  __shared__ float red[16][OM + 1];
+  const int m = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int B = l.B;
+  float C[OM], D[OM];
+  if (NORM) norm_consts<OM>(p, m, lane, C, D);
+  const float rh = 1.f / (float)(p.seg_off[m + 1] - p.seg_off[m]);
+  if (l.lrm && tid == 0 && !isfinite(l.lrm[m])) l.flag[1] = 1;
+  float loss = 0.f, gs[OM];
+#pragma unroll
+  for (int o = 0; o < OM; ++o) gs[o] = 0.f;
+  for (int b = tid; b < Bp; b += blockDim.x) {
+    float G[OM], P[OM], mu = 0.f, r = 0.f, a1 = 0.f, a2 = 0.f;
+    if (b < B) {
+      merge_pieces<OM, NORM>(p, part, m, Bp, b, C, P, &mu, &r);
+      float L[OM];
+#pragma unroll
+      for (int o = 0; o < OM; ++o) L[o] = NORM ? P[o] + D[o] : P[o];
+      if (l.Y) {
+#pragma unroll
+        for (int o = 0; o < OM; ++o) {
+          const float d = o < p.O ? L[o] - l.Y[(int64_t)b * p.O + o] : 0.f;
+          loss = fmaf(d, d, loss);
+          G[o] = 2.f * d * scale;
+        }
+      } else {
+        float mx = -INFINITY, se = 0.f, ly = 0.f;
+#pragma unroll
+        for (int o = 0; o < OM; ++o) mx = o < p.O ? fmaxf(mx, L[o]) : mx;
+#pragma unroll
+        for (int o = 0; o < OM; ++o)
+          if (o < p.O) se += expf(L[o] - mx);
+        const float lse = mx + logf(se);
+        const int yb = l.y[b];
+        if (yb < 0 || yb >= p.O) l.flag[0] = 1;
+#pragma unroll
+        for (int o = 0; o < OM; ++o) {
+          if (o == yb) ly = L[o];
+          G[o] = o < p.O ? (expf(L[o] - lse) - (o == yb ? 1.f : 0.f)) * scale : 0.f;
+        }
+        loss += lse - ly;
+      }
+      if (NORM) {
+#pragma unroll
+        for (int o = 0; o < OM; ++o) {
+          gs[o] += G[o];
+          a1 = fmaf(G[o], C[o], a1);
+          a2 = fmaf(G[o], P[o], a2);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int o = 0; o < OM; ++o) G[o] = 0.f;
+    }
+    float* row = l.G + ((int64_t)m * Bp + b) * p.O;
+#pragma unroll
+    for (int o = 0; o < OM; ++o)
+      if (o < p.O) row[o] = G[o];
+    if (NORM) *(f32x4*)(l.R + ((int64_t)m * Bp + b) * 4) = f32x4{mu, r, a1 * rh, a2 * rh};
+  }
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) {
+    loss += __shfl_xor(loss, s);
+    if (NORM)
+#pragma unroll
+      for (int o = 0; o < OM; ++o) gs[o] += __shfl_xor(gs[o], s);
+  }
+  if (lane == 0) {
+    red[wave][OM] = loss;
+#pragma unroll
+    for (int o = 0; o < OM; ++o) red[wave][o] = gs[o];
+  }
+  __syncthreads();
+  const int nw = blockDim.x >> 6;
+  if (tid == 0) {
+    float s = 0.f;
+    for (int w = 0; w < nw; ++w) s += red[w][OM];
+    l.loss[m] = s * scale;
+    if (!isfinite(s)) atomicAdd(l.flag + 2, 1);
+  }
+  if (NORM && tid < p.O) {
+    float s = 0.f;
+    for (int w = 0; w < nw; ++w) s += red[w][tid];
+    l.Gs[(int64_t)m * p.O + tid] = s;
+  }
+}
+
+// dZ over Z and dU over U; the gradients of W2, gain and shift.  LG lanes take a
+// unit's samples, four each and 4 LG a pass.  Bound by reading and writing Z and U
+// once.
+template <int OM, bool GATED, bool NORM>
+__global__ __launch_bounds__(kBlock) void k_blk_bwd(BlkPack p, float* __restrict__ Zt,
+                                                    float* __restrict__ Ut, int Bp, int LG,
+                                                    const float* __restrict__ G,
+                                                    const float* __restrict__ R,
+                                                    const float* __restrict__ Gs, BlkGrads out) {
+  const int lane = threadIdx.x & 63;
+  const int64_t wv = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int NG = 64 / LG, g = lane / LG, l = lane - g * LG;
+  const int64_t n = wv * NG + g;
+  if (n >= p.N) return;
+  const int m = p.mid[n], a = p.actn[n];
+  const float gn = NORM ? p.gain[n] : 1.f;
+  float w[OM], T[OM];
+#pragma unroll
+  for (int o = 0; o < OM; ++o) {
+    w[o] = o < p.O ? p.W2[(int64_t)o * p.ldw + n] : 0.f;
+    T[o] = 0.f;
+  }
+  for (int b = 4 * l; b < Bp; b += 4 * LG) {
+    f32x4 z = *(const f32x4*)(Zt + n * Bp + b), u = f32x4{1.f, 1.f, 1.f, 1.f};
+    if (GATED) u = *(const f32x4*)(Ut + n * Bp + b);
+    const float* gr = G + ((int64_t)m * Bp + b) * p.O;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float d;
+      const float av = act_fwd_bwd(a, z[i], &d);
+      float hv = GATED ? av * u[i] : av;
+      f32x4 st;
+      if (NORM) {
+        st = *(const f32x4*)(R + ((int64_t)m * Bp + b + i) * 4);
+        hv = (hv - st[0]) * st[1];
+      }
+      float dn = 0.f;
+#pragma unroll
+      for (int o = 0; o < OM; ++o)
+        if (o < p.O) {
+          const float go = gr[i * p.O + o];
+          dn = fmaf(go, w[o], dn);
+          T[o] = fmaf(go, hv, T[o]);
+        }
+      if (NORM) dn = st[1] * (gn * dn - st[2] - hv * st[3]);
+      z[i] = dn * u[i] * d;
+      u[i] = dn * av;
+    }
+    *(f32x4*)(Zt + n * Bp + b) = z;
+    if (GATED) *(f32x4*)(Ut + n * Bp + b) = u;
+  }
+#pragma unroll
+  for (int o = 0; o < OM; ++o) T[o] = group_sum_to_last(T[o], LG);
+  if (l != LG - 1) return;
+  const float sn = NORM ? p.shift[n] : 0.f;
+  const float rate = out.lrm ? out.lrm[m] : out.lr;
+  float dg = 0.f, ds = 0.f;
+#pragma unroll
+  for (int o = 0; o < OM; ++o)
+    if (o < p.O) {
+      float dw = T[o];
+      if (NORM) {
+        const float s = Gs[(int64_t)m * p.O + o];
+        dg = fmaf(w[o], T[o], dg);
+        ds = fmaf(w[o], s, ds);
+        dw = fmaf(gn, T[o], sn * s);
+      }
+      if (out.dW2) out.dW2[(int64_t)o * p.N + n] = dw;
+      else p.W2[(int64_t)o * p.ldw + n] = w[o] - rate * dw;
+    }
+  if (NORM) {
+    if (out.dW2) {
+      out.dgain[n] = dg;
+      out.dshift[n] = ds;
+    } else {
+      p.gain[n] = gn - rate * dg;
+      p.shift[n] = sn - rate * ds;
+    }
+  }
+}
+
+__global__ __launch_bounds__(kBlock) void k_blk_init(float* V1, int64_t N, int F, int F4, float bound,
+                                                     uint64_t key, float* gain, float* shift) {
+  const int64_t step = (int64_t)gridDim.x * kBlock, i0 = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+  if (V1)
+    for (int64_t i = i0; i < N * F; i += step) {
+      const int64_t n = i / F;
+      V1[n * F4 + (i - n * F)] = uniform_weight(key, 6, (uint64_t)i, bound);
+    }
+  if (gain)
+    for (int64_t i = i0; i < N; i += step) {
+      gain[i] = 1.f;
+      shift[i] = 0.f;
+    }
+}
+
+// lanes per unit: four samples each, at most a wave
+int lanes_per_unit(int32_t Bp) {
+  int lg = 4;
+  while (lg < 64 && 4 * lg < Bp) lg <<= 1;
+  return lg;
+}
+
+}  // namespace
+
+#define PMLP_BLK_OM(O, CALL) \
+  do {                       \
+    if ((O) <= 2) CALL(2);   \
+    else if ((O) <= 4) CALL(4); \
+    else if ((O) <= 8) CALL(8); \
+    else CALL(16);           \
+  } while (0)
+
+hipError_t launch_blk_fwd(const BlkPack& p, const float* Zt, const float* Ut, int32_t Bp,
+                          float* part, hipStream_t s) {
+  note_variant("k_blk_fwd", kArithNone);
+  const int LG = lanes_per_unit(Bp), nb = ceil_div_i(Bp, 4 * LG);
+  const int64_t waves = (int64_t)p.npieces * nb;
+  if (waves > (int64_t)0x3fffffff) return hipErrorInvalidValue;
+  const unsigned grid = (unsigned)ceil_div_i(waves, 4);
+#define PMLP_CALL(OM)                                                                        \
+  do {                                                                                       \
+    if (Ut && p.gain) k_blk_fwd<OM, true, true><<<grid, kBlock, 0, s>>>(p, Zt, Ut, Bp, LG, nb, part); \
+    else if (Ut) k_blk_fwd<OM, true, false><<<grid, kBlock, 0, s>>>(p, Zt, Ut, Bp, LG, nb, part);     \
+    else k_blk_fwd<OM, false, true><<<grid, kBlock, 0, s>>>(p, Zt, Ut, Bp, LG, nb, part);     \
+  } while (0)
+  PMLP_BLK_OM(p.O, PMLP_CALL);
+#undef PMLP_CALL
+  return hipGetLastError();
+}
+
+hipError_t launch_blk_out(const BlkPack& p, const float* part, int32_t Bp, int32_t B, float* out,
+                          int64_t sm, int64_t sb, hipStream_t s) {
+  note_variant("k_blk_out", kArithNone);
+  const int nblk = ceil_div_i(B, kOutSamples);
+  const int64_t waves = (int64_t)p.M * nblk;
+  if (waves > (int64_t)0x3fffffff) return hipErrorInvalidValue;
+  const unsigned grid = (unsigned)ceil_div_i(waves, 4);
+#define PMLP_CALL(OM)                                                                           \
+  do {                                                                                          \
+    if (p.gain) k_blk_out<OM, true><<<grid, kBlock, 0, s>>>(p, part, Bp, B, nblk, out, sm, sb);  \
+    else k_blk_out<OM, false><<<grid, kBlock, 0, s>>>(p, part, Bp, B, nblk, out, sm, sb);        \
+  } while (0)
+  PMLP_BLK_OM(p.O, PMLP_CALL);
+#undef PMLP_CALL
+  return hipGetLastError();
+}
+
+hipError_t launch_blk_loss(const BlkPack& p, const float* part, int32_t Bp, const BlkLoss& l,
+                           hipStream_t s) {
+  note_variant("k_blk_loss", kArithNone);
+  const int threads = Bp >= 1024 ? 1024 : (Bp + 63) & ~63;
+  const float scale = l.Y ? 1.f / ((float)l.B * (float)p.O) : 1.f / (float)l.B;
+#define PMLP_CALL(OM)                                                                  \
+  do {                                                                                 \
+    if (p.gain) k_blk_loss<OM, true><<<(unsigned)p.M, threads, 0, s>>>(p, part, Bp, l, scale);  \
+    else k_blk_loss<OM, false><<<(unsigned)p.M, threads, 0, s>>>(p, part, Bp, l, scale);        \
+  } while (0)
+  PMLP_BLK_OM(p.O, PMLP_CALL);
+#undef PMLP_CALL
+  return hipGetLastError();
+}
+
+hipError_t launch_blk_bwd(const BlkPack& p, float* Zt, float* Ut, int32_t Bp, const float* G,
+                          const float* R, const float* Gs, const BlkGrads& g, hipStream_t s) {
+  note_variant("k_blk_bwd", kArithNone);
+  const int LG = lanes_per_unit(Bp);
+  const int64_t waves = (p.N + 64 / LG - 1) / (64 / LG);
+  if (waves > (int64_t)0x7ffffff0) return hipErrorInvalidValue;
+  const unsigned grid = (unsigned)ceil_div_i(waves, 4);
+#define PMLP_CALL(OM)                                                                           \
+  do {                                                                                          \
+    if (Ut && p.gain)                                                                           \
+      k_blk_bwd<OM, true, true><<<grid, kBlock, 0, s>>>(p, Zt, Ut, Bp, LG, G, R, Gs, g);         \
+    else if (Ut)                                                                                \
+      k_blk_bwd<OM, true, false><<<grid, kBlock, 0, s>>>(p, Zt, Ut, Bp, LG, G, R, Gs, g);        \
+    else                                                                                        \
+      k_blk_bwd<OM, false, true><<<grid, kBlock, 0, s>>>(p, Zt, Ut, Bp, LG, G, R, Gs, g);        \
+  } while (0)
+  PMLP_BLK_OM(p.O, PMLP_CALL);
+#undef PMLP_CALL
+  return hipGetLastError();
+}
+
+hipError_t launch_blk_init(float* V1, int64_t N, int32_t F, int32_t F4, float bound, uint64_t key,
+                           float* gain, float* shift, hipStream_t s) {
+  const int64_t n = V1 ? N * F : N;
+  k_blk_init<<<grid_for(n), kBlock, 0, s>>>(V1, N, F, F4, bound, key, gain, shift);
+  return hipGetLastError();
+}
+
+}  // namespace pmlpk

@@ -1,0 +1,495 @@
+"""GPU parity of block packs (pmlp_create_block: gated hidden layer, layer norm
+over each model's hidden units) with the float64 reference, element by element
+within its error bounds, and what their entry points do besides."""
+import zlib
+
+import numpy as np
+import pytest
+
+import block_reference as ref
+import pmlp_workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+KINDS = {"gated": (True, False), "norm": (False, True), "both": (True, True)}
+SMOOTH = (0, 2, 3, 4, 6, 7, 8, 9, 12)   # activations without a kink
+GRADS = ("W1", "V1", "W2", "gain", "shift")
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a HIP device"
+    torch.cuda.set_device(0)
+    return torch
+
+
+@pytest.fixture(scope="module")
+def pm(torch):
+    import paper_2206_08369_amd as pm
+    pm.load_library()
+    return pm
+
+
+def dev(torch, a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def make(pm, hs, acts, p, F, O, kind, head="ce"):
+    gated, norm = KINDS[kind]
+    net = pm.BlockPackedMLP(F, O, hs, acts, seed=3, gated=gated, norm=norm, head=head)
+    net.set_params(**p)
+    return net
+
+
+def data(rng, F, O, B, head):
+    X = rng.standard_normal((B, F)).astype(np.float32)
+    y = (rng.standard_normal((B, O)).astype(np.float32) if head == "mse"
+         else rng.integers(0, O, B).astype(np.int32))
+    return X, y
+
+
+def within(got, want, what):
+    val, bound = want
+    d = np.abs(got.astype(np.float64) - val)
+    bad = ~(d <= bound + 1e-30)
+    assert not bad.any(), "%s: %d of %d outside, worst %.3g times its bound at %s" % (
+        what, bad.sum(), bad.size, (d / (bound + 1e-30)).max(),
+        np.unravel_index((d / (bound + 1e-30)).argmax(), d.shape))
+
+
+# (models, widest, F, O, B): one sample, one feature, odd sizes, every batch
+# class and past it, inputs at and around the kernels' limits, models of one unit,
+# wide models
+SHAPES = {
+    "one_of_everything": (1, 1, 1, 2, 1),
+    "two_units": (3, 2, 3, 2, 2),
+    "b1": (40, 30, 10, 2, 1),
+    "b1_f100": (30, 60, 100, 2, 1),
+    "b5_f37_o3": (25, 50, 37, 3, 5),
+    "b16_f32": (20, 40, 32, 2, 16),
+    "b17_f33_o4": (20, 45, 33, 4, 17),
+    "b32_o10": (12, 90, 32, 10, 32),
+    "b33_f64_o16": (10, 70, 64, 16, 33),
+    "b64_f95_o7": (10, 60, 95, 7, 64),
+    "b100_f96": (9, 80, 96, 2, 100),
+    "b128_f50": (20, 100, 50, 2, 128),
+    "b129_f97_o5": (9, 70, 97, 5, 129),
+    "b255_f100": (9, 100, 100, 2, 255),
+    "b256_f112_o3": (8, 90, 112, 3, 256),
+    "b200_f128": (7, 90, 128, 2, 200),
+    "b256_f129": (7, 64, 129, 2, 256),
+    "b257_f20": (9, 60, 20, 2, 257),
+    "b300_f100_o4": (7, 60, 100, 4, 300),
+    "b70_f300": (6, 50, 300, 2, 70),
+    "b600_f150_o9": (4, 40, 150, 9, 600),
+    "wide": (3, 1500, 20, 2, 40),
+    "wide_f100": (2, 1100, 100, 3, 130),
+    "many": (700, 5, 8, 2, 32),
+}
+
+
+def shape_problem(name, kind, head, wmin=1):
+    M, wmax, F, O, B = SHAPES[name]
+    rng = np.random.default_rng(zlib.crc32((name + kind + head).encode()))
+    hs = rng.integers(wmin, wmax + 1, M).astype(np.int32)
+    hs[-1] = wmax
+    acts = rng.choice(SMOOTH, M).astype(np.int32)
+    gated, norm = KINDS[kind]
+    return hs, acts, ref.random_params(rng, hs, F, O, gated, norm), F, O, *data(rng, F, O, B, head)
+
+
+@pytest.mark.parametrize("kind", sorted(KINDS))
+@pytest.mark.parametrize("name", sorted(SHAPES))
+def test_parity(pm, torch, name, kind):
+    head = "mse" if len(name) % 3 == 0 else "ce"
+    hs, acts, p, F, O, X, y = shape_problem(name, kind, head)
+    net = make(pm, hs, acts, p, F, O, kind, head)
+    want = ref.pack(hs, acts, p, X, y, head)
+    Xd, yd = dev(torch, X), dev(torch, y)
+    within(net.forward(Xd).cpu().numpy(), want["logits"], "logits")
+    got = dict(zip(net.param_names, net.gradients(Xd, yd)))
+    within(net.losses(), want["loss"], "loss")
+    assert set(got) == set(p)
+    for k, v in got.items():
+        within(v.cpu().numpy(), want[k], "d" + k)
+    # the same bits again
+    for k, v in zip(net.param_names, net.gradients(Xd, yd)):
+        assert torch.equal(v, got[k]), k
+    net.close()
+
+
+@pytest.mark.parametrize("kind", ["gated", "both"])
+def test_parity_generic_kernels(pm, torch, kind, monkeypatch):
+    monkeypatch.setenv("PMLP_GENERIC_KERNELS", "1")
+    hs, acts, p, F, O, X, y = shape_problem("b128_f50", kind, "ce")
+    net = make(pm, hs, acts, p, F, O, kind)
+    want = ref.pack(hs, acts, p, X, y)
+    within(net.forward(dev(torch, X)).cpu().numpy(), want["logits"], "logits")
+    for k, v in zip(net.param_names, net.gradients(dev(torch, X), dev(torch, y))):
+        within(v.cpu().numpy(), want[k], "d" + k)
+    net.close()
+
+
+@pytest.mark.parametrize("kind", sorted(KINDS))
+@pytest.mark.parametrize("B", [3, 40, 130, 300])
+def test_kinked_activations(pm, torch, kind, B):
+    """ReLU, LeakyReLU, SELU and Hardshrink where every pre-activation is an odd
+    multiple of 1/16 (exact in float32, off the kinks at 0 and the jump at 1/2)."""
+    rng = np.random.default_rng(B)
+    F, O, M = 6, 3, 16
+    hs = rng.integers(1, 40, M).astype(np.int32)
+    acts = np.resize([1, 5, 10, 11], M).astype(np.int32)
+    gated, norm = KINDS[kind]
+    p = ref.random_params(rng, hs, F, O, gated, norm)
+    N = int(hs.sum())
+    p["W1"] = (rng.integers(-4, 5, (N, F)) / 8).astype(np.float32)
+    p["W1"][:, 0] = (2 * rng.integers(-4, 4, N) + 1) / 16
+    X = rng.integers(-3, 4, (B, F)).astype(np.float32)
+    X[:, 0] = 2 * rng.integers(-2, 2, B) + 1
+    y = rng.integers(0, O, B).astype(np.int32)
+    net = make(pm, hs, acts, p, F, O, kind)
+    want = ref.pack(hs, acts, p, X, y)
+    within(net.forward(dev(torch, X)).cpu().numpy(), want["logits"], "logits")
+    for k, v in zip(net.param_names, net.gradients(dev(torch, X), dev(torch, y))):
+        within(v.cpu().numpy(), want[k], "d" + k)
+    net.close()
+
+
+@pytest.mark.parametrize("B", [1, 30, 130, 256, 400])
+def test_gradients_against_differences_of_losses(pm, torch, B):
+    """Central differences of the float64 reference's loss along the GPU's own
+    gradient direction."""
+    hs, acts, p, F, O, X, y = shape_problem("b128_f50", "both", "ce", wmin=4)
+    rng = np.random.default_rng(B)
+    X, y = data(rng, F, O, B, "ce")
+    net = make(pm, hs, acts, p, F, O, "both")
+    got = dict(zip(net.param_names, [v.cpu().numpy().astype(np.float64)
+                                     for v in net.gradients(dev(torch, X), dev(torch, y))]))
+    net.close()
+    norm2 = sum((v * v).sum() for v in got.values())
+    step = 1e-4 / np.sqrt(norm2)
+    f = []
+    for s in (step, -step):
+        q = {k: v.astype(np.float64) + s * got[k] for k, v in p.items()}
+        f.append(ref.pack(hs, acts, q, X, y)["loss"][0].sum())
+    # truncation: 1e-8 of the third derivative along a unit direction over the norm
+    assert abs((f[0] - f[1]) / (2 * step) / norm2 - 1) < 1e-4
+
+
+def test_norm_of_one_unit(pm, torch):
+    """A normalised model of one unit is a constant: its input weights have an
+    exactly zero gradient, whatever its hidden value."""
+    hs, acts = np.ones(20, np.int32), np.resize(SMOOTH, 20).astype(np.int32)
+    rng = np.random.default_rng(0)
+    p = ref.random_params(rng, hs, 9, 3, True, True)
+    X, y = data(rng, 9, 3, 77, "ce")
+    net = make(pm, hs, acts, p, 9, 3, "both")
+    dW1, dV1, dW2, dg, ds = net.gradients(dev(torch, X), dev(torch, y))
+    assert not dW1.any() and not dV1.any() and not dg.any()
+    L = net.forward(dev(torch, X)).cpu().numpy()
+    assert np.allclose(L, (p["W2"] * p["shift"]).T[None], rtol=1e-6, atol=0)
+    net.close()
+
+
+def test_initial_values(pm, torch):
+    hs = np.array([3, 1, 200, 17], np.int32)
+    F, O = 13, 3
+    plain = pm.PackedMLP(F, O, hs, [0, 1, 2, 3], seed=11)
+    net = pm.BlockPackedMLP(F, O, hs, [0, 1, 2, 3], seed=11, gated=True, norm=True)
+    W1, W2 = plain.get_params()
+    a, v, b, g, s = net.get_params()
+    assert np.array_equal(a, W1) and np.array_equal(b, W2)
+    assert np.all(g == 1) and not s.any()
+    mask = (1 << 64) - 1
+
+    def sm(x):
+        z = (x + 0x9E3779B97F4A7C15) & mask
+        z = ((z ^ (z >> 30)) * 0xBF58476D1CE4E5B9) & mask
+        z = ((z ^ (z >> 27)) * 0x94D049BB133111EB) & mask
+        return z ^ (z >> 31)
+
+    key, bound = sm(11), np.float32(1 / np.sqrt(F))
+    for n, f in ((0, 0), (0, 12), (5, 7), (220, 12)):
+        u = (sm(key ^ (6 << 60) ^ (n * F + f)) >> 40) * 2.0 ** -24
+        assert v[n, f] == np.float32(2 * u - 1) * bound
+    plain.close()
+    net.close()
+
+
+@pytest.mark.parametrize("kind", sorted(KINDS))
+@pytest.mark.parametrize("mode", ["lr", "rates", "mse"])
+@pytest.mark.parametrize("shape", ["b128_f50", "b300_f100_o4", "b33_f64_o16", "b1"])
+def test_train_step_is_sgd_on_the_gradients(pm, torch, kind, mode, shape):
+    head = "mse" if mode == "mse" else "ce"
+    hs, acts, p, F, O, X, y = shape_problem(shape, kind, head)
+    net = make(pm, hs, acts, p, F, O, kind, head)
+    Xd, yd = dev(torch, X), dev(torch, y)
+    grads = {k: v.cpu().numpy() for k, v in zip(net.param_names, net.gradients(Xd, yd))}
+    loss = net.losses()
+    rng = np.random.default_rng(1)
+    rates = (0.1 * rng.uniform(0.5, 1.5, len(hs))).astype(np.float32)
+    net.train_step(Xd, yd, dev(torch, rates) if mode == "rates" else 0.1)
+    assert np.array_equal(net.losses(), loss)
+    per_unit = np.repeat(rates if mode == "rates" else np.float32([0.1] * len(hs)), hs)
+    for k, w in zip(net.param_names, net.get_params()):
+        r = per_unit.reshape((1, -1) if k == "W2" else (-1,) + (1,) * (w.ndim - 1))
+        old, step = p[k].astype(np.float64), r.astype(np.float64) * grads[k]
+        # the rounding of the product and of the difference (or of one fma), and
+        # sums of the gradient in another order in the update's instance
+        tol = 2 * ref.U * (np.abs(old) + np.abs(step)) + 1e-5 * np.abs(step).max()
+        assert np.all(np.abs(w - (old - step)) <= tol), k
+    net.close()
+
+
+def test_an_epoch_of_training(pm, torch):
+    """The pool as it is used: an epoch of SGD over ragged batches, against the
+    reference trained the same way, then validation, prediction of one sample, and
+    the trained weights handed to another handle."""
+    rng = np.random.default_rng(5)
+    hs = rng.integers(4, 40, 30).astype(np.int32)
+    acts = rng.choice(SMOOTH, 30).astype(np.int32)
+    F, O, B, S = 12, 3, 48, 230
+    X, y = wl.make_dataset(F, O, S, seed=5)
+    p = ref.random_params(rng, hs, F, O, True, True)
+    net = make(pm, hs, acts, p, F, O, "both")
+    Xd, yd = dev(torch, X), dev(torch, y)
+    q = {k: v.astype(np.float64) for k, v in p.items()}
+    for s in range(0, S, B):
+        net.train_step(Xd[s:s + B], yd[s:s + B], 0.05)
+        g = ref.pack(hs, acts, q, X[s:s + B], y[s:s + B])
+        q = {k: v - np.float64(np.float32(0.05)) * g[k][0] for k, v in q.items()}
+    for k, w in zip(net.param_names, net.get_params()):
+        assert np.linalg.norm(w - q[k]) <= 1e-5 * np.linalg.norm(q[k]), k
+    assert net.nonfinite_count() == 0
+    w = dict(zip(net.param_names, net.get_params()))
+    want = ref.pack(hs, acts, w, X)["logits"]
+    L = net.forward(Xd)
+    within(L.cpu().numpy(), want, "validation")
+    within(net.forward(Xd[17:18].contiguous()).cpu().numpy(), (want[0][17:18], want[1][17:18]),
+           "one sample")
+    other = make(pm, hs, acts, w, F, O, "both")
+    assert torch.equal(other.forward(Xd), L)
+    net.close()
+    other.close()
+
+
+def test_forward_in_slices(pm, torch):
+    """A batch whose pre-activations exceed what a pass stores at once, next to the
+    same samples a few at a time."""
+    rng = np.random.default_rng(8)
+    hs = rng.integers(600, 1400, 60).astype(np.int32)
+    acts = rng.choice(SMOOTH, 60).astype(np.int32)
+    F, O, B = 130, 3, 4999
+    p = ref.random_params(rng, hs, F, O, True, True)
+    net = make(pm, hs, acts, p, F, O, "both")
+    Xd = dev(torch, rng.standard_normal((B, F)).astype(np.float32))
+    L = net.forward(Xd)
+    for s in (0, 2300, B - 70):
+        part = net.forward(Xd[s:s + 70].contiguous())
+        # sums of at most 1,400 and 130 terms in another order, through the norm of
+        # models whose hidden values spread
+        assert (part - L[s:s + 70]).abs().max() < 2e-5
+    net.close()
+
+
+@pytest.mark.parametrize("kind", sorted(KINDS))
+@pytest.mark.parametrize("shape", ["b33_f64_o16", "b255_f100", "b600_f150_o9"])
+def test_outputs_alone_are_written(pm, torch, kind, shape):
+    """Rows behind the batch and values around the gradients stay as they were."""
+    hs, acts, p, F, O, X, y = shape_problem(shape, kind, "ce")
+    net = make(pm, hs, acts, p, F, O, kind)
+    Xd, yd = dev(torch, X), dev(torch, y)
+    n = len(X) * net.M * O
+    buf = torch.full((n + 4096,), 7.5, device="cuda")
+    net.forward(Xd, out=buf[2048:2048 + n].view(len(X), net.M, O))
+    assert torch.all(buf[:2048] == 7.5) and torch.all(buf[2048 + n:] == 7.5)
+    assert not torch.any(buf[2048:2048 + n] == 7.5)
+    sizes = {"W1": net.N * F, "V1": net.N * F, "W2": O * net.N, "gain": net.N, "shift": net.N}
+    bufs = {k: torch.full((v + 128,), 7.5, device="cuda") for k, v in sizes.items()}
+    net._stream()
+    pm.pmlp_gradients_block(net.handle, Xd, yd, len(X),
+                            *[bufs[k][64:] if k in p else None for k in GRADS])
+    torch.cuda.synchronize()
+    for k, b in bufs.items():
+        edge = torch.cat([b[:64], b[64 + sizes[k]:]]) if k in p else b
+        assert torch.all(edge == 7.5), k
+    net.close()
+
+
+def test_logits_over_the_samples(pm, torch):
+    """The logits may lie over the samples they come from."""
+    hs, acts, p, F, O, X, _ = shape_problem("b128_f50", "both", "ce")
+    net = make(pm, hs, acts, p, F, O, "both")
+    want = net.forward(dev(torch, X))
+    buf = torch.zeros(max(want.numel(), X.size), device="cuda")
+    buf[:X.size] = dev(torch, X).flatten()
+    net._stream()
+    pm.pmlp_forward(net.handle, buf.data_ptr(), len(X), buf.data_ptr())
+    assert torch.equal(buf[:want.numel()].view_as(want), want)
+    net.close()
+
+
+@pytest.mark.parametrize("kind", sorted(KINDS))
+@pytest.mark.parametrize("shape", ["b100_f96", "b70_f300", "b17_f33_o4"])
+def test_what_is_not_finite_stays_where_it_is(pm, torch, kind, shape):
+    """A sample with NaN or infinite features changes no other sample's logits; a
+    model with such a weight changes no other model's logits and gradients, and is
+    counted."""
+    hs, acts, p, F, O, X, y = shape_problem(shape, kind, "ce")
+    acts[:] = 7
+    net = make(pm, hs, acts, p, F, O, kind)
+    Xd, yd = dev(torch, X), dev(torch, y)
+    L = net.forward(Xd)
+    ref_grads = net.gradients(Xd, yd)
+    for v in (float("nan"), float("inf"), -3e38):
+        Xb = Xd.clone()
+        Xb[3, F // 2] = v
+        Lb = net.forward(Xb)
+        keep = torch.arange(len(X), device="cuda") != 3
+        assert torch.equal(Lb[keep], L[keep])
+        if v != v:
+            assert torch.isnan(Lb[3]).all()
+    off = np.concatenate([[0], np.cumsum(hs)])
+    m = 1
+    bad = {k: v.copy() for k, v in p.items()}
+    bad["W1"][off[m], 0] = np.nan
+    net.set_params(W1=bad["W1"])
+    net.nonfinite_count()
+    keep = torch.arange(len(hs), device="cuda") != m
+    assert torch.equal(net.forward(Xd)[:, keep], L[:, keep])
+    rows = torch.ones(net.N, dtype=torch.bool, device="cuda")
+    rows[off[m]:off[m + 1]] = False
+    for k, g, w in zip(net.param_names, net.gradients(Xd, yd), ref_grads):
+        assert torch.equal(g[:, rows] if k == "W2" else g[rows],
+                           w[:, rows] if k == "W2" else w[rows]), k
+    assert net.nonfinite_count() == 1
+    net.close()
+
+
+def test_labels_out_of_range_are_reported(pm, torch):
+    hs, acts, p, F, O, X, y = shape_problem("b33_f64_o16", "both", "ce")
+    net = make(pm, hs, acts, p, F, O, "both")
+    y[4] = O
+    net.gradients(dev(torch, X), dev(torch, y))
+    with pytest.raises(pm.PmlpError) as e:
+        net.losses()
+    assert e.value.code == pm.PMLP_EINVAL and "label" in str(e.value)
+    y[4] = 0
+    rates = np.full(len(hs), 0.1, np.float32)
+    rates[2] = np.inf
+    net.train_step(dev(torch, X), dev(torch, y), dev(torch, rates))
+    with pytest.raises(pm.PmlpError) as e:
+        net.losses()
+    assert "rate" in str(e.value)
+    net.close()
+
+
+@pytest.mark.parametrize("shape", ["b64_f95_o7", "b300_f100_o4"])
+def test_graph_replays(pm, torch, shape):
+    """A captured step and forward pass, replayed with eager work on the same handle
+    in between (a larger batch, which replaces the workspace, among it)."""
+    hs, acts, p, F, O, X, y = shape_problem(shape, "both", "ce")
+    net = make(pm, hs, acts, p, F, O, "both")
+    twin = make(pm, hs, acts, p, F, O, "both")
+    Xd, yd = dev(torch, X), dev(torch, y)
+    out = torch.zeros(len(X), net.M, O, device="cuda")
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        net.train_step(Xd, yd, 0.0)   # sizes the workspace, changes nothing
+        net.forward(Xd, out=out)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        net.train_step(Xd, yd, 0.05)
+        net.forward(Xd, out=out)
+    rng = np.random.default_rng(0)
+    for rep in range(4):
+        Xd.copy_(dev(torch, rng.standard_normal(X.shape).astype(np.float32)))
+        graph.replay()
+        torch.cuda.synchronize()
+        twin.train_step(Xd, yd, 0.05)
+        assert torch.equal(out, twin.forward(Xd))
+        assert np.array_equal(net.losses(), twin.losses())
+        big = dev(torch, rng.standard_normal((len(X) * (rep + 2), F)).astype(np.float32))
+        assert torch.equal(net.forward(big), twin.forward(big))
+    net._stream()
+    net.close()
+    twin.close()
+
+
+def test_capture_without_a_workspace_is_refused(pm, torch):
+    hs, acts, p, F, O, X, y = shape_problem("b300_f100_o4", "both", "ce")
+    net = make(pm, hs, acts, p, F, O, "both")
+    Xd, yd = dev(torch, X), dev(torch, y)
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        with pytest.raises(pm.PmlpError) as e:
+            net.train_step(Xd, yd, 0.1)
+        assert e.value.code == pm.PMLP_ESTATE and "capture" in str(e.value)
+    net.gradients(Xd, yd)
+    assert np.all(np.isfinite(net.losses()))
+    net.close()
+
+
+def test_on_another_stream(pm, torch):
+    """Calls run on the stream that is current when they are made."""
+    hs, acts, p, F, O, X, y = shape_problem("b128_f50", "both", "ce")
+    net = make(pm, hs, acts, p, F, O, "both")
+    Xd, yd = dev(torch, X), dev(torch, y)
+    want = [g.clone() for g in net.gradients(Xd, yd)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        late = torch.zeros_like(Xd)
+        for _ in range(50):
+            late.add_(Xd, alpha=0.02)
+        late.copy_(Xd)
+        got = net.gradients(late, yd)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    net._stream()
+    net.close()
+
+
+def test_calls_that_block_packs_do_not_provide(pm, torch):
+    hs, acts, p, F, O, X, y = shape_problem("b1", "gated", "ce")
+    net = make(pm, hs, acts, p, F, O, "gated")
+    plain = pm.PackedMLP(F, O, hs, acts)
+    Xd, yd, g = dev(torch, X), dev(torch, y), torch.zeros(net.N * max(F, O), device="cuda")
+    h = net.handle
+    for call in (lambda: pm.pmlp_gradients(h, Xd, yd, 1, g, g),
+                 lambda: pm.pmlp_hidden(h, Xd, 1, g, g),
+                 lambda: pm.pmlp_get_params(h),
+                 lambda: pm.pmlp_set_params(h, None, None),
+                 lambda: pm.pmlp_get_models(h, [0], hs),
+                 lambda: pm.pmlp_get_biases(h, net.N, net.M, O),
+                 lambda: pm.pmlp_set_feature_mask(h, np.ones((net.M, F))),
+                 lambda: pm.pmlp_train_step_noalloc(h, Xd, yd, 1, 0.1),
+                 lambda: pm.pmlp_train_step_mse(h, Xd, Xd, 1, 0.1),
+                 lambda: pm.pmlp_gradients_block_mse(h, Xd, Xd, 1, g, g, g, None, None),
+                 lambda: pm.pmlp_gradients_deep(h, Xd, yd, 1, g, g, g),
+                 lambda: pm.pmlp_set_precision(h, pm.PMLP_BF16_GEMM),
+                 lambda: pm.pmlp_set_precision(h, pm.PMLP_BF16_STORE),
+                 lambda: pm.pmlp_gradients_block(plain.handle, Xd, yd, 1, g, g, g, None, None),
+                 lambda: pm.pmlp_get_params_block(plain.handle, ("W1",))):
+        with pytest.raises(pm.PmlpError) as e:
+            call()
+        assert e.value.code == pm.PMLP_ESTATE
+    for call in (lambda: pm.pmlp_gradients_block(h, Xd, yd, 1, g, None, g, None, None),
+                 lambda: pm.pmlp_gradients_block(h, Xd, None, 1, g, g, g, None, None),
+                 lambda: pm.pmlp_gradients_block(h, None, yd, 1, g, g, g, None, None),
+                 lambda: pm.pmlp_gradients_block(h, Xd, yd, 0, g, g, g, None, None),
+                 lambda: pm.pmlp_forward(h, Xd, (1 << 20) + 1, g),
+                 lambda: net.set_params(gain=np.ones(net.N)),
+                 lambda: net.train_step(Xd, yd, float("nan"))):
+        with pytest.raises(pm.PmlpError) as e:
+            call()
+        assert e.value.code == pm.PMLP_EINVAL
+    with pytest.raises(ValueError):
+        net.set_params(V1=np.ones((net.N, F + 1)))
+    with pytest.raises(ValueError):
+        net.gradients(Xd.double(), yd)
+    net.close()
+    plain.close()

@@ -110,6 +110,10 @@ struct PmlpBlock {
   BlkPiece* d_pieces = nullptr;
   int32_t* d_poff = nullptr;  // [M+1]
   int32_t npieces = 0;
+  BlkTile* d_tiles = nullptr;
+  int32_t* d_toff = nullptr;  // [M+1]
+  int32_t ntiles = 0;
+  int slots[5] = {-1, -1, -1, -1, -1};  // of the fused forward's batch classes
   // Workspace.  A captured graph keeps the addresses it was captured with, so a
   // buffer that a larger batch replaces lives until the handle goes.
   unsigned char* ws = nullptr;
@@ -251,6 +255,8 @@ void release(pmlp* h) {
     dfree(k->shift);
     dfree(k->d_pieces);
     dfree(k->d_poff);
+    dfree(k->d_tiles);
+    dfree(k->d_toff);
     dfree(k->ws);
     for (unsigned char*& p : k->retired) dfree(p);
     delete k;
@@ -1327,6 +1333,19 @@ void block_pieces(const std::vector<int32_t>& hs, int64_t cap, std::vector<BlkPi
   poff.push_back((int32_t)pieces.size());
 }
 
+// Tiles of the fused kernels: 16 units of a model, the last of it fewer.
+void block_tiles(const std::vector<int32_t>& hs, std::vector<BlkTile>& tiles,
+                 std::vector<int32_t>& toff) {
+  int64_t n = 0;
+  for (size_t m = 0; m < hs.size(); ++m) {
+    toff.push_back((int32_t)tiles.size());
+    for (int32_t at = 0; at < hs[m]; at += 16)
+      tiles.push_back(BlkTile{(int32_t)(n + at), std::min(16, hs[m] - at), (int32_t)m, 0});
+    n += hs[m];
+  }
+  toff.push_back((int32_t)tiles.size());
+}
+
 BlkPack block_pack(const pmlp* h) {
   const PmlpBlock* k = h->block;
   BlkPack p{};
@@ -1468,7 +1487,72 @@ int block_weight_grad(pmlp* h, const float* dZt, const float* Xt, int32_t Bp, fl
   return run(h, KID_GEMM_BWD, [&] { return launch_gemm(g, dW ? EPI_GRAD : EPI_SGD, h->stream); });
 }
 
+// ---- the fused forward ---------------------------------------------------------
+
+constexpr int kBlkClasses = 5;
+constexpr int kBlkWaves[kBlkClasses] = {0, 1, 2, 4, 8};
+
+#define PMLP_BY_WAVES(c, call)  \
+  switch (kBlkWaves[c]) {       \
+    case 0: return call(0);     \
+    case 1: return call(1);     \
+    case 2: return call(2);     \
+    case 4: return call(4);     \
+    default: return call(8);    \
+  }
+
+int blk_fwd_slots(int c, const BlkPack& p) {
+#define PMLP_CALL(NW) blk_fwd_slots_##NW(p)
+  PMLP_BY_WAVES(c, PMLP_CALL)
+#undef PMLP_CALL
+}
+
+hipError_t launch_blk_fused_fwd(int c, const BlkPack& p, const BlkFwdArgs& a, hipStream_t s) {
+  note_variant("k_blk_fused_fwd", kArithX3);
+#define PMLP_CALL(NW) launch_blk_fused_fwd_##NW(p, a, s)
+  PMLP_BY_WAVES(c, PMLP_CALL)
+#undef PMLP_CALL
+}
+
+// How a batch runs through the fused forward: its class, batches of bs samples,
+// workgroups for each.  c < 0: it does not.
+struct BlkRun {
+  int c = -1;
+  int32_t bs = 0, nchunk = 0, wpc = 0;
+};
+
+BlkRun block_run(pmlp* h, int32_t B) {
+  PmlpBlock* k = h->block;
+  BlkRun best;
+  if (!h->lds_kernels) return best;
+  const BlkPack p = block_pack(h);
+  double least = 0;
+  for (int c = 0; c < kBlkClasses; ++c) {
+    const int nw = kBlkWaves[c];
+    const int32_t bs = nw ? 32 * nw : 16, nchunk = div_up(B, bs);
+    if (nchunk > 1 && nw < 2) continue;  // more samples than a small class takes
+    if (k->slots[c] < 0) k->slots[c] = blk_fwd_slots(c, p);
+    const int64_t slots = k->slots[c];
+    if (slots <= 0) continue;
+    const int64_t fit = std::max<int64_t>(1, slots / nchunk);
+    for (int64_t w = fit; w <= std::max<int64_t>(fit, 32); ++w) {
+      const int64_t wpc = std::min<int64_t>(w, k->ntiles);
+      const int64_t rounds = (nchunk * wpc + slots - 1) / slots;
+      const double cost =
+          (double)rounds * (div_up(k->ntiles, wpc) + 3) * (nw > 1 ? nw : 1) * 256.0 / (double)slots *
+          (nw > 1 ? 1 + 0.3 / nw : 1);
+      if (best.c < 0 || cost < least) {
+        least = cost;
+        best = BlkRun{c, bs, nchunk, (int32_t)wpc};
+      }
+    }
+    if (nchunk == 1) break;
+  }
+  return best;
+}
+
 constexpr size_t kBlockSlice = (size_t)1 << 30;  // bytes of Z that a forward pass stores at once
+constexpr size_t kRecordSlice = (size_t)256 << 20;  // bytes of records of the fused one
 
 // Forward pass of a block pack.  A forward pass that stores its pre-activations
 // takes its samples in slices of at most kBlockSlice bytes of them (or 256 samples).
@@ -1477,7 +1561,13 @@ int forward_block(pmlp* h, const float* X, int32_t B, float* out) {
   const BlkPack p = block_pack(h);
   const size_t rows = (size_t)h->Npad * (k->gated ? 2 : 1);
   int32_t slice = B;
-  if ((size_t)pad_batch(B) * rows * sizeof(float) > kBlockSlice) {
+  const BlkRun whole = block_run(h, B);
+  const bool fused = whole.c >= 0;
+  const size_t rec = (size_t)h->M * blk_planes(p) * sizeof(float);  // (about) per sample
+  if (fused) {
+    if (rec * B > kRecordSlice)
+      slice = (int32_t)std::min<size_t>(std::max<size_t>(kRecordSlice / rec / 256 * 256, 256), B);
+  } else if ((size_t)pad_batch(B) * rows * sizeof(float) > kBlockSlice) {
     const size_t fit = kBlockSlice / (rows * sizeof(float)) / 256 * 256;
     slice = (int32_t)std::min<size_t>(std::max<size_t>(fit, 256), (size_t)B);
   }
@@ -1488,15 +1578,34 @@ int forward_block(pmlp* h, const float* X, int32_t B, float* out) {
   const uintptr_t l0 = (uintptr_t)out, l1 = l0 + (size_t)nout * sizeof(float);
   const bool over = x0 < l1 && l0 < x1;
   const int32_t Bp = pad_batch(slice);
+  const BlkRun r0 = block_run(h, slice), r1 = block_run(h, B % slice ? B % slice : slice);
   Carver c;
-  const size_t oXp = c.take((size_t)Bp * h->F4), oXt = c.take((size_t)Bp * h->F4);
-  const size_t oZ = c.take(rows * Bp), oP = c.take((size_t)k->npieces * blk_planes(p) * Bp);
+  const size_t oXp = c.take(fused ? 0 : (size_t)Bp * h->F4),
+               oXt = c.take(fused ? 0 : (size_t)Bp * h->F4), oZ = c.take(fused ? 0 : rows * Bp);
+  auto records = [&](const BlkRun& r) {
+    return (size_t)(h->M + r.wpc) * blk_planes(p) * ((size_t)r.nchunk * r.bs);
+  };
+  const size_t oP = c.take(fused ? std::max(records(r0), records(r1))
+                                 : (size_t)k->npieces * blk_planes(p) * Bp);
   const size_t oL = over ? c.take((size_t)nout) : 0;
   if (int rc = ensure_block_ws(h, c.bytes)) return rc;
   float *Xp = (float*)(k->ws + oXp), *Xt = (float*)(k->ws + oXt), *Zt = (float*)(k->ws + oZ),
         *part = (float*)(k->ws + oP), *dst = over ? (float*)(k->ws + oL) : out;
   for (int32_t b0 = 0; b0 < B; b0 += slice) {
     const int32_t n = std::min(slice, B - b0), np = pad_batch(n);
+    if (fused) {
+      const BlkRun& r = n == slice ? r0 : r1;
+      const int32_t br = r.nchunk * r.bs;
+      const BlkFwdArgs f{X + (int64_t)b0 * h->F, n, h->F, k->d_tiles, k->ntiles, r.wpc, part, br};
+      if (int rc = run(h, KID_FWD_M3, [&] { return launch_blk_fused_fwd(r.c, p, f, h->stream); }))
+        return rc;
+      const BlkMap map{k->d_toff, k->ntiles, r.wpc};
+      if (int rc = run(h, KID_CE, [&] {
+            return launch_blk_out(p, map, part, br, n, dst + b0 * sb, h->O, sb, h->stream);
+          }))
+        return rc;
+      continue;
+    }
     if (int rc = run(h, KID_PACK_X, [&] {
           return launch_pack_x(X + (int64_t)b0 * h->F, n, h->F, np, h->F4, -1, Xp, Xt, nullptr, 0,
                                h->stream);
@@ -1508,7 +1617,7 @@ int forward_block(pmlp* h, const float* X, int32_t B, float* out) {
         }))
       return rc;
     if (int rc = run(h, KID_CE, [&] {
-          return launch_blk_out(p, part, np, n, dst + b0 * sb, h->O, sb, h->stream);
+          return launch_blk_out(p, BlkMap{}, part, np, n, dst + b0 * sb, h->O, sb, h->stream);
         }))
       return rc;
   }
@@ -1547,7 +1656,7 @@ int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_
                    [&] { return launch_blk_fwd(p, Zt, Ut, Bp, at(oP), h->stream); }))
     return rc;
   const BlkLoss l{y, Y, B, at(oG), at(oR), at(oS), h->loss, h->flag, d.dW1 ? nullptr : lrm};
-  if (int rc = run(h, KID_CE, [&] { return launch_blk_loss(p, at(oP), Bp, l, h->stream); }))
+  if (int rc = run(h, KID_CE, [&] { return launch_blk_loss(p, BlkMap{}, at(oP), Bp, Bp, l, h->stream); }))
     return rc;
   const BlkGrads g{d.dW2, d.dgain, d.dshift, lr, lrm};
   if (int rc = run(h, KID_M3_BWD, [&] {
@@ -2214,21 +2323,26 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
   k->gated = (flags & PMLP_GATED) != 0;
   k->norm = (flags & PMLP_NORM) != 0;
   std::vector<BlkPiece> pieces;
-  std::vector<int32_t> poff;
+  std::vector<BlkTile> tiles;
+  std::vector<int32_t> poff, toff;
   try {
     block_pieces(h->hs, tile_cap(h->N), pieces, poff);
+    block_tiles(h->hs, tiles, toff);
   } catch (const std::bad_alloc&) {
     pmlp_destroy(h);
     return fail(PMLP_ENOMEM, "host allocation failed");
   }
   k->npieces = (int32_t)pieces.size();
+  k->ntiles = (int32_t)tiles.size();
   const size_t half = (size_t)h->Npad * h->F4, units = (size_t)h->Npad * sizeof(float);
   float* W = nullptr;
   if ((k->gated && hipMalloc(&W, (2 * half + 64) * sizeof(float)) != hipSuccess) ||
       (k->norm && (hipMalloc(&k->gain, units) != hipSuccess ||
                    hipMalloc(&k->shift, units) != hipSuccess)) ||
       hipMalloc(&k->d_pieces, pieces.size() * sizeof(BlkPiece)) != hipSuccess ||
-      hipMalloc(&k->d_poff, poff.size() * sizeof(int32_t)) != hipSuccess) {
+      hipMalloc(&k->d_poff, poff.size() * sizeof(int32_t)) != hipSuccess ||
+      hipMalloc(&k->d_tiles, tiles.size() * sizeof(BlkTile)) != hipSuccess ||
+      hipMalloc(&k->d_toff, toff.size() * sizeof(int32_t)) != hipSuccess) {
     (void)hipGetLastError();
     dfree(W);
     pmlp_destroy(h);
@@ -2248,6 +2362,10 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
     PMLP_HIP(hipMemcpy(k->d_pieces, pieces.data(), pieces.size() * sizeof(BlkPiece),
                        hipMemcpyHostToDevice));
     PMLP_HIP(hipMemcpy(k->d_poff, poff.data(), poff.size() * sizeof(int32_t),
+                       hipMemcpyHostToDevice));
+    PMLP_HIP(hipMemcpy(k->d_tiles, tiles.data(), tiles.size() * sizeof(BlkTile),
+                       hipMemcpyHostToDevice));
+    PMLP_HIP(hipMemcpy(k->d_toff, toff.data(), toff.size() * sizeof(int32_t),
                        hipMemcpyHostToDevice));
     PMLP_HIP(launch_blk_init(k->V1, h->N, F, h->F4, (float)(1.0 / std::sqrt((double)F)),
                              splitmix64_host(seed), k->gain, k->shift, nullptr));

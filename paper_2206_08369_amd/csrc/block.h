@@ -36,6 +36,40 @@ struct BlkPack {
   int32_t npieces;
 };
 
+// The forward's tiles: up to 16 units of one model, in unit order.
+struct BlkTile {
+  int32_t n0, cnt, m, spare;
+};
+static_assert(sizeof(BlkTile) == 16, "BlkTile layout");
+
+// Where the sums of model m lie: in the stored path its pieces poff[m] ..
+// poff[m+1]-1; in the fused path (toff set), whose W workgroups per batch take runs
+// of the T tiles, one record per workgroup w that has tiles of it, at m + w (both
+// grow along the tiles, so no two records meet).
+struct BlkMap {
+  const int32_t* toff;  // [M+1] first tile of each model, or null
+  int32_t T, W;
+};
+
+struct BlkFwdArgs {
+  const float* X;  // [B][F]
+  int32_t B, F;
+  const BlkTile* tiles;
+  int32_t ntiles;
+  int32_t wpc;     // workgroups per batch of samples
+  float* part;     // records of blk_planes planes of Bp samples
+  int32_t Bp;      // whole batches of samples
+};
+#define PMLP_BLK_FWD_DECL(NW)             \
+  int blk_fwd_slots_##NW(const BlkPack& p); \
+  hipError_t launch_blk_fused_fwd_##NW(const BlkPack& p, const BlkFwdArgs& a, hipStream_t s);
+PMLP_BLK_FWD_DECL(0)
+PMLP_BLK_FWD_DECL(1)
+PMLP_BLK_FWD_DECL(2)
+PMLP_BLK_FWD_DECL(4)
+PMLP_BLK_FWD_DECL(8)
+#undef PMLP_BLK_FWD_DECL
+
 // Per piece and sample, planar: part[(piece * PQ + q) * Bp + b], q < O the sums
 // S_o over the piece's units, and with a norm the mean and the sum of squared
 // deviations of its hidden values after them.
@@ -46,8 +80,8 @@ hipError_t launch_blk_fwd(const BlkPack& p, const float* Zt, const float* Ut, in
                           float* part, hipStream_t s);
 
 // Logits out[b sb + m sm + o] of B samples from the pieces' sums.
-hipError_t launch_blk_out(const BlkPack& p, const float* part, int32_t Bp, int32_t B, float* out,
-                          int64_t sm, int64_t sb, hipStream_t s);
+hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, const float* part, int32_t Bp,
+                          int32_t B, float* out, int64_t sm, int64_t sb, hipStream_t s);
 
 // Losses and what the backward reads, from the pieces' sums:
 //   G [M][Bp][O]  dLoss/dlogits (0 past the batch)
@@ -66,8 +100,9 @@ struct BlkLoss {
   int32_t* flag;
   const float* lrm;
 };
-hipError_t launch_blk_loss(const BlkPack& p, const float* part, int32_t Bp, const BlkLoss& l,
-                           hipStream_t s);
+// Br: the records' sample stride, Bp: G's and R's.
+hipError_t launch_blk_loss(const BlkPack& p, const BlkMap& map, const float* part, int32_t Br,
+                           int32_t Bp, const BlkLoss& l, hipStream_t s);
 
 // Gradients of the output weights, gains and shifts (stored, or applied with
 // the rate lr or lrm[m] where dW2 is null).

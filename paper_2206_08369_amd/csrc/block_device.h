@@ -1,0 +1,45 @@
+// Device code shared by the fused kernels of block packs.
+#pragma once
+
+#include "block.h"
+#include "device_common.h"
+
+namespace pmlpk {
+
+// (n, mean, M2) of the union of two sets (Chan, Golub and LeVeque)
+__device__ __forceinline__ void merge_stats(float& n, float& mean, float& m2, float nb, float meanb,
+                                            float m2b) {
+  const float t = n + nb;
+  const float f = t > 0.f ? nb / t : 0.f;
+  const float d = meanb - mean;
+  mean = fmaf(d, f, mean);
+  m2 += m2b + d * d * n * f;
+  n = t;
+}
+
+#define PMLP_EVERY_ACT                                                                      \
+  PMLP_ACT(0) PMLP_ACT(1) PMLP_ACT(2) PMLP_ACT(3) PMLP_ACT(4) PMLP_ACT(5) PMLP_ACT(6)       \
+  PMLP_ACT(7) PMLP_ACT(8) PMLP_ACT(9) PMLP_ACT(10) PMLP_ACT(11) PMLP_ACT(12)
+
+// act_fwd with NaN for NaN also where its choice of a branch would drop it
+__device__ __forceinline__ float blk_act(int a, float z) {
+  if (a == 1) return z <= 0.f ? 0.f : z;
+  if (a == 11) return fabsf(z) <= 0.5f ? 0.f : z;
+  return act_fwd(a, z);
+}
+
+// Activation id a (uniform over the wave) of NV values.
+template <int NV>
+__device__ __forceinline__ void blk_acts(int a, const float (&z)[NV], float (&v)[NV]) {
+  switch (a) {
+#define PMLP_ACT(AA)                                                     \
+  case AA: {                                                             \
+    _Pragma("unroll") for (int j = 0; j < NV; ++j) v[j] = blk_act(AA, z[j]); \
+    break;                                                               \
+  }
+    PMLP_EVERY_ACT
+#undef PMLP_ACT
+  }
+}
+
+}  // namespace pmlpk

@@ -20,25 +20,13 @@
 // of squares minus a squared mean would lose the variance of a layer whose mean is
 // large.  S_o - mu C_o cancels no worse than H - mu does.
 
-#include "block.h"
-#include "device_common.h"
+#include "block_device.h"
 
 namespace pmlpk {
 
 namespace {
 
 constexpr int kFU = 4;  // units per lane group whose loads are in flight
-
-// (n, mean, M2) of the union of two sets
-__device__ __forceinline__ void merge_stats(float& n, float& mean, float& m2, float nb, float meanb,
-                                            float m2b) {
-  const float t = n + nb;
-  const float f = t > 0.f ? nb / t : 0.f;
-  const float d = meanb - mean;
-  mean = fmaf(d, f, mean);
-  m2 += m2b + d * d * n * f;
-  n = t;
-}
 
 // One wave per (piece, block of 4 LG samples).  Lane l takes four samples and
 // every NG-th unit (LG = lanes per unit, NG = 64 / LG), as k_m3_fwd.  Bound by
@@ -83,7 +71,7 @@ __global__ __launch_bounds__(kBlock) void k_blk_fwd(BlkPack p, const float* __re
       const float rc = NORM ? 1.f / cnt : 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float h = act_fwd(a, z[u][i]);
+        float h = blk_act(a, z[u][i]);
         if (GATED) h *= v[u][i];
         if (NORM) {
           const float d = h - mean[i];
@@ -151,21 +139,40 @@ __device__ __forceinline__ void norm_consts(const BlkPack& p, int m, int lane, f
 // statistics (mu, r), else the logits.  r = 0 for a model of one unit, whose norm
 // is constant, so that its gradient is exactly zero.
 template <int OM, bool NORM>
-__device__ __forceinline__ void merge_pieces(const BlkPack& p, const float* __restrict__ part, int m,
+__device__ __forceinline__ void merge_pieces(const BlkPack& p, const BlkMap& map,
+                                             const float* __restrict__ part, int m,
                                              int Bp, int b, const float (&C)[OM], float (&P)[OM],
                                              float* mu, float* r) {
   float n = 0.f, mean = 0.f, m2 = 0.f;
 #pragma unroll
   for (int o = 0; o < OM; ++o) P[o] = 0.f;
-  const int k1 = p.poff[m + 1];
-  for (int k = p.poff[m]; k < k1; ++k) {
+  int k0, k1, tf = 0;
+  if (map.toff) {
+    tf = map.toff[m];
+    k0 = m + (int)(((int64_t)(tf + 1) * map.W - 1) / map.T);
+    k1 = m + (int)(((int64_t)map.toff[m + 1] * map.W - 1) / map.T) + 1;
+  } else {
+    k0 = p.poff[m];
+    k1 = p.poff[m + 1];
+  }
+  for (int k = k0; k < k1; ++k) {
     const float* src = part + (int64_t)k * (p.O + (NORM ? 2 : 0)) * Bp + b;
 #pragma unroll
     for (int o = 0; o < OM; ++o)
       if (o < p.O) P[o] += src[(int64_t)o * Bp];
-    if (NORM)
-      merge_stats(n, mean, m2, (float)p.pieces[k].len, src[(int64_t)p.O * Bp],
+    if (NORM) {
+      int units;
+      if (map.toff) {  // of the tiles of m in workgroup k - m
+        const int a = (int)((int64_t)(k - m) * map.T / map.W) - tf;
+        const int e = (int)((int64_t)(k - m + 1) * map.T / map.W) - tf;
+        const int h = (int)(p.seg_off[m + 1] - p.seg_off[m]);
+        units = min(h, 16 * e) - max(0, 16 * a);
+      } else {
+        units = p.pieces[k].len;
+      }
+      merge_stats(n, mean, m2, (float)units, src[(int64_t)p.O * Bp],
                   src[(int64_t)(p.O + 1) * Bp]);
+    }
   }
   if (NORM) {
     const float rr = n > 1.f ? 1.f / sqrtf(m2 / n + kNormEps) : 0.f;
@@ -179,7 +186,7 @@ __device__ __forceinline__ void merge_pieces(const BlkPack& p, const float* __re
 constexpr int kOutSamples = 1024;  // samples of a model per wave, at most
 
 template <int OM, bool NORM>
-__global__ __launch_bounds__(kBlock) void k_blk_out(BlkPack p, const float* __restrict__ part,
+__global__ __launch_bounds__(kBlock) void k_blk_out(BlkPack p, BlkMap map, const float* __restrict__ part,
                                                     int Bp, int B, int nblk, float* __restrict__ out,
                                                     int64_t sm, int64_t sb) {
   const int lane = threadIdx.x & 63;
@@ -191,7 +198,7 @@ __global__ __launch_bounds__(kBlock) void k_blk_out(BlkPack p, const float* __re
   if (NORM) norm_consts<OM>(p, m, lane, C, D);
   for (int b = b0 + lane; b < B && b < b0 + kOutSamples; b += 64) {
     float P[OM], mu, r;
-    merge_pieces<OM, NORM>(p, part, m, Bp, b, C, P, &mu, &r);
+    merge_pieces<OM, NORM>(p, map, part, m, Bp, b, C, P, &mu, &r);
 #pragma unroll
     for (int o = 0; o < OM; ++o)
       if (o < p.O) out[(int64_t)b * sb + (int64_t)m * sm + o] = NORM ? P[o] + D[o] : P[o];
@@ -200,7 +207,8 @@ __global__ __launch_bounds__(kBlock) void k_blk_out(BlkPack p, const float* __re
 
 // One workgroup per model, its threads over the samples.
 template <int OM, bool NORM>
-__global__ __launch_bounds__(1024) void k_blk_loss(BlkPack p, const float* __restrict__ part, int Bp,
+__global__ __launch_bounds__(1024) void k_blk_loss(BlkPack p, BlkMap map,
+                                                   const float* __restrict__ part, int Br, int Bp,
                                                    BlkLoss l, float scale) {
   __shared__ float red[16][OM + 1];
   const int m = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -215,7 +223,7 @@ __global__ __launch_bounds__(1024) void k_blk_loss(BlkPack p, const float* __res
   for (int b = tid; b < Bp; b += blockDim.x) {
     float G[OM], P[OM], mu = 0.f, r = 0.f, a1 = 0.f, a2 = 0.f;
     if (b < B) {
-      merge_pieces<OM, NORM>(p, part, m, Bp, b, C, P, &mu, &r);
+      merge_pieces<OM, NORM>(p, map, part, m, Br, b, C, P, &mu, &r);
       float L[OM];
 #pragma unroll
       for (int o = 0; o < OM; ++o) L[o] = NORM ? P[o] + D[o] : P[o];
@@ -419,8 +427,8 @@ hipError_t launch_blk_fwd(const BlkPack& p, const float* Zt, const float* Ut, in
   return hipGetLastError();
 }
 
-hipError_t launch_blk_out(const BlkPack& p, const float* part, int32_t Bp, int32_t B, float* out,
-                          int64_t sm, int64_t sb, hipStream_t s) {
+hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, const float* part, int32_t Bp,
+                          int32_t B, float* out, int64_t sm, int64_t sb, hipStream_t s) {
   note_variant("k_blk_out", kArithNone);
   const int nblk = ceil_div_i(B, kOutSamples);
   const int64_t waves = (int64_t)p.M * nblk;
@@ -428,23 +436,23 @@ hipError_t launch_blk_out(const BlkPack& p, const float* part, int32_t Bp, int32
   const unsigned grid = (unsigned)ceil_div_i(waves, 4);
 #define PMLP_CALL(OM)                                                                           \
   do {                                                                                          \
-    if (p.gain) k_blk_out<OM, true><<<grid, kBlock, 0, s>>>(p, part, Bp, B, nblk, out, sm, sb);  \
-    else k_blk_out<OM, false><<<grid, kBlock, 0, s>>>(p, part, Bp, B, nblk, out, sm, sb);        \
+    if (p.gain) k_blk_out<OM, true><<<grid, kBlock, 0, s>>>(p, map, part, Bp, B, nblk, out, sm, sb);  \
+    else k_blk_out<OM, false><<<grid, kBlock, 0, s>>>(p, map, part, Bp, B, nblk, out, sm, sb);        \
   } while (0)
   PMLP_BLK_OM(p.O, PMLP_CALL);
 #undef PMLP_CALL
   return hipGetLastError();
 }
 
-hipError_t launch_blk_loss(const BlkPack& p, const float* part, int32_t Bp, const BlkLoss& l,
-                           hipStream_t s) {
+hipError_t launch_blk_loss(const BlkPack& p, const BlkMap& map, const float* part, int32_t Br,
+                           int32_t Bp, const BlkLoss& l, hipStream_t s) {
   note_variant("k_blk_loss", kArithNone);
   const int threads = Bp >= 1024 ? 1024 : (Bp + 63) & ~63;
   const float scale = l.Y ? 1.f / ((float)l.B * (float)p.O) : 1.f / (float)l.B;
 #define PMLP_CALL(OM)                                                                  \
   do {                                                                                 \
-    if (p.gain) k_blk_loss<OM, true><<<(unsigned)p.M, threads, 0, s>>>(p, part, Bp, l, scale);  \
-    else k_blk_loss<OM, false><<<(unsigned)p.M, threads, 0, s>>>(p, part, Bp, l, scale);        \
+    if (p.gain) k_blk_loss<OM, true><<<(unsigned)p.M, threads, 0, s>>>(p, map, part, Br, Bp, l, scale);  \
+    else k_blk_loss<OM, false><<<(unsigned)p.M, threads, 0, s>>>(p, map, part, Br, Bp, l, scale);        \
   } while (0)
   PMLP_BLK_OM(p.O, PMLP_CALL);
 #undef PMLP_CALL

@@ -1514,6 +1514,16 @@ hipError_t launch_blk_fused_fwd(int c, const BlkPack& p, const BlkFwdArgs& a, hi
 #undef PMLP_CALL
 }
 
+hipError_t launch_blk_fused_bwd(const BlkPack& p, const BlkBwdArgs& a, hipStream_t s) {
+  note_variant("k_blk_fused_bwd", kArithX3);
+  switch (blk_om(p.O)) {
+    case 2: return launch_blk_fused_bwd_2(p, a, s);
+    case 4: return launch_blk_fused_bwd_4(p, a, s);
+    case 8: return launch_blk_fused_bwd_8(p, a, s);
+    default: return launch_blk_fused_bwd_16(p, a, s);
+  }
+}
+
 // How a batch runs through the fused forward: its class, batches of bs samples,
 // workgroups for each.  c < 0: it does not.
 struct BlkRun {
@@ -1524,7 +1534,7 @@ struct BlkRun {
 BlkRun block_run(pmlp* h, int32_t B) {
   PmlpBlock* k = h->block;
   BlkRun best;
-  if (!h->lds_kernels) return best;
+  if (!h->lds_kernels || h->F4 > kBlkFusedCols) return best;
   const BlkPack p = block_pack(h);
   double least = 0;
   for (int c = 0; c < kBlkClasses; ++c) {
@@ -1639,12 +1649,33 @@ int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_
   if (int rc = use_device(h)) return rc;
   const size_t rows = (size_t)h->Npad * (k->gated ? 2 : 1), mb = (size_t)h->M * Bp;
   Carver c;
-  const size_t oXp = c.take((size_t)Bp * h->F4), oXt = c.take((size_t)Bp * h->F4);
-  const size_t oG = c.take(mb * h->O), oR = c.take(k->norm ? mb * 4 : 0),
+  const BlkRun r = block_run(h, B);
+  const bool fused = r.c >= 0;
+  const int32_t br = fused ? r.nchunk * r.bs : Bp;
+  const size_t oXp = c.take(fused ? 0 : (size_t)Bp * h->F4),
+               oXt = c.take(fused ? 0 : (size_t)Bp * h->F4);
+  const size_t oG = c.take(mb * blk_om(h->O)), oR = c.take(k->norm ? mb * 4 : 0),
                oS = c.take(k->norm ? (size_t)h->M * h->O : 0);
-  const size_t oP = c.take((size_t)k->npieces * blk_planes(p) * Bp), oZ = c.take(rows * Bp);
+  const size_t oP = c.take((size_t)(fused ? h->M + r.wpc : k->npieces) * blk_planes(p) * br),
+               oZ = c.take(fused ? 0 : rows * Bp);
   if (int rc = ensure_block_ws(h, c.bytes)) return rc;
   auto at = [&](size_t o) { return (float*)(k->ws + o); };
+  const BlkLoss l{y, Y, B, at(oG), at(oR), at(oS), h->loss, h->flag, d.dW1 ? nullptr : lrm};
+  const BlkGrads g{d.dW2, d.dgain, d.dshift, lr, lrm};
+  if (fused) {
+    const BlkFwdArgs f{X, B, h->F, k->d_tiles, k->ntiles, r.wpc, at(oP), br};
+    if (int rc = run(h, KID_FWD_M3, [&] { return launch_blk_fused_fwd(r.c, p, f, h->stream); }))
+      return rc;
+    const BlkMap map{k->d_toff, k->ntiles, r.wpc};
+    if (int rc = run(h, KID_CE,
+                     [&] { return launch_blk_loss(p, map, at(oP), br, Bp, l, h->stream); }))
+      return rc;
+    const BlkBwdArgs b{X, B, h->F, Bp, 0, at(oG), at(oR), at(oS), d.dW1, d.dV1, g};
+    if (int rc = run(h, KID_BWD_FUSED, [&] { return launch_blk_fused_bwd(p, b, h->stream); }))
+      return rc;
+    h->have_loss = true;
+    return PMLP_OK;
+  }
   float* const Zt = at(oZ);
   float* const Ut = k->gated ? Zt + h->Npad * Bp : nullptr;
   if (int rc = run(h, KID_PACK_X, [&] {
@@ -1655,10 +1686,8 @@ int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_
   if (int rc = run(h, KID_M3_FWD,
                    [&] { return launch_blk_fwd(p, Zt, Ut, Bp, at(oP), h->stream); }))
     return rc;
-  const BlkLoss l{y, Y, B, at(oG), at(oR), at(oS), h->loss, h->flag, d.dW1 ? nullptr : lrm};
   if (int rc = run(h, KID_CE, [&] { return launch_blk_loss(p, BlkMap{}, at(oP), Bp, Bp, l, h->stream); }))
     return rc;
-  const BlkGrads g{d.dW2, d.dgain, d.dshift, lr, lrm};
   if (int rc = run(h, KID_M3_BWD, [&] {
         return launch_blk_bwd(p, Zt, Ut, Bp, at(oG), at(oR), at(oS), g, h->stream);
       }))

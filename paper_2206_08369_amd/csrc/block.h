@@ -84,11 +84,13 @@ hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, const float* part
                           int32_t B, float* out, int64_t sm, int64_t sb, hipStream_t s);
 
 // Losses and what the backward reads, from the pieces' sums:
-//   G [M][Bp][O]  dLoss/dlogits (0 past the batch)
+//   G [M][Bp][blk_om]  dLoss/dlogits (0 past the batch and the outputs)
 //   R [M][Bp][4]  with a norm: mu, r, a1, a2 (see k_blk_bwd)
 //   Gs [M][O]     with a norm: sum_b G
 // y: labels int32 [B], or Y float [B][O] for the regression head; flags as
 // launch_ce.
+// (outputs padded to 2, 4, 8 or 16)
+inline int blk_om(int32_t O) { return O <= 2 ? 2 : O <= 4 ? 4 : O <= 8 ? 8 : 16; }
 struct BlkLoss {
   const int32_t* y;
   const float* Y;
@@ -116,6 +118,25 @@ struct BlkGrads {
 // dZ over Zt and dU over Ut, in place.
 hipError_t launch_blk_bwd(const BlkPack& p, float* Zt, float* Ut, int32_t Bp, const float* G,
                           const float* R, const float* Gs, const BlkGrads& g, hipStream_t s);
+
+// The whole backward, with Z computed again: dW1 and dV1 [N][F] stored, or applied
+// to W1 and V1 where dW1 is null; the rest as launch_blk_bwd.  Bp: a multiple of 16.
+struct BlkBwdArgs {
+  const float* X;  // [B][F]
+  int32_t B, F, Bp;
+  int32_t SC;      // (set by the launcher) samples a chunk
+  const float *G, *R, *Gs;
+  float *dW1, *dV1;
+  BlkGrads g;
+};
+constexpr int32_t kBlkFusedCols = 128;  // input columns (F4) of the fused kernels, at most
+#define PMLP_BLK_BWD_DECL(OM) \
+  hipError_t launch_blk_fused_bwd_##OM(const BlkPack& p, BlkBwdArgs a, hipStream_t s);
+PMLP_BLK_BWD_DECL(2)
+PMLP_BLK_BWD_DECL(4)
+PMLP_BLK_BWD_DECL(8)
+PMLP_BLK_BWD_DECL(16)
+#undef PMLP_BLK_BWD_DECL
 
 // V1 (tag 6, like W1), gain 1, shift 0 (either may be null).
 hipError_t launch_blk_init(float* V1, int64_t N, int32_t F, int32_t F4, float bound, uint64_t key,

@@ -42,4 +42,38 @@ __device__ __forceinline__ void blk_acts(int a, const float (&z)[NV], float (&v)
   }
 }
 
+// The gradients of unit n's output weights, gain and shift from T_o, stored or
+// applied.  w: its output weights.
+template <int OM, bool NORM>
+__device__ __forceinline__ void blk_unit_grads(const BlkPack& p, const BlkGrads& out,
+                                               const float* __restrict__ Gs, int64_t n, int m,
+                                               float gn, const float (&w)[OM],
+                                               const float (&T)[OM]) {
+  const float sn = NORM ? p.shift[n] : 0.f;
+  const float rate = out.lrm ? out.lrm[m] : out.lr;
+  float dg = 0.f, ds = 0.f;
+#pragma unroll
+  for (int o = 0; o < OM; ++o)
+    if (o < p.O) {
+      float dw = T[o];
+      if (NORM) {
+        const float s = Gs[(int64_t)m * p.O + o];
+        dg = fmaf(w[o], T[o], dg);
+        ds = fmaf(w[o], s, ds);
+        dw = fmaf(gn, T[o], sn * s);
+      }
+      if (out.dW2) out.dW2[(int64_t)o * p.N + n] = dw;
+      else p.W2[(int64_t)o * p.ldw + n] = w[o] - rate * dw;
+    }
+  if (NORM) {
+    if (out.dW2) {
+      out.dgain[n] = dg;
+      out.dshift[n] = ds;
+    } else {
+      p.gain[n] = gn - rate * dg;
+      p.shift[n] = sn - rate * ds;
+    }
+  }
+}
+
 }  // namespace pmlpk

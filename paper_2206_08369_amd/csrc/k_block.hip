@@ -230,7 +230,7 @@ __global__ __launch_bounds__(1024) void k_blk_loss(BlkPack p, BlkMap map,
       if (l.Y) {
 #pragma unroll
         for (int o = 0; o < OM; ++o) {
-          const float d = o < p.O ? L[o] - l.Y[(int64_t)b * p.O + o] : 0.f;
+          const float d = o < p.O ? L[o] - l.Y[(int64_t)b * p.O + (o < p.O ? o : 0)] : 0.f;
           loss = fmaf(d, d, loss);
           G[o] = 2.f * d * scale;
         }
@@ -263,10 +263,9 @@ __global__ __launch_bounds__(1024) void k_blk_loss(BlkPack p, BlkMap map,
 #pragma unroll
       for (int o = 0; o < OM; ++o) G[o] = 0.f;
     }
-    float* row = l.G + ((int64_t)m * Bp + b) * p.O;
+    float* row = l.G + ((int64_t)m * Bp + b) * OM;
 #pragma unroll
-    for (int o = 0; o < OM; ++o)
-      if (o < p.O) row[o] = G[o];
+    for (int o = 0; o < OM; o += 2) *(f32x2*)(row + o) = f32x2{G[o], G[o + 1]};
     if (NORM) *(f32x4*)(l.R + ((int64_t)m * Bp + b) * 4) = f32x4{mu, r, a1 * rh, a2 * rh};
   }
 #pragma unroll
@@ -321,7 +320,7 @@ __global__ __launch_bounds__(kBlock) void k_blk_bwd(BlkPack p, float* __restrict
   for (int b = 4 * l; b < Bp; b += 4 * LG) {
     f32x4 z = *(const f32x4*)(Zt + n * Bp + b), u = f32x4{1.f, 1.f, 1.f, 1.f};
     if (GATED) u = *(const f32x4*)(Ut + n * Bp + b);
-    const float* gr = G + ((int64_t)m * Bp + b) * p.O;
+    const float* gr = G + ((int64_t)m * Bp + b) * OM;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float d;
@@ -334,12 +333,11 @@ __global__ __launch_bounds__(kBlock) void k_blk_bwd(BlkPack p, float* __restrict
       }
       float dn = 0.f;
 #pragma unroll
-      for (int o = 0; o < OM; ++o)
-        if (o < p.O) {
-          const float go = gr[i * p.O + o];
-          dn = fmaf(go, w[o], dn);
-          T[o] = fmaf(go, hv, T[o]);
-        }
+      for (int o = 0; o < OM; ++o) {
+        const float go = gr[i * OM + o];
+        dn = fmaf(go, w[o], dn);
+        T[o] = fmaf(go, hv, T[o]);
+      }
       if (NORM) dn = st[1] * (gn * dn - st[2] - hv * st[3]);
       z[i] = dn * u[i] * d;
       u[i] = dn * av;
@@ -350,31 +348,7 @@ __global__ __launch_bounds__(kBlock) void k_blk_bwd(BlkPack p, float* __restrict
 #pragma unroll
   for (int o = 0; o < OM; ++o) T[o] = group_sum_to_last(T[o], LG);
   if (l != LG - 1) return;
-  const float sn = NORM ? p.shift[n] : 0.f;
-  const float rate = out.lrm ? out.lrm[m] : out.lr;
-  float dg = 0.f, ds = 0.f;
-#pragma unroll
-  for (int o = 0; o < OM; ++o)
-    if (o < p.O) {
-      float dw = T[o];
-      if (NORM) {
-        const float s = Gs[(int64_t)m * p.O + o];
-        dg = fmaf(w[o], T[o], dg);
-        ds = fmaf(w[o], s, ds);
-        dw = fmaf(gn, T[o], sn * s);
-      }
-      if (out.dW2) out.dW2[(int64_t)o * p.N + n] = dw;
-      else p.W2[(int64_t)o * p.ldw + n] = w[o] - rate * dw;
-    }
-  if (NORM) {
-    if (out.dW2) {
-      out.dgain[n] = dg;
-      out.dshift[n] = ds;
-    } else {
-      p.gain[n] = gn - rate * dg;
-      p.shift[n] = sn - rate * ds;
-    }
-  }
+  blk_unit_grads<OM, NORM>(p, out, Gs, n, m, gn, w, T);
 }
 
 __global__ __launch_bounds__(kBlock) void k_blk_init(float* V1, int64_t N, int F, int F4, float bound,

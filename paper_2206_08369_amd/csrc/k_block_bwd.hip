@@ -1,0 +1,367 @@
+// Block packs: the backward pass in one kernel, for inputs of up to 128 columns.
+// Compiled once per class of outputs (PMLP_BLK_OM: 2, 4, 8 or 16).
+//
+// A wave takes 16 consecutive hidden units (whatever models they belong to) and all
+// samples, so that its weights' gradients need no other wave; it holds the three
+// bf16 pieces of its units' W1 (and V1) rows and their gradients' accumulators in
+// registers.  The samples' pieces lie in LDS once, sample by sample (chunks of
+// them in turn, where they do not fit), and serve both products: read as rows they
+// are the operand of Z = X W1^T, which is computed again rather than stored by the
+// forward and read back, and read through the transposing LDS load the operand of
+// dW1 = dZ^T X.  A step takes 32 samples: after Z the lane (li, lk) holds unit li of
+// the samples 4 lk + r of both blocks of 16, forms dZ there, and those eight values
+// are, as they lie, a row of the second product's first operand (the sums over
+// samples run in that order in both of its operands).
+// The norm's gradient needs no sums over units (see k_block.hip).
+//
+// Rows of the pieces are 16 NF columns and eight of padding: 16 bytes times an odd
+// number, which spreads 16 rows over all banks.
+
+#include "block_device.h"
+
+#include <algorithm>
+
+#ifndef PMLP_BLK_OM
+#error "compile with -DPMLP_BLK_OM=2|4|8|16"
+#endif
+
+namespace pmlpk {
+
+namespace {
+
+constexpr int OM = PMLP_BLK_OM;
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+// row bytes of the pieces
+__host__ __device__ constexpr int row_bytes(int NF) { return 32 * NF + 16; }
+
+// LDS of SC samples: three planes, 16 bytes of zeros, and what a transposing load of
+// the last rows' columns may pass them by
+constexpr size_t lds_bytes(int NF, int SC) { return (size_t)3 * SC * row_bytes(NF) + 64; }
+
+// Values and slopes of activation id A (uniform, or each lane's own arow where the
+// lanes' units differ; then once per id).
+template <int NV>
+__device__ __forceinline__ void acts_bwd(bool one, int arow, const float (&z)[NV], float (&v)[NV],
+                                         float (&d)[NV]) {
+  int A = __builtin_amdgcn_readfirstlane(arow);
+  bool done = false;
+#pragma unroll 1
+  while (true) {
+    float x[NV], tv[NV], td[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {  // (opaque: nothing of an id's terms outside its case)
+      x[j] = z[j];
+      asm volatile("" : "+v"(x[j]));
+    }
+    switch (A) {
+#define PMLP_ACT(AA)                                                                        \
+  case AA: {                                                                                \
+    _Pragma("unroll") for (int j = 0; j < NV; ++j) tv[j] = act_fwd_bwd(AA, x[j], &td[j]); \
+    break;                                                                                  \
+  }
+      PMLP_EVERY_ACT
+#undef PMLP_ACT
+    }
+    const bool mine = one || (!done && arow == A);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      v[j] = mine ? tv[j] : v[j];
+      d[j] = mine ? td[j] : d[j];
+    }
+    if (one) return;
+    done |= mine;
+    const uint64_t left = __ballot(!done);
+    if (!left) return;
+    A = __builtin_amdgcn_readlane(arow, __builtin_ctzll(left));
+  }
+}
+
+template <int NF, bool GATED, bool NORM>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(NF <= 2 ? 3 : 2)))
+void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
+  constexpr int NC = (NF + 1) / 2, K = GATED ? 2 : 1, RB = row_bytes(NF);
+  extern __shared__ __align__(16) char lds[];
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
+  const int F = a.F, F4 = p.F4, SC = a.SC, plane = SC * RB;
+  const int ntiles = (int)((p.N + 15) >> 4);
+  const int rounds = (ntiles + gridDim.x * nw - 1) / (gridDim.x * nw);
+  const int zeros = 3 * plane;  // of 16 bytes
+  if (tid < 16) ((int*)(lds + zeros))[tid] = 0;
+
+  // the pieces of SC samples from b0 on (zero past the batch and the columns)
+  auto fill = [&](int b0) {
+    constexpr int QR = 4 * NF;  // quads of a row
+    for (int q = tid; q < SC * QR; q += blockDim.x) {
+      const int s = q / QR, k = 4 * (q - s * QR), b = b0 + s;
+      const float* xr = a.X + (int64_t)(b < a.B ? b : a.B - 1) * F;
+      f32x2 x[2];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v = xr[k + e < F ? k + e : F - 1];
+        x[e >> 1][e & 1] = k + e < F && b < a.B ? v : 0.f;
+      }
+      uint32_t p0[2], p1[2], p2[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        p0[e] = bf16_pair(x[e]);
+        const f32x2 r1 = x[e] - bf16_pair_value(p0[e]);
+        p1[e] = bf16_pair(r1);
+        p2[e] = bf16_pair(r1 - bf16_pair_value(p1[e]));
+      }
+      char* d = lds + s * RB + 2 * k;
+      *(uint2*)d = make_uint2(p0[0], p0[1]);
+      *(uint2*)(d + plane) = make_uint2(p1[0], p1[1]);
+      *(uint2*)(d + 2 * plane) = make_uint2(p2[0], p2[1]);
+    }
+  };
+  const int nchunk = (a.Bp + SC - 1) / SC;
+  if (nchunk == 1) {
+    fill(0);
+    __syncthreads();
+  }
+  // this lane's places in the pieces: a row of the first product, and of the second
+  const int zrow = li * RB + 16 * lk;
+  const int trow = (4 * lk + (li >> 2)) * RB + 8 * (li & 3);
+
+#pragma unroll 1
+  for (int round = 0; round < rounds; ++round) {
+    const int tile = (round * (int)gridDim.x + (int)blockIdx.x) * nw + wave;
+    const bool live = tile < ntiles;
+    const int64_t n0 = (int64_t)(live ? tile : ntiles - 1) * 16;
+    const int64_t n = n0 + li < p.N ? n0 + li : p.N - 1;
+    const int m = p.mid[n], act = p.actn[n];
+    const bool one_act = __all(act == __builtin_amdgcn_readfirstlane(act));
+    const float gn = NORM ? p.gain[n] : 1.f;
+    float w2[OM], T[OM];
+#pragma unroll
+    for (int o = 0; o < OM; ++o) {
+      w2[o] = o < p.O ? p.W2[(int64_t)o * p.ldw + n] : 0.f;
+      T[o] = 0.f;
+    }
+    bf16x8 wp[K][NC][3];
+#pragma unroll
+    for (int mt = 0; mt < K; ++mt) {
+      const float* row = (mt ? p.V1 : p.W1) + n * F4;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        f32x4 q[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int k = 32 * c + 8 * lk + 4 * e;
+          q[e] = *(const f32x4*)(row + (k < F4 ? k : F4 - 4));
+          if (k >= F4) q[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        split3(q[0], q[1], wp[mt][c][0], wp[mt][c][1], wp[mt][c][2]);
+      }
+    }
+    f32x4 acc[K][NF];
+#pragma unroll
+    for (int mt = 0; mt < K; ++mt)
+#pragma unroll
+      for (int j = 0; j < NF; ++j) acc[mt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+#pragma unroll 1
+    for (int b0 = 0; b0 < a.Bp; b0 += SC) {
+      if (nchunk > 1) {
+        __syncthreads();
+        fill(b0);
+        __syncthreads();
+      }
+      if (!live) continue;
+      const int steps = ((a.Bp - b0 < SC ? a.Bp - b0 : SC) + 31) >> 5;
+#pragma unroll 1
+      for (int st = 0; st < steps; ++st) {
+        const int s = 32 * st;
+        // ---- Z (and U) of 32 samples ------------------------------------------
+        f32x4 z[K][2];
+#pragma unroll
+        for (int mt = 0; mt < K; ++mt)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) z[mt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          bf16x8 x[2][3];
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 3; ++e) {
+              int at = e * plane + (s + 16 * i) * RB + zrow + 64 * c;
+              // (half of an odd last chunk is past the row)
+              if ((NF & 1) && c == NC - 1) at = lk < 2 ? at : zeros;
+              x[i][e] = *(const bf16x8*)(lds + at);
+            }
+#define PMLP_PIECE(E, Q)                                            \
+_Pragma("unroll") for (int mt = 0; mt < K; ++mt)                    \
+_Pragma("unroll") for (int i = 0; i < 2; ++i) z[mt][i] =            \
+    __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i][E], wp[mt][c][Q], z[mt][i], 0, 0, 0)
+          PMLP_PIECE(2, 0);
+          PMLP_PIECE(1, 1);
+          PMLP_PIECE(0, 2);
+          PMLP_PIECE(1, 0);
+          PMLP_PIECE(0, 1);
+          PMLP_PIECE(0, 0);
+#undef PMLP_PIECE
+        }
+        // ---- dZ (and dU) ------------------------------------------------------
+        float zv[8], av[8], dv[8];
+#pragma unroll
+        for (int v = 0; v < 8; ++v) zv[v] = z[0][v >> 2][v & 3];
+        acts_bwd<8>(one_act, act, zv, av, dv);
+        f32x4 dz[K][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int64_t b = (int64_t)m * a.Bp + b0 + s + 16 * i + 4 * lk;
+          const bool in = b0 + s + 16 * i < a.Bp;  // (Bp is a multiple of 16)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int v = 4 * i + r;
+            const float u = GATED ? z[K - 1][i][r] : 1.f;
+            float h = GATED ? av[v] * u : av[v];
+            f32x4 R;
+            if (NORM) {
+              R = in ? *(const f32x4*)(a.R + (b + r) * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+              h = (h - R[0]) * R[1];
+            }
+            float dn = 0.f;
+#pragma unroll
+            for (int o = 0; o < OM; o += 2) {
+              const f32x2 G = in ? *(const f32x2*)(a.G + (b + r) * OM + o) : f32x2{0.f, 0.f};
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                dn = fmaf(G[e], w2[o + e], dn);
+                T[o + e] = fmaf(G[e], h, T[o + e]);
+              }
+            }
+            if (NORM) dn = R[1] * (fmaf(gn, dn, -R[2]) - h * R[3]);
+            dz[0][i][r] = GATED ? dn * u * dv[v] : dn * dv[v];
+            if (GATED) dz[K - 1][i][r] = dn * av[v];
+          }
+        }
+        // ---- dW1 (and dV1) += dZ^T X ------------------------------------------
+        bf16x8 dp[K][3];
+#pragma unroll
+        for (int mt = 0; mt < K; ++mt)
+          split3(dz[mt][0], dz[mt][1], dp[mt][0], dp[mt][1], dp[mt][2]);
+#pragma unroll
+        for (int j = 0; j < NF; ++j) {
+          bf16x8 x[3];
+#pragma unroll
+          for (int e = 0; e < 3; ++e) {
+            const lds_char* at = (const lds_char*)lds + (e * plane + s * RB + trow + 32 * j);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4*)at);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4*)(at + 16 * RB));
+            x[e] = __builtin_bit_cast(
+                bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+          }
+#define PMLP_PIECE(Q, E)                                             \
+_Pragma("unroll") for (int mt = 0; mt < K; ++mt) acc[mt][j] =        \
+    __builtin_amdgcn_mfma_f32_16x16x32_bf16(dp[mt][Q], x[E], acc[mt][j], 0, 0, 0)
+          PMLP_PIECE(2, 0);
+          PMLP_PIECE(1, 1);
+          PMLP_PIECE(0, 2);
+          PMLP_PIECE(1, 0);
+          PMLP_PIECE(0, 1);
+          PMLP_PIECE(0, 0);
+#undef PMLP_PIECE
+        }
+      }
+    }
+    if (!live) continue;
+    // ---- the gradients, stored or applied ---------------------------------------
+#pragma unroll
+    for (int mt = 0; mt < K; ++mt) {
+      float* const dW = mt ? a.dV1 : a.dW1;
+      float* const W = const_cast<float*>(mt ? p.V1 : p.W1);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t nr = n0 + 4 * lk + r;
+        if (nr >= p.N) continue;
+        const float rate = a.g.lrm ? a.g.lrm[p.mid[nr]] : a.g.lr;
+#pragma unroll
+        for (int j = 0; j < NF; ++j) {
+          const int f = 16 * j + li;
+          if (f >= F) continue;
+          if (dW) dW[nr * F + f] = acc[mt][j][r];
+          else W[nr * F4 + f] -= rate * acc[mt][j][r];
+        }
+      }
+    }
+#pragma unroll
+    for (int o = 0; o < OM; ++o) {
+      T[o] += __shfl_xor(T[o], 16);
+      T[o] += __shfl_xor(T[o], 32);
+    }
+    if (lk == 0 && n0 + li < p.N) blk_unit_grads<OM, NORM>(p, a.g, a.Gs, n, m, gn, w2, T);
+  }
+}
+
+typedef void (*BlkBwdFn)(BlkPack, BlkBwdArgs);
+
+template <int NF>
+BlkBwdFn bwd_kind(bool gated, bool norm) {
+  if (gated && norm) return k_blk_fused_bwd<NF, true, true>;
+  if (gated) return k_blk_fused_bwd<NF, true, false>;
+  return k_blk_fused_bwd<NF, false, true>;
+}
+
+BlkBwdFn bwd_of(const BlkPack& p) {
+  const bool g = p.V1 != nullptr, n = p.gain != nullptr;
+  switch ((p.F4 + 15) / 16) {
+    case 1: return bwd_kind<1>(g, n);
+    case 2: return bwd_kind<2>(g, n);
+    case 3: return bwd_kind<3>(g, n);
+    case 4: return bwd_kind<4>(g, n);
+    case 5: return bwd_kind<5>(g, n);
+    case 6: return bwd_kind<6>(g, n);
+    case 7: return bwd_kind<7>(g, n);
+    case 8: return bwd_kind<8>(g, n);
+    default: return nullptr;
+  }
+}
+
+// Samples a chunk: all of them where they fit in LDS, else the most equal parts.
+int chunk_samples(int NF, int Bp, size_t lds_max) {
+  const int all = (Bp + 31) & ~31;
+  for (int parts = 1;; ++parts) {
+    const int SC = ((all + parts - 1) / parts + 31) & ~31;
+    if (lds_bytes(NF, SC) <= lds_max) return SC;
+    if (SC == 32) return 0;
+  }
+}
+
+}  // namespace
+
+#define PMLP_CAT_(a, b) a##b
+#define PMLP_CAT(a, b) PMLP_CAT_(a, b)
+
+hipError_t PMLP_CAT(launch_blk_fused_bwd_, PMLP_BLK_OM)(const BlkPack& p, BlkBwdArgs a,
+                                                        hipStream_t s) {
+  const BlkBwdFn fn = bwd_of(p);
+  const int NF = (p.F4 + 15) / 16;
+  int dev = 0, lmax = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess)
+    e = hipDeviceGetAttribute(&lmax, hipDeviceAttributeMaxSharedMemoryPerBlock, dev);
+  if (e != hipSuccess) return e;
+  a.SC = fn ? chunk_samples(NF, a.Bp, (size_t)lmax) : 0;
+  if (a.SC <= 0 || a.Bp < 16 || a.Bp % 16 || a.B < 1 || a.B > a.Bp || p.O > OM || p.N < 1)
+    return hipErrorInvalidValue;
+  const size_t lds = lds_bytes(NF, a.SC);
+  const int64_t tiles = (p.N + 15) / 16;
+  // eight waves share the samples' pieces where those leave room for one workgroup
+  // only, four where there is more
+  const int waves = 4 * lds > (size_t)lmax ? 8 : 4;
+  const int slots = resident_blocks((const void*)fn, 64 * waves, lds);
+  if (slots <= 0) return hipErrorInvalidValue;
+  const int64_t grid = std::min<int64_t>(slots, (tiles + waves - 1) / waves);
+  fn<<<(unsigned)grid, 64 * waves, lds, s>>>(p, a);
+  return hipGetLastError();
+}
+
+}  // namespace pmlpk

@@ -1334,13 +1334,16 @@ void block_pieces(const std::vector<int32_t>& hs, int64_t cap, std::vector<BlkPi
 }
 
 // Tiles of the fused kernels: 16 units of a model, the last of it fewer.
-void block_tiles(const std::vector<int32_t>& hs, std::vector<BlkTile>& tiles,
-                 std::vector<int32_t>& toff) {
+void block_tiles(const std::vector<int32_t>& hs, const std::vector<int32_t>& acts,
+                 std::vector<BlkTile>& tiles, std::vector<int32_t>& toff) {
   int64_t n = 0;
   for (size_t m = 0; m < hs.size(); ++m) {
     toff.push_back((int32_t)tiles.size());
     for (int32_t at = 0; at < hs[m]; at += 16)
-      tiles.push_back(BlkTile{(int32_t)(n + at), std::min(16, hs[m] - at), (int32_t)m, 0});
+      tiles.push_back(BlkTile{(int32_t)(n + at), (int32_t)m,
+                              std::min(16, hs[m] - at) + 256 * acts[m] +
+                                  (at + 16 >= hs[m] ? kBlkLast : 0),
+                              0});
     n += hs[m];
   }
   toff.push_back((int32_t)tiles.size());
@@ -1519,7 +1522,6 @@ hipError_t launch_blk_fused_bwd(const BlkPack& p, const BlkBwdArgs& a, hipStream
   switch (blk_om(p.O)) {
     case 2: return launch_blk_fused_bwd_2(p, a, s);
     case 4: return launch_blk_fused_bwd_4(p, a, s);
-    case 8: return launch_blk_fused_bwd_8(p, a, s);
     default: return launch_blk_fused_bwd_16(p, a, s);
   }
 }
@@ -1645,12 +1647,12 @@ int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_
                const float* lrm, const BlockGrads& d) {
   const PmlpBlock* k = h->block;
   const BlkPack p = block_pack(h);
-  const int32_t Bp = pad_batch(B);
   if (int rc = use_device(h)) return rc;
-  const size_t rows = (size_t)h->Npad * (k->gated ? 2 : 1), mb = (size_t)h->M * Bp;
-  Carver c;
   const BlkRun r = block_run(h, B);
   const bool fused = r.c >= 0;
+  const int32_t Bp = fused ? (B + 31) & ~31 : pad_batch(B);
+  const size_t rows = (size_t)h->Npad * (k->gated ? 2 : 1), mb = (size_t)h->M * Bp;
+  Carver c;
   const int32_t br = fused ? r.nchunk * r.bs : Bp;
   const size_t oXp = c.take(fused ? 0 : (size_t)Bp * h->F4),
                oXt = c.take(fused ? 0 : (size_t)Bp * h->F4);
@@ -2356,7 +2358,7 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
   std::vector<int32_t> poff, toff;
   try {
     block_pieces(h->hs, tile_cap(h->N), pieces, poff);
-    block_tiles(h->hs, tiles, toff);
+    block_tiles(h->hs, h->acts, tiles, toff);
   } catch (const std::bad_alloc&) {
     pmlp_destroy(h);
     return fail(PMLP_ENOMEM, "host allocation failed");

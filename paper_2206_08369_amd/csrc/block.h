@@ -38,8 +38,11 @@ struct BlkPack {
 
 // The forward's tiles: up to 16 units of one model, in unit order.
 struct BlkTile {
-  int32_t n0, cnt, m, spare;
+  int32_t n0, m;
+  int32_t info;  // units, + 256 activation id, + kBlkLast at a model's last tile
+  int32_t spare;
 };
+constexpr int kBlkLast = 65536;
 static_assert(sizeof(BlkTile) == 16, "BlkTile layout");
 
 // Where the sums of model m lie: in the stored path its pieces poff[m] ..
@@ -89,8 +92,8 @@ hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, const float* part
 //   Gs [M][O]     with a norm: sum_b G
 // y: labels int32 [B], or Y float [B][O] for the regression head; flags as
 // launch_ce.
-// (outputs padded to 2, 4, 8 or 16)
-inline int blk_om(int32_t O) { return O <= 2 ? 2 : O <= 4 ? 4 : O <= 8 ? 8 : 16; }
+// (outputs padded to 2, 4 or 16)
+inline int blk_om(int32_t O) { return O <= 2 ? 2 : O <= 4 ? 4 : 16; }
 struct BlkLoss {
   const int32_t* y;
   const float* Y;
@@ -120,7 +123,7 @@ hipError_t launch_blk_bwd(const BlkPack& p, float* Zt, float* Ut, int32_t Bp, co
                           const float* R, const float* Gs, const BlkGrads& g, hipStream_t s);
 
 // The whole backward, with Z computed again: dW1 and dV1 [N][F] stored, or applied
-// to W1 and V1 where dW1 is null; the rest as launch_blk_bwd.  Bp: a multiple of 16.
+// to W1 and V1 where dW1 is null; the rest as launch_blk_bwd.  Bp: a multiple of 32.
 struct BlkBwdArgs {
   const float* X;  // [B][F]
   int32_t B, F, Bp;
@@ -134,7 +137,6 @@ constexpr int32_t kBlkFusedCols = 128;  // input columns (F4) of the fused kerne
   hipError_t launch_blk_fused_bwd_##OM(const BlkPack& p, BlkBwdArgs a, hipStream_t s);
 PMLP_BLK_BWD_DECL(2)
 PMLP_BLK_BWD_DECL(4)
-PMLP_BLK_BWD_DECL(8)
 PMLP_BLK_BWD_DECL(16)
 #undef PMLP_BLK_BWD_DECL
 

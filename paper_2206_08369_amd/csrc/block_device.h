@@ -17,6 +17,23 @@ __device__ __forceinline__ void merge_stats(float& n, float& mean, float& m2, fl
   n = t;
 }
 
+// The same value, of which the compiler knows nothing: a load whose result passes
+// through here is made where it stands, not in a branch on whether it is wanted
+// (such branches made every load of a row wait for the one before).
+template <class T>
+__device__ __forceinline__ T opaque(T v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// A barrier for what lies in LDS.  (__syncthreads also waits for the loads from
+// memory that are on their way into registers for the next stage.)
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 #define PMLP_EVERY_ACT                                                                      \
   PMLP_ACT(0) PMLP_ACT(1) PMLP_ACT(2) PMLP_ACT(3) PMLP_ACT(4) PMLP_ACT(5) PMLP_ACT(6)       \
   PMLP_ACT(7) PMLP_ACT(8) PMLP_ACT(9) PMLP_ACT(10) PMLP_ACT(11) PMLP_ACT(12)

@@ -117,13 +117,18 @@ __device__ __forceinline__ void norm_consts(const BlkPack& p, int m, int lane, f
                                             float (&D)[OM]) {
 #pragma unroll
   for (int o = 0; o < OM; ++o) C[o] = D[o] = 0.f;
-  for (int64_t n = p.seg_off[m] + lane; n < p.seg_off[m + 1]; n += 64) {
-    const float gn = p.gain[n], sn = p.shift[n];
+  const int64_t e = p.seg_off[m + 1];
+  for (int64_t n0 = p.seg_off[m]; n0 < e; n0 += 256) {  // (four units' loads in flight)
 #pragma unroll
-    for (int o = 0; o < OM; ++o) {
-      const float w = o < p.O ? p.W2[(int64_t)o * p.ldw + n] : 0.f;
-      C[o] = fmaf(gn, w, C[o]);
-      D[o] = fmaf(sn, w, D[o]);
+    for (int u = 0; u < 4; ++u) {
+      const int64_t k = n0 + 64 * u + lane, n = k < e ? k : e - 1;
+      const float gn = k < e ? p.gain[n] : 0.f, sn = k < e ? p.shift[n] : 0.f;
+#pragma unroll
+      for (int o = 0; o < OM; ++o) {
+        const float w = p.W2[(int64_t)(o < p.O ? o : 0) * p.ldw + n];
+        C[o] = fmaf(gn, w, C[o]);
+        D[o] = fmaf(sn, w, D[o]);
+      }
     }
   }
 #pragma unroll
@@ -183,20 +188,19 @@ __device__ __forceinline__ void merge_pieces(const BlkPack& p, const BlkMap& map
   }
 }
 
-constexpr int kOutSamples = 1024;  // samples of a model per wave, at most
-
 template <int OM, bool NORM>
 __global__ __launch_bounds__(kBlock) void k_blk_out(BlkPack p, BlkMap map, const float* __restrict__ part,
-                                                    int Bp, int B, int nblk, float* __restrict__ out,
-                                                    int64_t sm, int64_t sb) {
+                                                    int Bp, int B, int per, int nblk,
+                                                    float* __restrict__ out, int64_t sm,
+                                                    int64_t sb) {
   const int lane = threadIdx.x & 63;
   const int64_t wv = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int m = (int)(wv / nblk);
   if (m >= p.M) return;
-  const int b0 = (int)(wv - (int64_t)m * nblk) * kOutSamples;
+  const int b0 = (int)(wv - (int64_t)m * nblk) * per;
   float C[OM], D[OM];
   if (NORM) norm_consts<OM>(p, m, lane, C, D);
-  for (int b = b0 + lane; b < B && b < b0 + kOutSamples; b += 64) {
+  for (int b = b0 + lane; b < B && b < b0 + per; b += 64) {
     float P[OM], mu, r;
     merge_pieces<OM, NORM>(p, map, part, m, Bp, b, C, P, &mu, &r);
 #pragma unroll
@@ -379,7 +383,6 @@ int lanes_per_unit(int32_t Bp) {
   do {                       \
     if ((O) <= 2) CALL(2);   \
     else if ((O) <= 4) CALL(4); \
-    else if ((O) <= 8) CALL(8); \
     else CALL(16);           \
   } while (0)
 
@@ -404,14 +407,16 @@ hipError_t launch_blk_fwd(const BlkPack& p, const float* Zt, const float* Ut, in
 hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, const float* part, int32_t Bp,
                           int32_t B, float* out, int64_t sm, int64_t sb, hipStream_t s) {
   note_variant("k_blk_out", kArithNone);
-  const int nblk = ceil_div_i(B, kOutSamples);
+  int per = 1024;  // samples of a model per wave: fewer where that leaves the device idle
+  while (per > 64 && (int64_t)p.M * ceil_div_i(B, per) < 8192) per >>= 1;
+  const int nblk = ceil_div_i(B, per);
   const int64_t waves = (int64_t)p.M * nblk;
   if (waves > (int64_t)0x3fffffff) return hipErrorInvalidValue;
   const unsigned grid = (unsigned)ceil_div_i(waves, 4);
 #define PMLP_CALL(OM)                                                                           \
   do {                                                                                          \
-    if (p.gain) k_blk_out<OM, true><<<grid, kBlock, 0, s>>>(p, map, part, Bp, B, nblk, out, sm, sb);  \
-    else k_blk_out<OM, false><<<grid, kBlock, 0, s>>>(p, map, part, Bp, B, nblk, out, sm, sb);        \
+    if (p.gain) k_blk_out<OM, true><<<grid, kBlock, 0, s>>>(p, map, part, Bp, B, per, nblk, out, sm, sb);  \
+    else k_blk_out<OM, false><<<grid, kBlock, 0, s>>>(p, map, part, Bp, B, per, nblk, out, sm, sb);        \
   } while (0)
   PMLP_BLK_OM(p.O, PMLP_CALL);
 #undef PMLP_CALL

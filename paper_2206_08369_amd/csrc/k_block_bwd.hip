@@ -1,5 +1,5 @@
 // Block packs: the backward pass in one kernel, for inputs of up to 128 columns.
-// Compiled once per class of outputs (PMLP_BLK_OM: 2, 4, 8 or 16).
+// Compiled once per class of outputs (PMLP_BLK_OM: 2, 4 or 16).
 //
 // A wave takes 16 consecutive hidden units (whatever models they belong to) and all
 // samples, so that its weights' gradients need no other wave; it holds the three
@@ -22,7 +22,7 @@
 #include <algorithm>
 
 #ifndef PMLP_BLK_OM
-#error "compile with -DPMLP_BLK_OM=2|4|8|16"
+#error "compile with -DPMLP_BLK_OM=2|4|16"
 #endif
 
 namespace pmlpk {
@@ -30,6 +30,8 @@ namespace pmlpk {
 namespace {
 
 constexpr int OM = PMLP_BLK_OM;
+constexpr bool MF = OM > 4;  // the output layer's products by matrix instructions
+constexpr int NO = MF ? 4 : OM;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
@@ -41,41 +43,40 @@ __host__ __device__ constexpr int row_bytes(int NF) { return 32 * NF + 16; }
 // the last rows' columns may pass them by
 constexpr size_t lds_bytes(int NF, int SC) { return (size_t)3 * SC * row_bytes(NF) + 64; }
 
-// Values and slopes of activation id A (uniform, or each lane's own arow where the
-// lanes' units differ; then once per id).
+// Values and slopes of activation id A.
 template <int NV>
-__device__ __forceinline__ void acts_bwd(bool one, int arow, const float (&z)[NV], float (&v)[NV],
-                                         float (&d)[NV]) {
-  int A = __builtin_amdgcn_readfirstlane(arow);
-  bool done = false;
+__device__ __forceinline__ void act_and_slope(int A, const float (&z)[NV], float (&v)[NV],
+                                              float (&d)[NV]) {
+  switch (A) {
+#define PMLP_ACT(AA)                                                                     \
+  case AA: {                                                                             \
+    _Pragma("unroll") for (int j = 0; j < NV; ++j) v[j] = act_fwd_bwd(AA, z[j], &d[j]); \
+    break;                                                                               \
+  }
+    PMLP_EVERY_ACT
+#undef PMLP_ACT
+  }
+}
+
+// The same for lanes whose units have activations of their own: once per id.
+template <int NV>
+__device__ __forceinline__ void mixed_act_and_slope(int arow, const float (&z)[NV], float (&v)[NV],
+                                                    float (&d)[NV]) {
+  uint64_t left = ~0ull;
 #pragma unroll 1
-  while (true) {
+  while (left) {
+    const int A = __builtin_amdgcn_readlane(arow, __builtin_ctzll(left));
     float x[NV], tv[NV], td[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {  // (opaque: nothing of an id's terms outside its case)
-      x[j] = z[j];
-      asm volatile("" : "+v"(x[j]));
-    }
-    switch (A) {
-#define PMLP_ACT(AA)                                                                        \
-  case AA: {                                                                                \
-    _Pragma("unroll") for (int j = 0; j < NV; ++j) tv[j] = act_fwd_bwd(AA, x[j], &td[j]); \
-    break;                                                                                  \
-  }
-      PMLP_EVERY_ACT
-#undef PMLP_ACT
-    }
-    const bool mine = one || (!done && arow == A);
+    for (int j = 0; j < NV; ++j) x[j] = opaque(z[j]);  // (or every id's terms would leave the loop)
+    act_and_slope<NV>(A, x, tv, td);
+    const bool mine = arow == A;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       v[j] = mine ? tv[j] : v[j];
       d[j] = mine ? td[j] : d[j];
     }
-    if (one) return;
-    done |= mine;
-    const uint64_t left = __ballot(!done);
-    if (!left) return;
-    A = __builtin_amdgcn_readlane(arow, __builtin_ctzll(left));
+    left &= ~__ballot(mine);
   }
 }
 
@@ -99,10 +100,13 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
       const int s = q / QR, k = 4 * (q - s * QR), b = b0 + s;
       const float* xr = a.X + (int64_t)(b < a.B ? b : a.B - 1) * F;
       f32x2 x[2];
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = xr[k + e < F ? k + e : F - 1];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float v = xr[k + e < F ? k + e : F - 1];
-        x[e >> 1][e & 1] = k + e < F && b < a.B ? v : 0.f;
+        const float w = opaque(v[e]);
+        x[e >> 1][e & 1] = k + e < F && b < a.B ? w : 0.f;
       }
       uint32_t p0[2], p1[2], p2[2];
 #pragma unroll
@@ -121,7 +125,7 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
   const int nchunk = (a.Bp + SC - 1) / SC;
   if (nchunk == 1) {
     fill(0);
-    __syncthreads();
+    lds_barrier();
   }
   // this lane's places in the pieces: a row of the first product, and of the second
   const int zrow = li * RB + 16 * lk;
@@ -136,28 +140,40 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
     const int m = p.mid[n], act = p.actn[n];
     const bool one_act = __all(act == __builtin_amdgcn_readfirstlane(act));
     const float gn = NORM ? p.gain[n] : 1.f;
-    float w2[OM], T[OM];
+    // Up to four outputs: each lane its unit's weights and sums T_o.  More go through
+    // fp32 matrix products, a model at a time: w2[0..3] are then outputs 4 lk + q of
+    // unit li, and T[0..3] their sums.
+    float w2[NO], T[NO];
 #pragma unroll
-    for (int o = 0; o < OM; ++o) {
-      w2[o] = o < p.O ? p.W2[(int64_t)o * p.ldw + n] : 0.f;
+    for (int o = 0; o < NO; ++o) {
+      const int ow = MF ? 4 * lk + o : o;
+      w2[o] = ow < p.O ? p.W2[(int64_t)ow * p.ldw + n] : 0.f;
       T[o] = 0.f;
     }
+    const int m_lo = __builtin_amdgcn_readfirstlane(m), m_hi = __builtin_amdgcn_readlane(m, 15);
     bf16x8 wp[K][NC][3];
 #pragma unroll
     for (int mt = 0; mt < K; ++mt) {
       const float* row = (mt ? p.V1 : p.W1) + n * F4;
+      f32x4 w[2 * NC];
+#pragma unroll
+      for (int e = 0; e < 2 * NC; ++e) {
+        const int k = 32 * (e >> 1) + 8 * lk + 4 * (e & 1);
+        w[e] = *(const f32x4*)(row + (k < F4 ? k : F4 - 4));
+      }
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         f32x4 q[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int k = 32 * c + 8 * lk + 4 * e;
-          q[e] = *(const f32x4*)(row + (k < F4 ? k : F4 - 4));
-          if (k >= F4) q[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+          q[e] = opaque(w[2 * c + e]);
+          if (32 * c + 8 * lk + 4 * e >= F4) q[e] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         split3(q[0], q[1], wp[mt][c][0], wp[mt][c][1], wp[mt][c][2]);
       }
     }
+    const float* const Gm = a.G + (int64_t)m * a.Bp * OM;
+    const float* const Rm = a.R + (int64_t)m * a.Bp * 4;
     f32x4 acc[K][NF];
 #pragma unroll
     for (int mt = 0; mt < K; ++mt)
@@ -167,12 +183,12 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
 #pragma unroll 1
     for (int b0 = 0; b0 < a.Bp; b0 += SC) {
       if (nchunk > 1) {
-        __syncthreads();
+        lds_barrier();
         fill(b0);
-        __syncthreads();
+        lds_barrier();
       }
       if (!live) continue;
-      const int steps = ((a.Bp - b0 < SC ? a.Bp - b0 : SC) + 31) >> 5;
+      const int steps = (a.Bp - b0 < SC ? a.Bp - b0 : SC) >> 5;
 #pragma unroll 1
       for (int st = 0; st < steps; ++st) {
         const int s = 32 * st;
@@ -210,35 +226,64 @@ _Pragma("unroll") for (int i = 0; i < 2; ++i) z[mt][i] =            \
         float zv[8], av[8], dv[8];
 #pragma unroll
         for (int v = 0; v < 8; ++v) zv[v] = z[0][v >> 2][v & 3];
-        acts_bwd<8>(one_act, act, zv, av, dv);
+        if (one_act) act_and_slope<8>(__builtin_amdgcn_readfirstlane(act), zv, av, dv);
+        else mixed_act_and_slope<8>(act, zv, av, dv);
         f32x4 dz[K][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int64_t b = (int64_t)m * a.Bp + b0 + s + 16 * i + 4 * lk;
-          const bool in = b0 + s + 16 * i < a.Bp;  // (Bp is a multiple of 16)
+          const uint32_t b = (uint32_t)(b0 + s + 16 * i + 4 * lk);  // first of four samples
+          f32x4 h, dn = f32x4{0.f, 0.f, 0.f, 0.f}, R[NORM ? 4 : 1];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            h[r] = GATED ? av[4 * i + r] * z[K - 1][i][r] : av[4 * i + r];
+            if (NORM) {
+              R[r] = *(const f32x4*)(Rm + (b + r) * 4);
+              h[r] = (h[r] - R[r][0]) * R[r][1];
+            }
+          }
+          if (MF) {
+            // dN = G W2 and T += G^T h, the sums in the order of the registers
+            f32x4 t = f32x4{T[0], T[1], T[2], T[3]};
+#pragma unroll 1
+            for (int mm = m_lo; mm <= m_hi; ++mm) {
+              const float* const gm = a.G + (int64_t)mm * a.Bp * OM;
+              const f32x4 ga = *(const f32x4*)(gm + (uint32_t)(b0 + s + 16 * i + li) * OM + 4 * lk);
+              f32x4 gt, d = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int r = 0; r < 4; ++r) gt[r] = gm[(b + r) * OM + li];
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                d = __builtin_amdgcn_mfma_f32_16x16x4f32(ga[q], w2[q % NO], d, 0, 0, 0);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                dn[r] = m == mm ? d[r] : dn[r];
+                t = __builtin_amdgcn_mfma_f32_16x16x4f32(gt[r], m == mm ? h[r] : 0.f, t, 0, 0, 0);
+              }
+            }
+#pragma unroll
+            for (int o = 0; o < 4; ++o) T[o % NO] = t[o];
+          } else {
+            float G[4 * OM];
+#pragma unroll
+            for (int v = 0; v < OM; ++v) {
+              const f32x4 q = *(const f32x4*)(Gm + b * OM + 4 * v);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) G[4 * v + e] = q[e];
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+              for (int o = 0; o < NO; ++o) {
+                dn[r] = fmaf(G[r * OM + o], w2[o], dn[r]);
+                T[o] = fmaf(G[r * OM + o], h[r], T[o]);
+              }
+          }
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int v = 4 * i + r;
-            const float u = GATED ? z[K - 1][i][r] : 1.f;
-            float h = GATED ? av[v] * u : av[v];
-            f32x4 R;
-            if (NORM) {
-              R = in ? *(const f32x4*)(a.R + (b + r) * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
-              h = (h - R[0]) * R[1];
-            }
-            float dn = 0.f;
-#pragma unroll
-            for (int o = 0; o < OM; o += 2) {
-              const f32x2 G = in ? *(const f32x2*)(a.G + (b + r) * OM + o) : f32x2{0.f, 0.f};
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                dn = fmaf(G[e], w2[o + e], dn);
-                T[o + e] = fmaf(G[e], h, T[o + e]);
-              }
-            }
-            if (NORM) dn = R[1] * (fmaf(gn, dn, -R[2]) - h * R[3]);
-            dz[0][i][r] = GATED ? dn * u * dv[v] : dn * dv[v];
-            if (GATED) dz[K - 1][i][r] = dn * av[v];
+            if (NORM) dn[r] = R[r][1] * (fmaf(gn, dn[r], -R[r][2]) - h[r] * R[r][3]);
+            dz[0][i][r] = GATED ? dn[r] * z[K - 1][i][r] * dv[v] : dn[r] * dv[v];
+            if (GATED) dz[K - 1][i][r] = dn[r] * av[v];
           }
         }
         // ---- dW1 (and dV1) += dZ^T X ------------------------------------------
@@ -292,12 +337,48 @@ _Pragma("unroll") for (int mt = 0; mt < K; ++mt) acc[mt][j] =        \
         }
       }
     }
+    if (MF) {
+      if (n0 + li >= p.N) continue;
+      float dg = 0.f, ds = 0.f;
+      const float sn = NORM ? p.shift[n] : 0.f;
+      const float rate = a.g.lrm ? a.g.lrm[m] : a.g.lr;
 #pragma unroll
-    for (int o = 0; o < OM; ++o) {
-      T[o] += __shfl_xor(T[o], 16);
-      T[o] += __shfl_xor(T[o], 32);
+      for (int q = 0; q < NO; ++q) {
+        const int o = 4 * lk + q;
+        if (o >= p.O) continue;
+        float dw = T[q];
+        if (NORM) {
+          const float s = a.Gs[(int64_t)m * p.O + o];
+          dg = fmaf(w2[q], T[q], dg);
+          ds = fmaf(w2[q], s, ds);
+          dw = fmaf(gn, T[q], sn * s);
+        }
+        if (a.g.dW2) a.g.dW2[(int64_t)o * p.N + n] = dw;
+        else p.W2[(int64_t)o * p.ldw + n] = w2[q] - rate * dw;
+      }
+      if (NORM) {  // (the four lk of a unit are all here or none is)
+        dg += __shfl_xor(dg, 16);
+        ds += __shfl_xor(ds, 16);
+        dg += __shfl_xor(dg, 32);
+        ds += __shfl_xor(ds, 32);
+        if (lk == 0) {
+          if (a.g.dW2) {
+            a.g.dgain[n] = dg;
+            a.g.dshift[n] = ds;
+          } else {
+            p.gain[n] = gn - rate * dg;
+            p.shift[n] = sn - rate * ds;
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int o = 0; o < NO; ++o) {
+        T[o] += __shfl_xor(T[o], 16);
+        T[o] += __shfl_xor(T[o], 32);
+      }
+      if (lk == 0 && n0 + li < p.N) blk_unit_grads<NO, NORM>(p, a.g, a.Gs, n, m, gn, w2, T);
     }
-    if (lk == 0 && n0 + li < p.N) blk_unit_grads<OM, NORM>(p, a.g, a.Gs, n, m, gn, w2, T);
   }
 }
 
@@ -350,7 +431,7 @@ hipError_t PMLP_CAT(launch_blk_fused_bwd_, PMLP_BLK_OM)(const BlkPack& p, BlkBwd
     e = hipDeviceGetAttribute(&lmax, hipDeviceAttributeMaxSharedMemoryPerBlock, dev);
   if (e != hipSuccess) return e;
   a.SC = fn ? chunk_samples(NF, a.Bp, (size_t)lmax) : 0;
-  if (a.SC <= 0 || a.Bp < 16 || a.Bp % 16 || a.B < 1 || a.B > a.Bp || p.O > OM || p.N < 1)
+  if (a.SC <= 0 || a.Bp < 32 || a.Bp % 32 || a.B < 1 || a.B > a.Bp || p.O > OM || p.N < 1)
     return hipErrorInvalidValue;
   const size_t lds = lds_bytes(NF, a.SC);
   const int64_t tiles = (p.N + 15) / 16;

@@ -18,6 +18,8 @@
 
 #include "block_device.h"
 
+#include <algorithm>
+
 #ifndef PMLP_BLK_NW
 #error "compile with -DPMLP_BLK_NW=0|1|2|4|8"
 #endif
@@ -41,7 +43,7 @@ template <int NC, int RM, int OM, bool GATED>
 struct TileLds {
   static constexpr int K = GATED ? 2 : 1;
   static constexpr int kW2 = K * (NC * 3072 + RM * 256);
-  static constexpr int bytes = kW2 + OM * 64;
+  static constexpr int bytes = kW2 + OM * 64 + 16;  // (and the tile's info and model)
 };
 
 template <int NC, int RM, int OM, bool GATED, bool NORM>
@@ -70,40 +72,78 @@ void k_blk_fused_fwd(BlkPack p, BlkFwdArgs a) {
   for (int i = 0; i < NI; ++i) {
     const int b = chunk * kBS + 16 * (wave * NI + i) + li;
     const float* xr = a.X + (int64_t)(b < a.B ? b : a.B - 1) * F;
+    float v[NC > 0 ? 8 * NC : 1], t[RM > 0 ? RM : 1];  // all loads first
+#pragma unroll
+    for (int e = 0; e < 8 * NC; ++e) {
+      const int k = 32 * (e >> 3) + 8 * lk + (e & 7);
+      v[e] = xr[k < F ? k : F - 1];
+    }
+#pragma unroll
+    for (int q = 0; q < RM; ++q) {
+      const int k = 32 * NC + 4 * q + lk;
+      t[q] = xr[k < F ? k : F - 1];
+    }
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       f32x4 q[2];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int k = 32 * c + 8 * lk + e;
-        const float v = xr[k < F ? k : F - 1];
-        q[e >> 2][e & 3] = k < F && b < a.B ? v : 0.f;
+        const float w = opaque(v[8 * c + e]);
+        q[e >> 2][e & 3] = 32 * c + 8 * lk + e < F && b < a.B ? w : 0.f;
       }
       split3(q[0], q[1], x0[i][c], x1[i][c], x2[i][c]);
     }
 #pragma unroll
     for (int q = 0; q < RM; ++q) {
-      const int k = 32 * NC + 4 * q + lk;
-      const float v = xr[k < F ? k : F - 1];
-      xt[i][q] = q < rem && k < F && b < a.B ? v : 0.f;
+      const float w = opaque(t[q]);
+      xt[i][q] = q < rem && 32 * NC + 4 * q + lk < F && b < a.B ? w : 0.f;
     }
   }
 
-  struct Raw {  // this wave's part of a stage, as loaded
+  // This wave's part of a stage: up to UPW chunk strips, RPW remainder strips and
+  // one tile's output rows.  Every load is made, of the last strip or tile again
+  // where there is none, so that waits count what is in flight; descriptors come by
+  // scalar loads a stage ahead of the loads that need them.
+  constexpr int NPART = UPW + RPW + 1;
+  const auto* const tiles = (const __attribute__((address_space(4))) BlkTile*)(uintptr_t)a.tiles;
+  auto part_tile = [&](int i) {  // tile within the stage of part i
+    if (i < UPW) return NC ? std::min(wave + i * NW, UNITS - 1) / (K * (NC ? NC : 1)) : 0;
+    if (i < UPW + RPW) return std::min(wave + (i - UPW) * NW, REMS - 1) / K;
+    return std::min(wave, ST - 1);
+  };
+  struct Desc {
+    int n0[NPART], info[NPART], m;  // (m: of tile `wave`)
+  };
+  auto load_desc = [&](int ts) {
+    Desc d;
+#pragma unroll
+    for (int i = 0; i < NPART; ++i) {
+      const int t = std::min(ts + part_tile(i), t1 - 1);
+      d.n0[i] = tiles[t].n0;
+      d.info[i] = tiles[t].info;
+      if (i == NPART - 1) d.m = tiles[t].m;
+    }
+    return d;
+  };
+  struct Raw {
     f32x4 c[2 * UPW];
     float t[RPW][RM > 0 ? RM : 1];
     float w2[W2E], g[W2E];
+    int cnt[NPART];
+    int word, m;  // of tile `wave`
   } raw;
-  // row li of tile t, or the tile's last unit (put() makes such rows zero)
-  auto fetch = [&](int ts) {
+  // row li of a tile, or the tile's last unit (put() makes such rows zero)
+  const float *W1 = p.W1, *V1 = p.V1;
+  asm volatile("" : "+s"(W1), "+s"(V1));  // (or each choice of one is a load of its address)
+  auto fetch = [&](const Desc& ds) {
 #pragma unroll
-    for (int i = 0; i < UPW; ++i) {
-      const int u = wave + i * NW;
-      if (NC == 0 || u >= UNITS) continue;
-      const int j = u / (K * NC), v = u - j * (K * NC), mat = v / (NC ? NC : 1), c = v - mat * NC;
-      if (ts + j >= t1) continue;
-      const BlkTile q = a.tiles[ts + j];
-      const float* row = (mat ? p.V1 : p.W1) + (int64_t)(q.n0 + (li < q.cnt ? li : q.cnt - 1)) * F4;
+    for (int i = 0; i < NPART; ++i) raw.cnt[i] = ds.info[i] & 255;
+#pragma unroll
+    for (int i = 0; i < (NC ? UPW : 0); ++i) {
+      const int u = std::min(wave + i * NW, UNITS - 1), v = u % (K * (NC ? NC : 1));
+      const int mat = v / (NC ? NC : 1), c = v - mat * NC;
+      const float* row =
+          (mat ? V1 : W1) + (int64_t)(ds.n0[i] + std::min(li, raw.cnt[i] - 1)) * F4;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int k = 32 * c + 8 * lk + 4 * e;
@@ -111,65 +151,67 @@ void k_blk_fused_fwd(BlkPack p, BlkFwdArgs a) {
       }
     }
 #pragma unroll
-    for (int i = 0; i < RPW; ++i) {
-      const int u = wave + i * NW;
-      if (RM == 0 || u >= REMS || ts + u / K >= t1) continue;
-      const BlkTile q = a.tiles[ts + u / K];
-      const float* row =
-          (u % K ? p.V1 : p.W1) + (int64_t)(q.n0 + (li < q.cnt ? li : q.cnt - 1)) * F4;
+    for (int i = 0; i < (RM ? RPW : 0); ++i) {
+      const float* row = (std::min(wave + i * NW, REMS - 1) % K ? V1 : W1) +
+                         (int64_t)(ds.n0[UPW + i] + std::min(li, raw.cnt[UPW + i] - 1)) * F4;
 #pragma unroll
       for (int s = 0; s < RM; ++s) raw.t[i][s] = row[s < rem ? 32 * NC + 4 * s + lk : 0];
     }
-    if (wave < ST && ts + wave < t1) {
-      const BlkTile q = a.tiles[ts + wave];
+    const int n0 = ds.n0[NPART - 1], cnt = raw.cnt[NPART - 1];
 #pragma unroll
-      for (int e = 0; e < W2E; ++e) {
-        const int v = lane + 64 * e, o = v >> 4, u = v & 15;
-        const bool in = o < p.O && u < q.cnt;
-        const int64_t n = q.n0 + (in ? u : 0);
-        raw.w2[e] = in ? p.W2[(int64_t)o * p.ldw + n] : 0.f;
-        raw.g[e] = NORM && in ? p.gain[n] : 1.f;
-      }
+    for (int e = 0; e < W2E; ++e) {
+      const int v = lane + 64 * e, o = v >> 4, u = v & 15;
+      const int64_t n = n0 + (u < cnt ? u : 0);
+      raw.w2[e] = p.W2[(int64_t)(o < p.O ? o : 0) * p.ldw + n];
+      raw.g[e] = NORM ? p.gain[n] : 1.f;
     }
+    raw.word = ds.info[NPART - 1];
+    raw.m = ds.m;
   };
-  auto put = [&](int ts, int buf) {
+  auto put = [&](int buf) {
     char* const base = lds + buf * ST * L::bytes;
 #pragma unroll
-    for (int i = 0; i < UPW; ++i) {
+    for (int i = 0; i < (NC ? UPW : 0); ++i) {
       const int u = wave + i * NW;
-      if (NC == 0 || u >= UNITS) continue;
-      const int j = u / (K * NC), v = u - j * (K * NC), mat = v / (NC ? NC : 1), c = v - mat * NC;
-      if (ts + j >= t1) continue;
-      const bool in = li < a.tiles[ts + j].cnt;
+      const int j = u / (K * (NC ? NC : 1)), v = u - j * (K * NC), c = v % (NC ? NC : 1);
+      const bool in = li < raw.cnt[i];
       f32x4 r[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
+        const f32x4 w = opaque(raw.c[2 * i + e]);
         const bool ok = in && 32 * c + 8 * lk + 4 * e < F4;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) r[e][q] = ok ? raw.c[2 * i + e][q] : 0.f;
+        for (int q = 0; q < 4; ++q) r[e][q] = ok ? w[q] : 0.f;
       }
       bf16x8 p0, p1, p2;
       split3(r[0], r[1], p0, p1, p2);
-      bf16x8* d = (bf16x8*)(base + j * L::bytes + (mat * NC + c) * 3072) + lane;
-      d[0] = p0;
-      d[64] = p1;
-      d[128] = p2;
+      if (u < UNITS) {
+        bf16x8* d = (bf16x8*)(base + j * L::bytes + v * 3072) + lane;
+        d[0] = p0;
+        d[64] = p1;
+        d[128] = p2;
+      }
     }
 #pragma unroll
-    for (int i = 0; i < RPW; ++i) {
+    for (int i = 0; i < (RM ? RPW : 0); ++i) {
       const int u = wave + i * NW;
-      if (RM == 0 || u >= REMS || ts + u / K >= t1) continue;
-      const bool in = li < a.tiles[ts + u / K].cnt;
+      const bool in = li < raw.cnt[UPW + i];
       float* d = (float*)(base + (u / K) * L::bytes + K * NC * 3072 + (u % K) * (RM * 256)) + lane;
 #pragma unroll
-      for (int s = 0; s < RM; ++s) d[64 * s] = in && s < rem ? raw.t[i][s] : 0.f;
+      for (int s = 0; s < RM; ++s) {
+        const float w = opaque(raw.t[i][s]);
+        if (u < REMS) d[64 * s] = in && s < rem ? w : 0.f;
+      }
     }
-    if (wave < ST && ts + wave < t1) {
-      float* d = (float*)(base + wave * L::bytes + L::kW2) + lane;
+    float* d = (float*)(base + wave * L::bytes + L::kW2) + lane;
 #pragma unroll
-      for (int e = 0; e < W2E; ++e)
-        if (lane + 64 * e < 16 * OM) d[64 * e] = raw.w2[e] * raw.g[e];
+    for (int e = 0; e < W2E; ++e) {
+      const int v = lane + 64 * e;
+      const float w = opaque(raw.w2[e]) * opaque(raw.g[e]);
+      if (wave < ST && v < 16 * OM)
+        d[64 * e] = (v >> 4) < p.O && (v & 15) < raw.cnt[NPART - 1] ? w : 0.f;
     }
+    if (wave < ST && lane < 2) ((int*)d)[16 * OM] = lane ? raw.m : raw.word;
   };
 
   // running sums of the open model: outputs (lane's own units; with matrix products
@@ -232,17 +274,26 @@ void k_blk_fused_fwd(BlkPack p, BlkFwdArgs a) {
     reset();
   };
 
-  fetch(t0);
-  put(t0, 0);
-  if (t0 + ST < t1) fetch(t0 + ST);
-  __syncthreads();
+  Desc next = load_desc(t0);
+  fetch(next);
+  next = load_desc(t0 + ST);
+  put(0);
+  fetch(next);
+  next = load_desc(t0 + 2 * ST);
+  lds_barrier();
   int buf = 0;
 #pragma unroll 1
   for (int ts = t0; ts < t1; ts += ST, buf ^= 1) {
 #pragma unroll 1
     for (int j = 0; j < ST && ts + j < t1; ++j) {
-      const BlkTile q = a.tiles[ts + j];
       const char* const base = lds + (buf * ST + j) * L::bytes;
+      const int2 word = *(const int2*)(base + L::kW2 + 64 * OM);
+      float wt[K][RM > 0 ? RM : 1];
+#pragma unroll
+      for (int mt = 0; mt < K; ++mt)
+#pragma unroll
+        for (int s = 0; s < RM; ++s)
+          wt[mt][s] = ((const float*)(base + K * NC * 3072 + mt * (RM * 256)))[64 * s + lane];
       f32x4 acc[K][NI];
 #pragma unroll
       for (int mt = 0; mt < K; ++mt)
@@ -250,47 +301,46 @@ void k_blk_fused_fwd(BlkPack p, BlkFwdArgs a) {
         for (int i = 0; i < NI; ++i) acc[mt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
+        bf16x8 wc[K][3];
 #pragma unroll
-        for (int mt = 0; mt < K; ++mt) {
-          bf16x8 wc[3];
+        for (int mt = 0; mt < K; ++mt)
 #pragma unroll
           for (int e = 0; e < 3; ++e)
-            wc[e] = ((const bf16x8*)(base + (mt * NC + c) * 3072))[64 * e + lane];
-          // the piece products smallest first
+            wc[mt][e] = ((const bf16x8*)(base + (mt * NC + c) * 3072))[64 * e + lane];
+        // the piece products smallest first, the blocks and projections in turn
 #define PMLP_PIECE(E, XP)                                     \
+_Pragma("unroll") for (int mt = 0; mt < K; ++mt)              \
 _Pragma("unroll") for (int i = 0; i < NI; ++i) acc[mt][i] = \
-    __builtin_amdgcn_mfma_f32_16x16x32_bf16(wc[E], XP[i][c], acc[mt][i], 0, 0, 0)
-          PMLP_PIECE(0, x2);
-          PMLP_PIECE(1, x1);
-          PMLP_PIECE(2, x0);
-          PMLP_PIECE(0, x1);
-          PMLP_PIECE(1, x0);
-          PMLP_PIECE(0, x0);
+    __builtin_amdgcn_mfma_f32_16x16x32_bf16(wc[mt][E], XP[i][c], acc[mt][i], 0, 0, 0)
+        PMLP_PIECE(0, x2);
+        PMLP_PIECE(1, x1);
+        PMLP_PIECE(2, x0);
+        PMLP_PIECE(0, x1);
+        PMLP_PIECE(1, x0);
+        PMLP_PIECE(0, x0);
 #undef PMLP_PIECE
-        }
       }
 #pragma unroll
       for (int s = 0; s < RM; ++s)
         if (s < rem) {
 #pragma unroll
-          for (int mt = 0; mt < K; ++mt) {
-            const float wt = ((const float*)(base + K * NC * 3072 + mt * (RM * 256)))[64 * s + lane];
+          for (int mt = 0; mt < K; ++mt)
 #pragma unroll
             for (int i = 0; i < NI; ++i)
               acc[mt][i] =
-                  __builtin_amdgcn_mfma_f32_16x16x4f32(wt, xt[i][s], acc[mt][i], 0, 0, 0);
-          }
+                  __builtin_amdgcn_mfma_f32_16x16x4f32(wt[mt][s], xt[i][s], acc[mt][i], 0, 0, 0);
         }
+      const int info = __builtin_amdgcn_readfirstlane(word.x), tcnt = info & 255;
       float z[4 * NI], h[4 * NI];
 #pragma unroll
       for (int v = 0; v < 4 * NI; ++v) z[v] = acc[0][v >> 2][v & 3];
-      blk_acts<4 * NI>(p.actn[q.n0], z, h);
+      blk_acts<4 * NI>((info >> 8) & 255, z, h);
       if (GATED) {
 #pragma unroll
         for (int v = 0; v < 4 * NI; ++v) h[v] *= acc[K - 1][v >> 2][v & 3];
       }
-      const int mine = q.cnt - 4 * lk;  // units of this lane: min(4, mine), if positive
-      if (q.cnt < 16) {
+      const int mine = tcnt - 4 * lk;  // units of this lane: min(4, mine), if positive
+      if (tcnt < 16) {
 #pragma unroll
         for (int v = 0; v < 4 * NI; ++v) h[v] = (v & 3) < mine ? h[v] : 0.f;
       }
@@ -313,7 +363,7 @@ _Pragma("unroll") for (int i = 0; i < NI; ++i) acc[mt][i] = \
         }
       }
       if (NORM) {
-        if (q.cnt == 16) {
+        if (tcnt == 16) {
           const float n = cnt + 4.f, f = 4.f * frcp(n), nf = cnt * f;
 #pragma unroll
           for (int i = 0; i < NI; ++i) {
@@ -343,13 +393,12 @@ _Pragma("unroll") for (int i = 0; i < NI; ++i) acc[mt][i] = \
           cnt = n;
         }
       }
-      if (ts + j + 1 == t1 || a.tiles[ts + j + 1].m != q.m) emit(q.m);
+      if (ts + j + 1 == t1 || (info & kBlkLast)) emit(__builtin_amdgcn_readfirstlane(word.y));
     }
-    if (ts + ST < t1) {
-      put(ts + ST, buf ^ 1);
-      if (ts + 2 * ST < t1) fetch(ts + 2 * ST);
-    }
-    __syncthreads();
+    put(buf ^ 1);
+    fetch(next);
+    next = load_desc(ts + 3 * ST);
+    lds_barrier();
   }
 }
 

@@ -15,12 +15,11 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libpmlp.so")
-# (source, extra flags); the one-kernel forward passes are compiled once per padded
-# batch size (waves per workgroup), the one-kernel backward pass once per class of
-# outputs
+# (source, extra flags); the one-kernel forward pass is compiled once per padded
+# batch size, those of block packs once per class of outputs
 SOURCES = [("k_lds.hip", [])]
 SOURCES += [("k_fwd_s.hip", ["-DPMLP_FWD_BP=%d" % bp]) for bp in (256, 128, 64, 32, 16)]
-SOURCES += [("k_block_fwd.hip", ["-DPMLP_BLK_NW=%d" % nw]) for nw in (8, 4, 2, 1, 0)]
+SOURCES += [("k_block_fwd.hip", ["-DPMLP_BLK_OM=%d" % om]) for om in (16, 2)]
 SOURCES += [("k_block_bwd.hip", ["-DPMLP_BLK_OM=%d" % om]) for om in (16, 4, 2)]
 SOURCES += [(s, []) for s in ("k_gemm_bf16.hip", "k_m3.hip", "k_misc.hip", "k_gemm.hip", "k_deep.hip",
                               "k_block.hip", "api.hip")]

@@ -100,6 +100,12 @@ struct PmlpDeep {
   float* Zt2 = nullptr;       // [N2pad][Bp]
 };
 
+// How a batch runs through the fused forward of a block pack: SC samples a workgroup,
+// wpc workgroups of `waves` waves for each SC samples.  SC = 0: it does not.
+struct BlkRun {
+  int32_t SC = 0, wpc = 0, waves = 0;
+};
+
 // The gate and the norm of a pack made by pmlp_create_block (W1 is then the
 // first half of one allocation whose second half, if gated, is V1).
 struct PmlpBlock {
@@ -113,7 +119,8 @@ struct PmlpBlock {
   BlkTile* d_tiles = nullptr;
   int32_t* d_toff = nullptr;  // [M+1]
   int32_t ntiles = 0;
-  int slots[5] = {-1, -1, -1, -1, -1};  // of the fused forward's batch classes
+  int32_t planned = 0;  // batch size of `plan` (0: none yet)
+  BlkRun plan;
   // Workspace.  A captured graph keeps the addresses it was captured with, so a
   // buffer that a larger batch replaces lives until the handle goes.
   unsigned char* ws = nullptr;
@@ -1340,10 +1347,7 @@ void block_tiles(const std::vector<int32_t>& hs, const std::vector<int32_t>& act
   for (size_t m = 0; m < hs.size(); ++m) {
     toff.push_back((int32_t)tiles.size());
     for (int32_t at = 0; at < hs[m]; at += 16)
-      tiles.push_back(BlkTile{(int32_t)(n + at), (int32_t)m,
-                              std::min(16, hs[m] - at) + 256 * acts[m] +
-                                  (at + 16 >= hs[m] ? kBlkLast : 0),
-                              0});
+      tiles.push_back(BlkTile{(int32_t)(n + at), std::min(16, hs[m] - at), (int32_t)m, acts[m]});
     n += hs[m];
   }
   toff.push_back((int32_t)tiles.size());
@@ -1490,31 +1494,11 @@ int block_weight_grad(pmlp* h, const float* dZt, const float* Xt, int32_t Bp, fl
   return run(h, KID_GEMM_BWD, [&] { return launch_gemm(g, dW ? EPI_GRAD : EPI_SGD, h->stream); });
 }
 
-// ---- the fused forward ---------------------------------------------------------
+// ---- the fused kernels -----------------------------------------------------------
 
-constexpr int kBlkClasses = 5;
-constexpr int kBlkWaves[kBlkClasses] = {0, 1, 2, 4, 8};
-
-#define PMLP_BY_WAVES(c, call)  \
-  switch (kBlkWaves[c]) {       \
-    case 0: return call(0);     \
-    case 1: return call(1);     \
-    case 2: return call(2);     \
-    case 4: return call(4);     \
-    default: return call(8);    \
-  }
-
-int blk_fwd_slots(int c, const BlkPack& p) {
-#define PMLP_CALL(NW) blk_fwd_slots_##NW(p)
-  PMLP_BY_WAVES(c, PMLP_CALL)
-#undef PMLP_CALL
-}
-
-hipError_t launch_blk_fused_fwd(int c, const BlkPack& p, const BlkFwdArgs& a, hipStream_t s) {
+hipError_t launch_blk_fused_fwd(const BlkPack& p, const BlkFwdArgs& a, hipStream_t s) {
   note_variant("k_blk_fused_fwd", kArithX3);
-#define PMLP_CALL(NW) launch_blk_fused_fwd_##NW(p, a, s)
-  PMLP_BY_WAVES(c, PMLP_CALL)
-#undef PMLP_CALL
+  return p.O <= 2 ? launch_blk_fused_fwd_2(p, a, s) : launch_blk_fused_fwd_16(p, a, s);
 }
 
 hipError_t launch_blk_fused_bwd(const BlkPack& p, const BlkBwdArgs& a, hipStream_t s) {
@@ -1526,40 +1510,43 @@ hipError_t launch_blk_fused_bwd(const BlkPack& p, const BlkBwdArgs& a, hipStream
   }
 }
 
-// How a batch runs through the fused forward: its class, batches of bs samples,
-// workgroups for each.  c < 0: it does not.
-struct BlkRun {
-  int c = -1;
-  int32_t bs = 0, nchunk = 0, wpc = 0;
-};
-
+// The run of B samples: the samples of a workgroup and the waves that share them, by
+// what a launch costs.  A wave's step of 32 samples takes its share of the SIMD, a
+// tile the wait for its weights and their splitting (as long as three steps), and a
+// workgroup the pieces of its samples (as long as six and, for each 32 samples, one
+// over its waves).
 BlkRun block_run(pmlp* h, int32_t B) {
   PmlpBlock* k = h->block;
-  BlkRun best;
-  if (!h->lds_kernels || h->F4 > kBlkFusedCols) return best;
+  if (!h->lds_kernels || h->F4 > kBlkFusedCols) return BlkRun{};
+  if (k->planned == B) return k->plan;
   const BlkPack p = block_pack(h);
+  BlkRun best;
   double least = 0;
-  for (int c = 0; c < kBlkClasses; ++c) {
-    const int nw = kBlkWaves[c];
-    const int32_t bs = nw ? 32 * nw : 16, nchunk = div_up(B, bs);
-    if (nchunk > 1 && nw < 2) continue;  // more samples than a small class takes
-    if (k->slots[c] < 0) k->slots[c] = blk_fwd_slots(c, p);
-    const int64_t slots = k->slots[c];
-    if (slots <= 0) continue;
-    const int64_t fit = std::max<int64_t>(1, slots / nchunk);
-    for (int64_t w = fit; w <= std::max<int64_t>(fit, 32); ++w) {
-      const int64_t wpc = std::min<int64_t>(w, k->ntiles);
-      const int64_t rounds = (nchunk * wpc + slots - 1) / slots;
-      const double cost =
-          (double)rounds * (div_up(k->ntiles, wpc) + 3) * (nw > 1 ? nw : 1) * 256.0 / (double)slots *
-          (nw > 1 ? 1 + 0.3 / nw : 1);
-      if (best.c < 0 || cost < least) {
-        least = cost;
-        best = BlkRun{c, bs, nchunk, (int32_t)wpc};
+  int32_t last = 0;
+  for (int32_t most = 256; most >= 32; most >>= 1) {
+    const int32_t nchunk = div_up(B, most), SC = (div_up(B, nchunk) + 31) & ~31;
+    if (SC == last) continue;
+    last = SC;
+    for (int32_t waves = 4; waves <= 16; waves += 4) {
+      const int64_t slots = p.O <= 2 ? blk_fwd_slots_2(p, SC, waves) : blk_fwd_slots_16(p, SC, waves);
+      if (slots <= 0) continue;
+      const int64_t fit = std::max<int64_t>(1, slots / nchunk), want = div_up(k->ntiles, waves);
+      for (int64_t w = fit; w <= std::max<int64_t>(fit, 32); ++w) {
+        const int64_t wpc = std::min(w, want), wgs = nchunk * wpc;
+        const int64_t rounds = (wgs + slots - 1) / slots;
+        const double simd = std::max(1.0, (double)waves * std::min(wgs, slots) / 1024);
+        const double steps = SC / 32, tiles = div_up(k->ntiles, wpc * waves);
+        const double cost = rounds * (tiles * (steps * simd + 3) + 6 + 8 * steps / waves);
+        if (!best.SC || cost < least * 0.999) {
+          least = cost;
+          best = BlkRun{SC, (int32_t)wpc, waves};
+        }
+        if (w >= want) break;
       }
     }
-    if (nchunk == 1) break;
   }
+  k->planned = B;
+  k->plan = best;
   return best;
 }
 
@@ -1574,8 +1561,8 @@ int forward_block(pmlp* h, const float* X, int32_t B, float* out) {
   const size_t rows = (size_t)h->Npad * (k->gated ? 2 : 1);
   int32_t slice = B;
   const BlkRun whole = block_run(h, B);
-  const bool fused = whole.c >= 0;
-  const size_t rec = (size_t)h->M * blk_planes(p) * sizeof(float);  // (about) per sample
+  const bool fused = whole.SC > 0;
+  const size_t rec = (size_t)k->ntiles * blk_planes(p) * sizeof(float);  // per sample
   if (fused) {
     if (rec * B > kRecordSlice)
       slice = (int32_t)std::min<size_t>(std::max<size_t>(kRecordSlice / rec / 256 * 256, 256), B);
@@ -1590,15 +1577,11 @@ int forward_block(pmlp* h, const float* X, int32_t B, float* out) {
   const uintptr_t l0 = (uintptr_t)out, l1 = l0 + (size_t)nout * sizeof(float);
   const bool over = x0 < l1 && l0 < x1;
   const int32_t Bp = pad_batch(slice);
-  const BlkRun r0 = block_run(h, slice), r1 = block_run(h, B % slice ? B % slice : slice);
   Carver c;
   const size_t oXp = c.take(fused ? 0 : (size_t)Bp * h->F4),
                oXt = c.take(fused ? 0 : (size_t)Bp * h->F4), oZ = c.take(fused ? 0 : rows * Bp);
-  auto records = [&](const BlkRun& r) {
-    return (size_t)(h->M + r.wpc) * blk_planes(p) * ((size_t)r.nchunk * r.bs);
-  };
-  const size_t oP = c.take(fused ? std::max(records(r0), records(r1))
-                                 : (size_t)k->npieces * blk_planes(p) * Bp);
+  const int32_t br = fused ? (slice + 31) & ~31 : Bp;  // samples of a record
+  const size_t oP = c.take((size_t)(fused ? k->ntiles : k->npieces) * blk_planes(p) * br);
   const size_t oL = over ? c.take((size_t)nout) : 0;
   if (int rc = ensure_block_ws(h, c.bytes)) return rc;
   float *Xp = (float*)(k->ws + oXp), *Xt = (float*)(k->ws + oXt), *Zt = (float*)(k->ws + oZ),
@@ -1606,14 +1589,14 @@ int forward_block(pmlp* h, const float* X, int32_t B, float* out) {
   for (int32_t b0 = 0; b0 < B; b0 += slice) {
     const int32_t n = std::min(slice, B - b0), np = pad_batch(n);
     if (fused) {
-      const BlkRun& r = n == slice ? r0 : r1;
-      const int32_t br = r.nchunk * r.bs;
-      const BlkFwdArgs f{X + (int64_t)b0 * h->F, n, h->F, k->d_tiles, k->ntiles, r.wpc, part, br};
-      if (int rc = run(h, KID_FWD_M3, [&] { return launch_blk_fused_fwd(r.c, p, f, h->stream); }))
+      const BlkRun r = block_run(h, n);
+      const BlkFwdArgs f{X + (int64_t)b0 * h->F, n, h->F, k->d_tiles, k->ntiles, r.SC, r.wpc,
+                         r.waves, part, br};
+      if (int rc = run(h, KID_FWD_M3, [&] { return launch_blk_fused_fwd(p, f, h->stream); }))
         return rc;
-      const BlkMap map{k->d_toff, k->ntiles, r.wpc};
       if (int rc = run(h, KID_CE, [&] {
-            return launch_blk_out(p, map, part, br, n, dst + b0 * sb, h->O, sb, h->stream);
+            return launch_blk_out(p, BlkMap{k->d_toff, k->ntiles}, part, br, n, dst + b0 * sb, h->O, sb,
+                                  h->stream);
           }))
         return rc;
       continue;
@@ -1649,28 +1632,28 @@ int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_
   const BlkPack p = block_pack(h);
   if (int rc = use_device(h)) return rc;
   const BlkRun r = block_run(h, B);
-  const bool fused = r.c >= 0;
+  const bool fused = r.SC > 0;
   const int32_t Bp = fused ? (B + 31) & ~31 : pad_batch(B);
   const size_t rows = (size_t)h->Npad * (k->gated ? 2 : 1), mb = (size_t)h->M * Bp;
   Carver c;
-  const int32_t br = fused ? r.nchunk * r.bs : Bp;
   const size_t oXp = c.take(fused ? 0 : (size_t)Bp * h->F4),
                oXt = c.take(fused ? 0 : (size_t)Bp * h->F4);
   const size_t oG = c.take(mb * blk_om(h->O)), oR = c.take(k->norm ? mb * 4 : 0),
                oS = c.take(k->norm ? (size_t)h->M * h->O : 0);
-  const size_t oP = c.take((size_t)(fused ? h->M + r.wpc : k->npieces) * blk_planes(p) * br),
+  const size_t oP = c.take((size_t)(fused ? k->ntiles : k->npieces) * blk_planes(p) * Bp),
                oZ = c.take(fused ? 0 : rows * Bp);
   if (int rc = ensure_block_ws(h, c.bytes)) return rc;
   auto at = [&](size_t o) { return (float*)(k->ws + o); };
   const BlkLoss l{y, Y, B, at(oG), at(oR), at(oS), h->loss, h->flag, d.dW1 ? nullptr : lrm};
   const BlkGrads g{d.dW2, d.dgain, d.dshift, lr, lrm};
   if (fused) {
-    const BlkFwdArgs f{X, B, h->F, k->d_tiles, k->ntiles, r.wpc, at(oP), br};
-    if (int rc = run(h, KID_FWD_M3, [&] { return launch_blk_fused_fwd(r.c, p, f, h->stream); }))
+    const BlkFwdArgs f{X,    B,     h->F,    k->d_tiles, k->ntiles,
+                       r.SC, r.wpc, r.waves, at(oP),     Bp};
+    if (int rc = run(h, KID_FWD_M3, [&] { return launch_blk_fused_fwd(p, f, h->stream); }))
       return rc;
-    const BlkMap map{k->d_toff, k->ntiles, r.wpc};
-    if (int rc = run(h, KID_CE,
-                     [&] { return launch_blk_loss(p, map, at(oP), br, Bp, l, h->stream); }))
+    if (int rc = run(h, KID_CE, [&] {
+          return launch_blk_loss(p, BlkMap{k->d_toff, k->ntiles}, at(oP), Bp, Bp, l, h->stream);
+        }))
       return rc;
     const BlkBwdArgs b{X, B, h->F, Bp, 0, at(oG), at(oR), at(oS), d.dW1, d.dV1, g};
     if (int rc = run(h, KID_BWD_FUSED, [&] { return launch_blk_fused_bwd(p, b, h->stream); }))

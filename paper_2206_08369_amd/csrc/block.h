@@ -38,20 +38,15 @@ struct BlkPack {
 
 // The forward's tiles: up to 16 units of one model, in unit order.
 struct BlkTile {
-  int32_t n0, m;
-  int32_t info;  // units, + 256 activation id, + kBlkLast at a model's last tile
-  int32_t spare;
+  int32_t n0, cnt, m, act;
 };
-constexpr int kBlkLast = 65536;
 static_assert(sizeof(BlkTile) == 16, "BlkTile layout");
 
 // Where the sums of model m lie: in the stored path its pieces poff[m] ..
-// poff[m+1]-1; in the fused path (toff set), whose W workgroups per batch take runs
-// of the T tiles, one record per workgroup w that has tiles of it, at m + w (both
-// grow along the tiles, so no two records meet).
+// poff[m+1]-1; in the fused path (toff set) its tiles.
 struct BlkMap {
   const int32_t* toff;  // [M+1] first tile of each model, or null
-  int32_t T, W;
+  int32_t pieces;       // tiles
 };
 
 struct BlkFwdArgs {
@@ -59,18 +54,17 @@ struct BlkFwdArgs {
   int32_t B, F;
   const BlkTile* tiles;
   int32_t ntiles;
-  int32_t wpc;     // workgroups per batch of samples
-  float* part;     // records of blk_planes planes of Bp samples
-  int32_t Bp;      // whole batches of samples
+  int32_t SC;      // samples of a workgroup, a multiple of 32
+  int32_t wpc;     // workgroups for each SC samples
+  int32_t waves;   // of a workgroup
+  float* part;     // records of blk_planes planes of Br samples
+  int32_t Br;      // multiple of 32
 };
-#define PMLP_BLK_FWD_DECL(NW)             \
-  int blk_fwd_slots_##NW(const BlkPack& p); \
-  hipError_t launch_blk_fused_fwd_##NW(const BlkPack& p, const BlkFwdArgs& a, hipStream_t s);
-PMLP_BLK_FWD_DECL(0)
-PMLP_BLK_FWD_DECL(1)
+#define PMLP_BLK_FWD_DECL(OM)                                               \
+  int blk_fwd_slots_##OM(const BlkPack& p, int32_t SC, int32_t waves);       \
+  hipError_t launch_blk_fused_fwd_##OM(const BlkPack& p, const BlkFwdArgs& a, hipStream_t s);
 PMLP_BLK_FWD_DECL(2)
-PMLP_BLK_FWD_DECL(4)
-PMLP_BLK_FWD_DECL(8)
+PMLP_BLK_FWD_DECL(16)
 #undef PMLP_BLK_FWD_DECL
 
 // Per piece and sample, planar: part[(piece * PQ + q) * Bp + b], q < O the sums

@@ -59,6 +59,143 @@ __device__ __forceinline__ void blk_acts(int a, const float (&z)[NV], float (&v)
   }
 }
 
+// ---------------------------------------------------------------------------
+// The samples' three bf16 pieces in LDS, sample by sample, for both fused kernels.
+// ---------------------------------------------------------------------------
+
+// Row bytes of the pieces of 32 NC columns and up to eight more: 16 bytes times an
+// odd number, which spreads 16 rows over all banks.
+__host__ __device__ constexpr int row_bytes(int NC) { return 16 * (4 * NC + 1); }
+
+// LDS of SC samples: three planes, and what a transposing load of the last row's
+// columns may pass them by
+inline size_t pieces_bytes(int NC, int SC) { return (size_t)3 * SC * row_bytes(NC) + 32; }
+
+// The pieces of the SC samples from b0 on (zero past the batch and the columns).
+template <int NC>
+__device__ __forceinline__ void fill_pieces(char* lds, int SC, const float* X, int b0, int B,
+                                            int F, int tid, int threads) {
+  constexpr int RB = row_bytes(NC), QR = RB / 8;  // quads of a row
+  const int plane = SC * RB;
+  for (int q = tid; q < SC * QR; q += threads) {
+    const int s = q / QR, k = 4 * (q - s * QR), b = b0 + s;
+    const float* xr = X + (int64_t)(b < B ? b : B - 1) * F;
+    f32x2 x[2];
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = xr[k + e < F ? k + e : F - 1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float w = opaque(v[e]);
+      x[e >> 1][e & 1] = k + e < F && b < B ? w : 0.f;
+    }
+    uint32_t p0[2], p1[2], p2[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      p0[e] = bf16_pair(x[e]);
+      const f32x2 r1 = x[e] - bf16_pair_value(p0[e]);
+      p1[e] = bf16_pair(r1);
+      p2[e] = bf16_pair(r1 - bf16_pair_value(p1[e]));
+    }
+    char* d = lds + s * RB + 2 * k;
+    *(uint2*)d = make_uint2(p0[0], p0[1]);
+    *(uint2*)(d + plane) = make_uint2(p1[0], p1[1]);
+    *(uint2*)(d + 2 * plane) = make_uint2(p2[0], p2[1]);
+  }
+}
+
+// A unit's row of W1 and V1: the pieces of 32 NC columns and RM fp32 columns, as the
+// lane (row li, columns 8 lk ..) holds them for a product's operand.
+template <int NC, int RM, int K>
+struct UnitRows {
+  static constexpr int NCA = NC > 0 ? NC : 1, RMA = RM > 0 ? RM : 1;
+  bf16x8 p[K][NCA][3];
+  float t[K][RMA];
+  __device__ __forceinline__ void load(const BlkPack& pk, int64_t n, int lk, int rem) {
+    const int F4 = pk.F4;
+#pragma unroll
+    for (int mt = 0; mt < K; ++mt) {
+      const float* row = (mt ? pk.V1 : pk.W1) + n * F4;
+      f32x4 w[2 * NCA];
+#pragma unroll
+      for (int e = 0; e < 2 * NC; ++e) {
+        const int k = 32 * (e >> 1) + 8 * lk + 4 * (e & 1);
+        w[e] = *(const f32x4*)(row + (k < F4 ? k : F4 - 4));
+      }
+#pragma unroll
+      for (int q = 0; q < RM; ++q) t[mt][q] = row[q < rem ? 32 * NC + 4 * q + lk : 0];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        f32x4 q[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          q[e] = opaque(w[2 * c + e]);
+          if (32 * c + 8 * lk + 4 * e >= F4) q[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        split3(q[0], q[1], p[mt][c][0], p[mt][c][1], p[mt][c][2]);
+      }
+    }
+  }
+};
+
+// Z and U of 16 units and the 32 samples whose pieces start at `at` (this lane's row):
+// UNITS_FIRST: lane (li, lk) ends with units 4 lk + r of sample li, else with samples
+// 4 lk + r of unit li; z[mt][i] of the samples' block i.  xat: its fp32 columns.
+template <int NC, int RM, int K, bool UNITS_FIRST>
+__device__ __forceinline__ void unit_products(const UnitRows<NC, RM, K>& w, const char* at,
+                                              const char* xat, int plane, int rem,
+                                              f32x4 (&z)[K][2]) {
+  constexpr int RB = row_bytes(NC);
+#pragma unroll
+  for (int mt = 0; mt < K; ++mt)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) z[mt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    bf16x8 x[2][3];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 3; ++e) x[i][e] = *(const bf16x8*)(at + e * plane + (16 * i * RB + 64 * c));
+    // the piece products smallest first, blocks and projections in turn
+#define PMLP_PIECE(E, Q)                                                                   \
+_Pragma("unroll") for (int mt = 0; mt < K; ++mt) _Pragma("unroll") for (int i = 0; i < 2; ++i) \
+    z[mt][i] = UNITS_FIRST                                                                 \
+                   ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.p[mt][c][Q], x[i][E], z[mt][i], 0, 0, 0) \
+                   : __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i][E], w.p[mt][c][Q], z[mt][i], 0, 0, 0)
+    PMLP_PIECE(2, 0);
+    PMLP_PIECE(1, 1);
+    PMLP_PIECE(0, 2);
+    PMLP_PIECE(1, 0);
+    PMLP_PIECE(0, 1);
+    PMLP_PIECE(0, 0);
+#undef PMLP_PIECE
+  }
+#pragma unroll
+  for (int q = 0; q < RM; ++q)
+    if (q < rem) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float x = 0.f;  // the column again, exactly: the sum of its pieces
+#pragma unroll
+        for (int e = 2; e >= 0; --e)
+          x += bf16_bits_to_f32(*(const unsigned short*)(xat + e * plane + (16 * i * RB + 8 * q)));
+#pragma unroll
+        for (int mt = 0; mt < K; ++mt)
+          z[mt][i] = UNITS_FIRST
+                         ? __builtin_amdgcn_mfma_f32_16x16x4f32(w.t[mt][q], x, z[mt][i], 0, 0, 0)
+                         : __builtin_amdgcn_mfma_f32_16x16x4f32(x, w.t[mt][q], z[mt][i], 0, 0, 0);
+      }
+    }
+}
+
+// The instance for F4 columns: NC chunks of 32 in three-piece products and up to two
+// fp32 steps of four (odd numbers), or else a last chunk that is padded.
+inline int blk_shape(int F4) {
+  const int c = F4 / 32, r = F4 % 32 / 4;
+  return r == 0 ? 2 * c : r <= 2 ? 2 * c + 1 : 2 * c + 2;
+}
+
 // The gradients of unit n's output weights, gain and shift from T_o, stored or
 // applied.  w: its output weights.
 template <int OM, bool NORM>

@@ -111,132 +111,207 @@ __global__ __launch_bounds__(kBlock) void k_blk_fwd(BlkPack p, const float* __re
   }
 }
 
-// C_o and D_o of model m, summed by the 64 lanes of a wave.
+// C_o and D_o of model m, summed by the waves of a workgroup (wave of nw) through
+// `red`, or by one wave for itself (nw = 1).
 template <int OM>
-__device__ __forceinline__ void norm_consts(const BlkPack& p, int m, int lane, float (&C)[OM],
-                                            float (&D)[OM]) {
+__device__ __forceinline__ void norm_consts(const BlkPack& p, int m, int lane, int wave, int nw,
+                                            float (*red)[2 * OM], float (&C)[OM], float (&D)[OM]) {
 #pragma unroll
   for (int o = 0; o < OM; ++o) C[o] = D[o] = 0.f;
   const int64_t e = p.seg_off[m + 1];
-  for (int64_t n0 = p.seg_off[m]; n0 < e; n0 += 256) {  // (four units' loads in flight)
+  for (int64_t n0 = p.seg_off[m] + 64 * wave; n0 < e; n0 += 128 * nw) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int64_t k = n0 + 64 * u + lane, n = k < e ? k : e - 1;
-      const float gn = k < e ? p.gain[n] : 0.f, sn = k < e ? p.shift[n] : 0.f;
+    for (int u = 0; u < 2; ++u) {  // (two units' loads in flight)
+      const int64_t k = n0 + 64 * nw * u + lane, n = k < e ? k : e - 1;
+      const float gn = p.gain[n], sn = p.shift[n];
 #pragma unroll
       for (int o = 0; o < OM; ++o) {
         const float w = p.W2[(int64_t)(o < p.O ? o : 0) * p.ldw + n];
-        C[o] = fmaf(gn, w, C[o]);
-        D[o] = fmaf(sn, w, D[o]);
+        C[o] = fmaf(k < e ? gn : 0.f, w, C[o]);
+        D[o] = fmaf(k < e ? sn : 0.f, w, D[o]);
       }
     }
   }
 #pragma unroll
-  for (int s = 32; s > 0; s >>= 1)
+  for (int o = 0; o < OM; ++o) {
+    C[o] = group_sum_to_last(C[o], 64);
+    D[o] = group_sum_to_last(D[o], 64);
+  }
+  if (nw == 1) {
 #pragma unroll
     for (int o = 0; o < OM; ++o) {
-      C[o] += __shfl_xor(C[o], s);
-      D[o] += __shfl_xor(D[o], s);
+      C[o] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(C[o]), 63));
+      D[o] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(D[o]), 63));
     }
+    return;
+  }
+  if (lane == 63) {
+#pragma unroll
+    for (int o = 0; o < OM; ++o) {
+      red[wave][o] = C[o];
+      red[wave][OM + o] = D[o];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int o = 0; o < OM; ++o) {
+    C[o] = D[o] = 0.f;
+    for (int w = 0; w < nw; ++w) {
+      C[o] += red[w][o];
+      D[o] += red[w][OM + o];
+    }
+  }
+  __syncthreads();
 }
 
-// The sums of model m and sample b over its pieces: with a norm P_o and the
-// statistics (mu, r), else the logits.  r = 0 for a model of one unit, whose norm
-// is constant, so that its gradient is exactly zero.
+// A model's sums for one sample over some of its pieces.
+template <int OM>
+struct Merged {
+  float P[OM], n, mean, m2;
+};
+
+// Those of pieces k0 + g, k0 + g + G, .. of model m, four pieces' loads in flight.
 template <int OM, bool NORM>
 __device__ __forceinline__ void merge_pieces(const BlkPack& p, const BlkMap& map,
-                                             const float* __restrict__ part, int m,
-                                             int Bp, int b, const float (&C)[OM], float (&P)[OM],
-                                             float* mu, float* r) {
-  float n = 0.f, mean = 0.f, m2 = 0.f;
+                                             const float* __restrict__ part, int m, int Br, int b,
+                                             int g, int G, Merged<OM>& s) {
+  s.n = s.mean = s.m2 = 0.f;
 #pragma unroll
-  for (int o = 0; o < OM; ++o) P[o] = 0.f;
-  int k0, k1, tf = 0;
-  if (map.toff) {
-    tf = map.toff[m];
-    k0 = m + (int)(((int64_t)(tf + 1) * map.W - 1) / map.T);
-    k1 = m + (int)(((int64_t)map.toff[m + 1] * map.W - 1) / map.T) + 1;
-  } else {
-    k0 = p.poff[m];
-    k1 = p.poff[m + 1];
-  }
-  for (int k = k0; k < k1; ++k) {
-    const float* src = part + (int64_t)k * (p.O + (NORM ? 2 : 0)) * Bp + b;
+  for (int o = 0; o < OM; ++o) s.P[o] = 0.f;
+  const int k0 = (map.toff ? map.toff : p.poff)[m], k1 = (map.toff ? map.toff : p.poff)[m + 1];
+  const int width = (int)(p.seg_off[m + 1] - p.seg_off[m]);
+  constexpr int U = OM <= 4 ? 4 : 2;
+  for (int k = k0 + g; k < k1; k += U * G) {
+    float v[U][OM], mb[U], qb[U];
 #pragma unroll
-    for (int o = 0; o < OM; ++o)
-      if (o < p.O) P[o] += src[(int64_t)o * Bp];
-    if (NORM) {
-      int units;
-      if (map.toff) {  // of the tiles of m in workgroup k - m
-        const int a = (int)((int64_t)(k - m) * map.T / map.W) - tf;
-        const int e = (int)((int64_t)(k - m + 1) * map.T / map.W) - tf;
-        const int h = (int)(p.seg_off[m + 1] - p.seg_off[m]);
-        units = min(h, 16 * e) - max(0, 16 * a);
-      } else {
-        units = p.pieces[k].len;
+    for (int u = 0; u < U; ++u) {  // (past the last: it again, not used)
+      const int ku = k + u * G < k1 ? k + u * G : k1 - 1;
+      const float* src = part + (int64_t)ku * (p.O + (NORM ? 2 : 0)) * Br + b;
+#pragma unroll
+      for (int o = 0; o < OM; ++o) v[u][o] = src[(int64_t)(o < p.O ? o : 0) * Br];
+      if (NORM) {
+        mb[u] = src[(int64_t)p.O * Br];
+        qb[u] = src[(int64_t)(p.O + 1) * Br];
       }
-      merge_stats(n, mean, m2, (float)units, src[(int64_t)p.O * Bp],
-                  src[(int64_t)(p.O + 1) * Bp]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (k + u * G >= k1) break;
+#pragma unroll
+      for (int o = 0; o < OM; ++o) s.P[o] += v[u][o];
+      if (NORM) {
+        const int ku = k + u * G;
+        const int units = map.toff ? min(16, width - 16 * (ku - k0)) : p.pieces[ku].len;
+        merge_stats(s.n, s.mean, s.m2, (float)units, mb[u], qb[u]);
+      }
     }
   }
-  if (NORM) {
-    const float rr = n > 1.f ? 1.f / sqrtf(m2 / n + kNormEps) : 0.f;
-#pragma unroll
-    for (int o = 0; o < OM; ++o) P[o] = rr * (P[o] - mean * C[o]);
-    *mu = mean;
-    *r = rr;
-  }
 }
 
+// The groups g of a workgroup (G of them, nb threads each) merge what each has for
+// the same sample, in the order of g; group 0 ends with the whole.
 template <int OM, bool NORM>
-__global__ __launch_bounds__(kBlock) void k_blk_out(BlkPack p, BlkMap map, const float* __restrict__ part,
-                                                    int Bp, int B, int per, int nblk,
-                                                    float* __restrict__ out, int64_t sm,
-                                                    int64_t sb) {
-  const int lane = threadIdx.x & 63;
-  const int64_t wv = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int m = (int)(wv / nblk);
+__device__ __forceinline__ void merge_groups(Merged<OM>& s, int g, int G, int nb, int l,
+                                             float* lds) {
+  if (G == 1) return;
+  constexpr int W = OM + 3;
+  if (g > 0) {
+    float* d = lds + (size_t)(g - 1) * W * nb + l;
+#pragma unroll
+    for (int o = 0; o < OM; ++o) d[o * nb] = s.P[o];
+    d[OM * nb] = s.n;
+    d[(OM + 1) * nb] = s.mean;
+    d[(OM + 2) * nb] = s.m2;
+  }
+  __syncthreads();
+  if (g == 0) {
+    for (int k = 0; k < G - 1; ++k) {
+      const float* d = lds + (size_t)k * W * nb + l;
+#pragma unroll
+      for (int o = 0; o < OM; ++o) s.P[o] += d[o * nb];
+      if (NORM) merge_stats(s.n, s.mean, s.m2, d[OM * nb], d[(OM + 1) * nb], d[(OM + 2) * nb]);
+    }
+  }
+  __syncthreads();
+}
+
+// With a norm: the statistics, and P_o.  r = 0 for a model of one unit, whose norm is
+// constant, so that its gradient is exactly zero.
+template <int OM>
+__device__ __forceinline__ void apply_norm(Merged<OM>& s, const float (&C)[OM], float* r) {
+  *r = s.n > 1.f ? 1.f / sqrtf(s.m2 / s.n + kNormEps) : 0.f;
+#pragma unroll
+  for (int o = 0; o < OM; ++o) s.P[o] = *r * (s.P[o] - s.mean * C[o]);
+}
+
+// One workgroup for nb samples of a model, G groups of threads over its pieces, or
+// (nb = 64, G = 1, alone) one wave.
+template <int OM, bool NORM>
+__global__ __launch_bounds__(1024) void k_blk_out(BlkPack p, BlkMap map,
+                                                  const float* __restrict__ part, int Br, int B,
+                                                  int per, int nblk, int G, int alone,
+                                                  float* __restrict__ out, int64_t sm, int64_t sb) {
+  extern __shared__ float lds[];
+  __shared__ float red[16][2 * OM];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
+  const int64_t wk = alone ? (int64_t)blockIdx.x * nw + wave : blockIdx.x;
+  const int m = (int)(wk / nblk);
   if (m >= p.M) return;
-  const int b0 = (int)(wv - (int64_t)m * nblk) * per;
+  const int b0 = (int)(wk - (int64_t)m * nblk) * per;
+  const int nb = alone ? 64 : blockDim.x / G, g = alone ? 0 : tid / nb, l = alone ? lane : tid - g * nb;
   float C[OM], D[OM];
-  if (NORM) norm_consts<OM>(p, m, lane, C, D);
-  for (int b = b0 + lane; b < B && b < b0 + per; b += 64) {
-    float P[OM], mu, r;
-    merge_pieces<OM, NORM>(p, map, part, m, Bp, b, C, P, &mu, &r);
+  if (NORM) norm_consts<OM>(p, m, lane, alone ? 0 : wave, alone ? 1 : nw, red, C, D);
+  for (int s0 = b0; s0 < B && s0 < b0 + per; s0 += nb) {
+    const int b = s0 + l < B ? s0 + l : B - 1;
+    Merged<OM> s;
+    merge_pieces<OM, NORM>(p, map, part, m, Br, b, g, G, s);
+    merge_groups<OM, NORM>(s, g, G, nb, l, lds);
+    if (g > 0 || s0 + l >= B) continue;
+    float r;
+    if (NORM) apply_norm<OM>(s, C, &r);
 #pragma unroll
     for (int o = 0; o < OM; ++o)
-      if (o < p.O) out[(int64_t)b * sb + (int64_t)m * sm + o] = NORM ? P[o] + D[o] : P[o];
+      if (o < p.O) out[(int64_t)b * sb + (int64_t)m * sm + o] = NORM ? s.P[o] + D[o] : s.P[o];
   }
 }
 
-// One workgroup per model, its threads over the samples.
+// One workgroup per model, its threads over the samples and (G groups) its pieces.
 template <int OM, bool NORM>
 __global__ __launch_bounds__(1024) void k_blk_loss(BlkPack p, BlkMap map,
                                                    const float* __restrict__ part, int Br, int Bp,
-                                                   BlkLoss l, float scale) {
-  __shared__ float red[16][OM + 1];
-  const int m = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+                                                   int G, BlkLoss l, float scale) {
+  extern __shared__ float lds[];
+  __shared__ float red[16][2 * OM + 1];
+  const int m = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
+  const int nb = blockDim.x / G, g = tid / nb, at = tid - g * nb;
   const int B = l.B;
   float C[OM], D[OM];
-  if (NORM) norm_consts<OM>(p, m, lane, C, D);
+  if (NORM) norm_consts<OM>(p, m, lane, wave, nw, (float(*)[2 * OM])red, C, D);
   const float rh = 1.f / (float)(p.seg_off[m + 1] - p.seg_off[m]);
   if (l.lrm && tid == 0 && !isfinite(l.lrm[m])) l.flag[1] = 1;
   float loss = 0.f, gs[OM];
 #pragma unroll
   for (int o = 0; o < OM; ++o) gs[o] = 0.f;
-  for (int b = tid; b < Bp; b += blockDim.x) {
-    float G[OM], P[OM], mu = 0.f, r = 0.f, a1 = 0.f, a2 = 0.f;
+  for (int s0 = 0; s0 < Bp; s0 += nb) {
+    const int b = s0 + at;
+    float Gr[OM], r = 0.f, a1 = 0.f, a2 = 0.f;
+    Merged<OM> s;
+    merge_pieces<OM, NORM>(p, map, part, m, Br, b < B ? b : B - 1, g, G, s);
+    merge_groups<OM, NORM>(s, g, G, nb, at, lds);
+    if (g > 0 || b >= Bp) continue;
     if (b < B) {
-      merge_pieces<OM, NORM>(p, map, part, m, Br, b, C, P, &mu, &r);
+      if (NORM) apply_norm<OM>(s, C, &r);
       float L[OM];
 #pragma unroll
-      for (int o = 0; o < OM; ++o) L[o] = NORM ? P[o] + D[o] : P[o];
+      for (int o = 0; o < OM; ++o) L[o] = NORM ? s.P[o] + D[o] : s.P[o];
       if (l.Y) {
 #pragma unroll
         for (int o = 0; o < OM; ++o) {
           const float d = o < p.O ? L[o] - l.Y[(int64_t)b * p.O + (o < p.O ? o : 0)] : 0.f;
           loss = fmaf(d, d, loss);
-          G[o] = 2.f * d * scale;
+          Gr[o] = 2.f * d * scale;
         }
       } else {
         float mx = -INFINITY, se = 0.f, ly = 0.f;
@@ -251,44 +326,42 @@ __global__ __launch_bounds__(1024) void k_blk_loss(BlkPack p, BlkMap map,
 #pragma unroll
         for (int o = 0; o < OM; ++o) {
           if (o == yb) ly = L[o];
-          G[o] = o < p.O ? (expf(L[o] - lse) - (o == yb ? 1.f : 0.f)) * scale : 0.f;
+          Gr[o] = o < p.O ? (expf(L[o] - lse) - (o == yb ? 1.f : 0.f)) * scale : 0.f;
         }
         loss += lse - ly;
       }
       if (NORM) {
 #pragma unroll
         for (int o = 0; o < OM; ++o) {
-          gs[o] += G[o];
-          a1 = fmaf(G[o], C[o], a1);
-          a2 = fmaf(G[o], P[o], a2);
+          gs[o] += Gr[o];
+          a1 = fmaf(Gr[o], C[o], a1);
+          a2 = fmaf(Gr[o], s.P[o], a2);
         }
       }
     } else {
+      s.mean = 0.f;
 #pragma unroll
-      for (int o = 0; o < OM; ++o) G[o] = 0.f;
+      for (int o = 0; o < OM; ++o) Gr[o] = 0.f;
     }
     float* row = l.G + ((int64_t)m * Bp + b) * OM;
 #pragma unroll
-    for (int o = 0; o < OM; o += 2) *(f32x2*)(row + o) = f32x2{G[o], G[o + 1]};
-    if (NORM) *(f32x4*)(l.R + ((int64_t)m * Bp + b) * 4) = f32x4{mu, r, a1 * rh, a2 * rh};
+    for (int o = 0; o < OM; o += 2) *(f32x2*)(row + o) = f32x2{Gr[o], Gr[o + 1]};
+    if (NORM) *(f32x4*)(l.R + ((int64_t)m * Bp + b) * 4) = f32x4{s.mean, r, a1 * rh, a2 * rh};
   }
+  loss = group_sum_to_last(loss, 64);
+  if (NORM)
 #pragma unroll
-  for (int s = 32; s > 0; s >>= 1) {
-    loss += __shfl_xor(loss, s);
-    if (NORM)
-#pragma unroll
-      for (int o = 0; o < OM; ++o) gs[o] += __shfl_xor(gs[o], s);
-  }
-  if (lane == 0) {
-    red[wave][OM] = loss;
+    for (int o = 0; o < OM; ++o) gs[o] = group_sum_to_last(gs[o], 64);
+  __syncthreads();
+  if (lane == 63) {
+    red[wave][2 * OM] = loss;
 #pragma unroll
     for (int o = 0; o < OM; ++o) red[wave][o] = gs[o];
   }
   __syncthreads();
-  const int nw = blockDim.x >> 6;
   if (tid == 0) {
     float s = 0.f;
-    for (int w = 0; w < nw; ++w) s += red[w][OM];
+    for (int w = 0; w < nw; ++w) s += red[w][2 * OM];
     l.loss[m] = s * scale;
     if (!isfinite(s)) atomicAdd(l.flag + 2, 1);
   }
@@ -404,19 +477,36 @@ hipError_t launch_blk_fwd(const BlkPack& p, const float* Zt, const float* Ut, in
   return hipGetLastError();
 }
 
-hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, const float* part, int32_t Bp,
+// Groups of threads over a model's pieces: by the pieces of an average model.
+static int piece_groups(const BlkPack& p, const BlkMap& map, int most) {
+  const int64_t pieces = (map.toff ? map.pieces : p.npieces) / p.M;
+  int G = 1;
+  while (G < most && pieces >= 8 * G) G <<= 1;
+  return G;
+}
+
+static size_t groups_lds(const BlkPack& p, int G, int nb) {
+  return (size_t)(G - 1) * nb * (blk_om(p.O) + 3) * sizeof(float);
+}
+
+hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, const float* part, int32_t Br,
                           int32_t B, float* out, int64_t sm, int64_t sb, hipStream_t s) {
   note_variant("k_blk_out", kArithNone);
-  int per = 1024;  // samples of a model per wave: fewer where that leaves the device idle
-  while (per > 64 && (int64_t)p.M * ceil_div_i(B, per) < 8192) per >>= 1;
-  const int nblk = ceil_div_i(B, per);
-  const int64_t waves = (int64_t)p.M * nblk;
-  if (waves > (int64_t)0x3fffffff) return hipErrorInvalidValue;
-  const unsigned grid = (unsigned)ceil_div_i(waves, 4);
-#define PMLP_CALL(OM)                                                                           \
-  do {                                                                                          \
-    if (p.gain) k_blk_out<OM, true><<<grid, kBlock, 0, s>>>(p, map, part, Bp, B, per, nblk, out, sm, sb);  \
-    else k_blk_out<OM, false><<<grid, kBlock, 0, s>>>(p, map, part, Bp, B, per, nblk, out, sm, sb);        \
+  const int G = piece_groups(p, map, 8), alone = G == 1, nb = 64;
+  int per = 1024;  // samples of a model at once: fewer where that leaves the device idle
+  while (per > nb && (int64_t)p.M * ceil_div_i(B, per) < (alone ? 8192 : 1024)) per >>= 1;
+  const int nblk = ceil_div_i(B, per), threads = alone ? 256 : nb * G;
+  const int64_t grid = alone ? ((int64_t)p.M * nblk + 3) / 4 : (int64_t)p.M * nblk;
+  if (grid > (int64_t)0x7fffffff) return hipErrorInvalidValue;
+  const size_t lds = groups_lds(p, G, nb);
+#define PMLP_CALL(OM)                                                                          \
+  do {                                                                                         \
+    if (p.gain)                                                                                \
+      k_blk_out<OM, true><<<(unsigned)grid, threads, lds, s>>>(p, map, part, Br, B, per, nblk, G, \
+                                                               alone, out, sm, sb);             \
+    else                                                                                       \
+      k_blk_out<OM, false><<<(unsigned)grid, threads, lds, s>>>(p, map, part, Br, B, per, nblk, \
+                                                                G, alone, out, sm, sb);         \
   } while (0)
   PMLP_BLK_OM(p.O, PMLP_CALL);
 #undef PMLP_CALL
@@ -426,12 +516,17 @@ hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, const float* part
 hipError_t launch_blk_loss(const BlkPack& p, const BlkMap& map, const float* part, int32_t Br,
                            int32_t Bp, const BlkLoss& l, hipStream_t s) {
   note_variant("k_blk_loss", kArithNone);
-  const int threads = Bp >= 1024 ? 1024 : (Bp + 63) & ~63;
+  const int nb = Bp >= 256 ? 256 : (Bp + 63) & ~63;
+  const int most = 1024 / nb, G = piece_groups(p, map, most >= 8 ? 8 : most >= 4 ? 4 : most >= 2 ? 2 : 1);
+  const int threads = G == 1 && Bp >= 1024 ? 1024 : nb * G;
+  const size_t lds = groups_lds(p, G, threads / G);
   const float scale = l.Y ? 1.f / ((float)l.B * (float)p.O) : 1.f / (float)l.B;
-#define PMLP_CALL(OM)                                                                  \
-  do {                                                                                 \
-    if (p.gain) k_blk_loss<OM, true><<<(unsigned)p.M, threads, 0, s>>>(p, map, part, Br, Bp, l, scale);  \
-    else k_blk_loss<OM, false><<<(unsigned)p.M, threads, 0, s>>>(p, map, part, Br, Bp, l, scale);        \
+#define PMLP_CALL(OM)                                                                              \
+  do {                                                                                             \
+    if (p.gain)                                                                                    \
+      k_blk_loss<OM, true><<<(unsigned)p.M, threads, lds, s>>>(p, map, part, Br, Bp, G, l, scale);  \
+    else                                                                                           \
+      k_blk_loss<OM, false><<<(unsigned)p.M, threads, lds, s>>>(p, map, part, Br, Bp, G, l, scale); \
   } while (0)
   PMLP_BLK_OM(p.O, PMLP_CALL);
 #undef PMLP_CALL

@@ -14,8 +14,9 @@
 // samples run in that order in both of its operands).
 // The norm's gradient needs no sums over units (see k_block.hip).
 //
-// Rows of the pieces are 16 NF columns and eight of padding: 16 bytes times an odd
-// number, which spreads 16 rows over all banks.
+// The second product takes NF = 2 NC blocks of 16 columns, and one more for the fp32
+// columns of the first; the last block may read past its columns into the next row,
+// for columns that no one stores.
 
 #include "block_device.h"
 
@@ -35,13 +36,6 @@ constexpr int NO = MF ? 4 : OM;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
-
-// row bytes of the pieces
-__host__ __device__ constexpr int row_bytes(int NF) { return 32 * NF + 16; }
-
-// LDS of SC samples: three planes, 16 bytes of zeros, and what a transposing load of
-// the last rows' columns may pass them by
-constexpr size_t lds_bytes(int NF, int SC) { return (size_t)3 * SC * row_bytes(NF) + 64; }
 
 // Values and slopes of activation id A.
 template <int NV>
@@ -80,55 +74,26 @@ __device__ __forceinline__ void mixed_act_and_slope(int arow, const float (&z)[N
   }
 }
 
-template <int NF, bool GATED, bool NORM>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(NF <= 2 ? 3 : 2)))
+template <int NC, int RM, bool GATED, bool NORM>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(NC <= 1 && !MF ? 3 : 2)))
 void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
-  constexpr int NC = (NF + 1) / 2, K = GATED ? 2 : 1, RB = row_bytes(NF);
+  constexpr int NF = 2 * NC + (RM ? 1 : 0), K = GATED ? 2 : 1, RB = row_bytes(NC);
+
   extern __shared__ __align__(16) char lds[];
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
   const int F = a.F, F4 = p.F4, SC = a.SC, plane = SC * RB;
   const int ntiles = (int)((p.N + 15) >> 4);
   const int rounds = (ntiles + gridDim.x * nw - 1) / (gridDim.x * nw);
-  const int zeros = 3 * plane;  // of 16 bytes
-  if (tid < 16) ((int*)(lds + zeros))[tid] = 0;
+  const int rem = RM ? (F4 - 32 * NC) >> 2 : 0;
 
-  // the pieces of SC samples from b0 on (zero past the batch and the columns)
-  auto fill = [&](int b0) {
-    constexpr int QR = 4 * NF;  // quads of a row
-    for (int q = tid; q < SC * QR; q += blockDim.x) {
-      const int s = q / QR, k = 4 * (q - s * QR), b = b0 + s;
-      const float* xr = a.X + (int64_t)(b < a.B ? b : a.B - 1) * F;
-      f32x2 x[2];
-      float v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = xr[k + e < F ? k + e : F - 1];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float w = opaque(v[e]);
-        x[e >> 1][e & 1] = k + e < F && b < a.B ? w : 0.f;
-      }
-      uint32_t p0[2], p1[2], p2[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        p0[e] = bf16_pair(x[e]);
-        const f32x2 r1 = x[e] - bf16_pair_value(p0[e]);
-        p1[e] = bf16_pair(r1);
-        p2[e] = bf16_pair(r1 - bf16_pair_value(p1[e]));
-      }
-      char* d = lds + s * RB + 2 * k;
-      *(uint2*)d = make_uint2(p0[0], p0[1]);
-      *(uint2*)(d + plane) = make_uint2(p1[0], p1[1]);
-      *(uint2*)(d + 2 * plane) = make_uint2(p2[0], p2[1]);
-    }
-  };
   const int nchunk = (a.Bp + SC - 1) / SC;
   if (nchunk == 1) {
-    fill(0);
+    fill_pieces<NC>(lds, SC, a.X, 0, a.B, F, tid, blockDim.x);
     lds_barrier();
   }
   // this lane's places in the pieces: a row of the first product, and of the second
-  const int zrow = li * RB + 16 * lk;
+  const int zrow = li * RB + 16 * lk, xrow = li * RB + 64 * NC + 2 * lk;
   const int trow = (4 * lk + (li >> 2)) * RB + 8 * (li & 3);
 
 #pragma unroll 1
@@ -151,27 +116,8 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
       T[o] = 0.f;
     }
     const int m_lo = __builtin_amdgcn_readfirstlane(m), m_hi = __builtin_amdgcn_readlane(m, 15);
-    bf16x8 wp[K][NC][3];
-#pragma unroll
-    for (int mt = 0; mt < K; ++mt) {
-      const float* row = (mt ? p.V1 : p.W1) + n * F4;
-      f32x4 w[2 * NC];
-#pragma unroll
-      for (int e = 0; e < 2 * NC; ++e) {
-        const int k = 32 * (e >> 1) + 8 * lk + 4 * (e & 1);
-        w[e] = *(const f32x4*)(row + (k < F4 ? k : F4 - 4));
-      }
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        f32x4 q[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          q[e] = opaque(w[2 * c + e]);
-          if (32 * c + 8 * lk + 4 * e >= F4) q[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-        split3(q[0], q[1], wp[mt][c][0], wp[mt][c][1], wp[mt][c][2]);
-      }
-    }
+    UnitRows<NC, RM, K> w;
+    w.load(p, n, lk, rem);
     const float* const Gm = a.G + (int64_t)m * a.Bp * OM;
     const float* const Rm = a.R + (int64_t)m * a.Bp * 4;
     f32x4 acc[K][NF];
@@ -184,7 +130,7 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
     for (int b0 = 0; b0 < a.Bp; b0 += SC) {
       if (nchunk > 1) {
         lds_barrier();
-        fill(b0);
+        fill_pieces<NC>(lds, SC, a.X, b0, a.B, F, tid, blockDim.x);
         lds_barrier();
       }
       if (!live) continue;
@@ -194,34 +140,7 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
         const int s = 32 * st;
         // ---- Z (and U) of 32 samples ------------------------------------------
         f32x4 z[K][2];
-#pragma unroll
-        for (int mt = 0; mt < K; ++mt)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) z[mt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          bf16x8 x[2][3];
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e = 0; e < 3; ++e) {
-              int at = e * plane + (s + 16 * i) * RB + zrow + 64 * c;
-              // (half of an odd last chunk is past the row)
-              if ((NF & 1) && c == NC - 1) at = lk < 2 ? at : zeros;
-              x[i][e] = *(const bf16x8*)(lds + at);
-            }
-#define PMLP_PIECE(E, Q)                                            \
-_Pragma("unroll") for (int mt = 0; mt < K; ++mt)                    \
-_Pragma("unroll") for (int i = 0; i < 2; ++i) z[mt][i] =            \
-    __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i][E], wp[mt][c][Q], z[mt][i], 0, 0, 0)
-          PMLP_PIECE(2, 0);
-          PMLP_PIECE(1, 1);
-          PMLP_PIECE(0, 2);
-          PMLP_PIECE(1, 0);
-          PMLP_PIECE(0, 1);
-          PMLP_PIECE(0, 0);
-#undef PMLP_PIECE
-        }
+        unit_products<NC, RM, K, false>(w, lds + s * RB + zrow, lds + s * RB + xrow, plane, rem, z);
         // ---- dZ (and dU) ------------------------------------------------------
         float zv[8], av[8], dv[8];
 #pragma unroll
@@ -384,34 +303,38 @@ _Pragma("unroll") for (int mt = 0; mt < K; ++mt) acc[mt][j] =        \
 
 typedef void (*BlkBwdFn)(BlkPack, BlkBwdArgs);
 
-template <int NF>
-BlkBwdFn bwd_kind(bool gated, bool norm) {
-  if (gated && norm) return k_blk_fused_bwd<NF, true, true>;
-  if (gated) return k_blk_fused_bwd<NF, true, false>;
-  return k_blk_fused_bwd<NF, false, true>;
+struct BlkBwdInst {
+  BlkBwdFn fn;
+  int NC;
+};
+
+template <int NC, int RM>
+BlkBwdInst bwd_kind(bool gated, bool norm) {
+  if (gated && norm) return {k_blk_fused_bwd<NC, RM, true, true>, NC};
+  if (gated) return {k_blk_fused_bwd<NC, RM, true, false>, NC};
+  return {k_blk_fused_bwd<NC, RM, false, true>, NC};
 }
 
-BlkBwdFn bwd_of(const BlkPack& p) {
+BlkBwdInst bwd_of(const BlkPack& p) {
   const bool g = p.V1 != nullptr, n = p.gain != nullptr;
-  switch ((p.F4 + 15) / 16) {
-    case 1: return bwd_kind<1>(g, n);
-    case 2: return bwd_kind<2>(g, n);
-    case 3: return bwd_kind<3>(g, n);
-    case 4: return bwd_kind<4>(g, n);
-    case 5: return bwd_kind<5>(g, n);
-    case 6: return bwd_kind<6>(g, n);
-    case 7: return bwd_kind<7>(g, n);
-    case 8: return bwd_kind<8>(g, n);
-    default: return nullptr;
+  switch (blk_shape(p.F4)) {
+    case 1: return bwd_kind<0, 2>(g, n);
+    case 2: return bwd_kind<1, 0>(g, n);
+    case 3: return bwd_kind<1, 2>(g, n);
+    case 4: return bwd_kind<2, 0>(g, n);
+    case 5: return bwd_kind<2, 2>(g, n);
+    case 6: return bwd_kind<3, 0>(g, n);
+    case 7: return bwd_kind<3, 2>(g, n);
+    case 8: return bwd_kind<4, 0>(g, n);
+    default: return {nullptr, 0};
   }
 }
 
 // Samples a chunk: all of them where they fit in LDS, else the most equal parts.
-int chunk_samples(int NF, int Bp, size_t lds_max) {
-  const int all = (Bp + 31) & ~31;
+int chunk_samples(int NC, int Bp, size_t lds_max) {
   for (int parts = 1;; ++parts) {
-    const int SC = ((all + parts - 1) / parts + 31) & ~31;
-    if (lds_bytes(NF, SC) <= lds_max) return SC;
+    const int SC = ((Bp + parts - 1) / parts + 31) & ~31;
+    if (pieces_bytes(NC, SC) <= lds_max) return SC;
     if (SC == 32) return 0;
   }
 }
@@ -423,17 +346,17 @@ int chunk_samples(int NF, int Bp, size_t lds_max) {
 
 hipError_t PMLP_CAT(launch_blk_fused_bwd_, PMLP_BLK_OM)(const BlkPack& p, BlkBwdArgs a,
                                                         hipStream_t s) {
-  const BlkBwdFn fn = bwd_of(p);
-  const int NF = (p.F4 + 15) / 16;
+  const BlkBwdInst inst = bwd_of(p);
+  const BlkBwdFn fn = inst.fn;
   int dev = 0, lmax = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e == hipSuccess)
     e = hipDeviceGetAttribute(&lmax, hipDeviceAttributeMaxSharedMemoryPerBlock, dev);
   if (e != hipSuccess) return e;
-  a.SC = fn ? chunk_samples(NF, a.Bp, (size_t)lmax) : 0;
+  a.SC = fn ? chunk_samples(inst.NC, a.Bp, (size_t)lmax) : 0;
   if (a.SC <= 0 || a.Bp < 32 || a.Bp % 32 || a.B < 1 || a.B > a.Bp || p.O > OM || p.N < 1)
     return hipErrorInvalidValue;
-  const size_t lds = lds_bytes(NF, a.SC);
+  const size_t lds = pieces_bytes(inst.NC, a.SC);
   const int64_t tiles = (p.N + 15) / 16;
   // eight waves share the samples' pieces where those leave room for one workgroup
   // only, four where there is more

@@ -116,9 +116,11 @@ struct PmlpBlock {
   BlkPiece* d_pieces = nullptr;
   int32_t* d_poff = nullptr;  // [M+1]
   int32_t npieces = 0;
-  BlkTile* d_tiles = nullptr;
-  int32_t* d_toff = nullptr;  // [M+1]
+  BlkTile* d_tiles = nullptr;   // of the forward, by model
+  int32_t* d_toff = nullptr;    // [M+1]
   int32_t ntiles = 0;
+  BlkTile* d_btiles = nullptr;  // of the backward, by activation
+  int32_t nbtiles = 0;
   int32_t planned = 0;  // batch size of `plan` (0: none yet)
   BlkRun plan;
   // Workspace.  A captured graph keeps the addresses it was captured with, so a
@@ -263,6 +265,7 @@ void release(pmlp* h) {
     dfree(k->d_pieces);
     dfree(k->d_poff);
     dfree(k->d_tiles);
+    dfree(k->d_btiles);
     dfree(k->d_toff);
     dfree(k->ws);
     for (unsigned char*& p : k->retired) dfree(p);
@@ -1340,9 +1343,11 @@ void block_pieces(const std::vector<int32_t>& hs, int64_t cap, std::vector<BlkPi
   poff.push_back((int32_t)pieces.size());
 }
 
-// Tiles of the fused kernels: 16 units of a model, the last of it fewer.
+// Tiles of the fused kernels, 16 units each or fewer: of the forward, of one model; of
+// the backward, of one activation (in pools of narrow models a fraction of those).
 void block_tiles(const std::vector<int32_t>& hs, const std::vector<int32_t>& acts,
-                 std::vector<BlkTile>& tiles, std::vector<int32_t>& toff) {
+                 std::vector<BlkTile>& tiles, std::vector<int32_t>& toff,
+                 std::vector<BlkTile>& btiles) {
   int64_t n = 0;
   for (size_t m = 0; m < hs.size(); ++m) {
     toff.push_back((int32_t)tiles.size());
@@ -1351,6 +1356,15 @@ void block_tiles(const std::vector<int32_t>& hs, const std::vector<int32_t>& act
     n += hs[m];
   }
   toff.push_back((int32_t)tiles.size());
+  for (const BlkTile& t : tiles) {
+    for (int32_t at = 0; at < t.cnt;) {
+      if (btiles.empty() || btiles.back().cnt == 16 || btiles.back().act != t.act)
+        btiles.push_back(BlkTile{t.n0 + at, 0, t.m, t.act});
+      const int32_t take = std::min(16 - btiles.back().cnt, t.cnt - at);
+      btiles.back().cnt += take;
+      at += take;
+    }
+  }
 }
 
 BlkPack block_pack(const pmlp* h) {
@@ -1655,7 +1669,7 @@ int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_
           return launch_blk_loss(p, BlkMap{k->d_toff, k->ntiles}, at(oP), Bp, Bp, l, h->stream);
         }))
       return rc;
-    const BlkBwdArgs b{X, B, h->F, Bp, 0, at(oG), at(oR), at(oS), d.dW1, d.dV1, g};
+    const BlkBwdArgs b{X, B, h->F, Bp, 0, k->d_btiles, k->nbtiles, at(oG), at(oR), at(oS), d.dW1, d.dV1, g};
     if (int rc = run(h, KID_BWD_FUSED, [&] { return launch_blk_fused_bwd(p, b, h->stream); }))
       return rc;
     h->have_loss = true;
@@ -2337,17 +2351,18 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
   k->gated = (flags & PMLP_GATED) != 0;
   k->norm = (flags & PMLP_NORM) != 0;
   std::vector<BlkPiece> pieces;
-  std::vector<BlkTile> tiles;
+  std::vector<BlkTile> tiles, btiles;
   std::vector<int32_t> poff, toff;
   try {
     block_pieces(h->hs, tile_cap(h->N), pieces, poff);
-    block_tiles(h->hs, h->acts, tiles, toff);
+    block_tiles(h->hs, h->acts, tiles, toff, btiles);
   } catch (const std::bad_alloc&) {
     pmlp_destroy(h);
     return fail(PMLP_ENOMEM, "host allocation failed");
   }
   k->npieces = (int32_t)pieces.size();
   k->ntiles = (int32_t)tiles.size();
+  k->nbtiles = (int32_t)btiles.size();
   const size_t half = (size_t)h->Npad * h->F4, units = (size_t)h->Npad * sizeof(float);
   float* W = nullptr;
   if ((k->gated && hipMalloc(&W, (2 * half + 64) * sizeof(float)) != hipSuccess) ||
@@ -2356,6 +2371,7 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
       hipMalloc(&k->d_pieces, pieces.size() * sizeof(BlkPiece)) != hipSuccess ||
       hipMalloc(&k->d_poff, poff.size() * sizeof(int32_t)) != hipSuccess ||
       hipMalloc(&k->d_tiles, tiles.size() * sizeof(BlkTile)) != hipSuccess ||
+      hipMalloc(&k->d_btiles, btiles.size() * sizeof(BlkTile)) != hipSuccess ||
       hipMalloc(&k->d_toff, toff.size() * sizeof(int32_t)) != hipSuccess) {
     (void)hipGetLastError();
     dfree(W);
@@ -2378,6 +2394,8 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
     PMLP_HIP(hipMemcpy(k->d_poff, poff.data(), poff.size() * sizeof(int32_t),
                        hipMemcpyHostToDevice));
     PMLP_HIP(hipMemcpy(k->d_tiles, tiles.data(), tiles.size() * sizeof(BlkTile),
+                       hipMemcpyHostToDevice));
+    PMLP_HIP(hipMemcpy(k->d_btiles, btiles.data(), btiles.size() * sizeof(BlkTile),
                        hipMemcpyHostToDevice));
     PMLP_HIP(hipMemcpy(k->d_toff, toff.data(), toff.size() * sizeof(int32_t),
                        hipMemcpyHostToDevice));

@@ -122,6 +122,8 @@ struct BlkBwdArgs {
   const float* X;  // [B][F]
   int32_t B, F, Bp;
   int32_t SC;      // (set by the launcher) samples a chunk
+  const BlkTile* tiles;
+  int32_t ntiles;
   const float *G, *R, *Gs;
   float *dW1, *dV1;
   BlkGrads g;

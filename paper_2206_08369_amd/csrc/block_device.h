@@ -111,7 +111,7 @@ struct UnitRows {
   static constexpr int NCA = NC > 0 ? NC : 1, RMA = RM > 0 ? RM : 1;
   bf16x8 p[K][NCA][3];
   float t[K][RMA];
-  __device__ __forceinline__ void load(const BlkPack& pk, int64_t n, int lk, int rem) {
+  __device__ __forceinline__ void load(const BlkPack& pk, int64_t n, int lk) {
     const int F4 = pk.F4;
 #pragma unroll
     for (int mt = 0; mt < K; ++mt) {
@@ -123,7 +123,7 @@ struct UnitRows {
         w[e] = *(const f32x4*)(row + (k < F4 ? k : F4 - 4));
       }
 #pragma unroll
-      for (int q = 0; q < RM; ++q) t[mt][q] = row[q < rem ? 32 * NC + 4 * q + lk : 0];
+      for (int q = 0; q < RM; ++q) t[mt][q] = row[32 * NC + 4 * q + lk];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         f32x4 q[2];
@@ -143,9 +143,17 @@ struct UnitRows {
 // 4 lk + r of unit li; z[mt][i] of the samples' block i.  xat: its fp32 columns.
 template <int NC, int RM, int K, bool UNITS_FIRST>
 __device__ __forceinline__ void unit_products(const UnitRows<NC, RM, K>& w, const char* at,
-                                              const char* xat, int plane, int rem,
+                                              const char* xat, int plane,
                                               f32x4 (&z)[K][2]) {
   constexpr int RB = row_bytes(NC);
+  unsigned short xp[RM > 0 ? RM : 1][2][3];
+#pragma unroll
+  for (int q = 0; q < RM; ++q)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        xp[q][i][e] = *(const unsigned short*)(xat + e * plane + (16 * i * RB + 8 * q));
 #pragma unroll
   for (int mt = 0; mt < K; ++mt)
 #pragma unroll
@@ -173,28 +181,36 @@ _Pragma("unroll") for (int mt = 0; mt < K; ++mt) _Pragma("unroll") for (int i = 
   }
 #pragma unroll
   for (int q = 0; q < RM; ++q)
-    if (q < rem) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float x = 0.f;  // the column again, exactly: the sum of its pieces
+    for (int i = 0; i < 2; ++i) {  // the column again, exactly: the sum of its pieces
+      const float x = (bf16_bits_to_f32(xp[q][i][2]) + bf16_bits_to_f32(xp[q][i][1])) +
+                      bf16_bits_to_f32(xp[q][i][0]);
 #pragma unroll
-        for (int e = 2; e >= 0; --e)
-          x += bf16_bits_to_f32(*(const unsigned short*)(xat + e * plane + (16 * i * RB + 8 * q)));
-#pragma unroll
-        for (int mt = 0; mt < K; ++mt)
-          z[mt][i] = UNITS_FIRST
-                         ? __builtin_amdgcn_mfma_f32_16x16x4f32(w.t[mt][q], x, z[mt][i], 0, 0, 0)
-                         : __builtin_amdgcn_mfma_f32_16x16x4f32(x, w.t[mt][q], z[mt][i], 0, 0, 0);
-      }
+      for (int mt = 0; mt < K; ++mt)
+        z[mt][i] = UNITS_FIRST
+                       ? __builtin_amdgcn_mfma_f32_16x16x4f32(w.t[mt][q], x, z[mt][i], 0, 0, 0)
+                       : __builtin_amdgcn_mfma_f32_16x16x4f32(x, w.t[mt][q], z[mt][i], 0, 0, 0);
     }
 }
 
-// The instance for F4 columns: NC chunks of 32 in three-piece products and up to two
-// fp32 steps of four (odd numbers), or else a last chunk that is padded.
-inline int blk_shape(int F4) {
-  const int c = F4 / 32, r = F4 % 32 / 4;
-  return r == 0 ? 2 * c : r <= 2 ? 2 * c + 1 : 2 * c + 2;
-}
+// The instance for F4 columns: NC chunks of 32 in three-piece products and RM fp32
+// steps of four, or else a last chunk that is padded.  CALL(NC, RM) returns it.
+#define PMLP_BLK_SHAPE(F4, CALL)                                       \
+  switch ((F4) / 32 * 3 + ((F4) % 32 == 0 ? 0 : (F4) % 32 == 4 ? 1 : (F4) % 32 == 8 ? 2 : 3)) { \
+    case 1: return CALL(0, 1);                                          \
+    case 2: return CALL(0, 2);                                          \
+    case 3: return CALL(1, 0);                                          \
+    case 4: return CALL(1, 1);                                          \
+    case 5: return CALL(1, 2);                                          \
+    case 6: return CALL(2, 0);                                          \
+    case 7: return CALL(2, 1);                                          \
+    case 8: return CALL(2, 2);                                          \
+    case 9: return CALL(3, 0);                                          \
+    case 10: return CALL(3, 1);                                         \
+    case 11: return CALL(3, 2);                                         \
+    case 12: return CALL(4, 0);                                         \
+    default: break;                                                     \
+  }
 
 // The gradients of unit n's output weights, gain and shift from T_o, stored or
 // applied.  w: its output weights.

@@ -1,8 +1,8 @@
 // Block packs: the backward pass in one kernel, for inputs of up to 128 columns.
 // Compiled once per class of outputs (PMLP_BLK_OM: 2, 4 or 16).
 //
-// A wave takes 16 consecutive hidden units (whatever models they belong to) and all
-// samples, so that its weights' gradients need no other wave; it holds the three
+// A wave takes a tile, up to 16 consecutive hidden units of one activation (of whatever
+// models), and all samples, so that its weights' gradients need no other wave; it holds the three
 // bf16 pieces of its units' W1 (and V1) rows and their gradients' accumulators in
 // registers.  The samples' pieces lie in LDS once, sample by sample (chunks of
 // them in turn, where they do not fit), and serve both products: read as rows they
@@ -52,28 +52,6 @@ __device__ __forceinline__ void act_and_slope(int A, const float (&z)[NV], float
   }
 }
 
-// The same for lanes whose units have activations of their own: once per id.
-template <int NV>
-__device__ __forceinline__ void mixed_act_and_slope(int arow, const float (&z)[NV], float (&v)[NV],
-                                                    float (&d)[NV]) {
-  uint64_t left = ~0ull;
-#pragma unroll 1
-  while (left) {
-    const int A = __builtin_amdgcn_readlane(arow, __builtin_ctzll(left));
-    float x[NV], tv[NV], td[NV];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) x[j] = opaque(z[j]);  // (or every id's terms would leave the loop)
-    act_and_slope<NV>(A, x, tv, td);
-    const bool mine = arow == A;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      v[j] = mine ? tv[j] : v[j];
-      d[j] = mine ? td[j] : d[j];
-    }
-    left &= ~__ballot(mine);
-  }
-}
-
 template <int NC, int RM, bool GATED, bool NORM>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(NC <= 1 && !MF ? 3 : 2)))
 void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
@@ -83,9 +61,7 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
   const int F = a.F, F4 = p.F4, SC = a.SC, plane = SC * RB;
-  const int ntiles = (int)((p.N + 15) >> 4);
-  const int rounds = (ntiles + gridDim.x * nw - 1) / (gridDim.x * nw);
-  const int rem = RM ? (F4 - 32 * NC) >> 2 : 0;
+  const int rounds = (a.ntiles + gridDim.x * nw - 1) / (gridDim.x * nw);
 
   const int nchunk = (a.Bp + SC - 1) / SC;
   if (nchunk == 1) {
@@ -99,11 +75,13 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
 #pragma unroll 1
   for (int round = 0; round < rounds; ++round) {
     const int tile = (round * (int)gridDim.x + (int)blockIdx.x) * nw + wave;
-    const bool live = tile < ntiles;
-    const int64_t n0 = (int64_t)(live ? tile : ntiles - 1) * 16;
-    const int64_t n = n0 + li < p.N ? n0 + li : p.N - 1;
-    const int m = p.mid[n], act = p.actn[n];
-    const bool one_act = __all(act == __builtin_amdgcn_readfirstlane(act));
+    const bool live = tile < a.ntiles;
+    const BlkTile q = a.tiles[live ? tile : a.ntiles - 1];
+    const int n0 = __builtin_amdgcn_readfirstlane(q.n0);
+    const int cnt = __builtin_amdgcn_readfirstlane(q.cnt), act = __builtin_amdgcn_readfirstlane(q.act);
+    const int64_t n = n0 + std::min(li, cnt - 1);
+    const int m = p.mid[n];
+    const int m_lo = __builtin_amdgcn_readfirstlane(m), m_hi = __builtin_amdgcn_readlane(m, 15);
     const float gn = NORM ? p.gain[n] : 1.f;
     // Up to four outputs: each lane its unit's weights and sums T_o.  More go through
     // fp32 matrix products, a model at a time: w2[0..3] are then outputs 4 lk + q of
@@ -112,12 +90,12 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
 #pragma unroll
     for (int o = 0; o < NO; ++o) {
       const int ow = MF ? 4 * lk + o : o;
-      w2[o] = ow < p.O ? p.W2[(int64_t)ow * p.ldw + n] : 0.f;
+      const float v = p.W2[(int64_t)(ow < p.O ? ow : 0) * p.ldw + n];
+      w2[o] = ow < p.O ? v : 0.f;
       T[o] = 0.f;
     }
-    const int m_lo = __builtin_amdgcn_readfirstlane(m), m_hi = __builtin_amdgcn_readlane(m, 15);
     UnitRows<NC, RM, K> w;
-    w.load(p, n, lk, rem);
+    w.load(p, n, lk);
     const float* const Gm = a.G + (int64_t)m * a.Bp * OM;
     const float* const Rm = a.R + (int64_t)m * a.Bp * 4;
     f32x4 acc[K][NF];
@@ -139,70 +117,98 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
       for (int st = 0; st < steps; ++st) {
         const int s = 32 * st;
         // ---- Z (and U) of 32 samples ------------------------------------------
-        f32x4 z[K][2];
-        unit_products<NC, RM, K, false>(w, lds + s * RB + zrow, lds + s * RB + xrow, plane, rem, z);
-        // ---- dZ (and dU) ------------------------------------------------------
-        float zv[8], av[8], dv[8];
+        // a block's output gradients and statistics, loaded a block ahead
+        struct Up {
+          f32x4 g[MF ? 2 : OM], r[NORM ? 4 : 1];
+        };
+        auto load_up = [&](int i) {
+          Up u;
+          const uint32_t b = (uint32_t)(b0 + s + 16 * i + 4 * lk);  // first of four samples
+          if (MF) {
+            const float* const g = a.G + (int64_t)m_lo * a.Bp * OM;
+            u.g[0] = *(const f32x4*)(g + (uint32_t)(b0 + s + 16 * i + li) * OM + 4 * lk);
 #pragma unroll
-        for (int v = 0; v < 8; ++v) zv[v] = z[0][v >> 2][v & 3];
-        if (one_act) act_and_slope<8>(__builtin_amdgcn_readfirstlane(act), zv, av, dv);
-        else mixed_act_and_slope<8>(act, zv, av, dv);
+            for (int r = 0; r < 4; ++r) u.g[1][r] = g[(b + r) * OM + li];
+          } else {
+#pragma unroll
+            for (int v = 0; v < NO; ++v) u.g[MF ? 0 : v] = *(const f32x4*)(Gm + b * OM + 4 * v);
+          }
+#pragma unroll
+          for (int r = 0; r < (NORM ? 4 : 0); ++r)
+            u.r[NORM ? r : 0] = *(const f32x4*)(Rm + (b + r) * 4);
+          return u;
+        };
+        auto pin = [&](Up& u) {  // (the loads stay where they are)
+#pragma unroll
+          for (int v = 0; v < (MF ? 2 : OM); ++v) u.g[v] = opaque(u.g[v]);
+#pragma unroll
+          for (int r = 0; r < (NORM ? 4 : 0); ++r) u.r[NORM ? r : 0] = opaque(u.r[NORM ? r : 0]);
+        };
+        Up up = load_up(0);
+        f32x4 z[K][2];
+        unit_products<NC, RM, K, false>(w, lds + s * RB + zrow, lds + s * RB + xrow, plane, z);
+        pin(up);
+        // ---- dZ (and dU) ------------------------------------------------------
         f32x4 dz[K][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const uint32_t b = (uint32_t)(b0 + s + 16 * i + 4 * lk);  // first of four samples
-          f32x4 h, dn = f32x4{0.f, 0.f, 0.f, 0.f}, R[NORM ? 4 : 1];
+          Up next;
+          if (i == 0) next = load_up(1);
+          float zv[4], av[4], dv[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) zv[r] = z[0][i][r];
+          act_and_slope<4>(act, zv, av, dv);
+          f32x4 h, dn = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            h[r] = GATED ? av[4 * i + r] * z[K - 1][i][r] : av[4 * i + r];
-            if (NORM) {
-              R[r] = *(const f32x4*)(Rm + (b + r) * 4);
-              h[r] = (h[r] - R[r][0]) * R[r][1];
-            }
+            h[r] = GATED ? av[r] * z[K - 1][i][r] : av[r];
+            if (NORM) h[r] = (h[r] - up.r[NORM ? r : 0][0]) * up.r[NORM ? r : 0][1];
           }
           if (MF) {
             // dN = G W2 and T += G^T h, the sums in the order of the registers
-            f32x4 t = f32x4{T[0], T[1], T[2], T[3]};
+            f32x4 t = f32x4{T[0], T[1], T[2 % NO], T[3 % NO]};
+            f32x4 ga = up.g[0], gt = up.g[MF ? 1 : 0];
 #pragma unroll 1
-            for (int mm = m_lo; mm <= m_hi; ++mm) {
-              const float* const gm = a.G + (int64_t)mm * a.Bp * OM;
-              const f32x4 ga = *(const f32x4*)(gm + (uint32_t)(b0 + s + 16 * i + li) * OM + 4 * lk);
-              f32x4 gt, d = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-              for (int r = 0; r < 4; ++r) gt[r] = gm[(b + r) * OM + li];
-#pragma unroll
-              for (int q = 0; q < 4; ++q)
-                d = __builtin_amdgcn_mfma_f32_16x16x4f32(ga[q], w2[q % NO], d, 0, 0, 0);
+            for (int mm = m_lo;;) {
+              f32x4 d = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
-                dn[r] = m == mm ? d[r] : dn[r];
+                d = __builtin_amdgcn_mfma_f32_16x16x4f32(ga[r], w2[r % NO], d, 0, 0, 0);
                 t = __builtin_amdgcn_mfma_f32_16x16x4f32(gt[r], m == mm ? h[r] : 0.f, t, 0, 0, 0);
               }
+#pragma unroll
+              for (int r = 0; r < 4; ++r) dn[r] = m == mm ? d[r] : dn[r];
+              if (++mm > m_hi) break;
+              const uint32_t b = (uint32_t)(b0 + s + 16 * i + 4 * lk);
+              const float* const g = a.G + (int64_t)mm * a.Bp * OM;
+              ga = *(const f32x4*)(g + (uint32_t)(b0 + s + 16 * i + li) * OM + 4 * lk);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) gt[r] = g[(b + r) * OM + li];
             }
 #pragma unroll
             for (int o = 0; o < 4; ++o) T[o % NO] = t[o];
           } else {
-            float G[4 * OM];
-#pragma unroll
-            for (int v = 0; v < OM; ++v) {
-              const f32x4 q = *(const f32x4*)(Gm + b * OM + 4 * v);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) G[4 * v + e] = q[e];
-            }
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
               for (int o = 0; o < NO; ++o) {
-                dn[r] = fmaf(G[r * OM + o], w2[o], dn[r]);
-                T[o] = fmaf(G[r * OM + o], h[r], T[o]);
+                const float G = up.g[MF ? 0 : (r * OM + o) >> 2][(r * OM + o) & 3];
+                dn[r] = fmaf(G, w2[o], dn[r]);
+                T[o] = fmaf(G, h[r], T[o]);
               }
           }
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int v = 4 * i + r;
-            if (NORM) dn[r] = R[r][1] * (fmaf(gn, dn[r], -R[r][2]) - h[r] * R[r][3]);
-            dz[0][i][r] = GATED ? dn[r] * z[K - 1][i][r] * dv[v] : dn[r] * dv[v];
-            if (GATED) dz[K - 1][i][r] = dn[r] * av[v];
+            if (NORM) {
+              const f32x4 q = up.r[NORM ? r : 0];
+              dn[r] = q[1] * (fmaf(gn, dn[r], -q[2]) - h[r] * q[3]);
+            }
+            dz[0][i][r] = GATED ? dn[r] * z[K - 1][i][r] * dv[r] : dn[r] * dv[r];
+            if (GATED) dz[K - 1][i][r] = dn[r] * av[r];
+          }
+          if (i == 0) {
+            pin(next);
+            up = next;
           }
         }
         // ---- dW1 (and dV1) += dZ^T X ------------------------------------------
@@ -238,29 +244,29 @@ _Pragma("unroll") for (int mt = 0; mt < K; ++mt) acc[mt][j] =        \
     }
     if (!live) continue;
     // ---- the gradients, stored or applied ---------------------------------------
+    const float rate = a.g.lrm ? a.g.lrm[m] : a.g.lr;
 #pragma unroll
     for (int mt = 0; mt < K; ++mt) {
       float* const dW = mt ? a.dV1 : a.dW1;
       float* const W = const_cast<float*>(mt ? p.V1 : p.W1);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
+        if (4 * lk + r >= cnt) continue;
         const int64_t nr = n0 + 4 * lk + r;
-        if (nr >= p.N) continue;
-        const float rate = a.g.lrm ? a.g.lrm[p.mid[nr]] : a.g.lr;
+        const float row_rate = a.g.lrm ? a.g.lrm[p.mid[nr]] : a.g.lr;
 #pragma unroll
         for (int j = 0; j < NF; ++j) {
           const int f = 16 * j + li;
           if (f >= F) continue;
           if (dW) dW[nr * F + f] = acc[mt][j][r];
-          else W[nr * F4 + f] -= rate * acc[mt][j][r];
+          else W[nr * F4 + f] -= row_rate * acc[mt][j][r];
         }
       }
     }
     if (MF) {
-      if (n0 + li >= p.N) continue;
+      if (li >= cnt) continue;
       float dg = 0.f, ds = 0.f;
       const float sn = NORM ? p.shift[n] : 0.f;
-      const float rate = a.g.lrm ? a.g.lrm[m] : a.g.lr;
 #pragma unroll
       for (int q = 0; q < NO; ++q) {
         const int o = 4 * lk + q;
@@ -296,7 +302,7 @@ _Pragma("unroll") for (int mt = 0; mt < K; ++mt) acc[mt][j] =        \
         T[o] += __shfl_xor(T[o], 16);
         T[o] += __shfl_xor(T[o], 32);
       }
-      if (lk == 0 && n0 + li < p.N) blk_unit_grads<NO, NORM>(p, a.g, a.Gs, n, m, gn, w2, T);
+      if (lk == 0 && li < cnt) blk_unit_grads<NO, NORM>(p, a.g, a.Gs, n, m, gn, w2, T);
     }
   }
 }
@@ -317,17 +323,10 @@ BlkBwdInst bwd_kind(bool gated, bool norm) {
 
 BlkBwdInst bwd_of(const BlkPack& p) {
   const bool g = p.V1 != nullptr, n = p.gain != nullptr;
-  switch (blk_shape(p.F4)) {
-    case 1: return bwd_kind<0, 2>(g, n);
-    case 2: return bwd_kind<1, 0>(g, n);
-    case 3: return bwd_kind<1, 2>(g, n);
-    case 4: return bwd_kind<2, 0>(g, n);
-    case 5: return bwd_kind<2, 2>(g, n);
-    case 6: return bwd_kind<3, 0>(g, n);
-    case 7: return bwd_kind<3, 2>(g, n);
-    case 8: return bwd_kind<4, 0>(g, n);
-    default: return {nullptr, 0};
-  }
+#define PMLP_CALL(NC, RM) bwd_kind<NC, RM>(g, n)
+  PMLP_BLK_SHAPE(p.F4, PMLP_CALL)
+#undef PMLP_CALL
+  return {nullptr, 0};
 }
 
 // Samples a chunk: all of them where they fit in LDS, else the most equal parts.
@@ -354,16 +353,15 @@ hipError_t PMLP_CAT(launch_blk_fused_bwd_, PMLP_BLK_OM)(const BlkPack& p, BlkBwd
     e = hipDeviceGetAttribute(&lmax, hipDeviceAttributeMaxSharedMemoryPerBlock, dev);
   if (e != hipSuccess) return e;
   a.SC = fn ? chunk_samples(inst.NC, a.Bp, (size_t)lmax) : 0;
-  if (a.SC <= 0 || a.Bp < 32 || a.Bp % 32 || a.B < 1 || a.B > a.Bp || p.O > OM || p.N < 1)
+  if (a.SC <= 0 || a.Bp < 32 || a.Bp % 32 || a.B < 1 || a.B > a.Bp || p.O > OM || a.ntiles < 1)
     return hipErrorInvalidValue;
   const size_t lds = pieces_bytes(inst.NC, a.SC);
-  const int64_t tiles = (p.N + 15) / 16;
   // eight waves share the samples' pieces where those leave room for one workgroup
   // only, four where there is more
   const int waves = 4 * lds > (size_t)lmax ? 8 : 4;
   const int slots = resident_blocks((const void*)fn, 64 * waves, lds);
   if (slots <= 0) return hipErrorInvalidValue;
-  const int64_t grid = std::min<int64_t>(slots, (tiles + waves - 1) / waves);
+  const int64_t grid = std::min<int64_t>(slots, (a.ntiles + waves - 1) / waves);
   fn<<<(unsigned)grid, 64 * waves, lds, s>>>(p, a);
   return hipGetLastError();
 }

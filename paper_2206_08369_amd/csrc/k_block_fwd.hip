@@ -63,7 +63,6 @@ void k_blk_fused_fwd(BlkPack p, BlkFwdArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
   const int chunk = blockIdx.x / a.wpc, wg = blockIdx.x - chunk * a.wpc;
   const int SC = a.SC, plane = SC * RB, b0 = chunk * SC;
-  const int rem = RM ? (p.F4 - 32 * NC) >> 2 : 0;
   fill_pieces<NC>(lds, SC, a.X, b0, a.B, a.F, tid, blockDim.x);
   lds_barrier();
   const int steps = (std::min(SC, a.B - b0) + 31) >> 5;
@@ -77,7 +76,7 @@ void k_blk_fused_fwd(BlkPack p, BlkFwdArgs a) {
     const int n0 = __builtin_amdgcn_readfirstlane(q.n0);
     const int cnt = __builtin_amdgcn_readfirstlane(q.cnt), act = __builtin_amdgcn_readfirstlane(q.act);
     UnitRows<NC, RM, K> w;
-    w.load(p, n0 + std::min(li, cnt - 1), lk, rem);
+    w.load(p, n0 + std::min(li, cnt - 1), lk);
     // gain * W2 of the outputs (MF: of output li) and this lane's units
     f32x4 w2[MF ? 1 : 2];
     const int mine = cnt - 4 * lk;  // units of this lane: min(4, mine), if positive
@@ -98,7 +97,7 @@ void k_blk_fused_fwd(BlkPack p, BlkFwdArgs a) {
     for (int st = 0; st < steps; ++st) {
       const int at = 32 * st * RB;
       f32x4 z[K][2];
-      unit_products<NC, RM, K, true>(w, zrow + at, xrow + at, plane, rem, z);
+      unit_products<NC, RM, K, true>(w, zrow + at, xrow + at, plane, z);
       float zv[8], h[8];
 #pragma unroll
       for (int v = 0; v < 8; ++v) zv[v] = z[0][v >> 2][v & 3];
@@ -178,17 +177,10 @@ BlkFwdInst fwd_kind(bool gated, bool norm) {
 
 BlkFwdInst fwd_of(const BlkPack& p) {
   const bool g = p.V1 != nullptr, n = p.gain != nullptr;
-  switch (blk_shape(p.F4)) {
-    case 1: return fwd_kind<0, 2>(g, n);
-    case 2: return fwd_kind<1, 0>(g, n);
-    case 3: return fwd_kind<1, 2>(g, n);
-    case 4: return fwd_kind<2, 0>(g, n);
-    case 5: return fwd_kind<2, 2>(g, n);
-    case 6: return fwd_kind<3, 0>(g, n);
-    case 7: return fwd_kind<3, 2>(g, n);
-    case 8: return fwd_kind<4, 0>(g, n);
-    default: return {nullptr, 0, 0};
-  }
+#define PMLP_CALL(NC, RM) fwd_kind<NC, RM>(g, n)
+  PMLP_BLK_SHAPE(p.F4, PMLP_CALL)
+#undef PMLP_CALL
+  return {nullptr, 0, 0};
 }
 
 }  // namespace

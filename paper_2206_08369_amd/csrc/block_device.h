@@ -104,32 +104,43 @@ __device__ __forceinline__ void fill_pieces(char* lds, int SC, const float* X, i
   }
 }
 
-// A unit's row of W1 and V1: the pieces of 32 NC columns and RM fp32 columns, as the
-// lane (row li, columns 8 lk ..) holds them for a product's operand.
+// A unit's row of W1 and V1 as the lane (row li, columns 8 lk ..) holds it for a
+// product's operand: 32 NC columns and RM fp32 steps of four, as loaded ..
 template <int NC, int RM, int K>
-struct UnitRows {
-  static constexpr int NCA = NC > 0 ? NC : 1, RMA = RM > 0 ? RM : 1;
-  bf16x8 p[K][NCA][3];
-  float t[K][RMA];
+struct UnitRaw {
+  f32x4 w[K][NC > 0 ? 2 * NC : 1];
+  float t[K][RM > 0 ? RM : 1];
   __device__ __forceinline__ void load(const BlkPack& pk, int64_t n, int lk) {
-    const int F4 = pk.F4;
 #pragma unroll
     for (int mt = 0; mt < K; ++mt) {
-      const float* row = (mt ? pk.V1 : pk.W1) + n * F4;
-      f32x4 w[2 * NCA];
+      const float* row = (mt ? pk.V1 : pk.W1) + n * pk.F4;
 #pragma unroll
       for (int e = 0; e < 2 * NC; ++e) {
         const int k = 32 * (e >> 1) + 8 * lk + 4 * (e & 1);
-        w[e] = *(const f32x4*)(row + (k < F4 ? k : F4 - 4));
+        w[mt][e] = *(const f32x4*)(row + (k < pk.F4 ? k : pk.F4 - 4));
       }
 #pragma unroll
       for (int q = 0; q < RM; ++q) t[mt][q] = row[32 * NC + 4 * q + lk];
+    }
+  }
+};
+
+// .. and in pieces.
+template <int NC, int RM, int K>
+struct UnitRows {
+  bf16x8 p[K][NC > 0 ? NC : 1][3];
+  float t[K][RM > 0 ? RM : 1];
+  __device__ __forceinline__ void split(const UnitRaw<NC, RM, K>& r, int F4, int lk) {
+#pragma unroll
+    for (int mt = 0; mt < K; ++mt) {
+#pragma unroll
+      for (int q = 0; q < RM; ++q) t[mt][q] = opaque(r.t[mt][q]);
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         f32x4 q[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          q[e] = opaque(w[2 * c + e]);
+          q[e] = opaque(r.w[mt][2 * c + e]);
           if (32 * c + 8 * lk + 4 * e >= F4) q[e] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         split3(q[0], q[1], p[mt][c][0], p[mt][c][1], p[mt][c][2]);

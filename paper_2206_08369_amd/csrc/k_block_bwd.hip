@@ -53,7 +53,7 @@ __device__ __forceinline__ void act_and_slope(int A, const float (&z)[NV], float
 }
 
 template <int NC, int RM, bool GATED, bool NORM>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(NC <= 1 && !MF ? 3 : 2)))
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(NC <= 1 && !MF && !(GATED && NORM) ? 3 : 2)))
 void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
   constexpr int NF = 2 * NC + (RM ? 1 : 0), K = GATED ? 2 : 1, RB = row_bytes(NC);
 
@@ -72,32 +72,102 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
   const int zrow = li * RB + 16 * lk, xrow = li * RB + 64 * NC + 2 * lk;
   const int trow = (4 * lk + (li >> 2)) * RB + 8 * (li & 3);
 
+  // Up to four outputs: each lane its unit's weights and sums T_o.  More go through
+  // fp32 matrix products, a model at a time: w2[0..3] are then outputs 4 lk + q of
+  // unit li, and T[0..3] their sums.
+  //
+  // Loads run ahead of their use and of the stores of the tile before (they return in
+  // order): a block's output gradients and statistics by a block, over the ends of
+  // tiles, and where a tile's rows leave registers free those by a tile.
+  constexpr bool AHEAD = NC <= 1;
+  struct Next {
+    UnitRaw<NC, RM, K> w;
+    float w2[NO], gs[NORM ? NO : 1], g, s;
+  } nx;
+  auto fetch = [&](int64_t n, int m) {
+    nx.w.load(p, n, lk);
+    nx.g = NORM ? p.gain[n] : 1.f;
+    nx.s = NORM ? p.shift[n] : 0.f;
+#pragma unroll
+    for (int o = 0; o < NO; ++o) {
+      const int ow = MF ? 4 * lk + o : o, oc = ow < p.O ? ow : 0;
+      nx.w2[o] = p.W2[(int64_t)oc * p.ldw + n];
+      if (NORM) nx.gs[NORM ? o : 0] = a.Gs[(int64_t)m * p.O + oc];
+    }
+  };
+  UnitRows<NC, RM, K> w;
+  float w2[NO], gs[NORM ? NO : 1], gn = 1.f, sn = 0.f;  // (gs: sum_b G of the unit's model)
+  auto take = [&] {
+    w.split(nx.w, F4, lk);
+    gn = opaque(nx.g);
+    sn = opaque(nx.s);
+#pragma unroll
+    for (int o = 0; o < NO; ++o) {
+      const float v = opaque(nx.w2[o]);
+      w2[o] = (MF ? 4 * lk + o : o) < p.O ? v : 0.f;
+      if (NORM) gs[NORM ? o : 0] = opaque(nx.gs[NORM ? o : 0]);
+    }
+  };
+  struct Up {
+    f32x4 g[MF ? 2 : OM], r[NORM ? 4 : 1];
+  };
+  // block b (its first sample) of the lanes' models m
+  auto load_up = [&](int m, int b) {
+    Up u;
+    const uint32_t at = (uint32_t)(b + 4 * lk);  // first of four samples
+    if (MF) {
+      const float* const g =
+          a.G + (int64_t)__builtin_amdgcn_readfirstlane(m) * a.Bp * OM;
+      u.g[0] = *(const f32x4*)(g + (uint32_t)(b + li) * OM + 4 * lk);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) u.g[MF ? 1 : 0][r] = g[(at + r) * OM + li];
+    } else {
+      const float* const g = a.G + ((int64_t)m * a.Bp + at) * OM;
+#pragma unroll
+      for (int v = 0; v < NO; ++v) u.g[MF ? 0 : v] = *(const f32x4*)(g + 4 * v);
+    }
+    if (NORM) {
+      const float* const R = a.R + ((int64_t)m * a.Bp + at) * 4;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) u.r[NORM ? r : 0] = *(const f32x4*)(R + 4 * r);
+    }
+    return u;
+  };
+  auto pin = [&](Up& u) {  // (the loads stay where they are)
+#pragma unroll
+    for (int v = 0; v < (MF ? 2 : OM); ++v) u.g[v] = opaque(u.g[v]);
+#pragma unroll
+    for (int r = 0; r < (NORM ? 4 : 0); ++r) u.r[NORM ? r : 0] = opaque(u.r[NORM ? r : 0]);
+  };
+  const int stride = gridDim.x * nw;
+  auto tile_at = [&](int t) { return a.tiles[std::min(t, a.ntiles - 1)]; };
+  auto unit_of = [&](const BlkTile& q) { return (int64_t)q.n0 + std::min(li, q.cnt - 1); };
+  int tile = (int)blockIdx.x * nw + wave;
+  BlkTile q = tile_at(tile), qn = tile_at(tile + stride);
+  int m = p.mid[unit_of(q)];
+  Up up = load_up(m, 0);
+  if (AHEAD) {
+    fetch(unit_of(q), m);
+    take();
+  }
 #pragma unroll 1
-  for (int round = 0; round < rounds; ++round) {
-    const int tile = (round * (int)gridDim.x + (int)blockIdx.x) * nw + wave;
+  for (int round = 0; round < rounds; ++round, tile += stride) {
     const bool live = tile < a.ntiles;
-    const BlkTile q = a.tiles[live ? tile : a.ntiles - 1];
     const int n0 = __builtin_amdgcn_readfirstlane(q.n0);
     const int cnt = __builtin_amdgcn_readfirstlane(q.cnt), act = __builtin_amdgcn_readfirstlane(q.act);
     const int64_t n = n0 + std::min(li, cnt - 1);
-    const int m = p.mid[n];
     const int m_lo = __builtin_amdgcn_readfirstlane(m), m_hi = __builtin_amdgcn_readlane(m, 15);
-    const float gn = NORM ? p.gain[n] : 1.f;
-    // Up to four outputs: each lane its unit's weights and sums T_o.  More go through
-    // fp32 matrix products, a model at a time: w2[0..3] are then outputs 4 lk + q of
-    // unit li, and T[0..3] their sums.
-    float w2[NO], T[NO];
-#pragma unroll
-    for (int o = 0; o < NO; ++o) {
-      const int ow = MF ? 4 * lk + o : o;
-      const float v = p.W2[(int64_t)(ow < p.O ? ow : 0) * p.ldw + n];
-      w2[o] = ow < p.O ? v : 0.f;
-      T[o] = 0.f;
+    const BlkTile qnn = tile_at(tile + 2 * stride);
+    const int mn = p.mid[unit_of(qn)];
+    if (AHEAD) {
+      fetch(unit_of(qn), mn);
+    } else {
+      fetch(n, m);
+      take();
     }
-    UnitRows<NC, RM, K> w;
-    w.load(p, n, lk);
-    const float* const Gm = a.G + (int64_t)m * a.Bp * OM;
-    const float* const Rm = a.R + (int64_t)m * a.Bp * 4;
+    float T[NO];
+#pragma unroll
+    for (int o = 0; o < NO; ++o) T[o] = 0.f;
     f32x4 acc[K][NF];
 #pragma unroll
     for (int mt = 0; mt < K; ++mt)
@@ -117,34 +187,6 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
       for (int st = 0; st < steps; ++st) {
         const int s = 32 * st;
         // ---- Z (and U) of 32 samples ------------------------------------------
-        // a block's output gradients and statistics, loaded a block ahead
-        struct Up {
-          f32x4 g[MF ? 2 : OM], r[NORM ? 4 : 1];
-        };
-        auto load_up = [&](int i) {
-          Up u;
-          const uint32_t b = (uint32_t)(b0 + s + 16 * i + 4 * lk);  // first of four samples
-          if (MF) {
-            const float* const g = a.G + (int64_t)m_lo * a.Bp * OM;
-            u.g[0] = *(const f32x4*)(g + (uint32_t)(b0 + s + 16 * i + li) * OM + 4 * lk);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) u.g[1][r] = g[(b + r) * OM + li];
-          } else {
-#pragma unroll
-            for (int v = 0; v < NO; ++v) u.g[MF ? 0 : v] = *(const f32x4*)(Gm + b * OM + 4 * v);
-          }
-#pragma unroll
-          for (int r = 0; r < (NORM ? 4 : 0); ++r)
-            u.r[NORM ? r : 0] = *(const f32x4*)(Rm + (b + r) * 4);
-          return u;
-        };
-        auto pin = [&](Up& u) {  // (the loads stay where they are)
-#pragma unroll
-          for (int v = 0; v < (MF ? 2 : OM); ++v) u.g[v] = opaque(u.g[v]);
-#pragma unroll
-          for (int r = 0; r < (NORM ? 4 : 0); ++r) u.r[NORM ? r : 0] = opaque(u.r[NORM ? r : 0]);
-        };
-        Up up = load_up(0);
         f32x4 z[K][2];
         unit_products<NC, RM, K, false>(w, lds + s * RB + zrow, lds + s * RB + xrow, plane, z);
         pin(up);
@@ -152,8 +194,8 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
         f32x4 dz[K][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          Up next;
-          if (i == 0) next = load_up(1);
+          const bool last = i == 1 && b0 + s + 32 >= a.Bp;
+          Up next = load_up(last ? mn : m, last ? 0 : b0 + s + 16 * (i + 1));
           float zv[4], av[4], dv[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r) zv[r] = z[0][i][r];
@@ -206,10 +248,8 @@ void k_blk_fused_bwd(BlkPack p, BlkBwdArgs a) {
             dz[0][i][r] = GATED ? dn[r] * z[K - 1][i][r] * dv[r] : dn[r] * dv[r];
             if (GATED) dz[K - 1][i][r] = dn[r] * av[r];
           }
-          if (i == 0) {
-            pin(next);
-            up = next;
-          }
+          if (i == 0) pin(next);
+          up = next;
         }
         // ---- dW1 (and dV1) += dZ^T X ------------------------------------------
         bf16x8 dp[K][3];
@@ -242,68 +282,73 @@ _Pragma("unroll") for (int mt = 0; mt < K; ++mt) acc[mt][j] =        \
         }
       }
     }
-    if (!live) continue;
     // ---- the gradients, stored or applied ---------------------------------------
     const float rate = a.g.lrm ? a.g.lrm[m] : a.g.lr;
+    float dw[NO], dg = 0.f, ds = 0.f, old[NO];
 #pragma unroll
-    for (int mt = 0; mt < K; ++mt) {
-      float* const dW = mt ? a.dV1 : a.dW1;
-      float* const W = const_cast<float*>(mt ? p.V1 : p.W1);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if (4 * lk + r >= cnt) continue;
-        const int64_t nr = n0 + 4 * lk + r;
-        const float row_rate = a.g.lrm ? a.g.lrm[p.mid[nr]] : a.g.lr;
-#pragma unroll
-        for (int j = 0; j < NF; ++j) {
-          const int f = 16 * j + li;
-          if (f >= F) continue;
-          if (dW) dW[nr * F + f] = acc[mt][j][r];
-          else W[nr * F4 + f] -= row_rate * acc[mt][j][r];
-        }
+    for (int o = 0; o < NO; ++o) {
+      if (!MF) {
+        T[o] += __shfl_xor(T[o], 16);
+        T[o] += __shfl_xor(T[o], 32);
+      }
+      dw[o] = T[o];
+      old[o] = w2[o];
+      if (NORM) {
+        const float sg = gs[NORM ? o : 0];
+        dg = fmaf(w2[o], T[o], dg);
+        ds = fmaf(w2[o], sg, ds);
+        dw[o] = fmaf(gn, T[o], sn * sg);
       }
     }
-    if (MF) {
-      if (li >= cnt) continue;
-      float dg = 0.f, ds = 0.f;
-      const float sn = NORM ? p.shift[n] : 0.f;
+    if (NORM && MF) {
+      dg += __shfl_xor(dg, 16);
+      ds += __shfl_xor(ds, 16);
+      dg += __shfl_xor(dg, 32);
+      ds += __shfl_xor(ds, 32);
+    }
+    const float og = gn, os = sn;
+    if (AHEAD) take();
+    if (live) {
 #pragma unroll
-      for (int q = 0; q < NO; ++q) {
-        const int o = 4 * lk + q;
-        if (o >= p.O) continue;
-        float dw = T[q];
-        if (NORM) {
-          const float s = a.Gs[(int64_t)m * p.O + o];
-          dg = fmaf(w2[q], T[q], dg);
-          ds = fmaf(w2[q], s, ds);
-          dw = fmaf(gn, T[q], sn * s);
+      for (int r = 0; r < 4; ++r) {
+        const float row_rate = __shfl(rate, 4 * lk + r);
+        if (4 * lk + r >= cnt) continue;
+        const int64_t nr = n0 + 4 * lk + r;
+#pragma unroll
+        for (int mt = 0; mt < K; ++mt) {
+          float* const dW = mt ? a.dV1 : a.dW1;
+          float* const W = const_cast<float*>(mt ? p.V1 : p.W1);
+#pragma unroll
+          for (int j = 0; j < NF; ++j) {
+            const int f = 16 * j + li;
+            if (f >= F) continue;
+            if (dW) dW[nr * F + f] = acc[mt][j][r];
+            else W[nr * F4 + f] -= row_rate * acc[mt][j][r];
+          }
         }
-        if (a.g.dW2) a.g.dW2[(int64_t)o * p.N + n] = dw;
-        else p.W2[(int64_t)o * p.ldw + n] = w2[q] - rate * dw;
       }
-      if (NORM) {  // (the four lk of a unit are all here or none is)
-        dg += __shfl_xor(dg, 16);
-        ds += __shfl_xor(ds, 16);
-        dg += __shfl_xor(dg, 32);
-        ds += __shfl_xor(ds, 32);
-        if (lk == 0) {
+      if (li < cnt && (MF || lk == 0)) {
+#pragma unroll
+        for (int q = 0; q < NO; ++q) {
+          const int o = MF ? 4 * lk + q : q;
+          if (o >= p.O) continue;
+          if (a.g.dW2) a.g.dW2[(int64_t)o * p.N + n] = dw[q];
+          else p.W2[(int64_t)o * p.ldw + n] = old[q] - rate * dw[q];
+        }
+        if (NORM && lk == 0) {
           if (a.g.dW2) {
             a.g.dgain[n] = dg;
             a.g.dshift[n] = ds;
           } else {
-            p.gain[n] = gn - rate * dg;
-            p.shift[n] = sn - rate * ds;
+            p.gain[n] = og - rate * dg;
+            p.shift[n] = os - rate * ds;
           }
         }
       }
-    } else {
-#pragma unroll
-      for (int o = 0; o < NO; ++o) {
-        T[o] += __shfl_xor(T[o], 16);
-        T[o] += __shfl_xor(T[o], 32);
-      }
-      if (lk == 0 && li < cnt) blk_unit_grads<NO, NORM>(p, a.g, a.Gs, n, m, gn, w2, T);
     }
+    q = qn;
+    qn = qnn;
+    m = mn;
   }
 }
 

@@ -51,7 +51,7 @@ __device__ __forceinline__ float sum16(float a, float b) {
 // spilling, four, three or two.
 template <int NC, bool GATED>
 constexpr int max_threads() {
-  return GATED ? (NC <= 1 ? 1024 : NC <= 3 ? 768 : 512) : (NC <= 3 ? 1024 : 768);
+  return GATED ? (NC == 0 ? 1024 : NC <= 3 ? 768 : 512) : (NC <= 3 ? 1024 : 768);
 }
 
 template <int NC, int RM, bool GATED, bool NORM>
@@ -70,27 +70,48 @@ void k_blk_fused_fwd(BlkPack p, BlkFwdArgs a) {
   const char* const xrow = lds + li * RB + 64 * NC + 2 * lk;
   const int PQ = p.O + (NORM ? 2 : 0);
 
-#pragma unroll 1
-  for (int t = wg * nw + wave; t < a.ntiles; t += a.wpc * nw) {
-    const BlkTile q = a.tiles[t];
-    const int n0 = __builtin_amdgcn_readfirstlane(q.n0);
-    const int cnt = __builtin_amdgcn_readfirstlane(q.cnt), act = __builtin_amdgcn_readfirstlane(q.act);
-    UnitRows<NC, RM, K> w;
-    w.load(p, n0 + std::min(li, cnt - 1), lk);
-    // gain * W2 of the outputs (MF: of output li) and this lane's units
-    f32x4 w2[MF ? 1 : 2];
-    const int mine = cnt - 4 * lk;  // units of this lane: min(4, mine), if positive
+  // Where a tile's rows leave registers free the next tile's are loaded while this one
+  // is at work (a tile of few steps is as long as its wait for them).
+  constexpr bool AHEAD = NC <= 1;
+  struct Next {  // a tile's rows, and gain and W2 of the outputs (MF: of output li)
+    UnitRaw<NC, RM, K> w;
+    float w2[MF ? 1 : 2][4], g[4];
+  } nx;
+  auto fetch = [&](int n0, int cnt) {
+    nx.w.load(p, n0 + std::min(li, cnt - 1), lk);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int64_t n = n0 + (r < mine ? 4 * lk + r : 0);
-      const float g = NORM ? p.gain[n] : 1.f;
+      const int64_t n = n0 + std::min(4 * lk + r, cnt - 1);
+      nx.g[r] = NORM ? p.gain[n] : 1.f;
 #pragma unroll
       for (int o = 0; o < (MF ? 1 : 2); ++o) {
         const int ow = MF ? li : o;
-        const float v = p.W2[(int64_t)(ow < p.O ? ow : 0) * p.ldw + n] * g;
-        w2[o][r] = ow < p.O && r < mine ? v : 0.f;
+        nx.w2[o][r] = p.W2[(int64_t)(ow < p.O ? ow : 0) * p.ldw + n];
       }
     }
+  };
+  const int step = a.wpc * nw;
+  auto tile_at = [&](int t) { return a.tiles[std::min(t, a.ntiles - 1)]; };
+  BlkTile q = tile_at(wg * nw + wave), qn = tile_at(wg * nw + wave + step);
+  if (AHEAD) fetch(q.n0, q.cnt);
+#pragma unroll 1
+  for (int t = wg * nw + wave; t < a.ntiles; t += step) {
+    const int n0 = __builtin_amdgcn_readfirstlane(q.n0);
+    const int cnt = __builtin_amdgcn_readfirstlane(q.cnt), act = __builtin_amdgcn_readfirstlane(q.act);
+    const BlkTile qnn = tile_at(t + 2 * step);
+    if (!AHEAD) fetch(n0, cnt);
+    UnitRows<NC, RM, K> w;
+    w.split(nx.w, p.F4, lk);
+    f32x4 w2[MF ? 1 : 2];  // gain * W2 of this lane's units
+    const int mine = cnt - 4 * lk;  // units of this lane: min(4, mine), if positive
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int o = 0; o < (MF ? 1 : 2); ++o) {
+        const float v = opaque(nx.w2[o][r]) * opaque(nx.g[r]);
+        w2[o][r] = (MF ? li : o) < p.O && r < mine ? v : 0.f;
+      }
+    if (AHEAD) fetch(qn.n0, qn.cnt);
     float* const rec = a.part + (int64_t)t * PQ * a.Br + b0 + li;
     const float rn = 1.f / (float)cnt;
 #pragma unroll 1
@@ -159,6 +180,8 @@ void k_blk_fused_fwd(BlkPack p, BlkFwdArgs a) {
         dst[(int64_t)(p.O + (lk >> 1)) * a.Br + 16 * (lk & 1)] = v;
       }
     }
+    q = qn;
+    qn = qnn;
   }
 }
 

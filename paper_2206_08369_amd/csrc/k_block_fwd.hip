@@ -18,9 +18,7 @@
 // the mean: (h - K)^2 exceeds the variance at most 15 times over 16 values, so that
 // loses four bits at worst, wherever the mean is.
 
-#include "block_device.h"
-
-#include <algorithm>
+#include "block_tiles.h"
 
 #ifndef PMLP_BLK_OM
 #error "compile with -DPMLP_BLK_OM=2|16"
@@ -32,21 +30,6 @@ namespace {
 
 constexpr bool MF = PMLP_BLK_OM > 2;
 
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-
-// a summed over lanes l and l ^ 32 in the lower half of the wave, b in the upper
-__device__ __forceinline__ float sum32(float a, float b) {
-  const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false,
-                                                   false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-// a summed over lanes l and l ^ 16 in the even rows of 16, b in the odd
-__device__ __forceinline__ float sum16(float a, float b) {
-  const u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false,
-                                                   false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
 // Threads of a workgroup, at most: as many waves as a SIMD's registers hold without
 // spilling, four, three or two.
 template <int NC, bool GATED>
@@ -57,132 +40,16 @@ constexpr int max_threads() {
 template <int NC, int RM, bool GATED, bool NORM>
 __global__ __launch_bounds__((max_threads<NC, GATED>()))
 void k_blk_fused_fwd(BlkPack p, BlkFwdArgs a) {
-  constexpr int K = GATED ? 2 : 1, RB = row_bytes(NC);
   extern __shared__ __align__(16) char lds[];
-  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
+  const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
   const int chunk = blockIdx.x / a.wpc, wg = blockIdx.x - chunk * a.wpc;
-  const int SC = a.SC, plane = SC * RB, b0 = chunk * SC;
+  const int SC = a.SC, b0 = chunk * SC;
   fill_pieces<NC>(lds, SC, a.X, b0, a.B, a.F, tid, blockDim.x);
   lds_barrier();
   const int steps = (std::min(SC, a.B - b0) + 31) >> 5;
-  const char* const zrow = lds + li * RB + 16 * lk;
-  const char* const xrow = lds + li * RB + 64 * NC + 2 * lk;
-  const int PQ = p.O + (NORM ? 2 : 0);
-
-  // Where a tile's rows leave registers free the next tile's are loaded while this one
-  // is at work (a tile of few steps is as long as its wait for them).
-  constexpr bool AHEAD = NC <= 1;
-  struct Next {  // a tile's rows, and gain and W2 of the outputs (MF: of output li)
-    UnitRaw<NC, RM, K> w;
-    float w2[MF ? 1 : 2][4], g[4];
-  } nx;
-  auto fetch = [&](int n0, int cnt) {
-    nx.w.load(p, n0 + std::min(li, cnt - 1), lk);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int64_t n = n0 + std::min(4 * lk + r, cnt - 1);
-      nx.g[r] = NORM ? p.gain[n] : 1.f;
-#pragma unroll
-      for (int o = 0; o < (MF ? 1 : 2); ++o) {
-        const int ow = MF ? li : o;
-        nx.w2[o][r] = p.W2[(int64_t)(ow < p.O ? ow : 0) * p.ldw + n];
-      }
-    }
-  };
-  const int step = a.wpc * nw;
-  auto tile_at = [&](int t) { return a.tiles[std::min(t, a.ntiles - 1)]; };
-  BlkTile q = tile_at(wg * nw + wave), qn = tile_at(wg * nw + wave + step);
-  if (AHEAD) fetch(q.n0, q.cnt);
-#pragma unroll 1
-  for (int t = wg * nw + wave; t < a.ntiles; t += step) {
-    const int n0 = __builtin_amdgcn_readfirstlane(q.n0);
-    const int cnt = __builtin_amdgcn_readfirstlane(q.cnt), act = __builtin_amdgcn_readfirstlane(q.act);
-    const BlkTile qnn = tile_at(t + 2 * step);
-    if (!AHEAD) fetch(n0, cnt);
-    UnitRows<NC, RM, K> w;
-    w.split(nx.w, p.F4, lk);
-    f32x4 w2[MF ? 1 : 2];  // gain * W2 of this lane's units
-    const int mine = cnt - 4 * lk;  // units of this lane: min(4, mine), if positive
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int o = 0; o < (MF ? 1 : 2); ++o) {
-        const float v = opaque(nx.w2[o][r]) * opaque(nx.g[r]);
-        w2[o][r] = (MF ? li : o) < p.O && r < mine ? v : 0.f;
-      }
-    if (AHEAD) fetch(qn.n0, qn.cnt);
-    float* const rec = a.part + (int64_t)t * PQ * a.Br + b0 + li;
-    const float rn = 1.f / (float)cnt;
-#pragma unroll 1
-    for (int st = 0; st < steps; ++st) {
-      const int at = 32 * st * RB;
-      f32x4 z[K][2];
-      unit_products<NC, RM, K, true>(w, zrow + at, xrow + at, plane, z);
-      float zv[8], h[8];
-#pragma unroll
-      for (int v = 0; v < 8; ++v) zv[v] = z[0][v >> 2][v & 3];
-      blk_acts<8>(act, zv, h);
-      if (GATED) {
-#pragma unroll
-        for (int v = 0; v < 8; ++v) h[v] *= z[K - 1][v >> 2][v & 3];
-      }
-      if (cnt < 16) {
-#pragma unroll
-        for (int v = 0; v < 8; ++v) h[v] = (v & 3) < mine ? h[v] : 0.f;
-      }
-      float* const dst = rec + 32 * st;
-      if (MF) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            s = __builtin_amdgcn_mfma_f32_16x16x4f32(w2[0][r], h[4 * i + r], s, 0, 0, 0);
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (4 * lk + r < p.O) dst[(int64_t)(4 * lk + r) * a.Br + 16 * i] = s[r];
-        }
-      } else {
-        float s[2][2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int o = 0; o < 2; ++o) {
-            s[i][o] = h[4 * i] * w2[MF ? 0 : o][0];
-#pragma unroll
-            for (int r = 1; r < 4; ++r) s[i][o] = fmaf(h[4 * i + r], w2[MF ? 0 : o][r], s[i][o]);
-          }
-        // row lk ends with block lk & 1 of output lk >> 1
-        const float v = sum16(sum32(s[0][0], s[0][1]), sum32(s[1][0], s[1][1]));
-        dst[(int64_t)(lk >> 1) * a.Br + 16 * (lk & 1)] = v;
-      }
-      if (NORM) {
-        float mean[2], m2[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float piv = __shfl(h[4 * i], li);  // the first unit's value
-          float d = 0.f, e = 0.f;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float v = (cnt == 16 || r < mine) ? h[4 * i + r] - piv : 0.f;
-            d += v;
-            e = fmaf(v, v, e);
-          }
-          d = sum32(d, d);
-          e = sum32(e, e);
-          d = sum16(d, d);
-          e = sum16(e, e);
-          mean[i] = fmaf(d, rn, piv);
-          m2[i] = fmaxf(fmaf(-d * rn, d, e), e != e ? e : 0.f);
-        }
-        const float v = lk & 2 ? (lk & 1 ? m2[1] : m2[0]) : (lk & 1 ? mean[1] : mean[0]);
-        dst[(int64_t)(p.O + (lk >> 1)) * a.Br + 16 * (lk & 1)] = v;
-      }
-    }
-    q = qn;
-    qn = qnn;
-  }
+  fwd_tiles<NC, RM, MF, GATED, NORM>(p, a, lds, SC, b0, steps, wg * nw + wave, a.ntiles,
+                                     a.wpc * nw);
 }
 
 typedef void (*BlkFwdFn)(BlkPack, BlkFwdArgs);

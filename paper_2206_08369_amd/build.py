@@ -20,7 +20,8 @@ LIB = os.path.join(PKG, "libpmlp.so")
 SOURCES = [("k_lds.hip", [])]
 SOURCES += [("k_fwd_s.hip", ["-DPMLP_FWD_BP=%d" % bp]) for bp in (256, 128, 64, 32, 16)]
 SOURCES += [("k_block_fwd.hip", ["-DPMLP_BLK_OM=%d" % om]) for om in (16, 2)]
-SOURCES += [("k_block_bwd.hip", ["-DPMLP_BLK_OM=%d" % om]) for om in (16, 4, 2)]
+SOURCES += [(src, ["-DPMLP_BLK_OM=%d" % om]) for om in (16, 4, 2)
+            for src in ("k_block_bwd.hip", "k_block_local.hip")]
 SOURCES += [(s, []) for s in ("k_gemm_bf16.hip", "k_m3.hip", "k_misc.hip", "k_gemm.hip", "k_deep.hip",
                               "k_block.hip", "api.hip")]
 

@@ -121,8 +121,11 @@ struct PmlpBlock {
   int32_t ntiles = 0;
   BlkTile* d_btiles = nullptr;  // of the backward, by activation
   int32_t nbtiles = 0;
+  int32_t most[kBlkLocalGroup] = {};  // [g - 1]: tiles of the largest group (see BlkLocal)
   int32_t planned = 0;  // batch size of `plan` (0: none yet)
   BlkRun plan;
+  int32_t lplanned = 0;  // padded batch size of `lplan`
+  BlkLocal lplan{};
   // Workspace.  A captured graph keeps the addresses it was captured with, so a
   // buffer that a larger batch replaces lives until the handle goes.
   unsigned char* ws = nullptr;
@@ -1524,6 +1527,44 @@ hipError_t launch_blk_fused_bwd(const BlkPack& p, const BlkBwdArgs& a, hipStream
   }
 }
 
+hipError_t launch_blk_local(const BlkPack& p, const BlkLocal& g, const BlkFwdArgs& f,
+                            const BlkLoss& l, const BlkBwdArgs& b, hipStream_t s) {
+  note_variant("k_blk_local", kArithX3);
+  switch (blk_om(p.O)) {
+    case 2: return launch_blk_local_2(p, g, f, l, b, s);
+    case 4: return launch_blk_local_4(p, g, f, l, b, s);
+    default: return launch_blk_local_16(p, g, f, l, b, s);
+  }
+}
+
+int blk_local_slots(const BlkPack& p, int32_t Bp, int32_t group) {
+  switch (blk_om(p.O)) {
+    case 2: return blk_local_slots_2(p, Bp, group);
+    case 4: return blk_local_slots_4(p, Bp, group);
+    default: return blk_local_slots_16(p, Bp, group);
+  }
+}
+
+// How a training step of Bp samples runs in one launch (group 0: it does not): with a
+// tile for each wave, all workgroups at once, and no more than 1024 of samples times a
+// model's tiles: past that few wide models gain from the samples' split over workgroups
+// (16 models of 128 units, 100 columns, 256 samples: 66 us in three launches, 79 in one;
+// 128 samples: 49 and 52; 256 such models 79 and 68).
+BlkLocal block_local(pmlp* h, int32_t Bp) {
+  PmlpBlock* k = h->block;
+  if (k->lplanned == Bp) return k->lplan;
+  BlkLocal best{};
+  if (Bp <= kBlkLocalBatch && Bp * k->most[0] <= 1024) {
+    const BlkPack p = block_pack(h);
+    for (int32_t group = 1; group <= kBlkLocalGroup && !best.group; ++group)
+      if (k->most[group - 1] <= kBlkLocalGroup &&
+          div_up(k->ntiles, group) <= blk_local_slots(p, Bp, group))
+        best = BlkLocal{group, k->d_toff};
+  }
+  k->lplanned = Bp;
+  return k->lplan = best;
+}
+
 // The run of B samples: the samples of a workgroup and the waves that share them, by
 // what a launch costs.  A wave's step of 32 samples takes its share of the SIMD, a
 // tile the wait for its weights and their splitting (as long as three steps), and a
@@ -1660,6 +1701,16 @@ int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_
   auto at = [&](size_t o) { return (float*)(k->ws + o); };
   const BlkLoss l{y, Y, B, at(oG), at(oR), at(oS), h->loss, h->flag, d.dW1 ? nullptr : lrm};
   const BlkGrads g{d.dW2, d.dgain, d.dshift, lr, lrm};
+  const BlkLocal one = fused ? block_local(h, Bp) : BlkLocal{};
+  if (one.group) {
+    const BlkFwdArgs f{X, B, h->F, k->d_tiles, k->ntiles, 0, 0, 0, at(oP), Bp};
+    const BlkBwdArgs b{X,      B,      h->F,   Bp,     0,     k->d_tiles, k->ntiles, at(oG),
+                       at(oR), at(oS), d.dW1, d.dV1, g};
+    if (int rc = run(h, KID_BWD_FUSED, [&] { return launch_blk_local(p, one, f, l, b, h->stream); }))
+      return rc;
+    h->have_loss = true;
+    return PMLP_OK;
+  }
   if (fused) {
     const BlkFwdArgs f{X,    B,     h->F,    k->d_tiles, k->ntiles,
                        r.SC, r.wpc, r.waves, at(oP),     Bp};
@@ -2363,6 +2414,15 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
   k->npieces = (int32_t)pieces.size();
   k->ntiles = (int32_t)tiles.size();
   k->nbtiles = (int32_t)btiles.size();
+  for (int32_t g = 1; g <= kBlkLocalGroup; ++g) {
+    int32_t tiles_of = 0, group = -1;
+    for (int32_t m = 0; m < M; ++m) {
+      if (toff[m] / g != group) tiles_of = 0;
+      group = toff[m] / g;
+      tiles_of += toff[m + 1] - toff[m];
+      k->most[g - 1] = std::max(k->most[g - 1], tiles_of);
+    }
+  }
   const size_t half = (size_t)h->Npad * h->F4, units = (size_t)h->Npad * sizeof(float);
   float* W = nullptr;
   if ((k->gated && hipMalloc(&W, (2 * half + 64) * sizeof(float)) != hipSuccess) ||

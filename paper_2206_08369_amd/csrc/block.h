@@ -136,6 +136,26 @@ PMLP_BLK_BWD_DECL(4)
 PMLP_BLK_BWD_DECL(16)
 #undef PMLP_BLK_BWD_DECL
 
+// Forward, loss and backward in one launch: workgroup w takes the models whose first
+// tile is one of tiles w * group .. (w + 1) * group - 1, for all samples.  As
+// launch_blk_fused_fwd (f.SC, f.wpc and f.waves are not read), launch_blk_loss and
+// launch_blk_fused_bwd (b.tiles: the forward's).
+constexpr int32_t kBlkLocalBatch = 256;  // samples, at most
+constexpr int32_t kBlkLocalGroup = 8;    // waves of a workgroup, and `group` at most
+struct BlkLocal {
+  int32_t group;
+  const int32_t* toff;
+};
+// (slots: workgroups that the device holds at once, 0: it cannot run)
+#define PMLP_BLK_LOCAL_DECL(OM)                                                           \
+  int blk_local_slots_##OM(const BlkPack& p, int32_t Bp, int32_t group);                  \
+  hipError_t launch_blk_local_##OM(const BlkPack& p, const BlkLocal& g, const BlkFwdArgs& f, \
+                                   const BlkLoss& l, const BlkBwdArgs& b, hipStream_t s);
+PMLP_BLK_LOCAL_DECL(2)
+PMLP_BLK_LOCAL_DECL(4)
+PMLP_BLK_LOCAL_DECL(16)
+#undef PMLP_BLK_LOCAL_DECL
+
 // V1 (tag 6, like W1), gain 1, shift 0 (either may be null).
 hipError_t launch_blk_init(float* V1, int64_t N, int32_t F, int32_t F4, float bound, uint64_t key,
                            float* gain, float* shift, hipStream_t s);

@@ -195,52 +195,4 @@ __device__ __forceinline__ void sample_grads(const BlkPack& p, const BlkLoss& l,
   if (NORM) *(f32x4*)(l.R + ((int64_t)m * Bp + b) * 4) = f32x4{s.mean, r, a1 * rh, a2 * rh};
 }
 
-// The same for a whole model, by one wave.
-template <int OM, bool NORM>
-__device__ __forceinline__ void wave_loss(const BlkPack& p, const BlkMap& map, const float* part,
-                                          int m, int Br, int Bp, const BlkLoss& l, float scale,
-                                          int lane) {
-  float C[OM], D[OM], gs[OM], loss = 0.f;
-  if (NORM) norm_consts<OM>(p, m, lane, 0, 1, nullptr, C, D);
-  const float rh = 1.f / (float)(p.seg_off[m + 1] - p.seg_off[m]);
-#pragma unroll
-  for (int o = 0; o < OM; ++o) gs[o] = 0.f;
-  for (int b = lane; b < Bp; b += 64) {
-    Merged<OM> s;
-    merge_pieces<OM, NORM>(p, map, part, m, Br, b < l.B ? b : l.B - 1, 0, 1, s);
-    sample_grads<OM, NORM>(p, l, m, b, Bp, s, C, D, rh, scale, loss, gs);
-  }
-  loss = group_sum_to_last(loss, 64);
-  if (lane == 63) {
-    l.loss[m] = loss * scale;
-    if (!isfinite(loss)) atomicAdd(l.flag + 2, 1);
-    if (l.lrm && !isfinite(l.lrm[m])) l.flag[1] = 1;
-  }
-  if (NORM) {
-#pragma unroll
-    for (int o = 0; o < OM; ++o) {
-      gs[o] = group_sum_to_last(gs[o], 64);
-      if (lane == 63 && o < p.O) l.Gs[(int64_t)m * p.O + o] = gs[o];
-    }
-  }
-}
-
-// A model's logits, by one wave.
-template <int OM, bool NORM>
-__device__ __forceinline__ void wave_out(const BlkPack& p, const BlkMap& map, const float* part,
-                                         int m, int Br, int b0, int b1, float* out, int64_t sm,
-                                         int64_t sb, int lane) {
-  float C[OM], D[OM];
-  if (NORM) norm_consts<OM>(p, m, lane, 0, 1, nullptr, C, D);
-  for (int b = b0 + lane; b < b1; b += 64) {
-    Merged<OM> s;
-    float r;
-    merge_pieces<OM, NORM>(p, map, part, m, Br, b, 0, 1, s);
-    if (NORM) apply_norm<OM>(s, C, &r);
-#pragma unroll
-    for (int o = 0; o < OM; ++o)
-      if (o < p.O) out[(int64_t)b * sb + (int64_t)m * sm + o] = NORM ? s.P[o] + D[o] : s.P[o];
-  }
-}
-
 }  // namespace pmlpk

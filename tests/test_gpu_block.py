@@ -119,6 +119,48 @@ def test_parity(pm, torch, name, kind):
     net.close()
 
 
+@pytest.mark.parametrize("O", [2, 3, 9])
+@pytest.mark.parametrize("F", [1, 4, 8, 12, 36, 40, 44, 64, 68, 72, 76, 100, 104, 108, 124, 128, 132])
+def test_parity_columns(pm, torch, F, O):
+    """Input columns at and around every shape of the fused kernels, with a batch that
+    runs in three launches (past 256) and in chunks, and one that may run in one."""
+    rng = np.random.default_rng(31 * F + O)
+    kind = sorted(KINDS)[(F // 4 + O) % 3]
+    gated, norm = KINDS[kind]
+    hs = rng.integers(4 if norm else 1, 40, 12).astype(np.int32)
+    acts = rng.choice(SMOOTH, hs.size).astype(np.int32)
+    p = ref.random_params(rng, hs, F, O, gated, norm)
+    net = make(pm, hs, acts, p, F, O, kind)
+    for B in (290, 75):
+        X, y = data(rng, F, O, B, "ce")
+        want = ref.pack(hs, acts, p, X, y)
+        within(net.forward(dev(torch, X)).cpu().numpy(), want["logits"], "logits")
+        for k, v in zip(net.param_names, net.gradients(dev(torch, X), dev(torch, y))):
+            within(v.cpu().numpy(), want[k], "d" + k)
+    net.close()
+
+
+@pytest.mark.parametrize("B", [1, 31, 64, 200])
+@pytest.mark.parametrize("O", [2, 4, 11])
+def test_parity_large_pool(pm, torch, O, B):
+    """More tiles than one launch takes (for 200 samples: in groups), tiles of the
+    backward that hold several models, runs of one activation of every length."""
+    rng = np.random.default_rng(100 * O + B)
+    M, F = (9000 if B < 200 else 1500), 9
+    hs = rng.integers(1, 9, M).astype(np.int32)
+    acts = np.repeat(rng.choice(SMOOTH, M), rng.integers(1, 7, M))[:M].astype(np.int32)
+    kind = ("both", "gated", "norm")[(O + B) % 3]
+    gated, norm = KINDS[kind]
+    p = ref.random_params(rng, hs, F, O, gated, norm)
+    net = make(pm, hs, acts, p, F, O, kind)
+    X, y = data(rng, F, O, B, "ce")
+    want = ref.pack(hs, acts, p, X, y)
+    within(net.forward(dev(torch, X)).cpu().numpy(), want["logits"], "logits")
+    for k, v in zip(net.param_names, net.gradients(dev(torch, X), dev(torch, y))):
+        within(v.cpu().numpy(), want[k], "d" + k)
+    net.close()
+
+
 @pytest.mark.parametrize("kind", ["gated", "both"])
 def test_parity_generic_kernels(pm, torch, kind, monkeypatch):
     monkeypatch.setenv("PMLP_GENERIC_KERNELS", "1")

@@ -101,9 +101,11 @@ struct PmlpDeep {
 };
 
 // How a batch runs through the fused forward of a block pack: SC samples a workgroup,
-// wpc workgroups of `waves` waves for each SC samples.  SC = 0: it does not.
+// wpc workgroups of `waves` waves for each SC samples, runs of `run` tiles (BlkMap), so
+// many records.  SC = 0: it does not.
 struct BlkRun {
-  int32_t SC = 0, wpc = 0, waves = 0;
+  int32_t SC = 0, wpc = 0, waves = 0, run = 1;
+  int64_t records = 0;
 };
 
 // The gate and the norm of a pack made by pmlp_create_block (W1 is then the
@@ -122,8 +124,8 @@ struct PmlpBlock {
   BlkTile* d_btiles = nullptr;  // of the backward, by activation
   int32_t nbtiles = 0;
   int32_t most[kBlkLocalGroup] = {};  // [g - 1]: tiles of the largest group (see BlkLocal)
-  int32_t planned = 0;  // batch size of `plan` (0: none yet)
-  BlkRun plan;
+  int32_t planned[2] = {};  // batch sizes of `plan` (0: none yet), the latest last
+  BlkRun plan[2];
   int32_t lplanned = 0;  // padded batch size of `lplan`
   BlkLocal lplan{};
   // Workspace.  A captured graph keeps the addresses it was captured with, so a
@@ -1573,8 +1575,14 @@ BlkLocal block_local(pmlp* h, int32_t Bp) {
 BlkRun block_run(pmlp* h, int32_t B) {
   PmlpBlock* k = h->block;
   if (!h->lds_kernels || h->F4 > kBlkFusedCols) return BlkRun{};
-  if (k->planned == B) return k->plan;
+  for (int i = 0; i < 2; ++i)
+    if (k->planned[i] == B) return k->plan[i];
   const BlkPack p = block_pack(h);
+  // Runs of several tiles save records and their merging, and cost LDS.  Models of 3.6
+  // tiles, 50 columns, both, 10000 samples: 735 us without, 705 with; of 32 tiles, 32
+  // columns, ten outputs, 32 samples: forward and loss 161 and 132.  A batch of up to 32
+  // has short records: models of 3.6 tiles, 100 columns, one sample 64 and 66.
+  const bool runs = k->ntiles >= (int64_t)(B > 32 ? 2 : 8) * h->M;
   BlkRun best;
   double least = 0;
   int32_t last = 0;
@@ -1583,7 +1591,8 @@ BlkRun block_run(pmlp* h, int32_t B) {
     if (SC == last) continue;
     last = SC;
     for (int32_t waves = 4; waves <= 16; waves += 4) {
-      const int64_t slots = p.O <= 2 ? blk_fwd_slots_2(p, SC, waves) : blk_fwd_slots_16(p, SC, waves);
+      const int64_t slots = p.O <= 2 ? blk_fwd_slots_2(p, SC, waves, runs)
+                                     : blk_fwd_slots_16(p, SC, waves, runs);
       if (slots <= 0) continue;
       const int64_t fit = std::max<int64_t>(1, slots / nchunk), want = div_up(k->ntiles, waves);
       for (int64_t w = fit; w <= std::max<int64_t>(fit, 32); ++w) {
@@ -1600,9 +1609,16 @@ BlkRun block_run(pmlp* h, int32_t B) {
       }
     }
   }
-  k->planned = B;
-  k->plan = best;
-  return best;
+  // a wave's tiles in equal runs of four or fewer (longer ones leave a wave with fewer
+  // activations, and waves uneven: a gated paper pool's forward 232 us with four, 248
+  // with eight)
+  const int32_t tiles = div_up(k->ntiles, best.wpc * best.waves);
+  best.run = runs ? div_up(tiles, div_up(tiles, 4)) : 1;
+  best.records = blk_records(p, k->ntiles, best.run);
+  std::swap(k->planned[0], k->planned[1]);
+  std::swap(k->plan[0], k->plan[1]);
+  k->planned[1] = B;
+  return k->plan[1] = best;
 }
 
 constexpr size_t kBlockSlice = (size_t)1 << 30;  // bytes of Z that a forward pass stores at once
@@ -1615,12 +1631,14 @@ int forward_block(pmlp* h, const float* X, int32_t B, float* out) {
   const BlkPack p = block_pack(h);
   const size_t rows = (size_t)h->Npad * (k->gated ? 2 : 1);
   int32_t slice = B;
-  const BlkRun whole = block_run(h, B);
-  const bool fused = whole.SC > 0;
-  const size_t rec = (size_t)k->ntiles * blk_planes(p) * sizeof(float);  // per sample
+  BlkRun r = block_run(h, B);
+  const bool fused = r.SC > 0;
   if (fused) {
-    if (rec * B > kRecordSlice)
-      slice = (int32_t)std::min<size_t>(std::max<size_t>(kRecordSlice / rec / 256 * 256, 256), B);
+    const size_t rec = (size_t)r.records * blk_planes(p) * sizeof(float);  // of a sample
+    if (const int32_t parts = (int32_t)std::min<size_t>(div_up((int64_t)(rec * B), (int64_t)kRecordSlice), div_up(B, 256)); parts > 1) {
+      slice = div_up(div_up(B, parts), 256) * 256;
+      r = block_run(h, slice);
+    }
   } else if ((size_t)pad_batch(B) * rows * sizeof(float) > kBlockSlice) {
     const size_t fit = kBlockSlice / (rows * sizeof(float)) / 256 * 256;
     slice = (int32_t)std::min<size_t>(std::max<size_t>(fit, 256), (size_t)B);
@@ -1636,7 +1654,7 @@ int forward_block(pmlp* h, const float* X, int32_t B, float* out) {
   const size_t oXp = c.take(fused ? 0 : (size_t)Bp * h->F4),
                oXt = c.take(fused ? 0 : (size_t)Bp * h->F4), oZ = c.take(fused ? 0 : rows * Bp);
   const int32_t br = fused ? (slice + 31) & ~31 : Bp;  // samples of a record
-  const size_t oP = c.take((size_t)(fused ? k->ntiles : k->npieces) * blk_planes(p) * br);
+  const size_t oP = c.take((size_t)(fused ? r.records : k->npieces) * blk_planes(p) * br);
   const size_t oL = over ? c.take((size_t)nout) : 0;
   if (int rc = ensure_block_ws(h, c.bytes)) return rc;
   float *Xp = (float*)(k->ws + oXp), *Xt = (float*)(k->ws + oXt), *Zt = (float*)(k->ws + oZ),
@@ -1644,13 +1662,12 @@ int forward_block(pmlp* h, const float* X, int32_t B, float* out) {
   for (int32_t b0 = 0; b0 < B; b0 += slice) {
     const int32_t n = std::min(slice, B - b0), np = pad_batch(n);
     if (fused) {
-      const BlkRun r = block_run(h, n);
-      const BlkFwdArgs f{X + (int64_t)b0 * h->F, n, h->F, k->d_tiles, k->ntiles, r.SC, r.wpc,
-                         r.waves, part, br};
+      const BlkFwdArgs f{X + (int64_t)b0 * h->F, n,     h->F,  k->d_tiles, k->ntiles, r.SC, r.wpc,
+                         r.waves,                r.run, part, br};
       if (int rc = run(h, KID_FWD_M3, [&] { return launch_blk_fused_fwd(p, f, h->stream); }))
         return rc;
       if (int rc = run(h, KID_CE, [&] {
-            return launch_blk_out(p, BlkMap{k->d_toff, k->ntiles}, part, br, n, dst + b0 * sb, h->O, sb,
+            return launch_blk_out(p, BlkMap{k->d_toff, r.run}, r.records, part, br, n, dst + b0 * sb, h->O, sb,
                                   h->stream);
           }))
         return rc;
@@ -1667,7 +1684,7 @@ int forward_block(pmlp* h, const float* X, int32_t B, float* out) {
         }))
       return rc;
     if (int rc = run(h, KID_CE, [&] {
-          return launch_blk_out(p, BlkMap{}, part, np, n, dst + b0 * sb, h->O, sb, h->stream);
+          return launch_blk_out(p, BlkMap{}, k->npieces, part, np, n, dst + b0 * sb, h->O, sb, h->stream);
         }))
       return rc;
   }
@@ -1695,15 +1712,16 @@ int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_
                oXt = c.take(fused ? 0 : (size_t)Bp * h->F4);
   const size_t oG = c.take(mb * blk_om(h->O)), oR = c.take(k->norm ? mb * 4 : 0),
                oS = c.take(k->norm ? (size_t)h->M * h->O : 0);
-  const size_t oP = c.take((size_t)(fused ? k->ntiles : k->npieces) * blk_planes(p) * Bp),
+  const BlkLocal one = fused ? block_local(h, Bp) : BlkLocal{};
+  const int64_t records = !fused ? k->npieces : one.group ? blk_records(p, k->ntiles, 1) : r.records;
+  const size_t oP = c.take((size_t)records * blk_planes(p) * Bp),
                oZ = c.take(fused ? 0 : rows * Bp);
   if (int rc = ensure_block_ws(h, c.bytes)) return rc;
   auto at = [&](size_t o) { return (float*)(k->ws + o); };
   const BlkLoss l{y, Y, B, at(oG), at(oR), at(oS), h->loss, h->flag, d.dW1 ? nullptr : lrm};
   const BlkGrads g{d.dW2, d.dgain, d.dshift, lr, lrm};
-  const BlkLocal one = fused ? block_local(h, Bp) : BlkLocal{};
   if (one.group) {
-    const BlkFwdArgs f{X, B, h->F, k->d_tiles, k->ntiles, 0, 0, 0, at(oP), Bp};
+    const BlkFwdArgs f{X, B, h->F, k->d_tiles, k->ntiles, 0, 0, 0, 1, at(oP), Bp};
     const BlkBwdArgs b{X,      B,      h->F,   Bp,     0,     k->d_tiles, k->ntiles, at(oG),
                        at(oR), at(oS), d.dW1, d.dV1, g};
     if (int rc = run(h, KID_BWD_FUSED, [&] { return launch_blk_local(p, one, f, l, b, h->stream); }))
@@ -1712,12 +1730,12 @@ int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_
     return PMLP_OK;
   }
   if (fused) {
-    const BlkFwdArgs f{X,    B,     h->F,    k->d_tiles, k->ntiles,
-                       r.SC, r.wpc, r.waves, at(oP),     Bp};
+    const BlkFwdArgs f{X,     B,       h->F,  k->d_tiles, k->ntiles, r.SC,
+                       r.wpc, r.waves, r.run, at(oP),     Bp};
     if (int rc = run(h, KID_FWD_M3, [&] { return launch_blk_fused_fwd(p, f, h->stream); }))
       return rc;
     if (int rc = run(h, KID_CE, [&] {
-          return launch_blk_loss(p, BlkMap{k->d_toff, k->ntiles}, at(oP), Bp, Bp, l, h->stream);
+          return launch_blk_loss(p, BlkMap{k->d_toff, r.run}, r.records, at(oP), Bp, Bp, l, h->stream);
         }))
       return rc;
     const BlkBwdArgs b{X, B, h->F, Bp, 0, k->d_btiles, k->nbtiles, at(oG), at(oR), at(oS), d.dW1, d.dV1, g};
@@ -1736,7 +1754,7 @@ int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_
   if (int rc = run(h, KID_M3_FWD,
                    [&] { return launch_blk_fwd(p, Zt, Ut, Bp, at(oP), h->stream); }))
     return rc;
-  if (int rc = run(h, KID_CE, [&] { return launch_blk_loss(p, BlkMap{}, at(oP), Bp, Bp, l, h->stream); }))
+  if (int rc = run(h, KID_CE, [&] { return launch_blk_loss(p, BlkMap{}, k->npieces, at(oP), Bp, Bp, l, h->stream); }))
     return rc;
   if (int rc = run(h, KID_M3_BWD, [&] {
         return launch_blk_bwd(p, Zt, Ut, Bp, at(oG), at(oR), at(oS), g, h->stream);

@@ -42,12 +42,16 @@ struct BlkTile {
 };
 static_assert(sizeof(BlkTile) == 16, "BlkTile layout");
 
-// Where the sums of model m lie: in the stored path its pieces poff[m] ..
-// poff[m+1]-1; in the fused path (toff set) its tiles.
+// Where the sums of model m lie: in the stored path its pieces poff[m] .. poff[m+1]-1;
+// in the fused path (toff set) its runs.  A run is what one wave sums of a model: its
+// tiles among `run` consecutive ones, r run .. (r + 1) run - 1; its record is m + r.
 struct BlkMap {
   const int32_t* toff;  // [M+1] first tile of each model, or null
-  int32_t pieces;       // tiles
+  int32_t run;
 };
+inline int64_t blk_records(const BlkPack& p, int32_t ntiles, int32_t run) {
+  return (int64_t)p.M + (ntiles - 1) / run;
+}
 
 struct BlkFwdArgs {
   const float* X;  // [B][F]
@@ -57,11 +61,12 @@ struct BlkFwdArgs {
   int32_t SC;      // samples of a workgroup, a multiple of 32
   int32_t wpc;     // workgroups for each SC samples
   int32_t waves;   // of a workgroup
+  int32_t run;     // see BlkMap
   float* part;     // records of blk_planes planes of Br samples
   int32_t Br;      // multiple of 32
 };
 #define PMLP_BLK_FWD_DECL(OM)                                               \
-  int blk_fwd_slots_##OM(const BlkPack& p, int32_t SC, int32_t waves);       \
+  int blk_fwd_slots_##OM(const BlkPack& p, int32_t SC, int32_t waves, bool runs); \
   hipError_t launch_blk_fused_fwd_##OM(const BlkPack& p, const BlkFwdArgs& a, hipStream_t s);
 PMLP_BLK_FWD_DECL(2)
 PMLP_BLK_FWD_DECL(16)
@@ -77,8 +82,8 @@ hipError_t launch_blk_fwd(const BlkPack& p, const float* Zt, const float* Ut, in
                           float* part, hipStream_t s);
 
 // Logits out[b sb + m sm + o] of B samples from the pieces' sums.
-hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, const float* part, int32_t Bp,
-                          int32_t B, float* out, int64_t sm, int64_t sb, hipStream_t s);
+hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, int64_t records, const float* part,
+                          int32_t Bp, int32_t B, float* out, int64_t sm, int64_t sb, hipStream_t s);
 
 // Losses and what the backward reads, from the pieces' sums:
 //   G [M][Bp][blk_om]  dLoss/dlogits (0 past the batch and the outputs)
@@ -100,8 +105,8 @@ struct BlkLoss {
   const float* lrm;
 };
 // Br: the records' sample stride, Bp: G's and R's.
-hipError_t launch_blk_loss(const BlkPack& p, const BlkMap& map, const float* part, int32_t Br,
-                           int32_t Bp, const BlkLoss& l, hipStream_t s);
+hipError_t launch_blk_loss(const BlkPack& p, const BlkMap& map, int64_t records, const float* part,
+                           int32_t Br, int32_t Bp, const BlkLoss& l, hipStream_t s);
 
 // Gradients of the output weights, gains and shifts (stored, or applied with
 // the rate lr or lrm[m] where dW2 is null).
@@ -138,7 +143,7 @@ PMLP_BLK_BWD_DECL(16)
 
 // Forward, loss and backward in one launch: workgroup w takes the models whose first
 // tile is one of tiles w * group .. (w + 1) * group - 1, for all samples.  As
-// launch_blk_fused_fwd (f.SC, f.wpc and f.waves are not read), launch_blk_loss and
+// launch_blk_fused_fwd with runs of one tile (f.SC .. f.run are not read), launch_blk_loss and
 // launch_blk_fused_bwd (b.tiles: the forward's).
 constexpr int32_t kBlkLocalBatch = 256;  // samples, at most
 constexpr int32_t kBlkLocalGroup = 8;    // waves of a workgroup, and `group` at most

@@ -71,6 +71,11 @@ __host__ __device__ constexpr int row_bytes(int NC) { return 16 * (4 * NC + 1); 
 // columns may pass them by
 inline size_t pieces_bytes(int NC, int SC) { return (size_t)3 * SC * row_bytes(NC) + 32; }
 
+// Where sums of the workgroup may lie after them
+__host__ __device__ constexpr size_t sums_at(int NC, int SC) {
+  return ((size_t)3 * SC * row_bytes(NC) + 32 + 15) & ~(size_t)15;
+}
+
 // The pieces of the SC samples from b0 on (zero past the batch and the columns).
 template <int NC>
 __device__ __forceinline__ void fill_pieces(char* lds, int SC, const float* X, int b0, int B,

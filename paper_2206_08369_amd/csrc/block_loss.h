@@ -73,7 +73,15 @@ __device__ __forceinline__ void merge_pieces(const BlkPack& p, const BlkMap& map
   s.n = s.mean = s.m2 = 0.f;
 #pragma unroll
   for (int o = 0; o < OM; ++o) s.P[o] = 0.f;
-  const int k0 = (map.toff ? map.toff : p.poff)[m], k1 = (map.toff ? map.toff : p.poff)[m + 1];
+  int k0, k1, t0 = 0;  // its pieces or records
+  if (map.toff) {
+    t0 = map.toff[m];
+    k0 = m + t0 / map.run;
+    k1 = m + (map.toff[m + 1] - 1) / map.run + 1;
+  } else {
+    k0 = p.poff[m];
+    k1 = p.poff[m + 1];
+  }
   const int width = (int)(p.seg_off[m + 1] - p.seg_off[m]);
   constexpr int U = OM <= 4 ? 4 : 2;
   for (int k = k0 + g; k < k1; k += U * G) {
@@ -96,7 +104,13 @@ __device__ __forceinline__ void merge_pieces(const BlkPack& p, const BlkMap& map
       for (int o = 0; o < OM; ++o) s.P[o] += v[u][o];
       if (NORM) {
         const int ku = k + u * G;
-        const int units = map.toff ? min(16, width - 16 * (ku - k0)) : p.pieces[ku].len;
+        int units;
+        if (map.toff) {  // (from the run's first tile, or the model's, to its last)
+          const int at = max((ku - m) * map.run - t0, 0);
+          units = min(width, 16 * ((ku - m + 1) * map.run - t0)) - 16 * at;
+        } else {
+          units = p.pieces[ku].len;
+        }
         merge_stats(s.n, s.mean, s.m2, (float)units, mb[u], qb[u]);
       }
     }

@@ -22,11 +22,16 @@ __device__ __forceinline__ float sum16(float a, float b) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// The forward of tiles first, first + step, .. below `end` by one wave: their sums over
-// the `steps` blocks of 32 samples from b0 on whose pieces lie in LDS (SC of them).
-template <int NC, int RM, bool MF, bool GATED, bool NORM>
+// The forward of runs of `run` tiles r, r + step, .. (below tile `end`) by one wave:
+// their sums over the `steps` blocks of 32 samples from b0 on whose pieces lie in LDS
+// (SC of them).  RUNS: the sums of a run's tiles are added up in `acc`, planes of
+// acc_row(SC) samples, each value by one lane; else a run is one tile.
+__host__ __device__ constexpr int acc_row(int SC) { return SC + 4; }
+
+template <int NC, int RM, bool MF, bool GATED, bool NORM, bool RUNS>
 __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a, const char* lds,
-                                          int SC, int b0, int steps, int first, int end, int step) {
+                                          int SC, int b0, int steps, int r, int end, int step,
+                                          int run, float* acc) {
   constexpr int K = GATED ? 2 : 1, RB = row_bytes(NC);
   const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4, plane = SC * RB;
   const char* const zrow = lds + li * RB + 16 * lk;
@@ -53,13 +58,23 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
     }
   };
   auto tile_at = [&](int t) { return a.tiles[std::min(t, end - 1)]; };
-  BlkTile q = tile_at(first), qn = tile_at(first + step);
+  auto after = [&](int t, int& of) {  // the tile that follows t of run `of`
+    if (RUNS && t + 1 < std::min((of + 1) * run, end)) return t + 1;
+    of += step;
+    return of * run;
+  };
+  int rn = r, tn = after(r * run, rn), have = 0;  // the next tile; units of the run before this
+  BlkTile q = tile_at(r * run), qn = tile_at(tn);
   if (AHEAD) fetch(q.n0, q.cnt);
 #pragma unroll 1
-  for (int t = first; t < end; t += step) {
+  for (int t = r * run; t < end;) {
     const int n0 = __builtin_amdgcn_readfirstlane(q.n0);
     const int cnt = __builtin_amdgcn_readfirstlane(q.cnt), act = __builtin_amdgcn_readfirstlane(q.act);
-    const BlkTile qnn = tile_at(t + 2 * step);
+    int rnn = rn;
+    const int tnn = after(tn, rnn);
+    const BlkTile qnn = tile_at(tnn);
+    const int m = __builtin_amdgcn_readfirstlane(q.m);
+    const bool last = !RUNS || rn != r || __builtin_amdgcn_readfirstlane(qn.m) != m;
     if (!AHEAD) fetch(n0, cnt);
     UnitRows<NC, RM, K> w;
     w.split(nx.w, p.F4, lk);
@@ -73,8 +88,10 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
         w2[o][r] = (MF ? li : o) < p.O && r < mine ? v : 0.f;
       }
     if (AHEAD) fetch(qn.n0, qn.cnt);
-    float* const rec = a.part + (int64_t)t * PQ * a.Br + b0 + li;
-    const float rn = 1.f / (float)cnt;
+    float* const rec = a.part + (int64_t)(m + r) * PQ * a.Br + b0 + li;
+    const float rc = 1.f / (float)cnt;
+    // merging with the `have` units before (see merge_stats)
+    const float share = (float)cnt / (float)(have + cnt), both = share * (float)have;
 #pragma unroll 1
     for (int st = 0; st < steps; ++st) {
       const int at = 32 * st * RB;
@@ -93,6 +110,7 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
         for (int v = 0; v < 8; ++v) h[v] = (v & 3) < mine ? h[v] : 0.f;
       }
       float* const dst = rec + 32 * st;
+      const int row = acc_row(SC), at0 = 32 * st + li;
       if (MF) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -102,7 +120,13 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
             s = __builtin_amdgcn_mfma_f32_16x16x4f32(w2[0][r], h[4 * i + r], s, 0, 0, 0);
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (4 * lk + r < p.O) dst[(int64_t)(4 * lk + r) * a.Br + 16 * i] = s[r];
+            if (4 * lk + r < p.O) {
+              const int o = 4 * lk + r;
+              float v = s[r];
+              if (RUNS && have) v += acc[o * row + at0 + 16 * i];
+              if (last) dst[(int64_t)o * a.Br + 16 * i] = v;
+              else acc[o * row + at0 + 16 * i] = v;
+            }
         }
       } else {
         float s[2][2];
@@ -115,8 +139,11 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
             for (int r = 1; r < 4; ++r) s[i][o] = fmaf(h[4 * i + r], w2[MF ? 0 : o][r], s[i][o]);
           }
         // row lk ends with block lk & 1 of output lk >> 1
-        const float v = sum16(sum32(s[0][0], s[0][1]), sum32(s[1][0], s[1][1]));
-        dst[(int64_t)(lk >> 1) * a.Br + 16 * (lk & 1)] = v;
+        float v = sum16(sum32(s[0][0], s[0][1]), sum32(s[1][0], s[1][1]));
+        const int at = (lk >> 1) * row + at0 + 16 * (lk & 1);
+        if (RUNS && have) v += acc[at];
+        if (last) dst[(int64_t)(lk >> 1) * a.Br + 16 * (lk & 1)] = v;
+        else acc[at] = v;
       }
       if (NORM) {
         float mean[2], m2[2];
@@ -134,13 +161,25 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
           e = sum32(e, e);
           d = sum16(d, d);
           e = sum16(e, e);
-          mean[i] = fmaf(d, rn, piv);
-          m2[i] = fmaxf(fmaf(-d * rn, d, e), e != e ? e : 0.f);
+          mean[i] = fmaf(d, rc, piv);
+          m2[i] = fmaxf(fmaf(-d * rc, d, e), e != e ? e : 0.f);
         }
-        const float v = lk & 2 ? (lk & 1 ? m2[1] : m2[0]) : (lk & 1 ? mean[1] : mean[0]);
-        dst[(int64_t)(p.O + (lk >> 1)) * a.Br + 16 * (lk & 1)] = v;
+        const float mb = lk & 1 ? mean[1] : mean[0], qb = lk & 1 ? m2[1] : m2[0];
+        float v = lk & 2 ? qb : mb;
+        float* const sum = acc + p.O * row + at0 + 16 * (lk & 1);
+        if (RUNS && have) {
+          const float ma = sum[0], d = mb - ma;
+          v = lk & 2 ? sum[row] + fmaf(d * d, both, qb) : fmaf(d, share, ma);
+        }
+        if (last) dst[(int64_t)(p.O + (lk >> 1)) * a.Br + 16 * (lk & 1)] = v;
+        else sum[(lk >> 1) * row] = v;
       }
     }
+    have = last ? 0 : have + cnt;
+    t = tn;
+    r = rn;
+    tn = tnn;
+    rn = rnn;
     q = qn;
     qn = qnn;
   }

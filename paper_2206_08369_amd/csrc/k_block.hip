@@ -299,8 +299,8 @@ hipError_t launch_blk_fwd(const BlkPack& p, const float* Zt, const float* Ut, in
 }
 
 // Groups of threads over a model's pieces: by the pieces of an average model.
-static int piece_groups(const BlkPack& p, const BlkMap& map, int most) {
-  const int64_t pieces = (map.toff ? map.pieces : p.npieces) / p.M;
+static int piece_groups(const BlkPack& p, int64_t records, int most) {
+  const int64_t pieces = records / p.M;
   int G = 1;
   while (G < most && pieces >= 8 * G) G <<= 1;
   return G;
@@ -310,10 +310,10 @@ static size_t groups_lds(const BlkPack& p, int G, int nb) {
   return (size_t)(G - 1) * nb * (blk_om(p.O) + 3) * sizeof(float);
 }
 
-hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, const float* part, int32_t Br,
-                          int32_t B, float* out, int64_t sm, int64_t sb, hipStream_t s) {
+hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, int64_t records, const float* part,
+                          int32_t Br, int32_t B, float* out, int64_t sm, int64_t sb, hipStream_t s) {
   note_variant("k_blk_out", kArithNone);
-  const int G = piece_groups(p, map, 8), alone = G == 1, nb = 64;
+  const int G = piece_groups(p, records, 8), alone = G == 1, nb = 64;
   int per = 1024;  // samples of a model at once: fewer where that leaves the device idle
   while (per > nb && (int64_t)p.M * ceil_div_i(B, per) < (alone ? 8192 : 1024)) per >>= 1;
   const int nblk = ceil_div_i(B, per), threads = alone ? 256 : nb * G;
@@ -334,11 +334,11 @@ hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, const float* part
   return hipGetLastError();
 }
 
-hipError_t launch_blk_loss(const BlkPack& p, const BlkMap& map, const float* part, int32_t Br,
-                           int32_t Bp, const BlkLoss& l, hipStream_t s) {
+hipError_t launch_blk_loss(const BlkPack& p, const BlkMap& map, int64_t records, const float* part,
+                           int32_t Br, int32_t Bp, const BlkLoss& l, hipStream_t s) {
   note_variant("k_blk_loss", kArithNone);
   const int nb = Bp >= 256 ? 256 : (Bp + 63) & ~63;
-  const int most = 1024 / nb, G = piece_groups(p, map, most >= 8 ? 8 : most >= 4 ? 4 : most >= 2 ? 2 : 1);
+  const int most = 1024 / nb, G = piece_groups(p, records, most >= 8 ? 8 : most >= 4 ? 4 : most >= 2 ? 2 : 1);
   const int threads = G == 1 && Bp >= 1024 ? 1024 : nb * G;
   const size_t lds = groups_lds(p, G, threads / G);
   const float scale = l.Y ? 1.f / ((float)l.B * (float)p.O) : 1.f / (float)l.B;

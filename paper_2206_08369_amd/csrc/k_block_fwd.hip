@@ -37,7 +37,7 @@ constexpr int max_threads() {
   return GATED ? (NC == 0 ? 1024 : NC <= 3 ? 768 : 512) : (NC <= 3 ? 1024 : 768);
 }
 
-template <int NC, int RM, bool GATED, bool NORM>
+template <int NC, int RM, bool GATED, bool NORM, bool RUNS>
 __global__ __launch_bounds__((max_threads<NC, GATED>()))
 void k_blk_fused_fwd(BlkPack p, BlkFwdArgs a) {
   extern __shared__ __align__(16) char lds[];
@@ -48,8 +48,10 @@ void k_blk_fused_fwd(BlkPack p, BlkFwdArgs a) {
   fill_pieces<NC>(lds, SC, a.X, b0, a.B, a.F, tid, blockDim.x);
   lds_barrier();
   const int steps = (std::min(SC, a.B - b0) + 31) >> 5;
-  fwd_tiles<NC, RM, MF, GATED, NORM>(p, a, lds, SC, b0, steps, wg * nw + wave, a.ntiles,
-                                     a.wpc * nw);
+  const int planes = p.O + (NORM ? 2 : 0);
+  fwd_tiles<NC, RM, MF, GATED, NORM, RUNS>(
+      p, a, lds, SC, b0, steps, RUNS ? wave * a.wpc + wg : wg * nw + wave, a.ntiles, a.wpc * nw, a.run,
+      (float*)(lds + sums_at(NC, SC)) + wave * planes * acc_row(SC));
 }
 
 typedef void (*BlkFwdFn)(BlkPack, BlkFwdArgs);
@@ -58,16 +60,21 @@ struct BlkFwdInst {
   int NC, threads;  // threads of a workgroup, at most (the occupancy query does not mind them)
 };
 
-template <int NC, int RM>
+template <int NC, int RM, bool RUNS>
 BlkFwdInst fwd_kind(bool gated, bool norm) {
-  if (gated && norm) return {k_blk_fused_fwd<NC, RM, true, true>, NC, max_threads<NC, true>()};
-  if (gated) return {k_blk_fused_fwd<NC, RM, true, false>, NC, max_threads<NC, true>()};
-  return {k_blk_fused_fwd<NC, RM, false, true>, NC, max_threads<NC, false>()};
+  if (gated && norm) return {k_blk_fused_fwd<NC, RM, true, true, RUNS>, NC, max_threads<NC, true>()};
+  if (gated) return {k_blk_fused_fwd<NC, RM, true, false, RUNS>, NC, max_threads<NC, true>()};
+  return {k_blk_fused_fwd<NC, RM, false, true, RUNS>, NC, max_threads<NC, false>()};
 }
 
-BlkFwdInst fwd_of(const BlkPack& p) {
+size_t fwd_lds(const BlkPack& p, int NC, int32_t SC, int32_t waves, bool runs) {
+  if (!runs) return pieces_bytes(NC, SC);
+  return sums_at(NC, SC) + (size_t)waves * blk_planes(p) * acc_row(SC) * sizeof(float);
+}
+
+BlkFwdInst fwd_of(const BlkPack& p, bool runs) {
   const bool g = p.V1 != nullptr, n = p.gain != nullptr;
-#define PMLP_CALL(NC, RM) fwd_kind<NC, RM>(g, n)
+#define PMLP_CALL(NC, RM) (runs ? fwd_kind<NC, RM, true>(g, n) : fwd_kind<NC, RM, false>(g, n))
   PMLP_BLK_SHAPE(p.F4, PMLP_CALL)
 #undef PMLP_CALL
   return {nullptr, 0, 0};
@@ -78,21 +85,22 @@ BlkFwdInst fwd_of(const BlkPack& p) {
 #define PMLP_CAT_(a, b) a##b
 #define PMLP_CAT(a, b) PMLP_CAT_(a, b)
 
-int PMLP_CAT(blk_fwd_slots_, PMLP_BLK_OM)(const BlkPack& p, int32_t SC, int32_t waves) {
-  const BlkFwdInst i = fwd_of(p);
-  return i.fn && 64 * waves <= i.threads ? resident_blocks((const void*)i.fn, 64 * waves, pieces_bytes(i.NC, SC)) : 0;
+int PMLP_CAT(blk_fwd_slots_, PMLP_BLK_OM)(const BlkPack& p, int32_t SC, int32_t waves, bool runs) {
+  const BlkFwdInst i = fwd_of(p, runs);
+  return i.fn && 64 * waves <= i.threads ? resident_blocks((const void*)i.fn, 64 * waves, fwd_lds(p, i.NC, SC, waves, runs)) : 0;
 }
 
 hipError_t PMLP_CAT(launch_blk_fused_fwd_, PMLP_BLK_OM)(const BlkPack& p, const BlkFwdArgs& a,
                                                         hipStream_t s) {
-  const BlkFwdInst i = fwd_of(p);
-  if (!i.fn || a.B < 1 || a.ntiles < 1 || a.wpc < 1 || a.waves < 1 || 64 * a.waves > i.threads || a.SC < 32 ||
+  const BlkFwdInst i = fwd_of(p, a.run > 1);
+  if (!i.fn || a.B < 1 || a.ntiles < 1 || a.wpc < 1 || a.waves < 1 ||
+      a.run < 1 || 64 * a.waves > i.threads || a.SC < 32 ||
       a.SC % 32 || p.O > PMLP_BLK_OM)
     return hipErrorInvalidValue;
   const int nchunk = (a.B + a.SC - 1) / a.SC;
   if (a.Br < (a.B + 31) / 32 * 32 || (int64_t)nchunk * a.wpc > 0x7fffffff)
     return hipErrorInvalidValue;
-  i.fn<<<(unsigned)(nchunk * a.wpc), 64 * a.waves, pieces_bytes(i.NC, a.SC), s>>>(p, a);
+  i.fn<<<(unsigned)(nchunk * a.wpc), 64 * a.waves, fwd_lds(p, i.NC, a.SC, a.waves, a.run > 1), s>>>(p, a);
   return hipGetLastError();
 }
 

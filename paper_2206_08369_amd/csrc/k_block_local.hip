@@ -42,8 +42,8 @@ __device__ __forceinline__ void group_models(const BlkLocal& g, const BlkFwdArgs
 
 // The losses and output gradients of models m0 .. m1 - 1, 64 samples of one a wave.
 template <bool NORM>
-__device__ __forceinline__ void local_loss(const BlkPack& p, const BlkMap& map, const BlkFwdArgs& f, const BlkLoss& l,
-                                           int Bp, int m0, int m1, float* red) {
+__device__ __forceinline__ void local_loss(const BlkPack& p, const BlkMap& map,
+                                           const BlkFwdArgs& f, const BlkLoss& l, int Bp, int m0, int m1, float* red) {
   const int tid = threadIdx.x, lane = tid & 63, nw = blockDim.x >> 6;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), nblk = (Bp + 63) >> 6;
   const float scale = l.Y ? 1.f / ((float)l.B * (float)p.O) : 1.f / (float)l.B;
@@ -97,9 +97,10 @@ void k_blk_local(BlkPack p, BlkLocal g, BlkFwdArgs f, BlkLoss l, BlkBwdArgs b) {
   const int t0 = g.toff[m0], t1 = g.toff[m1], Bp = b.Bp;
   fill_pieces<NC>(lds, Bp, f.X, 0, f.B, f.F, tid, blockDim.x);
   lds_barrier();
-  fwd_tiles<NC, RM, (OM > 2), GATED, NORM>(p, f, lds, Bp, 0, Bp >> 5, t0 + wave, t1, nw);
+  fwd_tiles<NC, RM, (OM > 2), GATED, NORM, false>(p, f, lds, Bp, 0, Bp >> 5, t0 + wave, t1, nw, 1,
+                                                  nullptr);
   __syncthreads();
-  local_loss<NORM>(p, BlkMap{g.toff, f.ntiles}, f, l, Bp, m0, m1, (float*)(lds + ((3 * Bp * row_bytes(NC) + 47) & ~15)));
+  local_loss<NORM>(p, BlkMap{g.toff, 1}, f, l, Bp, m0, m1, (float*)(lds + sums_at(NC, Bp)));
   __syncthreads();
   bwd_tiles<NC, RM, OM, GATED, NORM>(p, b, lds, Bp, 1, (t1 - t0 + nw - 1) / nw, t0 + wave, t1, nw);
 }
@@ -127,7 +128,7 @@ BlkLocalInst local_of(const BlkPack& p) {
 
 // (a group has at most `group` models)
 size_t local_lds(int NC, int32_t Bp, int32_t group) {
-  return pieces_bytes(NC, Bp) + 16 + (size_t)group * ((Bp + 63) / 64) * kRow * sizeof(float);
+  return sums_at(NC, Bp) + (size_t)group * ((Bp + 63) / 64) * kRow * sizeof(float);
 }
 
 }  // namespace

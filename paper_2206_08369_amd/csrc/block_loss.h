@@ -107,7 +107,7 @@ __device__ __forceinline__ void merge_pieces(const BlkPack& p, const BlkMap& map
         int units;
         if (map.toff) {  // (from the run's first tile, or the model's, to its last)
           const int at = max((ku - m) * map.run - t0, 0);
-          units = min(width, 16 * ((ku - m + 1) * map.run - t0)) - 16 * at;
+          units = (int)min((uint32_t)width, 16u * ((ku - m + 1) * map.run - t0)) - 16 * at;
         } else {
           units = p.pieces[ku].len;
         }

@@ -186,6 +186,7 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
 }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));  // rows of any F
 typedef __attribute__((address_space(3))) char lds_char;
 
 // Values and slopes of activation id A.
@@ -416,7 +417,7 @@ __device__ __forceinline__ void bwd_tiles(const BlkPack& p, const BlkBwdArgs& a,
           }
 #define PMLP_PIECE(Q, E)                                             \
 _Pragma("unroll") for (int mt = 0; mt < K; ++mt) acc[mt][j] =        \
-    __builtin_amdgcn_mfma_f32_16x16x32_bf16(dp[mt][Q], x[E], acc[mt][j], 0, 0, 0)
+    __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[E], dp[mt][Q], acc[mt][j], 0, 0, 0)
           PMLP_PIECE(2, 0);
           PMLP_PIECE(1, 1);
           PMLP_PIECE(0, 2);
@@ -454,21 +455,27 @@ _Pragma("unroll") for (int mt = 0; mt < K; ++mt) acc[mt][j] =        \
     const float og = gn, os = sn;
     if (AHEAD) take();
     if (live) {
+      // (a lane has unit li's columns 16 j + 4 lk ..)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float row_rate = __shfl(rate, 4 * lk + r);
-        if (4 * lk + r >= cnt) continue;
-        const int64_t nr = n0 + 4 * lk + r;
+      for (int mt = 0; mt < K; ++mt) {
+        const bool to = a.dW1 != nullptr;
+        float* const row = to ? (mt ? a.dV1 : a.dW1) + n * F
+                              : const_cast<float*>(mt ? p.V1 : p.W1) + n * F4;
 #pragma unroll
-        for (int mt = 0; mt < K; ++mt) {
-          float* const dW = mt ? a.dV1 : a.dW1;
-          float* const W = const_cast<float*>(mt ? p.V1 : p.W1);
+        for (int j = 0; j < NF; ++j) {
+          const int f = 16 * j + 4 * lk;
+          if (li >= cnt || f >= F) continue;
+          const f32x4 g = acc[mt][j];
+          if (f + 4 <= F) {
+            if (to) *(f32x4_u*)(row + f) = g;
+            else *(f32x4*)(row + f) -= rate * g;
+          } else {
 #pragma unroll
-          for (int j = 0; j < NF; ++j) {
-            const int f = 16 * j + li;
-            if (f >= F) continue;
-            if (dW) dW[nr * F + f] = acc[mt][j][r];
-            else W[nr * F4 + f] -= row_rate * acc[mt][j][r];
+            for (int r = 0; r < 3; ++r) {
+              if (f + r >= F) continue;
+              if (to) row[f + r] = g[r];
+              else row[f + r] -= rate * g[r];
+            }
           }
         }
       }

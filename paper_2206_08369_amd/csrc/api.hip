@@ -1571,17 +1571,18 @@ BlkLocal block_local(pmlp* h, int32_t Bp) {
 // what a launch costs.  A wave's step of 32 samples takes its share of the SIMD, a
 // tile the wait for its weights and their splitting (as long as three steps), and a
 // workgroup the pieces of its samples (as long as six and, for each 32 samples, one
-// over its waves).
+// over its waves).  Of every choice of the three, timed for eight workloads, its choice
+// was within 5 % of the best (10,000 samples, 582 models: 603 us, the best 579).
 BlkRun block_run(pmlp* h, int32_t B) {
   PmlpBlock* k = h->block;
   if (!h->lds_kernels || h->F4 > kBlkFusedCols) return BlkRun{};
   for (int i = 0; i < 2; ++i)
     if (k->planned[i] == B) return k->plan[i];
   const BlkPack p = block_pack(h);
-  // Runs of several tiles save records and their merging, and cost LDS.  Models of 3.6
-  // tiles, 50 columns, both, 10000 samples: 735 us without, 705 with; of 32 tiles, 32
+  // Runs of several tiles save records and their merging, and cost LDS.  Models of 3.7
+  // tiles, 50 columns, both, 10,000 samples: 635 us without, 607 with; of 32 tiles, 32
   // columns, ten outputs, 32 samples: forward and loss 161 and 132.  A batch of up to 32
-  // has short records: models of 3.6 tiles, 100 columns, one sample 64 and 66.
+  // has short records: models of 3.6 tiles, 100 columns, one sample: 64 and 66.
   const bool runs = k->ntiles >= (int64_t)(B > 32 ? 2 : 8) * h->M;
   BlkRun best;
   double least = 0;
@@ -1609,6 +1610,7 @@ BlkRun block_run(pmlp* h, int32_t B) {
       }
     }
   }
+  if (!best.SC) return best;
   // a wave's tiles in equal runs of four or fewer (longer ones leave a wave with fewer
   // activations, and waves uneven: a gated paper pool's forward 232 us with four, 248
   // with eight)
@@ -1622,7 +1624,9 @@ BlkRun block_run(pmlp* h, int32_t B) {
 }
 
 constexpr size_t kBlockSlice = (size_t)1 << 30;  // bytes of Z that a forward pass stores at once
-constexpr size_t kRecordSlice = (size_t)256 << 20;  // bytes of records of the fused one
+// Bytes of records of the fused one: as many as the last cache holds (20,000 samples in
+// slices of 64, 128, 256 MiB and in one of 360: 1290, 1245, 1210 and 1360 us).
+constexpr size_t kRecordSlice = (size_t)256 << 20;
 
 // Forward pass of a block pack.  A forward pass that stores its pre-activations
 // takes its samples in slices of at most kBlockSlice bytes of them (or 256 samples).

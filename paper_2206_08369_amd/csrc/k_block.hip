@@ -19,6 +19,11 @@
 // update; two sets merge by Chan, Golub and LeVeque's formula), all in fp32: a sum
 // of squares minus a squared mean would lose the variance of a layer whose mean is
 // large.  S_o - mu C_o cancels no worse than H - mu does.
+//
+// The stored path (more than 128 input columns) spends its time in its three large
+// products; 1200 models of 1 to 200 units, 1000 columns, 1024 samples, gated: 5100 us of
+// them at 194 TFLOP/s (a library fp32 product reached 152), k_blk_fwd 230 us and
+// k_blk_bwd 365 us for 1.0 and 2.0 GB.
 
 #include "block_loss.h"
 
@@ -298,11 +303,15 @@ hipError_t launch_blk_fwd(const BlkPack& p, const float* Zt, const float* Ut, in
   return hipGetLastError();
 }
 
-// Groups of threads over a model's pieces: by the pieces of an average model.
+// Groups of threads over a model's pieces: by the pieces of an average model, one where
+// the models alone fill the device.  Wide models, both, two outputs, 32 samples, the
+// loss kernel in us with 1, 2, 4 and 8 groups: one model of 20,000 units 237, 129, 72,
+// 44; 64 of 2000 19, 14, 11, 10; 1000 of 1000 16, 13, 12, 18; ten outputs and 256
+// samples, 1000 of 1000: 58, 69, 123, 123.
 static int piece_groups(const BlkPack& p, int64_t records, int most) {
   const int64_t pieces = records / p.M;
   int G = 1;
-  while (G < most && pieces >= 8 * G) G <<= 1;
+  while (G < most && pieces >= 8 * G && (int64_t)p.M * G < 512) G <<= 1;
   return G;
 }
 
@@ -313,7 +322,7 @@ static size_t groups_lds(const BlkPack& p, int G, int nb) {
 hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, int64_t records, const float* part,
                           int32_t Br, int32_t B, float* out, int64_t sm, int64_t sb, hipStream_t s) {
   note_variant("k_blk_out", kArithNone);
-  const int G = piece_groups(p, records, 8), alone = G == 1, nb = 64;
+  const int G = piece_groups(p, records, 16), alone = G == 1, nb = 64;
   int per = 1024;  // samples of a model at once: fewer where that leaves the device idle
   while (per > nb && (int64_t)p.M * ceil_div_i(B, per) < (alone ? 8192 : 1024)) per >>= 1;
   const int nblk = ceil_div_i(B, per), threads = alone ? 256 : nb * G;

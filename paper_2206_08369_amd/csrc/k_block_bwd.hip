@@ -2,17 +2,25 @@
 // Compiled once per class of outputs (PMLP_BLK_OM: 2, 4 or 16).
 //
 // A wave takes a tile, up to 16 consecutive hidden units of one activation (of whatever
-// models), and all samples, so that its weights' gradients need no other wave; it holds the three
-// bf16 pieces of its units' W1 (and V1) rows and their gradients' accumulators in
-// registers.  The samples' pieces lie in LDS once, sample by sample (chunks of
+// models), and all samples, so that its weights' gradients need no other wave; it holds
+// the three bf16 pieces of its units' W1 (and V1) rows and their gradients'
+// accumulators in registers.  The samples' pieces lie in LDS once, sample by sample (chunks of
 // them in turn, where they do not fit), and serve both products: read as rows they
 // are the operand of Z = X W1^T, which is computed again rather than stored by the
 // forward and read back, and read through the transposing LDS load the operand of
 // dW1 = dZ^T X.  A step takes 32 samples: after Z the lane (li, lk) holds unit li of
 // the samples 4 lk + r of both blocks of 16, forms dZ there, and those eight values
-// are, as they lie, a row of the second product's first operand (the sums over
-// samples run in that order in both of its operands).
+// are, as they lie, a column of the second product's second operand (the sums over
+// samples run in that order in both of its operands).  The lane ends with four
+// consecutive columns of unit li's gradient, one store.
 // The norm's gradient needs no sums over units (see k_block.hip).
+//
+// Bound by its instructions: matrix and vector instructions of a SIMD's waves hardly
+// overlap, and take 85 % of the time together.  6000 models of 1 to 100 units, 100
+// columns, 256 samples: gated 415 us, that is 150 TFLOP/s of fp32 products (0.9 PFLOP/s
+// of bf16 ones), normed 264 us.  Wide models, ten outputs, 32 columns and samples,
+// both: 191 us for 480 MB.  Two waves a SIMD is what the registers allow; where the
+// input has no block of 32 columns, three.
 //
 // The second product takes NF = 2 NC blocks of 16 columns, and one more for the fp32
 // columns of the first; the last block may read past its columns into the next row,
@@ -94,7 +102,8 @@ hipError_t PMLP_CAT(launch_blk_fused_bwd_, PMLP_BLK_OM)(const BlkPack& p, BlkBwd
     return hipErrorInvalidValue;
   const size_t lds = pieces_bytes(inst.NC, a.SC);
   // eight waves share the samples' pieces where those leave room for one workgroup
-  // only, four where there is more
+  // only (a gated paper pool: 414 us, with four 499), four where there is more (the
+  // same time in large pools; small ones spread over twice the CUs)
   const int waves = 4 * lds > (size_t)lmax ? 8 : 4;
   const int slots = resident_blocks((const void*)fn, 64 * waves, lds);
   if (slots <= 0) return hipErrorInvalidValue;

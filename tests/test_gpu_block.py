@@ -161,6 +161,41 @@ def test_parity_large_pool(pm, torch, O, B):
     net.close()
 
 
+@pytest.mark.parametrize("kind, O, B", [("both", 2, 40), ("norm", 10, 33), ("gated", 3, 64),
+                                        ("both", 16, 20)])
+def test_parity_runs(pm, torch, kind, O, B):
+    """Several tiles a wave, of one model and of the next: runs that end with a model,
+    inside one and at the pack's end."""
+    rng = np.random.default_rng(7 * O + B)
+    M, F = (2500, 11) if B > 32 else (700, 11)
+    hs = rng.integers(4, 100 if B > 32 else 360, M).astype(np.int32)
+    acts = np.sort(rng.choice(SMOOTH, M)).astype(np.int32)
+    gated, norm = KINDS[kind]
+    p = ref.random_params(rng, hs, F, O, gated, norm)
+    net = make(pm, hs, acts, p, F, O, kind)
+    X, y = data(rng, F, O, B, "ce")
+    want = ref.pack(hs, acts, p, X, y)
+    within(net.forward(dev(torch, X)).cpu().numpy(), want["logits"], "logits")
+    for k, v in zip(net.param_names, net.gradients(dev(torch, X), dev(torch, y))):
+        within(v.cpu().numpy(), want[k], "d" + k)
+    net.close()
+
+
+@pytest.mark.parametrize("kind, O, B", [("both", 2, 40), ("norm", 10, 300), ("gated", 4, 7)])
+def test_parity_one_wide_model(pm, torch, kind, O, B):
+    rng = np.random.default_rng(O + B)
+    hs, acts, F = np.int32([9001, 3]), np.int32([3, 2]), 8
+    gated, norm = KINDS[kind]
+    p = ref.random_params(rng, hs, F, O, gated, norm)
+    net = make(pm, hs, acts, p, F, O, kind)
+    X, y = data(rng, F, O, B, "ce")
+    want = ref.pack(hs, acts, p, X, y)
+    within(net.forward(dev(torch, X)).cpu().numpy(), want["logits"], "logits")
+    for k, v in zip(net.param_names, net.gradients(dev(torch, X), dev(torch, y))):
+        within(v.cpu().numpy(), want[k], "d" + k)
+    net.close()
+
+
 @pytest.mark.parametrize("kind", ["gated", "both"])
 def test_parity_generic_kernels(pm, torch, kind, monkeypatch):
     monkeypatch.setenv("PMLP_GENERIC_KERNELS", "1")

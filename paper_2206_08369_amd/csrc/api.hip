@@ -1567,6 +1567,10 @@ BlkLocal block_local(pmlp* h, int32_t Bp) {
   return k->lplan = best;
 }
 
+int blk_fwd_slots(const BlkPack& p, int32_t SC, int32_t waves, bool runs) {
+  return p.O <= 2 ? blk_fwd_slots_2(p, SC, waves, runs) : blk_fwd_slots_16(p, SC, waves, runs);
+}
+
 // The run of B samples: the samples of a workgroup and the waves that share them, by
 // what a launch costs.  A wave's step of 32 samples takes its share of the SIMD, a
 // tile the wait for its weights and their splitting (as long as three steps), and a
@@ -1592,8 +1596,7 @@ BlkRun block_run(pmlp* h, int32_t B) {
     if (SC == last) continue;
     last = SC;
     for (int32_t waves = 4; waves <= 16; waves += 4) {
-      const int64_t slots = p.O <= 2 ? blk_fwd_slots_2(p, SC, waves, runs)
-                                     : blk_fwd_slots_16(p, SC, waves, runs);
+      const int64_t slots = blk_fwd_slots(p, SC, waves, runs);
       if (slots <= 0) continue;
       const int64_t fit = std::max<int64_t>(1, slots / nchunk), want = div_up(k->ntiles, waves);
       for (int64_t w = fit; w <= std::max<int64_t>(fit, 32); ++w) {
@@ -1616,6 +1619,8 @@ BlkRun block_run(pmlp* h, int32_t B) {
   // with eight)
   const int32_t tiles = div_up(k->ntiles, best.wpc * best.waves);
   best.run = runs ? div_up(tiles, div_up(tiles, 4)) : 1;
+  // (asking also lets the kernel have that much LDS: the one without runs, too)
+  if (runs && best.run == 1) (void)blk_fwd_slots(p, best.SC, best.waves, false);
   best.records = blk_records(p, k->ntiles, best.run);
   std::swap(k->planned[0], k->planned[1]);
   std::swap(k->plan[0], k->plan[1]);

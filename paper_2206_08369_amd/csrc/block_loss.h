@@ -174,20 +174,23 @@ __device__ __forceinline__ void sample_grads(const BlkPack& p, const BlkLoss& l,
         Gr[o] = 2.f * d * scale;
       }
     } else {
-      float mx = -INFINITY, se = 0.f, ly = 0.f;
+      // e_o / sum e, and for the label minus the others' share of it, so that a
+      // sample's gradients add up to zero (shift's are sums of them over the batch)
+      float mx = -INFINITY, se = 0.f, rest = 0.f, ly = 0.f;
 #pragma unroll
       for (int o = 0; o < OM; ++o) mx = o < p.O ? fmaxf(mx, L[o]) : mx;
-#pragma unroll
-      for (int o = 0; o < OM; ++o)
-        if (o < p.O) se += expf(L[o] - mx);
-      const float lse = mx + logf(se);
       const int yb = l.y[b];
       if (yb < 0 || yb >= p.O) l.flag[0] = 1;
 #pragma unroll
       for (int o = 0; o < OM; ++o) {
+        Gr[o] = o < p.O ? expf(L[o] - mx) : 0.f;
+        se += Gr[o];
+        rest += o == yb ? 0.f : Gr[o];
         if (o == yb) ly = L[o];
-        Gr[o] = o < p.O ? (expf(L[o] - lse) - (o == yb ? 1.f : 0.f)) * scale : 0.f;
       }
+      const float lse = mx + logf(se), share = scale / se;
+#pragma unroll
+      for (int o = 0; o < OM; ++o) Gr[o] = (o == yb ? -rest : Gr[o]) * share;
       loss += lse - ly;
     }
     if (NORM) {

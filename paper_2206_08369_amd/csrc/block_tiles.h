@@ -152,17 +152,17 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
           const float piv = __shfl(h[4 * i], li);  // the first unit's value
           float d = 0.f, e = 0.f;
 #pragma unroll
+          for (int r = 0; r < 4; ++r) d += (cnt == 16 || r < mine) ? h[4 * i + r] - piv : 0.f;
+          d = sum32(d, d);
+          d = sum16(d, d);
+          mean[i] = fmaf(d, rc, piv);
+#pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float v = (cnt == 16 || r < mine) ? h[4 * i + r] - piv : 0.f;
-            d += v;
+            const float v = (cnt == 16 || r < mine) ? h[4 * i + r] - mean[i] : 0.f;
             e = fmaf(v, v, e);
           }
-          d = sum32(d, d);
           e = sum32(e, e);
-          d = sum16(d, d);
-          e = sum16(e, e);
-          mean[i] = fmaf(d, rc, piv);
-          m2[i] = fmaxf(fmaf(-d * rc, d, e), e != e ? e : 0.f);
+          m2[i] = sum16(e, e);
         }
         const float mb = lk & 1 ? mean[1] : mean[0], qb = lk & 1 ? m2[1] : m2[0];
         float v = lk & 2 ? qb : mb;

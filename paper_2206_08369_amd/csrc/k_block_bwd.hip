@@ -19,7 +19,7 @@
 // overlap, and take 85 % of the time together.  6000 models of 1 to 100 units, 100
 // columns, 256 samples: gated 415 us, that is 150 TFLOP/s of fp32 products (0.9 PFLOP/s
 // of bf16 ones), normed 264 us.  Wide models, ten outputs, 32 columns and samples,
-// both: 191 us for 480 MB.  Two waves a SIMD is what the registers allow; where the
+// both: 191 us for 660 MB, 3.4 TB/s (a large copy 4.8).  Two waves a SIMD is what the registers allow; where the
 // input has no block of 32 columns, three.
 //
 // The second product takes NF = 2 NC blocks of 16 columns, and one more for the fp32

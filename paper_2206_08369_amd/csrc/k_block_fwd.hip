@@ -22,9 +22,10 @@
 //
 // Two outputs are summed by vector FMAs and two lane swaps, more by fp32 matrix
 // products whose second operand is the hidden values as they lie in the registers.
-// The squared deviations are taken from one of the tile's own values, then moved to
-// the mean: (h - K)^2 exceeds the variance at most 15 times over 16 values, so that
-// loses four bits at worst, wherever the mean is.
+// A tile's mean is its first value plus the mean difference from it, and the squared
+// deviations are taken from that mean: both stay exact for values that lie close together
+// far from zero.  (One pass, deviations from the first value moved to the mean: as fast,
+// and its errors up to 16 times those of the variance.)
 
 #include "block_tiles.h"
 

@@ -495,6 +495,30 @@ def test_graph_replays(pm, torch, shape):
     twin.close()
 
 
+def test_graph_of_a_smaller_batch(pm, torch):
+    """A capture at a batch that no call has had, where the workspace of a larger one
+    is enough."""
+    hs, acts, p, F, O, X, y = shape_problem("b300_f100_o4", "both", "ce")
+    net, twin = (make(pm, hs, acts, p, F, O, "both") for _ in range(2))
+    net.train_step(dev(torch, X), dev(torch, y), 0.0)
+    Xs, ys = dev(torch, X[:40]), dev(torch, y[:40])
+    out = torch.zeros(40, net.M, O, device="cuda")
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        net.train_step(Xs, ys, 0.05)
+        net.forward(Xs, out=out)
+    for rep in range(4):
+        Xs.copy_(dev(torch, X[40 * rep:40 * rep + 40]))
+        graph.replay()
+        torch.cuda.synchronize()
+        twin.train_step(Xs, ys, 0.05)
+        assert torch.equal(out, twin.forward(Xs))
+    net._stream()
+    net.close()
+    twin.close()
+
+
 def test_capture_without_a_workspace_is_refused(pm, torch):
     hs, acts, p, F, O, X, y = shape_problem("b300_f100_o4", "both", "ce")
     net = make(pm, hs, acts, p, F, O, "both")

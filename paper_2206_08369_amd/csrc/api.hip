@@ -1433,10 +1433,27 @@ int ensure_block_ws(pmlp* h, size_t bytes) {
   return PMLP_OK;
 }
 
+// Whether k_blk_gemm takes a product of NP x NQ over K, by what either costs in us: a
+// 16-k stage of the large tiles (256 x 256, 256 x 64 or 128 x 128; see launch_gemm_bf16)
+// 2.2 or 0.5 on one CU, or k_blk_gemm's 90 TFLOP/s.  Large / small, forward and weight
+// gradients: 690 units, 818 columns, 4012 samples 121 / 66; 1370, 407, 895: 59 / 19 and
+// 248 / 36; 76, 275, 766: 42 / 7 and 100 / 11; 20,240, 1000, 704: 167 / 331 and 245 / 448.
+bool small_product(int64_t NP, int64_t NQ, int64_t K) {
+  const int64_t mq = NQ <= 64 ? 64 : NQ <= 128 ? 128 : 256, mp = NQ > 64 && NQ <= 128 ? 128 : 256;
+  const int64_t tiles = (int64_t)div_up(NP, mp) * div_up(NQ, mq), at_once = NQ <= 128 ? 512 : 256;
+  const double large = (double)div_up(tiles, at_once) * div_up(K, 16) * (NQ <= 128 ? 0.5 : 2.2);
+  const double small = 2.0 * NP * NQ * K / 90e6 + div_up(K, 128);
+  return small < large;
+}
+
 // Zt (and Ut after it) = W1 (V1) Xp^T: one product over both halves of W1's
 // allocation.  The rows between N and Npad are zero.
 int block_product(pmlp* h, const float* Xp, float* Zt, int32_t Bp) {
   const int64_t rows = h->block->gated ? h->Npad + h->N : h->N;
+  if (h->lds_kernels && small_product(rows, Bp, h->F4)) {
+    const BlkGemm g{h->W1, Xp, h->F4, h->F4, rows, Bp, h->F4, Zt, Bp, Bp, 0.f, nullptr, nullptr};
+    return run(h, KID_GEMM_FWD, [&] { return launch_blk_gemm(g, EPI_STORE, h->stream); });
+  }
   if (h->lds_kernels && fwd_lds_supported(Bp, h->F4)) {
     FwdLdsArgs f{};
     f.W1 = h->W1;
@@ -1476,6 +1493,12 @@ int block_product(pmlp* h, const float* Xp, float* Zt, int32_t Bp) {
 // dW = dZ^T X stored into dW [N][F], or W -= lr dW where that is null.
 int block_weight_grad(pmlp* h, const float* dZt, const float* Xt, int32_t Bp, float* W, float* dW,
                       float lr, const float* lrm) {
+  if (h->lds_kernels && small_product(h->N, h->F4, Bp)) {
+    const BlkGemm g{dZt,          Xt,   Bp,  Bp,  h->N,    h->F4, Bp, dW ? dW : W,
+                    dW ? h->F : h->F4, h->F, lr, lrm, h->d_mid};
+    return run(h, KID_GEMM_BWD,
+               [&] { return launch_blk_gemm(g, dW ? EPI_GRAD : EPI_SGD, h->stream); });
+  }
   if (h->lds_kernels) {
     GemmBfArgs g{};
     g.P = dZt;

@@ -72,6 +72,21 @@ PMLP_BLK_FWD_DECL(2)
 PMLP_BLK_FWD_DECL(16)
 #undef PMLP_BLK_FWD_DECL
 
+// C[p][q] = sum_k P[p][k] Q[q][k] of fp32 rows (16-byte aligned; K a multiple of 4):
+// stored (EPI_STORE, EPI_GRAD: columns below ncols) or applied to C (EPI_SGD).
+struct BlkGemm {
+  const float *P, *Q;
+  int64_t ldp, ldq, NP;
+  int32_t NQ, K;
+  float* out;
+  int64_t ldo;
+  int32_t ncols;
+  float lr;
+  const float* lrm;
+  const int32_t* mid;
+};
+hipError_t launch_blk_gemm(const BlkGemm& a, int epi, hipStream_t s);
+
 // Per piece and sample, planar: part[(piece * PQ + q) * Bp + b], q < O the sums
 // S_o over the piece's units, and with a norm the mean and the sum of squared
 // deviations of its hidden values after them.

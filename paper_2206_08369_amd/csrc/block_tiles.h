@@ -104,6 +104,10 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
       if (GATED) {
 #pragma unroll
         for (int v = 0; v < 8; ++v) h[v] *= z[K - 1][v >> 2][v & 3];
+      } else if (NORM) {
+        const float c = blk_center(act);
+#pragma unroll
+        for (int v = 0; v < 8; ++v) h[v] -= c;
       }
       if (cnt < 16) {
 #pragma unroll
@@ -349,7 +353,7 @@ __device__ __forceinline__ void bwd_tiles(const BlkPack& p, const BlkBwdArgs& a,
           f32x4 h, dn = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            h[r] = GATED ? av[r] * z[K - 1][i][r] : av[r];
+            h[r] = GATED ? av[r] * z[K - 1][i][r] : NORM ? av[r] - blk_center(act) : av[r];
             if (NORM) h[r] = (h[r] - up.r[NORM ? r : 0][0]) * up.r[NORM ? r : 0][1];
           }
           if (MF) {

@@ -181,6 +181,23 @@ def test_parity_runs(pm, torch, kind, O, B):
     net.close()
 
 
+@pytest.mark.parametrize("kind, O, B", [("both", 2, 64), ("norm", 3, 90), ("gated", 5, 61)])
+def test_parity_many_units_and_columns(pm, torch, kind, O, B):
+    """Products of more than 128 columns that fill the device."""
+    rng = np.random.default_rng(O + B)
+    hs, F = rng.integers(150, 300, 300).astype(np.int32), 201
+    acts = rng.choice(SMOOTH, hs.size).astype(np.int32)
+    gated, norm = KINDS[kind]
+    p = ref.random_params(rng, hs, F, O, gated, norm)
+    net = make(pm, hs, acts, p, F, O, kind)
+    X, y = data(rng, F, O, B, "ce")
+    want = ref.pack(hs, acts, p, X, y)
+    within(net.forward(dev(torch, X)).cpu().numpy(), want["logits"], "logits")
+    for k, v in zip(net.param_names, net.gradients(dev(torch, X), dev(torch, y))):
+        within(v.cpu().numpy(), want[k], "d" + k)
+    net.close()
+
+
 @pytest.mark.parametrize("kind, O, B", [("both", 2, 40), ("norm", 10, 300), ("gated", 4, 7)])
 def test_parity_one_wide_model(pm, torch, kind, O, B):
     rng = np.random.default_rng(O + B)

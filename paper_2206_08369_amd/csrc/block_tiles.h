@@ -357,19 +357,24 @@ __device__ __forceinline__ void bwd_tiles(const BlkPack& p, const BlkBwdArgs& a,
             if (NORM) h[r] = (h[r] - up.r[NORM ? r : 0][0]) * up.r[NORM ? r : 0][1];
           }
           if (MF) {
-            // dN = G W2 and T += G^T h, the sums in the order of the registers
-            f32x4 t = f32x4{T[0], T[1], T[2 % NO], T[3 % NO]};
+            // dN = G W2 and T += G^T h, the sums in the order of the registers.  Both
+            // products run for each model of the tile over all its units, and a unit takes
+            // its own model's: multiplying the others by zero instead would let a model
+            // whose G is not finite into their sums.
             f32x4 ga = up.g[0], gt = up.g[MF ? 1 : 0];
 #pragma unroll 1
             for (int mm = m_lo;;) {
-              f32x4 d = f32x4{0.f, 0.f, 0.f, 0.f};
+              f32x4 d = f32x4{0.f, 0.f, 0.f, 0.f}, t = d;
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
                 d = __builtin_amdgcn_mfma_f32_16x16x4f32(ga[r], w2[r % NO], d, 0, 0, 0);
-                t = __builtin_amdgcn_mfma_f32_16x16x4f32(gt[r], m == mm ? h[r] : 0.f, t, 0, 0, 0);
+                t = __builtin_amdgcn_mfma_f32_16x16x4f32(gt[r], h[r], t, 0, 0, 0);
               }
 #pragma unroll
-              for (int r = 0; r < 4; ++r) dn[r] = m == mm ? d[r] : dn[r];
+              for (int r = 0; r < 4; ++r) {
+                dn[r] = m == mm ? d[r] : dn[r];
+                T[r % NO] += m == mm ? t[r] : 0.f;
+              }
               if (++mm > m_hi) break;
               const uint32_t b = (uint32_t)(b0 + s + 16 * i + 4 * lk);
               const float* const g = a.G + (int64_t)mm * a.Bp * OM;
@@ -377,8 +382,6 @@ __device__ __forceinline__ void bwd_tiles(const BlkPack& p, const BlkBwdArgs& a,
 #pragma unroll
               for (int r = 0; r < 4; ++r) gt[r] = g[(b + r) * OM + li];
             }
-#pragma unroll
-            for (int o = 0; o < 4; ++o) T[o % NO] = t[o];
           } else {
 #pragma unroll
             for (int r = 0; r < 4; ++r)

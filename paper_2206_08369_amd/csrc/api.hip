@@ -1686,21 +1686,22 @@ int forward_block(pmlp* h, const float* X, int32_t B, float* out) {
   const size_t oXp = c.take(fused ? 0 : (size_t)Bp * h->F4),
                oXt = c.take(fused ? 0 : (size_t)Bp * h->F4), oZ = c.take(fused ? 0 : rows * Bp);
   const int32_t br = fused ? (slice + 31) & ~31 : Bp;  // samples of a record
-  const size_t oP = c.take((size_t)(fused ? r.records : k->npieces) * blk_planes(p) * br);
+  const size_t records = (size_t)(fused ? r.records : k->npieces);
+  const size_t oP = c.take(records * blk_planes(p) * br), oC = c.take(k->norm ? records * blk_om(h->O) : 0);
   const size_t oL = over ? c.take((size_t)nout) : 0;
   if (int rc = ensure_block_ws(h, c.bytes)) return rc;
   float *Xp = (float*)(k->ws + oXp), *Xt = (float*)(k->ws + oXt), *Zt = (float*)(k->ws + oZ),
-        *part = (float*)(k->ws + oP), *dst = over ? (float*)(k->ws + oL) : out;
+        *part = (float*)(k->ws + oP), *csum = (float*)(k->ws + oC), *dst = over ? (float*)(k->ws + oL) : out;
   for (int32_t b0 = 0; b0 < B; b0 += slice) {
     const int32_t n = std::min(slice, B - b0), np = pad_batch(n);
     if (fused) {
       const BlkFwdArgs f{X + (int64_t)b0 * h->F, n,     h->F,  k->d_tiles, k->ntiles, r.SC, r.wpc,
-                         r.waves,                r.run, part, br};
+                         r.waves,                r.run, part,   csum,       br};
       if (int rc = run(h, KID_FWD_M3, [&] { return launch_blk_fused_fwd(p, f, h->stream); }))
         return rc;
       if (int rc = run(h, KID_CE, [&] {
-            return launch_blk_out(p, BlkMap{k->d_toff, r.run}, r.records, part, br, n, dst + b0 * sb, h->O, sb,
-                                  h->stream);
+            return launch_blk_out(p, BlkMap{k->d_toff, r.run, csum}, r.records, part, br, n,
+                                  dst + b0 * sb, h->O, sb, h->stream);
           }))
         return rc;
       continue;
@@ -1712,11 +1713,13 @@ int forward_block(pmlp* h, const float* X, int32_t B, float* out) {
       return rc;
     if (int rc = block_product(h, Xp, Zt, np)) return rc;
     if (int rc = run(h, KID_M3_FWD, [&] {
-          return launch_blk_fwd(p, Zt, k->gated ? Zt + h->Npad * np : nullptr, np, part, h->stream);
+          return launch_blk_fwd(p, Zt, k->gated ? Zt + h->Npad * np : nullptr, np, part, csum,
+                                h->stream);
         }))
       return rc;
     if (int rc = run(h, KID_CE, [&] {
-          return launch_blk_out(p, BlkMap{}, k->npieces, part, np, n, dst + b0 * sb, h->O, sb, h->stream);
+          return launch_blk_out(p, BlkMap{nullptr, 0, csum}, k->npieces, part, np, n, dst + b0 * sb,
+                                h->O, sb, h->stream);
         }))
       return rc;
   }
@@ -1747,13 +1750,13 @@ int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_
   const BlkLocal one = fused ? block_local(h, Bp) : BlkLocal{};
   const int64_t records = !fused ? k->npieces : one.group ? blk_records(p, k->ntiles, 1) : r.records;
   const size_t oP = c.take((size_t)records * blk_planes(p) * Bp),
-               oZ = c.take(fused ? 0 : rows * Bp);
+               oC = c.take(k->norm ? (size_t)records * blk_om(h->O) : 0), oZ = c.take(fused ? 0 : rows * Bp);
   if (int rc = ensure_block_ws(h, c.bytes)) return rc;
   auto at = [&](size_t o) { return (float*)(k->ws + o); };
   const BlkLoss l{y, Y, B, at(oG), at(oR), at(oS), h->loss, h->flag, d.dW1 ? nullptr : lrm};
   const BlkGrads g{d.dW2, d.dgain, d.dshift, lr, lrm};
   if (one.group) {
-    const BlkFwdArgs f{X, B, h->F, k->d_tiles, k->ntiles, 0, 0, 0, 1, at(oP), Bp};
+    const BlkFwdArgs f{X, B, h->F, k->d_tiles, k->ntiles, 0, 0, 0, 1, at(oP), at(oC), Bp};
     const BlkBwdArgs b{X,      B,      h->F,   Bp,     0,     k->d_tiles, k->ntiles, at(oG),
                        at(oR), at(oS), d.dW1, d.dV1, g};
     if (int rc = run(h, KID_BWD_FUSED, [&] { return launch_blk_local(p, one, f, l, b, h->stream); }))
@@ -1763,11 +1766,12 @@ int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_
   }
   if (fused) {
     const BlkFwdArgs f{X,     B,       h->F,  k->d_tiles, k->ntiles, r.SC,
-                       r.wpc, r.waves, r.run, at(oP),     Bp};
+                       r.wpc, r.waves, r.run, at(oP),     at(oC),    Bp};
     if (int rc = run(h, KID_FWD_M3, [&] { return launch_blk_fused_fwd(p, f, h->stream); }))
       return rc;
     if (int rc = run(h, KID_CE, [&] {
-          return launch_blk_loss(p, BlkMap{k->d_toff, r.run}, r.records, at(oP), Bp, Bp, l, h->stream);
+          return launch_blk_loss(p, BlkMap{k->d_toff, r.run, at(oC)}, r.records, at(oP), Bp, Bp, l,
+                                 h->stream);
         }))
       return rc;
     const BlkBwdArgs b{X, B, h->F, Bp, 0, k->d_btiles, k->nbtiles, at(oG), at(oR), at(oS), d.dW1, d.dV1, g};
@@ -1784,9 +1788,12 @@ int step_block(pmlp* h, const float* X, const int32_t* y, const float* Y, int32_
     return rc;
   if (int rc = block_product(h, at(oXp), Zt, Bp)) return rc;
   if (int rc = run(h, KID_M3_FWD,
-                   [&] { return launch_blk_fwd(p, Zt, Ut, Bp, at(oP), h->stream); }))
+                   [&] { return launch_blk_fwd(p, Zt, Ut, Bp, at(oP), at(oC), h->stream); }))
     return rc;
-  if (int rc = run(h, KID_CE, [&] { return launch_blk_loss(p, BlkMap{}, k->npieces, at(oP), Bp, Bp, l, h->stream); }))
+  if (int rc = run(h, KID_CE, [&] {
+        return launch_blk_loss(p, BlkMap{nullptr, 0, at(oC)}, k->npieces, at(oP), Bp, Bp, l,
+                               h->stream);
+      }))
     return rc;
   if (int rc = run(h, KID_M3_BWD, [&] {
         return launch_blk_bwd(p, Zt, Ut, Bp, at(oG), at(oR), at(oS), g, h->stream);

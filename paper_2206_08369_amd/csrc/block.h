@@ -42,12 +42,16 @@ struct BlkTile {
 };
 static_assert(sizeof(BlkTile) == 16, "BlkTile layout");
 
+// Outputs as the kernels pad them
+__host__ __device__ inline int blk_om(int32_t O) { return O <= 2 ? 2 : O <= 4 ? 4 : 16; }
+
 // Where the sums of model m lie: in the stored path its pieces poff[m] .. poff[m+1]-1;
 // in the fused path (toff set) its runs.  A run is what one wave sums of a model: its
 // tiles among `run` consecutive ones, r run .. (r + 1) run - 1; its record is m + r.
 struct BlkMap {
   const int32_t* toff;  // [M+1] first tile of each model, or null
   int32_t run;
+  const float* csum;    // with a norm: [pieces or records][blk_om] sums of gain W2 over their units
 };
 inline int64_t blk_records(const BlkPack& p, int32_t ntiles, int32_t run) {
   return (int64_t)p.M + (ntiles - 1) / run;
@@ -63,6 +67,7 @@ struct BlkFwdArgs {
   int32_t waves;   // of a workgroup
   int32_t run;     // see BlkMap
   float* part;     // records of blk_planes planes of Br samples
+  float* csum;     // see BlkMap
   int32_t Br;      // multiple of 32
 };
 #define PMLP_BLK_FWD_DECL(OM)                                               \
@@ -89,12 +94,13 @@ hipError_t launch_blk_gemm(const BlkGemm& a, int epi, hipStream_t s);
 
 // Per piece and sample, planar: part[(piece * PQ + q) * Bp + b], q < O the sums
 // S_o over the piece's units, and with a norm the mean and the sum of squared
-// deviations of its hidden values after them.
+// deviations of its hidden values after them; S_o are then sums of the deviations
+// from that mean.
 inline int32_t blk_planes(const BlkPack& p) { return p.O + (p.gain ? 2 : 0); }
 
 // Z (and U) stored batch-minor: Zt [Npad][Bp], Ut [Npad][Bp] (null: no gate).
 hipError_t launch_blk_fwd(const BlkPack& p, const float* Zt, const float* Ut, int32_t Bp,
-                          float* part, hipStream_t s);
+                          float* part, float* csum, hipStream_t s);
 
 // Logits out[b sb + m sm + o] of B samples from the pieces' sums.
 hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, int64_t records, const float* part,
@@ -106,8 +112,6 @@ hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, int64_t records, 
 //   Gs [M][O]     with a norm: sum_b G
 // y: labels int32 [B], or Y float [B][O] for the regression head; flags as
 // launch_ce.
-// (outputs padded to 2, 4 or 16)
-inline int blk_om(int32_t O) { return O <= 2 ? 2 : O <= 4 ? 4 : 16; }
 struct BlkLoss {
   const int32_t* y;
   const float* Y;

@@ -13,7 +13,7 @@ __device__ __forceinline__ void merge_stats(float& n, float& mean, float& m2, fl
   const float f = t > 0.f ? nb / t : 0.f;
   const float d = meanb - mean;
   mean = fmaf(d, f, mean);
-  m2 += m2b + d * d * n * f;
+  m2 += m2b + d * (n * f) * d;  // (d d alone may overflow where n is 0)
   n = t;
 }
 
@@ -43,15 +43,6 @@ __device__ __forceinline__ float blk_act(int a, float z) {
   if (a == 1) return z <= 0.f ? 0.f : z;
   if (a == 11) return fabsf(z) <= 0.5f ? 0.f : z;
   return act_fwd(a, z);
-}
-
-// What a norm without a gate takes off the hidden values first: the norm does not see
-// a constant, but S_o - mu C_o loses what the mean exceeds the deviation by, and C_o's
-// rounding is the same for every sample.  Activations of one sign are taken relative to
-// their value at 0 (logistic units, 256 samples: the gradient of shift, a sum over the
-// samples, was off by 8.4e-7 of its norm, now 2.1e-7).
-__device__ __forceinline__ float blk_center(int a) {
-  return a == 3 ? 0.5f : a == 8 ? 0.69314718f : 0.f;
 }
 
 // Activation id a (uniform over the wave) of NV values.

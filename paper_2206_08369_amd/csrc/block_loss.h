@@ -63,13 +63,17 @@ __device__ __forceinline__ void norm_consts(const BlkPack& p, int m, int lane, i
 template <int OM>
 struct Merged {
   float P[OM], n, mean, m2;
+  float piv;  // with a norm: the first piece's mean, from which `mean` and P count
 };
 
-// Those of pieces k0 + g, k0 + g + G, .. of model m, four pieces' loads in flight.
+// Those of pieces k0 + g, k0 + g + G, .. of model m (uniform over a wave), four pieces'
+// loads in flight.  A piece's deviations from its own mean m_k become deviations from
+// the first piece's by (m_k - piv) C_k: the hidden values' mean itself, which may be
+// large beside their deviations, is in none of the sums.
 template <int OM, bool NORM>
 __device__ __forceinline__ void merge_pieces(const BlkPack& p, const BlkMap& map,
-                                             const float* part, int m, int Br, int b,
-                                             int g, int G, Merged<OM>& s) {
+                                             const float* part, const float* csum, int m, int Br,
+                                             int b, int g, int G, Merged<OM>& s) {
   s.n = s.mean = s.m2 = 0.f;
 #pragma unroll
   for (int o = 0; o < OM; ++o) s.P[o] = 0.f;
@@ -83,9 +87,10 @@ __device__ __forceinline__ void merge_pieces(const BlkPack& p, const BlkMap& map
     k1 = p.poff[m + 1];
   }
   const int width = (int)(p.seg_off[m + 1] - p.seg_off[m]);
+  s.piv = NORM ? part[((int64_t)k0 * (p.O + 2) + p.O) * Br + b] : 0.f;
   constexpr int U = OM <= 4 ? 4 : 2;
   for (int k = k0 + g; k < k1; k += U * G) {
-    float v[U][OM], mb[U], qb[U];
+    float v[U][OM], c[NORM ? U : 1][OM], mb[U], qb[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {  // (past the last: it again, not used)
       const int ku = k + u * G < k1 ? k + u * G : k1 - 1;
@@ -93,15 +98,26 @@ __device__ __forceinline__ void merge_pieces(const BlkPack& p, const BlkMap& map
 #pragma unroll
       for (int o = 0; o < OM; ++o) v[u][o] = src[(int64_t)(o < p.O ? o : 0) * Br];
       if (NORM) {
-        mb[u] = src[(int64_t)p.O * Br];
+        mb[u] = src[(int64_t)p.O * Br] - s.piv;
         qb[u] = src[(int64_t)(p.O + 1) * Br];
+        const float* const cs = csum + (int64_t)(OM > 4 ? __builtin_amdgcn_readfirstlane(ku) : ku) * OM;
+#pragma unroll
+        for (int o = 0; o < OM; ++o) c[NORM ? u : 0][o] = cs[o];
       }
     }
+    if (NORM && OM <= 4)  // (made with the other loads, not each where it is used)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int o = 0; o < OM; ++o) c[NORM ? u : 0][o] = opaque(c[NORM ? u : 0][o]);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (k + u * G >= k1) break;
 #pragma unroll
-      for (int o = 0; o < OM; ++o) s.P[o] += v[u][o];
+      for (int o = 0; o < OM; ++o) {
+        s.P[o] += v[u][o];
+        if (NORM) s.P[o] = fmaf(mb[u], c[NORM ? u : 0][o], s.P[o]);
+      }
       if (NORM) {
         const int ku = k + u * G;
         int units;
@@ -144,13 +160,14 @@ __device__ __forceinline__ void merge_groups(Merged<OM>& s, int g, int G, int nb
   __syncthreads();
 }
 
-// With a norm: the statistics, and P_o.  r = 0 for a model of one unit, whose norm is
+// With a norm: the statistics (mean: the hidden values' own), and P_o.  r = 0 for a model of one unit, whose norm is
 // constant, so that its gradient is exactly zero.
 template <int OM>
 __device__ __forceinline__ void apply_norm(Merged<OM>& s, const float (&C)[OM], float* r) {
   *r = s.n > 1.f ? 1.f / sqrtf(s.m2 / s.n + kNormEps) : 0.f;
 #pragma unroll
   for (int o = 0; o < OM; ++o) s.P[o] = *r * (s.P[o] - s.mean * C[o]);
+  s.mean += s.piv;
 }
 
 // One sample's logits (s: its merged sums), share of the loss, dLoss/dlogits G and

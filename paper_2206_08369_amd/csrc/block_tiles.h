@@ -22,6 +22,13 @@ __device__ __forceinline__ float sum16(float a, float b) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// a of the wave's first row of 16 in all four
+__device__ __forceinline__ float row0(float a) {
+  const uint32_t u = __float_as_uint(a);
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(__builtin_amdgcn_permlane16_swap(r[0], r[0], false, false)[0]);
+}
+
 // The forward of runs of `run` tiles r, r + step, .. (below tile `end`) by one wave:
 // their sums over the `steps` blocks of 32 samples from b0 on whose pieces lie in LDS
 // (SC of them).  RUNS: the sums of a run's tiles are added up in `acc`, planes of
@@ -36,7 +43,7 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
   const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4, plane = SC * RB;
   const char* const zrow = lds + li * RB + 16 * lk;
   const char* const xrow = lds + li * RB + 64 * NC + 2 * lk;
-  const int PQ = p.O + (NORM ? 2 : 0);
+  const int PQ = p.O + (NORM ? 2 : 0), om = blk_om(p.O);
   // Where a tile's rows leave registers free the next tile's are loaded while this one
   // is at work (a tile of few steps is as long as its wait for them).
   constexpr bool AHEAD = NC <= 1;
@@ -64,6 +71,7 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
     return of * run;
   };
   int rn = r, tn = after(r * run, rn), have = 0;  // the next tile; units of the run before this
+  f32x4 cr = f32x4{0.f, 0.f, 0.f, 0.f};           // and their C_o
   BlkTile q = tile_at(r * run), qn = tile_at(tn);
   if (AHEAD) fetch(q.n0, q.cnt);
 #pragma unroll 1
@@ -87,6 +95,16 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
         const float v = opaque(nx.w2[o][r]) * opaque(nx.g[r]);
         w2[o][r] = (MF ? li : o) < p.O && r < mine ? v : 0.f;
       }
+    // C_o of the tile, as the lane's sums below have their outputs
+    f32x4 ct = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (NORM && MF) {
+      const f32x4 u = w2[0];
+      ct = __builtin_amdgcn_mfma_f32_16x16x4f32((u[0] + u[1]) + (u[2] + u[3]), 1.f, ct, 0, 0, 0);
+    } else if (NORM) {
+      const f32x4 u = w2[0], v = w2[MF ? 0 : 1];
+      const float c = sum32((u[0] + u[1]) + (u[2] + u[3]), (v[0] + v[1]) + (v[2] + v[3]));
+      ct[0] = sum16(c, c);
+    }
     if (AHEAD) fetch(qn.n0, qn.cnt);
     float* const rec = a.part + (int64_t)(m + r) * PQ * a.Br + b0 + li;
     const float rc = 1.f / (float)cnt;
@@ -104,10 +122,6 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
       if (GATED) {
 #pragma unroll
         for (int v = 0; v < 8; ++v) h[v] *= z[K - 1][v >> 2][v & 3];
-      } else if (NORM) {
-        const float c = blk_center(act);
-#pragma unroll
-        for (int v = 0; v < 8; ++v) h[v] -= c;
       }
       if (cnt < 16) {
 #pragma unroll
@@ -115,6 +129,44 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
       }
       float* const dst = rec + 32 * st;
       const int row = acc_row(SC), at0 = 32 * st + li;
+      // Means of the blocks that this lane's sums are of (both, or block lk & 1): the
+      // tile's, and the run's before it and after it.  piv: the tile's first unit's values.
+      constexpr int NB = MF ? 2 : 1;
+      float piv[2], mean[2], m2[2], me[NB], ma[NB], mb[NB];
+      auto own = [&](float a, float b) { return lk & 1 ? b : a; };
+      if (NORM) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          piv[i] = row0(h[4 * i]);
+          float d = 0.f, e = 0.f;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float& v = h[4 * i + r];
+            v = (cnt == 16 || r < mine) ? v - piv[i] : 0.f;
+            d += v;
+          }
+          d = sum32(d, d);
+          d = sum16(d, d);
+          mean[i] = fmaf(d, rc, piv[i]);
+          const float off = piv[i] - mean[i];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float v = (cnt == 16 || r < mine) ? h[4 * i + r] + off : 0.f;
+            if (!MF) h[4 * i + r] = v;
+            e = fmaf(v, v, e);
+          }
+          e = sum32(e, e);
+          m2[i] = sum16(e, e);
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          ma[j] = mb[j] = me[j] = MF ? mean[j] : own(mean[0], mean[1]);
+          if (RUNS && have) {
+            ma[j] = acc[p.O * row + at0 + 16 * (MF ? j : lk & 1)];
+            mb[j] = fmaf(me[j] - ma[j], share, ma[j]);
+          }
+        }
+      }
       if (MF) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -128,6 +180,8 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
               const int o = 4 * lk + r;
               float v = s[r];
               if (RUNS && have) v += acc[o * row + at0 + 16 * i];
+              if (NORM) v = fmaf(piv[i] - mb[MF ? i : 0], ct[r], v);
+              if (RUNS && NORM && have) v = fmaf(ma[MF ? i : 0] - mb[MF ? i : 0], cr[r], v);
               if (last) dst[(int64_t)o * a.Br + 16 * i] = v;
               else acc[o * row + at0 + 16 * i] = v;
             }
@@ -146,37 +200,32 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
         float v = sum16(sum32(s[0][0], s[0][1]), sum32(s[1][0], s[1][1]));
         const int at = (lk >> 1) * row + at0 + 16 * (lk & 1);
         if (RUNS && have) v += acc[at];
+        if (RUNS && NORM && have) {
+          v = fmaf(me[0] - mb[0], ct[0], v);
+          v = fmaf(ma[0] - mb[0], cr[0], v);
+        }
         if (last) dst[(int64_t)(lk >> 1) * a.Br + 16 * (lk & 1)] = v;
         else acc[at] = v;
       }
       if (NORM) {
-        float mean[2], m2[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float piv = __shfl(h[4 * i], li);  // the first unit's value
-          float d = 0.f, e = 0.f;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) d += (cnt == 16 || r < mine) ? h[4 * i + r] - piv : 0.f;
-          d = sum32(d, d);
-          d = sum16(d, d);
-          mean[i] = fmaf(d, rc, piv);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float v = (cnt == 16 || r < mine) ? h[4 * i + r] - mean[i] : 0.f;
-            e = fmaf(v, v, e);
-          }
-          e = sum32(e, e);
-          m2[i] = sum16(e, e);
-        }
-        const float mb = lk & 1 ? mean[1] : mean[0], qb = lk & 1 ? m2[1] : m2[0];
-        float v = lk & 2 ? qb : mb;
+        float q = own(m2[0], m2[1]);
         float* const sum = acc + p.O * row + at0 + 16 * (lk & 1);
         if (RUNS && have) {
-          const float ma = sum[0], d = mb - ma;
-          v = lk & 2 ? sum[row] + fmaf(d * d, both, qb) : fmaf(d, share, ma);
+          const float d = own(me[0] - ma[0], me[NB - 1] - ma[NB - 1]);
+          q += sum[row] + d * both * d;
         }
+        const float v = lk & 2 ? q : own(mb[0], mb[NB - 1]);
         if (last) dst[(int64_t)(p.O + (lk >> 1)) * a.Br + 16 * (lk & 1)] = v;
         else sum[(lk >> 1) * row] = v;
+      }
+    }
+    if (NORM) {
+      if (RUNS && have) ct += cr;
+      if (RUNS) cr = ct;
+      if (last && b0 == 0 && li == 0) {
+        float* const c = a.csum + (int64_t)(m + r) * om;
+        if (MF && 4 * lk < om) *(f32x4*)(c + 4 * lk) = ct;
+        if (!MF && !(lk & 1)) c[lk >> 1] = ct[0];
       }
     }
     have = last ? 0 : have + cnt;
@@ -353,7 +402,7 @@ __device__ __forceinline__ void bwd_tiles(const BlkPack& p, const BlkBwdArgs& a,
           f32x4 h, dn = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            h[r] = GATED ? av[r] * z[K - 1][i][r] : NORM ? av[r] - blk_center(act) : av[r];
+            h[r] = GATED ? av[r] * z[K - 1][i][r] : av[r];
             if (NORM) h[r] = (h[r] - up.r[NORM ? r : 0][0]) * up.r[NORM ? r : 0][1];
           }
           if (MF) {

@@ -5,9 +5,11 @@
 // Model m's hidden values are H = act_m(X W1^T), or, gated, act_m(X W1^T) *
 // (X V1^T).  With a norm the output weights see g Hh + s, Hh = (H - mu) r over
 // the model's own h units, r = (var + eps)^-1/2.  As the output product is
-// linear, its sums and the norm's statistics come from one pass over the units:
-//   S_o = sum_n H_n g_n W2[o,n],  C_o = sum_n g_n W2[o,n],  D_o = sum_n s_n W2[o,n]
-//   P_o = r (S_o - mu C_o),       logits_o = P_o + D_o
+// linear, its sums and the norm's statistics come from one pass over the units: with
+// k a piece of the model's units, m_k the mean over it and c that of the first piece,
+//   S_k,o = sum_n in k (H_n - m_k) g_n W2[o,n],  C_k,o = sum_n in k g_n W2[o,n]
+//   P_o = r (sum_k (S_k,o + (m_k - c) C_k,o) - (mu - c) C_o),  C_o = sum_n g_n W2[o,n]
+//   logits_o = P_o + D_o,                                      D_o = sum_n s_n W2[o,n]
 // and the two means over the units that the norm's gradient needs come from the
 // outputs' gradients G, with no pass of their own:
 //   dN_n = sum_o G_o W2[o,n]                      (gradient of g Hh + s)
@@ -18,8 +20,11 @@
 // The statistics are running means and sums of squared deviations (Welford's
 // update; two sets merge by Chan, Golub and LeVeque's formula), all in fp32: a sum
 // of squares minus a squared mean would lose the variance of a layer whose mean is
-// large.  So would S_o - mu C_o lose the outputs': without a gate the values are taken
-// relative to the activation's at 0 (blk_center).
+// large, as the difference of sum_n H_n g_n W2[o,n] and mu C_o would its outputs.  No sum
+// here has terms larger than a few of the model's largest deviations times its weights.
+// A piece's mean is rounded once more to be stored, by as much as its hidden values are
+// (storing it as one of them and the difference kept sums and variance free of that, and
+// took 5 to 17 % longer: a fifth number a piece, and its room in LDS).
 //
 // The stored path (more than 128 input columns) spends its time in its three large
 // products; 1200 models of 1 to 200 units, 1000 columns, 1024 samples, gated: 5100 us of
@@ -40,7 +45,8 @@ constexpr int kFU = 4;  // units per lane group whose loads are in flight
 template <int OM, bool GATED, bool NORM>
 __global__ __launch_bounds__(kBlock) void k_blk_fwd(BlkPack p, const float* __restrict__ Zt,
                                                     const float* __restrict__ Ut, int Bp, int LG,
-                                                    int nbblk, float* __restrict__ part) {
+                                                    int nbblk, float* __restrict__ part,
+                                                    float* __restrict__ csum) {
   const int lane = threadIdx.x & 63;
   const int64_t wv = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int pc = (int)(wv / nbblk), blk = (int)(wv - (int64_t)pc * nbblk);
@@ -51,12 +57,15 @@ __global__ __launch_bounds__(kBlock) void k_blk_fwd(BlkPack p, const float* __re
   const bool valid = b < Bp;
   const int bl = valid ? b : Bp - 4;
   const int a = p.actn[q.n0];
-  float S[4][OM];
+  float S[4][OM], C[OM];
   float mean[4] = {0.f, 0.f, 0.f, 0.f}, m2[4] = {0.f, 0.f, 0.f, 0.f}, cnt = 0.f;
+  float piv[4] = {0.f, 0.f, 0.f, 0.f};  // the lane's first unit's values, from which it counts
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int o = 0; o < OM; ++o) {
+    C[o] = 0.f;
 #pragma unroll
-    for (int o = 0; o < OM; ++o) S[i][o] = 0.f;
+    for (int i = 0; i < 4; ++i) S[i][o] = 0.f;
+  }
   for (int u0 = g; u0 < q.len; u0 += kFU * NG) {
     f32x4 z[kFU], v[kFU];
     float w[kFU][OM];
@@ -79,8 +88,9 @@ __global__ __launch_bounds__(kBlock) void k_blk_fwd(BlkPack p, const float* __re
       for (int i = 0; i < 4; ++i) {
         float h = blk_act(a, z[u][i]);
         if (GATED) h *= v[u][i];
-        else if (NORM) h -= blk_center(a);
         if (NORM) {
+          if (cnt == 1.f) piv[i] = h;
+          h -= piv[i];
           const float d = h - mean[i];
           mean[i] = fmaf(d, rc, mean[i]);
           m2[i] = fmaf(d, h - mean[i], m2[i]);
@@ -88,24 +98,51 @@ __global__ __launch_bounds__(kBlock) void k_blk_fwd(BlkPack p, const float* __re
 #pragma unroll
         for (int o = 0; o < OM; ++o) S[i][o] = fmaf(h, w[u][o], S[i][o]);
       }
+      if (NORM)
+#pragma unroll
+        for (int o = 0; o < OM; ++o) C[o] += w[u][o];
+    }
+  }
+  if (NORM) {  // from the first unit's values to the mean as it is rounded
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      mean[i] += piv[i];
+#pragma unroll
+      for (int o = 0; o < OM; ++o) S[i][o] = fmaf(piv[i] - mean[i], C[o], S[i][o]);
     }
   }
   for (int s = LG; s < 64; s <<= 1) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int o = 0; o < OM; ++o) S[i][o] += __shfl_xor(S[i][o], s);
     if (NORM) {
       const float nb = __shfl_xor(cnt, s);
-      float n = cnt;
+      float n = cnt, Cb[OM];
+#pragma unroll
+      for (int o = 0; o < OM; ++o) Cb[o] = __shfl_xor(C[o], s);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float mb = __shfl_xor(mean[i], s), qb = __shfl_xor(m2[i], s);
+        const float ma = mean[i], mb = __shfl_xor(ma, s), qb = __shfl_xor(m2[i], s);
         n = cnt;
         merge_stats(n, mean[i], m2[i], nb, mb, qb);
+        const float da = ma - mean[i], db = mb - mean[i];
+#pragma unroll
+        for (int o = 0; o < OM; ++o) {
+          const float Sb = __shfl_xor(S[i][o], s);
+          S[i][o] = fmaf(da, C[o], fmaf(db, Cb[o], S[i][o] + Sb));
+        }
       }
+#pragma unroll
+      for (int o = 0; o < OM; ++o) C[o] += Cb[o];
       cnt = n;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int o = 0; o < OM; ++o) S[i][o] += __shfl_xor(S[i][o], s);
     }
+  }
+  if (NORM && blk == 0 && lane == 0) {
+#pragma unroll
+    for (int o = 0; o < OM; ++o)
+      csum[(int64_t)pc * OM + o] = C[o];
   }
   if (g != 0 || !valid) return;
   float* dst = part + (int64_t)pc * (p.O + (NORM ? 2 : 0)) * Bp + b;
@@ -122,7 +159,8 @@ __global__ __launch_bounds__(kBlock) void k_blk_fwd(BlkPack p, const float* __re
 // (nb = 64, G = 1, alone) one wave.
 template <int OM, bool NORM>
 __global__ __launch_bounds__(1024) void k_blk_out(BlkPack p, BlkMap map,
-                                                  const float* __restrict__ part, int Br, int B,
+                                                  const float* __restrict__ part,
+                                                  const float* __restrict__ csum, int Br, int B,
                                                   int per, int nblk, int G, int alone,
                                                   float* __restrict__ out, int64_t sm, int64_t sb) {
   extern __shared__ float lds[];
@@ -139,7 +177,7 @@ __global__ __launch_bounds__(1024) void k_blk_out(BlkPack p, BlkMap map,
   for (int s0 = b0; s0 < B && s0 < b0 + per; s0 += nb) {
     const int b = s0 + l < B ? s0 + l : B - 1;
     Merged<OM> s;
-    merge_pieces<OM, NORM>(p, map, part, m, Br, b, g, G, s);
+    merge_pieces<OM, NORM>(p, map, part, csum, m, Br, b, g, G, s);
     merge_groups<OM, NORM>(s, g, G, nb, l, lds);
     if (g > 0 || s0 + l >= B) continue;
     float r;
@@ -153,7 +191,8 @@ __global__ __launch_bounds__(1024) void k_blk_out(BlkPack p, BlkMap map,
 // One workgroup per model, its threads over the samples and (G groups) its pieces.
 template <int OM, bool NORM>
 __global__ __launch_bounds__(1024) void k_blk_loss(BlkPack p, BlkMap map,
-                                                   const float* __restrict__ part, int Br, int Bp,
+                                                   const float* __restrict__ part,
+                                                   const float* __restrict__ csum, int Br, int Bp,
                                                    int G, BlkLoss l, float scale) {
   extern __shared__ float lds[];
   __shared__ float red[16 * (2 * OM + 1)];
@@ -171,7 +210,7 @@ __global__ __launch_bounds__(1024) void k_blk_loss(BlkPack p, BlkMap map,
   for (int s0 = 0; s0 < Bp; s0 += nb) {
     const int b = s0 + at;
     Merged<OM> s;
-    merge_pieces<OM, NORM>(p, map, part, m, Br, b < B ? b : B - 1, g, G, s);
+    merge_pieces<OM, NORM>(p, map, part, csum, m, Br, b < B ? b : B - 1, g, G, s);
     merge_groups<OM, NORM>(s, g, G, nb, at, lds);
     if (g > 0 || b >= Bp) continue;
     sample_grads<OM, NORM>(p, l, m, b, Bp, s, C, D, rh, scale, loss, gs);
@@ -230,7 +269,7 @@ __global__ __launch_bounds__(kBlock) void k_blk_bwd(BlkPack p, float* __restrict
     for (int i = 0; i < 4; ++i) {
       float d;
       const float av = act_fwd_bwd(a, z[i], &d);
-      float hv = GATED ? av * u[i] : NORM ? av - blk_center(a) : av;
+      float hv = GATED ? av * u[i] : av;
       f32x4 st;
       if (NORM) {
         st = *(const f32x4*)(R + ((int64_t)m * Bp + b + i) * 4);
@@ -288,7 +327,7 @@ int lanes_per_unit(int32_t Bp) {
   } while (0)
 
 hipError_t launch_blk_fwd(const BlkPack& p, const float* Zt, const float* Ut, int32_t Bp,
-                          float* part, hipStream_t s) {
+                          float* part, float* csum, hipStream_t s) {
   note_variant("k_blk_fwd", kArithNone);
   const int LG = lanes_per_unit(Bp), nb = ceil_div_i(Bp, 4 * LG);
   const int64_t waves = (int64_t)p.npieces * nb;
@@ -296,9 +335,9 @@ hipError_t launch_blk_fwd(const BlkPack& p, const float* Zt, const float* Ut, in
   const unsigned grid = (unsigned)ceil_div_i(waves, 4);
 #define PMLP_CALL(OM)                                                                        \
   do {                                                                                       \
-    if (Ut && p.gain) k_blk_fwd<OM, true, true><<<grid, kBlock, 0, s>>>(p, Zt, Ut, Bp, LG, nb, part); \
-    else if (Ut) k_blk_fwd<OM, true, false><<<grid, kBlock, 0, s>>>(p, Zt, Ut, Bp, LG, nb, part);     \
-    else k_blk_fwd<OM, false, true><<<grid, kBlock, 0, s>>>(p, Zt, Ut, Bp, LG, nb, part);     \
+    if (Ut && p.gain) k_blk_fwd<OM, true, true><<<grid, kBlock, 0, s>>>(p, Zt, Ut, Bp, LG, nb, part, csum); \
+    else if (Ut) k_blk_fwd<OM, true, false><<<grid, kBlock, 0, s>>>(p, Zt, Ut, Bp, LG, nb, part, csum);     \
+    else k_blk_fwd<OM, false, true><<<grid, kBlock, 0, s>>>(p, Zt, Ut, Bp, LG, nb, part, csum);     \
   } while (0)
   PMLP_BLK_OM(p.O, PMLP_CALL);
 #undef PMLP_CALL
@@ -334,10 +373,10 @@ hipError_t launch_blk_out(const BlkPack& p, const BlkMap& map, int64_t records, 
 #define PMLP_CALL(OM)                                                                          \
   do {                                                                                         \
     if (p.gain)                                                                                \
-      k_blk_out<OM, true><<<(unsigned)grid, threads, lds, s>>>(p, map, part, Br, B, per, nblk, G, \
+      k_blk_out<OM, true><<<(unsigned)grid, threads, lds, s>>>(p, map, part, map.csum, Br, B, per, nblk, G, \
                                                                alone, out, sm, sb);             \
     else                                                                                       \
-      k_blk_out<OM, false><<<(unsigned)grid, threads, lds, s>>>(p, map, part, Br, B, per, nblk, \
+      k_blk_out<OM, false><<<(unsigned)grid, threads, lds, s>>>(p, map, part, map.csum, Br, B, per, nblk, \
                                                                 G, alone, out, sm, sb);         \
   } while (0)
   PMLP_BLK_OM(p.O, PMLP_CALL);
@@ -356,9 +395,9 @@ hipError_t launch_blk_loss(const BlkPack& p, const BlkMap& map, int64_t records,
 #define PMLP_CALL(OM)                                                                              \
   do {                                                                                             \
     if (p.gain)                                                                                    \
-      k_blk_loss<OM, true><<<(unsigned)p.M, threads, lds, s>>>(p, map, part, Br, Bp, G, l, scale);  \
+      k_blk_loss<OM, true><<<(unsigned)p.M, threads, lds, s>>>(p, map, part, map.csum, Br, Bp, G, l, scale);  \
     else                                                                                           \
-      k_blk_loss<OM, false><<<(unsigned)p.M, threads, lds, s>>>(p, map, part, Br, Bp, G, l, scale); \
+      k_blk_loss<OM, false><<<(unsigned)p.M, threads, lds, s>>>(p, map, part, map.csum, Br, Bp, G, l, scale); \
   } while (0)
   PMLP_BLK_OM(p.O, PMLP_CALL);
 #undef PMLP_CALL

@@ -23,9 +23,11 @@
 // Two outputs are summed by vector FMAs and two lane swaps, more by fp32 matrix
 // products whose second operand is the hidden values as they lie in the registers.
 // A tile's mean is its first value plus the mean difference from it, and the squared
-// deviations are taken from that mean: both stay exact for values that lie close together
-// far from zero.  (One pass, deviations from the first value moved to the mean: as fast,
-// and its errors up to 16 times those of the variance.)
+// deviations, as the outputs' sums, are taken from that mean: both stay exact for values
+// that lie close together far from zero.  (One pass, deviations from the first value moved
+// to the mean: as fast, and its errors up to 16 times those of the variance.)  The matrix
+// products of many outputs start from the first value, before the mean is known, and
+// move to it afterwards.
 
 #include "block_tiles.h"
 
@@ -39,11 +41,13 @@ namespace {
 
 constexpr bool MF = PMLP_BLK_OM > 2;
 
-// Threads of a workgroup, at most: as many waves as a SIMD's registers hold without
-// spilling, four, three or two.
+// Threads of a workgroup, at most: as many waves as a SIMD's registers hold with few
+// spilled, four, three or two (normed, 16 outputs, 100 columns, 1000 samples of 40 models
+// of 500 to 1000 units: 95 us with three, 110 with four; two outputs, 6000 models of 4 to 100
+// units, 256 samples: 183 and 177).
 template <int NC, bool GATED>
 constexpr int max_threads() {
-  return GATED ? (NC == 0 ? 1024 : NC <= 3 ? 768 : 512) : (NC <= 3 ? 1024 : 768);
+  return GATED ? (NC == 0 ? 1024 : NC <= 3 ? 768 : 512) : (NC <= (MF ? 2 : 3) ? 1024 : 768);
 }
 
 template <int NC, int RM, bool GATED, bool NORM, bool RUNS>

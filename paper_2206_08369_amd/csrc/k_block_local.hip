@@ -56,7 +56,7 @@ __device__ __forceinline__ void local_loss(const BlkPack& p, const BlkMap& map,
     for (int o = 0; o < OM; ++o) gs[o] = 0.f;
     if (b < Bp) {
       Merged<OM> s;
-      merge_pieces<OM, NORM>(p, map, f.part, m, f.Br, b < l.B ? b : l.B - 1, 0, 1, s);
+      merge_pieces<OM, NORM>(p, map, f.part, f.csum, m, f.Br, b < l.B ? b : l.B - 1, 0, 1, s);
       sample_grads<OM, NORM>(p, l, m, b, Bp, s, C, D, rh, scale, loss, gs);
     }
     loss = group_sum_to_last(loss, 64);
@@ -100,7 +100,7 @@ void k_blk_local(BlkPack p, BlkLocal g, BlkFwdArgs f, BlkLoss l, BlkBwdArgs b) {
   fwd_tiles<NC, RM, (OM > 2), GATED, NORM, false>(p, f, lds, Bp, 0, Bp >> 5, t0 + wave, t1, nw, 1,
                                                   nullptr);
   __syncthreads();
-  local_loss<NORM>(p, BlkMap{g.toff, 1}, f, l, Bp, m0, m1, (float*)(lds + sums_at(NC, Bp)));
+  local_loss<NORM>(p, BlkMap{g.toff, 1, f.csum}, f, l, Bp, m0, m1, (float*)(lds + sums_at(NC, Bp)));
   __syncthreads();
   bwd_tiles<NC, RM, OM, GATED, NORM>(p, b, lds, Bp, 1, (t1 - t0 + nw - 1) / nw, t0 + wave, t1, nw);
 }

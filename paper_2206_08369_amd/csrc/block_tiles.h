@@ -249,7 +249,7 @@ __device__ __forceinline__ void act_and_slope(int A, const float (&z)[NV], float
   switch (A) {
 #define PMLP_ACT(AA)                                                                     \
   case AA: {                                                                             \
-    _Pragma("unroll") for (int j = 0; j < NV; ++j) v[j] = act_fwd_bwd(AA, z[j], &d[j]); \
+    _Pragma("unroll") for (int j = 0; j < NV; ++j) v[j] = blk_act_slope(AA, z[j], &d[j]); \
     break;                                                                               \
   }
     PMLP_EVERY_ACT

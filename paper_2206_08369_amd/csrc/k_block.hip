@@ -268,7 +268,7 @@ __global__ __launch_bounds__(kBlock) void k_blk_bwd(BlkPack p, float* __restrict
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float d;
-      const float av = act_fwd_bwd(a, z[i], &d);
+      const float av = blk_act_slope(a, z[i], &d);
       float hv = GATED ? av * u[i] : av;
       f32x4 st;
       if (NORM) {

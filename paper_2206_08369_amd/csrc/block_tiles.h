@@ -130,29 +130,29 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
       float* const dst = rec + 32 * st;
       const int row = acc_row(SC), at0 = 32 * st + li;
       // Means of the blocks that this lane's sums are of (both, or block lk & 1): the
-      // tile's, and the run's before it and after it.  piv: the tile's first unit's values.
+      // tile's, and the run's before it and after it.
       constexpr int NB = MF ? 2 : 1;
-      float piv[2], mean[2], m2[2], me[NB], ma[NB], mb[NB];
+      float mean[2], m2[2], me[NB], ma[NB], mb[NB];
       auto own = [&](float a, float b) { return lk & 1 ? b : a; };
       if (NORM) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          piv[i] = row0(h[4 * i]);
+          const float piv = row0(h[4 * i]);  // the first unit's value
           float d = 0.f, e = 0.f;
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             float& v = h[4 * i + r];
-            v = (cnt == 16 || r < mine) ? v - piv[i] : 0.f;
+            v = (cnt == 16 || r < mine) ? v - piv : 0.f;
             d += v;
           }
           d = sum32(d, d);
           d = sum16(d, d);
-          mean[i] = fmaf(d, rc, piv[i]);
-          const float off = piv[i] - mean[i];
+          mean[i] = fmaf(d, rc, piv);
+          const float off = piv - mean[i];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const float v = (cnt == 16 || r < mine) ? h[4 * i + r] + off : 0.f;
-            if (!MF) h[4 * i + r] = v;
+            h[4 * i + r] = v;
             e = fmaf(v, v, e);
           }
           e = sum32(e, e);
@@ -180,8 +180,11 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
               const int o = 4 * lk + r;
               float v = s[r];
               if (RUNS && have) v += acc[o * row + at0 + 16 * i];
-              if (NORM) v = fmaf(piv[i] - mb[MF ? i : 0], ct[r], v);
-              if (RUNS && NORM && have) v = fmaf(ma[MF ? i : 0] - mb[MF ? i : 0], cr[r], v);
+              if (RUNS && NORM && have) {
+                const int j = MF ? i : 0;
+                v = fmaf(me[j] - mb[j], ct[r], v);
+                v = fmaf(ma[j] - mb[j], cr[r], v);
+              }
               if (last) dst[(int64_t)o * a.Br + 16 * i] = v;
               else acc[o * row + at0 + 16 * i] = v;
             }

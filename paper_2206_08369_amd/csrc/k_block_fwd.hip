@@ -25,9 +25,7 @@
 // A tile's mean is its first value plus the mean difference from it, and the squared
 // deviations, as the outputs' sums, are taken from that mean: both stay exact for values
 // that lie close together far from zero.  (One pass, deviations from the first value moved
-// to the mean: as fast, and its errors up to 16 times those of the variance.)  The matrix
-// products of many outputs start from the first value, before the mean is known, and
-// move to it afterwards.
+// to the mean: as fast, and its errors up to 16 times those of the variance.)
 
 #include "block_tiles.h"
 

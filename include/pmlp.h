@@ -184,10 +184,11 @@ int pmlp_info_deep(pmlp_t h, int64_t* N2, int64_t* K);
  * Such a handle takes pmlp_forward, pmlp_train_step[_lr|_mse], pmlp_losses,
  * pmlp_nonfinite, pmlp_info, pmlp_set_stream, profiling and the _block calls below;
  * the other calls, the bf16 modes, biases and feature masks return PMLP_ESTATE.
- * Workspaces that a larger batch replaces are kept until pmlp_destroy, so that
- * graphs captured with them stay valid; a capture that would have to grow them
- * returns PMLP_ESTATE (call once with that batch size first).  Calls and graph
- * replays of one handle share its workspace: keep them in order.
+ * A call that needs a larger workspace than those before it waits for the device
+ * and frees the old one; a workspace that a call under graph capture has used is kept
+ * until pmlp_destroy instead, so that the graph stays valid.  A capture that would have
+ * to grow it returns PMLP_ESTATE (call once with that batch size first).  Calls and
+ * graph replays of one handle share its workspace: keep them in order.
  * Arguments as for pmlp_create. */
 int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* hidden_sizes,
                       const int32_t* act_ids, uint64_t seed, int32_t flags);

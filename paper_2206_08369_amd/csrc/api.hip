@@ -129,9 +129,10 @@ struct PmlpBlock {
   int32_t lplanned = 0;  // padded batch size of `lplan`
   BlkLocal lplan{};
   // Workspace.  A captured graph keeps the addresses it was captured with, so a
-  // buffer that a larger batch replaces lives until the handle goes.
+  // buffer that one has and a larger batch replaces lives until the handle goes.
   unsigned char* ws = nullptr;
   size_t cap = 0;
+  bool captured = false;
   std::vector<unsigned char*> retired;
 };
 
@@ -1407,28 +1408,59 @@ struct Carver {
 
 int ensure_block_ws(pmlp* h, size_t bytes) {
   PmlpBlock* k = h->block;
-  if (bytes <= k->cap) return PMLP_OK;
+  // (the null stream cannot be asked while another one captures; the capture goes on)
   hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-  PMLP_HIP(hipStreamIsCapturing(h->stream, &st));
+  if (!k->captured || bytes > k->cap) {
+    if (hipStreamIsCapturing(h->stream, &st) != hipSuccess) {
+      (void)hipGetLastError();
+      st = hipStreamCaptureStatusActive;
+    }
+  }
+  if (bytes <= k->cap) {
+    k->captured |= st != hipStreamCaptureStatusNone;
+    return PMLP_OK;
+  }
   if (st != hipStreamCaptureStatusNone)
     return fail(PMLP_ESTATE, "under graph capture a block pack needs an earlier call of this kind "
                              "and batch size");
   size_t want = bytes;
   if (bytes < (size_t)64 << 20)  // few small buffers on the way to a large batch
     for (want = (size_t)1 << 16; want < bytes;) want <<= 1;
+  // (calls on an earlier stream too may still be using the old one)
+  auto drop = [&]() -> int {
+    PMLP_HIP(hipDeviceSynchronize());
+    dfree(k->ws);
+    k->cap = 0;
+    return PMLP_OK;
+  };
   unsigned char* p = nullptr;
-  if (hipMalloc(&p, want) != hipSuccess) {
+  hipError_t e = hipMalloc(&p, want);
+  if (e == hipErrorOutOfMemory && k->ws && !k->captured) {  // not both at once
+    (void)hipGetLastError();
+    if (int rc = drop()) return rc;
+    e = hipMalloc(&p, want);
+  }
+  if (e != hipSuccess) {
     (void)hipGetLastError();
     return fail(PMLP_ENOMEM, "block workspace allocation failed (" + std::to_string(want >> 20) +
                                  " MiB)");
   }
-  try {
-    if (k->ws) k->retired.push_back(k->ws);
-  } catch (const std::bad_alloc&) {
+  int rc = PMLP_OK;
+  if (k->ws && k->captured) {
+    try {
+      k->retired.push_back(k->ws);
+    } catch (const std::bad_alloc&) {
+      rc = fail(PMLP_ENOMEM, "host allocation failed");
+    }
+  } else if (k->ws) {
+    rc = drop();
+  }
+  if (rc) {
     dfree(p);
-    return fail(PMLP_ENOMEM, "host allocation failed");
+    return rc;
   }
   k->ws = p;
+  k->captured = false;
   k->cap = want;
   return PMLP_OK;
 }

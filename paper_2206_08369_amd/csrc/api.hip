@@ -1856,17 +1856,11 @@ int block_grads(pmlp* h, float* dW1, float* dV1, float* dW2, float* dgain, float
   return PMLP_OK;
 }
 
-}  // namespace
+// ---- handles ---------------------------------------------------------------------
 
-extern "C" {
-
-int pmlp_create(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* hidden_sizes,
-                const int32_t* act_ids, uint64_t seed) {
-  return pmlp_create_ex(out, F, O, M, hidden_sizes, act_ids, seed, 0);
-}
-
-int pmlp_create_ex(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* hidden_sizes,
-                   const int32_t* act_ids, uint64_t seed, int32_t flags) {
+// pmlp_create_ex with room behind W1 for `halves - 1` more such matrices (zero).
+int create_packed(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* hidden_sizes,
+                  const int32_t* act_ids, uint64_t seed, int32_t flags, int halves) {
   if (!out) return fail(PMLP_EINVAL, "null output handle pointer");
   *out = nullptr;
   if (flags & ~(PMLP_BIAS | PMLP_MSE)) return fail(PMLP_EINVAL, "unknown flags");
@@ -1934,7 +1928,7 @@ int pmlp_create_ex(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* 
   h->dev = dev;
   float* d_bound2 = nullptr;
   const int64_t Npad = h->Npad;
-  const size_t w1_bytes = ((size_t)Npad * F4 + 64) * sizeof(float);  // slack for clamped loads
+  const size_t w1_bytes = (halves * (size_t)Npad * F4 + 64) * sizeof(float);  // slack for clamped loads
   if (hipMalloc(&h->W1, w1_bytes) != hipSuccess ||
       hipMalloc(&h->W2, (size_t)O * Npad * sizeof(float)) != hipSuccess ||
       hipMalloc(&h->d_seg_off, ((size_t)M + 1) * sizeof(int64_t)) != hipSuccess ||
@@ -1980,6 +1974,20 @@ int pmlp_create_ex(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* 
   if (rc) return bail(rc);
   *out = h;
   return PMLP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int pmlp_create(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* hidden_sizes,
+                const int32_t* act_ids, uint64_t seed) {
+  return pmlp_create_ex(out, F, O, M, hidden_sizes, act_ids, seed, 0);
+}
+
+int pmlp_create_ex(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* hidden_sizes,
+                   const int32_t* act_ids, uint64_t seed, int32_t flags) {
+  return create_packed(out, F, O, M, hidden_sizes, act_ids, seed, flags, 1);
 }
 
 int pmlp_destroy(pmlp_t h) {
@@ -2481,7 +2489,9 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
     return fail(PMLP_EINVAL, "a block pack has a gate, a norm or both (pmlp_create_ex makes packs "
                              "without)");
   pmlp_t h = nullptr;  // checks the rest
-  if (int rc = pmlp_create_ex(&h, F, O, M, hidden_sizes, act_ids, seed, flags & PMLP_MSE)) return rc;
+  if (int rc = create_packed(&h, F, O, M, hidden_sizes, act_ids, seed, flags & PMLP_MSE,
+                             flags & PMLP_GATED ? 2 : 1))
+    return rc;
   PmlpBlock* k = new (std::nothrow) PmlpBlock();
   if (!k) {
     pmlp_destroy(h);
@@ -2512,10 +2522,9 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
       k->most[g - 1] = std::max(k->most[g - 1], tiles_of);
     }
   }
-  const size_t half = (size_t)h->Npad * h->F4, units = (size_t)h->Npad * sizeof(float);
-  float* W = nullptr;
-  if ((k->gated && hipMalloc(&W, (2 * half + 64) * sizeof(float)) != hipSuccess) ||
-      (k->norm && (hipMalloc(&k->gain, units) != hipSuccess ||
+  if (k->gated) k->V1 = h->W1 + (size_t)h->Npad * h->F4;
+  const size_t units = (size_t)h->Npad * sizeof(float);
+  if ((k->norm && (hipMalloc(&k->gain, units) != hipSuccess ||
                    hipMalloc(&k->shift, units) != hipSuccess)) ||
       hipMalloc(&k->d_pieces, pieces.size() * sizeof(BlkPiece)) != hipSuccess ||
       hipMalloc(&k->d_poff, poff.size() * sizeof(int32_t)) != hipSuccess ||
@@ -2523,17 +2532,10 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
       hipMalloc(&k->d_btiles, btiles.size() * sizeof(BlkTile)) != hipSuccess ||
       hipMalloc(&k->d_toff, toff.size() * sizeof(int32_t)) != hipSuccess) {
     (void)hipGetLastError();
-    dfree(W);
     pmlp_destroy(h);
     return fail(PMLP_ENOMEM, "device allocation failed for the block parameters");
   }
   auto setup = [&]() -> int {
-    if (k->gated) {
-      PMLP_HIP(hipMemset(W, 0, (2 * half + 64) * sizeof(float)));
-      PMLP_HIP(hipMemcpy(W, h->W1, half * sizeof(float), hipMemcpyDeviceToDevice));
-      std::swap(W, h->W1);
-      k->V1 = h->W1 + half;
-    }
     if (k->norm) {
       PMLP_HIP(hipMemset(k->gain, 0, units));
       PMLP_HIP(hipMemset(k->shift, 0, units));
@@ -2553,9 +2555,7 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
     PMLP_HIP(hipStreamSynchronize(nullptr));
     return PMLP_OK;
   };
-  const int rc = setup();
-  dfree(W);
-  if (rc) {
+  if (int rc = setup()) {
     pmlp_destroy(h);
     return rc;
   }

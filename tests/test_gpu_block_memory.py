@@ -104,3 +104,23 @@ def test_a_captured_workspace_outlives_larger_batches(pm, torch):
     net._stream()
     net.close()
     twin.close()
+
+
+def test_a_pool_that_fits_is_created(pm, torch):
+    """A gated pool of two weight matrices of 4 GiB, where the device has 11 GiB left: it
+    needs no third one on the way."""
+    F, hs = 1024, np.full(10486, 100, np.int32)
+    torch.cuda.empty_cache()
+    free, _ = torch.cuda.mem_get_info()
+    held = torch.empty(free - (11 << 30), dtype=torch.uint8, device="cuda")
+    try:
+        net = pm.BlockPackedMLP(F, 2, hs, np.zeros(hs.size), seed=1, gated=True)
+        with pytest.raises(pm.PmlpError) as e:
+            pm.BlockPackedMLP(F, 2, hs, np.zeros(hs.size), seed=1, gated=True)
+        assert e.value.code == pm.PMLP_ENOMEM
+        L = net.forward(torch.ones(1, F, device="cuda"))
+        assert torch.isfinite(L).all()
+        net.close()
+    finally:
+        del held
+        torch.cuda.empty_cache()

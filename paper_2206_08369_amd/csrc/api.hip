@@ -12,6 +12,7 @@
 #include <cstring>
 #include <mutex>
 #include <new>
+#include <stdexcept>
 #include <string>
 #include <vector>
 
@@ -1858,6 +1859,30 @@ int block_grads(pmlp* h, float* dW1, float* dV1, float* dW2, float* dgain, float
 
 // ---- handles ---------------------------------------------------------------------
 
+// A handle in the making: freed where its maker returns (or throws) before done().
+struct Unfinished {
+  pmlp* h;
+  ~Unfinished() {
+    if (!h) return;
+    release(h);
+    delete h;
+  }
+  pmlp* done() {
+    pmlp* const p = h;
+    h = nullptr;
+    return p;
+  }
+};
+
+// The end of a C entry whose body allocates on the host: no exception leaves it.
+#define PMLP_NO_THROW                                       \
+  catch (const std::bad_alloc&) {                           \
+    return fail(PMLP_ENOMEM, "host allocation failed");     \
+  }                                                         \
+  catch (const std::length_error&) {                        \
+    return fail(PMLP_ENOMEM, "host allocation failed");     \
+  }
+
 // pmlp_create_ex with room behind W1 for `halves - 1` more such matrices (zero).
 int create_packed(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* hidden_sizes,
                   const int32_t* act_ids, uint64_t seed, int32_t flags, int halves) {
@@ -1884,6 +1909,7 @@ int create_packed(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* h
 
   pmlp* h = new (std::nothrow) pmlp();
   if (!h) return fail(PMLP_ENOMEM, "host allocation failed");
+  Unfinished made{h};
   h->F = F;
   h->F4 = F4;
   h->mse = (flags & PMLP_MSE) != 0;
@@ -1915,15 +1941,10 @@ int create_packed(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* h
   for (int32_t m = 0; m < M; ++m) bound2[m] = (float)(1.0 / std::sqrt((double)hidden_sizes[m]));
   const float bound1 = (float)(1.0 / std::sqrt((double)F));
 
-  auto bail = [&](int rc) {
-    release(h);
-    delete h;
-    return rc;
-  };
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) {
     (void)hipGetLastError();
-    return bail(fail(PMLP_EDEVICE, "no HIP device available"));
+    return fail(PMLP_EDEVICE, "no HIP device available");
   }
   h->dev = dev;
   float* d_bound2 = nullptr;
@@ -1943,7 +1964,7 @@ int create_packed(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* h
       (biases && hipMalloc(&h->b2, (size_t)M * O * sizeof(float)) != hipSuccess)) {
     (void)hipGetLastError();
     dfree(d_bound2);
-    return bail(fail(PMLP_ENOMEM, "device allocation failed for the packed parameters"));
+    return fail(PMLP_ENOMEM, "device allocation failed for the packed parameters");
   }
   auto setup = [&]() -> int {
     PMLP_HIP(hipMemcpy(h->d_seg_off, h->seg_off.data(), ((size_t)M + 1) * sizeof(int64_t),
@@ -1971,8 +1992,8 @@ int create_packed(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* h
   };
   int rc = setup();
   dfree(d_bound2);
-  if (rc) return bail(rc);
-  *out = h;
+  if (rc) return rc;
+  *out = made.done();
   return PMLP_OK;
 }
 
@@ -1986,9 +2007,10 @@ int pmlp_create(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* hid
 }
 
 int pmlp_create_ex(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* hidden_sizes,
-                   const int32_t* act_ids, uint64_t seed, int32_t flags) {
+                   const int32_t* act_ids, uint64_t seed, int32_t flags) try {
   return create_packed(out, F, O, M, hidden_sizes, act_ids, seed, flags, 1);
 }
+PMLP_NO_THROW
 
 int pmlp_destroy(pmlp_t h) {
   if (!h) return PMLP_OK;
@@ -2355,7 +2377,7 @@ int pmlp_profile_reset(pmlp_t h) {
 }
 
 int pmlp_create_deep(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* h1,
-                     const int32_t* h2, const int32_t* act_ids, uint64_t seed) {
+                     const int32_t* h2, const int32_t* act_ids, uint64_t seed) try {
   if (!out) return fail(PMLP_EINVAL, "null output handle pointer");
   *out = nullptr;
   if (M < 1) return fail(PMLP_EINVAL, "M must be >= 1");
@@ -2369,11 +2391,9 @@ int pmlp_create_deep(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t
   if (N2 > ((int64_t)1 << 31) - 1) return fail(PMLP_EINVAL, "second-layer units exceed 2^31-1");
   pmlp_t h = nullptr;
   if (int rc = pmlp_create_ex(&h, F, O, M, h1, act_ids, seed, 0)) return rc;  // checks the rest
+  Unfinished made{h};
   PmlpDeep* d = new (std::nothrow) PmlpDeep();
-  if (!d) {
-    pmlp_destroy(h);
-    return fail(PMLP_ENOMEM, "host allocation failed");
-  }
+  if (!d) return fail(PMLP_ENOMEM, "host allocation failed");
   h->deep = d;
   d->N2 = N2;
   d->N2pad = (N2 + 63) / 64 * 64;
@@ -2401,7 +2421,6 @@ int pmlp_create_deep(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t
       for (int32_t j = 0; j < h1[m]; j += 64) tgrad.push_back(SegTile{m, i, j, 0});
   }
   if (ufwd.size() > 0x7fffffff || uback.size() > 0x7fffffff || tgrad.size() > 0x7fffffff) {
-    pmlp_destroy(h);
     return fail(PMLP_EINVAL, "too many work units for one launch");
   }
   d->nufwd = (int32_t)ufwd.size();
@@ -2436,7 +2455,6 @@ int pmlp_create_deep(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t
     (void)hipGetLastError();
     dfree(d_b12);
     dfree(d_b2);
-    pmlp_destroy(h);
     return fail(PMLP_ENOMEM, "device allocation failed for the second hidden layer");
   }
   auto setup = [&]() -> int {
@@ -2473,15 +2491,15 @@ int pmlp_create_deep(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t
   dfree(d_b12);
   dfree(d_b2);
   if (rc) {
-    pmlp_destroy(h);
     return rc;
   }
-  *out = h;
+  *out = made.done();
   return PMLP_OK;
 }
+PMLP_NO_THROW
 
 int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_t* hidden_sizes,
-                      const int32_t* act_ids, uint64_t seed, int32_t flags) {
+                      const int32_t* act_ids, uint64_t seed, int32_t flags) try {
   if (!out) return fail(PMLP_EINVAL, "null output handle pointer");
   *out = nullptr;
   if (flags & ~(PMLP_GATED | PMLP_NORM | PMLP_MSE)) return fail(PMLP_EINVAL, "unknown flags");
@@ -2492,24 +2510,17 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
   if (int rc = create_packed(&h, F, O, M, hidden_sizes, act_ids, seed, flags & PMLP_MSE,
                              flags & PMLP_GATED ? 2 : 1))
     return rc;
+  Unfinished made{h};
   PmlpBlock* k = new (std::nothrow) PmlpBlock();
-  if (!k) {
-    pmlp_destroy(h);
-    return fail(PMLP_ENOMEM, "host allocation failed");
-  }
+  if (!k) return fail(PMLP_ENOMEM, "host allocation failed");
   h->block = k;
   k->gated = (flags & PMLP_GATED) != 0;
   k->norm = (flags & PMLP_NORM) != 0;
   std::vector<BlkPiece> pieces;
   std::vector<BlkTile> tiles, btiles;
   std::vector<int32_t> poff, toff;
-  try {
-    block_pieces(h->hs, tile_cap(h->N), pieces, poff);
-    block_tiles(h->hs, h->acts, tiles, toff, btiles);
-  } catch (const std::bad_alloc&) {
-    pmlp_destroy(h);
-    return fail(PMLP_ENOMEM, "host allocation failed");
-  }
+  block_pieces(h->hs, tile_cap(h->N), pieces, poff);
+  block_tiles(h->hs, h->acts, tiles, toff, btiles);
   k->npieces = (int32_t)pieces.size();
   k->ntiles = (int32_t)tiles.size();
   k->nbtiles = (int32_t)btiles.size();
@@ -2532,7 +2543,6 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
       hipMalloc(&k->d_btiles, btiles.size() * sizeof(BlkTile)) != hipSuccess ||
       hipMalloc(&k->d_toff, toff.size() * sizeof(int32_t)) != hipSuccess) {
     (void)hipGetLastError();
-    pmlp_destroy(h);
     return fail(PMLP_ENOMEM, "device allocation failed for the block parameters");
   }
   auto setup = [&]() -> int {
@@ -2556,12 +2566,12 @@ int pmlp_create_block(pmlp_t* out, int32_t F, int32_t O, int32_t M, const int32_
     return PMLP_OK;
   };
   if (int rc = setup()) {
-    pmlp_destroy(h);
     return rc;
   }
-  *out = h;
+  *out = made.done();
   return PMLP_OK;
 }
+PMLP_NO_THROW
 
 int pmlp_gradients_block(pmlp_t h, const float* X_dev, const int32_t* y_dev, int32_t B,
                          float* dW1_dev, float* dV1_dev, float* dW2_dev, float* dgain_dev,

@@ -1343,8 +1343,8 @@ void block_pieces(const std::vector<int32_t>& hs, int64_t cap, std::vector<BlkPi
   for (size_t m = 0; m < hs.size(); ++m) {
     poff.push_back((int32_t)pieces.size());
     const int32_t k = div_up(hs[m], cap), len = div_up(hs[m], k);
-    for (int32_t at = 0; at < hs[m]; at += len)
-      pieces.push_back(BlkPiece{n + at, std::min(len, hs[m] - at), (int32_t)m});
+    for (int64_t at = 0; at < hs[m]; at += len)  // (past the last it may exceed 31 bits)
+      pieces.push_back(BlkPiece{n + at, (int32_t)std::min<int64_t>(len, hs[m] - at), (int32_t)m});
     n += hs[m];
   }
   poff.push_back((int32_t)pieces.size());
@@ -1358,8 +1358,9 @@ void block_tiles(const std::vector<int32_t>& hs, const std::vector<int32_t>& act
   int64_t n = 0;
   for (size_t m = 0; m < hs.size(); ++m) {
     toff.push_back((int32_t)tiles.size());
-    for (int32_t at = 0; at < hs[m]; at += 16)
-      tiles.push_back(BlkTile{(int32_t)(n + at), std::min(16, hs[m] - at), (int32_t)m, acts[m]});
+    for (int64_t at = 0; at < hs[m]; at += 16)
+      tiles.push_back(BlkTile{(int32_t)(n + at), (int32_t)std::min<int64_t>(16, hs[m] - at), (int32_t)m,
+                              acts[m]});
     n += hs[m];
   }
   toff.push_back((int32_t)tiles.size());
@@ -1612,7 +1613,7 @@ BlkLocal block_local(pmlp* h, int32_t Bp) {
   PmlpBlock* k = h->block;
   if (k->lplanned == Bp) return k->lplan;
   BlkLocal best{};
-  if (Bp <= kBlkLocalBatch && Bp * k->most[0] <= 1024) {
+  if (Bp <= kBlkLocalBatch && (int64_t)Bp * k->most[0] <= 1024) {
     const BlkPack p = block_pack(h);
     for (int32_t group = 1; group <= kBlkLocalGroup && !best.group; ++group)
       if (k->most[group - 1] <= kBlkLocalGroup &&

@@ -22,11 +22,12 @@ __device__ __forceinline__ float sum16(float a, float b) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// a of the wave's first row of 16 in all four
-__device__ __forceinline__ float row0(float a) {
+// a of the lower half of the wave in both, of the upper half in both
+__device__ __forceinline__ void halves(float a, float& lower, float& upper) {
   const uint32_t u = __float_as_uint(a);
   const u32x2 r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return __uint_as_float(__builtin_amdgcn_permlane16_swap(r[0], r[0], false, false)[0]);
+  lower = __uint_as_float(r[0]);
+  upper = __uint_as_float(r[1]);
 }
 
 // The forward of runs of `run` tiles r, r + step, .. (below tile `end`) by one wave:
@@ -102,8 +103,8 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
       ct = __builtin_amdgcn_mfma_f32_16x16x4f32((u[0] + u[1]) + (u[2] + u[3]), 1.f, ct, 0, 0, 0);
     } else if (NORM) {
       const f32x4 u = w2[0], v = w2[MF ? 0 : 1];
-      const float c = sum32((u[0] + u[1]) + (u[2] + u[3]), (v[0] + v[1]) + (v[2] + v[3]));
-      ct[0] = sum16(c, c);
+      const float c = (u[0] + u[1]) + (u[2] + u[3]), d = (v[0] + v[1]) + (v[2] + v[3]);
+      ct[0] = sum16(sum32(c, c), sum32(d, d));
     }
     if (AHEAD) fetch(qn.n0, qn.cnt);
     float* const rec = a.part + (int64_t)(m + r) * PQ * a.Br + b0 + li;
@@ -129,40 +130,43 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
       }
       float* const dst = rec + 32 * st;
       const int row = acc_row(SC), at0 = 32 * st + li;
-      // Means of the blocks that this lane's sums are of (both, or block lk & 1): the
-      // tile's, and the run's before it and after it.
+      // Means of the blocks that this lane's sums are of (both, or its half's, lk >> 1):
+      // the tile's, and the run's before it and after it.
       constexpr int NB = MF ? 2 : 1;
-      float mean[2], m2[2], me[NB], ma[NB], mb[NB];
-      auto own = [&](float a, float b) { return lk & 1 ? b : a; };
+      float mean[2], m2, me[NB], ma[NB], mb[NB];
+      auto own = [&](float a, float b) { return lk >> 1 ? b : a; };
       if (NORM) {
+        float piv[2], d[2] = {0.f, 0.f}, e[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float piv = row0(h[4 * i]);  // the first unit's value
-          float d = 0.f, e = 0.f;
+          piv[i] = __shfl(h[4 * i], li);  // the first unit's value
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             float& v = h[4 * i + r];
-            v = (cnt == 16 || r < mine) ? v - piv : 0.f;
-            d += v;
+            v = (cnt == 16 || r < mine) ? v - piv[i] : 0.f;
+            d[i] += v;
           }
-          d = sum32(d, d);
-          d = sum16(d, d);
-          mean[i] = fmaf(d, rc, piv);
-          const float off = piv - mean[i];
+        }
+        m2 = sum32(d[0], d[1]);
+        halves(sum16(m2, m2), d[0], d[1]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          mean[i] = fmaf(d[i], rc, piv[i]);
+          const float off = piv[i] - mean[i];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float v = (cnt == 16 || r < mine) ? h[4 * i + r] + off : 0.f;
-            h[4 * i + r] = v;
-            e = fmaf(v, v, e);
+            float& v = h[4 * i + r];
+            v = (cnt == 16 || r < mine) ? v + off : 0.f;
+            e[i] = fmaf(v, v, e[i]);
           }
-          e = sum32(e, e);
-          m2[i] = sum16(e, e);
         }
+        m2 = sum32(e[0], e[1]);
+        m2 = sum16(m2, m2);
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
           ma[j] = mb[j] = me[j] = MF ? mean[j] : own(mean[0], mean[1]);
           if (RUNS && have) {
-            ma[j] = acc[p.O * row + at0 + 16 * (MF ? j : lk & 1)];
+            ma[j] = acc[p.O * row + at0 + 16 * (MF ? j : lk >> 1)];
             mb[j] = fmaf(me[j] - ma[j], share, ma[j]);
           }
         }
@@ -199,27 +203,26 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
 #pragma unroll
             for (int r = 1; r < 4; ++r) s[i][o] = fmaf(h[4 * i + r], w2[MF ? 0 : o][r], s[i][o]);
           }
-        // row lk ends with block lk & 1 of output lk >> 1
-        float v = sum16(sum32(s[0][0], s[0][1]), sum32(s[1][0], s[1][1]));
-        const int at = (lk >> 1) * row + at0 + 16 * (lk & 1);
+        // row lk ends with block lk >> 1 of output lk & 1
+        float v = sum16(sum32(s[0][0], s[1][0]), sum32(s[0][1], s[1][1]));
+        const int at = (lk & 1) * row + at0 + 16 * (lk >> 1);
         if (RUNS && have) v += acc[at];
         if (RUNS && NORM && have) {
           v = fmaf(me[0] - mb[0], ct[0], v);
           v = fmaf(ma[0] - mb[0], cr[0], v);
         }
-        if (last) dst[(int64_t)(lk >> 1) * a.Br + 16 * (lk & 1)] = v;
+        if (last) dst[(int64_t)(lk & 1) * a.Br + 16 * (lk >> 1)] = v;
         else acc[at] = v;
       }
       if (NORM) {
-        float q = own(m2[0], m2[1]);
-        float* const sum = acc + p.O * row + at0 + 16 * (lk & 1);
+        float* const sum = acc + p.O * row + at0 + 16 * (lk >> 1);
         if (RUNS && have) {
           const float d = own(me[0] - ma[0], me[NB - 1] - ma[NB - 1]);
-          q += sum[row] + d * both * d;
+          m2 += sum[row] + d * both * d;
         }
-        const float v = lk & 2 ? q : own(mb[0], mb[NB - 1]);
-        if (last) dst[(int64_t)(p.O + (lk >> 1)) * a.Br + 16 * (lk & 1)] = v;
-        else sum[(lk >> 1) * row] = v;
+        const float v = lk & 1 ? m2 : own(mb[0], mb[NB - 1]);
+        if (last) dst[(int64_t)(p.O + (lk & 1)) * a.Br + 16 * (lk >> 1)] = v;
+        else sum[(lk & 1) * row] = v;
       }
     }
     if (NORM) {
@@ -228,7 +231,7 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
       if (last && b0 == 0 && li == 0) {
         float* const c = a.csum + (int64_t)(m + r) * om;
         if (MF && 4 * lk < om) *(f32x4*)(c + 4 * lk) = ct;
-        if (!MF && !(lk & 1)) c[lk >> 1] = ct[0];
+        if (!MF && lk < 2) c[lk] = ct[0];
       }
     }
     have = last ? 0 : have + cnt;

@@ -42,7 +42,8 @@ __device__ __forceinline__ void lds_barrier() {
 // divides by a deviation that may be as small, and the forms of act_fwd that subtract
 // from 1 are off by 1e-7 however small the result.  (tanh units of pre-activations about
 // 1e-3, normalised: outputs off by 5e-5 of their size with act_fwd.)  The polynomials are
-// minimax ones of the relative error, below 0.25 units in the last place.
+// minimax ones of the relative error, below 0.25 units in the last place.  Both forms are
+// computed and one taken: a branch for each value cost more than either.
 
 // tanh z: z + z^3 R(z^2) up to 1/2
 __device__ __forceinline__ float blk_tanh(float z) {
@@ -50,7 +51,8 @@ __device__ __forceinline__ float blk_tanh(float z) {
   float r = fmaf(0.017256992f, q, -0.05305295f);
   r = fmaf(r, q, 0.13325988f);
   r = fmaf(r, q, -0.3333315f);
-  return fabsf(z) < 0.5f ? fmaf(z * q, r, z) : act_fwd(2, z);
+  const float small = fmaf(z * q, r, z), wide = act_fwd(2, z);
+  return fabsf(z) < 0.5f ? small : wide;
 }
 
 // e^z - 1, given e^z, for z <= 0: z + z^2 R(z) down to -1/2
@@ -59,7 +61,8 @@ __device__ __forceinline__ float blk_expm1(float z, float ez) {
   r = fmaf(r, z, 0.041633245f);
   r = fmaf(r, z, 0.1666631f);
   r = fmaf(r, z, 0.49999988f);
-  return z > -0.5f ? fmaf(z * z, r, z) : ez - 1.f;
+  const float small = fmaf(z * z, r, z), wide = ez - 1.f;
+  return z > -0.5f ? small : wide;
 }
 
 // log(1 + e), 0 <= e <= 1: 2 atanh s = 2 s + 2 s^3 R(s^2) of s = e / (2 + e)
@@ -71,15 +74,26 @@ __device__ __forceinline__ float blk_log1p(float e) {
   return 2.f * fmaf(s * q, r, s);
 }
 
+// ELU (up, down 1) and SELU, given e^z
+__device__ __forceinline__ float blk_elu(float z, float ez, float up, float down) {
+  const float above = up * z, below = down * blk_expm1(z, ez);
+  return z > 0.f ? above : below;
+}
+
+// softplus z, given e^-|z|
+__device__ __forceinline__ float blk_softplus(float z, float e) {
+  const float s = fmaxf(z, 0.f) + blk_log1p(e);
+  return z > 20.f ? z : s;
+}
+
 // (NaN for NaN also where act_fwd's choice of a branch would drop it)
 __device__ __forceinline__ float blk_act(int a, float z) {
   switch (a) {
     case 1: return z <= 0.f ? 0.f : z;
     case 2: return blk_tanh(z);
-    case 4: return z > 0.f ? z : blk_expm1(z, fexp(z));
-    case 8: return z > 20.f ? z : fmaxf(z, 0.f) + blk_log1p(fexp(-fabsf(z)));
-    case 10:
-      return z > 0.f ? kSeluLambda * z : (kSeluLambda * kSeluAlpha) * blk_expm1(z, fexp(z));
+    case 4: return blk_elu(z, fexp(z), 1.f, 1.f);
+    case 8: return blk_softplus(z, fexp(-fabsf(z)));
+    case 10: return blk_elu(z, fexp(z), kSeluLambda, kSeluLambda * kSeluAlpha);
     case 11: return fabsf(z) <= 0.5f ? 0.f : z;
     default: return act_fwd(a, z);
   }
@@ -96,14 +110,15 @@ __device__ __forceinline__ float blk_act_slope(int a, float z, float* d) {
     case 4:
     case 10: {
       const float up = a == 10 ? kSeluLambda : 1.f, down = a == 10 ? kSeluLambda * kSeluAlpha : 1.f;
-      const float e = fexp(z);
-      *d = z > 0.f ? up : down * e;
-      return z > 0.f ? up * z : down * blk_expm1(z, e);
+      const float e = fexp(z), below = down * e;
+      *d = z > 0.f ? up : below;
+      return blk_elu(z, e, up, down);
     }
     case 8: {
       const float e = fexp(-fabsf(z)), r = frcp(1.f + e);
-      *d = z > 20.f ? 1.f : (z >= 0.f ? r : e * r);
-      return z > 20.f ? z : fmaxf(z, 0.f) + blk_log1p(e);
+      const float s = (z >= 0.f ? 1.f : e) * r;
+      *d = z > 20.f ? 1.f : s;
+      return blk_softplus(z, e);
     }
     default: return act_fwd_bwd(a, z, d);
   }

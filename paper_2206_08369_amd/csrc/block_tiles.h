@@ -30,6 +30,11 @@ __device__ __forceinline__ void halves(float a, float& lower, float& upper) {
   upper = __uint_as_float(r[1]);
 }
 
+// a, the same in every lane, in a scalar register
+__device__ __forceinline__ float uniform(float a) {
+  return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(a)));
+}
+
 // The forward of runs of `run` tiles r, r + step, .. (below tile `end`) by one wave:
 // their sums over the `steps` blocks of 32 samples from b0 on whose pieces lie in LDS
 // (SC of them).  RUNS: the sums of a run's tiles are added up in `acc`, planes of
@@ -107,10 +112,10 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
       ct[0] = sum16(sum32(c, c), sum32(d, d));
     }
     if (AHEAD) fetch(qn.n0, qn.cnt);
-    float* const rec = a.part + (int64_t)(m + r) * PQ * a.Br + b0 + li;
-    const float rc = 1.f / (float)cnt;
+    float* const rec = a.part + (int64_t)(m + r) * PQ * a.Br + b0;  // (at 32-bit offsets)
+    const float rc = uniform(1.f / (float)cnt);
     // merging with the `have` units before (see merge_stats)
-    const float share = (float)cnt / (float)(have + cnt), both = share * (float)have;
+    const float share = uniform((float)cnt / (float)(have + cnt)), both = uniform(share * (float)have);
 #pragma unroll 1
     for (int st = 0; st < steps; ++st) {
       const int at = 32 * st * RB;
@@ -128,7 +133,6 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
 #pragma unroll
         for (int v = 0; v < 8; ++v) h[v] = (v & 3) < mine ? h[v] : 0.f;
       }
-      float* const dst = rec + 32 * st;
       const int row = acc_row(SC), at0 = 32 * st + li;
       // Means of the blocks that this lane's sums are of (both, or its half's, lk >> 1):
       // the tile's, and the run's before it and after it.
@@ -189,7 +193,7 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
                 v = fmaf(me[j] - mb[j], ct[r], v);
                 v = fmaf(ma[j] - mb[j], cr[r], v);
               }
-              if (last) dst[(int64_t)o * a.Br + 16 * i] = v;
+              if (last) rec[(uint32_t)(o * a.Br + at0 + 16 * i)] = v;
               else acc[o * row + at0 + 16 * i] = v;
             }
         }
@@ -211,7 +215,7 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
           v = fmaf(me[0] - mb[0], ct[0], v);
           v = fmaf(ma[0] - mb[0], cr[0], v);
         }
-        if (last) dst[(int64_t)(lk & 1) * a.Br + 16 * (lk >> 1)] = v;
+        if (last) rec[(uint32_t)((lk & 1) * a.Br + at0 + 16 * (lk >> 1))] = v;
         else acc[at] = v;
       }
       if (NORM) {
@@ -221,7 +225,7 @@ __device__ __forceinline__ void fwd_tiles(const BlkPack& p, const BlkFwdArgs& a,
           m2 += sum[row] + d * both * d;
         }
         const float v = lk & 1 ? m2 : own(mb[0], mb[NB - 1]);
-        if (last) dst[(int64_t)(p.O + (lk & 1)) * a.Br + 16 * (lk >> 1)] = v;
+        if (last) rec[(uint32_t)((p.O + (lk & 1)) * a.Br + at0 + 16 * (lk >> 1))] = v;
         else sum[(lk & 1) * row] = v;
       }
     }
@@ -288,9 +292,9 @@ __device__ __forceinline__ void bwd_tiles(const BlkPack& p, const BlkBwdArgs& a,
   constexpr bool AHEAD = NC <= 1;
   struct Next {
     UnitRaw<NC, RM, K> w;
-    float w2[NO], gs[NORM ? NO : 1], g, s;
+    float w2[NO], g, s;
   } nx;
-  auto fetch = [&](int64_t n, int m) {
+  auto fetch = [&](int64_t n) {
     nx.w.load(p, n, lk);
     nx.g = NORM ? p.gain[n] : 1.f;
     nx.s = NORM ? p.shift[n] : 0.f;
@@ -298,11 +302,10 @@ __device__ __forceinline__ void bwd_tiles(const BlkPack& p, const BlkBwdArgs& a,
     for (int o = 0; o < NO; ++o) {
       const int ow = MF ? 4 * lk + o : o, oc = ow < p.O ? ow : 0;
       nx.w2[o] = p.W2[(int64_t)oc * p.ldw + n];
-      if (NORM) nx.gs[NORM ? o : 0] = a.Gs[(int64_t)m * p.O + oc];
     }
   };
   UnitRows<NC, RM, K> w;
-  float w2[NO], gs[NORM ? NO : 1], gn = 1.f, sn = 0.f;  // (gs: sum_b G of the unit's model)
+  float w2[NO], gn = 1.f, sn = 0.f;
   auto take = [&] {
     w.split(nx.w, F4, lk);
     gn = opaque(nx.g);
@@ -311,7 +314,6 @@ __device__ __forceinline__ void bwd_tiles(const BlkPack& p, const BlkBwdArgs& a,
     for (int o = 0; o < NO; ++o) {
       const float v = opaque(nx.w2[o]);
       w2[o] = (MF ? 4 * lk + o : o) < p.O ? v : 0.f;
-      if (NORM) gs[NORM ? o : 0] = opaque(nx.gs[NORM ? o : 0]);
     }
   };
   struct Up {
@@ -320,10 +322,10 @@ __device__ __forceinline__ void bwd_tiles(const BlkPack& p, const BlkBwdArgs& a,
   // block b (its first sample) of the lanes' models m
   auto load_up = [&](int m, int b) {
     Up u;
+    const int ml = __builtin_amdgcn_readfirstlane(m);
     const uint32_t at = (uint32_t)(b + 4 * lk);  // first of four samples
     if (MF) {
-      const float* const g =
-          a.G + (int64_t)__builtin_amdgcn_readfirstlane(m) * a.Bp * OM;
+      const float* const g = a.G + (int64_t)ml * a.Bp * OM;
       u.g[0] = *(const f32x4*)(g + (uint32_t)(b + li) * OM + 4 * lk);
 #pragma unroll
       for (int r = 0; r < 4; ++r) u.g[MF ? 1 : 0][r] = g[(at + r) * OM + li];
@@ -333,7 +335,11 @@ __device__ __forceinline__ void bwd_tiles(const BlkPack& p, const BlkBwdArgs& a,
       for (int v = 0; v < NO; ++v) u.g[MF ? 0 : v] = *(const f32x4*)(g + 4 * v);
     }
     if (NORM) {
-      const float* const R = a.R + ((int64_t)m * a.Bp + at) * 4;
+      // (with many outputs at a 32-bit offset: two registers fewer keep the loads ahead
+      // from waiting for a spilled one; with few it was slower)
+      const float* const R = MF ? a.R + (int64_t)ml * a.Bp * 4 +
+                                      ((uint32_t)(m - ml) * (uint32_t)a.Bp + at) * 4u
+                                : a.R + ((int64_t)m * a.Bp + at) * 4;
 #pragma unroll
       for (int r = 0; r < 4; ++r) u.r[NORM ? r : 0] = *(const f32x4*)(R + 4 * r);
     }
@@ -352,7 +358,7 @@ __device__ __forceinline__ void bwd_tiles(const BlkPack& p, const BlkBwdArgs& a,
   int m = p.mid[unit_of(q)];
   Up up = load_up(m, 0);
   if (AHEAD) {
-    fetch(unit_of(q), m);
+    fetch(unit_of(q));
     take();
   }
 #pragma unroll 1
@@ -365,9 +371,9 @@ __device__ __forceinline__ void bwd_tiles(const BlkPack& p, const BlkBwdArgs& a,
     const BlkTile qnn = tile_at(tile + 2 * stride);
     const int mn = p.mid[unit_of(qn)];
     if (AHEAD) {
-      fetch(unit_of(qn), mn);
+      fetch(unit_of(qn));
     } else {
-      fetch(n, m);
+      fetch(n);
       take();
     }
     float T[NO];
@@ -492,6 +498,12 @@ _Pragma("unroll") for (int mt = 0; mt < K; ++mt) acc[mt][j] =        \
     }
     // ---- the gradients, stored or applied ---------------------------------------
     const float rate = a.g.lrm ? a.g.lrm[m] : a.g.lr;
+    float gs[NORM ? NO : 1];  // sum_b G of the unit's model
+#pragma unroll
+    for (int o = 0; o < (NORM ? NO : 0); ++o) {
+      const int ow = MF ? 4 * lk + o : o;
+      gs[NORM ? o : 0] = a.Gs[(int64_t)m * p.O + (ow < p.O ? ow : 0)];
+    }
     float dw[NO], dg = 0.f, ds = 0.f, old[NO];
 #pragma unroll
     for (int o = 0; o < NO; ++o) {

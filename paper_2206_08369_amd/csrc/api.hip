@@ -1641,8 +1641,8 @@ BlkRun block_run(pmlp* h, int32_t B) {
     if (k->planned[i] == B) return k->plan[i];
   const BlkPack p = block_pack(h);
   // Runs of several tiles save records and their merging, and cost LDS.  Models of 3.7
-  // tiles, 50 columns, both, 10,000 samples: 635 us without, 607 with; of 32 tiles, 32
-  // columns, ten outputs, 32 samples: forward and loss 161 and 132.  A batch of up to 32
+  // tiles, 50 columns, both, 10,000 samples: 637 us without, 613 with; of 32 tiles, 32
+  // columns, ten outputs, 32 samples: forward and loss 166 and 140.  A batch of up to 32
   // has short records: models of 3.6 tiles, 100 columns, one sample: 64 and 66.
   const bool runs = k->ntiles >= (int64_t)(B > 32 ? 2 : 8) * h->M;
   BlkRun best;

@@ -27,9 +27,10 @@
 // took 5 to 17 % longer: a fifth number a piece, and its room in LDS).
 //
 // The stored path (more than 128 input columns) spends its time in its three large
-// products; 1200 models of 1 to 200 units, 1000 columns, 1024 samples, gated: 5100 us of
-// them at 194 TFLOP/s (a library fp32 product reached 152), k_blk_fwd 230 us and
-// k_blk_bwd 365 us for 1.0 and 2.0 GB.
+// products; 1200 models of 1 to 200 units, 1000 columns, 1024 samples, gated, in a trace of
+// four passes: 5650 us of them at 175 TFLOP/s (a library fp32 product reached 152; a pass
+// among a hundred takes 5600 us in all, them at about 200), k_blk_fwd 222 us and k_blk_bwd
+// 374 us for 1.0 and 2.0 GB.
 
 #include "block_loss.h"
 
@@ -41,7 +42,8 @@ constexpr int kFU = 4;  // units per lane group whose loads are in flight
 
 // One wave per (piece, block of 4 LG samples).  Lane l takes four samples and
 // every NG-th unit (LG = lanes per unit, NG = 64 / LG), as k_m3_fwd.  Bound by
-// reading Z and U once.
+// reading Z and U once with two outputs, by its vector instructions with many (1114
+// models, 151 columns, ten outputs, 60 samples: 0.9 TB/s).
 template <int OM, bool GATED, bool NORM>
 __global__ __launch_bounds__(kBlock) void k_blk_fwd(BlkPack p, const float* __restrict__ Zt,
                                                     const float* __restrict__ Ut, int Bp, int LG,
@@ -241,7 +243,7 @@ __global__ __launch_bounds__(1024) void k_blk_loss(BlkPack p, BlkMap map,
 
 // dZ over Z and dU over U; the gradients of W2, gain and shift.  LG lanes take a
 // unit's samples, four each and 4 LG a pass.  Bound by reading and writing Z and U
-// once.
+// once, with many outputs by its vector instructions.
 template <int OM, bool GATED, bool NORM>
 __global__ __launch_bounds__(kBlock) void k_blk_bwd(BlkPack p, float* __restrict__ Zt,
                                                     float* __restrict__ Ut, int Bp, int LG,

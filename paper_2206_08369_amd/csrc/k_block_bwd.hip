@@ -15,12 +15,12 @@
 // consecutive columns of unit li's gradient, one store.
 // The norm's gradient needs no sums over units (see k_block.hip).
 //
-// Bound by its instructions: matrix and vector instructions of a SIMD's waves hardly
-// overlap, and take 85 % of the time together.  6000 models of 1 to 100 units, 100
-// columns, 256 samples: gated 415 us, that is 150 TFLOP/s of fp32 products (0.9 PFLOP/s
-// of bf16 ones), normed 264 us.  Wide models, ten outputs, 32 columns and samples,
-// both: 191 us for 660 MB, 3.4 TB/s (a large copy 4.8).  Two waves a SIMD is what the registers allow; where the
-// input has no block of 32 columns, three.
+// Bound by its instructions.  6000 models of 1 to 100 units, 100 columns, 256 samples (in
+// a trace of four passes): gated 381 us, that is 163 TFLOP/s of fp32 products (1.0 PFLOP/s
+// of bf16 ones), the matrix units busy 0.56 of the time and the vector units 0.45; normed
+// 250 us, 0.40 and 0.52.  Wide models, ten outputs, 32 columns and samples, both: 180 us for
+// 669 MB, 3.7 TB/s (a large copy 4.8).  Two waves a SIMD is what the registers allow;
+// where the input has no block of 32 columns, three.
 //
 // The second product takes NF = 2 NC blocks of 16 columns, and one more for the fp32
 // columns of the first; the last block may read past its columns into the next row,
@@ -102,7 +102,7 @@ hipError_t PMLP_CAT(launch_blk_fused_bwd_, PMLP_BLK_OM)(const BlkPack& p, BlkBwd
     return hipErrorInvalidValue;
   const size_t lds = pieces_bytes(inst.NC, a.SC);
   // eight waves share the samples' pieces where those leave room for one workgroup
-  // only (a gated paper pool: 414 us, with four 499), four where there is more (the
+  // only (a gated paper pool: 418 us, with four 492), four where there is more (the
   // same time in large pools; small ones spread over twice the CUs)
   const int waves = 4 * lds > (size_t)lmax ? 8 : 4;
   const int slots = resident_blocks((const void*)fn, 64 * waves, lds);

@@ -14,8 +14,9 @@
 // pre-activations.
 //
 // Bound by its instructions, as the backward.  6000 models of 1 to 100 units, 100
-// columns, 256 samples: gated 225 us, 138 TFLOP/s of fp32 products (0.83 PFLOP/s of
-// bf16 ones), normed 163 us.  With one sample it is bound by the weights: gated, 56 us
+// columns, 256 samples (in a trace of four passes): gated 205 us, 151 TFLOP/s of fp32
+// products (0.91 PFLOP/s of bf16 ones), matrix and vector units busy 0.59 each; normed
+// 150 us, 0.37 and 0.80.  With one sample it is bound by the weights: gated, 56 us
 // for 245 MB (4.4 TB/s).  (A form with the tiles of whole models in one workgroup,
 // which merged them itself, saved the output kernel's 7 us there and lost more by its
 // uneven groups: 59 -> 66 us in all, at 10,000 samples 669 -> 692.)
@@ -40,12 +41,12 @@ namespace {
 constexpr bool MF = PMLP_BLK_OM > 2;
 
 // Threads of a workgroup, at most: as many waves as a SIMD's registers hold with few
-// spilled, four, three or two (normed, 16 outputs, 100 columns, 1000 samples of 40 models
-// of 500 to 1000 units: 95 us with three, 110 with four; two outputs, 6000 models of 4 to 100
-// units, 256 samples: 183 and 177).
+// spilled, four, three or two (normed, 100 columns: 6000 models of 4 to 100 units, 256
+// samples, 166 us with four, 170 with three; 16 outputs, 1000 samples of 40 models of 500 to
+// 1000 units 90 with either).
 template <int NC, bool GATED>
 constexpr int max_threads() {
-  return GATED ? (NC == 0 ? 1024 : NC <= 3 ? 768 : 512) : (NC <= (MF ? 2 : 3) ? 1024 : 768);
+  return GATED ? (NC == 0 ? 1024 : NC <= 3 ? 768 : 512) : (NC <= 3 ? 1024 : 768);
 }
 
 template <int NC, int RM, bool GATED, bool NORM, bool RUNS>

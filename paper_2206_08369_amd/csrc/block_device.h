@@ -45,13 +45,13 @@ __device__ __forceinline__ void lds_barrier() {
 // minimax ones of the relative error, below 0.25 units in the last place.  Both forms are
 // computed and one taken: a branch for each value cost more than either.
 
-// tanh z: z + z^3 R(z^2) up to 1/2
-__device__ __forceinline__ float blk_tanh(float z) {
+// tanh z, given e = e^-2|z| and r = 1 / (1 + e): z + z^3 R(z^2) up to 1/2
+__device__ __forceinline__ float blk_tanh(float z, float e, float r) {
   const float q = z * z;
-  float r = fmaf(0.017256992f, q, -0.05305295f);
-  r = fmaf(r, q, 0.13325988f);
-  r = fmaf(r, q, -0.3333315f);
-  const float small = fmaf(z * q, r, z), wide = act_fwd(2, z);
+  float p = fmaf(0.017256992f, q, -0.05305295f);
+  p = fmaf(p, q, 0.13325988f);
+  p = fmaf(p, q, -0.3333315f);
+  const float small = fmaf(z * q, p, z), wide = copysignf((1.f - e) * r, z);
   return fabsf(z) < 0.5f ? small : wide;
 }
 
@@ -90,7 +90,10 @@ __device__ __forceinline__ float blk_softplus(float z, float e) {
 __device__ __forceinline__ float blk_act(int a, float z) {
   switch (a) {
     case 1: return z <= 0.f ? 0.f : z;
-    case 2: return blk_tanh(z);
+    case 2: {
+      const float e = fexp(-2.f * fabsf(z));
+      return blk_tanh(z, e, frcp(1.f + e));
+    }
     case 4: return blk_elu(z, fexp(z), 1.f, 1.f);
     case 8: return blk_softplus(z, fexp(-fabsf(z)));
     case 10: return blk_elu(z, fexp(z), kSeluLambda, kSeluLambda * kSeluAlpha);
@@ -103,9 +106,9 @@ __device__ __forceinline__ float blk_act(int a, float z) {
 __device__ __forceinline__ float blk_act_slope(int a, float z, float* d) {
   switch (a) {
     case 2: {
-      const float t = blk_tanh(z);
-      *d = 1.f - t * t;
-      return t;
+      const float e = fexp(-2.f * fabsf(z)), r = frcp(1.f + e);
+      *d = 4.f * e * r * r;  // 1 / cosh^2: 1 - tanh^2 would leave nothing of a small one
+      return blk_tanh(z, e, r);
     }
     case 4:
     case 10: {

@@ -27,11 +27,13 @@ def one_model(a, p, X, y=None):
     A, S = ref.act(a, Z)
     # (slopes grow by at most 1.3 |dz|; SELU's jumps by 0.7 at 0)
     eA = (np.abs(S) + 0.8 + 2 * eZ) * eZ + (8 + 2 * np.abs(Z)) * U * np.abs(A)
-    if a in (3, 8):
+    if a in (2, 3, 8):
         eA = (np.abs(S) + eZ) * eZ + (8 + 2 * np.abs(Z)) * U * np.abs(A)
     if a == 6:
         eA = eA + 1.5e-7 * np.abs(Z)
     eS = 2 * eZ + 1e-6
+    if a == 2:  # 1 / cosh^2 z: relative, twice the error of z (and of its exponential)
+        eS = np.abs(S) * (2 * eZ + 4 * eZ * eZ + (12 + 4 * np.abs(Z)) * U)
     if "V1" in p:
         Q, eQ = ref.dot(X, zero(X), p["V1"].T, zero(p["V1"]).T)
         H = A * Q

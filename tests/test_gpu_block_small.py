@@ -82,3 +82,12 @@ def test_small_pre_activations_of_selu(pm, torch, kind, F, O, B, scale):
 @pytest.mark.parametrize("offset", [0, -3, -9, 12])
 def test_softplus_and_sigmoid_off_zero(pm, torch, kind, F, O, B, offset):
     check(pm, torch, (8, 3), kind, F, O, B, 1.0, offset, F + O + B)
+
+
+@pytest.mark.parametrize("kind", sorted(KINDS))
+@pytest.mark.parametrize("F, O, B", SIZES)
+@pytest.mark.parametrize("offset", [-6, -4, 4, 6])
+def test_slopes_of_saturated_tanh(pm, torch, kind, F, O, B, offset):
+    """Slopes of 1e-3 to 1e-6, accurate relative to themselves: one minus the square of a
+    value next to one is not."""
+    check(pm, torch, (2,), kind, F, O, B, 1.0, offset, F + O + B)

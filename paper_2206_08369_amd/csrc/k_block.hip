@@ -24,13 +24,13 @@
 // here has terms larger than a few of the model's largest deviations times its weights.
 // A piece's mean is rounded once more to be stored, by as much as its hidden values are
 // (storing it as one of them and the difference kept sums and variance free of that, and
-// took 5 to 17 % longer: a fifth number a piece, and its room in LDS).
+// took up to 14 % longer: a fifth number a piece, and its room in LDS).
 //
 // The stored path (more than 128 input columns) spends its time in its three large
 // products; 1200 models of 1 to 200 units, 1000 columns, 1024 samples, gated, in a trace of
-// four passes: 5650 us of them at 175 TFLOP/s (a library fp32 product reached 152; a pass
+// four passes: 5680 us of them at 174 TFLOP/s (a library fp32 product reached 152; a pass
 // among a hundred takes 5600 us in all, them at about 200), k_blk_fwd 222 us and k_blk_bwd
-// 374 us for 1.0 and 2.0 GB.
+// 372 us for 1.0 and 2.0 GB.
 
 #include "block_loss.h"
 

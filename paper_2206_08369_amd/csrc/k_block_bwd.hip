@@ -16,10 +16,10 @@
 // The norm's gradient needs no sums over units (see k_block.hip).
 //
 // Bound by its instructions.  6000 models of 1 to 100 units, 100 columns, 256 samples (in
-// a trace of four passes): gated 381 us, that is 163 TFLOP/s of fp32 products (1.0 PFLOP/s
+// a trace of four passes): gated 390 us, that is 159 TFLOP/s of fp32 products (0.95 PFLOP/s
 // of bf16 ones), the matrix units busy 0.56 of the time and the vector units 0.45; normed
-// 250 us, 0.40 and 0.52.  Wide models, ten outputs, 32 columns and samples, both: 180 us for
-// 669 MB, 3.7 TB/s (a large copy 4.8).  Two waves a SIMD is what the registers allow;
+// 253 us, 0.40 and 0.52.  Wide models, ten outputs, 32 columns and samples, both: 181 us for
+// 668 MB, 3.7 TB/s (a large copy 4.8).  Two waves a SIMD is what the registers allow;
 // where the input has no block of 32 columns, three.
 //
 // The second product takes NF = 2 NC blocks of 16 columns, and one more for the fp32

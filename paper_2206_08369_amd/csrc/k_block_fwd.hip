@@ -14,9 +14,9 @@
 // pre-activations.
 //
 // Bound by its instructions, as the backward.  6000 models of 1 to 100 units, 100
-// columns, 256 samples (in a trace of four passes): gated 205 us, 151 TFLOP/s of fp32
-// products (0.91 PFLOP/s of bf16 ones), matrix and vector units busy 0.59 each; normed
-// 150 us, 0.37 and 0.80.  With one sample it is bound by the weights: gated, 56 us
+// columns, 256 samples (in a trace of four passes): gated 207 us, 150 TFLOP/s of fp32
+// products (0.90 PFLOP/s of bf16 ones), matrix and vector units busy 0.58 and 0.59; normed
+// 152 us, 0.37 and 0.80.  With one sample it is bound by the weights: gated, 56 us
 // for 245 MB (4.4 TB/s).  (A form with the tiles of whole models in one workgroup,
 // which merged them itself, saved the output kernel's 7 us there and lost more by its
 // uneven groups: 59 -> 66 us in all, at 10,000 samples 669 -> 692.)

@@ -94,6 +94,11 @@ extern "C" {
 #define PMLP_NORM 8       /* the activations multiply; a layer norm over each model's
                              hidden units */
 
+#define PMLP_MAT_W1 0     /* the weight matrices of pmlp_orthogonalize and */
+#define PMLP_MAT_V1 1     /* pmlp_muon_step */
+#define PMLP_MAT_W2 2
+#define PMLP_MAT_W12 3
+
 typedef struct pmlp* pmlp_t;
 
 /* Create a packed model of M MLPs with F inputs and O outputs each.
@@ -212,6 +217,75 @@ int pmlp_get_params_block(pmlp_t h, float* W1_host, float* V1_host, float* W2_ho
                           float* gain_host, float* shift_host);
 int pmlp_set_params_block(pmlp_t h, const float* W1_host, const float* V1_host,
                           const float* W2_host, const float* gain_host, const float* shift_host);
+
+/* A pack as a mixture: every sample is answered by K of the models.
+ *
+ * pmlp_route chooses them: scores_dev [B, M] fp32, K in [1, 16]; the K best scores of
+ * each sample, best first (of equal scores the lower index first), into idx_dev [B, K]
+ * int32, and the softmax over the chosen scores into weight_dev [B, K].  A score of
+ * -inf or NaN is never chosen: where fewer than K are left, the slots behind them have
+ * index -1 and weight 0.  (+inf makes the weights of its sample NaN.)
+ * pmlp_route_backward: dscores_dev [B, M] from the gradients dweight_dev [B, K] of the
+ * weights, 0 for models that were not chosen.
+ * Both are for every handle; the buffers of a call must not overlap. */
+int pmlp_route(pmlp_t h, const float* scores_dev, int32_t B, int32_t K, int32_t* idx_dev,
+               float* weight_dev);
+int pmlp_route_backward(pmlp_t h, const int32_t* idx_dev, const float* weight_dev,
+                        const float* dweight_dev, int32_t B, int32_t K, float* dscores_dev);
+
+/* The mixture's answers: Y_dev [B, O],
+ *   Y[b, o] = sum_k weight[b, k] logits[b, idx[b, k], o]
+ * with the logits of pmlp_forward; models that a sample did not choose compute nothing
+ * for it.  idx_dev and weight_dev as pmlp_route gives them, or the caller's own: any
+ * weights, the same model twice, -1 for a slot that is not used (a sample without any
+ * gives 0).  Other indices outside [0, M) count as -1 and are reported by the next
+ * pmlp_routed_status.
+ * pmlp_gradients_routed: the gradients of a loss from dY_dev [B, O] = dLoss/dY, summed
+ * over the samples that chose a model: dW1_dev [N, F], dV1_dev [N, F] (gated packs,
+ * otherwise ignored), dW2_dev [O, N] (0 for models that no sample chose; features that a
+ * mask hides have gradient 0) and dweight_dev [B, K] (0 for unused slots).
+ * For packs with one hidden layer, gated or not, without biases and norm, in PMLP_FP32;
+ * others return PMLP_ESTATE.  Neither call changes the losses of pmlp_losses.  Results
+ * do not depend on timing.  Outputs must not overlap inputs or each other.
+ * The calls, and those of pmlp_orthogonalize and pmlp_muon_step, share one workspace of the
+ * handle that behaves as that of pmlp_create_block: a call that needs a larger one than
+ * those before it waits for the device, one under graph capture returns PMLP_ESTATE
+ * instead, and calls and graph replays of one handle have to be kept in order. */
+int pmlp_forward_routed(pmlp_t h, const float* X_dev, int32_t B, const int32_t* idx_dev,
+                        const float* weight_dev, int32_t K, float* Y_dev);
+int pmlp_gradients_routed(pmlp_t h, const float* X_dev, int32_t B, const int32_t* idx_dev,
+                          const float* weight_dev, int32_t K, const float* dY_dev, float* dW1_dev,
+                          float* dV1_dev, float* dW2_dev, float* dweight_dev);
+
+/* Synchronises the stream.  PMLP_EINVAL if a routed call since the last one of these saw
+ * a model index outside [-1, M). */
+int pmlp_routed_status(pmlp_t h);
+
+/* The orthogonalised direction of a weight matrix of every model (the update of the Muon
+ * optimiser): with U = G, or with momentum
+ *   mom_out = mu mom_in + G,  U = mom_out, or G + mu mom_out (nesterov != 0),
+ * X = U / |U|_F (Frobenius norm; a zero matrix stays zero) and `steps` times
+ *   A = X X^T,  X = 3.4445 X + (-4.7750 A + 2.0315 A A) X
+ * (equal to the same steps on X^T), which takes all singular values of U to about 1; out
+ * receives X.  matrix: PMLP_MAT_W1 or PMLP_MAT_V1 (buffers [N, F], model m's matrix its
+ * rows), PMLP_MAT_W2 ([O, N], its columns; [O, N2] of a two-hidden-layer pack) or
+ * PMLP_MAT_W12 ([K] as pmlp_get_params_deep).  A matrix the pack does not have returns
+ * PMLP_ESTATE.  steps in [1, 32] (5 is usual).  fp32; a model whose U is not finite gets
+ * NaN, the others what they get without it.  mom_in and mom_out may be the same buffer or
+ * both null, out may be G; otherwise the buffers must not overlap. */
+int pmlp_orthogonalize(pmlp_t h, int32_t matrix, const float* G_dev, const float* mom_in_dev,
+                       float* mom_out_dev, float mu, int32_t nesterov, int32_t steps,
+                       float* out_dev);
+
+/* One update of a weight matrix of every model by that direction (mom_dev is updated in
+ * place; null: no momentum):
+ *   W -= rate_m (decay W + sqrt(max(1, rows / cols)) X),
+ * rows x cols the shape of the model's matrix (W1: h_m x F), rate_m = lr, or lr_dev[m] where
+ * lr_dev is not null (device, [M]; a non-finite one is reported as by pmlp_train_step_lr).
+ * steps in [0, 32]; 0 takes U itself in place of sqrt(..) X: SGD with momentum.  Weights
+ * of features that a model does not see stay zero. */
+int pmlp_muon_step(pmlp_t h, int32_t matrix, const float* G_dev, float* mom_dev, float mu,
+                   int32_t nesterov, int32_t steps, float lr, const float* lr_dev, float decay);
 
 /* Free the handle and every device buffer it owns (synchronises its
  * stream first).  A null handle is accepted. */

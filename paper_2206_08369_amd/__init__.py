@@ -31,6 +31,8 @@ __all__ = [
     "PMLP_ARITH_NONE", "PMLP_ARITH_FP32", "PMLP_ARITH_X3", "PMLP_ARITH_BF16", "PackedMLP",
     "DeepPackedMLP", "PMLP_GATED", "PMLP_NORM", "pmlp_create_block", "pmlp_gradients_block",
     "pmlp_gradients_block_mse", "pmlp_get_params_block", "pmlp_set_params_block", "BlockPackedMLP",
+    "pmlp_route", "pmlp_route_backward", "pmlp_forward_routed", "pmlp_gradients_routed",
+    "pmlp_routed_status", "pmlp_orthogonalize", "pmlp_muon_step", "MATRIX_IDS",
 ]
 
 PMLP_OK = 0
@@ -52,6 +54,9 @@ ACT_IDS = {
     "gelu": 6, "silu": 7, "softplus": 8, "swish2": 9,
     "selu": 10, "hardshrink": 11, "mish": 12,
 }
+
+# the weight matrices of pmlp_orthogonalize and pmlp_muon_step
+MATRIX_IDS = {"W1": 0, "V1": 1, "W2": 2, "W12": 3}
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _lib = None
@@ -114,6 +119,13 @@ def load_library():
         "pmlp_gradients_block_mse": [P, P, P, i32, P, P, P, P, P],
         "pmlp_get_params_block": [P, P, P, P, P, P],
         "pmlp_set_params_block": [P, P, P, P, P, P],
+        "pmlp_route": [P, P, i32, i32, P, P],
+        "pmlp_route_backward": [P, P, P, P, i32, i32, P],
+        "pmlp_forward_routed": [P, P, i32, P, P, i32, P],
+        "pmlp_gradients_routed": [P, P, i32, P, P, i32, P, P, P, P, P],
+        "pmlp_routed_status": [P],
+        "pmlp_orthogonalize": [P, i32, P, P, P, f32, i32, i32, P],
+        "pmlp_muon_step": [P, i32, P, P, f32, i32, i32, f32, P, f32],
         "pmlp_kernel_variant": [P, i32, C.POINTER(C.c_char_p), C.POINTER(i32)],
     }
     for name, args in sig.items():
@@ -396,6 +408,47 @@ def pmlp_set_params_block(h: int, W1=None, V1=None, W2=None, gain=None, shift=No
                                                      for c in arrs]), "pmlp_set_params_block")
 
 
+def pmlp_route(h: int, scores, B: int, K: int, idx, weight) -> None:
+    _check(load_library().pmlp_route(h, _ptr(scores), int(B), int(K), _ptr(idx), _ptr(weight)),
+           "pmlp_route")
+
+
+def pmlp_route_backward(h: int, idx, weight, dweight, B: int, K: int, dscores) -> None:
+    _check(load_library().pmlp_route_backward(h, _ptr(idx), _ptr(weight), _ptr(dweight), int(B),
+                                              int(K), _ptr(dscores)), "pmlp_route_backward")
+
+
+def pmlp_forward_routed(h: int, X, B: int, idx, weight, K: int, Y) -> None:
+    _check(load_library().pmlp_forward_routed(h, _ptr(X), int(B), _ptr(idx), _ptr(weight), int(K),
+                                              _ptr(Y)), "pmlp_forward_routed")
+
+
+def pmlp_gradients_routed(h: int, X, B: int, idx, weight, K: int, dY, dW1, dV1, dW2,
+                          dweight) -> None:
+    _check(load_library().pmlp_gradients_routed(h, _ptr(X), int(B), _ptr(idx), _ptr(weight), int(K),
+                                                _ptr(dY), _ptr(dW1), _ptr(dV1), _ptr(dW2),
+                                                _ptr(dweight)), "pmlp_gradients_routed")
+
+
+def pmlp_routed_status(h: int) -> None:
+    """Raises if a routed call since the last one of these saw a bad model index."""
+    _check(load_library().pmlp_routed_status(h), "pmlp_routed_status")
+
+
+def pmlp_orthogonalize(h: int, matrix: int, G, mom_in, mom_out, mu: float, nesterov: bool,
+                       steps: int, out) -> None:
+    _check(load_library().pmlp_orthogonalize(h, int(matrix), _ptr(G), _ptr(mom_in), _ptr(mom_out),
+                                             float(mu), 1 if nesterov else 0, int(steps),
+                                             _ptr(out)), "pmlp_orthogonalize")
+
+
+def pmlp_muon_step(h: int, matrix: int, G, mom, mu: float, nesterov: bool, steps: int, lr: float,
+                   lr_dev=None, decay: float = 0.0) -> None:
+    _check(load_library().pmlp_muon_step(h, int(matrix), _ptr(G), _ptr(mom), float(mu),
+                                         1 if nesterov else 0, int(steps), float(lr), _ptr(lr_dev),
+                                         float(decay)), "pmlp_muon_step")
+
+
 def pmlp_set_feature_mask(h: int, mask: Optional[np.ndarray]) -> None:
     if mask is None:
         _check(load_library().pmlp_set_feature_mask(h, None), "pmlp_set_feature_mask")
@@ -565,6 +618,125 @@ class PackedMLP:
         self._stream()
         pmlp_hidden(self.handle, X, B, Z, H)
         return Z, H
+
+    def _dev(self, t, dtype, shape, what):
+        """A contiguous tensor of that type and shape on the pack's device."""
+        if not (isinstance(t, self._torch.Tensor) and t.is_cuda and t.dtype == dtype
+                and t.is_contiguous() and tuple(t.shape) == tuple(shape)
+                and t.device == self.device):
+            raise ValueError("%s must be a contiguous %s %s tensor on %s"
+                             % (what, str(dtype).replace("torch.", ""), list(shape), self.device))
+        return t
+
+    def _empty(self, shape, dtype=None):
+        return self._torch.empty(shape, dtype=dtype or self._torch.float32, device=self.device)
+
+    def _choices(self, idx, weight, B=None):
+        t = self._torch
+        if not (isinstance(idx, t.Tensor) and idx.dim() == 2 and (B is None or idx.shape[0] == B)):
+            raise ValueError("idx must be an int32 [B, K] tensor")
+        self._dev(idx, t.int32, idx.shape, "idx")
+        self._dev(weight, t.float32, idx.shape, "weight")
+        return idx.shape
+
+    def route(self, scores, K: int):
+        """The K best models of each sample by scores [B, M], best first (of equal scores the
+        lower index), and the softmax of their scores: (idx int32 [B, K], weight [B, K]).
+        Scores of -inf or NaN are never chosen; unused slots have index -1 and weight 0."""
+        t = self._torch
+        if not (isinstance(scores, t.Tensor) and scores.dim() == 2):
+            raise ValueError("scores must be a float32 [B, %d] tensor" % self.M)
+        B = scores.shape[0]
+        self._dev(scores, t.float32, (B, self.M), "scores")
+        idx, weight = self._empty((B, max(int(K), 1)), t.int32), self._empty((B, max(int(K), 1)))
+        self._stream()
+        pmlp_route(self.handle, scores, B, K, idx, weight)
+        return idx, weight
+
+    def route_backward(self, idx, weight, dweight):
+        """Gradient [B, M] of the scores from that of the weights route gave."""
+        B, K = self._choices(idx, weight)
+        self._dev(dweight, self._torch.float32, (B, K), "dweight")
+        out = self._empty((B, self.M))
+        self._stream()
+        pmlp_route_backward(self.handle, idx, weight, dweight, B, K, out)
+        return out
+
+    def forward_routed(self, X, idx, weight, out=None):
+        """The pack as a mixture: [B, O] sums over each sample's models idx [B, K] of weight
+        times logits.  Only those models compute."""
+        B = self._x(X)
+        K = self._choices(idx, weight, B)[1]
+        if out is None:
+            out = self._empty((B, self.O))
+        else:
+            self._dev(out, self._torch.float32, (B, self.O), "out")
+        self._stream()
+        pmlp_forward_routed(self.handle, X, B, idx, weight, K, out)
+        return out
+
+    def gradients_routed(self, X, idx, weight, dY):
+        """Gradients of the mixture from dY [B, O]: dW1, (dV1 of a gated pack,) dW2 and the
+        gradient [B, K] of the weights."""
+        B = self._x(X)
+        K = self._choices(idx, weight, B)[1]
+        self._dev(dY, self._torch.float32, (B, self.O), "dY")
+        gated = getattr(self, "gated", False)
+        dW1, dW2 = self._empty((self.N, self.F)), self._empty((self.O, self.N))
+        dV1 = self._empty((self.N, self.F)) if gated else None
+        dweight = self._empty((B, K))
+        self._stream()
+        pmlp_gradients_routed(self.handle, X, B, idx, weight, K, dY, dW1, dV1, dW2, dweight)
+        return (dW1, dV1, dW2, dweight) if gated else (dW1, dW2, dweight)
+
+    def check_routed(self) -> None:
+        """Raises if a routed call since the last check saw a model index outside [-1, M)."""
+        pmlp_routed_status(self.handle)
+
+    def _matrix(self, matrix):
+        if matrix not in MATRIX_IDS:
+            raise ValueError("matrix must be one of %s" % ", ".join(sorted(MATRIX_IDS)))
+        if matrix == "W2":
+            return (self.O, getattr(self, "N2", self.N))
+        if matrix == "W12":
+            return (getattr(self, "K", 0),)
+        return (self.N, self.F)
+
+    def orthogonalize(self, G, matrix: str = "W1", steps: int = 5, momentum=None, mu: float = 0.95,
+                      nesterov: bool = True, momentum_out=None, out=None):
+        """The orthogonalised direction of every model's `matrix` from its gradient G, by
+        `steps` Newton-Schulz steps; momentum (if given) is advanced in place, or into
+        momentum_out."""
+        t = self._torch
+        shape = self._matrix(matrix)
+        self._dev(G, t.float32, shape, "G")
+        if momentum is None and momentum_out is not None:
+            raise ValueError("momentum_out needs momentum")
+        if momentum is not None:
+            self._dev(momentum, t.float32, shape, "momentum")
+            momentum_out = momentum if momentum_out is None else momentum_out
+            self._dev(momentum_out, t.float32, shape, "momentum_out")
+        out = self._empty(shape) if out is None else self._dev(out, t.float32, shape, "out")
+        self._stream()
+        pmlp_orthogonalize(self.handle, MATRIX_IDS[matrix], G, momentum, momentum_out, mu, nesterov,
+                           steps, out)
+        return out
+
+    def muon_step(self, G, lr, matrix: str = "W1", momentum=None, mu: float = 0.95,
+                  nesterov: bool = True, steps: int = 5, decay: float = 0.0) -> None:
+        """One update of every model's `matrix` by its orthogonalised direction (steps=0: by
+        the momentum itself); lr is one rate, or a float32 device tensor of M rates."""
+        t = self._torch
+        shape = self._matrix(matrix)
+        self._dev(G, t.float32, shape, "G")
+        if momentum is not None:
+            self._dev(momentum, t.float32, shape, "momentum")
+        rates = None
+        if isinstance(lr, t.Tensor):
+            rates, lr = self._dev(lr, t.float32, (self.M,), "per-model lr"), 0.0
+        self._stream()
+        pmlp_muon_step(self.handle, MATRIX_IDS[matrix], G, momentum, mu, nesterov, steps, lr, rates,
+                       decay)
 
     def losses(self) -> np.ndarray:
         return pmlp_losses(self.handle)

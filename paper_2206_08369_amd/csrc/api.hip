@@ -4,7 +4,9 @@
 
 #include "pmlp.h"
 #include "block.h"
+#include "newton.h"
 #include "pmlp_internal.h"
+#include "routed.h"
 
 #include <algorithm>
 #include <cmath>
@@ -101,6 +103,32 @@ struct PmlpDeep {
   float* Zt2 = nullptr;       // [N2pad][Bp]
 };
 
+// A workspace that grows with the calls.  A captured graph keeps the addresses it was
+// captured with, so a buffer that one has and a larger call replaces lives until the
+// handle goes.
+struct GrowingWs {
+  unsigned char* ws = nullptr;
+  size_t cap = 0;
+  bool captured = false;
+  std::vector<unsigned char*> retired;
+};
+
+// How pmlp_orthogonalize goes through one kind of weight matrix: slices of models whose
+// workspace is bounded, each with its runs of the item lists.
+struct NewtonSlice {
+  int32_t load0, load, sym0, sym;  // items: all tiles of X, lower tiles of A
+  int64_t nx, na;                  // entries of a plane
+};
+struct PmlpNewton {
+  NsMat* d_mats = nullptr;
+  NsPiece* d_pieces = nullptr;
+  NsItem* d_items = nullptr;
+  int32_t npieces = 0;
+  std::vector<NewtonSlice> slices;
+  int64_t nx = 0, na = 0;  // of the largest slice
+};
+constexpr int kMatrices = 4;  // PMLP_MAT_*
+
 // How a batch runs through the fused forward of a block pack: SC samples a workgroup,
 // wpc workgroups of `waves` waves for each SC samples, runs of `run` tiles (BlkMap), so
 // many records.  SC = 0: it does not.
@@ -111,7 +139,7 @@ struct BlkRun {
 
 // The gate and the norm of a pack made by pmlp_create_block (W1 is then the
 // first half of one allocation whose second half, if gated, is V1).
-struct PmlpBlock {
+struct PmlpBlock : GrowingWs {
   bool gated = false, norm = false;
   float* V1 = nullptr;     // [Npad][F4], inside W1's allocation
   float* gain = nullptr;   // [Npad]
@@ -129,12 +157,6 @@ struct PmlpBlock {
   BlkRun plan[2];
   int32_t lplanned = 0;  // padded batch size of `lplan`
   BlkLocal lplan{};
-  // Workspace.  A captured graph keeps the addresses it was captured with, so a
-  // buffer that one has and a larger batch replaces lives until the handle goes.
-  unsigned char* ws = nullptr;
-  size_t cap = 0;
-  bool captured = false;
-  std::vector<unsigned char*> retired;
 };
 
 // How a batch class (a padded batch size up to 256) divides the pack for
@@ -194,6 +216,8 @@ struct pmlp {
   bool w1b_valid = false;         // W1b equals bf16(W1)
   PmlpDeep* deep = nullptr;     // second hidden layer (pmlp_create_deep), or null
   PmlpBlock* block = nullptr;   // gate and norm (pmlp_create_block), or null
+  GrowingWs extra;              // of the routed calls and the orthogonalised updates
+  PmlpNewton* newton[kMatrices] = {};  // by matrix, made by its first call
   float* stage = nullptr;       // rows on their way to or from the host (copy_rows)
   size_t cap_stage = 0;         // floats, at most kStageFloats
   uint32_t* d_fmask = nullptr;  // per-model feature masks [M][fmw] (null: none)
@@ -278,6 +302,17 @@ void release(pmlp* h) {
     for (unsigned char*& p : k->retired) dfree(p);
     delete k;
     h->block = nullptr;
+  }
+  dfree(h->extra.ws);
+  for (unsigned char*& p : h->extra.retired) dfree(p);
+  h->extra = GrowingWs{};
+  for (PmlpNewton*& q : h->newton) {
+    if (!q) continue;
+    dfree(q->d_mats);
+    dfree(q->d_pieces);
+    dfree(q->d_items);
+    delete q;
+    q = nullptr;
   }
   h->w1b_valid = false;
   h->capBp = 0;
@@ -1408,8 +1443,8 @@ struct Carver {
   }
 };
 
-int ensure_block_ws(pmlp* h, size_t bytes) {
-  PmlpBlock* k = h->block;
+// what: the calls it is for, in messages
+int ensure_ws(pmlp* h, GrowingWs* k, size_t bytes, const char* what) {
   // (the null stream cannot be asked while another one captures; the capture goes on)
   hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
   if (!k->captured || bytes > k->cap) {
@@ -1423,8 +1458,8 @@ int ensure_block_ws(pmlp* h, size_t bytes) {
     return PMLP_OK;
   }
   if (st != hipStreamCaptureStatusNone)
-    return fail(PMLP_ESTATE, "under graph capture a block pack needs an earlier call of this kind "
-                             "and batch size");
+    return fail(PMLP_ESTATE, std::string("under graph capture ") + what +
+                                 " needs an earlier call of this kind and batch size");
   size_t want = bytes;
   if (bytes < (size_t)64 << 20)  // few small buffers on the way to a large batch
     for (want = (size_t)1 << 16; want < bytes;) want <<= 1;
@@ -1444,8 +1479,8 @@ int ensure_block_ws(pmlp* h, size_t bytes) {
   }
   if (e != hipSuccess) {
     (void)hipGetLastError();
-    return fail(PMLP_ENOMEM, "block workspace allocation failed (" + std::to_string(want >> 20) +
-                                 " MiB)");
+    return fail(PMLP_ENOMEM, std::string("workspace allocation of ") + what + " failed (" +
+                                 std::to_string(want >> 20) + " MiB)");
   }
   int rc = PMLP_OK;
   if (k->ws && k->captured) {
@@ -1466,6 +1501,8 @@ int ensure_block_ws(pmlp* h, size_t bytes) {
   k->cap = want;
   return PMLP_OK;
 }
+
+int ensure_block_ws(pmlp* h, size_t bytes) { return ensure_ws(h, h->block, bytes, "a block pack"); }
 
 // Whether k_blk_gemm takes a product of NP x NQ over K, by what either costs in us: a
 // 16-k stage of the large tiles (256 x 256, 256 x 64 or 128 x 128; see launch_gemm_bf16)
@@ -1855,6 +1892,415 @@ int block_grads(pmlp* h, float* dW1, float* dV1, float* dW2, float* dgain, float
     return fail(PMLP_EINVAL, "null gradient buffer");
   *out = BlockGrads{dW1, k->gated ? dV1 : nullptr, dW2, k->norm ? dgain : nullptr,
                     k->norm ? dshift : nullptr};
+  return PMLP_OK;
+}
+
+// ---- routed packs ------------------------------------------------------------------
+
+struct Span {
+  const void* p;
+  size_t bytes;
+};
+bool overlap(const Span& a, const Span& b) {
+  const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
+  return a.p && b.p && a0 < b0 + b.bytes && b0 < a0 + a.bytes;
+}
+
+int check_choices(pmlp* h, int32_t B, int32_t K) {
+  if (int rc = check_handle(h)) return rc;
+  if (B < 1 || B > kMaxBatch) return fail(PMLP_EINVAL, "batch size out of range [1, 2^20]");
+  if (K < 1 || K > kRtMaxK) return fail(PMLP_EINVAL, "K must be in [1, 16]");
+  return PMLP_OK;
+}
+
+// What the routed forward and gradients are provided for.
+int check_routed(pmlp* h, const void* X, int32_t B, const void* idx, const void* weight, int32_t K) {
+  if (int rc = check_choices(h, B, K)) return rc;
+  if (!X || !idx || !weight) return fail(PMLP_EINVAL, "null X, indices or weights");
+  if (h->deep || h->bcol >= 0 || (h->block && h->block->norm))
+    return fail(PMLP_ESTATE, "routed calls are for packs with one hidden layer and neither biases nor "
+                             "a norm");
+  if (h->precision != PMLP_FP32) return fail(PMLP_ESTATE, "routed calls are fp32 (pmlp_set_precision)");
+  return PMLP_OK;
+}
+
+// Tiles of the routed products: those of a wave that the pack and the mean number of rows
+// of a model fill.
+RtShape rt_shape(const pmlp* h, int64_t R) {
+  RtShape sh;
+  sh.na = h->N > (int64_t)64 * h->M ? 2 : 1;
+  sh.nb = R > (int64_t)64 * h->M ? 2 : 1;
+  return sh;
+}
+
+// Whether every slot goes to its model on its own.
+bool rt_few(const pmlp* h, int64_t R) { return R <= 16 || R <= 2 * (int64_t)h->M; }
+
+// Where the parts of a routed call's workspace lie.
+struct RtLayout {
+  Carver c;
+  RtPlan p{};
+  int64_t items = 0, jitems = 0;  // at most
+  size_t hist = 0, count = 0, place = 0, zoff = 0, ioff = 0, joff = 0, slot = 0, item = 0, jitem = 0;
+  bool fits = true;
+};
+
+RtLayout rt_layout(const pmlp* h, int64_t R, int32_t K, const RtShape& sh, bool train) {
+  RtLayout l;
+  RtPlan& p = l.p;
+  const bool gated = h->block && h->block->gated;
+  p.R = (int32_t)R;
+  p.K = K;
+  p.M = h->M;
+  const int64_t groups = std::min<int64_t>(h->M, R);  // that have rows, at most
+  const int64_t P = R + (kRtPad - 1) * groups;
+  p.P = (int32_t)P;
+  p.chunk = (int32_t)((R + kRtChunks - 1) / kRtChunks + 63) / 64 * 64;
+  p.nchunk = (int32_t)((R + p.chunk - 1) / p.chunk);
+  p.F = h->F;
+  p.O = h->O;
+  p.seg_off = h->d_seg_off;
+  p.flag = h->flag;
+  p.t.rt = rt_rows(sh);
+  p.t.uc = rt_units(sh, gated);
+  p.t.du = p.t.uc;
+  p.t.df = h->F > 64 ? 128 : 64;
+  const int64_t whole = (R + kRtPad - 1) / kRtPad * kRtPad;  // places of a model with every slot
+  p.t.part = (int32_t)whole;
+  l.items = (R / p.t.rt + groups) * div_up(h->widest, p.t.uc);
+  int64_t tiles = 0;
+  if (train) {
+    for (int32_t hm : h->hs) tiles += (int64_t)div_up(hm, p.t.du) * div_up(h->F, p.t.df);
+    // few tiles and many rows: parts of the rows side by side
+    if (tiles < 512) {
+      const int64_t parts = 1024 / tiles;
+      p.t.part = (int32_t)std::min<int64_t>(whole, std::max<int64_t>(256, (whole / parts + 31) / 32 * 32));
+    }
+    // (a model's last part may be short: one more for each model)
+    l.jitems = tiles * ((whole + p.t.part - 1) / p.t.part);
+    if (p.t.part < whole) l.jitems = std::min(l.jitems, tiles + div_up(P, p.t.part) * (int64_t)div_up(h->widest, p.t.du) * div_up(h->F, p.t.df));
+  }
+  l.fits = l.items < (1 << 30) && l.jitems < (1 << 30) && P < (1 << 30);
+  if (!l.fits) return l;
+  const size_t M = (size_t)h->M;
+  l.hist = l.c.take((size_t)p.nchunk * M);
+  l.count = l.c.take(M);
+  l.place = l.c.take(M + 1);
+  l.zoff = l.c.take(2 * (M + 1));
+  l.ioff = l.c.take(M + 1);
+  l.joff = l.c.take(M + 1);
+  l.slot = l.c.take((size_t)P);
+  l.item = l.c.take(4 * (size_t)l.items);
+  l.jitem = l.c.take(4 * (size_t)l.jitems);
+  return l;
+}
+
+void rt_place(RtLayout* l, unsigned char* ws, const int32_t* idx, bool train) {
+  RtPlan& p = l->p;
+  p.idx = idx;
+  p.hist = (int32_t*)(ws + l->hist);
+  p.count = (int32_t*)(ws + l->count);
+  p.place = (int32_t*)(ws + l->place);
+  p.zoff = (int64_t*)(ws + l->zoff);
+  p.ioff = (int32_t*)(ws + l->ioff);
+  p.joff = (int32_t*)(ws + l->joff);
+  p.slot = (int32_t*)(ws + l->slot);
+  p.items = (RtItem*)(ws + l->item);
+  p.jitems = train ? (RtItem*)(ws + l->jitem) : nullptr;
+}
+
+RtArgs rt_args(const pmlp* h, const float* X, const RtLayout& l) {
+  const RtPlan& p = l.p;
+  RtArgs a{};
+  a.X = X;
+  a.W1 = h->W1;
+  a.V1 = h->block ? h->block->V1 : nullptr;
+  a.W2 = h->W2;
+  a.ldw = h->Npad;
+  a.act = h->d_act;
+  a.seg_off = h->d_seg_off;
+  a.F = h->F;
+  a.F4 = h->F4;
+  a.O = h->O;
+  a.K = p.K;
+  a.M = h->M;
+  a.P = p.P;
+  a.count = p.count;
+  a.place = p.place;
+  a.zoff = p.zoff;
+  a.slot = p.slot;
+  a.items = p.items;
+  a.nitems = p.ioff + h->M;
+  a.most = (int32_t)l.items;
+  return a;
+}
+
+int too_large() { return fail(PMLP_EINVAL, "the batch times K is too large for this pack"); }
+
+int forward_routed(pmlp* h, const float* X, int32_t B, const int32_t* idx, const float* weight,
+                   int32_t K, float* Y) {
+  const int64_t R = (int64_t)B * K;
+  RtJoin j{idx, weight, h->d_seg_off, B, K, h->M, h->O, 0, 0, nullptr, Y};
+  if (rt_few(h, R)) {
+    const int32_t chunks = div_up(h->widest, kRtFewUnits);
+    if (R * chunks > INT32_MAX) return too_large();
+    Carver c;
+    c.take((size_t)R * chunks * h->O);
+    if (int rc = ensure_ws(h, &h->extra, c.bytes, "a routed pack")) return rc;
+    RtLayout none;
+    none.p.K = K;
+    RtArgs a = rt_args(h, X, none);
+    a.part = (float*)h->extra.ws;
+    a.parts = chunks;
+    j.parts = chunks;
+    j.uc = kRtFewUnits;
+    j.part = a.part;
+    const RtFew f{idx, (int32_t)R, chunks, h->flag};
+    if (int rc = run(h, KID_GEMM_FWD, [&] { return launch_rt_few(a, f, h->stream); })) return rc;
+    return run(h, KID_M3_FWD, [&] { return launch_rt_join(j, h->stream); });
+  }
+  const RtShape sh = rt_shape(h, R);
+  RtLayout l = rt_layout(h, R, K, sh, false);
+  if (!l.fits) return too_large();
+  const int32_t parts = 2 * div_up(h->widest, l.p.t.uc);  // (a wave each)
+  const size_t oP = l.c.take((size_t)R * parts * h->O);
+  if (int rc = ensure_ws(h, &h->extra, l.c.bytes, "a routed pack")) return rc;
+  rt_place(&l, h->extra.ws, idx, false);
+  if (int rc = run(h, KID_AUX, [&] { return launch_rt_plan(l.p, h->stream); })) return rc;
+  RtArgs a = rt_args(h, X, l);
+  a.part = (float*)(h->extra.ws + oP);
+  a.parts = parts;
+  j.parts = parts;
+  j.uc = l.p.t.uc / 2;
+  j.part = a.part;
+  if (int rc = run(h, KID_GEMM_FWD, [&] { return launch_rt_tile(a, sh, false, h->stream); })) return rc;
+  return run(h, KID_M3_FWD, [&] { return launch_rt_join(j, h->stream); });
+}
+
+int gradients_routed(pmlp* h, const float* X, int32_t B, const int32_t* idx, const float* weight,
+                     int32_t K, const float* dY, float* dW1, float* dV1, float* dW2, float* dweight) {
+  const int64_t R = (int64_t)B * K;
+  const bool gated = h->block && h->block->gated;
+  const RtShape sh = rt_shape(h, R);
+  RtLayout l = rt_layout(h, R, K, sh, true);
+  if (!l.fits) return too_large();
+  const int32_t parts = 2 * div_up(h->widest, l.p.t.uc);
+  const int64_t whole = (R + kRtPad - 1) / kRtPad * kRtPad;
+  const int32_t nparts = div_up(whole, l.p.t.part);
+  const size_t hidden = (size_t)h->widest * l.p.P, k = gated ? 2 : 1;
+  const size_t oD = l.c.take((size_t)R * parts), oZ = l.c.take(hidden), oH = l.c.take(hidden),
+               oU = l.c.take(gated ? hidden : 0), oY = l.c.take((size_t)h->O * l.p.P),
+               oW = l.c.take(nparts > 1 ? nparts * k * h->N * h->F : 0),
+               oV = l.c.take(nparts > 1 ? (size_t)nparts * h->O * h->N : 0);
+  if (int rc = ensure_ws(h, &h->extra, l.c.bytes, "a routed pack")) return rc;
+  unsigned char* const ws = h->extra.ws;
+  rt_place(&l, ws, idx, true);
+  if (int rc = run(h, KID_AUX, [&] { return launch_rt_plan(l.p, h->stream); })) return rc;
+  RtGrad g{};
+  g.a = rt_args(h, X, l);
+  g.a.parts = parts;
+  g.a.weight = weight;
+  g.a.dY = dY;
+  g.a.dwpart = (float*)(ws + oD);
+  g.a.dZ = (float*)(ws + oZ);
+  g.a.dU = (float*)(ws + oU);
+  g.a.H = (float*)(ws + oH);
+  g.t = l.p.t;
+  g.R = (int32_t)R;
+  g.N = h->N;
+  g.jitems = l.p.jitems;
+  g.njitems = l.p.joff + h->M;
+  g.jmost = (int32_t)l.jitems;
+  g.nparts = nparts;
+  g.dW1 = dW1;
+  g.dV1 = dV1;
+  g.dW2 = dW2;
+  g.wdy = (float*)(ws + oY);
+  g.wpart = (float*)(ws + oW);
+  g.w2part = (float*)(ws + oV);
+  g.mid = h->d_mid;
+  g.fmask = h->d_fmask;
+  g.fmw = h->fmw;
+  if (int rc = run(h, KID_GEMM_FWD, [&] { return launch_rt_tile(g.a, sh, true, h->stream); })) return rc;
+  RtShape shw = sh;
+  shw.nb = l.p.t.df / 64;
+  if (int rc = run(h, KID_GEMM_BWD, [&] { return launch_rt_weights(g, shw, h->stream); })) return rc;
+  const RtJoin j{idx, weight, h->d_seg_off, B, K, h->M, 1, parts, l.p.t.uc / 2, g.a.dwpart, dweight};
+  return run(h, KID_M3_BWD, [&] { return launch_rt_join_dw(j, h->stream); });
+}
+
+// ---- orthogonalised updates ----------------------------------------------------------
+
+// Bytes of a slice's workspace, about (a model's own matrices may need more).
+constexpr size_t kNewtonSlice = (size_t)2 << 30;
+
+size_t newton_bytes(int64_t nx, int64_t na) { return sizeof(_Float16) * (size_t)(8 * nx + 4 * na); }
+
+// The matrices of one kind: their shapes, pieces, slices and items.
+int ensure_newton(pmlp* h, int32_t mat) {
+  if (h->newton[mat]) return PMLP_OK;
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(h->stream, &st) != hipSuccess) {
+    (void)hipGetLastError();
+    st = hipStreamCaptureStatusActive;
+  }
+  if (st != hipStreamCaptureStatusNone)
+    return fail(PMLP_ESTATE, "under graph capture an update needs an earlier call for this matrix");
+  std::vector<NsMat> mats((size_t)h->M);
+  std::vector<NsPiece> pieces;
+  std::vector<NsItem> items;
+  struct Made {
+    PmlpNewton* q;
+    ~Made() {
+      if (!q) return;
+      dfree(q->d_mats);
+      dfree(q->d_pieces);
+      dfree(q->d_items);
+      delete q;
+    }
+  } made{new PmlpNewton()};
+  PmlpNewton* q = made.q;
+  std::vector<NsItem> load, sym;
+  NewtonSlice sl{};
+  auto close = [&] {
+    sl.load0 = (int32_t)items.size();
+    sl.load = (int32_t)load.size();
+    items.insert(items.end(), load.begin(), load.end());
+    sl.sym0 = (int32_t)items.size();
+    sl.sym = (int32_t)sym.size();
+    items.insert(items.end(), sym.begin(), sym.end());
+    q->slices.push_back(sl);
+    q->nx = std::max(q->nx, sl.nx);
+    q->na = std::max(q->na, sl.na);
+    load.clear();
+    sym.clear();
+    sl = NewtonSlice{};
+  };
+  for (int32_t m = 0; m < h->M; ++m) {
+    NsMat& t = mats[m];
+    t = NsMat{};
+    t.m = m;
+    const int64_t off = h->seg_off[m];
+    if (mat == PMLP_MAT_W2) {
+      const int64_t o2 = h->deep ? h->deep->off2[m] : off;
+      t.rows = h->O;
+      t.cols = h->deep ? h->deep->h2[m] : h->hs[m];
+      t.src = t.wsrc = o2;
+      t.ld = (int32_t)(h->deep ? h->deep->N2 : h->N);
+      t.wld = (int32_t)(h->deep ? h->deep->N2pad : h->Npad);
+    } else if (mat == PMLP_MAT_W12) {
+      t.rows = h->deep->h2[m];
+      t.cols = t.ld = t.wld = h->hs[m];
+      t.src = t.wsrc = h->deep->koff[m];
+    } else {
+      t.rows = h->hs[m];
+      t.cols = t.ld = h->F;
+      t.wld = h->F4;
+      t.src = off * h->F;
+      t.wsrc = off * h->F4;
+    }
+    t.r = std::min(t.rows, t.cols);
+    t.c = std::max(t.rows, t.cols);
+    if (t.c > (1 << 30)) return fail(PMLP_EINVAL, "a matrix is too large to be orthogonalised");
+    t.rp = (t.r + 31) / 32 * 32;
+    t.cp = (t.c + 31) / 32 * 32;
+    const int64_t nx = (int64_t)t.rp * t.cp, na = (int64_t)t.rp * t.rp;
+    if (sl.nx && newton_bytes(sl.nx + nx, sl.na + na) > kNewtonSlice) close();
+    t.xo = sl.nx;
+    t.ao = sl.na;
+    sl.nx += nx;
+    sl.na += na;
+    const int32_t ti = div_up(t.rp, kNsTile), tj = div_up(t.cp, kNsTile);
+    for (int32_t i = 0; i < ti; ++i) {
+      for (int32_t j = 0; j < tj; ++j) load.push_back(NsItem{m, i, j, 0});
+      for (int32_t j = 0; j <= i; ++j) sym.push_back(NsItem{m, i, j, 0});
+    }
+    t.piece0 = (int32_t)pieces.size();
+    const int32_t rows = std::max(1, kNsPiece / t.cols);
+    for (int32_t r = 0; r < t.rows; r += rows)
+      pieces.push_back(NsPiece{m, r, std::min(rows, t.rows - r), 0});
+    t.pieces = (int32_t)pieces.size() - t.piece0;
+  }
+  close();
+  q->npieces = (int32_t)pieces.size();
+  if (hipMalloc(&q->d_mats, mats.size() * sizeof(NsMat)) != hipSuccess ||
+      hipMalloc(&q->d_pieces, pieces.size() * sizeof(NsPiece)) != hipSuccess ||
+      hipMalloc(&q->d_items, items.size() * sizeof(NsItem)) != hipSuccess) {
+    (void)hipGetLastError();
+    return fail(PMLP_ENOMEM, "device allocation failed for the update's plan");
+  }
+  PMLP_HIP(hipMemcpy(q->d_mats, mats.data(), mats.size() * sizeof(NsMat), hipMemcpyHostToDevice));
+  PMLP_HIP(hipMemcpy(q->d_pieces, pieces.data(), pieces.size() * sizeof(NsPiece), hipMemcpyHostToDevice));
+  PMLP_HIP(hipMemcpy(q->d_items, items.data(), items.size() * sizeof(NsItem), hipMemcpyHostToDevice));
+  h->newton[mat] = q;
+  made.q = nullptr;
+  return PMLP_OK;
+}
+
+int check_matrix(pmlp* h, int32_t mat, const void* G) {
+  if (int rc = check_handle(h)) return rc;
+  if (mat < 0 || mat >= kMatrices) return fail(PMLP_EINVAL, "unknown matrix");
+  if (!G) return fail(PMLP_EINVAL, "null gradient");
+  if (mat == PMLP_MAT_V1 && !(h->block && h->block->gated))
+    return fail(PMLP_ESTATE, "the pack has no gate (V1)");
+  if (mat == PMLP_MAT_W12 && !h->deep)
+    return fail(PMLP_ESTATE, "the pack has no second hidden layer (W12)");
+  return PMLP_OK;
+}
+
+// Bytes of the caller's buffers for matrix `mat`.
+size_t matrix_bytes(const pmlp* h, int32_t mat) {
+  const int64_t n = mat == PMLP_MAT_W12  ? h->deep->K
+                    : mat == PMLP_MAT_W2 ? (int64_t)h->O * (h->deep ? h->deep->N2 : h->N)
+                                         : h->N * h->F;
+  return (size_t)n * sizeof(float);
+}
+
+// a: G, momentum, out or W and what belongs to it.
+int newton(pmlp* h, int32_t mat, NsArgs a, int32_t steps) {
+  if (int rc = use_device(h)) return rc;
+  if (int rc = ensure_newton(h, mat)) return rc;
+  const PmlpNewton* q = h->newton[mat];
+  a.mats = q->d_mats;
+  a.pieces = q->d_pieces;
+  a.flag = h->flag;
+  if (mat == PMLP_MAT_W1 && a.W) {
+    a.fmask = h->d_fmask;
+    a.fmw = h->fmw;
+  }
+  if (steps == 0)
+    return run(h, KID_AUX, [&] { return launch_ns_momentum(a, 0, q->npieces, true, h->stream); });
+  Carver c;
+  auto halves = [&](int64_t n) { return c.take((size_t)(n + 1) / 2); };
+  const size_t oS = c.take(2 * (size_t)q->npieces);
+  const size_t oX0 = halves(2 * q->nx), oX1 = halves(2 * q->nx), oT0 = halves(2 * q->nx),
+               oT1 = halves(2 * q->nx), oA = halves(2 * q->na), oP = halves(2 * q->na);
+  if (int rc = ensure_ws(h, &h->extra, c.bytes, "an orthogonalised update")) return rc;
+  unsigned char* const ws = h->extra.ws;
+  a.sums = (double*)(ws + oS);
+  a.X[0] = (_Float16*)(ws + oX0);
+  a.X[1] = (_Float16*)(ws + oX1);
+  a.XT[0] = (_Float16*)(ws + oT0);
+  a.XT[1] = (_Float16*)(ws + oT1);
+  a.A = (_Float16*)(ws + oA);
+  a.P = (_Float16*)(ws + oP);
+  a.nx = q->nx;
+  a.na = q->na;
+  if (int rc = run(h, KID_AUX, [&] { return launch_ns_momentum(a, 0, q->npieces, false, h->stream); }))
+    return rc;
+  for (const NewtonSlice& sl : q->slices) {
+    const NsItem *load = q->d_items + sl.load0, *sym = q->d_items + sl.sym0;
+    if (int rc = run(h, KID_AUX, [&] { return launch_ns_load(a, load, sl.load, h->stream); })) return rc;
+    for (int32_t t = 0; t < steps; ++t) {
+      const int from = t & 1;
+      if (int rc = run(h, KID_DEEP, [&] {
+            if (const hipError_t e = launch_ns_product(a, NS_GRAM, from, sym, sl.sym, h->stream)) return e;
+            if (const hipError_t e = launch_ns_product(a, NS_POLY, from, sym, sl.sym, h->stream)) return e;
+            return launch_ns_product(a, t + 1 < steps ? NS_STEP : NS_LAST, from, load, sl.load, h->stream);
+          }))
+        return rc;
+    }
+  }
   return PMLP_OK;
 }
 
@@ -2636,6 +3082,135 @@ int pmlp_set_params_block(pmlp_t h, const float* W1_host, const float* V1_host,
                     const_cast<float*>(W2_host), const_cast<float*>(gain_host),
                     const_cast<float*>(shift_host), false);
 }
+
+int pmlp_route(pmlp_t h, const float* scores_dev, int32_t B, int32_t K, int32_t* idx_dev,
+               float* weight_dev) {
+  if (int rc = check_choices(h, B, K)) return rc;
+  if (!scores_dev || !idx_dev || !weight_dev) return fail(PMLP_EINVAL, "null scores or output");
+  const size_t n = (size_t)B * K * 4;
+  const Span in{scores_dev, (size_t)B * h->M * 4}, i{idx_dev, n}, w{weight_dev, n};
+  if (overlap(in, i) || overlap(in, w) || overlap(i, w))
+    return fail(PMLP_EINVAL, "the buffers overlap");
+  if (int rc = use_device(h)) return rc;
+  return run(h, KID_AUX, [&] {
+    return launch_route(scores_dev, B, h->M, K, idx_dev, weight_dev, h->stream);
+  });
+}
+
+int pmlp_route_backward(pmlp_t h, const int32_t* idx_dev, const float* weight_dev,
+                        const float* dweight_dev, int32_t B, int32_t K, float* dscores_dev) {
+  if (int rc = check_choices(h, B, K)) return rc;
+  if (!idx_dev || !weight_dev || !dweight_dev || !dscores_dev)
+    return fail(PMLP_EINVAL, "null input or output");
+  const size_t n = (size_t)B * K * 4;
+  const Span out{dscores_dev, (size_t)B * h->M * 4};
+  if (overlap(out, {idx_dev, n}) || overlap(out, {weight_dev, n}) || overlap(out, {dweight_dev, n}))
+    return fail(PMLP_EINVAL, "the buffers overlap");
+  if (int rc = use_device(h)) return rc;
+  return run(h, KID_AUX, [&] {
+    return launch_route_bwd(idx_dev, weight_dev, dweight_dev, B, h->M, K, dscores_dev, h->stream);
+  });
+}
+
+int pmlp_forward_routed(pmlp_t h, const float* X_dev, int32_t B, const int32_t* idx_dev,
+                        const float* weight_dev, int32_t K, float* Y_dev) {
+  if (int rc = check_routed(h, X_dev, B, idx_dev, weight_dev, K)) return rc;
+  if (!Y_dev) return fail(PMLP_EINVAL, "null output");
+  const size_t n = (size_t)B * K * 4;
+  const Span y{Y_dev, (size_t)B * h->O * 4};
+  if (overlap(y, {idx_dev, n}) || overlap(y, {weight_dev, n}) ||
+      overlap(y, {X_dev, (size_t)B * h->F * 4}))
+    return fail(PMLP_EINVAL, "the output overlaps an input");
+  if (int rc = use_device(h)) return rc;
+  return forward_routed(h, X_dev, B, idx_dev, weight_dev, K, Y_dev);
+}
+
+int pmlp_gradients_routed(pmlp_t h, const float* X_dev, int32_t B, const int32_t* idx_dev,
+                          const float* weight_dev, int32_t K, const float* dY_dev, float* dW1_dev,
+                          float* dV1_dev, float* dW2_dev, float* dweight_dev) {
+  if (int rc = check_routed(h, X_dev, B, idx_dev, weight_dev, K)) return rc;
+  const bool gated = h->block && h->block->gated;
+  if (!dY_dev || !dW1_dev || !dW2_dev || !dweight_dev || (gated && !dV1_dev))
+    return fail(PMLP_EINVAL, "null output gradient or gradient buffer");
+  const size_t n = (size_t)B * K * 4, w1 = matrix_bytes(h, PMLP_MAT_W1);
+  const Span in[] = {{X_dev, (size_t)B * h->F * 4}, {idx_dev, n}, {weight_dev, n},
+                     {dY_dev, (size_t)B * h->O * 4}};
+  const Span out[] = {{dW1_dev, w1}, {gated ? dV1_dev : nullptr, w1},
+                      {dW2_dev, matrix_bytes(h, PMLP_MAT_W2)}, {dweight_dev, n}};
+  for (int i = 0; i < 4; ++i) {
+    for (const Span& s : in)
+      if (overlap(out[i], s)) return fail(PMLP_EINVAL, "a gradient buffer overlaps an input");
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i], out[j])) return fail(PMLP_EINVAL, "the gradient buffers overlap");
+  }
+  if (int rc = use_device(h)) return rc;
+  return gradients_routed(h, X_dev, B, idx_dev, weight_dev, K, dY_dev, dW1_dev,
+                          gated ? dV1_dev : nullptr, dW2_dev, dweight_dev);
+}
+
+int pmlp_routed_status(pmlp_t h) {
+  if (int rc = check_handle(h)) return rc;
+  if (int rc = use_device(h)) return rc;
+  PMLP_HIP(hipStreamSynchronize(h->stream));
+  int32_t bad = 0;
+  PMLP_HIP(hipMemcpy(&bad, h->flag + 3, sizeof(int32_t), hipMemcpyDeviceToHost));
+  if (!bad) return PMLP_OK;
+  PMLP_HIP(hipMemset(h->flag + 3, 0, sizeof(int32_t)));
+  return fail(PMLP_EINVAL, "a model index outside [-1, M) was seen since the last pmlp_routed_status "
+                           "call");
+}
+
+int pmlp_orthogonalize(pmlp_t h, int32_t matrix, const float* G_dev, const float* mom_in_dev,
+                       float* mom_out_dev, float mu, int32_t nesterov, int32_t steps,
+                       float* out_dev) try {
+  if (int rc = check_matrix(h, matrix, G_dev)) return rc;
+  if (!out_dev) return fail(PMLP_EINVAL, "null output");
+  if ((mom_in_dev == nullptr) != (mom_out_dev == nullptr))
+    return fail(PMLP_EINVAL, "the momentum needs both of its buffers (or neither)");
+  if (!std::isfinite(mu)) return fail(PMLP_EINVAL, "mu must be finite");
+  if (steps < 1 || steps > 32) return fail(PMLP_EINVAL, "steps must be in [1, 32]");
+  const size_t n = matrix_bytes(h, matrix);
+  const Span g{G_dev, n}, in{mom_in_dev, n}, mo{mom_out_dev, n}, out{out_dev, n};
+  if (overlap(mo, g) || overlap(mo, out) || overlap(in, out) ||
+      (overlap(g, out) && G_dev != out_dev) || (overlap(in, mo) && mom_in_dev != mom_out_dev))
+    return fail(PMLP_EINVAL, "the buffers overlap");
+  NsArgs a{};
+  a.G = G_dev;
+  a.mom_in = mom_in_dev;
+  a.mom_out = mom_out_dev;
+  a.mu = mu;
+  a.nesterov = nesterov;
+  a.out = out_dev;
+  return newton(h, matrix, a, steps);
+}
+PMLP_NO_THROW
+
+int pmlp_muon_step(pmlp_t h, int32_t matrix, const float* G_dev, float* mom_dev, float mu,
+                   int32_t nesterov, int32_t steps, float lr, const float* lr_dev,
+                   float decay) try {
+  if (int rc = check_matrix(h, matrix, G_dev)) return rc;
+  if (!std::isfinite(mu) || !std::isfinite(lr) || !std::isfinite(decay))
+    return fail(PMLP_EINVAL, "mu, lr and decay must be finite");
+  if (steps < 0 || steps > 32) return fail(PMLP_EINVAL, "steps must be in [0, 32]");
+  const size_t n = matrix_bytes(h, matrix);
+  if (overlap({G_dev, n}, {mom_dev, n})) return fail(PMLP_EINVAL, "the buffers overlap");
+  NsArgs a{};
+  a.G = G_dev;
+  a.mom_in = mom_dev;
+  a.mom_out = mom_dev;
+  a.mu = mu;
+  a.nesterov = nesterov;
+  a.W = matrix == PMLP_MAT_W1    ? h->W1
+        : matrix == PMLP_MAT_V1  ? h->block->V1
+        : matrix == PMLP_MAT_W12 ? h->deep->W12
+                                 : h->W2;
+  a.lr = lr;
+  a.lrm = lr_dev;
+  a.decay = decay;
+  if (matrix == PMLP_MAT_W1) h->w1b_valid = false;
+  return newton(h, matrix, a, steps);
+}
+PMLP_NO_THROW
 
 int pmlp_gradients_deep(pmlp_t h, const float* X_dev, const int32_t* y_dev, int32_t B,
                         float* dW1_dev, float* dW12_dev, float* dW2_dev) {

@@ -1,0 +1,653 @@
+// Products of routed packs: each model's rows of the batch with its own weights.
+
+#include "block_device.h"
+#include "routed.h"
+
+namespace pmlpk {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+namespace {
+
+// Four floats at any float's address
+struct __attribute__((packed, aligned(4))) Quad {
+  float v[4];
+};
+__device__ __forceinline__ f32x4 load_any4(const float* p) {
+  const Quad q = *(const Quad*)p;
+  return f32x4{q.v[0], q.v[1], q.v[2], q.v[3]};
+}
+
+constexpr int kKT = 32;           // columns of a stage
+constexpr int kRow = 2 * kKT;     // bytes of a row of one piece in LDS
+// Chunk c (8 columns) of a row: rows two apart share banks, so the chunks of every
+// second row change places.
+__device__ __forceinline__ int lds_chunk(int row, int c) {
+  return row * kRow + ((c ^ ((row >> 1) & 3)) << 4);
+}
+
+// acc += a b over 16 columns, the piece products smallest first
+__device__ __forceinline__ f32x16 mfma_x3_32(const bf16x8 (&a)[3], const bf16x8 (&b)[3], f32x16 acc) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[2], b[0], acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1], b[1], acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[2], acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1], b[0], acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[1], acc, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0], b[0], acc, 0, 0, 0);
+}
+
+// One 32-column stage of a workgroup's tile: RA rows of the first operand, RB of the
+// second, in three planes each.
+template <int RA, int RB>
+struct Stage {
+  static constexpr int kA = RA * kRow, kB = RB * kRow;
+  static constexpr int kBytes = 3 * (kA + kB);
+  __device__ static __forceinline__ void put(char* lds, bool second, int row, int c, const f32x4& u,
+                                             const f32x4& v) {
+    bf16x8 p[3];
+    split3(u, v, p[0], p[1], p[2]);
+    char* at = lds + (second ? 3 * kA : 0) + lds_chunk(row, c);
+#pragma unroll
+    for (int e = 0; e < 3; ++e) *(bf16x8*)(at + e * (second ? kB : kA)) = p[e];
+  }
+  // row a0 + 32 i + lane % 32 of the first operand, b0 + .. of the second
+  template <int NA, int NB>
+  __device__ static __forceinline__ void multiply(const char* lds, int a0, int b0, int lane,
+                                                  f32x16 (&acc)[NA][NB]) {
+#pragma unroll
+    for (int ks = 0; ks < kKT / 16; ++ks) {
+      const int c = 2 * ks + (lane >> 5), r = lane & 31;
+      bf16x8 a[NA][3], b[NB][3];
+#pragma unroll
+      for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          a[i][e] = *(const bf16x8*)(lds + e * kA + lds_chunk(a0 + 32 * i + r, c));
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          b[j][e] = *(const bf16x8*)(lds + 3 * kA + e * kB + lds_chunk(b0 + 32 * j + r, c));
+#pragma unroll
+      for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = mfma_x3_32(a[i], b[j], acc[i][j]);
+    }
+  }
+};
+
+// The unit (of the chunk) and the projection that row `r` of the first operand is: a
+// gated chunk interleaves 32 rows of W1 and 32 of V1, so that a wave has both of a unit.
+template <bool GATED>
+__device__ __forceinline__ int operand_unit(int r) {
+  return GATED ? ((r >> 6) << 5) + (r & 31) : r;
+}
+template <bool GATED>
+__device__ __forceinline__ bool operand_gate(int r) {
+  return GATED && (r & 32);
+}
+
+// Workgroups go to the eight dies in turn; each die takes a run of the items, so that
+// its cache holds the rows and weights that its workgroups share.
+__device__ __forceinline__ int die_order(int i, int n) {
+  const int each = (n + 7) / 8;
+  return (i & 7) * each + (i >> 3);
+}
+
+}  // namespace
+
+// Z (and U) of a chunk of units and a block of rows of one model, then the activation and
+// either the sums over the units with W2 (forward) or the hidden gradients (TRAIN).
+// Units are the first operand's rows and samples the second's: a lane has one sample and
+// 16 units of every tile.
+template <int NA, int NB, bool GATED, bool TRAIN>
+__global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
+  constexpr int RA = 64 * NA, RB = 64 * NB, UC = GATED ? 64 : RA, NU = GATED ? 1 : NA;
+  typedef Stage<RA, RB> St;
+  __shared__ __align__(16) char lds[St::kBytes];
+  __shared__ __align__(16) float w2s[kRtMaxO * UC];  // [O][UC]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wu = wave & 1, wr = wave >> 1;
+  const int n = *a.nitems, each = (n + 7) / 8;
+  for (int it = blockIdx.x; it < 8 * each; it += gridDim.x) {
+    const int at = die_order(it, n);
+    if (at >= n) continue;
+    const RtItem item = a.items[at];
+    const int m = item.m;
+    const int64_t n0 = a.seg_off[m] + (int64_t)item.b * UC;
+    const int left = (int)(a.seg_off[m + 1] - n0);  // units from here on
+    const int units = left < UC ? left : UC;
+    const int rows = a.count[m];
+    const int places = a.place[m + 1] - a.place[m];  // with the padding
+    const int p0 = item.a * RB;
+    const int32_t* slots = a.slot + a.place[m];
+
+    const float* ra[NA];
+    const float* rb[NB];
+    bool live[NB];
+#pragma unroll
+    for (int q = 0; q < NA; ++q) {
+      const int r = 64 * q + (tid >> 2);
+      int u = operand_unit<GATED>(r);
+      u = u < units ? u : units - 1;  // (a row that is there; its results are dropped)
+      ra[q] = (operand_gate<GATED>(r) ? a.V1 : a.W1) + (n0 + u) * a.F4;
+    }
+#pragma unroll
+    for (int q = 0; q < NB; ++q) {
+      const int p = p0 + 64 * q + (tid >> 2);
+      const int s = p < rows ? slots[p] : -1;
+      live[q] = s >= 0;
+      rb[q] = a.X + (int64_t)(live[q] ? s / a.K : 0) * a.F;
+    }
+    const int c = tid & 3;
+    f32x4 va[NA][2], vb[NB][2];
+    auto load = [&](int k0) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int k = k0 + 8 * c + 4 * e;
+#pragma unroll
+        for (int q = 0; q < NA; ++q)
+          va[q][e] = k < a.F4 ? *(const f32x4*)(ra[q] + k) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < NB; ++q) {
+          f32x4 v{0.f, 0.f, 0.f, 0.f};
+          if (live[q]) {
+            if (k + 4 <= a.F) v = load_any4(rb[q] + k);
+            else
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (k + j < a.F) v[j] = rb[q][k + j];
+          }
+          vb[q][e] = v;
+        }
+      }
+    };
+    f32x16 acc[NA][NB];
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    __syncthreads();  // the item before has read its LDS
+    for (int i = tid; i < a.O * UC; i += 256) {
+      const int o = i / UC, u = i % UC;
+      w2s[i] = u < units ? a.W2[(int64_t)o * a.ldw + n0 + u] : 0.f;
+    }
+    load(0);
+    for (int k0 = 0; k0 < a.F; k0 += kKT) {
+#pragma unroll
+      for (int q = 0; q < NA; ++q) St::put(lds, false, 64 * q + (tid >> 2), c, va[q][0], va[q][1]);
+#pragma unroll
+      for (int q = 0; q < NB; ++q) St::put(lds, true, 64 * q + (tid >> 2), c, vb[q][0], vb[q][1]);
+      if (k0 + kKT < a.F) load(k0 + kKT);
+      lds_barrier();
+      St::template multiply<NA, NB>(lds, wu * 32 * NA, wr * 32 * NB, lane, acc);
+      lds_barrier();
+    }
+
+    const int act = a.act[m];
+    const int half = 4 * (lane >> 5);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int p = p0 + (wr * NB + j) * 32 + (lane & 31);
+      const int s = p < rows ? slots[p] : -1;
+      const float* dy = nullptr;
+      float w = 0.f;
+      if (TRAIN && s >= 0) {
+        dy = a.dY + (int64_t)(s / a.K) * a.O;
+        w = a.weight[s];
+      }
+      float dw = 0.f;
+      float hid[NU][16];
+#pragma unroll
+      for (int i = 0; i < NU; ++i) {
+        const int u0 = (wu * NU + i) * 32;  // units u0 + 8 (e / 4) + half + e % 4
+        float z[16], v[16], d[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[e] = acc[i][j][e];
+        if (!TRAIN) {
+          blk_acts<16>(act, z, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[e] = blk_act_slope(act, z[e], &d[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const bool there = u0 + 8 * (e >> 2) + half + (e & 3) < units;
+          hid[i][e] = there ? (GATED ? v[e] * acc[NA - 1][j][e] : v[e]) : 0.f;
+        }
+        if (!TRAIN) continue;
+        float g[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) g[e] = 0.f;
+        for (int o = 0; o < a.O; ++o) {
+          const float y = s >= 0 ? dy[o] : 0.f;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x4 w2 = *(const f32x4*)(w2s + o * UC + u0 + 8 * q + half);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) g[4 * q + e] = fmaf(y, w2[e], g[4 * q + e]);
+          }
+        }
+        const int64_t z0 = a.zoff[m] + (int64_t)item.b * UC * places;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int u = u0 + 8 * (e >> 2) + half + (e & 3);
+          dw = fmaf(hid[i][e], g[e], dw);
+          if (u >= units || p >= places) continue;
+          const float dh = w * g[e];
+          const int64_t to = z0 + (int64_t)u * places + p;
+          a.H[to] = s >= 0 ? hid[i][e] : 0.f;
+          a.dZ[to] = s >= 0 ? dh * d[e] * (GATED ? acc[NA - 1][j][e] : 1.f) : 0.f;
+          if (GATED) a.dU[to] = s >= 0 ? dh * v[e] : 0.f;
+        }
+      }
+      const int part = 2 * item.b + wu;
+      if (TRAIN) {
+        dw += __shfl_xor(dw, 32);
+        if (s >= 0 && lane < 32) a.dwpart[(int64_t)s * a.parts + part] = dw;
+        continue;
+      }
+      for (int o = 0; o < a.O; ++o) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < NU; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x4 w2 = *(const f32x4*)(w2s + o * UC + (wu * NU + i) * 32 + 8 * q + half);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = fmaf(hid[i][4 * q + e], w2[e], sum);
+          }
+        sum += __shfl_xor(sum, 32);
+        if (s >= 0 && lane < 32) a.part[((int64_t)s * a.parts + part) * a.O + o] = sum;
+      }
+    }
+  }
+}
+
+namespace {
+
+// Workgroups for at most `most` items, whose number only the device knows: a multiple of
+// eight (die_order), and no more than some rounds of what the device holds at once.
+unsigned groups_for(int64_t most) {
+  const int64_t g = (most + 7) / 8 * 8;
+  return (unsigned)(g < 8 ? 8 : g > 8192 ? 8192 : g);
+}
+
+template <bool TRAIN>
+hipError_t tile(const RtArgs& a, const RtShape& sh, hipStream_t s) {
+#define PMLP_RT_TILE(NA, NB, G)                                                                   \
+  k_rt_tile<NA, NB, G, TRAIN><<<groups_for(a.most), 256, 0, s>>>(a)
+  if (a.V1) {
+    if (sh.nb == 2) PMLP_RT_TILE(2, 2, true);
+    else PMLP_RT_TILE(2, 1, true);
+  } else if (sh.na == 2) {
+    if (sh.nb == 2) PMLP_RT_TILE(2, 2, false);
+    else PMLP_RT_TILE(2, 1, false);
+  } else {
+    if (sh.nb == 2) PMLP_RT_TILE(1, 2, false);
+    else PMLP_RT_TILE(1, 1, false);
+  }
+#undef PMLP_RT_TILE
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rt_tile(const RtArgs& a, const RtShape& sh, bool train, hipStream_t s) {
+  note_variant("k_rt_tile", kArithX3);
+  return train ? tile<true>(a, sh, s) : tile<false>(a, sh, s);
+}
+
+// ---------------------------------------------------------------------------
+// Few slots: a workgroup takes 64 units of a slot's model, each wave 16 of them, four at
+// a time, 16 lanes along the columns of each.  Bound by the weights' read.
+// ---------------------------------------------------------------------------
+
+template <bool GATED>
+__global__ __launch_bounds__(256) void k_rt_few(RtArgs a, RtFew f) {
+  const int s = blockIdx.x / f.chunks, chunk = blockIdx.x % f.chunks;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int m = f.idx[s];
+  if (m < 0 || m >= a.M) {
+    if (m != -1 && tid == 0 && chunk == 0) f.flag[3] = 1;
+    return;
+  }
+  const int64_t first = a.seg_off[m], end = a.seg_off[m + 1];
+  const int64_t n0 = first + (int64_t)chunk * kRtFewUnits + 16 * wave;
+  if (first + (int64_t)chunk * kRtFewUnits >= end) return;
+  const float* x = a.X + (int64_t)(s / a.K) * a.F;
+  const int li = lane & 15, lu = lane >> 4;
+  float z[4] = {}, u[4] = {};  // unit n0 + 4 i + lu
+  const float *w[4], *v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t n = n0 + 4 * i + lu < end ? n0 + 4 * i + lu : end - 1;
+    w[i] = a.W1 + n * a.F4;
+    v[i] = GATED ? a.V1 + n * a.F4 : nullptr;
+  }
+  for (int k = 4 * li; k < a.F4; k += 64) {
+    f32x4 xv{0.f, 0.f, 0.f, 0.f};
+    if (k + 4 <= a.F) xv = load_any4(x + k);
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (k + j < a.F) xv[j] = x[k + j];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 wv = *(const f32x4*)(w[i] + k);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) z[i] = fmaf(wv[j], xv[j], z[i]);
+      if (GATED) {
+        const f32x4 vv = *(const f32x4*)(v[i] + k);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[i] = fmaf(vv[j], xv[j], u[i]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {  // sums end in lane 15 of each 16
+    z[i] = group_sum_to_last(z[i], 16);
+    if (GATED) u[i] = group_sum_to_last(u[i], 16);
+    z[i] = __shfl(z[i], lane | 15);
+    if (GATED) u[i] = __shfl(u[i], lane | 15);
+  }
+  float h[4];
+  blk_acts<4>(a.act[m], z, h);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (GATED) h[i] *= u[i];
+    if (n0 + 4 * i + lu >= end) h[i] = 0.f;
+  }
+  __shared__ float sums[4][kRtMaxO];
+  for (int o = 0; o < a.O; ++o) {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t n = n0 + 4 * i + lu;
+      if (n < end) t = fmaf(h[i], a.W2[(int64_t)o * a.ldw + n], t);
+    }
+    t += __shfl_xor(t, 16);
+    t += __shfl_xor(t, 32);
+    if (lane == 0) sums[wave][o] = t;
+  }
+  __syncthreads();
+  if (tid < a.O)
+    a.part[((int64_t)s * a.parts + chunk) * a.O + tid] =
+        (sums[0][tid] + sums[1][tid]) + (sums[2][tid] + sums[3][tid]);
+}
+
+hipError_t launch_rt_few(const RtArgs& a, const RtFew& f, hipStream_t s) {
+  note_variant("k_rt_few", kArithNone);
+  const unsigned grid = (unsigned)(f.R * f.chunks);
+  if (a.V1) k_rt_few<true><<<grid, 256, 0, s>>>(a, f);
+  else k_rt_few<false><<<grid, 256, 0, s>>>(a, f);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// Sums over a model's parts, in order.
+// ---------------------------------------------------------------------------
+
+namespace {
+__device__ __forceinline__ float slot_sum(const RtJoin& a, int64_t s, int m, int o) {
+  const int n = (int)((a.seg_off[m + 1] - a.seg_off[m] + a.uc - 1) / a.uc);
+  const float* at = a.part + s * a.parts * a.O + o;
+  float sum = 0.f;
+  for (int q = 0; q < n; ++q) sum += at[(int64_t)q * a.O];
+  return sum;
+}
+}  // namespace
+
+__global__ __launch_bounds__(256) void k_rt_join(RtJoin a) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (int64_t)a.B * a.O) return;
+  const int64_t b = i / a.O;
+  const int o = (int)(i - b * a.O);
+  float y = 0.f;
+  for (int k = 0; k < a.K; ++k) {
+    const int m = a.idx[b * a.K + k];
+    if (m < 0 || m >= a.M) continue;
+    y = fmaf(a.weight[b * a.K + k], slot_sum(a, b * a.K + k, m, o), y);
+  }
+  a.Y[i] = y;
+}
+
+__global__ __launch_bounds__(256) void k_rt_join_dw(RtJoin a) {
+  const int64_t s = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (s >= (int64_t)a.B * a.K) return;
+  const int m = a.idx[s];
+  a.Y[s] = m < 0 || m >= a.M ? 0.f : slot_sum(a, s, m, 0);
+}
+
+hipError_t launch_rt_join(const RtJoin& a, hipStream_t s) {
+  note_variant("k_rt_join", kArithNone);
+  k_rt_join<<<(unsigned)ceil_div_i((int64_t)a.B * a.O, 256), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_rt_join_dw(const RtJoin& a, hipStream_t s) {
+  note_variant("k_rt_join_dw", kArithNone);
+  k_rt_join_dw<<<(unsigned)ceil_div_i((int64_t)a.B * a.K, 256), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// Weight gradients: dW1_m = dZ_m X_m (and dV1_m = dU_m X_m) over the places of model m,
+// units the first operand's rows and columns of X the second's.
+// ---------------------------------------------------------------------------
+
+template <int NA, int NB, bool GATED>
+__global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
+  constexpr int RA = 64 * NA, RB = 64 * NB, UC = GATED ? 64 : RA;
+  typedef Stage<RA, RB> St;
+  __shared__ __align__(16) char lds[St::kBytes];
+  const RtArgs& a = g.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wu = wave & 1, wf = wave >> 1;
+  const int n = *g.njitems, each = (n + 7) / 8;
+  for (int it = blockIdx.x; it < 8 * each; it += gridDim.x) {
+    const int at = die_order(it, n);
+    if (at >= n) continue;
+    const RtItem item = g.jitems[at];
+    const int m = item.m;
+    const int64_t first = a.seg_off[m];
+    const int h = (int)(a.seg_off[m + 1] - first);
+    const int u0 = item.a * UC, f0 = item.b * RB;
+    const int units = h - u0 < UC ? h - u0 : UC;
+    const int places = a.place[m + 1] - a.place[m];
+    const int b0 = item.c * g.t.part, b1 = b0 + g.t.part < places ? b0 + g.t.part : places;
+    const bool split = places > g.t.part;
+    const int32_t* slots = a.slot + a.place[m];
+    const int c = tid & 3;
+    const float* ra[NA];
+#pragma unroll
+    for (int q = 0; q < NA; ++q) {
+      const int r = 64 * q + (tid >> 2);
+      int u = operand_unit<GATED>(r);
+      u = u < units ? u : units - 1;
+      ra[q] = (operand_gate<GATED>(r) ? a.dU : a.dZ) + a.zoff[m] + (int64_t)(u0 + u) * places;
+    }
+    // column f of X for eight places from 8 oct on: 256 / RB octets at a time
+    constexpr int PER = 256 / RB, NQ = 4 / PER;
+    const int f = f0 + tid % RB;
+    f32x4 va[NA][2], vb[NQ][2];
+    auto load = [&](int k0) {
+#pragma unroll
+      for (int q = 0; q < NA; ++q)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) va[q][e] = *(const f32x4*)(ra[q] + k0 + 8 * c + 4 * e);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int s = slots[k0 + 8 * (q * PER + tid / RB) + e];
+          vb[q][e >> 2][e & 3] = s >= 0 && f < a.F ? a.X[(int64_t)(s / a.K) * a.F + f] : 0.f;
+        }
+    };
+    f32x16 acc[NA][NB];
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    __syncthreads();
+    if (b0 < b1) load(b0);
+    for (int k0 = b0; k0 < b1; k0 += kKT) {
+#pragma unroll
+      for (int q = 0; q < NA; ++q) St::put(lds, false, 64 * q + (tid >> 2), c, va[q][0], va[q][1]);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+        St::put(lds, true, tid % RB, q * PER + tid / RB, vb[q][0], vb[q][1]);
+      if (k0 + kKT < b1) load(k0 + kKT);
+      lds_barrier();
+      St::template multiply<NA, NB>(lds, wu * 32 * NA, wf * 32 * NB, lane, acc);
+      lds_barrier();
+    }
+    const int half = 4 * (lane >> 5);
+    const int64_t size = g.N * a.F;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int col = f0 + (wf * NB + j) * 32 + (lane & 31);
+      if (col >= a.F) continue;
+      const bool seen = !g.fmask || (g.fmask[(int64_t)m * g.fmw + (col >> 5)] >> (col & 31) & 1u);
+#pragma unroll
+      for (int i = 0; i < NA; ++i) {
+        float* out = GATED && i ? g.dV1 : g.dW1;
+        if (split) out = g.wpart + ((int64_t)item.c * (GATED ? 2 : 1) + (GATED ? i : 0)) * size;
+        const int base = GATED ? wu * 32 : (wu * NA + i) * 32;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int u = base + 8 * (e >> 2) + half + (e & 3);
+          if (u < units) out[(first + u0 + u) * a.F + col] = seen ? acc[i][j][e] : 0.f;
+        }
+      }
+    }
+  }
+}
+
+// wdy[o][place] = weight dY_o of the place's slot, 0 where it holds none.
+__global__ __launch_bounds__(256) void k_rt_wdy(RtGrad g) {
+  const RtArgs& a = g.a;
+  const int total = a.place[a.M];
+  const int p = blockIdx.x * 256 + threadIdx.x;
+  if (p >= total) return;
+  const int s = a.slot[p];
+  const float w = s >= 0 ? a.weight[s] : 0.f;
+  for (int o = 0; o < a.O; ++o)
+    g.wdy[(int64_t)o * a.P + p] = s >= 0 ? w * a.dY[(int64_t)(s / a.K) * a.O + o] : 0.f;
+}
+
+// dW2[o][unit] = sum over the places of wdy[o] H[unit]: a wave takes four units and a part
+// of their model's places.
+constexpr int kDw2Units = 4;
+template <int OM>
+__global__ __launch_bounds__(256) void k_rt_dw2(RtGrad g) {
+  const RtArgs& a = g.a;
+  const int lane = threadIdx.x & 63;
+  const int64_t q = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t groups = (g.N + kDw2Units - 1) / kDw2Units;
+  if (q >= groups * g.nparts) return;
+  const int part = (int)(q / groups);
+  const int64_t n0 = q % groups * kDw2Units;
+#pragma unroll 1
+  for (int64_t n = n0; n < n0 + kDw2Units && n < g.N;) {
+    const int m = g.mid[n];
+    const int64_t end = a.seg_off[m + 1];
+    const int places = a.place[m + 1] - a.place[m];
+    const int b0 = part * g.t.part, b1 = b0 + g.t.part < places ? b0 + g.t.part : places;
+    int64_t last = n0 + kDw2Units;  // units n .. last - 1 are of model m
+    last = last < end ? last : end;
+    const int cnt = (int)(last - n);
+    if (part > 0 && b0 >= places) {
+      n = last;
+      continue;
+    }
+    const float* hrow[kDw2Units];
+#pragma unroll
+    for (int i = 0; i < kDw2Units; ++i) {
+      const int64_t u = n - a.seg_off[m] + (i < cnt ? i : cnt - 1);
+      hrow[i] = a.H + a.zoff[m] + u * places;
+    }
+    float sum[kDw2Units][OM];
+#pragma unroll
+    for (int i = 0; i < kDw2Units; ++i)
+#pragma unroll
+      for (int o = 0; o < OM; ++o) sum[i][o] = 0.f;
+    const float* wd = g.wdy + a.place[m];
+    for (int p = b0 + lane; p < b1; p += 64) {
+      float hv[kDw2Units];
+#pragma unroll
+      for (int i = 0; i < kDw2Units; ++i) hv[i] = hrow[i][p];
+#pragma unroll
+      for (int o = 0; o < OM; ++o) {
+        const float y = o < a.O ? wd[(int64_t)o * a.P + p] : 0.f;
+#pragma unroll
+        for (int i = 0; i < kDw2Units; ++i) sum[i][o] = fmaf(hv[i], y, sum[i][o]);
+      }
+    }
+    float* out = places > g.t.part ? g.w2part + (int64_t)part * a.O * g.N : g.dW2;
+#pragma unroll
+    for (int i = 0; i < kDw2Units; ++i)
+#pragma unroll
+      for (int o = 0; o < OM; ++o) {
+        const float t = group_sum_to_last(sum[i][o], 64);
+        if (lane == 63 && i < cnt && o < a.O) out[(int64_t)o * g.N + n + i] = t;
+      }
+    n = last;
+  }
+}
+
+// The sums of the parts of models that have several, in order.
+__global__ __launch_bounds__(256) void k_rt_sum_parts(RtGrad g) {
+  const RtArgs& a = g.a;
+  const int64_t n = blockIdx.x;
+  const int m = g.mid[n];
+  const int places = a.place[m + 1] - a.place[m];
+  if (places <= g.t.part) return;
+  const int parts = (places + g.t.part - 1) / g.t.part;
+  const int k = a.V1 ? 2 : 1;
+  const int64_t size = g.N * a.F;
+  for (int f = threadIdx.x; f < k * a.F; f += 256) {
+    const int v = f >= a.F;
+    const int64_t at = n * a.F + f - (v ? a.F : 0);
+    float t = 0.f;
+    for (int q = 0; q < parts; ++q) t += g.wpart[((int64_t)q * k + v) * size + at];
+    (v ? g.dV1 : g.dW1)[at] = t;
+  }
+  if (threadIdx.x < (unsigned)a.O) {
+    const int64_t at = threadIdx.x * g.N + n;
+    float t = 0.f;
+    for (int q = 0; q < parts; ++q) t += g.w2part[(int64_t)q * a.O * g.N + at];
+    g.dW2[at] = t;
+  }
+}
+
+hipError_t launch_rt_weights(const RtGrad& g, const RtShape& sh, hipStream_t s) {
+  note_variant("k_rt_dw", kArithX3);
+#define PMLP_RT_DW(NA, NB, G) \
+  k_rt_dw<NA, NB, G><<<groups_for(g.jmost), 256, 0, s>>>(g)
+  if (g.a.V1) {
+    if (sh.nb == 2) PMLP_RT_DW(2, 2, true);
+    else PMLP_RT_DW(2, 1, true);
+  } else if (sh.na == 2) {
+    if (sh.nb == 2) PMLP_RT_DW(2, 2, false);
+    else PMLP_RT_DW(2, 1, false);
+  } else {
+    if (sh.nb == 2) PMLP_RT_DW(1, 2, false);
+    else PMLP_RT_DW(1, 1, false);
+  }
+#undef PMLP_RT_DW
+  if (const hipError_t e = hipGetLastError()) return e;
+  k_rt_wdy<<<(unsigned)ceil_div_i(g.a.P, 256), 256, 0, s>>>(g);
+  const int64_t waves = (g.N + kDw2Units - 1) / kDw2Units * g.nparts;
+  const unsigned grid = (unsigned)((waves + 3) / 4);
+  if (g.a.O <= 2) k_rt_dw2<2><<<grid, 256, 0, s>>>(g);
+  else if (g.a.O <= 4) k_rt_dw2<4><<<grid, 256, 0, s>>>(g);
+  else k_rt_dw2<16><<<grid, 256, 0, s>>>(g);
+  if (g.nparts > 1) k_rt_sum_parts<<<(unsigned)g.N, 256, 0, s>>>(g);
+  return hipGetLastError();
+}
+
+}  // namespace pmlpk

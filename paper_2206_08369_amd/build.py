@@ -24,7 +24,7 @@ SOURCES += [(src, ["-DPMLP_BLK_OM=%d" % om]) for om in (16, 4, 2)
             for src in ("k_block_bwd.hip", "k_block_local.hip")]
 SOURCES += [(s, []) for s in ("k_gemm_bf16.hip", "k_m3.hip", "k_misc.hip", "k_gemm.hip", "k_deep.hip",
                               "k_block.hip", "k_block_gemm.hip", "k_route.hip", "k_routed.hip",
-                              "k_newton.hip", "api.hip")]
+                              "k_newton.hip", "k_newton_small.hip", "api.hip")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

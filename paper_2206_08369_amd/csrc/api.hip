@@ -123,9 +123,13 @@ struct PmlpNewton {
   NsMat* d_mats = nullptr;
   NsPiece* d_pieces = nullptr;
   NsItem* d_items = nullptr;
-  int32_t npieces = 0;
+  int32_t npieces = 0, nlarge = 0;  // pieces, and those of matrices that go in slices (first)
   std::vector<NewtonSlice> slices;
   int64_t nx = 0, na = 0;  // of the largest slice
+  int32_t tile = 128;      // (NsArgs)
+  int32_t* d_list = nullptr;  // matrices by class (ns_small_class), the dearest first
+  int32_t first[kNsClasses + 1] = {};
+  size_t lds[kNsClasses] = {};
 };
 constexpr int kMatrices = 4;  // PMLP_MAT_*
 
@@ -311,6 +315,7 @@ void release(pmlp* h) {
     dfree(q->d_mats);
     dfree(q->d_pieces);
     dfree(q->d_items);
+    dfree(q->d_list);
     delete q;
     q = nullptr;
   }
@@ -2156,6 +2161,7 @@ int ensure_newton(pmlp* h, int32_t mat) {
       dfree(q->d_mats);
       dfree(q->d_pieces);
       dfree(q->d_items);
+      dfree(q->d_list);
       delete q;
     }
   } made{new PmlpNewton()};
@@ -2176,6 +2182,17 @@ int ensure_newton(pmlp* h, int32_t mat) {
     sym.clear();
     sl = NewtonSlice{};
   };
+  auto cut = [&](int32_t m) {
+    NsMat& t = mats[m];
+    t.piece0 = (int32_t)pieces.size();
+    const int32_t rows = std::max(1, kNsPiece / t.cols);
+    for (int32_t r = 0; r < t.rows; r += rows)
+      pieces.push_back(NsPiece{m, r, std::min(rows, t.rows - r), 0});
+    t.pieces = (int32_t)pieces.size() - t.piece0;
+  };
+  std::vector<int32_t> by_class[kNsClasses], large;
+  int32_t nsmall = 0;
+  int64_t tiles = 0;  // of 128, of a product of the large ones
   for (int32_t m = 0; m < h->M; ++m) {
     NsMat& t = mats[m];
     t = NsMat{};
@@ -2204,34 +2221,63 @@ int ensure_newton(pmlp* h, int32_t mat) {
     if (t.c > (1 << 30)) return fail(PMLP_EINVAL, "a matrix is too large to be orthogonalised");
     t.rp = (t.r + 31) / 32 * 32;
     t.cp = (t.c + 31) / 32 * 32;
+    if (const int cls = ns_small_class(t.r, t.c); cls >= 0) {
+      by_class[cls].push_back(m);
+      ++nsmall;
+      continue;
+    }
+    large.push_back(m);
+    tiles += (int64_t)div_up(t.rp, 128) * div_up(t.cp, 128);
+  }
+  if (tiles < 1024) q->tile = 64;
+  for (int32_t m : large) {
+    NsMat& t = mats[m];
     const int64_t nx = (int64_t)t.rp * t.cp, na = (int64_t)t.rp * t.rp;
     if (sl.nx && newton_bytes(sl.nx + nx, sl.na + na) > kNewtonSlice) close();
     t.xo = sl.nx;
     t.ao = sl.na;
     sl.nx += nx;
     sl.na += na;
-    const int32_t ti = div_up(t.rp, kNsTile), tj = div_up(t.cp, kNsTile);
+    const int32_t ti = div_up(t.rp, q->tile), tj = div_up(t.cp, q->tile);
     for (int32_t i = 0; i < ti; ++i) {
       for (int32_t j = 0; j < tj; ++j) load.push_back(NsItem{m, i, j, 0});
       for (int32_t j = 0; j <= i; ++j) sym.push_back(NsItem{m, i, j, 0});
     }
-    t.piece0 = (int32_t)pieces.size();
-    const int32_t rows = std::max(1, kNsPiece / t.cols);
-    for (int32_t r = 0; r < t.rows; r += rows)
-      pieces.push_back(NsPiece{m, r, std::min(rows, t.rows - r), 0});
-    t.pieces = (int32_t)pieces.size() - t.piece0;
+    cut(m);
   }
-  close();
+  if (sl.nx) close();
+  q->nlarge = (int32_t)pieces.size();
+  std::vector<int32_t> list;
+  for (int k = 0; nsmall <= kNsOneLaunch && k + 1 < kNsClasses; ++k) {
+    by_class[kNsClasses - 1].insert(by_class[kNsClasses - 1].end(), by_class[k].begin(), by_class[k].end());
+    by_class[k].clear();
+  }
+  for (int k = 0; k < kNsClasses; ++k) {
+    std::vector<int32_t>& v = by_class[k];
+    for (int32_t m : v)
+      q->lds[k] = std::max(q->lds[k], ns_small_lds(mats[m].r, mats[m].c, k < 8 ? kNsWaves[k] : 8));
+    std::stable_sort(v.begin(), v.end(), [&](int32_t x, int32_t y) {
+      return (int64_t)mats[x].r * mats[x].cp > (int64_t)mats[y].r * mats[y].cp;
+    });
+    q->first[k] = (int32_t)list.size();
+    list.insert(list.end(), v.begin(), v.end());
+    for (int32_t m : v) cut(m);
+  }
+  q->first[kNsClasses] = (int32_t)list.size();
   q->npieces = (int32_t)pieces.size();
   if (hipMalloc(&q->d_mats, mats.size() * sizeof(NsMat)) != hipSuccess ||
       hipMalloc(&q->d_pieces, pieces.size() * sizeof(NsPiece)) != hipSuccess ||
-      hipMalloc(&q->d_items, items.size() * sizeof(NsItem)) != hipSuccess) {
+      (!items.empty() && hipMalloc(&q->d_items, items.size() * sizeof(NsItem)) != hipSuccess) ||
+      (!list.empty() && hipMalloc(&q->d_list, list.size() * sizeof(int32_t)) != hipSuccess)) {
     (void)hipGetLastError();
     return fail(PMLP_ENOMEM, "device allocation failed for the update's plan");
   }
   PMLP_HIP(hipMemcpy(q->d_mats, mats.data(), mats.size() * sizeof(NsMat), hipMemcpyHostToDevice));
   PMLP_HIP(hipMemcpy(q->d_pieces, pieces.data(), pieces.size() * sizeof(NsPiece), hipMemcpyHostToDevice));
-  PMLP_HIP(hipMemcpy(q->d_items, items.data(), items.size() * sizeof(NsItem), hipMemcpyHostToDevice));
+  if (!items.empty())
+    PMLP_HIP(hipMemcpy(q->d_items, items.data(), items.size() * sizeof(NsItem), hipMemcpyHostToDevice));
+  if (!list.empty())
+    PMLP_HIP(hipMemcpy(q->d_list, list.data(), list.size() * sizeof(int32_t), hipMemcpyHostToDevice));
   h->newton[mat] = q;
   made.q = nullptr;
   return PMLP_OK;
@@ -2270,9 +2316,16 @@ int newton(pmlp* h, int32_t mat, NsArgs a, int32_t steps) {
   }
   if (steps == 0)
     return run(h, KID_AUX, [&] { return launch_ns_momentum(a, 0, q->npieces, true, h->stream); });
+  for (int k = 0; k < kNsClasses; ++k)
+    if (const int32_t n = q->first[k + 1] - q->first[k])
+      if (int rc = run(h, KID_DEEP, [&] {
+            return launch_ns_small(a, k, q->lds[k], q->d_list + q->first[k], n, steps, h->stream);
+          }))
+        return rc;
+  if (!q->nlarge) return PMLP_OK;
   Carver c;
   auto halves = [&](int64_t n) { return c.take((size_t)(n + 1) / 2); };
-  const size_t oS = c.take(2 * (size_t)q->npieces);
+  const size_t oS = c.take(2 * (size_t)q->nlarge);
   const size_t oX0 = halves(2 * q->nx), oX1 = halves(2 * q->nx), oT0 = halves(2 * q->nx),
                oT1 = halves(2 * q->nx), oA = halves(2 * q->na), oP = halves(2 * q->na);
   if (int rc = ensure_ws(h, &h->extra, c.bytes, "an orthogonalised update")) return rc;
@@ -2286,7 +2339,8 @@ int newton(pmlp* h, int32_t mat, NsArgs a, int32_t steps) {
   a.P = (_Float16*)(ws + oP);
   a.nx = q->nx;
   a.na = q->na;
-  if (int rc = run(h, KID_AUX, [&] { return launch_ns_momentum(a, 0, q->npieces, false, h->stream); }))
+  a.tile = q->tile;
+  if (int rc = run(h, KID_AUX, [&] { return launch_ns_momentum(a, 0, q->nlarge, false, h->stream); }))
     return rc;
   for (const NewtonSlice& sl : q->slices) {
     const NsItem *load = q->d_items + sl.load0, *sym = q->d_items + sl.sym0;

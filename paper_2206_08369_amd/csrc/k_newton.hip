@@ -9,51 +9,9 @@
 // 2^-22 of each product, as fp32 sums of that length do.  (Six bf16 products would hold
 // values of any size; these are normalised.)
 
-#include "device_common.h"
-#include "newton.h"
+#include "newton_device.h"
 
 namespace pmlpk {
-
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-
-namespace {
-
-constexpr float kScale = 8192.f, kUnscale = 1.f / (8192.f * 8192.f);
-
-__device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
-  const float t = v * kScale;
-  hi = (_Float16)t;
-  lo = (_Float16)(t - (float)hi);
-}
-__device__ __forceinline__ float join(_Float16 hi, _Float16 lo) {
-  return ((float)hi + (float)lo) * (1.f / kScale);
-}
-
-__device__ __forceinline__ float direction(const NsArgs& a, int64_t at) {
-  const float g = a.G[at];
-  if (!a.mom_in) return g;
-  const float m = a.mom_out[at];
-  return a.nesterov ? fmaf(a.mu, m, g) : m;
-}
-
-// W <- W - lr (decay W + u) of model m's entry in column j (column masks: W1 only)
-__device__ __forceinline__ void apply(const NsArgs& a, const NsMat& t, int i, int j, float u) {
-  const float lr = a.lrm ? a.lrm[t.m] : a.lr;
-  const bool seen = !a.fmask || (a.fmask[(int64_t)t.m * a.fmw + (j >> 5)] >> (j & 31) & 1u);
-  float* w = a.W + t.wsrc + (int64_t)i * t.wld + j;
-  const float old = *w;
-  *w = seen ? old - lr * fmaf(a.decay, old, u) : 0.f;
-}
-
-__device__ __forceinline__ double wave_total(double v) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-  return v;
-}
-
-}  // namespace
 
 template <bool APPLY>
 __global__ __launch_bounds__(256) void k_ns_momentum(NsArgs a, int piece0) {
@@ -100,14 +58,13 @@ __global__ __launch_bounds__(256) void k_ns_load(NsArgs a, const NsItem* items) 
   const NsMat t = a.mats[it.mat];
   double total = 0;
   for (int q = 0; q < t.pieces; ++q) total += a.sums[t.piece0 + q];
-  // (a zero matrix stays zero; one that is not finite becomes NaN)
-  const double scale = !(total < INFINITY) ? (double)NAN : total > 0 ? 1 / sqrt(total) : 0;
+  const double scale = ns_scale(total) * kScale;
   const bool turned = t.rows > t.cols;
   const int x = threadIdx.x & 31, y0 = threadIdx.x >> 5;
   _Float16 *X = a.X[0] + t.xo, *XT = a.XT[0] + t.xo;
-  const int i1 = min(t.rp, (it.i + 1) * kNsTile), j1 = min(t.cp, (it.j + 1) * kNsTile);
-  for (int i0 = it.i * kNsTile; i0 < i1; i0 += 32)
-    for (int j0 = it.j * kNsTile; j0 < j1; j0 += 32) {
+  const int i1 = min(t.rp, (it.i + 1) * a.tile), j1 = min(t.cp, (it.j + 1) * a.tile);
+  for (int i0 = it.i * a.tile; i0 < i1; i0 += 32)
+    for (int j0 = it.j * a.tile; j0 < j1; j0 += 32) {
       __syncthreads();
       for (int y = y0; y < 32; y += 8) {
         // (along the matrix's rows: X's rows, or its columns)
@@ -121,11 +78,11 @@ __global__ __launch_bounds__(256) void k_ns_load(NsArgs a, const NsItem* items) 
       __syncthreads();
       for (int y = y0; y < 32; y += 8) {
         _Float16 hi, lo;
-        split(block[y][x], hi, lo);
+        halve(block[y][x], hi, lo);
         const int64_t at = (int64_t)(i0 + y) * t.cp + j0 + x;
         X[at] = hi;
         X[at + a.nx] = lo;
-        split(block[x][y], hi, lo);
+        halve(block[x][y], hi, lo);
         const int64_t to = (int64_t)(j0 + y) * t.rp + i0 + x;
         XT[to] = hi;
         XT[to + a.nx] = lo;
@@ -141,35 +98,40 @@ hipError_t launch_ns_load(const NsArgs& a, const NsItem* items, int32_t n, hipSt
 
 // ---------------------------------------------------------------------------
 // The products, all of the form C[i][j] = sum_k L[i][k] Q[j][k] with k contiguous in both
-// operands (the next X is stored in both orders for it).  Tiles of 128 x 128, four waves
-// of 64 x 64.  A and P are symmetric: only tiles with j <= i are computed, and stored twice.
+// operands (the next X is stored in both orders for it).  Tiles of T x T, four waves of
+// T / 2 x T / 2.  A and P are symmetric: only tiles with j <= i are computed, and stored
+// twice.  A lane ends with four consecutive rows of a column; a wave's block goes through
+// LDS, where it is read by rows of either order, 16 bytes a lane.
 // ---------------------------------------------------------------------------
 
-template <int WHAT>
+template <int WHAT, int T>
 __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const NsItem* items) {
-  constexpr int KT = 32, ROW = 2 * KT, T = kNsTile;
-  constexpr int PLANE = 2 * T * ROW;  // both operands' rows
-  __shared__ __align__(16) char lds[2 * PLANE];
+  constexpr int KT = 32, ROW = 2 * KT, W = T / 2, NT = W / 32, NQ = T / 32;
+  constexpr int PLANE = 2 * T * ROW;      // both operands' rows
+  constexpr int BR = 2 * W + 16;          // bytes of a row of a wave's block
+  constexpr int BLOCK = W * BR;
+  constexpr int LDS = 2 * PLANE > 4 * BLOCK ? 2 * PLANE : 4 * BLOCK;
+  __shared__ __align__(16) char lds[LDS];
   const NsItem it = items[blockIdx.x];
   const NsMat t = a.mats[it.mat];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wi = wave & 1, wj = wave >> 1;
   const int i0 = it.i * T, j0 = it.j * T;
-  const bool step = WHAT == NS_STEP || WHAT == NS_LAST;
+  constexpr bool step = WHAT == NS_STEP || WHAT == NS_LAST;
   const _Float16* L = WHAT == NS_GRAM ? a.X[from] + t.xo : WHAT == NS_POLY ? a.A + t.ao : a.P + t.ao;
   const _Float16* Q = WHAT == NS_GRAM ? L : WHAT == NS_POLY ? L : a.XT[from] + t.xo;
   const int64_t lplane = WHAT == NS_GRAM ? a.nx : a.na, qplane = WHAT == NS_POLY ? a.na : a.nx;
   const int K = WHAT == NS_GRAM ? t.cp : t.rp;
   const int nj = step ? t.cp : t.rp;
 
-  // 256 rows of four 16-byte chunks a plane: each thread takes one chunk of rows tid / 4 + 64 q
+  // 2 T rows of four 16-byte chunks a plane: each thread takes one chunk of rows tid / 4 + 64 q
   const int c = tid & 3;
-  const _Float16* row[4];
-  char* put[4];
+  const _Float16* row[NQ];
+  char* put[NQ];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
+  for (int q = 0; q < NQ; ++q) {
     const int r = 64 * q + (tid >> 2);
-    if (r < T) {
+    if (2 * q < NQ) {
       const int i = i0 + r < t.rp ? i0 + r : t.rp - 1;
       row[q] = L + (int64_t)i * K + 8 * c;
     } else {
@@ -178,26 +140,26 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
     }
     put[q] = lds + r * ROW + ((c ^ ((r >> 1) & 3)) << 4);
   }
-  f16x8 v[4][2];
+  f16x8 v[NQ][2];
   auto load = [&](int k) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < NQ; ++q) {
       v[q][0] = *(const f16x8*)(row[q] + k);
-      v[q][1] = *(const f16x8*)(row[q] + (q < 2 ? lplane : qplane) + k);
+      v[q][1] = *(const f16x8*)(row[q] + (2 * q < NQ ? lplane : qplane) + k);
     }
   };
-  f32x16 acc[2][2];
+  f32x16 acc[NT][NT];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < NT; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
   load(0);
   for (int k = 0; k < K; k += KT) {
     __syncthreads();
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < NQ; ++q) {
       *(f16x8*)put[q] = v[q][0];
       *(f16x8*)(put[q] + PLANE) = v[q][1];
     }
@@ -208,94 +170,157 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
 #pragma unroll
     for (int ks = 0; ks < KT / 16; ++ks) {
       const int cc = 2 * ks + (lane >> 5), r = lane & 31;
-      f16x8 x[2][2], y[2][2];
+      f16x8 x[NT][2], y[NT][2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < NT; ++i)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int ri = wi * 64 + 32 * i + r, rj = T + wj * 64 + 32 * i + r;
+          const int ri = wi * W + 32 * i + r, rj = T + wj * W + 32 * i + r;
           x[i][e] = *(const f16x8*)(lds + e * PLANE + ri * ROW + ((cc ^ ((ri >> 1) & 3)) << 4));
           y[i][e] = *(const f16x8*)(lds + e * PLANE + rj * ROW + ((cc ^ ((rj >> 1) & 3)) << 4));
         }
+      // (small products first, the tiles in turn)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int h = 0; h < 3; ++h)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][1], y[j][0], acc[i][j], 0, 0, 0);
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[j][1], acc[i][j], 0, 0, 0);
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], y[j][0], acc[i][j], 0, 0, 0);
-        }
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][h == 0], y[j][h == 1], acc[i][j], 0, 0, 0);
     }
   }
 
-  // lane: column j, rows 8 (e / 4) + 4 (lane / 32) + e % 4 of each 32
+  // This wave's block: rows bi0 .., columns bj0 .. of C
+  const int bi0 = i0 + wi * W, bj0 = j0 + wj * W;
   const int half = 4 * (lane >> 5);
-  const bool mirror = !step && it.i != it.j;
-  const float gain = step ? sqrtf(fmaxf(1.f, (float)t.rows / (float)t.cols)) : 0.f;
+  if (WHAT == NS_LAST) {
+    const bool turned = t.rows > t.cols;
+    const float gain = ns_gain(t);
 #pragma unroll
-  for (int bj = 0; bj < 2; ++bj) {
-    const int j = j0 + wj * 64 + 32 * bj + (lane & 31);
-    if (j >= nj) continue;
+    for (int bj = 0; bj < NT; ++bj) {
+      const int j = bj0 + 32 * bj + (lane & 31);
+      if (j >= nj) continue;
 #pragma unroll
-    for (int bi = 0; bi < 2; ++bi)
+      for (int bi = 0; bi < NT; ++bi)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int i = i0 + wi * 64 + 32 * bi + 8 * q + half;  // .. i + 3
-        if (i >= t.rp) continue;
-        f16x4 hi, lo;
+        for (int q = 0; q < 4; ++q) {
+          const int i = bi0 + 32 * bi + 8 * q + half;  // .. i + 3
+          if (i >= t.rp) continue;
+          const _Float16* old = a.XT[from] + t.xo + (int64_t)j * t.rp + i;
+          const f16x4 hi = *(const f16x4*)old, lo = *(const f16x4*)(old + a.nx);
+          f32x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float x = acc[bi][bj][4 * q + e] * kUnscale;
-          const int64_t at = (int64_t)(i + e) * nj + j;
-          if (WHAT == NS_POLY) {
-            const _Float16* old = a.A + t.ao + at;
-            x = fmaf(kNsC, x, kNsB * join(old[0], old[a.na]));
-          }
-          if (step) {
-            const _Float16* old = a.X[from] + t.xo + at;
-            x = fmaf(kNsA, join(old[0], old[a.nx]), x);
-          }
-          if (WHAT == NS_LAST) {
-            const bool turned = t.rows > t.cols;
+          for (int e = 0; e < 4; ++e) v[e] = acc[bi][bj][4 * q + e] * kUnscale;
+          v = add_held(kNsA, hi, lo, v);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float x = v[e] * kUnscale;
             const int gi = turned ? j : i + e, gj = turned ? i + e : j;
             if (gi >= t.rows || gj >= t.cols) continue;
             if (a.W) apply(a, t, gi, gj, gain * x);
             else a.out[t.src + (int64_t)gi * t.ld + gj] = x;
-            continue;
           }
-          _Float16 h, l;
-          split(x, h, l);
-          hi[e] = h;
-          lo[e] = l;
-          _Float16* to = (WHAT == NS_GRAM ? a.A + t.ao : WHAT == NS_POLY ? a.P + t.ao
-                                                                         : a.X[1 - from] + t.xo) + at;
-          to[0] = h;
-          to[WHAT == NS_STEP ? a.nx : a.na] = l;
         }
-        if (WHAT == NS_LAST) continue;
-        if (WHAT == NS_STEP || mirror) {
-          _Float16* to = (WHAT == NS_GRAM ? a.A + t.ao : WHAT == NS_POLY ? a.P + t.ao
-                                                                         : a.XT[1 - from] + t.xo) +
-                         (int64_t)j * t.rp + i;
-          *(f16x4*)to = hi;
-          *(f16x4*)(to + (WHAT == NS_STEP ? a.nx : a.na)) = lo;
-        }
-      }
+    }
+    if (a.W && a.lrm && it.i == 0 && it.j == 0 && tid == 0 && !(fabsf(a.lrm[t.m]) < INFINITY))
+      a.flag[1] = 1;
+    return;
   }
-  if (WHAT == NS_LAST && a.W && a.lrm && it.i == 0 && it.j == 0 && tid == 0 &&
-      !(fabsf(a.lrm[t.m]) < INFINITY))
-    a.flag[1] = 1;
+  if (bi0 >= t.rp || bj0 >= nj) {  // (no wave waits below)
+    __syncthreads();
+    return;
+  }
+  __syncthreads();  // the operands have been read: LDS is the waves' own from here on
+  char* block = lds + wave * BLOCK;  // [column][row]
+  constexpr int LPR = W / 8;         // lanes of 16 bytes to a row of the block
+  const int64_t plane = WHAT == NS_STEP ? a.nx : a.na;
+  _Float16* to = WHAT == NS_GRAM ? a.A + t.ao : WHAT == NS_POLY ? a.P + t.ao : a.X[1 - from] + t.xo;
+  _Float16* tt = WHAT == NS_STEP ? a.XT[1 - from] + t.xo : to;  // [j][i]: stride rp
+  const _Float16* old = WHAT == NS_POLY ? a.A + t.ao : a.XT[from] + t.xo;  // [j][i]
+#pragma unroll
+  for (int bi = 0; bi < NT; ++bi)
+#pragma unroll
+    for (int bj = 0; bj < NT; ++bj) acc[bi][bj] *= WHAT == NS_POLY ? kNsC * kUnscale : kUnscale;
+  if (WHAT != NS_GRAM) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int q = 0; q < W * LPR / 64; ++q) {
+        const int r = q * (64 / LPR) + lane / LPR, ch = lane % LPR;
+        const int j = min(bj0 + r, nj - 1), i = min(bi0 + 8 * ch, t.rp - 8);
+        *(f16x8*)(block + r * BR + 16 * ch) = *(const f16x8*)(old + h * plane + (int64_t)j * t.rp + i);
+      }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int bi = 0; bi < NT; ++bi)
+#pragma unroll
+        for (int bj = 0; bj < NT; ++bj)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f16x4 o = *(const f16x4*)(block + (32 * bj + (lane & 31)) * BR + 2 * (32 * bi + 8 * q + half));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              acc[bi][bj][4 * q + e] = fmaf(WHAT == NS_POLY ? kNsB : kNsA, (float)o[e], acc[bi][bj][4 * q + e]);
+          }
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+  const bool other = WHAT == NS_STEP || it.i != it.j;  // the order [i][j] too
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int bi = 0; bi < NT; ++bi)
+#pragma unroll
+      for (int bj = 0; bj < NT; ++bj)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          f16x4 hi, lo;
+          halve(f32x4{acc[bi][bj][4 * q], acc[bi][bj][4 * q + 1], acc[bi][bj][4 * q + 2], acc[bi][bj][4 * q + 3]},
+                hi, lo);
+          *(f16x4*)(block + (32 * bj + (lane & 31)) * BR + 2 * (32 * bi + 8 * q + half)) = h ? lo : hi;
+        }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int q = 0; q < W * LPR / 64; ++q) {
+      const int r = q * (64 / LPR) + lane / LPR, ch = lane % LPR;
+      const int j = bj0 + r, i = bi0 + 8 * ch;
+      if (j < nj && i < t.rp)
+        *(f16x8*)(tt + h * plane + (int64_t)j * t.rp + i) = *(const f16x8*)(block + r * BR + 16 * ch);
+    }
+    if (other) {
+      // transposing loads: lane (li, lk) gets row li of the block's 16, columns 8 lk .. + 7
+      const int li = lane & 15, lk = lane >> 4;
+#pragma unroll
+      for (int r = 0; r < W; r += 16)
+#pragma unroll
+        for (int cc = 0; cc < W; cc += 32) {
+          const char* at = block + (cc + 8 * lk + (li >> 2)) * BR + 2 * r + 8 * (li & 3);
+          const f16x8 o = columns(at, 4 * BR);
+          const int i = bi0 + r + li, j = bj0 + cc + 8 * lk;
+          if (i < t.rp && j < nj) *(f16x8*)(to + h * plane + (int64_t)i * nj + j) = o;
+        }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
 }
+
+namespace {
+template <int T>
+void product(const NsArgs& a, int what, int from, const NsItem* items, unsigned n, hipStream_t s) {
+  switch (what) {
+    case NS_GRAM: k_ns_product<NS_GRAM, T><<<n, 256, 0, s>>>(a, from, items); break;
+    case NS_POLY: k_ns_product<NS_POLY, T><<<n, 256, 0, s>>>(a, from, items); break;
+    case NS_STEP: k_ns_product<NS_STEP, T><<<n, 256, 0, s>>>(a, from, items); break;
+    default: k_ns_product<NS_LAST, T><<<n, 256, 0, s>>>(a, from, items); break;
+  }
+}
+}  // namespace
 
 hipError_t launch_ns_product(const NsArgs& a, int what, int from, const NsItem* items, int32_t n,
                              hipStream_t s) {
   note_variant("k_ns_product", kArithX3);
-  switch (what) {
-    case NS_GRAM: k_ns_product<NS_GRAM><<<(unsigned)n, 256, 0, s>>>(a, from, items); break;
-    case NS_POLY: k_ns_product<NS_POLY><<<(unsigned)n, 256, 0, s>>>(a, from, items); break;
-    case NS_STEP: k_ns_product<NS_STEP><<<(unsigned)n, 256, 0, s>>>(a, from, items); break;
-    default: k_ns_product<NS_LAST><<<(unsigned)n, 256, 0, s>>>(a, from, items); break;
-  }
+  if (a.tile == 64) product<64>(a, what, from, items, (unsigned)n, s);
+  else product<128>(a, what, from, items, (unsigned)n, s);
   return hipGetLastError();
 }
 

@@ -1,0 +1,382 @@
+// Newton-Schulz steps of matrices that fit a workgroup's LDS: one launch from the gradient
+// to the result.  (Values as in k_newton.hip: fp16 halves hi and lo of v 2^13.)
+//
+// LDS: X [RP][C], a plane of each half, and one such pair for A, which P replaces.  All
+// operands come from there:
+//   A = X X^T       rows of X for both operands;
+//   P = b A + c A A rows of A;
+//   X <- a X + X^T-columns x P:  D[col][row] = sum_k X[k][col] P[row][k], the first operand
+//       by transposing loads, so that a lane ends with four consecutive columns of a row and
+//       stores 8 bytes a plane.  The k of a fragment are then rows 4 lk + j and 16 + 4 lk + j;
+//       the columns of A and P lie in that order.
+// Rows are 16 bytes times an odd number apart, which spreads 16 of them over all banks.
+//
+// Bound by LDS reads and latency: a 2 x 4 block of tiles reads 12 fragments for its 24
+// matrix instructions, what one LDS feeds four SIMDs with.
+
+#include "newton_device.h"
+
+namespace pmlpk {
+
+namespace {
+
+// Bytes from the start of a row of A or P to its column 16 t + 4 k: each 32 columns lie in
+// the order in which the transposing loads bring 32 rows of X, 4 k + (0 .. 3) and
+// 16 + 4 k + (0 .. 3) for k = 0 .. 3.
+__device__ __forceinline__ int held_column(int t, int k) { return 64 * (t >> 1) + 8 * (t & 1) + 16 * k; }
+
+// Four consecutive values of a row, in both planes
+__device__ __forceinline__ void put4(char* at, int plane, const f32x4& v) {
+  f16x4 hi, lo;
+  halve(v, hi, lo);
+  *(f16x4*)at = hi;
+  *(f16x4*)(at + plane) = lo;
+}
+__device__ __forceinline__ f32x4 add4(float f, const char* at, int plane, const f32x4& v) {
+  return add_held(f, *(const f16x4*)at, *(const f16x4*)(at + plane), v);
+}
+
+// The lower triangle of a symmetric matrix in strips of two tiles: strip q is tiles
+// (ti, tj) and (ti, tj + 1), of which the second may lie above the diagonal.
+__device__ __forceinline__ void strip_of(int q, int& ti, int& tj) {
+  ti = 0;
+  while (q >= (ti >> 1) + 1) q -= (ti++ >> 1) + 1;
+  tj = 2 * q;
+}
+
+// This thread's entries of a matrix: row i, column j, `at` entries from its first one.
+template <int NT>
+struct Walk {
+  int i, j, di, dj, cols;
+  int64_t at, dat, wrap;
+  __device__ __forceinline__ Walk(int tid, const NsMat& t) : cols(t.cols) {
+    i = tid / cols;
+    j = tid - i * cols;
+    di = NT / cols;
+    dj = NT - di * cols;
+    at = (int64_t)i * t.ld + j;
+    dat = (int64_t)di * t.ld + dj;
+    wrap = t.ld - cols;
+  }
+  __device__ __forceinline__ void next() {
+    i += di;
+    j += dj;
+    at += dat;
+    if (j >= cols) {
+      j -= cols;
+      ++i;
+      at += wrap;
+    }
+  }
+};
+constexpr int kAhead = 8;  // entries that a thread loads at a time
+
+template <int TR, int NW, int UMAX, int EPT>
+__device__ __forceinline__ void small_matrix(const NsArgs& a, const NsMat& t, int steps, char* lds,
+                                             double* total) {
+  constexpr int NT = 64 * NW, RP = (TR + 1) / 2 * 32, TRB = RP / 32, NB = ns_strips(TR);
+  constexpr int NG = TR <= 4 ? 1 : 2, RG = (TR + NG - 1) / NG;  // row tiles of a unit
+  constexpr int KS = ns_small_split(TR, NW), PER = (NB + NW - 1) / NW;
+  constexpr int SP = 2 * RP + 16;
+  const int C = t.cp, SX = 2 * C + 16, pairs = C / 32;
+  const int xplane = 16 * TR * SX, pplane = 16 * TR * SP;
+  char *X = lds, *A = lds + 2 * xplane;
+  f32x4* part = (f32x4*)(A + 2 * pplane);  // [KS][NB][2][64]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int li = lane & 15, lk = lane >> 4;
+  const bool turned = t.rows > t.cols;
+  const int n = t.rows * t.cols;
+
+  // ---- momentum, norm, X ------------------------------------------------------------
+  for (int e = tid; e < (2 * xplane + 2 * pplane) / 16; e += NT) ((f32x4*)lds)[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const float* G = a.G + t.src;
+  const float* mom_in = a.mom_in ? a.mom_in + t.src : nullptr;
+  float* mom_out = a.mom_in ? a.mom_out + t.src : nullptr;
+  float u[EPT];  // entries tid, tid + NT, .. (of the first one again past the last)
+  double sum = 0;
+  {
+    Walk<NT> w(tid, t);
+#pragma unroll
+    for (int b = 0; b < EPT; b += kAhead) {
+      if (NT * b >= n) continue;
+      float m[kAhead];
+      int64_t at[kAhead];
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        at[q] = tid + NT * (b + q) < n ? w.at : 0;
+        w.next();
+        u[b + q] = G[at[q]];
+      }
+      if (mom_in) {
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) m[q] = mom_in[at[q]];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+          const float v = fmaf(a.mu, m[q], u[b + q]);
+          if (tid + NT * (b + q) < n) mom_out[at[q]] = v;
+          u[b + q] = a.nesterov ? fmaf(a.mu, v, u[b + q]) : v;
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q)
+        if (tid + NT * (b + q) < n) sum += (double)u[b + q] * (double)u[b + q];
+    }
+  }
+  sum = wave_total(sum);
+  if (lane == 0) total[wave] = sum;
+  __syncthreads();
+  sum = 0;
+  for (int w = 0; w < NW; ++w) sum += total[w];
+  const double scale = ns_scale(sum) * kScale;
+  const float scale32 = (float)scale;
+  const bool plain = scale > 1e-30 && scale < 1e30;  // (a factor of float32 is all they need)
+  {
+    Walk<NT> w(tid, t);
+#pragma unroll
+    for (int b = 0; b < EPT; ++b) {
+      if (tid + NT * b < n) {
+        _Float16 hi, lo;
+        halve(plain ? scale32 * u[b] : (float)(scale * (double)u[b]), hi, lo);
+        char* to = X + (turned ? w.j * SX + 2 * w.i : w.i * SX + 2 * w.j);
+        *(_Float16*)to = hi;
+        *(_Float16*)(to + xplane) = lo;
+      }
+      w.next();
+    }
+  }
+  __syncthreads();
+
+  // A tile of a symmetric matrix: rows 16 ti + 4 lk + e of column 16 tj + li, and mirrored
+  auto put_symmetric = [&](int ti, int tj, const f32x4& v) {
+    f16x4 hi, lo;
+    halve(v, hi, lo);
+    char* to = A + (16 * tj + li) * SP + held_column(ti, lk);
+    *(f16x4*)to = hi;
+    *(f16x4*)(to + pplane) = lo;
+    if (ti == tj) return;
+    char* at = A + (16 * ti + 4 * lk) * SP + held_column(tj, li >> 2) + 2 * (li & 3);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      *(_Float16*)(at + e * SP) = hi[e];
+      *(_Float16*)(at + e * SP + pplane) = lo[e];
+    }
+  };
+  // Tiles (ti, tj) and (ti, tj + 1) of S S^T over the 32-column steps k0 <= k < k1.
+  auto strip_product = [&](const char* S, int stride, int plane, int ti, int tj, int k0, int k1,
+                           f32x4 (&acc)[2]) {
+    acc[0] = acc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const char* x0 = S + (16 * ti + li) * stride + 16 * lk;
+    const char* y0 = S + (16 * tj + li) * stride + 16 * lk;
+    const int second = tj < ti ? 16 * stride : 0;
+    f16x8 x[2][2], y[2][2][2];  // [stage]
+    auto fetch = [&](int b, int k) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        x[b][h] = *(const f16x8*)(x0 + h * plane + 64 * k);
+        y[b][0][h] = *(const f16x8*)(y0 + h * plane + 64 * k);
+        y[b][1][h] = *(const f16x8*)(y0 + second + h * plane + 64 * k);
+      }
+    };
+    auto multiply = [&](int b) {
+#pragma unroll
+      for (int h = 0; h < 3; ++h)  // (small products first, the tiles in turn)
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          acc[q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[b][h == 0], y[b][q][h == 1], acc[q], 0, 0, 0);
+    };
+    fetch(0, k0);
+    for (int k = k0; k < k1; k += 2) {
+      if (k + 1 < k1) fetch(1, k + 1);
+      multiply(0);
+      if (k + 1 >= k1) break;
+      if (k + 2 < k1) fetch(0, k + 2);
+      multiply(1);
+    }
+  };
+
+  for (int step = 0; step < steps; ++step) {
+    // ---- A = X X^T ------------------------------------------------------------------
+    for (int q = wave; q < NB * KS; q += NW) {
+      const int b = q % NB, ks = q / NB;
+      int ti, tj;
+      strip_of(b, ti, tj);
+      f32x4 acc[2];
+      strip_product(X, SX, xplane, ti, tj, ks * pairs / KS, (ks + 1) * pairs / KS, acc);
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        if (KS > 1) part[((ks * NB + b) * 2 + r) * 64 + lane] = acc[r];
+        else if (tj + r <= ti) put_symmetric(ti, tj + r, acc[r] * kUnscale);
+      }
+    }
+    __syncthreads();
+    if (KS > 1) {
+      for (int q = wave; q < NB * 2; q += NW) {
+        int ti, tj;
+        strip_of(q / 2, ti, tj);
+        if (tj + (q & 1) > ti) continue;
+        f32x4 v = part[q * 64 + lane];
+#pragma unroll
+        for (int k = 1; k < KS; ++k) v += part[(k * NB * 2 + q) * 64 + lane];
+        put_symmetric(ti, tj + (q & 1), v * kUnscale);
+      }
+      __syncthreads();
+    }
+    // ---- P = b A + c A A, over A ------------------------------------------------------
+    f32x4 poly[PER][2];
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      if (wave + u * NW >= NB) continue;
+      int ti, tj;
+      strip_of(wave + u * NW, ti, tj);
+      strip_product(A, SP, pplane, ti, tj, 0, TRB, poly[u]);
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+        if (tj + r <= ti)
+          poly[u][r] = add4(kNsB, A + (16 * (tj + r) + li) * SP + held_column(ti, lk), pplane,
+                            (kNsC * kUnscale) * poly[u][r]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      if (wave + u * NW >= NB) continue;
+      int ti, tj;
+      strip_of(wave + u * NW, ti, tj);
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+        if (tj + r <= ti) put_symmetric(ti, tj + r, poly[u][r]);
+    }
+    __syncthreads();
+    // ---- X <- a X + P X ---------------------------------------------------------------
+    f32x4 next[UMAX][2][RG];
+#pragma unroll
+    for (int u = 0; u < UMAX; ++u) {
+      const int unit = wave + u * NW;
+      if (unit >= pairs * NG) continue;
+      const int pair = unit % pairs, r0 = unit / pairs * RG;
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int r = 0; r < RG; ++r) next[u][p][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const char* x0 = X + (4 * lk + (li >> 2)) * SX + 64 * pair + 8 * (li & 3);
+      const char* p0 = A + (16 * r0 + li) * SP + 16 * lk;
+#pragma unroll
+      for (int k = 0; k < TRB; ++k) {
+        f16x8 x[2][2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            // (16 rows are left of an odd number of tiles: their second reading meets the zeros
+            // in P's last 16 columns)
+            x[p][h] = columns(x0 + h * xplane + 32 * k * SX + 32 * p, 2 * k + 1 < TR ? 16 * SX : 0);
+        f16x8 y[RG][2];
+#pragma unroll
+        for (int r = 0; r < RG; ++r)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            // (a tile past the last one reads the last one again, and is not stored)
+            const int tile = NG * RG > TR && r0 + r >= TR ? r - 1 : r;
+            y[r][h] = *(const f16x8*)(p0 + h * pplane + 16 * tile * SP + 64 * k);
+          }
+#pragma unroll
+        for (int h = 0; h < 3; ++h)
+#pragma unroll
+          for (int r = 0; r < RG; ++r)
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+              next[u][p][r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[p][h == 0], y[r][h == 1], next[u][p][r], 0, 0, 0);
+      }
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int r = 0; r < RG; ++r) {
+          if (NG * RG > TR && r0 + r >= TR) continue;
+          next[u][p][r] = add4(kNsA, X + (16 * (r0 + r) + li) * SX + 2 * (32 * pair + 16 * p + 4 * lk),
+                               xplane, kUnscale * next[u][p][r]);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < UMAX; ++u) {
+      const int unit = wave + u * NW;
+      if (unit >= pairs * NG) continue;
+      const int pair = unit % pairs, r0 = unit / pairs * RG;
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int r = 0; r < RG; ++r) {
+          if (NG * RG > TR && r0 + r >= TR) continue;
+          const int row = 16 * (r0 + r) + li, col = 32 * pair + 16 * p + 4 * lk;
+          if (step + 1 < steps) put4(X + row * SX + 2 * col, xplane, next[u][p][r]);
+          else *(f32x4*)(X + row * (4 * C + 16) + 4 * col) = next[u][p][r];  // fp32 over both planes
+        }
+    }
+    __syncthreads();
+  }
+
+  // ---- the result ---------------------------------------------------------------------
+  const float gain = ns_gain(t);
+  Walk<NT> w(tid, t);
+#pragma unroll 4
+  for (int e = tid; e < n; e += NT) {
+    const float x = *(const float*)(X + (turned ? w.j * (4 * C + 16) + 4 * w.i : w.i * (4 * C + 16) + 4 * w.j));
+    if (a.W) apply(a, t, w.i, w.j, gain * (x * kUnscale));
+    else a.out[t.src + w.at] = x * kUnscale;
+    w.next();
+  }
+  if (a.W && a.lrm && tid == 0 && !(fabsf(a.lrm[t.m]) < INFINITY)) a.flag[1] = 1;
+}
+
+}  // namespace
+
+// TR tiles of rows, up to 128 columns.  (OCC: waves of a SIMD that LDS leaves room for.)
+template <int TR, int OCC>
+__global__ __launch_bounds__(64 * kNsWaves[TR - 1], OCC) void k_ns_small(NsArgs a, const int32_t* list,
+                                                                        int steps) {
+  constexpr int NW = kNsWaves[TR - 1];
+  extern __shared__ __align__(16) char lds[];
+  __shared__ double total[NW];
+  const NsMat t = a.mats[list[blockIdx.x]];
+  small_matrix<TR, NW, 1, (16 * TR * 128 + 64 * NW - 1) / (64 * NW)>(a, t, steps, lds, total);
+}
+
+// Any of them, and wider ones.
+__global__ __launch_bounds__(512, 2) void k_ns_small_any(NsArgs a, const int32_t* list, int steps) {
+  extern __shared__ __align__(16) char lds[];
+  __shared__ double total[8];
+  const NsMat t = a.mats[list[blockIdx.x]];
+  switch ((t.r + 15) / 16) {
+#define PMLP_NS(TR)                                                                        \
+  case TR:                                                                                 \
+    small_matrix<TR, 8, kNsUnits[(TR - 1) / 2], kNsEntries[(TR - 1) / 2]>(a, t, steps, lds, total); \
+    break;
+    PMLP_NS(1) PMLP_NS(2) PMLP_NS(3) PMLP_NS(4) PMLP_NS(5) PMLP_NS(6) PMLP_NS(7) PMLP_NS(8)
+#undef PMLP_NS
+    default: break;
+  }
+}
+
+hipError_t launch_ns_small(const NsArgs& a, int cls, size_t lds, const int32_t* list, int32_t n,
+                           int32_t steps, hipStream_t s) {
+  auto go = [&](auto fn, int nw) {
+    note_variant(cls < 8 ? "k_ns_small" : "k_ns_small_any", kArithX3);
+    if (const hipError_t e = hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)kNsSmallLds))
+      return e;
+    fn<<<(unsigned)n, 64 * nw, lds, s>>>(a, list, steps);
+    return hipGetLastError();
+  };
+  switch (cls) {
+    case 0: return go(k_ns_small<1, 4>, kNsWaves[0]);
+    case 1: return go(k_ns_small<2, 4>, kNsWaves[1]);
+    case 2: return go(k_ns_small<3, 4>, kNsWaves[2]);
+    case 3: return go(k_ns_small<4, 3>, kNsWaves[3]);
+    case 4: return go(k_ns_small<5, 4>, kNsWaves[4]);
+    case 5: return go(k_ns_small<6, 2>, kNsWaves[5]);
+    case 6: return go(k_ns_small<7, 2>, kNsWaves[6]);
+    case 7: return go(k_ns_small<8, 2>, kNsWaves[7]);
+    default: return go(k_ns_small_any, 8);
+  }
+}
+
+}  // namespace pmlpk

@@ -9,7 +9,6 @@ namespace pmlpk {
 // The quintic whose iteration takes every singular value in (0, 1] towards 1 (Muon:
 // Jordan and others, 2024): x <- x (a + b x^2 + c x^4).
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
-constexpr int32_t kNsTile = 128;   // rows and columns of a workgroup's tile
 constexpr int32_t kNsPiece = 8192; // entries of a piece of the momentum's pass, about
 
 // One model's matrix: rows x cols, with r = min(rows, cols) and c = max(rows, cols); the
@@ -44,6 +43,7 @@ struct NsArgs {
   _Float16 *X[2], *XT[2];  // [2][nx] each: X and its transpose, before and after a step
   _Float16 *A, *P;         // [2][na]
   int64_t nx, na;
+  int32_t tile;         // rows and columns of a workgroup's tile: 64 or 128
   // where the result goes: out, or the weights
   float* out;
   float* W;
@@ -63,5 +63,50 @@ enum NsProduct { NS_GRAM = 0, NS_POLY = 1, NS_STEP = 2, NS_LAST = 3 };
 // from X[from], XT[from]
 hipError_t launch_ns_product(const NsArgs& a, int what, int from, const NsItem* items, int32_t n,
                              hipStream_t s);
+
+// Matrices that fit LDS, a workgroup each: classes 0 .. 7 (r of 1 .. 8 tiles of 16, c up to
+// 128) and 8 .. 11 (wider, r up to 32, 64, 96, 128).
+constexpr int kNsClasses = 12;
+constexpr size_t kNsSmallLds = 160 * 1024 - 64;  // dynamic LDS of a workgroup, at most
+// Strips of two tiles in the lower triangle of tr x tr tiles.
+__host__ __device__ constexpr int ns_strips(int tr) {
+  int n = 0;
+  for (int i = 0; i < tr; ++i) n += i / 2 + 1;
+  return n;
+}
+// Parts that the columns are split in for A = X X^T, where its strips are fewer than the
+// waves.
+__host__ __device__ constexpr int ns_small_split(int tr, int waves) {
+  const int n = waves / ns_strips(tr);
+  return n < 1 ? 1 : n > 4 ? 4 : n;
+}
+// Waves of a workgroup of the classes up to 128 columns (the others have eight).
+constexpr int kNsWaves[8] = {4, 4, 4, 4, 8, 8, 8, 8};
+// For r up to 32, 64, 96, 128 in eight waves: units of work (32 columns and up to four tiles
+// of rows) a wave, and entries a thread loads, at most.
+constexpr int kNsUnits[4] = {5, 3, 3, 2}, kNsEntries[4] = {80, 64, 64, 48};
+// LDS of an r x c matrix in so many waves.
+inline size_t ns_small_lds(int32_t r, int32_t c, int waves) {
+  const int cp = (c + 31) / 32 * 32, rp = (r + 31) / 32 * 32, tr = (r + 15) / 16;
+  const int split = ns_small_split(tr, waves);
+  return (size_t)32 * tr * ((2 * cp + 16) + (2 * rp + 16)) +
+         (split > 1 ? (size_t)split * ns_strips(tr) * 2048 : 0);
+}
+// The class of an r x c matrix, or -1.
+inline int ns_small_class(int32_t r, int32_t c) {
+  if (r > 128 || c > 1280) return -1;
+  if (c <= 128) return (r + 15) / 16 - 1;
+  const int k = (r - 1) / 32, units = (c + 31) / 32 * (k >= 2 ? 2 : 1);
+  if (ns_small_lds(r, c, 8) > kNsSmallLds || units > 8 * kNsUnits[k] || r * c > 512 * kNsEntries[k])
+    return -1;
+  return 8 + k;
+}
+// Up to so many matrices go in one launch whatever their classes: each launch ends with
+// workgroups that wait for its longest.
+constexpr int kNsOneLaunch = 512;
+// From the gradient to the result, a workgroup for each matrix of the list; class 8 and
+// above: any of the classes.
+hipError_t launch_ns_small(const NsArgs& a, int cls, size_t lds, const int32_t* list, int32_t n,
+                           int32_t steps, hipStream_t s);
 
 }  // namespace pmlpk

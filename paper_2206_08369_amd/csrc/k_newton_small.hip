@@ -75,7 +75,7 @@ template <int TR, int NW, int UMAX, int EPT>
 __device__ __forceinline__ void small_matrix(const NsArgs& a, const NsMat& t, int steps, char* lds,
                                              double* total) {
   constexpr int NT = 64 * NW, RP = (TR + 1) / 2 * 32, TRB = RP / 32, NB = ns_strips(TR);
-  constexpr int NG = TR <= 4 ? 1 : 2, RG = (TR + NG - 1) / NG;  // row tiles of a unit
+  constexpr int NG = NW == 16 ? (TR + 1) / 2 : TR <= 4 ? 1 : 2, RG = (TR + NG - 1) / NG;  // row tiles of a unit
   constexpr int KS = ns_small_split(TR, NW), PER = (NB + NW - 1) / NW;
   constexpr int SP = 2 * RP + 16;
   const int C = t.cp, SX = 2 * C + 16, pairs = C / 32;
@@ -92,6 +92,7 @@ __device__ __forceinline__ void small_matrix(const NsArgs& a, const NsMat& t, in
   const float* G = a.G + t.src;
   const float* mom_in = a.mom_in ? a.mom_in + t.src : nullptr;
   float* mom_out = a.mom_in ? a.mom_out + t.src : nullptr;
+  static_assert(EPT % kAhead == 0, "entries are loaded so many at a time");
   float u[EPT];  // entries tid, tid + NT, .. (of the first one again past the last)
   double sum = 0;
   {
@@ -337,7 +338,8 @@ __global__ __launch_bounds__(64 * kNsWaves[TR - 1], OCC) void k_ns_small(NsArgs 
   extern __shared__ __align__(16) char lds[];
   __shared__ double total[NW];
   const NsMat t = a.mats[list[blockIdx.x]];
-  small_matrix<TR, NW, 1, (16 * TR * 128 + 64 * NW - 1) / (64 * NW)>(a, t, steps, lds, total);
+  constexpr int all = 16 * TR * 128 / (64 * NW);  // entries a thread
+  small_matrix<TR, NW, 1, (all + kAhead - 1) / kAhead * kAhead>(a, t, steps, lds, total);
 }
 
 // Any of them, and wider ones.
@@ -372,9 +374,9 @@ hipError_t launch_ns_small(const NsArgs& a, int cls, size_t lds, const int32_t* 
     case 2: return go(k_ns_small<3, 4>, kNsWaves[2]);
     case 3: return go(k_ns_small<4, 3>, kNsWaves[3]);
     case 4: return go(k_ns_small<5, 4>, kNsWaves[4]);
-    case 5: return go(k_ns_small<6, 2>, kNsWaves[5]);
-    case 6: return go(k_ns_small<7, 2>, kNsWaves[6]);
-    case 7: return go(k_ns_small<8, 2>, kNsWaves[7]);
+    case 5: return go(k_ns_small<6, 4>, kNsWaves[5]);
+    case 6: return go(k_ns_small<7, 4>, kNsWaves[6]);
+    case 7: return go(k_ns_small<8, 4>, kNsWaves[7]);
     default: return go(k_ns_small_any, 8);
   }
 }

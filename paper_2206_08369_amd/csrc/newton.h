@@ -67,7 +67,7 @@ hipError_t launch_ns_product(const NsArgs& a, int what, int from, const NsItem* 
 // Matrices that fit LDS, a workgroup each: classes 0 .. 7 (r of 1 .. 8 tiles of 16, c up to
 // 128) and 8 .. 11 (wider, r up to 32, 64, 96, 128).
 constexpr int kNsClasses = 12;
-constexpr size_t kNsSmallLds = 160 * 1024 - 64;  // dynamic LDS of a workgroup, at most
+constexpr size_t kNsSmallLds = 160 * 1024 - 128;  // dynamic LDS of a workgroup, at most
 // Strips of two tiles in the lower triangle of tr x tr tiles.
 __host__ __device__ constexpr int ns_strips(int tr) {
   int n = 0;
@@ -81,7 +81,7 @@ __host__ __device__ constexpr int ns_small_split(int tr, int waves) {
   return n < 1 ? 1 : n > 4 ? 4 : n;
 }
 // Waves of a workgroup of the classes up to 128 columns (the others have eight).
-constexpr int kNsWaves[8] = {4, 4, 4, 4, 8, 8, 8, 8};
+constexpr int kNsWaves[8] = {4, 4, 4, 4, 8, 16, 16, 16};
 // For r up to 32, 64, 96, 128 in eight waves: units of work (32 columns and up to four tiles
 // of rows) a wave, and entries a thread loads, at most.
 constexpr int kNsUnits[4] = {5, 3, 3, 2}, kNsEntries[4] = {80, 64, 64, 48};

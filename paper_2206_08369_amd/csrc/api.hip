@@ -1946,7 +1946,8 @@ struct RtLayout {
   Carver c;
   RtPlan p{};
   int64_t items = 0, jitems = 0;  // at most
-  size_t hist = 0, count = 0, place = 0, zoff = 0, ioff = 0, joff = 0, slot = 0, item = 0, jitem = 0;
+  size_t hist = 0, count = 0, place = 0, zoff = 0, ioff = 0, joff = 0, slot = 0, row = 0, wdy = 0,
+         item = 0, jitem = 0;
   bool fits = true;
 };
 
@@ -1965,6 +1966,7 @@ RtLayout rt_layout(const pmlp* h, int64_t R, int32_t K, const RtShape& sh, bool 
   p.F = h->F;
   p.O = h->O;
   p.seg_off = h->d_seg_off;
+  p.act = h->d_act;
   p.flag = h->flag;
   p.t.rt = rt_rows(sh);
   p.t.uc = rt_units(sh, gated);
@@ -1995,14 +1997,21 @@ RtLayout rt_layout(const pmlp* h, int64_t R, int32_t K, const RtShape& sh, bool 
   l.ioff = l.c.take(M + 1);
   l.joff = l.c.take(M + 1);
   l.slot = l.c.take((size_t)P);
-  l.item = l.c.take(4 * (size_t)l.items);
-  l.jitem = l.c.take(4 * (size_t)l.jitems);
+  l.row = l.c.take((size_t)P);
+  l.wdy = l.c.take(train ? (size_t)h->O * P : 0);
+  l.item = l.c.take(16 * (size_t)l.items);
+  l.jitem = l.c.take(16 * (size_t)l.jitems);
   return l;
 }
 
-void rt_place(RtLayout* l, unsigned char* ws, const int32_t* idx, bool train) {
+// dY null: forward
+void rt_place(RtLayout* l, unsigned char* ws, const int32_t* idx, const float* weight, const float* dY) {
   RtPlan& p = l->p;
   p.idx = idx;
+  p.row = (int32_t*)(ws + l->row);
+  p.weight = weight;
+  p.dY = dY;
+  p.wdy = dY ? (float*)(ws + l->wdy) : nullptr;
   p.hist = (int32_t*)(ws + l->hist);
   p.count = (int32_t*)(ws + l->count);
   p.place = (int32_t*)(ws + l->place);
@@ -2011,7 +2020,7 @@ void rt_place(RtLayout* l, unsigned char* ws, const int32_t* idx, bool train) {
   p.joff = (int32_t*)(ws + l->joff);
   p.slot = (int32_t*)(ws + l->slot);
   p.items = (RtItem*)(ws + l->item);
-  p.jitems = train ? (RtItem*)(ws + l->jitem) : nullptr;
+  p.jitems = dY ? (RtItem*)(ws + l->jitem) : nullptr;
 }
 
 RtArgs rt_args(const pmlp* h, const float* X, const RtLayout& l) {
@@ -2034,6 +2043,7 @@ RtArgs rt_args(const pmlp* h, const float* X, const RtLayout& l) {
   a.place = p.place;
   a.zoff = p.zoff;
   a.slot = p.slot;
+  a.row = p.row;
   a.items = p.items;
   a.nitems = p.ioff + h->M;
   a.most = (int32_t)l.items;
@@ -2070,7 +2080,7 @@ int forward_routed(pmlp* h, const float* X, int32_t B, const int32_t* idx, const
   const int32_t parts = 2 * div_up(h->widest, l.p.t.uc);  // (a wave each)
   const size_t oP = l.c.take((size_t)R * parts * h->O);
   if (int rc = ensure_ws(h, &h->extra, l.c.bytes, "a routed pack")) return rc;
-  rt_place(&l, h->extra.ws, idx, false);
+  rt_place(&l, h->extra.ws, idx, weight, nullptr);
   if (int rc = run(h, KID_AUX, [&] { return launch_rt_plan(l.p, h->stream); })) return rc;
   RtArgs a = rt_args(h, X, l);
   a.part = (float*)(h->extra.ws + oP);
@@ -2094,12 +2104,12 @@ int gradients_routed(pmlp* h, const float* X, int32_t B, const int32_t* idx, con
   const int32_t nparts = div_up(whole, l.p.t.part);
   const size_t hidden = (size_t)h->widest * l.p.P, k = gated ? 2 : 1;
   const size_t oD = l.c.take((size_t)R * parts), oZ = l.c.take(hidden), oH = l.c.take(hidden),
-               oU = l.c.take(gated ? hidden : 0), oY = l.c.take((size_t)h->O * l.p.P),
+               oU = l.c.take(gated ? hidden : 0),
                oW = l.c.take(nparts > 1 ? nparts * k * h->N * h->F : 0),
                oV = l.c.take(nparts > 1 ? (size_t)nparts * h->O * h->N : 0);
   if (int rc = ensure_ws(h, &h->extra, l.c.bytes, "a routed pack")) return rc;
   unsigned char* const ws = h->extra.ws;
-  rt_place(&l, ws, idx, true);
+  rt_place(&l, ws, idx, weight, dY);
   if (int rc = run(h, KID_AUX, [&] { return launch_rt_plan(l.p, h->stream); })) return rc;
   RtGrad g{};
   g.a = rt_args(h, X, l);
@@ -2120,7 +2130,7 @@ int gradients_routed(pmlp* h, const float* X, int32_t B, const int32_t* idx, con
   g.dW1 = dW1;
   g.dV1 = dV1;
   g.dW2 = dW2;
-  g.wdy = (float*)(ws + oY);
+  g.wdy = l.p.wdy;
   g.wpart = (float*)(ws + oW);
   g.w2part = (float*)(ws + oV);
   g.mid = h->d_mid;

@@ -31,32 +31,48 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
 
 }  // namespace
 
-// One round per choice: the best key below the last one.  The row is read once a round,
-// from cache after the first.  T threads a row.
-template <int T>
+// One round per choice: the best key below the last one.  T threads a row, E scores a
+// thread in registers (0: more than fit, read again from cache in every round); only the
+// thread that held the last choice looks for its next best.  6,000 scores of 32 samples,
+// four choices: 19 us where every round read them again, 5 so.
+template <int T, int E>
 __global__ __launch_bounds__(256) void k_route(const float* __restrict__ scores, int B, int M, int K,
                                                int32_t* __restrict__ idx, float* __restrict__ weight) {
-  __shared__ uint64_t best[4];
+  __shared__ uint64_t best[2][4];
   const int t = threadIdx.x % T, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t b = (int64_t)blockIdx.x * (256 / T) + threadIdx.x / T;
   if (T == 64 && b >= B) return;  // (a row is one wave: no barrier below)
   const float* row = scores + b * M;
-  uint64_t last = ~0ull, mine = 0;
-  for (int k = 0; k < K; ++k) {
+  float v[E > 0 ? E : 1];
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = t + T * e < M ? row[t + T * e] : -INFINITY;
+  auto own_best = [&](uint64_t last) {
     uint64_t top = 0;
-    for (int m = t; m < M; m += T) {
-      const uint64_t key = score_key(row[m], m);
-      top = key < last && key > top ? key : top;
+    if (E > 0) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const uint64_t key = score_key(v[e], t + T * e);
+        top = key < last && key > top ? key : top;
+      }
+    } else {
+      for (int m = t; m < M; m += T) {
+        const uint64_t key = score_key(row[m], m);
+        top = key < last && key > top ? key : top;
+      }
     }
-    top = wave_max(top);
+    return top;
+  };
+  uint64_t own = own_best(~0ull), mine = 0;
+  for (int k = 0; k < K; ++k) {
+    uint64_t top = wave_max(own);
     if (T > 64) {
+      if (lane == 0) best[k & 1][wave] = top;
       __syncthreads();
-      if (lane == 0) best[wave] = top;
-      __syncthreads();
-      for (int w = 0; w < T / 64; ++w) top = best[w] > top ? best[w] : top;
+      for (int w = 0; w < T / 64; ++w) top = best[k & 1][w] > top ? best[k & 1][w] : top;
     }
     if (lane == k) mine = top;
-    last = top;  // 0: none left, and none below it
+    if (top == 0) break;  // none left
+    if (own == top) own = own_best(top);
   }
   if (t >= 64) return;
   const float top = __shfl(key_score(mine), 0);
@@ -71,8 +87,11 @@ __global__ __launch_bounds__(256) void k_route(const float* __restrict__ scores,
 hipError_t launch_route(const float* scores, int32_t B, int32_t M, int32_t K, int32_t* idx,
                         float* weight, hipStream_t s) {
   note_variant("k_route", kArithNone);
-  if (M <= 1024) k_route<64><<<(unsigned)((B + 3) / 4), 256, 0, s>>>(scores, B, M, K, idx, weight);
-  else k_route<256><<<(unsigned)B, 256, 0, s>>>(scores, B, M, K, idx, weight);
+  const unsigned waves = (unsigned)((B + 3) / 4);
+  if (M <= 256) k_route<64, 4><<<waves, 256, 0, s>>>(scores, B, M, K, idx, weight);
+  else if (M <= 1024) k_route<64, 16><<<waves, 256, 0, s>>>(scores, B, M, K, idx, weight);
+  else if (M <= 8192) k_route<256, 32><<<(unsigned)B, 256, 0, s>>>(scores, B, M, K, idx, weight);
+  else k_route<256, 0><<<(unsigned)B, 256, 0, s>>>(scores, B, M, K, idx, weight);
   return hipGetLastError();
 }
 
@@ -91,14 +110,20 @@ __global__ __launch_bounds__(256) void k_route_bwd(const int32_t* __restrict__ i
   float mean = 0.f;
   for (int k = 0; k < K; ++k) mean = fmaf(__shfl(w, k), __shfl(d, k), mean);
   const float ds = w * (d - mean);
-  for (int m0 = 0; m0 < M; m0 += 64) {
-    const int m = m0 + lane;
+  // (the choices as scalars: a comparison and an addition each for 64 scores)
+  int ck[kRtMaxK];
+  float cs[kRtMaxK];
+#pragma unroll
+  for (int k = 0; k < kRtMaxK; ++k) {
+    ck[k] = k < K ? __builtin_amdgcn_readlane(i, k) : -1;
+    cs[k] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ds), k));
+  }
+  for (int m = lane; m < M; m += 64) {
     float v = 0.f;
-    for (int k = 0; k < K; ++k) {
-      const float s = __shfl(ds, k);
-      if (__shfl(i, k) == m) v += s;
-    }
-    if (m < M) dscores[b * M + m] = v;
+#pragma unroll
+    for (int k = 0; k < kRtMaxK; ++k)
+      if (k < K) v += ck[k] == m ? cs[k] : 0.f;
+    dscores[b * M + m] = v;
   }
 }
 
@@ -137,12 +162,14 @@ __device__ __forceinline__ uint64_t peers_of(int m) {
   return peers;
 }
 
-// Walks run c: `take(slot, model, rank in counter)` for each slot with a model.
+// Walks run c of `chunk` slots: `take(slot, model, rank in counter)` for each slot with a
+// model.
 template <class Take>
-__device__ __forceinline__ void walk(const RtPlan& p, int c, int32_t* counter, bool report, Take take) {
+__device__ __forceinline__ void walk(const RtPlan& p, int c, int chunk, int32_t* counter, bool report,
+                                     Take take) {
   const int lane = threadIdx.x & 63;
-  const int64_t first = (int64_t)c * p.chunk;
-  const int64_t end = first + p.chunk < p.R ? first + p.chunk : p.R;
+  const int64_t first = (int64_t)c * chunk;
+  const int64_t end = first + chunk < p.R ? first + chunk : p.R;
   for (int64_t s0 = first; s0 < end; s0 += 64) {
     const int m = slot_model(p, s0 + lane, end, report);
     const uint64_t peers = peers_of(m);
@@ -152,6 +179,25 @@ __device__ __forceinline__ void walk(const RtPlan& p, int c, int32_t* counter, b
     base = __shfl(base, leader);
     if (m >= 0) take(s0 + lane, m, base + __popcll(peers & ((1ull << lane) - 1)));
   }
+}
+
+// Places hold no slot yet.
+__device__ __forceinline__ void clear_places(const RtPlan& p, int64_t first, int64_t stride) {
+  for (int64_t i = first; i < p.P; i += stride) {
+    p.slot[i] = -1;
+    p.row[i] = -1;
+    if (p.wdy)
+      for (int o = 0; o < p.O; ++o) p.wdy[(int64_t)o * p.P + i] = 0.f;
+  }
+}
+
+__device__ __forceinline__ void put_slot(const RtPlan& p, int64_t s, int at) {
+  const int64_t b = s / p.K;
+  p.slot[at] = (int32_t)s;
+  p.row[at] = (int32_t)b;
+  if (!p.wdy) return;
+  const float w = p.weight[s];
+  for (int o = 0; o < p.O; ++o) p.wdy[(int64_t)o * p.P + at] = w * p.dY[b * p.O + o];
 }
 
 }  // namespace
@@ -165,32 +211,44 @@ __global__ __launch_bounds__(64) void k_rt_count(RtPlan p) {
   for (int m = threadIdx.x; m < p.M; m += 64) counter[m] = 0;
   __threadfence_block();
   __syncthreads();
-  walk(p, c, counter, true, [](int64_t, int, int) {});
+  walk(p, c, p.chunk, counter, true, [](int64_t, int, int) {});
   __syncthreads();
   if (in_lds)
     for (int m = threadIdx.x; m < p.M; m += 64) row[m] = lds[m];
-  // no slot yet
-  for (int64_t i = (int64_t)c * 64 + threadIdx.x; i < p.P; i += (int64_t)gridDim.x * 64) p.slot[i] = -1;
+  clear_places(p, (int64_t)c * 64 + threadIdx.x, (int64_t)gridDim.x * 64);
 }
 
+// Where each run's rows of a model start: 16 models a workgroup, 16 threads to each.
 __global__ __launch_bounds__(256) void k_rt_columns(RtPlan p) {
-  const int m = blockIdx.x * 256 + threadIdx.x;
-  if (m >= p.M) return;
-  int sum = 0;
-  for (int c = 0; c < p.nchunk; ++c) {
-    int32_t* at = p.hist + (int64_t)c * p.M + m;
-    const int n = *at;
-    *at = sum;
-    sum += n;
+  __shared__ int32_t sums[16][17];
+  constexpr int EACH = kRtChunks / 16;
+  const int q = threadIdx.x >> 4, m = blockIdx.x * 16 + (threadIdx.x & 15);
+  int v[EACH], sum = 0;
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const int c = q * EACH + e;
+    v[e] = m < p.M && c < p.nchunk ? p.hist[(int64_t)c * p.M + m] : 0;
   }
-  p.count[m] = sum;
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) sum += v[e];
+  sums[q][threadIdx.x & 15] = sum;
+  __syncthreads();
+  if (m >= p.M) return;
+  int at = 0;
+  for (int r = 0; r < q; ++r) at += sums[r][threadIdx.x & 15];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const int c = q * EACH + e;
+    if (c < p.nchunk) p.hist[(int64_t)c * p.M + m] = at;
+    at += v[e];
+  }
+  if (q == 15) p.count[m] = at;
 }
 
 namespace {
 
 __device__ __forceinline__ int up(int a, int b) { return (a + b - 1) / b; }
 
-// Exclusive sums over the 1,024 threads of a workgroup of four numbers each.
 struct Sums {
   int32_t place, item, jitem;
   int64_t z;
@@ -199,8 +257,8 @@ __device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) {
   return Sums{a.place + b.place, a.item + b.item, a.jitem + b.jitem, a.z + b.z};
 }
 
-__device__ __forceinline__ Sums model_sums(const RtPlan& p, int m) {
-  const int n = p.count[m], rows = up(n, kRtPad) * kRtPad;
+__device__ __forceinline__ Sums model_sums(const RtPlan& p, int m, int n) {
+  const int rows = up(n, kRtPad) * kRtPad;
   const int h = (int)(p.seg_off[m + 1] - p.seg_off[m]);
   Sums s;
   s.place = rows;
@@ -210,30 +268,36 @@ __device__ __forceinline__ Sums model_sums(const RtPlan& p, int m) {
   return s;
 }
 
-}  // namespace
+__device__ __forceinline__ Sums from_lane(const Sums& v, int lane) {
+  return Sums{__shfl(v.place, lane), __shfl(v.item, lane), __shfl(v.jitem, lane),
+              (int64_t)__shfl((long long)v.z, lane)};
+}
 
-__global__ __launch_bounds__(1024) void k_rt_scan(RtPlan p) {
-  __shared__ Sums lds[1024];
-  const int t = threadIdx.x, each = up(p.M, 1024);
+// The sums over models before each, by a workgroup of 1,024 threads; `counts(m)` slots.
+template <class Counts>
+__device__ __forceinline__ void scan_models(const RtPlan& p, Sums* lds, Counts counts) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, each = up(p.M, 1024);
   const int m0 = t * each < p.M ? t * each : p.M, m1 = m0 + each < p.M ? m0 + each : p.M;
   Sums mine{0, 0, 0, 0};
-  for (int m = m0; m < m1; ++m) mine = mine + model_sums(p, m);
-  lds[t] = mine;
-  __syncthreads();
-  for (int d = 1; d < 1024; d <<= 1) {
-    Sums v = lds[t];
-    if (t >= d) v = v + lds[t - d];
-    __syncthreads();
-    lds[t] = v;
-    __syncthreads();
+  for (int m = m0; m < m1; ++m) mine = mine + model_sums(p, m, counts(m));
+  Sums upto = mine;  // over the lanes up to this one
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const Sums v = from_lane(upto, lane - d);
+    if (lane >= d) upto = upto + v;
   }
-  Sums at = t ? lds[t - 1] : Sums{0, 0, 0, 0};
+  if (lane == 63) lds[wave] = upto;
+  __syncthreads();
+  Sums at{0, 0, 0, 0};
+  for (int w = 0; w < wave; ++w) at = at + lds[w];
+  at = at + upto;
+  at = Sums{at.place - mine.place, at.item - mine.item, at.jitem - mine.jitem, at.z - mine.z};
   for (int m = m0; m < m1; ++m) {
     p.place[m] = at.place;
     p.zoff[m] = at.z;
     p.ioff[m] = at.item;
     p.joff[m] = at.jitem;
-    at = at + model_sums(p, m);
+    at = at + model_sums(p, m, counts(m));
   }
   if (t == 1023) {
     p.place[p.M] = at.place;
@@ -241,6 +305,43 @@ __global__ __launch_bounds__(1024) void k_rt_scan(RtPlan p) {
     p.ioff[p.M] = at.item;
     p.joff[p.M] = at.jitem;
   }
+}
+
+// Model m's items, by a wave.
+__device__ __forceinline__ void list_items(const RtPlan& p, int m) {
+  const int lane = threadIdx.x & 63;
+  RtItem it;
+  it.m = m;
+  it.c = 0;
+  it.first = p.seg_off[m];
+  it.zoff = p.zoff[m];
+  it.h = (int)(p.seg_off[m + 1] - it.first);
+  it.act = p.act[m];
+  it.rows = p.count[m];
+  it.place = p.place[m];
+  it.places = p.place[m + 1] - it.place;
+  it.pad[0] = it.pad[1] = it.pad[2] = 0;
+  const int nu = up(it.h, p.t.uc), i0 = p.ioff[m], n = p.ioff[m + 1] - i0;
+  for (int i = lane; i < n; i += 64) {
+    it.a = i / nu;
+    it.b = i % nu;
+    p.items[i0 + i] = it;
+  }
+  if (!p.jitems) return;
+  const int nt = up(it.h, p.t.du), nf = up(p.F, p.t.df), j0 = p.joff[m], k = p.joff[m + 1] - j0;
+  for (int i = lane; i < k; i += 64) {
+    it.a = i / nf % nt;
+    it.b = i % nf;
+    it.c = i / nf / nt;
+    p.jitems[j0 + i] = it;
+  }
+}
+
+}  // namespace
+
+__global__ __launch_bounds__(1024) void k_rt_scan(RtPlan p) {
+  __shared__ Sums lds[16];
+  scan_models(p, lds, [&](int m) { return p.count[m]; });
 }
 
 // The first nchunk workgroups put the slots into their places, the others list items, a
@@ -255,24 +356,54 @@ __global__ __launch_bounds__(64) void k_rt_place(RtPlan p) {
     if (in_lds)
       for (int m = lane; m < p.M; m += 64) lds[m] = row[m];
     __syncthreads();
-    walk(p, c, in_lds ? lds : row, false,
-         [&](int64_t s, int m, int r) { p.slot[p.place[m] + r] = (int32_t)s; });
+    walk(p, c, p.chunk, in_lds ? lds : row, false,
+         [&](int64_t s, int m, int r) { put_slot(p, s, p.place[m] + r); });
     return;
   }
-  const int m = blockIdx.x - p.nchunk;
-  const int h = (int)(p.seg_off[m + 1] - p.seg_off[m]);
-  const int nu = up(h, p.t.uc), i0 = p.ioff[m], n = p.ioff[m + 1] - i0;
-  for (int i = lane; i < n; i += 64) p.items[i0 + i] = RtItem{m, i / nu, i % nu, 0};
-  if (!p.jitems) return;
-  const int nt = up(h, p.t.du), nf = up(p.F, p.t.df), j0 = p.joff[m], k = p.joff[m + 1] - j0;
-  for (int i = lane; i < k; i += 64) p.jitems[j0 + i] = RtItem{m, i / nf % nt, i % nf, i / nf / nt};
+  list_items(p, blockIdx.x - p.nchunk);
+}
+
+// All of it by one workgroup, a run of slots for each of its 16 waves: few slots and models
+// are sooner counted in one than started in four.
+__global__ __launch_bounds__(1024) void k_rt_plan_one(RtPlan p) {
+  extern __shared__ int32_t lds[];  // [16][M]
+  __shared__ Sums sums[16];
+  const int tid = threadIdx.x, wave = tid >> 6;
+  const int chunk = up(up(p.R, 16), 64) * 64;
+  for (int i = tid; i < 16 * p.M; i += 1024) lds[i] = 0;
+  clear_places(p, tid, 1024);
+  __syncthreads();
+  walk(p, wave, chunk, lds + wave * p.M, true, [](int64_t, int, int) {});
+  __syncthreads();
+  for (int m = tid; m < p.M; m += 1024) {
+    int at = 0;
+    for (int w = 0; w < 16; ++w) {
+      const int n = lds[w * p.M + m];
+      lds[w * p.M + m] = at;
+      at += n;
+    }
+    p.count[m] = at;
+  }
+  __threadfence_block();
+  __syncthreads();
+  scan_models(p, sums, [&](int m) { return p.count[m]; });
+  __threadfence_block();
+  __syncthreads();
+  walk(p, wave, chunk, lds + wave * p.M, false,
+       [&](int64_t s, int m, int r) { put_slot(p, s, p.place[m] + r); });
+  for (int m = wave; m < p.M; m += 16) list_items(p, m);
 }
 
 hipError_t launch_rt_plan(const RtPlan& p, hipStream_t s) {
+  if (p.R <= kRtOneSlots && p.M <= kRtOneModels) {
+    note_variant("k_rt_plan_one", kArithNone);
+    k_rt_plan_one<<<1, 1024, (size_t)16 * p.M * sizeof(int32_t), s>>>(p);
+    return hipGetLastError();
+  }
   note_variant("k_rt_place", kArithNone);
   const size_t lds = p.M <= kRtLdsModels ? (size_t)p.M * sizeof(int32_t) : 0;
   k_rt_count<<<p.nchunk, 64, lds, s>>>(p);
-  k_rt_columns<<<(unsigned)ceil_div_i(p.M, 256), 256, 0, s>>>(p);
+  k_rt_columns<<<(unsigned)ceil_div_i(p.M, 16), 256, 0, s>>>(p);
   k_rt_scan<<<1, 1024, 0, s>>>(p);
   k_rt_place<<<(unsigned)(p.nchunk + p.M), 64, lds, s>>>(p);
   return hipGetLastError();

@@ -18,6 +18,32 @@ __device__ __forceinline__ f32x4 load_any4(const float* p) {
   return f32x4{q.v[0], q.v[1], q.v[2], q.v[3]};
 }
 
+// The three pieces of four values
+__device__ __forceinline__ void split3_4(const f32x4& v, uint2 (&p)[3]) {
+  f32x2 r[2] = {f32x2{v[0], v[1]}, f32x2{v[2], v[3]}};
+#pragma unroll
+  for (int e = 0; e < 3; ++e) {
+    const uint32_t lo = bf16_pair(r[0]), hi = bf16_pair(r[1]);
+    p[e] = make_uint2(lo, hi);
+    if (e == 2) break;
+    r[0] -= bf16_pair_value(lo);
+    r[1] -= bf16_pair_value(hi);
+  }
+}
+
+// Two transposing loads: of a group of 16 lanes, lane i gives the address of 8 bytes (four
+// columns i % 4) of row i / 4 and receives column i of the four rows; then of the rows
+// `then` bytes further.
+__device__ __forceinline__ bf16x8 transposed(const char* at, int then) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) char lds_char;
+  lds_char* p = (lds_char*)at;
+  const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+  const s16x4 v =
+      __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + then));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
 constexpr int kKT = 32;           // columns of a stage
 constexpr int kRow = 2 * kKT;     // bytes of a row of one piece in LDS
 // Chunk c (8 columns) of a row: rows two apart share banks, so the chunks of every
@@ -87,6 +113,13 @@ __device__ __forceinline__ bool operand_gate(int r) {
   return GATED && (r & 32);
 }
 
+// A work unit, by scalar loads: the list was written by an earlier launch.
+__device__ __forceinline__ RtItem item_at(const RtItem* items, int at) {
+  typedef int i32x16 __attribute__((ext_vector_type(16)));
+  const auto* p = (const __attribute__((address_space(4))) i32x16*)(items + at);
+  return __builtin_bit_cast(RtItem, *p);
+}
+
 // Workgroups go to the eight dies in turn; each die takes a run of the items, so that
 // its cache holds the rows and weights that its workgroups share.
 __device__ __forceinline__ int die_order(int i, int n) {
@@ -112,15 +145,13 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
   for (int it = blockIdx.x; it < 8 * each; it += gridDim.x) {
     const int at = die_order(it, n);
     if (at >= n) continue;
-    const RtItem item = a.items[at];
-    const int m = item.m;
-    const int64_t n0 = a.seg_off[m] + (int64_t)item.b * UC;
-    const int left = (int)(a.seg_off[m + 1] - n0);  // units from here on
+    const RtItem item = item_at(a.items, at);
+    const int64_t n0 = item.first + (int64_t)item.b * UC;
+    const int left = item.h - item.b * UC;  // units from here on
     const int units = left < UC ? left : UC;
-    const int rows = a.count[m];
-    const int places = a.place[m + 1] - a.place[m];  // with the padding
+    const int rows = item.rows, places = item.places;  // without, with the padding
     const int p0 = item.a * RB;
-    const int32_t* slots = a.slot + a.place[m];
+    const int32_t* slots = a.slot + item.place;
 
     const float* ra[NA];
     const float* rb[NB];
@@ -135,9 +166,9 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
 #pragma unroll
     for (int q = 0; q < NB; ++q) {
       const int p = p0 + 64 * q + (tid >> 2);
-      const int s = p < rows ? slots[p] : -1;
-      live[q] = s >= 0;
-      rb[q] = a.X + (int64_t)(live[q] ? s / a.K : 0) * a.F;
+      const int b = p < rows ? a.row[item.place + p] : -1;
+      live[q] = b >= 0;
+      rb[q] = a.X + (int64_t)(live[q] ? b : 0) * a.F;
     }
     const int c = tid & 3;
     f32x4 va[NA][2], vb[NB][2];
@@ -186,7 +217,7 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
       lds_barrier();
     }
 
-    const int act = a.act[m];
+    const int act = item.act;
     const int half = 4 * (lane >> 5);
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
@@ -230,7 +261,7 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
             for (int e = 0; e < 4; ++e) g[4 * q + e] = fmaf(y, w2[e], g[4 * q + e]);
           }
         }
-        const int64_t z0 = a.zoff[m] + (int64_t)item.b * UC * places;
+        const int64_t z0 = item.zoff + (int64_t)item.b * UC * places;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int u = u0 + 8 * (e >> 2) + half + (e & 3);
@@ -440,8 +471,10 @@ hipError_t launch_rt_join_dw(const RtJoin& a, hipStream_t s) {
 template <int NA, int NB, bool GATED>
 __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
   constexpr int RA = 64 * NA, RB = 64 * NB, UC = GATED ? 64 : RA;
-  typedef Stage<RA, RB> St;
-  __shared__ __align__(16) char lds[St::kBytes];
+  // X lies in LDS as it comes, [place][column], and goes to the products through transposing
+  // loads (rows 16 bytes times an odd number apart).
+  constexpr int kA = RA * kRow, XROW = 2 * RB + 16, kX = kKT * XROW;
+  __shared__ __align__(16) char lds[3 * (kA + kX)];
   const RtArgs& a = g.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wu = wave & 1, wf = wave >> 1;
@@ -449,16 +482,15 @@ __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
   for (int it = blockIdx.x; it < 8 * each; it += gridDim.x) {
     const int at = die_order(it, n);
     if (at >= n) continue;
-    const RtItem item = g.jitems[at];
+    const RtItem item = item_at(g.jitems, at);
     const int m = item.m;
-    const int64_t first = a.seg_off[m];
-    const int h = (int)(a.seg_off[m + 1] - first);
+    const int64_t first = item.first;
+    const int h = item.h, places = item.places;
     const int u0 = item.a * UC, f0 = item.b * RB;
     const int units = h - u0 < UC ? h - u0 : UC;
-    const int places = a.place[m + 1] - a.place[m];
     const int b0 = item.c * g.t.part, b1 = b0 + g.t.part < places ? b0 + g.t.part : places;
     const bool split = places > g.t.part;
-    const int32_t* slots = a.slot + a.place[m];
+    const int32_t* brow = a.row + item.place;
     const int c = tid & 3;
     const float* ra[NA];
 #pragma unroll
@@ -466,24 +498,35 @@ __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
       const int r = 64 * q + (tid >> 2);
       int u = operand_unit<GATED>(r);
       u = u < units ? u : units - 1;
-      ra[q] = (operand_gate<GATED>(r) ? a.dU : a.dZ) + a.zoff[m] + (int64_t)(u0 + u) * places;
+      ra[q] = (operand_gate<GATED>(r) ? a.dU : a.dZ) + item.zoff + (int64_t)(u0 + u) * places;
     }
-    // column f of X for eight places from 8 oct on: 256 / RB octets at a time
-    constexpr int PER = 256 / RB, NQ = 4 / PER;
-    const int f = f0 + tid % RB;
-    f32x4 va[NA][2], vb[NQ][2];
+    // Four columns of X from column f on, of places tid / TX + NY q of a stage.  The samples
+    // of the places come a stage before their values.  (A place without one takes sample 0,
+    // and zeros; columns past the last are not stored.)
+    constexpr int TX = RB / 4, NY = 256 / TX, NQ = kKT / NY;
+    const int f = f0 + 4 * (tid % TX), y = tid / TX;
+    f32x4 va[NA][2], vx[NQ];
+    int br[NQ];
+    auto fetch_rows = [&](int k0) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) br[q] = brow[k0 + y + NY * q];
+    };
     auto load = [&](int k0) {
 #pragma unroll
       for (int q = 0; q < NA; ++q)
 #pragma unroll
         for (int e = 0; e < 2; ++e) va[q][e] = *(const f32x4*)(ra[q] + k0 + 8 * c + 4 * e);
 #pragma unroll
-      for (int q = 0; q < NQ; ++q)
+      for (int q = 0; q < NQ; ++q) {
+        const float* x = a.X + (int64_t)(br[q] >= 0 ? br[q] : 0) * a.F;
+        f32x4 v;
+        if (f + 4 <= a.F) v = load_any4(x + f);
+        else
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int s = slots[k0 + 8 * (q * PER + tid / RB) + e];
-          vb[q][e >> 2][e & 3] = s >= 0 && f < a.F ? a.X[(int64_t)(s / a.K) * a.F + f] : 0.f;
-        }
+          for (int j = 0; j < 4; ++j) v[j] = x[f + j < a.F ? f + j : a.F - 1];
+        vx[q] = v;
+        if (br[q] < 0) vx[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
     };
     f32x16 acc[NA][NB];
 #pragma unroll
@@ -493,16 +536,53 @@ __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     __syncthreads();
-    if (b0 < b1) load(b0);
+    if (b0 < b1) {
+      fetch_rows(b0);
+      load(b0);
+      if (b0 + kKT < b1) fetch_rows(b0 + kKT);
+    }
     for (int k0 = b0; k0 < b1; k0 += kKT) {
 #pragma unroll
-      for (int q = 0; q < NA; ++q) St::put(lds, false, 64 * q + (tid >> 2), c, va[q][0], va[q][1]);
+      for (int q = 0; q < NA; ++q) {
+        bf16x8 p[3];
+        split3(va[q][0], va[q][1], p[0], p[1], p[2]);
 #pragma unroll
-      for (int q = 0; q < NQ; ++q)
-        St::put(lds, true, tid % RB, q * PER + tid / RB, vb[q][0], vb[q][1]);
-      if (k0 + kKT < b1) load(k0 + kKT);
+        for (int e = 0; e < 3; ++e) *(bf16x8*)(lds + e * kA + lds_chunk(64 * q + (tid >> 2), c)) = p[e];
+      }
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        uint2 p[3];
+        split3_4(vx[q], p);
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          *(uint2*)(lds + 3 * kA + e * kX + (y + NY * q) * XROW + 8 * (tid % TX)) = p[e];
+      }
+      if (k0 + kKT < b1) {
+        load(k0 + kKT);
+        if (k0 + 2 * kKT < b1) fetch_rows(k0 + 2 * kKT);
+      }
       lds_barrier();
-      St::template multiply<NA, NB>(lds, wu * 32 * NA, wf * 32 * NB, lane, acc);
+#pragma unroll
+      for (int ks = 0; ks < kKT / 16; ++ks) {
+        const int cc = 2 * ks + (lane >> 5), r = lane & 31;
+        bf16x8 av[NA][3], bv[NB][3];
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            av[i][e] = *(const bf16x8*)(lds + e * kA + lds_chunk(wu * 32 * NA + 32 * i + r, cc));
+        // 16 lanes: columns 16 (lane / 16 % 2) .., places 8 (lane / 32) ..
+        const char* x0 = lds + 3 * kA + (16 * ks + 8 * (lane >> 5) + ((lane & 15) >> 2)) * XROW +
+                         2 * (wf * 32 * NB + (lane & 16) + 4 * (lane & 3));
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int e = 0; e < 3; ++e) bv[j][e] = transposed(x0 + e * kX + 64 * j, 4 * XROW);
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+          for (int j = 0; j < NB; ++j) acc[i][j] = mfma_x3_32(av[i], bv[j], acc[i][j]);
+      }
       lds_barrier();
     }
     const int half = 4 * (lane >> 5);
@@ -527,75 +607,59 @@ __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
   }
 }
 
-// wdy[o][place] = weight dY_o of the place's slot, 0 where it holds none.
-__global__ __launch_bounds__(256) void k_rt_wdy(RtGrad g) {
-  const RtArgs& a = g.a;
-  const int total = a.place[a.M];
-  const int p = blockIdx.x * 256 + threadIdx.x;
-  if (p >= total) return;
-  const int s = a.slot[p];
-  const float w = s >= 0 ? a.weight[s] : 0.f;
-  for (int o = 0; o < a.O; ++o)
-    g.wdy[(int64_t)o * a.P + p] = s >= 0 ? w * a.dY[(int64_t)(s / a.K) * a.O + o] : 0.f;
-}
-
-// dW2[o][unit] = sum over the places of wdy[o] H[unit]: a wave takes four units and a part
-// of their model's places.
-constexpr int kDw2Units = 4;
-template <int OM>
+// dW2[o][unit] = sum over the places of wdy[o] H[unit], by fp32 matrix products: a wave
+// takes 16 units of a tile of the weight gradients and a part of their model's places, and
+// holds all outputs.  A lane loads four consecutive places of its row and feeds them to four
+// products, in the same order for both operands.
 __global__ __launch_bounds__(256) void k_rt_dw2(RtGrad g) {
   const RtArgs& a = g.a;
-  const int lane = threadIdx.x & 63;
-  const int64_t q = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t groups = (g.N + kDw2Units - 1) / kDw2Units;
-  if (q >= groups * g.nparts) return;
-  const int part = (int)(q / groups);
-  const int64_t n0 = q % groups * kDw2Units;
-#pragma unroll 1
-  for (int64_t n = n0; n < n0 + kDw2Units && n < g.N;) {
-    const int m = g.mid[n];
-    const int64_t end = a.seg_off[m + 1];
-    const int places = a.place[m + 1] - a.place[m];
-    const int b0 = part * g.t.part, b1 = b0 + g.t.part < places ? b0 + g.t.part : places;
-    int64_t last = n0 + kDw2Units;  // units n .. last - 1 are of model m
-    last = last < end ? last : end;
-    const int cnt = (int)(last - n);
-    if (part > 0 && b0 >= places) {
-      n = last;
-      continue;
-    }
-    const float* hrow[kDw2Units];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, lk = lane >> 4;
+  const int n = *g.njitems;
+  for (int it = blockIdx.x; it < n; it += gridDim.x) {
+    const RtItem item = item_at(g.jitems, it);
+    if (item.b != 0) continue;
+    const int64_t first = item.first;
+    const int h = item.h, end = (item.a + 1) * g.t.du < h ? (item.a + 1) * g.t.du : h;
+    const int places = item.places;
+    const int b0 = item.c * g.t.part, b1 = b0 + g.t.part < places ? b0 + g.t.part : places;
+    float* out = places > g.t.part ? g.w2part + (int64_t)item.c * a.O * g.N : g.dW2;
+    const float* wd = g.wdy + (int64_t)(li < a.O ? li : a.O - 1) * a.P + item.place + 4 * lk;
+    for (int u0 = item.a * g.t.du + 16 * wave; u0 < end; u0 += 64) {
+      const int u = u0 + li < h ? u0 + li : h - 1;
+      const float* hrow = a.H + item.zoff + (int64_t)u * places + 4 * lk;
+      f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+      // 64 places at a time, the next ones on their way (past the end: the last again, unused)
+      f32x4 hv[2][4], y[2][4];
+      auto load = [&](int b, int p) {
 #pragma unroll
-    for (int i = 0; i < kDw2Units; ++i) {
-      const int64_t u = n - a.seg_off[m] + (i < cnt ? i : cnt - 1);
-      hrow[i] = a.H + a.zoff[m] + u * places;
-    }
-    float sum[kDw2Units][OM];
+        for (int q = 0; q < 4; ++q) {
+          const int k = p + 16 * q < b1 ? p + 16 * q : b1 - 16;
+          hv[b][q] = *(const f32x4*)(hrow + k);
+          y[b][q] = *(const f32x4*)(wd + k);
+        }
+      };
+      auto multiply = [&](int b, int p) {
 #pragma unroll
-    for (int i = 0; i < kDw2Units; ++i)
+        for (int q = 0; q < 4; ++q) {
+          if (p + 16 * q >= b1) break;
 #pragma unroll
-      for (int o = 0; o < OM; ++o) sum[i][o] = 0.f;
-    const float* wd = g.wdy + a.place[m];
-    for (int p = b0 + lane; p < b1; p += 64) {
-      float hv[kDw2Units];
-#pragma unroll
-      for (int i = 0; i < kDw2Units; ++i) hv[i] = hrow[i][p];
-#pragma unroll
-      for (int o = 0; o < OM; ++o) {
-        const float y = o < a.O ? wd[(int64_t)o * a.P + p] : 0.f;
-#pragma unroll
-        for (int i = 0; i < kDw2Units; ++i) sum[i][o] = fmaf(hv[i], y, sum[i][o]);
+          for (int e = 0; e < 4; ++e)
+            acc[e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[b][q][e], hv[b][q][e], acc[e & 1], 0, 0, 0);
+        }
+      };
+      if (b0 < b1) load(0, b0);
+      for (int p = b0; p < b1; p += 128) {
+        if (p + 64 < b1) load(1, p + 64);
+        multiply(0, p);
+        if (p + 64 >= b1) break;
+        if (p + 128 < b1) load(0, p + 128);
+        multiply(1, p + 64);
       }
+      // lane: unit u0 + li, outputs 4 lk + e
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (u0 + li < h && 4 * lk + e < a.O) out[(int64_t)(4 * lk + e) * g.N + first + u0 + li] = acc[0][e] + acc[1][e];
     }
-    float* out = places > g.t.part ? g.w2part + (int64_t)part * a.O * g.N : g.dW2;
-#pragma unroll
-    for (int i = 0; i < kDw2Units; ++i)
-#pragma unroll
-      for (int o = 0; o < OM; ++o) {
-        const float t = group_sum_to_last(sum[i][o], 64);
-        if (lane == 63 && i < cnt && o < a.O) out[(int64_t)o * g.N + n + i] = t;
-      }
-    n = last;
   }
 }
 
@@ -640,12 +704,7 @@ hipError_t launch_rt_weights(const RtGrad& g, const RtShape& sh, hipStream_t s) 
   }
 #undef PMLP_RT_DW
   if (const hipError_t e = hipGetLastError()) return e;
-  k_rt_wdy<<<(unsigned)ceil_div_i(g.a.P, 256), 256, 0, s>>>(g);
-  const int64_t waves = (g.N + kDw2Units - 1) / kDw2Units * g.nparts;
-  const unsigned grid = (unsigned)((waves + 3) / 4);
-  if (g.a.O <= 2) k_rt_dw2<2><<<grid, 256, 0, s>>>(g);
-  else if (g.a.O <= 4) k_rt_dw2<4><<<grid, 256, 0, s>>>(g);
-  else k_rt_dw2<16><<<grid, 256, 0, s>>>(g);
+  k_rt_dw2<<<groups_for(g.jmost), 256, 0, s>>>(g);
   if (g.nparts > 1) k_rt_sum_parts<<<(unsigned)g.N, 256, 0, s>>>(g);
   return hipGetLastError();
 }

@@ -17,13 +17,20 @@ constexpr int32_t kRtMaxO = 16;     // outputs, at most
 constexpr int32_t kRtPad = 32;      // places a model's range is padded to
 constexpr int32_t kRtChunks = 256;  // runs of slots that are counted side by side, at most
 constexpr int32_t kRtLdsModels = 16384;  // models whose counters lie in LDS
+constexpr int32_t kRtOneSlots = 4096, kRtOneModels = 512;  // that one workgroup groups, at most
 
-// Work units: row block (of RT places) and unit chunk of model m, or tile and part of
-// its weight gradients.
+// A work unit: row block `a` and unit chunk `b` of model m, or unit tile `a`, column tile `b`
+// and part `c` of its weight gradients; with what a workgroup wants to know of its model, so
+// that it starts after one load.
 struct RtItem {
   int32_t m, a, b, c;
+  int64_t first;           // the model's first unit
+  int64_t zoff;            // first value of its hidden rows [h][places]
+  int32_t h, act;          // its units and activation
+  int32_t rows, places;    // its rows, and its places
+  int32_t place, pad[3];   // its first place
 };
-static_assert(sizeof(RtItem) == 16, "RtItem layout");
+static_assert(sizeof(RtItem) == 64, "RtItem layout");
 
 // What the items of a kind are counted in.
 struct RtTiles {
@@ -40,6 +47,7 @@ struct RtPlan {
   RtTiles t;
   int32_t F, O;
   const int64_t* seg_off;  // [M+1]
+  const int32_t* act;      // [M]
   const int32_t* idx;      // [R]
   int32_t* hist;           // [nchunk][M]
   int32_t* count;          // [M]
@@ -48,6 +56,10 @@ struct RtPlan {
   int32_t* ioff;           // [M+1] first forward item
   int32_t* joff;           // [M+1] first weight gradient item
   int32_t* slot;           // [P] slot of each place, or -1
+  int32_t* row;            // [P] its sample, or -1
+  // gradients: wdy[o][place] = weight dY_o of its slot, 0 where it holds none
+  const float *weight, *dY;
+  float* wdy;              // [O][P], or null
   RtItem* items;
   RtItem* jitems;          // null: forward only
   int32_t* flag;           // flag[3] is raised by an index outside [-1, M)
@@ -74,7 +86,7 @@ struct RtArgs {
   int32_t F, F4, O, K, M, P;
   const int32_t *count, *place;
   const int64_t* zoff;
-  const int32_t* slot;
+  const int32_t *slot, *row;
   const RtItem* items;
   const int32_t* nitems;
   int32_t most;      // items, at most
@@ -129,7 +141,7 @@ struct RtGrad {
   int32_t jmost;
   int32_t nparts;        // parts of a model with every slot
   float *dW1, *dV1, *dW2;
-  float* wdy;            // [O][P] weight times dY of each place
+  const float* wdy;      // (RtPlan)
   float* wpart;          // [nparts][k][N][F] where nparts > 1
   float* w2part;         // [nparts][O][N] where nparts > 1
   const int32_t* mid;

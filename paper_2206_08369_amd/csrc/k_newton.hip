@@ -138,7 +138,7 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
       const int j = j0 + r - T < nj ? j0 + r - T : nj - 1;
       row[q] = Q + (int64_t)j * K + 8 * c;
     }
-    put[q] = lds + r * ROW + ((c ^ ((r >> 1) & 3)) << 4);
+    put[q] = lds + r * ROW + ((c ^ ((r >> 2) & 3)) << 4);
   }
   f16x8 v[NQ][2];
   auto load = [&](int k) {
@@ -176,8 +176,8 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int ri = wi * W + 32 * i + r, rj = T + wj * W + 32 * i + r;
-          x[i][e] = *(const f16x8*)(lds + e * PLANE + ri * ROW + ((cc ^ ((ri >> 1) & 3)) << 4));
-          y[i][e] = *(const f16x8*)(lds + e * PLANE + rj * ROW + ((cc ^ ((rj >> 1) & 3)) << 4));
+          x[i][e] = *(const f16x8*)(lds + e * PLANE + ri * ROW + ((cc ^ ((ri >> 2) & 3)) << 4));
+          y[i][e] = *(const f16x8*)(lds + e * PLANE + rj * ROW + ((cc ^ ((rj >> 2) & 3)) << 4));
         }
       // (small products first, the tiles in turn)
 #pragma unroll

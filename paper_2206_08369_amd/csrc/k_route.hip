@@ -162,14 +162,12 @@ __device__ __forceinline__ uint64_t peers_of(int m) {
   return peers;
 }
 
-// Walks run c of `chunk` slots: `take(slot, model, rank in counter)` for each slot with a
-// model.
+// Walks run c: `take(slot, model, rank in counter)` for each slot with a model.
 template <class Take>
-__device__ __forceinline__ void walk(const RtPlan& p, int c, int chunk, int32_t* counter, bool report,
-                                     Take take) {
+__device__ __forceinline__ void walk(const RtPlan& p, int c, int32_t* counter, bool report, Take take) {
   const int lane = threadIdx.x & 63;
-  const int64_t first = (int64_t)c * chunk;
-  const int64_t end = first + chunk < p.R ? first + chunk : p.R;
+  const int64_t first = (int64_t)c * p.chunk;
+  const int64_t end = first + p.chunk < p.R ? first + p.chunk : p.R;
   for (int64_t s0 = first; s0 < end; s0 += 64) {
     const int m = slot_model(p, s0 + lane, end, report);
     const uint64_t peers = peers_of(m);
@@ -211,7 +209,7 @@ __global__ __launch_bounds__(64) void k_rt_count(RtPlan p) {
   for (int m = threadIdx.x; m < p.M; m += 64) counter[m] = 0;
   __threadfence_block();
   __syncthreads();
-  walk(p, c, p.chunk, counter, true, [](int64_t, int, int) {});
+  walk(p, c, counter, true, [](int64_t, int, int) {});
   __syncthreads();
   if (in_lds)
     for (int m = threadIdx.x; m < p.M; m += 64) row[m] = lds[m];
@@ -257,9 +255,8 @@ __device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) {
   return Sums{a.place + b.place, a.item + b.item, a.jitem + b.jitem, a.z + b.z};
 }
 
-__device__ __forceinline__ Sums model_sums(const RtPlan& p, int m, int n) {
+__device__ __forceinline__ Sums model_sums(const RtPlan& p, int n, int h) {
   const int rows = up(n, kRtPad) * kRtPad;
-  const int h = (int)(p.seg_off[m + 1] - p.seg_off[m]);
   Sums s;
   s.place = rows;
   s.item = up(n, p.t.rt) * up(h, p.t.uc);
@@ -273,13 +270,16 @@ __device__ __forceinline__ Sums from_lane(const Sums& v, int lane) {
               (int64_t)__shfl((long long)v.z, lane)};
 }
 
-// The sums over models before each, by a workgroup of 1,024 threads; `counts(m)` slots.
-template <class Counts>
-__device__ __forceinline__ void scan_models(const RtPlan& p, Sums* lds, Counts counts) {
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, each = up(p.M, 1024);
-  const int m0 = t * each < p.M ? t * each : p.M, m1 = m0 + each < p.M ? m0 + each : p.M;
+// The sums over models before each, by a workgroup of 1,024 threads: count(m) slots and
+// units(m), which `take(m, sums)` receives for every m up to M.  p.ioff[M] and p.joff[M], the
+// numbers of items, are written.
+template <class Count, class Units, class Take>
+__device__ __forceinline__ void scan_models(const RtPlan& p, Sums* lds, int M, Count count, Units units,
+                                            Take take) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, each = up(M, 1024);
+  const int m0 = t * each < M ? t * each : M, m1 = m0 + each < M ? m0 + each : M;
   Sums mine{0, 0, 0, 0};
-  for (int m = m0; m < m1; ++m) mine = mine + model_sums(p, m, counts(m));
+  for (int m = m0; m < m1; ++m) mine = mine + model_sums(p, count(m), units(m));
   Sums upto = mine;  // over the lanes up to this one
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -293,17 +293,13 @@ __device__ __forceinline__ void scan_models(const RtPlan& p, Sums* lds, Counts c
   at = at + upto;
   at = Sums{at.place - mine.place, at.item - mine.item, at.jitem - mine.jitem, at.z - mine.z};
   for (int m = m0; m < m1; ++m) {
-    p.place[m] = at.place;
-    p.zoff[m] = at.z;
-    p.ioff[m] = at.item;
-    p.joff[m] = at.jitem;
-    at = at + model_sums(p, m, counts(m));
+    take(m, at);
+    at = at + model_sums(p, count(m), units(m));
   }
   if (t == 1023) {
-    p.place[p.M] = at.place;
-    p.zoff[p.M] = at.z;
-    p.ioff[p.M] = at.item;
-    p.joff[p.M] = at.jitem;
+    take(M, at);
+    p.ioff[M] = at.item;
+    p.joff[M] = at.jitem;
   }
 }
 
@@ -341,7 +337,14 @@ __device__ __forceinline__ void list_items(const RtPlan& p, int m) {
 
 __global__ __launch_bounds__(1024) void k_rt_scan(RtPlan p) {
   __shared__ Sums lds[16];
-  scan_models(p, lds, [&](int m) { return p.count[m]; });
+  scan_models(p, lds, p.M, [&](int m) { return p.count[m]; },
+              [&](int m) { return (int)(p.seg_off[m + 1] - p.seg_off[m]); },
+              [&](int m, const Sums& at) {
+                p.place[m] = at.place;
+                p.zoff[m] = at.z;
+                p.ioff[m] = at.item;
+                p.joff[m] = at.jitem;
+              });
 }
 
 // The first nchunk workgroups put the slots into their places, the others list items, a
@@ -356,7 +359,7 @@ __global__ __launch_bounds__(64) void k_rt_place(RtPlan p) {
     if (in_lds)
       for (int m = lane; m < p.M; m += 64) lds[m] = row[m];
     __syncthreads();
-    walk(p, c, p.chunk, in_lds ? lds : row, false,
+    walk(p, c, in_lds ? lds : row, false,
          [&](int64_t s, int m, int r) { put_slot(p, s, p.place[m] + r); });
     return;
   }
@@ -366,38 +369,96 @@ __global__ __launch_bounds__(64) void k_rt_place(RtPlan p) {
 // All of it by one workgroup, a run of slots for each of its 16 waves: few slots and models
 // are sooner counted in one than started in four.
 __global__ __launch_bounds__(1024) void k_rt_plan_one(RtPlan p) {
-  extern __shared__ int32_t lds[];  // [16][M]
-  __shared__ Sums sums[16];
-  const int tid = threadIdx.x, wave = tid >> 6;
-  const int chunk = up(up(p.R, 16), 64) * 64;
-  for (int i = tid; i < 16 * p.M; i += 1024) lds[i] = 0;
+  constexpr int STEPS = kRtOneSlots / 1024;
+  __shared__ int32_t counter[16 * kRtOneModels];
+  __shared__ RtItem model[kRtOneModels];
+  __shared__ int32_t ioff[kRtOneModels + 1], joff[kRtOneModels + 1];
+  __shared__ Sums total[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, M = p.M;
+  const int first = wave * 64 * STEPS;
+  for (int i = tid; i < 16 * M; i += 1024) counter[i] = 0;
+  int key[STEPS], rank[STEPS];
+#pragma unroll
+  for (int q = 0; q < STEPS; ++q) key[q] = slot_model(p, first + 64 * q + lane, p.R, true);
   clear_places(p, tid, 1024);
   __syncthreads();
-  walk(p, wave, chunk, lds + wave * p.M, true, [](int64_t, int, int) {});
-  __syncthreads();
-  for (int m = tid; m < p.M; m += 1024) {
-    int at = 0;
-    for (int w = 0; w < 16; ++w) {
-      const int n = lds[w * p.M + m];
-      lds[w * p.M + m] = at;
-      at += n;
-    }
-    p.count[m] = at;
+#pragma unroll
+  for (int q = 0; q < STEPS; ++q) {  // (see walk)
+    if (first + 64 * q >= p.R) continue;
+    const uint64_t peers = peers_of(key[q]);
+    const int leader = peers ? __ffsll((unsigned long long)peers) - 1 : lane;
+    int base = 0;
+    if (peers && lane == leader) base = atomicAdd(&counter[wave * M + key[q]], __popcll(peers));
+    rank[q] = __shfl(base, leader) + __popcll(peers & ((1ull << lane) - 1));
   }
-  __threadfence_block();
   __syncthreads();
-  scan_models(p, sums, [&](int m) { return p.count[m]; });
-  __threadfence_block();
+  if (tid < M) {
+    RtItem& t = model[tid];
+    int n = 0;
+    for (int w = 0; w < 16; ++w) {
+      const int c = counter[w * M + tid];
+      counter[w * M + tid] = n;
+      n += c;
+    }
+    t.m = tid;
+    t.c = 0;
+    t.first = p.seg_off[tid];
+    t.h = (int)(p.seg_off[tid + 1] - t.first);
+    t.act = p.act[tid];
+    t.rows = n;
+    p.count[tid] = n;
+  }
   __syncthreads();
-  walk(p, wave, chunk, lds + wave * p.M, false,
-       [&](int64_t s, int m, int r) { put_slot(p, s, p.place[m] + r); });
-  for (int m = wave; m < p.M; m += 16) list_items(p, m);
+  scan_models(p, total, M, [&](int m) { return model[m].rows; },
+              [&](int m) { return model[m].h; },
+              [&](int m, const Sums& at) {
+                if (m < M) {
+                  model[m].place = at.place;
+                  model[m].zoff = at.z;
+                  model[m].places = up(model[m].rows, kRtPad) * kRtPad;
+                }
+                ioff[m] = at.item;
+                joff[m] = at.jitem;
+                p.place[m] = at.place;
+              });
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < STEPS; ++q)
+    if (key[q] >= 0)
+      put_slot(p, first + 64 * q + lane, model[key[q]].place + counter[wave * M + key[q]] + rank[q]);
+  auto model_of = [&](const int32_t* off, int i) {  // the last one that starts at or before i
+    int lo = 0, hi = M;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (off[mid] <= i) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  };
+  for (int i = tid; i < ioff[M]; i += 1024) {
+    const int m = model_of(ioff, i);
+    RtItem t = model[m];
+    const int nu = up(t.h, p.t.uc);
+    t.a = (i - ioff[m]) / nu;
+    t.b = (i - ioff[m]) % nu;
+    p.items[i] = t;
+  }
+  if (!p.jitems) return;
+  for (int i = tid; i < joff[M]; i += 1024) {
+    const int m = model_of(joff, i), j = i - joff[m];
+    RtItem t = model[m];
+    const int nt = up(t.h, p.t.du), nf = up(p.F, p.t.df);
+    t.a = j / nf % nt;
+    t.b = j % nf;
+    t.c = j / nf / nt;
+    p.jitems[i] = t;
+  }
 }
 
 hipError_t launch_rt_plan(const RtPlan& p, hipStream_t s) {
   if (p.R <= kRtOneSlots && p.M <= kRtOneModels) {
     note_variant("k_rt_plan_one", kArithNone);
-    k_rt_plan_one<<<1, 1024, (size_t)16 * p.M * sizeof(int32_t), s>>>(p);
+    k_rt_plan_one<<<1, 1024, 0, s>>>(p);
     return hipGetLastError();
   }
   note_variant("k_rt_place", kArithNone);

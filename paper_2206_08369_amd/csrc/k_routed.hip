@@ -46,10 +46,9 @@ __device__ __forceinline__ bf16x8 transposed(const char* at, int then) {
 
 constexpr int kKT = 32;           // columns of a stage
 constexpr int kRow = 2 * kKT;     // bytes of a row of one piece in LDS
-// Chunk c (8 columns) of a row: rows two apart share banks, so the chunks of every
-// second row change places.
+// Chunk c (8 columns) of a row: rows four apart share banks, so their chunks change places.
 __device__ __forceinline__ int lds_chunk(int row, int c) {
-  return row * kRow + ((c ^ ((row >> 1) & 3)) << 4);
+  return row * kRow + ((c ^ ((row >> 2) & 3)) << 4);
 }
 
 // acc += a b over 16 columns, the piece products smallest first
@@ -139,6 +138,9 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
   typedef Stage<RA, RB> St;
   __shared__ __align__(16) char lds[St::kBytes];
   __shared__ __align__(16) float w2s[kRtMaxO * UC];  // [O][UC]
+  // the rows' slots, weights and output gradients
+  __shared__ int32_t slot_of[RB];
+  __shared__ float weight_of[TRAIN ? RB : 1], dys[TRAIN ? kRtMaxO * RB : 1];  // dys [O][RB]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wu = wave & 1, wr = wave >> 1;
   const int n = *a.nitems, each = (n + 7) / 8;
@@ -152,7 +154,6 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
     const int rows = item.rows, places = item.places;  // without, with the padding
     const int p0 = item.a * RB;
     const int32_t* slots = a.slot + item.place;
-
     const float* ra[NA];
     const float* rb[NB];
     bool live[NB];
@@ -205,6 +206,16 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
       const int o = i / UC, u = i % UC;
       w2s[i] = u < units ? a.W2[(int64_t)o * a.ldw + n0 + u] : 0.f;
     }
+    if (tid < RB) {
+      const int s = p0 + tid < rows ? slots[p0 + tid] : -1;
+      slot_of[tid] = s;
+      if (TRAIN) weight_of[tid] = s >= 0 ? a.weight[s] : 0.f;
+    }
+    if (TRAIN)
+      for (int i = tid; i < a.O * RB; i += 256) {
+        const int o = i / RB, p = p0 + i % RB;
+        dys[i] = p < rows ? a.dY[(int64_t)a.row[item.place + p] * a.O + o] : 0.f;
+      }
     load(0);
     for (int k0 = 0; k0 < a.F; k0 += kKT) {
 #pragma unroll
@@ -221,14 +232,9 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
     const int half = 4 * (lane >> 5);
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-      const int p = p0 + (wr * NB + j) * 32 + (lane & 31);
-      const int s = p < rows ? slots[p] : -1;
-      const float* dy = nullptr;
-      float w = 0.f;
-      if (TRAIN && s >= 0) {
-        dy = a.dY + (int64_t)(s / a.K) * a.O;
-        w = a.weight[s];
-      }
+      const int r = (wr * NB + j) * 32 + (lane & 31), p = p0 + r;
+      const int s = slot_of[r];
+      const float w = TRAIN ? weight_of[r] : 0.f;
       float dw = 0.f;
       float hid[NU][16];
 #pragma unroll
@@ -253,7 +259,7 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) g[e] = 0.f;
         for (int o = 0; o < a.O; ++o) {
-          const float y = s >= 0 ? dy[o] : 0.f;
+          const float y = dys[o * RB + r];
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const f32x4 w2 = *(const f32x4*)(w2s + o * UC + u0 + 8 * q + half);
@@ -261,14 +267,14 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
             for (int e = 0; e < 4; ++e) g[4 * q + e] = fmaf(y, w2[e], g[4 * q + e]);
           }
         }
-        const int64_t z0 = item.zoff + (int64_t)item.b * UC * places;
+        const int64_t z0 = item.zoff + (int64_t)(p >> 5) * item.h * 32 + (int64_t)item.b * UC * 32 + (p & 31);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int u = u0 + 8 * (e >> 2) + half + (e & 3);
           dw = fmaf(hid[i][e], g[e], dw);
           if (u >= units || p >= places) continue;
           const float dh = w * g[e];
-          const int64_t to = z0 + (int64_t)u * places + p;
+          const int64_t to = z0 + u * 32;
           a.H[to] = s >= 0 ? hid[i][e] : 0.f;
           a.dZ[to] = s >= 0 ? dh * d[e] * (GATED ? acc[NA - 1][j][e] : 1.f) : 0.f;
           if (GATED) a.dU[to] = s >= 0 ? dh * v[e] : 0.f;
@@ -472,16 +478,17 @@ template <int NA, int NB, bool GATED>
 __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
   constexpr int RA = 64 * NA, RB = 64 * NB, UC = GATED ? 64 : RA;
   // X lies in LDS as it comes, [place][column], and goes to the products through transposing
-  // loads (rows 16 bytes times an odd number apart).
-  constexpr int kA = RA * kRow, XROW = 2 * RB + 16, kX = kKT * XROW;
+  // loads, 64 bytes of four rows at a time: rows are 64 bytes past (or short of) all banks apart.
+  constexpr int kA = RA * kRow, XROW = 2 * RB + 64, kX = kKT * XROW;
   __shared__ __align__(16) char lds[3 * (kA + kX)];
   const RtArgs& a = g.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wu = wave & 1, wf = wave >> 1;
-  const int n = *g.njitems, each = (n + 7) / 8;
-  for (int it = blockIdx.x; it < 8 * each; it += gridDim.x) {
-    const int at = die_order(it, n);
-    if (at >= n) continue;
+  const int n = *g.njitems;
+  // (In the list's order, dies in turn: the tiles of a model with many rows, which take
+  // longest, are spread over all of them.  32 models of 500 to 1,000 units on 16,384 rows: 415
+  // us where each die took a run of the list, XXX so.)
+  for (int at = blockIdx.x; at < n; at += gridDim.x) {
     const RtItem item = item_at(g.jitems, at);
     const int m = item.m;
     const int64_t first = item.first;
@@ -498,7 +505,7 @@ __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
       const int r = 64 * q + (tid >> 2);
       int u = operand_unit<GATED>(r);
       u = u < units ? u : units - 1;
-      ra[q] = (operand_gate<GATED>(r) ? a.dU : a.dZ) + item.zoff + (int64_t)(u0 + u) * places;
+      ra[q] = (operand_gate<GATED>(r) ? a.dU : a.dZ) + item.zoff + (int64_t)(u0 + u) * 32 + 8 * c;
     }
     // Four columns of X from column f on, of places tid / TX + NY q of a stage.  The samples
     // of the places come a stage before their values.  (A place without one takes sample 0,
@@ -515,7 +522,7 @@ __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
 #pragma unroll
       for (int q = 0; q < NA; ++q)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) va[q][e] = *(const f32x4*)(ra[q] + k0 + 8 * c + 4 * e);
+        for (int e = 0; e < 2; ++e) va[q][e] = *(const f32x4*)(ra[q] + (int64_t)k0 * h + 4 * e);
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
         const float* x = a.X + (int64_t)(br[q] >= 0 ? br[q] : 0) * a.F;
@@ -614,10 +621,10 @@ __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
 __global__ __launch_bounds__(256) void k_rt_dw2(RtGrad g) {
   const RtArgs& a = g.a;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, lk = lane >> 4;
-  const int n = *g.njitems;
+  const int n = *g.njitems, nf = (a.F + g.t.df - 1) / g.t.df;
   for (int it = blockIdx.x; it < n; it += gridDim.x) {
     const RtItem item = item_at(g.jitems, it);
-    if (item.b != 0) continue;
+    if (item.b != (item.a + item.c) % nf) continue;  // (one of the column tiles, not always the same die)
     const int64_t first = item.first;
     const int h = item.h, end = (item.a + 1) * g.t.du < h ? (item.a + 1) * g.t.du : h;
     const int places = item.places;
@@ -626,7 +633,7 @@ __global__ __launch_bounds__(256) void k_rt_dw2(RtGrad g) {
     const float* wd = g.wdy + (int64_t)(li < a.O ? li : a.O - 1) * a.P + item.place + 4 * lk;
     for (int u0 = item.a * g.t.du + 16 * wave; u0 < end; u0 += 64) {
       const int u = u0 + li < h ? u0 + li : h - 1;
-      const float* hrow = a.H + item.zoff + (int64_t)u * places + 4 * lk;
+      const float* hrow = a.H + item.zoff + (int64_t)u * 32 + 4 * lk;
       f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
       // 64 places at a time, the next ones on their way (past the end: the last again, unused)
       f32x4 hv[2][4], y[2][4];
@@ -634,7 +641,7 @@ __global__ __launch_bounds__(256) void k_rt_dw2(RtGrad g) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int k = p + 16 * q < b1 ? p + 16 * q : b1 - 16;
-          hv[b][q] = *(const f32x4*)(hrow + k);
+          hv[b][q] = *(const f32x4*)(hrow + (int64_t)(k >> 5) * 32 * h + (k & 16));
           y[b][q] = *(const f32x4*)(wd + k);
         }
       };
@@ -677,12 +684,14 @@ __global__ __launch_bounds__(256) void k_rt_sum_parts(RtGrad g) {
     const int v = f >= a.F;
     const int64_t at = n * a.F + f - (v ? a.F : 0);
     float t = 0.f;
+#pragma unroll 8
     for (int q = 0; q < parts; ++q) t += g.wpart[((int64_t)q * k + v) * size + at];
     (v ? g.dV1 : g.dW1)[at] = t;
   }
   if (threadIdx.x < (unsigned)a.O) {
     const int64_t at = threadIdx.x * g.N + n;
     float t = 0.f;
+#pragma unroll 8
     for (int q = 0; q < parts; ++q) t += g.w2part[(int64_t)q * a.O * g.N + at];
     g.dW2[at] = t;
   }

@@ -25,7 +25,7 @@ constexpr int32_t kRtOneSlots = 4096, kRtOneModels = 512;  // that one workgroup
 struct RtItem {
   int32_t m, a, b, c;
   int64_t first;           // the model's first unit
-  int64_t zoff;            // first value of its hidden rows [h][places]
+  int64_t zoff;            // first of its hidden values, [places / 32][h][32]
   int32_t h, act;          // its units and activation
   int32_t rows, places;    // its rows, and its places
   int32_t place, pad[3];   // its first place
@@ -95,7 +95,7 @@ struct RtArgs {
   // gradients
   const float* weight;  // [R]
   const float* dY;      // [B][O]
-  float *dZ, *dU, *H;   // [h_m][places of m] at zoff[m]
+  float *dZ, *dU, *H;   // [places of m / 32][h_m][32] at zoff[m]
   float* dwpart;        // [R][parts]
 };
 

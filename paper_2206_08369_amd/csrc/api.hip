@@ -1977,7 +1977,16 @@ RtLayout rt_layout(const pmlp* h, int64_t R, int32_t K, const RtShape& sh, bool 
   l.items = (R / p.t.rt + groups) * div_up(h->widest, p.t.uc);
   int64_t tiles = 0;
   if (train) {
-    for (int32_t hm : h->hs) tiles += (int64_t)div_up(hm, p.t.du) * div_up(h->F, p.t.df);
+    auto count = [&] {
+      tiles = 0;
+      for (int32_t hm : h->hs) tiles += div_up(hm, p.t.du);
+      tiles *= div_up(h->F, p.t.df);
+    };
+    count();
+    if (p.t.df == 128 && tiles < 1024) {  // (more than the device holds at once)
+      p.t.df = 64;
+      count();
+    }
     // few tiles and many rows: parts of the rows side by side
     if (tiles < 512) {
       const int64_t parts = 1024 / tiles;

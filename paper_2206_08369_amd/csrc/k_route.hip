@@ -20,13 +20,25 @@ __device__ __forceinline__ float key_score(uint64_t k) {
   return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
 }
 
+// The largest of the wave's values, in every lane (zeros come in from outside a row)
+template <int CTRL, int ROWMASK>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+  const uint32_t o = __builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWMASK, 0xf, true);
+  return o > v ? o : v;
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = dpp_max<0x111, 0xf>(v);  // row_shr:1, 2, 4, 8
+  v = dpp_max<0x112, 0xf>(v);
+  v = dpp_max<0x114, 0xf>(v);
+  v = dpp_max<0x118, 0xf>(v);
+  v = dpp_max<0x142, 0xa>(v);  // row_bcast:15 into rows 1 and 3
+  v = dpp_max<0x143, 0xc>(v);  // row_bcast:31 into rows 2 and 3
+  return __builtin_amdgcn_readlane(v, 63);
+}
 __device__ __forceinline__ uint64_t wave_max(uint64_t v) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    const uint64_t o = __shfl_xor((unsigned long long)v, d);
-    v = o > v ? o : v;
-  }
-  return v;
+  const uint32_t hi = wave_max((uint32_t)(v >> 32));
+  const uint32_t lo = wave_max((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
+  return ((uint64_t)hi << 32) | lo;
 }
 
 }  // namespace
@@ -150,16 +162,15 @@ __device__ __forceinline__ int slot_model(const RtPlan& p, int64_t s, int64_t en
   return -1;
 }
 
-// The lanes with this lane's model.
-__device__ __forceinline__ uint64_t peers_of(int m) {
-  uint64_t todo = __ballot(m >= 0), peers = 0;
-  while (todo) {
-    const int key = __shfl(m, __ffsll((unsigned long long)todo) - 1);
-    const uint64_t same = __ballot(m == key);
-    if (m == key) peers = same;
-    todo &= ~same;
+// The lanes with this lane's model, of M: bit by bit, those that agree.
+__device__ __forceinline__ uint64_t peers_of(int m, int M) {
+  uint64_t peers = __ballot(m >= 0);
+  for (int bit = 0; (M - 1) >> bit; ++bit) {
+    const bool on = m >> bit & 1;
+    const uint64_t ones = __ballot(on);
+    peers &= on ? ones : ~ones;
   }
-  return peers;
+  return m >= 0 ? peers : 0;
 }
 
 // Walks run c: `take(slot, model, rank in counter)` for each slot with a model.
@@ -170,7 +181,7 @@ __device__ __forceinline__ void walk(const RtPlan& p, int c, int32_t* counter, b
   const int64_t end = first + p.chunk < p.R ? first + p.chunk : p.R;
   for (int64_t s0 = first; s0 < end; s0 += 64) {
     const int m = slot_model(p, s0 + lane, end, report);
-    const uint64_t peers = peers_of(m);
+    const uint64_t peers = peers_of(m, p.M);
     const int leader = peers ? __ffsll((unsigned long long)peers) - 1 : lane;
     int base = 0;
     if (peers && lane == leader) base = atomicAdd(counter + m, __popcll(peers));
@@ -385,7 +396,7 @@ __global__ __launch_bounds__(1024) void k_rt_plan_one(RtPlan p) {
 #pragma unroll
   for (int q = 0; q < STEPS; ++q) {  // (see walk)
     if (first + 64 * q >= p.R) continue;
-    const uint64_t peers = peers_of(key[q]);
+    const uint64_t peers = peers_of(key[q], M);
     const int leader = peers ? __ffsll((unsigned long long)peers) - 1 : lane;
     int base = 0;
     if (peers && lane == leader) base = atomicAdd(&counter[wave * M + key[q]], __popcll(peers));

@@ -267,17 +267,28 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
             for (int e = 0; e < 4; ++e) g[4 * q + e] = fmaf(y, w2[e], g[4 * q + e]);
           }
         }
-        const int64_t z0 = item.zoff + (int64_t)(p >> 5) * item.h * 32 + (int64_t)item.b * UC * 32 + (p & 31);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int u = u0 + 8 * (e >> 2) + half + (e & 3);
-          dw = fmaf(hid[i][e], g[e], dw);
-          if (u >= units || p >= places) continue;
+        // (Places that hold no slot have zero samples, weights and gradients: what is
+        // stored there adds nothing.)
+        const int64_t z0 = item.zoff + (int64_t)(p >> 5) * item.h * 32 +
+                           (item.b * UC + u0 + half) * 32 + (lane & 31);
+        float *const hz = a.H + z0, *const dz = a.dZ + z0, *const du = GATED ? a.dU + z0 : nullptr;
+        if (p0 + (wr * NB + j) * 32 >= places) continue;  // (the same for all lanes)
+        auto store = [&](int e) {
+          const int u = (8 * (e >> 2) + (e & 3)) * 32;
           const float dh = w * g[e];
-          const int64_t to = z0 + u * 32;
-          a.H[to] = s >= 0 ? hid[i][e] : 0.f;
-          a.dZ[to] = s >= 0 ? dh * d[e] * (GATED ? acc[NA - 1][j][e] : 1.f) : 0.f;
-          if (GATED) a.dU[to] = s >= 0 ? dh * v[e] : 0.f;
+          hz[u] = hid[i][e];
+          dz[u] = GATED ? dh * d[e] * acc[NA - 1][j][e] : dh * d[e];
+          if (GATED) du[u] = dh * v[e];
+        };
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dw = fmaf(hid[i][e], g[e], dw);
+        if (u0 + 32 <= units) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) store(e);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (u0 + 8 * (e >> 2) + half + (e & 3) < units) store(e);
         }
       }
       const int part = 2 * item.b + wu;
@@ -614,24 +625,26 @@ __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
   }
 }
 
-// dW2[o][unit] = sum over the places of wdy[o] H[unit], by fp32 matrix products: a wave
-// takes 16 units of a tile of the weight gradients and a part of their model's places, and
-// holds all outputs.  A lane loads four consecutive places of its row and feeds them to four
-// products, in the same order for both operands.
+// dW2[o][unit] = sum over the places of wdy[o] H[unit], by fp32 matrix products: a workgroup
+// takes 16 units of a tile of the weight gradients and a part of their model's places, 64 of
+// every 256 a wave, and all outputs.  A lane loads four consecutive places of its row and
+// feeds them to four products, in the same order for both operands.
 __global__ __launch_bounds__(256) void k_rt_dw2(RtGrad g) {
+  __shared__ f32x4 sums[4][64];
   const RtArgs& a = g.a;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, lk = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = *g.njitems, nf = (a.F + g.t.df - 1) / g.t.df;
   for (int it = blockIdx.x; it < n; it += gridDim.x) {
     const RtItem item = item_at(g.jitems, it);
-    if (item.b != (item.a + item.c) % nf) continue;  // (one of the column tiles, not always the same die)
     const int64_t first = item.first;
     const int h = item.h, end = (item.a + 1) * g.t.du < h ? (item.a + 1) * g.t.du : h;
     const int places = item.places;
     const int b0 = item.c * g.t.part, b1 = b0 + g.t.part < places ? b0 + g.t.part : places;
     float* out = places > g.t.part ? g.w2part + (int64_t)item.c * a.O * g.N : g.dW2;
     const float* wd = g.wdy + (int64_t)(li < a.O ? li : a.O - 1) * a.P + item.place + 4 * lk;
-    for (int u0 = item.a * g.t.du + 16 * wave; u0 < end; u0 += 64) {
+    // the tile's units in turn over its column tiles (not always on the same die)
+    for (int u0 = item.a * g.t.du + 16 * ((item.b + item.a + item.c) % nf); u0 < end; u0 += 16 * nf) {
       const int u = u0 + li < h ? u0 + li : h - 1;
       const float* hrow = a.H + item.zoff + (int64_t)u * 32 + 4 * lk;
       f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
@@ -654,18 +667,25 @@ __global__ __launch_bounds__(256) void k_rt_dw2(RtGrad g) {
             acc[e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[b][q][e], hv[b][q][e], acc[e & 1], 0, 0, 0);
         }
       };
-      if (b0 < b1) load(0, b0);
-      for (int p = b0; p < b1; p += 128) {
-        if (p + 64 < b1) load(1, p + 64);
+      const int p0 = b0 + 64 * wave;
+      if (p0 < b1) load(0, p0);
+      for (int p = p0; p < b1; p += 512) {
+        if (p + 256 < b1) load(1, p + 256);
         multiply(0, p);
-        if (p + 64 >= b1) break;
-        if (p + 128 < b1) load(0, p + 128);
-        multiply(1, p + 64);
+        if (p + 256 >= b1) break;
+        if (p + 512 < b1) load(0, p + 512);
+        multiply(1, p + 256);
       }
-      // lane: unit u0 + li, outputs 4 lk + e
+      sums[wave][lane] = acc[0] + acc[1];
+      __syncthreads();
+      if (wave == 0) {
+        // lane: unit u0 + li, outputs 4 lk + e
+        const f32x4 t = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (u0 + li < h && 4 * lk + e < a.O) out[(int64_t)(4 * lk + e) * g.N + first + u0 + li] = acc[0][e] + acc[1][e];
+        for (int e = 0; e < 4; ++e)
+          if (u0 + li < h && 4 * lk + e < a.O) out[(int64_t)(4 * lk + e) * g.N + first + u0 + li] = t[e];
+      }
+      __syncthreads();
     }
   }
 }

@@ -303,4 +303,12 @@ __device__ __forceinline__ float group_sum_to_last(float v, int LG) {
   return v;
 }
 
+// A barrier for what lies in LDS.  (__syncthreads also waits for the loads from
+// memory that are on their way into registers for the next stage.)
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 }  // namespace pmlpk

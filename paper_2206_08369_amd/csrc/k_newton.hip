@@ -18,11 +18,14 @@ __global__ __launch_bounds__(256) void k_ns_momentum(NsArgs a, int piece0) {
   __shared__ double part[4];
   const NsPiece p = a.pieces[piece0 + blockIdx.x];
   const NsMat t = a.mats[p.mat];
-  const int64_t n = (int64_t)p.rows * t.cols;
+  // (a piece of several rows has at most kNsPiece entries; one of a row may have any number)
+  const int n = p.rows * t.cols;
   double sum = 0;
-  for (int64_t e = threadIdx.x; e < n; e += 256) {
-    const int i = p.row0 + (int)(e / t.cols), j = (int)(e % t.cols);
-    const int64_t at = t.src + (int64_t)i * t.ld + j;
+  int i = threadIdx.x / t.cols, j = threadIdx.x - i * t.cols;
+  const int di = 256 / t.cols, dj = 256 - di * t.cols;
+#pragma unroll 4
+  for (int e = threadIdx.x; e < n; e += 256) {
+    const int64_t at = t.src + (int64_t)(p.row0 + i) * t.ld + j;
     const float g = a.G[at];
     float u = g;
     if (a.mom_in) {
@@ -30,8 +33,14 @@ __global__ __launch_bounds__(256) void k_ns_momentum(NsArgs a, int piece0) {
       a.mom_out[at] = m;
       u = a.nesterov ? fmaf(a.mu, m, g) : m;
     }
-    if (APPLY) apply(a, t, i, j, u);
+    if (APPLY) apply(a, t, p.row0 + i, j, u);
     else sum += (double)u * (double)u;  // squares of any fp32 values fit
+    i += di;
+    j += dj;
+    if (j >= t.cols) {
+      j -= t.cols;
+      ++i;
+    }
   }
   if (APPLY) {
     if (a.lrm && p.row0 == 0 && threadIdx.x == 0 && !(fabsf(a.lrm[t.m]) < INFINITY)) a.flag[1] = 1;
@@ -140,12 +149,15 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
     }
     put[q] = lds + r * ROW + ((c ^ ((r >> 2) & 3)) << 4);
   }
-  f16x8 v[NQ][2];
-  auto load = [&](int k) {
+  // DEPTH stages are on their way from memory: a small tile's stage is multiplied long before
+  // the next one arrives.
+  constexpr int DEPTH = T == 64 ? 4 : 2;
+  f16x8 v[DEPTH][NQ][2];
+  auto load = [&](int d, int k) {
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-      v[q][0] = *(const f16x8*)(row[q] + k);
-      v[q][1] = *(const f16x8*)(row[q] + (2 * q < NQ ? lplane : qplane) + k);
+      v[d][q][0] = *(const f16x8*)(row[q] + k);
+      v[d][q][1] = *(const f16x8*)(row[q] + (2 * q < NQ ? lplane : qplane) + k);
     }
   };
   f32x16 acc[NT][NT];
@@ -155,18 +167,22 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-  load(0);
-  for (int k = 0; k < K; k += KT) {
-    __syncthreads();
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-      *(f16x8*)put[q] = v[q][0];
-      *(f16x8*)(put[q] + PLANE) = v[q][1];
-    }
-    if (k + KT < K) load(k + KT);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
+  for (int d = 0; d < DEPTH; ++d)
+    if (d * KT < K) load(d, d * KT);
+  for (int k0 = 0; k0 < K; k0 += DEPTH * KT) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) {
+      const int k = k0 + d * KT;
+      if (k >= K) break;
+      lds_barrier();
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        *(f16x8*)put[q] = v[d][q][0];
+        *(f16x8*)(put[q] + PLANE) = v[d][q][1];
+      }
+      if (k + DEPTH * KT < K) load(d, k + DEPTH * KT);
+      lds_barrier();
 #pragma unroll
     for (int ks = 0; ks < KT / 16; ++ks) {
       const int cc = 2 * ks + (lane >> 5), r = lane & 31;
@@ -187,6 +203,7 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
 #pragma unroll
           for (int j = 0; j < NT; ++j)
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][h == 0], y[j][h == 1], acc[i][j], 0, 0, 0);
+    }
     }
   }
 

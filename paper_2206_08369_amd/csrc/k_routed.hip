@@ -172,14 +172,15 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
       rb[q] = a.X + (int64_t)(live[q] ? b : 0) * a.F;
     }
     const int c = tid & 3;
-    f32x4 va[NA][2], vb[NB][2];
-    auto load = [&](int k0) {
+    // (two stages on their way: few columns arrive at once)
+    f32x4 va[2][NA][2], vb[2][NB][2];
+    auto load = [&](int d, int k0) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int k = k0 + 8 * c + 4 * e;
 #pragma unroll
         for (int q = 0; q < NA; ++q)
-          va[q][e] = k < a.F4 ? *(const f32x4*)(ra[q] + k) : f32x4{0.f, 0.f, 0.f, 0.f};
+          va[d][q][e] = k < a.F4 ? *(const f32x4*)(ra[q] + k) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int q = 0; q < NB; ++q) {
           f32x4 v{0.f, 0.f, 0.f, 0.f};
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
               for (int j = 0; j < 4; ++j)
                 if (k + j < a.F) v[j] = rb[q][k + j];
           }
-          vb[q][e] = v;
+          vb[d][q][e] = v;
         }
       }
     };
@@ -216,16 +217,22 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
         const int o = i / RB, p = p0 + i % RB;
         dys[i] = p < rows ? a.dY[(int64_t)a.row[item.place + p] * a.O + o] : 0.f;
       }
-    load(0);
-    for (int k0 = 0; k0 < a.F; k0 += kKT) {
+    load(0, 0);
+    if (kKT < a.F) load(1, kKT);
+    for (int k0 = 0; k0 < a.F; k0 += 2 * kKT) {
 #pragma unroll
-      for (int q = 0; q < NA; ++q) St::put(lds, false, 64 * q + (tid >> 2), c, va[q][0], va[q][1]);
+      for (int d = 0; d < 2; ++d) {
+        const int k = k0 + d * kKT;
+        if (k >= a.F) break;
 #pragma unroll
-      for (int q = 0; q < NB; ++q) St::put(lds, true, 64 * q + (tid >> 2), c, vb[q][0], vb[q][1]);
-      if (k0 + kKT < a.F) load(k0 + kKT);
-      lds_barrier();
-      St::template multiply<NA, NB>(lds, wu * 32 * NA, wr * 32 * NB, lane, acc);
-      lds_barrier();
+        for (int q = 0; q < NA; ++q) St::put(lds, false, 64 * q + (tid >> 2), c, va[d][q][0], va[d][q][1]);
+#pragma unroll
+        for (int q = 0; q < NB; ++q) St::put(lds, true, 64 * q + (tid >> 2), c, vb[d][q][0], vb[d][q][1]);
+        if (k + 2 * kKT < a.F) load(d, k + 2 * kKT);
+        lds_barrier();
+        St::template multiply<NA, NB>(lds, wu * 32 * NA, wr * 32 * NB, lane, acc);
+        lds_barrier();
+      }
     }
 
     const int act = item.act;

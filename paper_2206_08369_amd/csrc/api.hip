@@ -116,7 +116,7 @@ struct GrowingWs {
 // How pmlp_orthogonalize goes through one kind of weight matrix: slices of models whose
 // workspace is bounded, each with its runs of the item lists.
 struct NewtonSlice {
-  int32_t load0, load, sym0, sym;  // items: all tiles of X, lower tiles of A
+  int32_t load0, load, sym0, sym, step0, step;  // items: tiles of X, lower ones of A, the steps'
   int64_t nx, na;                  // entries of a plane
 };
 struct PmlpNewton {
@@ -2185,7 +2185,7 @@ int ensure_newton(pmlp* h, int32_t mat) {
     }
   } made{new PmlpNewton()};
   PmlpNewton* q = made.q;
-  std::vector<NsItem> load, sym;
+  std::vector<NsItem> load, sym, step;
   NewtonSlice sl{};
   auto close = [&] {
     sl.load0 = (int32_t)items.size();
@@ -2194,11 +2194,15 @@ int ensure_newton(pmlp* h, int32_t mat) {
     sl.sym0 = (int32_t)items.size();
     sl.sym = (int32_t)sym.size();
     items.insert(items.end(), sym.begin(), sym.end());
+    sl.step0 = (int32_t)items.size();
+    sl.step = (int32_t)step.size();
+    items.insert(items.end(), step.begin(), step.end());
     q->slices.push_back(sl);
     q->nx = std::max(q->nx, sl.nx);
     q->na = std::max(q->na, sl.na);
     load.clear();
     sym.clear();
+    step.clear();
     sl = NewtonSlice{};
   };
   auto cut = [&](int32_t m) {
@@ -2261,6 +2265,8 @@ int ensure_newton(pmlp* h, int32_t mat) {
     for (int32_t i = 0; i < ti; ++i) {
       for (int32_t j = 0; j < tj; ++j) load.push_back(NsItem{m, i, j, 0});
       for (int32_t j = 0; j <= i; ++j) sym.push_back(NsItem{m, i, j, 0});
+      for (int32_t j = 0; j < div_up(t.cp, ns_step_columns(q->tile)); ++j)
+        step.push_back(NsItem{m, i, j, 0});
     }
     cut(m);
   }
@@ -2362,14 +2368,15 @@ int newton(pmlp* h, int32_t mat, NsArgs a, int32_t steps) {
   if (int rc = run(h, KID_AUX, [&] { return launch_ns_momentum(a, 0, q->nlarge, false, h->stream); }))
     return rc;
   for (const NewtonSlice& sl : q->slices) {
-    const NsItem *load = q->d_items + sl.load0, *sym = q->d_items + sl.sym0;
+    const NsItem *load = q->d_items + sl.load0, *sym = q->d_items + sl.sym0,
+                 *step = q->d_items + sl.step0;
     if (int rc = run(h, KID_AUX, [&] { return launch_ns_load(a, load, sl.load, h->stream); })) return rc;
     for (int32_t t = 0; t < steps; ++t) {
       const int from = t & 1;
       if (int rc = run(h, KID_DEEP, [&] {
             if (const hipError_t e = launch_ns_product(a, NS_GRAM, from, sym, sl.sym, h->stream)) return e;
             if (const hipError_t e = launch_ns_product(a, NS_POLY, from, sym, sl.sym, h->stream)) return e;
-            return launch_ns_product(a, t + 1 < steps ? NS_STEP : NS_LAST, from, load, sl.load, h->stream);
+            return launch_ns_product(a, t + 1 < steps ? NS_STEP : NS_LAST, from, step, sl.step, h->stream);
           }))
         return rc;
     }

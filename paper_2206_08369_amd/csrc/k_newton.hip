@@ -107,25 +107,31 @@ hipError_t launch_ns_load(const NsArgs& a, const NsItem* items, int32_t n, hipSt
 
 // ---------------------------------------------------------------------------
 // The products, all of the form C[i][j] = sum_k L[i][k] Q[j][k] with k contiguous in both
-// operands (the next X is stored in both orders for it).  Tiles of T x T, four waves of
-// T / 2 x T / 2.  A and P are symmetric: only tiles with j <= i are computed, and stored
+// operands (the next X is stored in both orders for it).  Tiles of T x TJ, four waves of
+// T / 2 x TJ / 2.  A and P are symmetric: only tiles with j <= i are computed, and stored
 // twice.  A lane ends with four consecutive rows of a column; a wave's block goes through
 // LDS, where it is read by rows of either order, 16 bytes a lane.
 // ---------------------------------------------------------------------------
 
-template <int WHAT, int T>
-__global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const NsItem* items) {
-  constexpr int KT = 32, ROW = 2 * KT, W = T / 2, NT = W / 32, NQ = T / 32;
-  constexpr int PLANE = 2 * T * ROW;      // both operands' rows
-  constexpr int BR = 2 * W + 16;          // bytes of a row of a wave's block
-  constexpr int BLOCK = W * BR;
+template <int WHAT, int T, int TJ>
+__global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const NsItem* items, int n) {
+  constexpr int KT = 32, ROW = 2 * KT, W = T / 2, WJ = TJ / 2, NT = W / 32, NJ = WJ / 32;
+  constexpr int NQ = (T + TJ) / 64, NQL = T / 64;
+  constexpr int PLANE = (T + TJ) * ROW;   // both operands' rows
+  constexpr int CB = WJ < 64 ? WJ : 64;   // columns of a wave's block that go through LDS at a time
+  constexpr int BR = 2 * W + 16;          // bytes of a column of it there
+  constexpr int BLOCK = CB * BR;
   constexpr int LDS = 2 * PLANE > 4 * BLOCK ? 2 * PLANE : 4 * BLOCK;
   __shared__ __align__(16) char lds[LDS];
-  const NsItem it = items[blockIdx.x];
+  // Workgroups go to the eight dies in turn; each die takes a run of the list, and with it
+  // whole matrices, whose tiles share rows in its cache.
+  const int at = (blockIdx.x & 7) * ((n + 7) / 8) + (blockIdx.x >> 3);
+  if (at >= n) return;
+  const NsItem it = items[at];
   const NsMat t = a.mats[it.mat];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wi = wave & 1, wj = wave >> 1;
-  const int i0 = it.i * T, j0 = it.j * T;
+  const int i0 = it.i * T, j0 = it.j * TJ;
   constexpr bool step = WHAT == NS_STEP || WHAT == NS_LAST;
   const _Float16* L = WHAT == NS_GRAM ? a.X[from] + t.xo : WHAT == NS_POLY ? a.A + t.ao : a.P + t.ao;
   const _Float16* Q = WHAT == NS_GRAM ? L : WHAT == NS_POLY ? L : a.XT[from] + t.xo;
@@ -133,14 +139,14 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
   const int K = WHAT == NS_GRAM ? t.cp : t.rp;
   const int nj = step ? t.cp : t.rp;
 
-  // 2 T rows of four 16-byte chunks a plane: each thread takes one chunk of rows tid / 4 + 64 q
+  // T + TJ rows of four 16-byte chunks a plane: each thread takes one chunk of rows tid / 4 + 64 q
   const int c = tid & 3;
   const _Float16* row[NQ];
   char* put[NQ];
 #pragma unroll
   for (int q = 0; q < NQ; ++q) {
     const int r = 64 * q + (tid >> 2);
-    if (2 * q < NQ) {
+    if (q < NQL) {
       const int i = i0 + r < t.rp ? i0 + r : t.rp - 1;
       row[q] = L + (int64_t)i * K + 8 * c;
     } else {
@@ -151,20 +157,20 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
   }
   // DEPTH stages are on their way from memory: a small tile's stage is multiplied long before
   // the next one arrives.
-  constexpr int DEPTH = T == 64 ? 4 : 2;
+  constexpr int DEPTH = T == 64 ? 4 : TJ == 128 ? 2 : 1;
   f16x8 v[DEPTH][NQ][2];
   auto load = [&](int d, int k) {
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
       v[d][q][0] = *(const f16x8*)(row[q] + k);
-      v[d][q][1] = *(const f16x8*)(row[q] + (2 * q < NQ ? lplane : qplane) + k);
+      v[d][q][1] = *(const f16x8*)(row[q] + (q < NQL ? lplane : qplane) + k);
     }
   };
-  f32x16 acc[NT][NT];
+  f32x16 acc[NT][NJ];
 #pragma unroll
   for (int i = 0; i < NT; ++i)
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 #pragma unroll
@@ -186,14 +192,20 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
 #pragma unroll
     for (int ks = 0; ks < KT / 16; ++ks) {
       const int cc = 2 * ks + (lane >> 5), r = lane & 31;
-      f16x8 x[NT][2], y[NT][2];
+      f16x8 x[NT][2], y[NJ][2];
 #pragma unroll
       for (int i = 0; i < NT; ++i)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int ri = wi * W + 32 * i + r, rj = T + wj * W + 32 * i + r;
+          const int ri = wi * W + 32 * i + r;
           x[i][e] = *(const f16x8*)(lds + e * PLANE + ri * ROW + ((cc ^ ((ri >> 2) & 3)) << 4));
-          y[i][e] = *(const f16x8*)(lds + e * PLANE + rj * ROW + ((cc ^ ((rj >> 2) & 3)) << 4));
+        }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int rj = T + wj * WJ + 32 * j + r;
+          y[j][e] = *(const f16x8*)(lds + e * PLANE + rj * ROW + ((cc ^ ((rj >> 2) & 3)) << 4));
         }
       // (small products first, the tiles in turn)
 #pragma unroll
@@ -201,21 +213,21 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll
-          for (int j = 0; j < NT; ++j)
+          for (int j = 0; j < NJ; ++j)
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][h == 0], y[j][h == 1], acc[i][j], 0, 0, 0);
     }
     }
   }
 
   // This wave's block: rows bi0 .., columns bj0 .. of C
-  const int bi0 = i0 + wi * W, bj0 = j0 + wj * W;
+  const int bi0 = i0 + wi * W, bw0 = j0 + wj * WJ;
   const int half = 4 * (lane >> 5);
   if (WHAT == NS_LAST) {
     const bool turned = t.rows > t.cols;
     const float gain = ns_gain(t);
 #pragma unroll
-    for (int bj = 0; bj < NT; ++bj) {
-      const int j = bj0 + 32 * bj + (lane & 31);
+    for (int bj = 0; bj < NJ; ++bj) {
+      const int j = bw0 + 32 * bj + (lane & 31);
       if (j >= nj) continue;
 #pragma unroll
       for (int bi = 0; bi < NT; ++bi)
@@ -243,7 +255,7 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
       a.flag[1] = 1;
     return;
   }
-  if (bi0 >= t.rp || bj0 >= nj) {  // (no wave waits below)
+  if (bi0 >= t.rp || bw0 >= nj) {  // (no wave waits below)
     __syncthreads();
     return;
   }
@@ -257,78 +269,86 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
 #pragma unroll
   for (int bi = 0; bi < NT; ++bi)
 #pragma unroll
-    for (int bj = 0; bj < NT; ++bj) acc[bi][bj] *= WHAT == NS_POLY ? kNsC * kUnscale : kUnscale;
-  if (WHAT != NS_GRAM) {
+    for (int bj = 0; bj < NJ; ++bj) acc[bi][bj] *= WHAT == NS_POLY ? kNsC * kUnscale : kUnscale;
+  const bool other = WHAT == NS_STEP || it.i != it.j;  // the order [i][j] too
+#pragma unroll
+  for (int cb = 0; cb < WJ / CB; ++cb) {
+    const int bj0 = bw0 + cb * CB;
+    if (bj0 >= nj) continue;
+    if (WHAT != NS_GRAM) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int q = 0; q < CB * LPR / 64; ++q) {
+          const int r = q * (64 / LPR) + lane / LPR, ch = lane % LPR;
+          const int j = min(bj0 + r, nj - 1), i = min(bi0 + 8 * ch, t.rp - 8);
+          *(f16x8*)(block + r * BR + 16 * ch) = *(const f16x8*)(old + h * plane + (int64_t)j * t.rp + i);
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int bi = 0; bi < NT; ++bi)
+#pragma unroll
+          for (int bj = 0; bj < CB / 32; ++bj)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              f32x16& c = acc[bi][cb * (CB / 32) + bj];
+              const f16x4 o = *(const f16x4*)(block + (32 * bj + (lane & 31)) * BR + 2 * (32 * bi + 8 * q + half));
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                c[4 * q + e] = fmaf(WHAT == NS_POLY ? kNsB : kNsA, (float)o[e], c[4 * q + e]);
+            }
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int q = 0; q < W * LPR / 64; ++q) {
-        const int r = q * (64 / LPR) + lane / LPR, ch = lane % LPR;
-        const int j = min(bj0 + r, nj - 1), i = min(bi0 + 8 * ch, t.rp - 8);
-        *(f16x8*)(block + r * BR + 16 * ch) = *(const f16x8*)(old + h * plane + (int64_t)j * t.rp + i);
-      }
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
       for (int bi = 0; bi < NT; ++bi)
 #pragma unroll
-        for (int bj = 0; bj < NT; ++bj)
+        for (int bj = 0; bj < CB / 32; ++bj)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const f16x4 o = *(const f16x4*)(block + (32 * bj + (lane & 31)) * BR + 2 * (32 * bi + 8 * q + half));
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              acc[bi][bj][4 * q + e] = fmaf(WHAT == NS_POLY ? kNsB : kNsA, (float)o[e], acc[bi][bj][4 * q + e]);
+            const f32x16& c = acc[bi][cb * (CB / 32) + bj];
+            f16x4 hi, lo;
+            halve(f32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]}, hi, lo);
+            *(f16x4*)(block + (32 * bj + (lane & 31)) * BR + 2 * (32 * bi + 8 * q + half)) = h ? lo : hi;
           }
       __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int q = 0; q < CB * LPR / 64; ++q) {
+        const int r = q * (64 / LPR) + lane / LPR, ch = lane % LPR;
+        const int j = bj0 + r, i = bi0 + 8 * ch;
+        if (j < nj && i < t.rp)
+          *(f16x8*)(tt + h * plane + (int64_t)j * t.rp + i) = *(const f16x8*)(block + r * BR + 16 * ch);
+      }
+      if (other) {
+        // transposing loads: lane (li, lk) gets row li of the block's 16, columns 8 lk .. + 7
+        const int li = lane & 15, lk = lane >> 4;
+#pragma unroll
+        for (int r = 0; r < W; r += 16)
+#pragma unroll
+          for (int cc = 0; cc < CB; cc += 32) {
+            const char* at = block + (cc + 8 * lk + (li >> 2)) * BR + 2 * r + 8 * (li & 3);
+            const f16x8 o = columns(at, 4 * BR);
+            const int i = bi0 + r + li, j = bj0 + cc + 8 * lk;
+            if (i < t.rp && j < nj) *(f16x8*)(to + h * plane + (int64_t)i * nj + j) = o;
+          }
+      }
+      __builtin_amdgcn_wave_barrier();
     }
-  }
-  const bool other = WHAT == NS_STEP || it.i != it.j;  // the order [i][j] too
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-#pragma unroll
-    for (int bi = 0; bi < NT; ++bi)
-#pragma unroll
-      for (int bj = 0; bj < NT; ++bj)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          f16x4 hi, lo;
-          halve(f32x4{acc[bi][bj][4 * q], acc[bi][bj][4 * q + 1], acc[bi][bj][4 * q + 2], acc[bi][bj][4 * q + 3]},
-                hi, lo);
-          *(f16x4*)(block + (32 * bj + (lane & 31)) * BR + 2 * (32 * bi + 8 * q + half)) = h ? lo : hi;
-        }
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int q = 0; q < W * LPR / 64; ++q) {
-      const int r = q * (64 / LPR) + lane / LPR, ch = lane % LPR;
-      const int j = bj0 + r, i = bi0 + 8 * ch;
-      if (j < nj && i < t.rp)
-        *(f16x8*)(tt + h * plane + (int64_t)j * t.rp + i) = *(const f16x8*)(block + r * BR + 16 * ch);
-    }
-    if (other) {
-      // transposing loads: lane (li, lk) gets row li of the block's 16, columns 8 lk .. + 7
-      const int li = lane & 15, lk = lane >> 4;
-#pragma unroll
-      for (int r = 0; r < W; r += 16)
-#pragma unroll
-        for (int cc = 0; cc < W; cc += 32) {
-          const char* at = block + (cc + 8 * lk + (li >> 2)) * BR + 2 * r + 8 * (li & 3);
-          const f16x8 o = columns(at, 4 * BR);
-          const int i = bi0 + r + li, j = bj0 + cc + 8 * lk;
-          if (i < t.rp && j < nj) *(f16x8*)(to + h * plane + (int64_t)i * nj + j) = o;
-        }
-    }
-    __builtin_amdgcn_wave_barrier();
   }
 }
 
 namespace {
-template <int T>
-void product(const NsArgs& a, int what, int from, const NsItem* items, unsigned n, hipStream_t s) {
+// (TS: columns of a tile of the steps)
+template <int T, int TS>
+void product(const NsArgs& a, int what, int from, const NsItem* items, int n, hipStream_t s) {
+  const unsigned grid = (unsigned)((n + 7) / 8 * 8);
   switch (what) {
-    case NS_GRAM: k_ns_product<NS_GRAM, T><<<n, 256, 0, s>>>(a, from, items); break;
-    case NS_POLY: k_ns_product<NS_POLY, T><<<n, 256, 0, s>>>(a, from, items); break;
-    case NS_STEP: k_ns_product<NS_STEP, T><<<n, 256, 0, s>>>(a, from, items); break;
-    default: k_ns_product<NS_LAST, T><<<n, 256, 0, s>>>(a, from, items); break;
+    case NS_GRAM: k_ns_product<NS_GRAM, T, T><<<grid, 256, 0, s>>>(a, from, items, n); break;
+    case NS_POLY: k_ns_product<NS_POLY, T, T><<<grid, 256, 0, s>>>(a, from, items, n); break;
+    case NS_STEP: k_ns_product<NS_STEP, T, TS><<<grid, 256, 0, s>>>(a, from, items, n); break;
+    default: k_ns_product<NS_LAST, T, TS><<<grid, 256, 0, s>>>(a, from, items, n); break;
   }
 }
 }  // namespace
@@ -336,8 +356,8 @@ void product(const NsArgs& a, int what, int from, const NsItem* items, unsigned 
 hipError_t launch_ns_product(const NsArgs& a, int what, int from, const NsItem* items, int32_t n,
                              hipStream_t s) {
   note_variant("k_ns_product", kArithX3);
-  if (a.tile == 64) product<64>(a, what, from, items, (unsigned)n, s);
-  else product<128>(a, what, from, items, (unsigned)n, s);
+  if (a.tile == 64) product<64, 64>(a, what, from, items, n, s);
+  else product<128, 256>(a, what, from, items, n, s);
   return hipGetLastError();
 }
 

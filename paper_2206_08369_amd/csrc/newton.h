@@ -60,7 +60,9 @@ hipError_t launch_ns_momentum(const NsArgs& a, int32_t piece0, int32_t pieces, b
 // X = U / |U|_F
 hipError_t launch_ns_load(const NsArgs& a, const NsItem* items, int32_t n, hipStream_t s);
 enum NsProduct { NS_GRAM = 0, NS_POLY = 1, NS_STEP = 2, NS_LAST = 3 };
-// from X[from], XT[from]
+// From X[from], XT[from].  items: tiles of `tile` x `tile` (j <= i) of A and P, of `tile` x
+// ns_step_columns(tile) of the steps.
+inline int32_t ns_step_columns(int32_t tile) { return tile == 64 ? 64 : 256; }
 hipError_t launch_ns_product(const NsArgs& a, int what, int from, const NsItem* items, int32_t n,
                              hipStream_t s);
 

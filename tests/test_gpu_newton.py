@@ -64,6 +64,16 @@ def test_many_matrices(pm, F, top):
     assert torch.equal(got, net.orthogonalize(G.cuda()))
 
 
+def test_many_large_matrices(pm):
+    """Enough of them for the larger tiles; three are compared."""
+    hs = [1000] * 17 + [129, 900]
+    net = pm.PackedMLP(1000, 2, hs, [0] * len(hs))
+    G = randn(3, sum(hs), 1000)
+    got = net.orthogonalize(G.cuda())
+    check(got, G, [blocks(1000, hs)[k] for k in (0, 17, 18)])
+    assert torch.equal(got, net.orthogonalize(G.cuda()))
+
+
 @pytest.mark.parametrize("n", [1, 2, 3, 8])
 def test_steps(pm, n):
     hs = [3, 40, 150]

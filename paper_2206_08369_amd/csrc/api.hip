@@ -2066,13 +2066,18 @@ int forward_routed(pmlp* h, const float* X, int32_t B, const int32_t* idx, const
   const int64_t R = (int64_t)B * K;
   RtJoin j{idx, weight, h->d_seg_off, B, K, h->M, h->O, 0, 0, nullptr, Y};
   if (rt_few(h, R)) {
+    RtLayout none;
+    none.p.K = K;
+    if (const int32_t c16 = div_up(h->widest, 16); (int64_t)K * c16 <= kRtSampleChunks) {
+      const RtArgs a = rt_args(h, X, none);
+      const RtFew f{idx, (int32_t)R, c16, h->flag};
+      return run(h, KID_GEMM_FWD, [&] { return launch_rt_sample(a, f, weight, Y, h->stream); });
+    }
     const int32_t chunks = div_up(h->widest, kRtFewUnits);
     if (R * chunks > INT32_MAX) return too_large();
     Carver c;
     c.take((size_t)R * chunks * h->O);
     if (int rc = ensure_ws(h, &h->extra, c.bytes, "a routed pack")) return rc;
-    RtLayout none;
-    none.p.K = K;
     RtArgs a = rt_args(h, X, none);
     a.part = (float*)h->extra.ws;
     a.parts = chunks;

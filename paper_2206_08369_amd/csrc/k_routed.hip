@@ -356,25 +356,19 @@ hipError_t launch_rt_tile(const RtArgs& a, const RtShape& sh, bool train, hipStr
 }
 
 // ---------------------------------------------------------------------------
-// Few slots: a workgroup takes 64 units of a slot's model, each wave 16 of them, four at
-// a time, 16 lanes along the columns of each.  Bound by the weights' read.
+// Few slots, each straight from its index.  A wave takes 16 units of the slot's model, four at
+// a time, 16 lanes along the columns of each: bound by the weights' read, or by launches.
 // ---------------------------------------------------------------------------
 
+namespace {
+
+// Units n0 + 4 i + lane / 16 for the sample x, those from `end` on 0 (the same in all 16
+// lanes of a unit).
 template <bool GATED>
-__global__ __launch_bounds__(256) void k_rt_few(RtArgs a, RtFew f) {
-  const int s = blockIdx.x / f.chunks, chunk = blockIdx.x % f.chunks;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int m = f.idx[s];
-  if (m < 0 || m >= a.M) {
-    if (m != -1 && tid == 0 && chunk == 0) f.flag[3] = 1;
-    return;
-  }
-  const int64_t first = a.seg_off[m], end = a.seg_off[m + 1];
-  const int64_t n0 = first + (int64_t)chunk * kRtFewUnits + 16 * wave;
-  if (first + (int64_t)chunk * kRtFewUnits >= end) return;
-  const float* x = a.X + (int64_t)(s / a.K) * a.F;
-  const int li = lane & 15, lu = lane >> 4;
-  float z[4] = {}, u[4] = {};  // unit n0 + 4 i + lu
+__device__ __forceinline__ void few_units(const RtArgs& a, const float* x, int64_t n0, int64_t end, int act,
+                                          float (&h)[4]) {
+  const int lane = threadIdx.x & 63, li = lane & 15, lu = lane >> 4;
+  float z[4] = {}, u[4] = {};
   const float *w[4], *v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -403,34 +397,93 @@ __global__ __launch_bounds__(256) void k_rt_few(RtArgs a, RtFew f) {
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {  // sums end in lane 15 of each 16
-    z[i] = group_sum_to_last(z[i], 16);
-    if (GATED) u[i] = group_sum_to_last(u[i], 16);
-    z[i] = __shfl(z[i], lane | 15);
-    if (GATED) u[i] = __shfl(u[i], lane | 15);
+    z[i] = __shfl(group_sum_to_last(z[i], 16), lane | 15);
+    if (GATED) u[i] = __shfl(group_sum_to_last(u[i], 16), lane | 15);
   }
-  float h[4];
-  blk_acts<4>(a.act[m], z, h);
+  blk_acts<4>(act, z, h);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (GATED) h[i] *= u[i];
     if (n0 + 4 * i + lu >= end) h[i] = 0.f;
   }
-  __shared__ float sums[4][kRtMaxO];
-  for (int o = 0; o < a.O; ++o) {
-    float t = 0.f;
+}
+
+// Their sum with W2's row o, in every lane.
+__device__ __forceinline__ float few_output(const RtArgs& a, int o, int64_t n0, int64_t end,
+                                            const float (&h)[4]) {
+  const int lu = (threadIdx.x & 63) >> 4;
+  float t = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t n = n0 + 4 * i + lu;
-      if (n < end) t = fmaf(h[i], a.W2[(int64_t)o * a.ldw + n], t);
-    }
-    t += __shfl_xor(t, 16);
-    t += __shfl_xor(t, 32);
+  for (int i = 0; i < 4; ++i) {
+    const int64_t n = n0 + 4 * i + lu;
+    if (n < end) t = fmaf(h[i], a.W2[(int64_t)o * a.ldw + n], t);
+  }
+  t += __shfl_xor(t, 16);
+  return t + __shfl_xor(t, 32);
+}
+
+}  // namespace
+
+// 64 units of a slot a workgroup
+template <bool GATED>
+__global__ __launch_bounds__(256) void k_rt_few(RtArgs a, RtFew f) {
+  const int s = blockIdx.x / f.chunks, chunk = blockIdx.x % f.chunks;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int m = f.idx[s];
+  if (m < 0 || m >= a.M) {
+    if (m != -1 && tid == 0 && chunk == 0) f.flag[3] = 1;
+    return;
+  }
+  const int64_t first = a.seg_off[m], end = a.seg_off[m + 1];
+  const int64_t n0 = first + (int64_t)chunk * kRtFewUnits + 16 * wave;
+  if (first + (int64_t)chunk * kRtFewUnits >= end) return;
+  __shared__ float sums[4][kRtMaxO];
+  float h[4];
+  few_units<GATED>(a, a.X + (int64_t)(s / a.K) * a.F, n0, end, a.act[m], h);
+  for (int o = 0; o < a.O; ++o) {
+    const float t = few_output(a, o, n0, end, h);
     if (lane == 0) sums[wave][o] = t;
   }
   __syncthreads();
   if (tid < a.O)
     a.part[((int64_t)s * a.parts + chunk) * a.O + tid] =
         (sums[0][tid] + sums[1][tid]) + (sums[2][tid] + sums[3][tid]);
+}
+
+// A sample a workgroup, its models' units in turn over the waves: Y without a second launch.
+template <bool GATED>
+__global__ __launch_bounds__(256) void k_rt_sample(RtArgs a, RtFew f, const float* weight, float* Y) {
+  const int64_t b = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ float sums[4][kRtMaxO];
+  float y = 0.f;  // lane o: output o
+  for (int q = wave; q < a.K * f.chunks; q += 4) {
+    const int k = q / f.chunks, m = f.idx[b * a.K + k];
+    if (m < 0 || m >= a.M) {
+      if (m != -1 && lane == 0) f.flag[3] = 1;
+      continue;
+    }
+    const int64_t end = a.seg_off[m + 1], n0 = a.seg_off[m] + 16 * (q % f.chunks);
+    if (n0 >= end) continue;
+    float h[4];
+    few_units<GATED>(a, a.X + b * a.F, n0, end, a.act[m], h);
+    const float w = weight[b * a.K + k];
+    for (int o = 0; o < a.O; ++o) {
+      const float t = few_output(a, o, n0, end, h);
+      if (lane == o) y = fmaf(w, t, y);
+    }
+  }
+  if (lane < kRtMaxO) sums[wave][lane] = y;
+  __syncthreads();
+  if (tid < a.O) Y[b * a.O + tid] = (sums[0][tid] + sums[1][tid]) + (sums[2][tid] + sums[3][tid]);
+}
+
+hipError_t launch_rt_sample(const RtArgs& a, const RtFew& f, const float* weight, float* Y, hipStream_t s) {
+  note_variant("k_rt_sample", kArithNone);
+  const unsigned grid = (unsigned)(f.R / a.K);
+  if (a.V1) k_rt_sample<true><<<grid, 256, 0, s>>>(a, f, weight, Y);
+  else k_rt_sample<false><<<grid, 256, 0, s>>>(a, f, weight, Y);
+  return hipGetLastError();
 }
 
 hipError_t launch_rt_few(const RtArgs& a, const RtFew& f, hipStream_t s) {

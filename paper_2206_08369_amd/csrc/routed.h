@@ -115,6 +115,9 @@ struct RtFew {
   int32_t* flag;
 };
 hipError_t launch_rt_few(const RtArgs& a, const RtFew& f, hipStream_t s);
+// The same and Y at once, a workgroup for each sample; chunks: of 16 units.
+constexpr int32_t kRtSampleChunks = 16;  // K times chunks, at most
+hipError_t launch_rt_sample(const RtArgs& a, const RtFew& f, const float* weight, float* Y, hipStream_t s);
 
 // Y[b] = sum_k weight[b][k] sum of the parts of slot (b, k) that its model has.
 struct RtJoin {

@@ -133,6 +133,21 @@ __device__ __forceinline__ void blk_acts(int a, const float (&z)[NV], float (&v)
   }
 }
 
+// Values and slopes of activation id A.
+template <int NV>
+__device__ __forceinline__ void act_and_slope(int A, const float (&z)[NV], float (&v)[NV],
+                                              float (&d)[NV]) {
+  switch (A) {
+#define PMLP_ACT(AA)                                                                     \
+  case AA: {                                                                             \
+    _Pragma("unroll") for (int j = 0; j < NV; ++j) v[j] = blk_act_slope(AA, z[j], &d[j]); \
+    break;                                                                               \
+  }
+    PMLP_EVERY_ACT
+#undef PMLP_ACT
+  }
+}
+
 // ---------------------------------------------------------------------------
 // The samples' three bf16 pieces in LDS, sample by sample, for both fused kernels.
 // ---------------------------------------------------------------------------

@@ -252,21 +252,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));  // rows of any F
 typedef __attribute__((address_space(3))) char lds_char;
 
-// Values and slopes of activation id A.
-template <int NV>
-__device__ __forceinline__ void act_and_slope(int A, const float (&z)[NV], float (&v)[NV],
-                                              float (&d)[NV]) {
-  switch (A) {
-#define PMLP_ACT(AA)                                                                     \
-  case AA: {                                                                             \
-    _Pragma("unroll") for (int j = 0; j < NV; ++j) v[j] = blk_act_slope(AA, z[j], &d[j]); \
-    break;                                                                               \
-  }
-    PMLP_EVERY_ACT
-#undef PMLP_ACT
-  }
-}
-
 // The backward of tiles first, first + stride, .. below `end` by one wave (as many
 // rounds for each wave of the workgroup); nchunk > 1: over chunks of SC samples, whose
 // pieces the workgroup makes in turn (else they lie in LDS).

@@ -253,8 +253,7 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
         if (!TRAIN) {
           blk_acts<16>(act, z, v);
         } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) v[e] = blk_act_slope(act, z[e], &d[e]);
+          act_and_slope<16>(act, z, v, d);
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {

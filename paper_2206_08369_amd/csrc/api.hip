@@ -205,7 +205,7 @@ struct pmlp {
   int32_t npacked = 0;  // tiles of another list behind those (m3_plan), or 0
   bool has_split = false;
   float* loss = nullptr;   // [M]
-  int32_t* flag = nullptr; // [4]: bad label, bad rate, count of non-finite losses, spare
+  int32_t* flag = nullptr; // [4]: bad label, bad rate, count of non-finite losses, bad model index
 
   int32_t capBp = 0;
   float* Xp = nullptr;
@@ -2153,9 +2153,8 @@ int gradients_routed(pmlp* h, const float* X, int32_t B, const int32_t* idx, con
   if (int rc = run(h, KID_GEMM_FWD, [&] { return launch_rt_tile(g.a, sh, true, h->stream); })) return rc;
   RtShape shw = sh;
   shw.nb = l.p.t.df / 64;
-  if (int rc = run(h, KID_GEMM_BWD, [&] { return launch_rt_weights(g, shw, h->stream); })) return rc;
   const RtJoin j{idx, weight, h->d_seg_off, B, K, h->M, 1, parts, l.p.t.uc / 2, g.a.dwpart, dweight};
-  return run(h, KID_M3_BWD, [&] { return launch_rt_join_dw(j, h->stream); });
+  return run(h, KID_GEMM_BWD, [&] { return launch_rt_weights(g, shw, j, h->stream); });
 }
 
 // ---- orthogonalised updates ----------------------------------------------------------

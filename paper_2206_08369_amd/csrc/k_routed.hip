@@ -276,7 +276,7 @@ __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
         // (Places that hold no slot have zero samples, weights and gradients: what is
         // stored there adds nothing.)
         const int64_t z0 = item.zoff + (int64_t)(p >> 5) * item.h * 32 +
-                           (item.b * UC + u0 + half) * 32 + (lane & 31);
+                           (int64_t)(item.b * UC + u0 + half) * 32 + (lane & 31);
         float *const hz = a.H + z0, *const dz = a.dZ + z0, *const du = GATED ? a.dU + z0 : nullptr;
         if (p0 + (wr * NB + j) * 32 >= places) continue;  // (the same for all lanes)
         auto store = [&](int e) {
@@ -521,36 +521,32 @@ __global__ __launch_bounds__(256) void k_rt_join(RtJoin a) {
   a.Y[i] = y;
 }
 
-__global__ __launch_bounds__(256) void k_rt_join_dw(RtJoin a) {
-  const int64_t s = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (s >= (int64_t)a.B * a.K) return;
-  const int m = a.idx[s];
-  a.Y[s] = m < 0 || m >= a.M ? 0.f : slot_sum(a, s, m, 0);
-}
-
 hipError_t launch_rt_join(const RtJoin& a, hipStream_t s) {
   note_variant("k_rt_join", kArithNone);
   k_rt_join<<<(unsigned)ceil_div_i((int64_t)a.B * a.O, 256), 256, 0, s>>>(a);
   return hipGetLastError();
 }
-hipError_t launch_rt_join_dw(const RtJoin& a, hipStream_t s) {
-  note_variant("k_rt_join_dw", kArithNone);
-  k_rt_join_dw<<<(unsigned)ceil_div_i((int64_t)a.B * a.K, 256), 256, 0, s>>>(a);
-  return hipGetLastError();
-}
-
 // ---------------------------------------------------------------------------
 // Weight gradients: dW1_m = dZ_m X_m (and dV1_m = dU_m X_m) over the places of model m,
 // units the first operand's rows and columns of X the second's.
 // ---------------------------------------------------------------------------
 
+namespace {
+
 template <int NA, int NB, bool GATED>
-__global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
-  constexpr int RA = 64 * NA, RB = 64 * NB, UC = GATED ? 64 : RA;
+struct DwTile {
+  static constexpr int RA = 64 * NA, RB = 64 * NB, UC = GATED ? 64 : RA;
   // X lies in LDS as it comes, [place][column], and goes to the products through transposing
   // loads, 64 bytes of four rows at a time: rows are 64 bytes past (or short of) all banks apart.
-  constexpr int kA = RA * kRow, XROW = 2 * RB + 64, kX = kKT * XROW;
-  __shared__ __align__(16) char lds[3 * (kA + kX)];
+  static constexpr int kA = RA * kRow, XROW = 2 * RB + 64, kX = kKT * XROW;
+  static constexpr int kBytes = 3 * (kA + kX);
+};
+
+// Workgroup `block` of `blocks`
+template <int NA, int NB, bool GATED>
+__device__ __forceinline__ void weight_tiles(const RtGrad& g, char* lds, int block, int blocks) {
+  typedef DwTile<NA, NB, GATED> T;
+  constexpr int RB = T::RB, UC = T::UC, kA = T::kA, XROW = T::XROW, kX = T::kX;
   const RtArgs& a = g.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wu = wave & 1, wf = wave >> 1;
@@ -558,7 +554,7 @@ __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
   // (In the list's order, dies in turn: the tiles of a model with many rows, which take
   // longest, are spread over all of them.  32 models of 500 to 1,000 units on 16,384 rows: 415
   // us where each die took a run of the list, XXX so.)
-  for (int at = blockIdx.x; at < n; at += gridDim.x) {
+  for (int at = block; at < n; at += blocks) {
     const RtItem item = item_at(g.jitems, at);
     const int m = item.m;
     const int64_t first = item.first;
@@ -688,13 +684,13 @@ __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g) {
 // takes 16 units of a tile of the weight gradients and a part of their model's places, 64 of
 // every 256 a wave, and all outputs.  A lane loads four consecutive places of its row and
 // feeds them to four products, in the same order for both operands.
-__global__ __launch_bounds__(256) void k_rt_dw2(RtGrad g) {
-  __shared__ f32x4 sums[4][64];
+// sums: [4][64] of the workgroup
+__device__ __forceinline__ void output_weights(const RtGrad& g, f32x4* sums, int block, int blocks) {
   const RtArgs& a = g.a;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = *g.njitems, nf = (a.F + g.t.df - 1) / g.t.df;
-  for (int it = blockIdx.x; it < n; it += gridDim.x) {
+  for (int it = block; it < n; it += blocks) {
     const RtItem item = item_at(g.jitems, it);
     const int64_t first = item.first;
     const int h = item.h, end = (item.a + 1) * g.t.du < h ? (item.a + 1) * g.t.du : h;
@@ -735,17 +731,37 @@ __global__ __launch_bounds__(256) void k_rt_dw2(RtGrad g) {
         if (p + 512 < b1) load(0, p + 512);
         multiply(1, p + 256);
       }
-      sums[wave][lane] = acc[0] + acc[1];
+      sums[64 * wave + lane] = acc[0] + acc[1];
       __syncthreads();
       if (wave == 0) {
         // lane: unit u0 + li, outputs 4 lk + e
-        const f32x4 t = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+        const f32x4 t = (sums[lane] + sums[64 + lane]) + (sums[128 + lane] + sums[192 + lane]);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (u0 + li < h && 4 * lk + e < a.O) out[(int64_t)(4 * lk + e) * g.N + first + u0 + li] = t[e];
       }
       __syncthreads();
     }
+  }
+}
+
+}  // namespace
+
+// All that the hidden gradients lead to, side by side: the first `tiles` workgroups take tiles
+// of the input weights' gradients, the next `outs` the output weights', the rest the slots'.
+template <int NA, int NB, bool GATED>
+__global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g, RtJoin j, int tiles, int outs) {
+  __shared__ __align__(16) char lds[DwTile<NA, NB, GATED>::kBytes];
+  const int block = blockIdx.x;
+  if (block < tiles) {
+    weight_tiles<NA, NB, GATED>(g, lds, block, tiles);
+  } else if (block < tiles + outs) {
+    output_weights(g, (f32x4*)lds, block - tiles, outs);
+  } else {
+    const int64_t s = (int64_t)(block - tiles - outs) * 256 + threadIdx.x;
+    if (s >= (int64_t)j.B * j.K) return;
+    const int m = j.idx[s];
+    j.Y[s] = m < 0 || m >= j.M ? 0.f : slot_sum(j, s, m, 0);
   }
 }
 
@@ -776,10 +792,11 @@ __global__ __launch_bounds__(256) void k_rt_sum_parts(RtGrad g) {
   }
 }
 
-hipError_t launch_rt_weights(const RtGrad& g, const RtShape& sh, hipStream_t s) {
+hipError_t launch_rt_weights(const RtGrad& g, const RtShape& sh, const RtJoin& j, hipStream_t s) {
   note_variant("k_rt_dw", kArithX3);
-#define PMLP_RT_DW(NA, NB, G) \
-  k_rt_dw<NA, NB, G><<<groups_for(g.jmost), 256, 0, s>>>(g)
+  const int tiles = (int)groups_for(g.jmost);
+  const unsigned grid = 2 * tiles + (unsigned)ceil_div_i((int64_t)j.B * j.K, 256);
+#define PMLP_RT_DW(NA, NB, G) k_rt_dw<NA, NB, G><<<grid, 256, 0, s>>>(g, j, tiles, tiles)
   if (g.a.V1) {
     if (sh.nb == 2) PMLP_RT_DW(2, 2, true);
     else PMLP_RT_DW(2, 1, true);
@@ -792,7 +809,6 @@ hipError_t launch_rt_weights(const RtGrad& g, const RtShape& sh, hipStream_t s) 
   }
 #undef PMLP_RT_DW
   if (const hipError_t e = hipGetLastError()) return e;
-  k_rt_dw2<<<groups_for(g.jmost), 256, 0, s>>>(g);
   if (g.nparts > 1) k_rt_sum_parts<<<(unsigned)g.N, 256, 0, s>>>(g);
   return hipGetLastError();
 }

@@ -131,8 +131,6 @@ struct RtJoin {
   float* Y;
 };
 hipError_t launch_rt_join(const RtJoin& a, hipStream_t s);
-// dweight[slot] = the sum of the parts, O = 1.
-hipError_t launch_rt_join_dw(const RtJoin& a, hipStream_t s);
 
 struct RtGrad {
   RtArgs a;
@@ -151,6 +149,8 @@ struct RtGrad {
   const uint32_t* fmask;
   int32_t fmw;
 };
-hipError_t launch_rt_weights(const RtGrad& g, const RtShape& sh, hipStream_t s);
+// Gradients of the weights and, from j (O = 1), of the slots' weights: Y[slot] = the sum of
+// its parts.
+hipError_t launch_rt_weights(const RtGrad& g, const RtShape& sh, const RtJoin& j, hipStream_t s);
 
 }  // namespace pmlpk

@@ -77,7 +77,7 @@ def check_route(pm, net, scores, K):
     return idx, w
 
 
-@pytest.mark.parametrize("M", [1, 2, 63, 64, 65, 1000, 1024, 1025, 5000])
+@pytest.mark.parametrize("M", [1, 2, 63, 64, 65, 256, 257, 1024, 1025, 5000, 8193])
 @pytest.mark.parametrize("K", [1, 2, 5, 16])
 def test_route(pm, M, K):
     rng = np.random.default_rng(M * 17 + K)
@@ -157,6 +157,9 @@ SHAPES = [
     # wide waves of models and rows
     (40, 2, [150, 90, 260], 500, 1),
     (66, 9, [150, 190], 1000, 2),
+    (20, 3, [10, 30], 400, 2),
+    # more slots than one workgroup groups
+    (9, 2, [5, 33, 8], 5000, 2),
 ]
 
 
@@ -243,6 +246,77 @@ def test_many_models(pm, M):
     got, want = p.gradients(X, idx, w, dY), p.want(X, idx, w, dY)
     for k in got:
         close(got[k], want[k], k)
+
+
+@pytest.mark.parametrize("gated,lo,hi", [(False, 1, 9), (True, 1, 9), (False, 60, 90)])
+def test_many_tiles(pm, gated, lo, hi):
+    """Enough tiles of the weight gradients for the wider ones."""
+    M, F = 1100, 70
+    rng = np.random.default_rng(hi)
+    p = Pool(pm, F, 3, rng.integers(lo, hi, M), rng.choice(rr.SMOOTH, M), gated, seed=hi)
+    X, dY = p.rand(2000, F), p.rand(2000, 3)
+    idx, w = p.choices(2000, 2)
+    close(p.forward(X, idx, w), p.want(X, idx, w)["Y"], "Y")
+    got, want = p.gradients(X, idx, w, dY), p.want(X, idx, w, dY)
+    for k in got:
+        close(got[k], want[k], k)
+
+
+def test_regression_packs(pm):
+    """The head of a pack is its own loss's; the mixture takes a gradient from outside."""
+    p = Pool(pm, 6, 2, [3, 40], [2, 7], False)
+    p.net.close()
+    p.net = pm.PackedMLP(6, 2, [3, 40], [2, 7], head="mse")
+    p.put()
+    X, dY = p.rand(90, 6), p.rand(90, 2)
+    idx, w = p.choices(90, 2)
+    close(p.forward(X, idx, w), p.want(X, idx, w)["Y"], "Y")
+    got, want = p.gradients(X, idx, w, dY), p.want(X, idx, w, dY)
+    for k in got:
+        close(got[k], want[k], k)
+    with pytest.raises(pm.PmlpError) as e:
+        p.net.losses()  # (no call of its own loss has run)
+    assert e.value.code == pm.PMLP_ESTATE
+
+
+def test_calls_under_way_keep_their_workspace(pm):
+    """A larger batch on another stream while calls that use the smaller workspace run."""
+    p = Pool(pm, 90, 2, [70, 200, 33], [7, 2, 3], True, seed=4)
+    small = [t.cuda() for t in (p.rand(800, 90), *p.choices(800, 2), p.rand(800, 2))]
+    large = [t.cuda() for t in (p.rand(9000, 90), *p.choices(9000, 2), p.rand(9000, 2))]
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(a):
+        first = [p.net.gradients_routed(*small) for _ in range(4)][-1]
+    with torch.cuda.stream(b):
+        second = p.net.gradients_routed(*large)
+    torch.cuda.synchronize()
+    for got, data in ((first, small), (second, large)):
+        want = p.want(*[t.cpu() for t in data[:3]], data[3].cpu())
+        for g, k in zip(got, ("W1", "V1", "W2", "weight")):
+            close(g, want[k], k)
+
+
+def test_memory_is_given_back(pm):
+    def in_use():
+        torch.cuda.synchronize()
+        free, total = torch.cuda.mem_get_info()
+        return total - free
+
+    p = Pool(pm, 40, 2, [300, 200], [7, 2], False)
+    before = in_use()
+    for B in range(20000, 60001, 10000):
+        X = torch.zeros(B, 40).cuda()
+        idx, w = torch.zeros(B, 1, dtype=torch.int32).cuda(), torch.zeros(B, 1).cuda()
+        p.net.gradients_routed(X, idx, w, torch.zeros(B, 2).cuda())
+        del X, idx, w
+    torch.cuda.empty_cache()
+    # hidden values of 60,000 rows of the widest model twice, and the rest: not one
+    # workspace a size
+    assert in_use() - before < 2 * 300 * 60100 * 4 + (128 << 20)
+    p.net.close()
+    torch.cuda.empty_cache()
+    assert in_use() - before < (64 << 20)
 
 
 @pytest.mark.parametrize("B", [1, 300])

@@ -1929,17 +1929,47 @@ int check_routed(pmlp* h, const void* X, int32_t B, const void* idx, const void*
   return PMLP_OK;
 }
 
-// Tiles of the routed products: those of a wave that the pack and the mean number of rows
-// of a model fill.
+// Tiles of the routed products.  Two 32-row tiles of units a wave for models of more than
+// 256 units on average (48 models of 500 to 1,000 units, 1,000 columns, 64 rows each: 77 us
+// against 104 with one; 200 of 100 to 200, 200 columns: 45 against 40); two of samples where
+// the models have more than 512 rows each and there are tiles for two rounds of the device
+// (the 48 at 1,000 rows: 524 against 608 us, at 64: 103 against 78; 600 models of 1 to 100
+// units, 256 rows: 83 against 77).
 RtShape rt_shape(const pmlp* h, int64_t R) {
   RtShape sh;
-  sh.na = h->N > (int64_t)64 * h->M ? 2 : 1;
-  sh.nb = R > (int64_t)64 * h->M ? 2 : 1;
+  const int64_t mean = h->N / h->M;
+  const bool gated = h->block && h->block->gated;
+  sh.na = mean > 256 ? 2 : 1;
+  const int64_t chunks = (mean + rt_units(sh, gated) - 1) / rt_units(sh, gated);
+  sh.nb = R > (int64_t)512 * h->M && R / 128 * chunks >= 1024 ? 2 : 1;
   return sh;
 }
 
-// Whether every slot goes to its model on its own.
-bool rt_few(const pmlp* h, int64_t R) { return R <= 16 || R <= 2 * (int64_t)h->M; }
+// Tiles of the weight gradients: 128 units for models of more than 64 on average, and then
+// 128 columns where there are enough for two rounds of the device (48 models of 500 to 1,000
+// units, 1,000 columns, 128 rows each: 250 us for a call against 263 with 64; 2,000 of 1 to
+// 60 units, 300 columns: 167 against 161).
+RtShape rt_weight_shape(const pmlp* h) {
+  RtShape sh;
+  const int64_t mean = h->N / h->M;
+  const bool gated = h->block && h->block->gated;
+  sh.na = mean > 64 ? 2 : 1;
+  const int64_t tiles = (int64_t)h->M * ((mean + rt_units(sh, gated) - 1) / rt_units(sh, gated)) *
+                        ((h->F + 127) / 128);
+  sh.nb = mean > 64 && h->F > 64 && tiles >= 1024 ? 2 : 1;
+  return sh;
+}
+
+// Whether every slot goes to its model on its own: while the weights they read, each its
+// model's, are 128 MB at most, or the models have three rows each at most.  (us, slot by
+// slot / grouped: 600 models of 1 to 100 units, 100 columns, 4,800 slots 26 / 34, 19,200
+// slots 76 / 37; 200 of 100 to 200 units, 200 columns, 1,200 slots 29 / 28; 48 of 500 to
+// 1,000 units, 1,000 columns, 96 slots 50 / 69, 192 slots 83 / 71; 6,000 of 1 to 100 units,
+// 100 columns, 12,000 slots 57 / 130.)
+bool rt_few(const pmlp* h, int64_t R) {
+  const double weights = 4.0 * h->N / h->M * h->F4 * (h->block && h->block->gated ? 2 : 1);
+  return R * weights <= (double)(128 << 20) || R <= 3 * (int64_t)h->M;
+}
 
 // Where the parts of a routed call's workspace lie.
 struct RtLayout {
@@ -1970,27 +2000,18 @@ RtLayout rt_layout(const pmlp* h, int64_t R, int32_t K, const RtShape& sh, bool 
   p.flag = h->flag;
   p.t.rt = rt_rows(sh);
   p.t.uc = rt_units(sh, gated);
-  p.t.du = p.t.uc;
-  p.t.df = h->F > 64 ? 128 : 64;
+  p.t.du = rt_units(rt_weight_shape(h), gated);
+  p.t.df = 64 * rt_weight_shape(h).nb;
   const int64_t whole = (R + kRtPad - 1) / kRtPad * kRtPad;  // places of a model with every slot
   p.t.part = (int32_t)whole;
   l.items = (R / p.t.rt + groups) * div_up(h->widest, p.t.uc);
   int64_t tiles = 0;
   if (train) {
-    auto count = [&] {
-      tiles = 0;
-      for (int32_t hm : h->hs) tiles += div_up(hm, p.t.du);
-      tiles *= div_up(h->F, p.t.df);
-    };
-    count();
-    if (p.t.df == 128 && tiles < 1024) {  // (more than the device holds at once)
-      p.t.df = 64;
-      count();
-    }
+    for (int32_t hm : h->hs) tiles += (int64_t)div_up(hm, p.t.du) * div_up(h->F, p.t.df);
     // few tiles and many rows: parts of the rows side by side
     if (tiles < 512) {
       const int64_t parts = 1024 / tiles;
-      p.t.part = (int32_t)std::min<int64_t>(whole, std::max<int64_t>(256, (whole / parts + 31) / 32 * 32));
+      p.t.part = (int32_t)std::min<int64_t>(whole, std::max<int64_t>(512, (whole / parts + 31) / 32 * 32));
     }
     // (a model's last part may be short: one more for each model)
     l.jitems = tiles * ((whole + p.t.part - 1) / p.t.part);
@@ -2151,10 +2172,8 @@ int gradients_routed(pmlp* h, const float* X, int32_t B, const int32_t* idx, con
   g.fmask = h->d_fmask;
   g.fmw = h->fmw;
   if (int rc = run(h, KID_GEMM_FWD, [&] { return launch_rt_tile(g.a, sh, true, h->stream); })) return rc;
-  RtShape shw = sh;
-  shw.nb = l.p.t.df / 64;
   const RtJoin j{idx, weight, h->d_seg_off, B, K, h->M, 1, parts, l.p.t.uc / 2, g.a.dwpart, dweight};
-  return run(h, KID_GEMM_BWD, [&] { return launch_rt_weights(g, shw, j, h->stream); });
+  return run(h, KID_GEMM_BWD, [&] { return launch_rt_weights(g, rt_weight_shape(h), j, h->stream); });
 }
 
 // ---- orthogonalised updates ----------------------------------------------------------
@@ -2219,7 +2238,7 @@ int ensure_newton(pmlp* h, int32_t mat) {
   };
   std::vector<int32_t> by_class[kNsClasses], large;
   int32_t nsmall = 0;
-  int64_t tiles = 0;  // of 128, of a product of the large ones
+  int64_t tiles = 0, tiles64 = 0;  // of 128 and of 64, of a product of the large ones
   for (int32_t m = 0; m < h->M; ++m) {
     NsMat& t = mats[m];
     t = NsMat{};
@@ -2255,8 +2274,13 @@ int ensure_newton(pmlp* h, int32_t mat) {
     }
     large.push_back(m);
     tiles += (int64_t)div_up(t.rp, 128) * div_up(t.cp, 128);
+    tiles64 += (int64_t)div_up(t.rp, 64) * div_up(t.cp, 64);
   }
-  if (tiles < 1024) q->tile = 64;
+  // Tiles of 128 take 0.77 of the time of four of 64 (32 matrices of 1,000 x 1,000: 2,942
+  // against 3,841 us) where there are enough of them (4 such matrices, 256 tiles: 705 against
+  // 589; 8: 930 against 999) and the last ones are not too empty (300 of 300 x 300: 1,951
+  // against 1,729).
+  if (tiles < 512 || 16 * tiles > 5 * tiles64) q->tile = 64;
   for (int32_t m : large) {
     NsMat& t = mats[m];
     const int64_t nx = (int64_t)t.rp * t.cp, na = (int64_t)t.rp * t.rp;

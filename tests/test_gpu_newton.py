@@ -55,12 +55,12 @@ def test_input_weights(pm, F, hs, strong):
 
 @pytest.mark.parametrize("F,top", [(100, 100), (128, 128), (9, 128), (140, 70)])
 def test_many_matrices(pm, F, top):
-    """More than 512 small ones go in launches by size."""
-    hs = [1 + (37 * m) % top for m in range(620)] + [150]
+    """More than 2,048 small ones go in launches by size; every ninth is compared."""
+    hs = [1 + (37 * m) % top for m in range(2100)] + [150]
     net = pm.PackedMLP(F, 2, hs, [0] * len(hs))
     G = randn(F + top, sum(hs), F)
     got = net.orthogonalize(G.cuda())
-    check(got, G, blocks(F, hs))
+    check(got, G, blocks(F, hs)[::9] + blocks(F, hs)[-1:])
     assert torch.equal(got, net.orthogonalize(G.cuda()))
 
 

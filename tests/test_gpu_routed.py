@@ -184,6 +184,29 @@ def test_forward_and_gradients(pm, shape, gated):
     p.net.check_routed()
 
 
+# forward passes that group the rows: their slots read more than 128 MB of weights
+GROUPED = [(1000, 3, [70, 200], 300, 1), (531, 5, [250, 1, 40], 700, 1), (131, 16, [64, 128], 3000, 1),
+           (29, 4, [1200], 1300, 1), (999, 2, [33, 520, 64, 700], 90, 3), (40, 10, [600, 260], 23000, 2)]
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("shape", GROUPED, ids=lambda s: "F%d-O%d-M%d-B%d-K%d" % (s[0], s[1], len(s[2]), s[3], s[4]))
+def test_grouped_forward(pm, shape, gated):
+    F, O, hs, B, K = shape
+    p = Pool(pm, F, O, hs, [rr.SMOOTH[(2 * m + F) % len(rr.SMOOTH)] for m in range(len(hs))], gated, seed=B)
+    X = p.rand(B, F)
+    idx, w = p.choices(B, K)
+    idx[1], idx[2] = -1, 0
+    X[1] = float("nan")
+    got = p.forward(X, idx, w)
+    X[1] = 0
+    close(got, p.want(X, idx, w)["Y"], "Y")
+    assert "k_rt_tile" == p.net.kernel_variants()["gemm_fwd"][0]
+    X[1] = float("inf")
+    assert torch.equal(got, p.forward(X, idx, w))
+    p.net.check_routed()
+
+
 @pytest.mark.parametrize("gated", [False, True])
 @pytest.mark.parametrize("B", [2, 200])
 def test_every_activation(pm, gated, B):
@@ -454,7 +477,7 @@ def test_capture_refuses_to_grow(pm):
     graph, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
     with torch.cuda.graph(graph, stream=s):
         with pytest.raises(pm.PmlpError, match="graph capture") as e:
-            p.net.forward_routed(X, idx, w, out=out)
+            p.net.gradients_routed(X, idx, w, dY)
         assert e.value.code == pm.PMLP_ESTATE
         with pytest.raises(pm.PmlpError, match="graph capture"):
             p.net.orthogonalize(G)

@@ -270,7 +270,7 @@ int pmlp_routed_status(pmlp_t h);
  * receives X.  matrix: PMLP_MAT_W1 or PMLP_MAT_V1 (buffers [N, F], model m's matrix its
  * rows), PMLP_MAT_W2 ([O, N], its columns; [O, N2] of a two-hidden-layer pack) or
  * PMLP_MAT_W12 ([K] as pmlp_get_params_deep).  A matrix the pack does not have returns
- * PMLP_ESTATE.  steps in [1, 32] (5 is usual).  fp32; a model whose U is not finite gets
+ * PMLP_ESTATE.  steps in [1, 10] (5 is usual).  fp32; a model whose U is not finite gets
  * NaN, the others what they get without it.  mom_in and mom_out may be the same buffer or
  * both null, out may be G; otherwise the buffers must not overlap. */
 int pmlp_orthogonalize(pmlp_t h, int32_t matrix, const float* G_dev, const float* mom_in_dev,
@@ -282,7 +282,7 @@ int pmlp_orthogonalize(pmlp_t h, int32_t matrix, const float* G_dev, const float
  *   W -= rate_m (decay W + sqrt(max(1, rows / cols)) X),
  * rows x cols the shape of the model's matrix (W1: h_m x F), rate_m = lr, or lr_dev[m] where
  * lr_dev is not null (device, [M]; a non-finite one is reported as by pmlp_train_step_lr).
- * steps in [0, 32]; 0 takes U itself in place of sqrt(..) X: SGD with momentum.  Weights
+ * steps in [0, 10]; 0 takes U itself in place of sqrt(..) X: SGD with momentum.  Weights
  * of features that a model does not see stay zero. */
 int pmlp_muon_step(pmlp_t h, int32_t matrix, const float* G_dev, float* mom_dev, float mu,
                    int32_t nesterov, int32_t steps, float lr, const float* lr_dev, float decay);

@@ -132,6 +132,7 @@ struct PmlpNewton {
   size_t lds[kNsClasses] = {};
 };
 constexpr int kMatrices = 4;  // PMLP_MAT_*
+constexpr int32_t kMaxSteps = 10;  // (rounding grows by up to 1.6 a step once the values are near 1)
 
 // How a batch runs through the fused forward of a block pack: SC samples a workgroup,
 // wpc workgroups of `waves` waves for each SC samples, runs of `run` tiles (BlkMap), so
@@ -1932,16 +1933,16 @@ int check_routed(pmlp* h, const void* X, int32_t B, const void* idx, const void*
 // Tiles of the routed products.  Two 32-row tiles of units a wave for models of more than
 // 256 units on average (48 models of 500 to 1,000 units, 1,000 columns, 64 rows each: 77 us
 // against 104 with one; 200 of 100 to 200, 200 columns: 45 against 40); two of samples where
-// the models have more than 512 rows each and there are tiles for two rounds of the device
-// (the 48 at 1,000 rows: 524 against 608 us, at 64: 103 against 78; 600 models of 1 to 100
-// units, 256 rows: 83 against 77).
+// the models have more than 384 rows each and there are tiles to fill the device (the 48 at
+// 1,000 rows: 524 against 608 us, at 64: 103 against 78; 600 models of 1 to 100 units, 256
+// rows: 83 against 77; gradients of 32 of 500 to 1,000 units, 512 rows: 262 against 288).
 RtShape rt_shape(const pmlp* h, int64_t R) {
   RtShape sh;
   const int64_t mean = h->N / h->M;
   const bool gated = h->block && h->block->gated;
   sh.na = mean > 256 ? 2 : 1;
   const int64_t chunks = (mean + rt_units(sh, gated) - 1) / rt_units(sh, gated);
-  sh.nb = R > (int64_t)512 * h->M && R / 128 * chunks >= 1024 ? 2 : 1;
+  sh.nb = R > (int64_t)384 * h->M && R / 128 * chunks >= 700 ? 2 : 1;
   return sh;
 }
 
@@ -2236,6 +2237,14 @@ int ensure_newton(pmlp* h, int32_t mat) {
       pieces.push_back(NsPiece{m, r, std::min(rows, t.rows - r), 0});
     t.pieces = (int32_t)pieces.size() - t.piece0;
   };
+  auto tile = [&](int32_t m, int32_t i, int32_t j) {
+    NsItem it{};
+    it.mat = m;
+    it.i = i;
+    it.j = j;
+    it.t = mats[m];
+    return it;
+  };
   std::vector<int32_t> by_class[kNsClasses], large;
   int32_t nsmall = 0;
   int64_t tiles = 0, tiles64 = 0;  // of 128 and of 64, of a product of the large ones
@@ -2289,14 +2298,14 @@ int ensure_newton(pmlp* h, int32_t mat) {
     t.ao = sl.na;
     sl.nx += nx;
     sl.na += na;
+    cut(m);
     const int32_t ti = div_up(t.rp, q->tile), tj = div_up(t.cp, q->tile);
     for (int32_t i = 0; i < ti; ++i) {
-      for (int32_t j = 0; j < tj; ++j) load.push_back(NsItem{m, i, j, 0});
-      for (int32_t j = 0; j <= i; ++j) sym.push_back(NsItem{m, i, j, 0});
+      for (int32_t j = 0; j < tj; ++j) load.push_back(tile(m, i, j));
+      for (int32_t j = 0; j <= i; ++j) sym.push_back(tile(m, i, j));
       for (int32_t j = 0; j < div_up(t.cp, ns_step_columns(q->tile)); ++j)
-        step.push_back(NsItem{m, i, j, 0});
+        step.push_back(tile(m, i, j));
     }
-    cut(m);
   }
   if (sl.nx) close();
   q->nlarge = (int32_t)pieces.size();
@@ -3276,7 +3285,7 @@ int pmlp_orthogonalize(pmlp_t h, int32_t matrix, const float* G_dev, const float
   if ((mom_in_dev == nullptr) != (mom_out_dev == nullptr))
     return fail(PMLP_EINVAL, "the momentum needs both of its buffers (or neither)");
   if (!std::isfinite(mu)) return fail(PMLP_EINVAL, "mu must be finite");
-  if (steps < 1 || steps > 32) return fail(PMLP_EINVAL, "steps must be in [1, 32]");
+  if (steps < 1 || steps > kMaxSteps) return fail(PMLP_EINVAL, "steps must be in [1, 10]");
   const size_t n = matrix_bytes(h, matrix);
   const Span g{G_dev, n}, in{mom_in_dev, n}, mo{mom_out_dev, n}, out{out_dev, n};
   if (overlap(mo, g) || overlap(mo, out) || overlap(in, out) ||
@@ -3299,7 +3308,7 @@ int pmlp_muon_step(pmlp_t h, int32_t matrix, const float* G_dev, float* mom_dev,
   if (int rc = check_matrix(h, matrix, G_dev)) return rc;
   if (!std::isfinite(mu) || !std::isfinite(lr) || !std::isfinite(decay))
     return fail(PMLP_EINVAL, "mu, lr and decay must be finite");
-  if (steps < 0 || steps > 32) return fail(PMLP_EINVAL, "steps must be in [0, 32]");
+  if (steps < 0 || steps > kMaxSteps) return fail(PMLP_EINVAL, "steps must be in [0, 10]");
   const size_t n = matrix_bytes(h, matrix);
   if (overlap({G_dev, n}, {mom_dev, n})) return fail(PMLP_EINVAL, "the buffers overlap");
   NsArgs a{};

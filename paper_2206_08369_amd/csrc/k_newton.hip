@@ -63,39 +63,48 @@ hipError_t launch_ns_momentum(const NsArgs& a, int32_t piece0, int32_t pieces, b
 // A 32 x 32 block at a time through LDS, for both orders of X.
 __global__ __launch_bounds__(256) void k_ns_load(NsArgs a, const NsItem* items) {
   __shared__ float block[32][33];
-  const NsItem it = items[blockIdx.x];
-  const NsMat t = a.mats[it.mat];
+  __shared__ double part[4];
+  const NsItem it = ns_item(items, blockIdx.x);
+  const NsMat& t = it.t;
+  const int tid = threadIdx.x;
   double total = 0;
-  for (int q = 0; q < t.pieces; ++q) total += a.sums[t.piece0 + q];
-  const double scale = ns_scale(total) * kScale;
+  for (int q = tid; q < t.pieces; q += 256) total += a.sums[t.piece0 + q];
+  total = wave_total(total);
+  if ((tid & 63) == 0) part[tid >> 6] = total;
+  __syncthreads();
+  const double scale = ns_scale((part[0] + part[1]) + (part[2] + part[3])) * kScale;
   const bool turned = t.rows > t.cols;
-  const int x = threadIdx.x & 31, y0 = threadIdx.x >> 5;
+  const int x = tid & 31, y0 = tid >> 5;        // reading: four rows, one column
+  const int y = tid >> 3, x4 = 4 * (tid & 7);   // storing: one row, four columns
   _Float16 *X = a.X[0] + t.xo, *XT = a.XT[0] + t.xo;
   const int i1 = min(t.rp, (it.i + 1) * a.tile), j1 = min(t.cp, (it.j + 1) * a.tile);
   for (int i0 = it.i * a.tile; i0 < i1; i0 += 32)
     for (int j0 = it.j * a.tile; j0 < j1; j0 += 32) {
-      __syncthreads();
-      for (int y = y0; y < 32; y += 8) {
+      float v[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
         // (along the matrix's rows: X's rows, or its columns)
-        const int gi = (turned ? j0 : i0) + y, gj = (turned ? i0 : j0) + x;
-        float v = 0.f;
-        if (gi < t.rows && gj < t.cols)
-          v = (float)(scale * (double)direction(a, t.src + (int64_t)gi * t.ld + gj));
-        if (turned) block[x][y] = v;
-        else block[y][x] = v;
+        const int gi = (turned ? j0 : i0) + y0 + 8 * q, gj = (turned ? i0 : j0) + x;
+        v[q] = gi < t.rows && gj < t.cols
+                   ? (float)(scale * (double)direction(a, t.src + (int64_t)gi * t.ld + gj))
+                   : 0.f;
       }
       __syncthreads();
-      for (int y = y0; y < 32; y += 8) {
-        _Float16 hi, lo;
-        halve(block[y][x], hi, lo);
-        const int64_t at = (int64_t)(i0 + y) * t.cp + j0 + x;
-        X[at] = hi;
-        X[at + a.nx] = lo;
-        halve(block[x][y], hi, lo);
-        const int64_t to = (int64_t)(j0 + y) * t.rp + i0 + x;
-        XT[to] = hi;
-        XT[to + a.nx] = lo;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (turned) block[x][y0 + 8 * q] = v[q];
+        else block[y0 + 8 * q][x] = v[q];
       }
+      __syncthreads();
+      f16x4 hi, lo;
+      halve(f32x4{block[y][x4], block[y][x4 + 1], block[y][x4 + 2], block[y][x4 + 3]}, hi, lo);
+      _Float16* at = X + (int64_t)(i0 + y) * t.cp + j0 + x4;
+      *(f16x4*)at = hi;
+      *(f16x4*)(at + a.nx) = lo;
+      halve(f32x4{block[x4][y], block[x4 + 1][y], block[x4 + 2][y], block[x4 + 3][y]}, hi, lo);
+      at = XT + (int64_t)(j0 + y) * t.rp + i0 + x4;
+      *(f16x4*)at = hi;
+      *(f16x4*)(at + a.nx) = lo;
     }
 }
 
@@ -127,8 +136,8 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
   // whole matrices, whose tiles share rows in its cache.
   const int at = (blockIdx.x & 7) * ((n + 7) / 8) + (blockIdx.x >> 3);
   if (at >= n) return;
-  const NsItem it = items[at];
-  const NsMat t = a.mats[it.mat];
+  const NsItem it = ns_item(items, at);
+  const NsMat& t = it.t;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wi = wave & 1, wj = wave >> 1;
   const int i0 = it.i * T, j0 = it.j * TJ;
@@ -176,6 +185,23 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
 #pragma unroll
   for (int d = 0; d < DEPTH; ++d)
     if (d * KT < K) load(d, d * KT);
+  // What the product is added to, [j][i]; a small tile has it before its last product.
+  constexpr int LPR = W / 8;         // lanes of 16 bytes to a row of the wave's block
+  constexpr bool AHEAD = T == 64 && WHAT != NS_GRAM && WHAT != NS_LAST;
+  const int bi0 = i0 + wi * W, bw0 = j0 + wj * WJ;  // this wave's block
+  const _Float16* old = WHAT == NS_POLY ? a.A + t.ao : a.XT[from] + t.xo;
+  const int64_t plane = step ? a.nx : a.na;
+  auto old_at = [&](int h, int q, int bj0) {
+    const int r = q * (64 / LPR) + lane / LPR, ch = lane % LPR;
+    const int j = min(bj0 + r, nj - 1), i = min(bi0 + 8 * ch, t.rp - 8);
+    return *(const f16x8*)(old + h * plane + (int64_t)j * t.rp + i);
+  };
+  f16x8 held[2][AHEAD ? CB * LPR / 64 : 1];
+  if (AHEAD)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int q = 0; q < CB * LPR / 64; ++q) held[h][q] = old_at(h, q, bw0);
   for (int k0 = 0; k0 < K; k0 += DEPTH * KT) {
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) {
@@ -219,8 +245,6 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
     }
   }
 
-  // This wave's block: rows bi0 .., columns bj0 .. of C
-  const int bi0 = i0 + wi * W, bw0 = j0 + wj * WJ;
   const int half = 4 * (lane >> 5);
   if (WHAT == NS_LAST) {
     const bool turned = t.rows > t.cols;
@@ -261,11 +285,8 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
   }
   __syncthreads();  // the operands have been read: LDS is the waves' own from here on
   char* block = lds + wave * BLOCK;  // [column][row]
-  constexpr int LPR = W / 8;         // lanes of 16 bytes to a row of the block
-  const int64_t plane = WHAT == NS_STEP ? a.nx : a.na;
   _Float16* to = WHAT == NS_GRAM ? a.A + t.ao : WHAT == NS_POLY ? a.P + t.ao : a.X[1 - from] + t.xo;
   _Float16* tt = WHAT == NS_STEP ? a.XT[1 - from] + t.xo : to;  // [j][i]: stride rp
-  const _Float16* old = WHAT == NS_POLY ? a.A + t.ao : a.XT[from] + t.xo;  // [j][i]
 #pragma unroll
   for (int bi = 0; bi < NT; ++bi)
 #pragma unroll
@@ -281,8 +302,7 @@ __global__ __launch_bounds__(256, 2) void k_ns_product(NsArgs a, int from, const
 #pragma unroll
         for (int q = 0; q < CB * LPR / 64; ++q) {
           const int r = q * (64 / LPR) + lane / LPR, ch = lane % LPR;
-          const int j = min(bj0 + r, nj - 1), i = min(bi0 + 8 * ch, t.rp - 8);
-          *(f16x8*)(block + r * BR + 16 * ch) = *(const f16x8*)(old + h * plane + (int64_t)j * t.rp + i);
+          *(f16x8*)(block + r * BR + 16 * ch) = AHEAD ? held[h][q] : old_at(h, q, bj0);
         }
         __builtin_amdgcn_wave_barrier();
 #pragma unroll

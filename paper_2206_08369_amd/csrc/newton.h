@@ -9,7 +9,7 @@ namespace pmlpk {
 // The quintic whose iteration takes every singular value in (0, 1] towards 1 (Muon:
 // Jordan and others, 2024): x <- x (a + b x^2 + c x^4).
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
-constexpr int32_t kNsPiece = 8192; // entries of a piece of the momentum's pass, about
+constexpr int32_t kNsPiece = 4096; // entries of a piece of the momentum's pass, about
 
 // One model's matrix: rows x cols, with r = min(rows, cols) and c = max(rows, cols); the
 // iteration's X is it, or its transpose where rows > cols.  rp, cp: r and c rounded up to
@@ -26,9 +26,12 @@ struct NsMat {
 struct NsPiece {
   int32_t mat, row0, rows, pad;
 };
+// Tile (i, j) of a matrix, with all that a workgroup wants to know of it.
 struct NsItem {
-  int32_t mat, i, j, pad;  // tile (i, j)
+  int32_t mat, i, j, pad[9];
+  NsMat t;
 };
+static_assert(sizeof(NsItem) == 128, "NsItem layout");
 
 struct NsArgs {
   const NsMat* mats;

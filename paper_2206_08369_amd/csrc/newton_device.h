@@ -30,6 +30,18 @@ __device__ __forceinline__ f32x4 add_held(float f, const f16x4& hi, const f16x4&
   return v;
 }
 
+// A tile, by scalar loads: the list was written before any launch that reads it.
+__device__ __forceinline__ NsItem ns_item(const NsItem* items, int at) {
+  typedef int i32x16 __attribute__((ext_vector_type(16)));
+  struct Two {
+    i32x16 a, b;
+  } v;
+  const auto* p = (const __attribute__((address_space(4))) i32x16*)(items + at);
+  v.a = p[0];
+  v.b = p[1];
+  return __builtin_bit_cast(NsItem, v);
+}
+
 // U at an entry whose momentum is up to date
 __device__ __forceinline__ float direction(const NsArgs& a, int64_t at) {
   const float g = a.G[at];

@@ -185,12 +185,13 @@ __device__ __forceinline__ void small_matrix(const NsArgs& a, const NsMat& t, in
         for (int q = 0; q < 2; ++q)
           acc[q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[b][h == 0], y[b][q][h == 1], acc[q], 0, 0, 0);
     };
-    fetch(0, k0);
+    // (past the last step that again: a branch around the loads would wait for all)
+    if (k0 < k1) fetch(0, k0);
     for (int k = k0; k < k1; k += 2) {
-      if (k + 1 < k1) fetch(1, k + 1);
+      fetch(1, k + 1 < k1 ? k + 1 : k1 - 1);
       multiply(0);
       if (k + 1 >= k1) break;
-      if (k + 2 < k1) fetch(0, k + 2);
+      fetch(0, k + 2 < k1 ? k + 2 : k1 - 1);
       multiply(1);
     }
   };

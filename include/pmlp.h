@@ -480,13 +480,16 @@ const char* pmlp_kernel_name(int32_t k);
  *   PMLP_ARITH_FP32  fp32 matrix-core products,
  *   PMLP_ARITH_X3    fp32 products as six bf16 products of three-piece
  *                    operand splits (fp32 accuracy),
- *   PMLP_ARITH_BF16  bf16 operands, fp32 accumulation.
+ *   PMLP_ARITH_BF16  bf16 operands, fp32 accumulation,
+ *   PMLP_ARITH_F16X2 products of values held as two fp16 halves, three fp16
+ *                    products with fp32 accumulation.
  * Either pointer may be null.  Lets a caller price a kernel against the
  * ceiling of the arithmetic it really ran. */
 #define PMLP_ARITH_NONE 0
 #define PMLP_ARITH_FP32 1
 #define PMLP_ARITH_X3 2
 #define PMLP_ARITH_BF16 3
+#define PMLP_ARITH_F16X2 4
 int pmlp_kernel_variant(pmlp_t h, int32_t k, const char** name, int32_t* arith);
 
 /* Message describing the last failure on the calling thread (a

@@ -28,7 +28,8 @@ __all__ = [
     "PMLP_MSE", "pmlp_train_step_mse", "pmlp_gradients_mse", "pmlp_nonfinite", "pmlp_train_step_noalloc",
     "pmlp_set_feature_mask", "pmlp_get_models", "pmlp_create_deep", "pmlp_gradients_deep",
     "pmlp_get_params_deep", "pmlp_set_params_deep", "pmlp_info_deep", "pmlp_kernel_variant",
-    "PMLP_ARITH_NONE", "PMLP_ARITH_FP32", "PMLP_ARITH_X3", "PMLP_ARITH_BF16", "PackedMLP",
+    "PMLP_ARITH_NONE", "PMLP_ARITH_FP32", "PMLP_ARITH_X3", "PMLP_ARITH_BF16", "PMLP_ARITH_F16X2",
+    "PackedMLP",
     "DeepPackedMLP", "PMLP_GATED", "PMLP_NORM", "pmlp_create_block", "pmlp_gradients_block",
     "pmlp_gradients_block_mse", "pmlp_get_params_block", "pmlp_set_params_block", "BlockPackedMLP",
     "pmlp_route", "pmlp_route_backward", "pmlp_forward_routed", "pmlp_gradients_routed",
@@ -478,7 +479,7 @@ def pmlp_kernel_time(h: int, k: int) -> Tuple[float, int]:
     return ms.value, n.value
 
 
-PMLP_ARITH_NONE, PMLP_ARITH_FP32, PMLP_ARITH_X3, PMLP_ARITH_BF16 = 0, 1, 2, 3
+PMLP_ARITH_NONE, PMLP_ARITH_FP32, PMLP_ARITH_X3, PMLP_ARITH_BF16, PMLP_ARITH_F16X2 = range(5)
 
 
 def pmlp_kernel_variant(h: int, k: int) -> Tuple[str, int]:

@@ -1966,8 +1966,9 @@ RtShape rt_weight_shape(const pmlp* h) {
 // slot / grouped: 600 models of 1 to 100 units, 100 columns, 4,800 slots 26 / 34, 19,200
 // slots 76 / 37; 200 of 100 to 200 units, 200 columns, 1,200 slots 29 / 28; 48 of 500 to
 // 1,000 units, 1,000 columns, 96 slots 50 / 69, 192 slots 83 / 71; 6,000 of 1 to 100 units,
-// 100 columns, 12,000 slots 57 / 130.)
+// 100 columns, 12,000 slots 57 / 130.)  A launch has fewer than 2^24 workgroups of 256.
 bool rt_few(const pmlp* h, int64_t R) {
+  if (R * div_up(h->widest, kRtFewUnits) >= (int64_t)1 << 24) return false;
   const double weights = 4.0 * h->N / h->M * h->F4 * (h->block && h->block->gated ? 2 : 1);
   return R * weights <= (double)(128 << 20) || R <= 3 * (int64_t)h->M;
 }
@@ -2096,7 +2097,6 @@ int forward_routed(pmlp* h, const float* X, int32_t B, const int32_t* idx, const
       return run(h, KID_GEMM_FWD, [&] { return launch_rt_sample(a, f, weight, Y, h->stream); });
     }
     const int32_t chunks = div_up(h->widest, kRtFewUnits);
-    if (R * chunks > INT32_MAX) return too_large();
     Carver c;
     c.take((size_t)R * chunks * h->O);
     if (int rc = ensure_ws(h, &h->extra, c.bytes, "a routed pack")) return rc;

@@ -9,6 +9,8 @@
 // 2^-22 of each product, as fp32 sums of that length do.  (Six bf16 products would hold
 // values of any size; these are normalised.)
 
+#include <algorithm>
+
 #include "newton_device.h"
 
 namespace pmlpk {
@@ -55,9 +57,13 @@ __global__ __launch_bounds__(256) void k_ns_momentum(NsArgs a, int piece0) {
 hipError_t launch_ns_momentum(const NsArgs& a, int32_t piece0, int32_t pieces, bool apply,
                               hipStream_t s) {
   note_variant("k_ns_momentum", kArithNone);
-  if (apply) k_ns_momentum<true><<<(unsigned)pieces, 256, 0, s>>>(a, piece0);
-  else k_ns_momentum<false><<<(unsigned)pieces, 256, 0, s>>>(a, piece0);
-  return hipGetLastError();
+  for (int32_t at = 0; at < pieces; at += kNsGrid) {
+    const unsigned grid = (unsigned)std::min(kNsGrid, pieces - at);
+    if (apply) k_ns_momentum<true><<<grid, 256, 0, s>>>(a, piece0 + at);
+    else k_ns_momentum<false><<<grid, 256, 0, s>>>(a, piece0 + at);
+    if (const hipError_t e = hipGetLastError()) return e;
+  }
+  return hipSuccess;
 }
 
 // A 32 x 32 block at a time through LDS, for both orders of X.
@@ -120,6 +126,11 @@ hipError_t launch_ns_load(const NsArgs& a, const NsItem* items, int32_t n, hipSt
 // T / 2 x TJ / 2.  A and P are symmetric: only tiles with j <= i are computed, and stored
 // twice.  A lane ends with four consecutive rows of a column; a wave's block goes through
 // LDS, where it is read by rows of either order, 16 bytes a lane.
+//
+// Bound by the matrix cores behind LDS and two barriers a stage, and by the stores of both
+// orders: 40 matrices of 500 to 1,000 x 1,000 119 us for A, 101 for P, 237 for a step (193, 181
+// and 194 TFLOP/s of the 355 that three fp16 products at a large library product's rate make;
+// MFMA busy 0.39, 0.39, 0.33).  Steps of 128 x 128 tiles took 254 us where these take 240.
 // ---------------------------------------------------------------------------
 
 template <int WHAT, int T, int TJ>
@@ -375,7 +386,7 @@ void product(const NsArgs& a, int what, int from, const NsItem* items, int n, hi
 
 hipError_t launch_ns_product(const NsArgs& a, int what, int from, const NsItem* items, int32_t n,
                              hipStream_t s) {
-  note_variant("k_ns_product", kArithX3);
+  note_variant("k_ns_product", kArithF16x2);
   if (a.tile == 64) product<64, 64>(a, what, from, items, n, s);
   else product<128, 256>(a, what, from, items, n, s);
   return hipGetLastError();

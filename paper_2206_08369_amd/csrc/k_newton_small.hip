@@ -14,6 +14,8 @@
 // Bound by LDS reads and latency: a 2 x 4 block of tiles reads 12 fragments for its 24
 // matrix instructions, what one LDS feeds four SIMDs with.
 
+#include <algorithm>
+
 #include "newton_device.h"
 
 namespace pmlpk {
@@ -362,12 +364,15 @@ __global__ __launch_bounds__(512, 2) void k_ns_small_any(NsArgs a, const int32_t
 hipError_t launch_ns_small(const NsArgs& a, int cls, size_t lds, const int32_t* list, int32_t n,
                            int32_t steps, hipStream_t s) {
   auto go = [&](auto fn, int nw) {
-    note_variant(cls < 8 ? "k_ns_small" : "k_ns_small_any", kArithX3);
+    note_variant(cls < 8 ? "k_ns_small" : "k_ns_small_any", kArithF16x2);
     if (const hipError_t e = hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize,
                                                  (int)kNsSmallLds))
       return e;
-    fn<<<(unsigned)n, 64 * nw, lds, s>>>(a, list, steps);
-    return hipGetLastError();
+    for (int32_t at = 0; at < n; at += kNsGrid) {
+      fn<<<(unsigned)std::min(kNsGrid, n - at), 64 * nw, lds, s>>>(a, list + at, steps);
+      if (const hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
   };
   switch (cls) {
     case 0: return go(k_ns_small<1, 4>, kNsWaves[0]);

@@ -131,7 +131,15 @@ __device__ __forceinline__ int die_order(int i, int n) {
 // Z (and U) of a chunk of units and a block of rows of one model, then the activation and
 // either the sums over the units with W2 (forward) or the hidden gradients (TRAIN).
 // Units are the first operand's rows and samples the second's: a lane has one sample and
-// 16 units of every tile.
+// 16 units of every tile.  (So a sample's sums over units are within a lane but for one swap,
+// and its hidden values are stored in lines of 32 places.)
+//
+// Bound by the matrix cores and the vector work of splitting beside them: an operand's value is
+// cut into pieces once a stage (some 11 instructions for two) and meets 64 or 128 rows of the
+// other.  48 gated models of 500 to 1,000 units, 1,000 columns, 16,384 samples of four choices:
+// 1,330 us, 145 TFLOP/s of the 187 that six bf16 products at a large library product's rate
+// make; MFMA busy 0.49 and VALU 0.40.  Two workgroups a compute unit take turns: one that has
+// two stages in LDS and cuts the next between the products of the last took 2,000 us.
 template <int NA, int NB, bool GATED, bool TRAIN>
 __global__ __launch_bounds__(256, 2) void k_rt_tile(RtArgs a) {
   constexpr int RA = 64 * NA, RB = 64 * NB, UC = GATED ? 64 : RA, NU = GATED ? 1 : NA;
@@ -356,7 +364,9 @@ hipError_t launch_rt_tile(const RtArgs& a, const RtShape& sh, bool train, hipStr
 
 // ---------------------------------------------------------------------------
 // Few slots, each straight from its index.  A wave takes 16 units of the slot's model, four at
-// a time, 16 lanes along the columns of each: bound by the weights' read, or by launches.
+// a time, 16 lanes along the columns of each: bound by the weights' read, or by launches (32
+// requests to 6,000 gated models of 1 to 100 units, four each: 5.6 us, and 3.4 for the join;
+// 2,331 slots of 1 to 250 units, 37 columns: 21 us, the chain of the widest models).
 // ---------------------------------------------------------------------------
 
 namespace {
@@ -494,7 +504,8 @@ hipError_t launch_rt_few(const RtArgs& a, const RtFew& f, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------------------
-// Sums over a model's parts, in order.
+// Sums over a model's parts, in order.  (32 requests of four choices 3 us, 65,536 slots of up
+// to 32 parts of ten sums 50: a chain of loads a thread.)
 // ---------------------------------------------------------------------------
 
 namespace {
@@ -553,7 +564,7 @@ __device__ __forceinline__ void weight_tiles(const RtGrad& g, char* lds, int blo
   const int n = *g.njitems;
   // (In the list's order, dies in turn: the tiles of a model with many rows, which take
   // longest, are spread over all of them.  32 models of 500 to 1,000 units on 16,384 rows: 415
-  // us where each die took a run of the list, XXX so.)
+  // us where each die took a run of the list, 278 so.)
   for (int at = block; at < n; at += blocks) {
     const RtItem item = item_at(g.jitems, at);
     const int m = item.m;
@@ -749,6 +760,12 @@ __device__ __forceinline__ void output_weights(const RtGrad& g, f32x4* sums, int
 
 // All that the hidden gradients lead to, side by side: the first `tiles` workgroups take tiles
 // of the input weights' gradients, the next `outs` the output weights', the rest the slots'.
+// (Three launches before: 600 models of 1 to 100 units, 32,768 slots 139 us a call, 127 so.)
+//
+// Bound as k_rt_tile, by the matrix cores and the cutting beside them, with the tails of models
+// of unlike numbers of rows: 32 models of 500 to 1,000 units, 1,000 columns, 16,384 slots 298
+// us, of which the products need 131 at the rate of k_rt_tile's comment; MFMA busy 0.32.  The
+// 600 small ones take 55 us, by how long a tile's chain of loads, cuts and products is.
 template <int NA, int NB, bool GATED>
 __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g, RtJoin j, int tiles, int outs) {
   __shared__ __align__(16) char lds[DwTile<NA, NB, GATED>::kBytes];

@@ -10,6 +10,7 @@ namespace pmlpk {
 // Jordan and others, 2024): x <- x (a + b x^2 + c x^4).
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr int32_t kNsPiece = 4096; // entries of a piece of the momentum's pass, about
+constexpr int32_t kNsGrid = 1 << 21;  // workgroups of a launch, at most (2^32 threads are too many)
 
 // One model's matrix: rows x cols, with r = min(rows, cols) and c = max(rows, cols); the
 // iteration's X is it, or its transpose where rows > cols.  rp, cp: r and c rounded up to

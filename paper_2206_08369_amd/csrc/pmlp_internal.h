@@ -47,7 +47,8 @@ inline KernelVariant& last_variant() {
   return v;
 }
 inline void note_variant(const char* name, int32_t arith) { last_variant() = KernelVariant{name, arith}; }
-constexpr int32_t kArithNone = 0, kArithFp32 = 1, kArithX3 = 2, kArithBf16 = 3;
+constexpr int32_t kArithNone = 0, kArithFp32 = 1, kArithX3 = 2, kArithBf16 = 3,
+                  kArithF16x2 = 4;
 
 // GEMM epilogues: C[p][q] = sum_k P[p][k] Q[q][k]
 enum GemmEpi {

@@ -271,6 +271,35 @@ def test_many_models(pm, M):
         close(got[k], want[k], k)
 
 
+def test_more_slots_than_a_launch_has_workgroups(pm):
+    # 3,600,000 slots of models of one unit, and one of 300: slot by slot they were 18 million
+    # workgroups of 256 threads, more than a launch may have
+    M, K, B, F, wide = 1_200_000, 4, 900_000, 4, 300
+    pack = Pool(pm, F, 2, [1] * (M - 1) + [wide], [0] * M, False, seed=5)
+    X = pack.rand(B, F)
+    idx, w = pack.choices(B, K)
+    idx[::1000, 1] = M - 1
+    got = pack.forward(X, idx, w).cpu().double()
+    Y, bound = torch.zeros(B, 2).double(), torch.zeros(B, 2).double()
+    W1, W2, Xd = pack.W1.double(), pack.W2.double(), X.double()
+
+    def add(b, units, weight):  # samples b, their slots' units [len(b), n]: the identity's sums
+        z, r = ((Xd[b][:, None] * W1[units]).sum(2), (Xd[b][:, None] * W1[units]).abs().sum(2))
+        e = 2 * (F + 8) * rr.U * r + rr.ACT_ABS + rr.ACT_REL * z.abs()
+        for o in range(2):
+            v = W2[o][units]
+            Y[b, o] += weight * (z * v).sum(1)
+            bound[b, o] += weight.abs() * ((e * v.abs()).sum(1) + (2 * (units.shape[1] + 8) + K + 2)
+                                           * rr.U * (z * v).abs().sum(1))
+    for k in range(K):
+        i, wk = idx[:, k].long(), w[:, k].double()
+        b = torch.nonzero((i >= 0) & (i < M - 1)).reshape(-1)
+        add(b, i[b][:, None], wk[b])
+        b = torch.nonzero(i == M - 1).reshape(-1)
+        add(b, torch.arange(M - 1, M - 1 + wide).repeat(len(b), 1), wk[b])
+    close(got, (Y, bound))
+
+
 @pytest.mark.parametrize("gated,lo,hi", [(False, 1, 9), (True, 1, 9), (False, 60, 90)])
 def test_many_tiles(pm, gated, lo, hi):
     """Enough tiles of the weight gradients for the wider ones."""

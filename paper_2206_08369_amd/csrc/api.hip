@@ -1962,15 +1962,17 @@ RtShape rt_weight_shape(const pmlp* h) {
 }
 
 // Whether every slot goes to its model on its own: while the weights they read, each its
-// model's, are 128 MB at most, or the models have three rows each at most.  (us, slot by
-// slot / grouped: 600 models of 1 to 100 units, 100 columns, 4,800 slots 26 / 34, 19,200
-// slots 76 / 37; 200 of 100 to 200 units, 200 columns, 1,200 slots 29 / 28; 48 of 500 to
-// 1,000 units, 1,000 columns, 96 slots 50 / 69, 192 slots 83 / 71; 6,000 of 1 to 100 units,
-// 100 columns, 12,000 slots 57 / 130.)  A launch has fewer than 2^24 workgroups of 256.
+// model's, are 128 MB at most, with 1.5 KB for a slot and 0.4 for an output of it, or the
+// models have three rows each at most.  (us, slot by slot / grouped: 600 gated models of 1 to
+// 100 units, 100 columns, 4,096 slots 35 / 40, 8,192 slots 59 / 42; 200 of 100 to 200 units, 200
+// columns, 1,024 slots 23 / 30, 2,048 slots 37 / 31; 60 of 1 to 10 units, ten columns, 32,768
+// slots 16 / 23, 131,072 slots 51 / 41; 300 of 20 to 60, 20 columns, 16 outputs, 8,192 slots 22 /
+// 26, 16,384 slots 36 / 27; 6,000 of 1 to 100, 100 columns, 16,384 slots 68 / 138, 131,072 slots
+// 474 / 157.)  A launch has fewer than 2^24 workgroups of 256.
 bool rt_few(const pmlp* h, int64_t R) {
   if (R * div_up(h->widest, kRtFewUnits) >= (int64_t)1 << 24) return false;
   const double weights = 4.0 * h->N / h->M * h->F4 * (h->block && h->block->gated ? 2 : 1);
-  return R * weights <= (double)(128 << 20) || R <= 3 * (int64_t)h->M;
+  return R * (weights + 1500 + 400 * h->O) <= (double)(128 << 20) || R <= 3 * (int64_t)h->M;
 }
 
 // Where the parts of a routed call's workspace lie.
@@ -2010,10 +2012,11 @@ RtLayout rt_layout(const pmlp* h, int64_t R, int32_t K, const RtShape& sh, bool 
   int64_t tiles = 0;
   if (train) {
     for (int32_t hm : h->hs) tiles += (int64_t)div_up(hm, p.t.du) * div_up(h->F, p.t.df);
-    // few tiles and many rows: parts of the rows side by side
+    // few tiles and many rows: parts of the rows side by side (nine models of 40 to 300 units,
+    // 61 columns, 19,998 slots: parts of 320 places 32 us, of 512 37)
     if (tiles < 512) {
       const int64_t parts = 1024 / tiles;
-      p.t.part = (int32_t)std::min<int64_t>(whole, std::max<int64_t>(512, (whole / parts + 31) / 32 * 32));
+      p.t.part = (int32_t)std::min<int64_t>(whole, std::max<int64_t>(256, (whole / parts + 31) / 32 * 32));
     }
     // (a model's last part may be short: one more for each model)
     l.jitems = tiles * ((whole + p.t.part - 1) / p.t.part);

@@ -1,5 +1,7 @@
 // Products of routed packs: each model's rows of the batch with its own weights.
 
+#include <algorithm>
+
 #include "block_device.h"
 #include "routed.h"
 
@@ -365,26 +367,58 @@ hipError_t launch_rt_tile(const RtArgs& a, const RtShape& sh, bool train, hipStr
 // ---------------------------------------------------------------------------
 // Few slots, each straight from its index.  A wave takes 16 units of the slot's model, four at
 // a time, 16 lanes along the columns of each: bound by the weights' read, or by launches (32
-// requests to 6,000 gated models of 1 to 100 units, four each: 5.6 us, and 3.4 for the join;
-// 2,331 slots of 1 to 250 units, 37 columns: 21 us, the chain of the widest models).
+// requests to 6,000 gated models of 1 to 100 units, four each: 4.6 us, and 3.3 for the join).
+// A unit's sum ends in one of its lanes, which takes the activation and the product with W2
+// (where all 16 lanes took both, 2,331 slots of 1 to 250 units, 37 columns took 17.5 us, 10.2
+// so).
 // ---------------------------------------------------------------------------
 
 namespace {
 
-// Units n0 + 4 i + lane / 16 for the sample x, those from `end` on 0 (the same in all 16
-// lanes of a unit).
-template <bool GATED>
-__device__ __forceinline__ void few_units(const RtArgs& a, const float* x, int64_t n0, int64_t end, int act,
-                                          float (&h)[4]) {
-  const int lane = threadIdx.x & 63, li = lane & 15, lu = lane >> 4;
-  float z[4] = {}, u[4] = {};
-  const float *w[4], *v[4];
+template <int CTRL>
+__device__ __forceinline__ float dpp_move(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+
+// Sums over 16 lanes of each of NI = 4 or 16 values, value li % NI to lane li: a lane keeps the
+// half with its bit and gives the other to the lane that keeps that.
+template <int CTRL, int N>
+__device__ __forceinline__ void give_half(bool upper, const float (&v)[N], float (&to)[N / 2]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t n = n0 + 4 * i + lu < end ? n0 + 4 * i + lu : end - 1;
-    w[i] = a.W1 + n * a.F4;
-    v[i] = GATED ? a.V1 + n * a.F4 : nullptr;
-  }
+  for (int j = 0; j < N / 2; ++j)
+    to[j] = (upper ? v[j + N / 2] : v[j]) + dpp_move<CTRL>(upper ? v[j] : v[j + N / 2]);
+}
+__device__ __forceinline__ float scatter_sums(const float (&v)[4]) {
+  const int li = threadIdx.x & 15;
+  float b[2], c[1];
+  give_half<0x4e>(li & 2, v, b);  // lane ^ 2
+  give_half<0xb1>(li & 1, b, c);  // lane ^ 1
+  const float t = dpp_add<0x128, 0xf>(c[0]);  // row_ror:8
+  return dpp_add<0x124, 0xf>(t);              // row_ror:4
+}
+__device__ __forceinline__ float scatter_sums(const float (&v)[16]) {
+  const int li = threadIdx.x & 15;
+  float a[8], b[4], c[2], d[1];
+  give_half<0x128>(li & 8, v, a);  // row_ror:8, lane ^ 8
+  give_half<0x141>(li & 4, a, b);  // row_half_mirror, lane ^ 7
+  give_half<0x4e>(li & 2, b, c);
+  give_half<0xb1>(li & 1, c, d);
+  return d[0];
+}
+
+// Unit few_unit(n0) of the NI * 4 from n0 on for the sample x, 0 from `end` on.
+template <int NI>
+__device__ __forceinline__ int64_t few_unit(int64_t n0) {
+  const int lane = threadIdx.x & 63;
+  return n0 + 4 * (lane & (NI - 1)) + (lane >> 4);
+}
+template <bool GATED, int NI>
+__device__ __forceinline__ float few_units(const RtArgs& a, const float* x, int64_t n0, int64_t end, int act) {
+  const int lane = threadIdx.x & 63, li = lane & 15, lu = lane >> 4;
+  float z[NI] = {}, u[NI] = {};
+  int64_t w[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) w[i] = (n0 + 4 * i + lu < end ? n0 + 4 * i + lu : end - 1) * a.F4;
   for (int k = 4 * li; k < a.F4; k += 64) {
     f32x4 xv{0.f, 0.f, 0.f, 0.f};
     if (k + 4 <= a.F) xv = load_any4(x + k);
@@ -393,42 +427,65 @@ __device__ __forceinline__ void few_units(const RtArgs& a, const float* x, int64
       for (int j = 0; j < 4; ++j)
         if (k + j < a.F) xv[j] = x[k + j];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f32x4 wv = *(const f32x4*)(w[i] + k);
+    for (int i = 0; i < NI; ++i) {
+      const f32x4 wv = *(const f32x4*)(a.W1 + w[i] + k);
 #pragma unroll
       for (int j = 0; j < 4; ++j) z[i] = fmaf(wv[j], xv[j], z[i]);
       if (GATED) {
-        const f32x4 vv = *(const f32x4*)(v[i] + k);
+        const f32x4 vv = *(const f32x4*)(a.V1 + w[i] + k);
 #pragma unroll
         for (int j = 0; j < 4; ++j) u[i] = fmaf(vv[j], xv[j], u[i]);
       }
     }
   }
+  const float zs[1] = {scatter_sums(z)};
+  float h[1];
+  blk_acts<1>(act, zs, h);
+  if (GATED) h[0] *= scatter_sums(u);
+  return few_unit<NI>(n0) < end ? h[0] : 0.f;
+}
+
+// W2 at the lane's unit, of outputs o0 .. o0 + 3 (NI = 16), or of li / 4, 4 + li / 4 .. (NI = 4)
+template <int NI>
+__device__ __forceinline__ void few_w2(const RtArgs& a, int64_t n0, int64_t end, int o0, float (&w)[4]) {
+  const int64_t n = few_unit<NI>(n0) < end ? few_unit<NI>(n0) : end - 1;
+  const int o = NI == 16 ? o0 : (threadIdx.x & 15) >> 2;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {  // sums end in lane 15 of each 16
-    z[i] = __shfl(group_sum_to_last(z[i], 16), lane | 15);
-    if (GATED) u[i] = __shfl(group_sum_to_last(u[i], 16), lane | 15);
-  }
-  blk_acts<4>(act, z, h);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (GATED) h[i] *= u[i];
-    if (n0 + 4 * i + lu >= end) h[i] = 0.f;
+  for (int q = 0; q < 4; ++q) {
+    const int oq = o + (NI == 16 ? 1 : 4) * q;
+    w[q] = a.W2[(int64_t)(oq < a.O ? oq : a.O - 1) * a.ldw + n];
   }
 }
 
-// Their sum with W2's row o, in every lane.
-__device__ __forceinline__ float few_output(const RtArgs& a, int o, int64_t n0, int64_t end,
-                                            const float (&h)[4]) {
-  const int lu = (threadIdx.x & 63) >> 4;
-  float t = 0.f;
+// The units' sums with W2, lane o's output o's; w: what few_w2 gives for o0 = 0.
+template <int NI>
+__device__ __forceinline__ float few_output(const RtArgs& a, int64_t n0, int64_t end, float h, float (&w)[4]) {
+  const int lane = threadIdx.x & 63;
+  const bool there = few_unit<NI>(n0) < end;
+  float y = 0.f;
+  if (NI == 16) {
+    for (int o0 = 0; o0 < a.O; o0 += 4) {
+      if (o0) few_w2<NI>(a, n0, end, o0, w);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t n = n0 + 4 * i + lu;
-    if (n < end) t = fmaf(h[i], a.W2[(int64_t)o * a.ldw + n], t);
+      for (int q = 0; q < 4; ++q) {
+        const float t = group_sum_to_last(there ? h * w[q] : 0.f, 64);
+        const float all = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(t), 63));
+        if (lane == o0 + q) y = all;
+      }
+    }
+    return y;
   }
-  t += __shfl_xor(t, 16);
-  return t + __shfl_xor(t, 32);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if (4 * q >= a.O) break;
+    float t = there ? h * w[q] : 0.f;
+    t += dpp_move<0xb1>(t);
+    t += dpp_move<0x4e>(t);
+    t += __shfl_xor(t, 16);
+    t += __shfl_xor(t, 32);
+    if ((lane & 3) == q) y = t;
+  }
+  return __shfl(y, 4 * (lane & 3) + ((lane >> 2) & 3));
 }
 
 }  // namespace
@@ -447,16 +504,38 @@ __global__ __launch_bounds__(256) void k_rt_few(RtArgs a, RtFew f) {
   const int64_t n0 = first + (int64_t)chunk * kRtFewUnits + 16 * wave;
   if (first + (int64_t)chunk * kRtFewUnits >= end) return;
   __shared__ float sums[4][kRtMaxO];
-  float h[4];
-  few_units<GATED>(a, a.X + (int64_t)(s / a.K) * a.F, n0, end, a.act[m], h);
-  for (int o = 0; o < a.O; ++o) {
-    const float t = few_output(a, o, n0, end, h);
-    if (lane == 0) sums[wave][o] = t;
-  }
+  float w2[4];
+  few_w2<4>(a, n0, end, 0, w2);
+  const float h = few_units<GATED, 4>(a, a.X + (int64_t)(s / a.K) * a.F, n0, end, a.act[m]);
+  const float t = few_output<4>(a, n0, end, h, w2);
+  if (lane < kRtMaxO) sums[wave][lane] = t;
   __syncthreads();
   if (tid < a.O)
     a.part[((int64_t)s * a.parts + chunk) * a.O + tid] =
         (sums[0][tid] + sums[1][tid]) + (sums[2][tid] + sums[3][tid]);
+}
+
+// .. and a wave, for up to 64 columns and 1,024 such chunks or more.  (130 models of 1 to 250
+// units, 37 columns, 2,048 slots 12.7 us against 18.0, 256 slots the same; 200 of 100 to 200, 200
+// columns, 1,024 slots 27.5 against 23.4.)
+template <bool GATED>
+__global__ __launch_bounds__(256) void k_rt_few_waves(RtArgs a, RtFew f) {
+  const int lane = threadIdx.x & 63;
+  const int64_t q = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (q >= (int64_t)f.R * f.chunks) return;
+  const int s = (int)(q / f.chunks), chunk = (int)(q % f.chunks);
+  const int m = f.idx[s];
+  if (m < 0 || m >= a.M) {
+    if (m != -1 && lane == 0 && chunk == 0) f.flag[3] = 1;
+    return;
+  }
+  const int64_t end = a.seg_off[m + 1], n0 = a.seg_off[m] + (int64_t)chunk * kRtFewUnits;
+  if (n0 >= end) return;
+  float w2[4];
+  few_w2<16>(a, n0, end, 0, w2);
+  const float h = few_units<GATED, 16>(a, a.X + (int64_t)(s / a.K) * a.F, n0, end, a.act[m]);
+  const float t = few_output<16>(a, n0, end, h, w2);
+  if (lane < a.O) a.part[q * a.O + lane] = t;
 }
 
 // A sample a workgroup, its models' units in turn over the waves: Y without a second launch.
@@ -465,7 +544,7 @@ __global__ __launch_bounds__(256) void k_rt_sample(RtArgs a, RtFew f, const floa
   const int64_t b = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   __shared__ float sums[4][kRtMaxO];
-  float y = 0.f;  // lane o: output o
+  float y = 0.f;  // lane o < 16: output o
   for (int q = wave; q < a.K * f.chunks; q += 4) {
     const int k = q / f.chunks, m = f.idx[b * a.K + k];
     if (m < 0 || m >= a.M) {
@@ -474,13 +553,11 @@ __global__ __launch_bounds__(256) void k_rt_sample(RtArgs a, RtFew f, const floa
     }
     const int64_t end = a.seg_off[m + 1], n0 = a.seg_off[m] + 16 * (q % f.chunks);
     if (n0 >= end) continue;
-    float h[4];
-    few_units<GATED>(a, a.X + b * a.F, n0, end, a.act[m], h);
+    float w2[4];
+    few_w2<4>(a, n0, end, 0, w2);
     const float w = weight[b * a.K + k];
-    for (int o = 0; o < a.O; ++o) {
-      const float t = few_output(a, o, n0, end, h);
-      if (lane == o) y = fmaf(w, t, y);
-    }
+    const float h = few_units<GATED, 4>(a, a.X + b * a.F, n0, end, a.act[m]);
+    y = fmaf(w, few_output<4>(a, n0, end, h, w2), y);
   }
   if (lane < kRtMaxO) sums[wave][lane] = y;
   __syncthreads();
@@ -496,9 +573,13 @@ hipError_t launch_rt_sample(const RtArgs& a, const RtFew& f, const float* weight
 }
 
 hipError_t launch_rt_few(const RtArgs& a, const RtFew& f, hipStream_t s) {
-  note_variant("k_rt_few", kArithNone);
   const unsigned grid = (unsigned)(f.R * f.chunks);
-  if (a.V1) k_rt_few<true><<<grid, 256, 0, s>>>(a, f);
+  const bool waves = grid >= 1024 && a.F4 <= 64;
+  note_variant(waves ? "k_rt_few_waves" : "k_rt_few", kArithNone);
+  if (waves) {
+    if (a.V1) k_rt_few_waves<true><<<(grid + 3) / 4, 256, 0, s>>>(a, f);
+    else k_rt_few_waves<false><<<(grid + 3) / 4, 256, 0, s>>>(a, f);
+  } else if (a.V1) k_rt_few<true><<<grid, 256, 0, s>>>(a, f);
   else k_rt_few<false><<<grid, 256, 0, s>>>(a, f);
   return hipGetLastError();
 }
@@ -701,8 +782,9 @@ __device__ __forceinline__ void output_weights(const RtGrad& g, f32x4* sums, int
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = *g.njitems, nf = (a.F + g.t.df - 1) / g.t.df;
-  for (int it = block; it < n; it += blocks) {
-    const RtItem item = item_at(g.jitems, it);
+  const int each = (g.t.du / 16 + nf - 1) / nf;  // runs of 16 units to an item, at most
+  for (int64_t it = block; it < (int64_t)n * each; it += blocks) {
+    const RtItem item = item_at(g.jitems, (int)(it / each));
     const int64_t first = item.first;
     const int h = item.h, end = (item.a + 1) * g.t.du < h ? (item.a + 1) * g.t.du : h;
     const int places = item.places;
@@ -710,7 +792,8 @@ __device__ __forceinline__ void output_weights(const RtGrad& g, f32x4* sums, int
     float* out = places > g.t.part ? g.w2part + (int64_t)item.c * a.O * g.N : g.dW2;
     const float* wd = g.wdy + (int64_t)(li < a.O ? li : a.O - 1) * a.P + item.place + 4 * lk;
     // the tile's units in turn over its column tiles (not always on the same die)
-    for (int u0 = item.a * g.t.du + 16 * ((item.b + item.a + item.c) % nf); u0 < end; u0 += 16 * nf) {
+    const int u0 = item.a * g.t.du + 16 * ((item.b + item.a + item.c) % nf + nf * (int)(it % each));
+    if (u0 < end) {
       const int u = u0 + li < h ? u0 + li : h - 1;
       const float* hrow = a.H + item.zoff + (int64_t)u * 32 + 4 * lk;
       f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
@@ -812,8 +895,9 @@ __global__ __launch_bounds__(256) void k_rt_sum_parts(RtGrad g) {
 hipError_t launch_rt_weights(const RtGrad& g, const RtShape& sh, const RtJoin& j, hipStream_t s) {
   note_variant("k_rt_dw", kArithX3);
   const int tiles = (int)groups_for(g.jmost);
-  const unsigned grid = 2 * tiles + (unsigned)ceil_div_i((int64_t)j.B * j.K, 256);
-#define PMLP_RT_DW(NA, NB, G) k_rt_dw<NA, NB, G><<<grid, 256, 0, s>>>(g, j, tiles, tiles)
+  const int outs = (int)groups_for((int64_t)g.jmost * std::max(1, g.t.du / 16 * g.t.df / g.a.F));
+  const unsigned grid = tiles + outs + (unsigned)ceil_div_i((int64_t)j.B * j.K, 256);
+#define PMLP_RT_DW(NA, NB, G) k_rt_dw<NA, NB, G><<<grid, 256, 0, s>>>(g, j, tiles, outs)
   if (g.a.V1) {
     if (sh.nb == 2) PMLP_RT_DW(2, 2, true);
     else PMLP_RT_DW(2, 1, true);

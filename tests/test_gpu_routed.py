@@ -184,7 +184,7 @@ def test_forward_and_gradients(pm, shape, gated):
     p.net.check_routed()
 
 
-# forward passes that group the rows: their slots read more than 128 MB of weights
+# forward passes that group the rows: their slots read more than 128 MB
 GROUPED = [(1000, 3, [70, 200], 300, 1), (531, 5, [250, 1, 40], 700, 1), (131, 16, [64, 128], 3000, 1),
            (29, 4, [1200], 1300, 1), (999, 2, [33, 520, 64, 700], 90, 3), (40, 10, [600, 260], 23000, 2)]
 
@@ -204,6 +204,34 @@ def test_grouped_forward(pm, shape, gated):
     assert "k_rt_tile" == p.net.kernel_variants()["gemm_fwd"][0]
     X[1] = float("inf")
     assert torch.equal(got, p.forward(X, idx, w))
+    p.net.check_routed()
+
+
+# .. and that do not: a wave to 64 units of a slot (up to 64 columns), or a workgroup
+SLOTS = [(37, 3, [250, 1, 66, 130], 500, 2, "k_rt_few_waves"), (64, 16, [300, 64, 65], 400, 1, "k_rt_few_waves"),
+         (3, 2, [1030], 80, 1, "k_rt_few_waves"), (4, 5, [17, 16, 700, 2], 111, 16, "k_rt_few_waves"),
+         (65, 4, [250, 1, 66, 130], 500, 2, "k_rt_few"), (37, 9, [300, 64, 65], 40, 2, "k_rt_few")]
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("shape", SLOTS, ids=lambda s: "F%d-O%d-M%d-B%d-K%d" % (s[0], s[1], len(s[2]), s[3], s[4]))
+def test_slot_by_slot_forward(pm, shape, gated):
+    F, O, hs, B, K, kernel = shape
+    p = Pool(pm, F, O, hs, [rr.SMOOTH[(2 * m + F) % len(rr.SMOOTH)] for m in range(len(hs))], gated, seed=B)
+    X = p.rand(B, F)
+    idx, w = p.choices(B, K)
+    idx[1], idx[2] = -1, 0
+    X[1] = float("nan")
+    got = p.forward(X, idx, w)
+    X[1] = 0
+    close(got, p.want(X, idx, w)["Y"], "Y")
+    assert kernel == p.net.kernel_variants()["gemm_fwd"][0]
+    # units of an infinite output weight behind a model's last one add nothing to it
+    if len(hs) > 1:
+        first = p.choices(B, K, unused=0)[0] * 0
+        p.W2[:, hs[0]] = float("inf")
+        p.put()
+        assert bool(torch.isfinite(p.forward(X, first, w)).all())
     p.net.check_routed()
 
 

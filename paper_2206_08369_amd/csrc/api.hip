@@ -2313,14 +2313,20 @@ int ensure_newton(pmlp* h, int32_t mat) {
   if (sl.nx) close();
   q->nlarge = (int32_t)pieces.size();
   std::vector<int32_t> list;
-  for (int k = 0; nsmall <= kNsOneLaunch && k + 1 < kNsClasses; ++k) {
-    by_class[kNsClasses - 1].insert(by_class[kNsClasses - 1].end(), by_class[k].begin(), by_class[k].end());
-    by_class[k].clear();
+  if (nsmall <= kNsOneLaunch) {
+    std::vector<int32_t> all;
+    bool low = true;
+    for (std::vector<int32_t>& v : by_class) {
+      for (int32_t m : v) low &= ns_low(mats[m].r, mats[m].c);
+      all.insert(all.end(), v.begin(), v.end());
+      v.clear();
+    }
+    by_class[low ? kNsLow : kNsAny] = std::move(all);
   }
   for (int k = 0; k < kNsClasses; ++k) {
     std::vector<int32_t>& v = by_class[k];
     for (int32_t m : v)
-      q->lds[k] = std::max(q->lds[k], ns_small_lds(mats[m].r, mats[m].c, k < 8 ? kNsWaves[k] : 8));
+      q->lds[k] = std::max(q->lds[k], ns_small_lds(mats[m].r, mats[m].c, kNsWaves[k]));
     std::stable_sort(v.begin(), v.end(), [&](int32_t x, int32_t y) {
       return (int64_t)mats[x].r * mats[x].cp > (int64_t)mats[y].r * mats[y].cp;
     });

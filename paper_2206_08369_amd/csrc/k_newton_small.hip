@@ -345,6 +345,16 @@ __global__ __launch_bounds__(64 * kNsWaves[TR - 1], OCC) void k_ns_small(NsArgs 
   small_matrix<TR, NW, 1, (all + kAhead - 1) / kAhead * kAhead>(a, t, steps, lds, total);
 }
 
+// Few rows and many columns.
+__global__ __launch_bounds__(64 * kNsWaves[kNsLow], 4) void k_ns_low(NsArgs a, const int32_t* list, int steps) {
+  constexpr int NW = kNsWaves[kNsLow];
+  extern __shared__ __align__(16) char lds[];
+  __shared__ double total[NW];
+  const NsMat t = a.mats[list[blockIdx.x]];
+  if (t.r <= 16) small_matrix<1, NW, 512 / 32 / NW, 16 * 512 / (64 * NW)>(a, t, steps, lds, total);
+  else small_matrix<2, NW, 256 / 32 / NW, 32 * 256 / (64 * NW)>(a, t, steps, lds, total);
+}
+
 // Any of them, and wider ones.
 __global__ __launch_bounds__(512, 2) void k_ns_small_any(NsArgs a, const int32_t* list, int steps) {
   extern __shared__ __align__(16) char lds[];
@@ -363,27 +373,28 @@ __global__ __launch_bounds__(512, 2) void k_ns_small_any(NsArgs a, const int32_t
 
 hipError_t launch_ns_small(const NsArgs& a, int cls, size_t lds, const int32_t* list, int32_t n,
                            int32_t steps, hipStream_t s) {
-  auto go = [&](auto fn, int nw) {
-    note_variant(cls < 8 ? "k_ns_small" : "k_ns_small_any", kArithF16x2);
+  auto go = [&](auto fn) {
+    note_variant(cls < kNsLow ? "k_ns_small" : cls == kNsLow ? "k_ns_low" : "k_ns_small_any", kArithF16x2);
     if (const hipError_t e = hipFuncSetAttribute((const void*)fn, hipFuncAttributeMaxDynamicSharedMemorySize,
                                                  (int)kNsSmallLds))
       return e;
     for (int32_t at = 0; at < n; at += kNsGrid) {
-      fn<<<(unsigned)std::min(kNsGrid, n - at), 64 * nw, lds, s>>>(a, list + at, steps);
+      fn<<<(unsigned)std::min(kNsGrid, n - at), 64 * kNsWaves[cls], lds, s>>>(a, list + at, steps);
       if (const hipError_t e = hipGetLastError()) return e;
     }
     return hipSuccess;
   };
   switch (cls) {
-    case 0: return go(k_ns_small<1, 4>, kNsWaves[0]);
-    case 1: return go(k_ns_small<2, 4>, kNsWaves[1]);
-    case 2: return go(k_ns_small<3, 4>, kNsWaves[2]);
-    case 3: return go(k_ns_small<4, 3>, kNsWaves[3]);
-    case 4: return go(k_ns_small<5, 4>, kNsWaves[4]);
-    case 5: return go(k_ns_small<6, 4>, kNsWaves[5]);
-    case 6: return go(k_ns_small<7, 4>, kNsWaves[6]);
-    case 7: return go(k_ns_small<8, 4>, kNsWaves[7]);
-    default: return go(k_ns_small_any, 8);
+    case 0: return go(k_ns_small<1, 4>);
+    case 1: return go(k_ns_small<2, 4>);
+    case 2: return go(k_ns_small<3, 4>);
+    case 3: return go(k_ns_small<4, 3>);
+    case 4: return go(k_ns_small<5, 4>);
+    case 5: return go(k_ns_small<6, 4>);
+    case 6: return go(k_ns_small<7, 4>);
+    case 7: return go(k_ns_small<8, 4>);
+    case kNsLow: return go(k_ns_low);
+    default: return go(k_ns_small_any);
   }
 }
 

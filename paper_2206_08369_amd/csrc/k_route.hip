@@ -102,12 +102,16 @@ hipError_t launch_route(const float* scores, int32_t B, int32_t M, int32_t K, in
   const unsigned waves = (unsigned)((B + 3) / 4);
   if (M <= 256) k_route<64, 4><<<waves, 256, 0, s>>>(scores, B, M, K, idx, weight);
   else if (M <= 1024) k_route<64, 16><<<waves, 256, 0, s>>>(scores, B, M, K, idx, weight);
+  else if (M <= 2048) k_route<256, 8><<<(unsigned)B, 256, 0, s>>>(scores, B, M, K, idx, weight);
+  else if (M <= 4096) k_route<256, 16><<<(unsigned)B, 256, 0, s>>>(scores, B, M, K, idx, weight);
   else if (M <= 8192) k_route<256, 32><<<(unsigned)B, 256, 0, s>>>(scores, B, M, K, idx, weight);
   else k_route<256, 0><<<(unsigned)B, 256, 0, s>>>(scores, B, M, K, idx, weight);
   return hipGetLastError();
 }
 
-// ds_k = w_k (dw_k - sum_j w_j dw_j), the gradient of a softmax, at the chosen scores.
+// ds_k = w_k (dw_k - sum_j w_j dw_j), the gradient of a softmax, at the chosen scores.  K is
+// KM at most.
+template <int KM>
 __global__ __launch_bounds__(256) void k_route_bwd(const int32_t* __restrict__ idx,
                                                    const float* __restrict__ weight,
                                                    const float* __restrict__ dweight, int B, int M,
@@ -123,18 +127,18 @@ __global__ __launch_bounds__(256) void k_route_bwd(const int32_t* __restrict__ i
   for (int k = 0; k < K; ++k) mean = fmaf(__shfl(w, k), __shfl(d, k), mean);
   const float ds = w * (d - mean);
   // (the choices as scalars: a comparison and an addition each for 64 scores)
-  int ck[kRtMaxK];
-  float cs[kRtMaxK];
+  int ck[KM];
+  float cs[KM];
 #pragma unroll
-  for (int k = 0; k < kRtMaxK; ++k) {
+  for (int k = 0; k < KM; ++k) {
     ck[k] = k < K ? __builtin_amdgcn_readlane(i, k) : -1;
     cs[k] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ds), k));
   }
+#pragma unroll 4
   for (int m = lane; m < M; m += 64) {
     float v = 0.f;
 #pragma unroll
-    for (int k = 0; k < kRtMaxK; ++k)
-      if (k < K) v += ck[k] == m ? cs[k] : 0.f;
+    for (int k = 0; k < KM; ++k) v += ck[k] == m ? cs[k] : 0.f;
     dscores[b * M + m] = v;
   }
 }
@@ -142,7 +146,11 @@ __global__ __launch_bounds__(256) void k_route_bwd(const int32_t* __restrict__ i
 hipError_t launch_route_bwd(const int32_t* idx, const float* weight, const float* dweight, int32_t B,
                             int32_t M, int32_t K, float* dscores, hipStream_t s) {
   note_variant("k_route_bwd", kArithNone);
-  k_route_bwd<<<(unsigned)((B + 3) / 4), 256, 0, s>>>(idx, weight, dweight, B, M, K, dscores);
+  const unsigned grid = (unsigned)((B + 3) / 4);
+  if (K <= 2) k_route_bwd<2><<<grid, 256, 0, s>>>(idx, weight, dweight, B, M, K, dscores);
+  else if (K <= 4) k_route_bwd<4><<<grid, 256, 0, s>>>(idx, weight, dweight, B, M, K, dscores);
+  else if (K <= 8) k_route_bwd<8><<<grid, 256, 0, s>>>(idx, weight, dweight, B, M, K, dscores);
+  else k_route_bwd<kRtMaxK><<<grid, 256, 0, s>>>(idx, weight, dweight, B, M, K, dscores);
   return hipGetLastError();
 }
 

@@ -71,8 +71,10 @@ hipError_t launch_ns_product(const NsArgs& a, int what, int from, const NsItem* 
                              hipStream_t s);
 
 // Matrices that fit LDS, a workgroup each: classes 0 .. 7 (r of 1 .. 8 tiles of 16, c up to
-// 128) and 8 .. 11 (wider, r up to 32, 64, 96, 128).
-constexpr int kNsClasses = 12;
+// 128), 8 (r up to 16 and c up to 512, or 32 and 256: output weights) and 9 .. 12 (wider, r up to
+// 32, 64, 96, 128; their kernel takes every class).
+constexpr int kNsClasses = 13, kNsLow = 8, kNsAny = 12;
+inline bool ns_low(int32_t r, int32_t c) { return (r <= 16 && c <= 512) || (r <= 32 && c <= 256); }
 constexpr size_t kNsSmallLds = 160 * 1024 - 128;  // dynamic LDS of a workgroup, at most
 // Strips of two tiles in the lower triangle of tr x tr tiles.
 __host__ __device__ constexpr int ns_strips(int tr) {
@@ -86,8 +88,8 @@ __host__ __device__ constexpr int ns_small_split(int tr, int waves) {
   const int n = waves / ns_strips(tr);
   return n < 1 ? 1 : n > 4 ? 4 : n;
 }
-// Waves of a workgroup of the classes up to 128 columns (the others have eight).
-constexpr int kNsWaves[8] = {4, 4, 4, 4, 8, 16, 16, 16};
+// Waves of a workgroup of each class.
+constexpr int kNsWaves[kNsClasses] = {4, 4, 4, 4, 8, 16, 16, 16, 4, 8, 8, 8, 8};
 // For r up to 32, 64, 96, 128 in eight waves: units of work (32 columns and up to four tiles
 // of rows) a wave, and entries a thread loads, at most.
 constexpr int kNsUnits[4] = {5, 3, 3, 2}, kNsEntries[4] = {80, 64, 64, 48};
@@ -102,17 +104,18 @@ inline size_t ns_small_lds(int32_t r, int32_t c, int waves) {
 inline int ns_small_class(int32_t r, int32_t c) {
   if (r > 128 || c > 1280) return -1;
   if (c <= 128) return (r + 15) / 16 - 1;
+  if (ns_low(r, c)) return kNsLow;
   const int k = (r - 1) / 32, units = (c + 31) / 32 * (k >= 2 ? 2 : 1);
   if (ns_small_lds(r, c, 8) > kNsSmallLds || units > 8 * kNsUnits[k] || r * c > 512 * kNsEntries[k])
     return -1;
-  return 8 + k;
+  return kNsLow + 1 + k;
 }
 // Up to so many matrices go in one launch whatever their classes: each launch ends with
 // workgroups that wait for its longest.  (1 to 100 rows, 100 columns, one launch / by class:
 // 300 matrices 56 / 200 us, 1,000: 120 / 204, 2,000: 227 / 269; 6,000 by class: 515.)
 constexpr int kNsOneLaunch = 2048;
-// From the gradient to the result, a workgroup for each matrix of the list; class 8 and
-// above: any of the classes.
+// From the gradient to the result, a workgroup for each matrix of the list; classes above
+// kNsLow: any of the classes.
 hipError_t launch_ns_small(const NsArgs& a, int cls, size_t lds, const int32_t* list, int32_t n,
                            int32_t steps, hipStream_t s);
 

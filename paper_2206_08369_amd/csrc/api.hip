@@ -2313,15 +2313,18 @@ int ensure_newton(pmlp* h, int32_t mat) {
   if (sl.nx) close();
   q->nlarge = (int32_t)pieces.size();
   std::vector<int32_t> list;
-  if (nsmall <= kNsOneLaunch) {
-    std::vector<int32_t> all;
-    bool low = true;
+  if (nsmall <= 2 * kNsOneLaunch) {
+    std::vector<int32_t> low, any;
     for (std::vector<int32_t>& v : by_class) {
-      for (int32_t m : v) low &= ns_low(mats[m].r, mats[m].c);
-      all.insert(all.end(), v.begin(), v.end());
+      for (int32_t m : v) (ns_low(mats[m].r, mats[m].c) ? low : any).push_back(m);
       v.clear();
     }
-    by_class[low ? kNsLow : kNsAny] = std::move(all);
+    if (!any.empty() && nsmall <= kNsOneLaunch) {
+      any.insert(any.end(), low.begin(), low.end());
+      low.clear();
+    }
+    by_class[kNsLow] = std::move(low);
+    by_class[kNsAny] = std::move(any);
   }
   for (int k = 0; k < kNsClasses; ++k) {
     std::vector<int32_t>& v = by_class[k];

@@ -110,10 +110,12 @@ inline int ns_small_class(int32_t r, int32_t c) {
     return -1;
   return kNsLow + 1 + k;
 }
-// Up to so many matrices go in one launch whatever their classes: each launch ends with
-// workgroups that wait for its longest.  (1 to 100 rows, 100 columns, one launch / by class:
-// 300 matrices 56 / 200 us, 1,000: 120 / 204, 2,000: 227 / 269; 6,000 by class: 515.)
-constexpr int kNsOneLaunch = 2048;
+// Up to so many matrices go in one launch whatever their classes, and up to twice as many in two,
+// the low ones and the others: each launch ends with workgroups that wait for its longest.  Low
+// ones alone are one launch of theirs.  (us, one / two / by class: 300 matrices of 1 to 100 rows,
+// 100 columns 56 / 73 / 200, 1,000: 121 / 124 / 204, 2,000: 227 / 217 / 269; 6,000 by class 507;
+// 2,040 of 1 to 64 rows, 64 columns 145 / 111.)
+constexpr int kNsOneLaunch = 1024;
 // From the gradient to the result, a workgroup for each matrix of the list; classes above
 // kNsLow: any of the classes.
 hipError_t launch_ns_small(const NsArgs& a, int cls, size_t lds, const int32_t* list, int32_t n,

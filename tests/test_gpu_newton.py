@@ -325,3 +325,22 @@ def test_refusals(pm):
                       ((3, G, None, 0.9, True, 5, 0.1), "second hidden layer")):
         with pytest.raises(pm.PmlpError, match=msg):
             pm.pmlp_muon_step(h, *args)
+
+
+# plans of small matrices: (F, O, widths, matrix) with few rows only, with both kinds in one
+# launch, in two, and by class
+PLANS = [(10, 2, [1 + 7 * i % 16 for i in range(300)], "W1"),
+         (300, 3, [512, 257, 129, 128, 16, 1] * 9, "W2"), (200, 2, [32, 31, 17, 16] * 5, "W1"),
+         (40, 2, [3, 33, 40, 16] * 250, "W1"), (40, 2, [3, 33, 40, 16] * 300, "W1"),
+         (140, 2, [3, 33, 16, 100] * 520, "W1"), (256, 16, [600, 513, 250, 8] * 4, "W2")]
+
+
+@pytest.mark.parametrize("F,O,hs,matrix", PLANS, ids=lambda v: "M%d" % len(v) if isinstance(v, list) else str(v))
+def test_plans_of_small_matrices(pm, F, O, hs, matrix):
+    net = pm.PackedMLP(F, O, hs, [7] * len(hs))
+    G = randn(F + len(hs), *((O, net.N) if matrix == "W2" else (net.N, F)))
+    got = net.orthogonalize(G.cuda(), matrix)
+    assert torch.equal(got, net.orthogonalize(G.cuda(), matrix))
+    if matrix == "W2":
+        got, G = got.t(), G.t()
+    check(got, G, blocks(F, hs)[::len(hs) // 60 | 1])  # (an odd step: widths of all kinds)

@@ -1997,6 +1997,7 @@ RtLayout rt_layout(const pmlp* h, int64_t R, int32_t K, const RtShape& sh, bool 
   p.P = (int32_t)P;
   p.chunk = (int32_t)((R + kRtChunks - 1) / kRtChunks + 63) / 64 * 64;
   p.nchunk = (int32_t)((R + p.chunk - 1) / p.chunk);
+  p.long_rows = (int32_t)(2 * R / h->M);
   p.F = h->F;
   p.O = h->O;
   p.seg_off = h->d_seg_off;

@@ -44,6 +44,7 @@ struct RtTiles {
 struct RtPlan {
   int32_t R, K, M, P;      // P: places, at most
   int32_t nchunk, chunk;   // runs of `chunk` slots (a multiple of 64)
+  int32_t long_rows;       // rows from which on a model's weight gradients come first
   RtTiles t;
   int32_t F, O;
   const int64_t* seg_off;  // [M+1]

@@ -328,6 +328,19 @@ def test_more_slots_than_a_launch_has_workgroups(pm):
     close(got, (Y, bound))
 
 
+@pytest.mark.parametrize("models", [9, 700])  # grouped by one workgroup, or by several
+def test_a_few_models_take_most_rows(pm, models):
+    hs = [1 + 5 * m % 20 for m in range(models)]
+    p = Pool(pm, 20, 3, hs, [rr.SMOOTH[m % len(rr.SMOOTH)] for m in range(models)], True, seed=models)
+    B = 1900 if models == 9 else 3000
+    X, dY = p.rand(B, 20), p.rand(B, 3)
+    idx, w = p.choices(B, 2)
+    idx[:B // 3, 0], idx[B // 2:, 1], idx[B // 2:B // 2 + 300, 0] = 5, models - 1, 0
+    got, want = p.gradients(X, idx, w, dY), p.want(X, idx, w, dY)
+    for k in got:
+        close(got[k], want[k], k)
+
+
 @pytest.mark.parametrize("gated,lo,hi", [(False, 1, 9), (True, 1, 9), (False, 60, 90)])
 def test_many_tiles(pm, gated, lo, hi):
     """Enough tiles of the weight gradients for the wider ones."""

@@ -846,8 +846,8 @@ __device__ __forceinline__ void output_weights(const RtGrad& g, f32x4* sums, int
 // (Three launches before: 600 models of 1 to 100 units, 32,768 slots 139 us a call, 127 so.)
 //
 // Bound as k_rt_tile, by the matrix cores and the cutting beside them, with the tails of models
-// of unlike numbers of rows: 32 models of 500 to 1,000 units, 1,000 columns, 16,384 slots 298
-// us, of which the products need 131 at the rate of k_rt_tile's comment; MFMA busy 0.32.  The
+// of unlike numbers of rows: 32 models of 500 to 1,000 units, 1,000 columns, 16,384 slots 250
+// us, of which the products need 131 at the rate of k_rt_tile's comment; MFMA busy 0.39.  The
 // 600 small ones take 55 us, by how long a tile's chain of loads, cuts and products is.
 template <int NA, int NB, bool GATED>
 __global__ __launch_bounds__(256, 2) void k_rt_dw(RtGrad g, RtJoin j, int tiles, int outs) {

@@ -250,7 +250,8 @@ int pmlp_route_backward(pmlp_t h, const int32_t* idx_dev, const float* weight_de
  * The calls, and those of pmlp_orthogonalize and pmlp_muon_step, share one workspace of the
  * handle that behaves as that of pmlp_create_block: a call that needs a larger one than
  * those before it waits for the device, one under graph capture returns PMLP_ESTATE
- * instead, and calls and graph replays of one handle have to be kept in order. */
+ * instead, and calls and graph replays of one handle have to be kept in order.  A call that
+ * returns either or PMLP_ENOMEM has started nothing. */
 int pmlp_forward_routed(pmlp_t h, const float* X_dev, int32_t B, const int32_t* idx_dev,
                         const float* weight_dev, int32_t K, float* Y_dev);
 int pmlp_gradients_routed(pmlp_t h, const float* X_dev, int32_t B, const int32_t* idx_dev,

@@ -2391,6 +2391,14 @@ int newton(pmlp* h, int32_t mat, NsArgs a, int32_t steps) {
   }
   if (steps == 0)
     return run(h, KID_AUX, [&] { return launch_ns_momentum(a, 0, q->npieces, true, h->stream); });
+  // (the workspace before any launch: a call that is refused leaves the momentum and the weights)
+  Carver c;
+  auto halves = [&](int64_t n) { return c.take((size_t)(n + 1) / 2); };
+  const size_t oS = c.take(2 * (size_t)q->nlarge);
+  const size_t oX0 = halves(2 * q->nx), oX1 = halves(2 * q->nx), oT0 = halves(2 * q->nx),
+               oT1 = halves(2 * q->nx), oA = halves(2 * q->na), oP = halves(2 * q->na);
+  if (q->nlarge)
+    if (int rc = ensure_ws(h, &h->extra, c.bytes, "an orthogonalised update")) return rc;
   for (int k = 0; k < kNsClasses; ++k)
     if (const int32_t n = q->first[k + 1] - q->first[k])
       if (int rc = run(h, KID_DEEP, [&] {
@@ -2398,12 +2406,6 @@ int newton(pmlp* h, int32_t mat, NsArgs a, int32_t steps) {
           }))
         return rc;
   if (!q->nlarge) return PMLP_OK;
-  Carver c;
-  auto halves = [&](int64_t n) { return c.take((size_t)(n + 1) / 2); };
-  const size_t oS = c.take(2 * (size_t)q->nlarge);
-  const size_t oX0 = halves(2 * q->nx), oX1 = halves(2 * q->nx), oT0 = halves(2 * q->nx),
-               oT1 = halves(2 * q->nx), oA = halves(2 * q->na), oP = halves(2 * q->na);
-  if (int rc = ensure_ws(h, &h->extra, c.bytes, "an orthogonalised update")) return rc;
   unsigned char* const ws = h->extra.ws;
   a.sums = (double*)(ws + oS);
   a.X[0] = (_Float16*)(ws + oX0);

@@ -271,8 +271,9 @@ int pmlp_routed_status(pmlp_t h);
  * receives X.  matrix: PMLP_MAT_W1 or PMLP_MAT_V1 (buffers [N, F], model m's matrix its
  * rows), PMLP_MAT_W2 ([O, N], its columns; [O, N2] of a two-hidden-layer pack) or
  * PMLP_MAT_W12 ([K] as pmlp_get_params_deep).  A matrix the pack does not have returns
- * PMLP_ESTATE.  steps in [1, 10] (5 is usual).  fp32; a model whose U is not finite gets
- * NaN, the others what they get without it.  mom_in and mom_out may be the same buffer or
+ * PMLP_ESTATE.  steps in [1, 10] (5 is usual).  In fp32's accuracy, also of rows and columns
+ * that are small beside the others; a model whose U is not finite gets NaN, the others what
+ * they get without it.  mom_in and mom_out may be the same buffer or
  * both null, out may be G; otherwise the buffers must not overlap. */
 int pmlp_orthogonalize(pmlp_t h, int32_t matrix, const float* G_dev, const float* mom_in_dev,
                        float* mom_out_dev, float mu, int32_t nesterov, int32_t steps,

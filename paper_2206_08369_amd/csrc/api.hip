@@ -117,6 +117,7 @@ struct GrowingWs {
 // workspace is bounded, each with its runs of the item lists.
 struct NewtonSlice {
   int32_t load0, load, sym0, sym, step0, step;  // items: tiles of X, lower ones of A, the steps'
+  int32_t turned;                  // of the tiles of X, those of transposed matrices (first)
   int64_t nx, na;                  // entries of a plane
 };
 struct PmlpNewton {
@@ -126,6 +127,7 @@ struct PmlpNewton {
   int32_t npieces = 0, nlarge = 0;  // pieces, and those of matrices that go in slices (first)
   std::vector<NewtonSlice> slices;
   int64_t nx = 0, na = 0;  // of the largest slice
+  int64_t nr = 0, nc = 0;  // rows and columns of all that go in slices
   int32_t tile = 128;      // (NsArgs)
   int32_t* d_list = nullptr;  // matrices by class (ns_small_class), the dearest first
   int32_t first[kNsClasses + 1] = {};
@@ -2213,11 +2215,13 @@ int ensure_newton(pmlp* h, int32_t mat) {
     }
   } made{new PmlpNewton()};
   PmlpNewton* q = made.q;
-  std::vector<NsItem> load, sym, step;
+  std::vector<NsItem> load, turned, sym, step;  // load: of the others
   NewtonSlice sl{};
   auto close = [&] {
     sl.load0 = (int32_t)items.size();
-    sl.load = (int32_t)load.size();
+    sl.turned = (int32_t)turned.size();
+    sl.load = (int32_t)(turned.size() + load.size());
+    items.insert(items.end(), turned.begin(), turned.end());
     items.insert(items.end(), load.begin(), load.end());
     sl.sym0 = (int32_t)items.size();
     sl.sym = (int32_t)sym.size();
@@ -2229,6 +2233,7 @@ int ensure_newton(pmlp* h, int32_t mat) {
     q->nx = std::max(q->nx, sl.nx);
     q->na = std::max(q->na, sl.na);
     load.clear();
+    turned.clear();
     sym.clear();
     step.clear();
     sl = NewtonSlice{};
@@ -2280,6 +2285,7 @@ int ensure_newton(pmlp* h, int32_t mat) {
     if (t.c > (1 << 30)) return fail(PMLP_EINVAL, "a matrix is too large to be orthogonalised");
     t.rp = (t.r + 31) / 32 * 32;
     t.cp = (t.c + 31) / 32 * 32;
+    ns_scales(&t);
     if (const int cls = ns_small_class(t.r, t.c); cls >= 0) {
       by_class[cls].push_back(m);
       ++nsmall;
@@ -2300,12 +2306,16 @@ int ensure_newton(pmlp* h, int32_t mat) {
     if (sl.nx && newton_bytes(sl.nx + nx, sl.na + na) > kNewtonSlice) close();
     t.xo = sl.nx;
     t.ao = sl.na;
+    t.ro = q->nr;
+    t.co = q->nc;
+    q->nr += t.rp;
+    q->nc += t.cp;
     sl.nx += nx;
     sl.na += na;
     cut(m);
     const int32_t ti = div_up(t.rp, q->tile), tj = div_up(t.cp, q->tile);
     for (int32_t i = 0; i < ti; ++i) {
-      for (int32_t j = 0; j < tj; ++j) load.push_back(tile(m, i, j));
+      for (int32_t j = 0; j < tj; ++j) (t.rows > t.cols ? turned : load).push_back(tile(m, i, j));
       for (int32_t j = 0; j <= i; ++j) sym.push_back(tile(m, i, j));
       for (int32_t j = 0; j < div_up(t.cp, ns_step_columns(q->tile)); ++j)
         step.push_back(tile(m, i, j));
@@ -2397,6 +2407,8 @@ int newton(pmlp* h, int32_t mat, NsArgs a, int32_t steps) {
   const size_t oS = c.take(2 * (size_t)q->nlarge);
   const size_t oX0 = halves(2 * q->nx), oX1 = halves(2 * q->nx), oT0 = halves(2 * q->nx),
                oT1 = halves(2 * q->nx), oA = halves(2 * q->na), oP = halves(2 * q->na);
+  const size_t oR = c.take((size_t)q->nr), oC = c.take(3 * (size_t)q->nc), oE = c.take((size_t)q->nr / 2),
+               oF = c.take((size_t)q->nc / 2), oU = c.take((size_t)h->M);
   if (q->nlarge)
     if (int rc = ensure_ws(h, &h->extra, c.bytes, "an orthogonalised update")) return rc;
   for (int k = 0; k < kNsClasses; ++k)
@@ -2417,18 +2429,26 @@ int newton(pmlp* h, int32_t mat, NsArgs a, int32_t steps) {
   a.nx = q->nx;
   a.na = q->na;
   a.tile = q->tile;
+  a.rmax = (uint32_t*)(ws + oR);
+  a.cmax = (uint32_t*)(ws + oC);
+  a.rows = (int8_t*)(ws + oE);
+  a.cols = (int8_t*)(ws + oF);
+  a.nr = q->nr;
+  a.nc = q->nc;
+  a.uneven = (int32_t*)(ws + oU);
   if (int rc = run(h, KID_AUX, [&] { return launch_ns_momentum(a, 0, q->nlarge, false, h->stream); }))
     return rc;
   for (const NewtonSlice& sl : q->slices) {
     const NsItem *load = q->d_items + sl.load0, *sym = q->d_items + sl.sym0,
                  *step = q->d_items + sl.step0;
+    if (sl.turned)
+      if (int rc = run(h, KID_AUX, [&] { return launch_ns_rows(a, load, sl.turned, h->stream); })) return rc;
     if (int rc = run(h, KID_AUX, [&] { return launch_ns_load(a, load, sl.load, h->stream); })) return rc;
     for (int32_t t = 0; t < steps; ++t) {
-      const int from = t & 1;
       if (int rc = run(h, KID_DEEP, [&] {
-            if (const hipError_t e = launch_ns_product(a, NS_GRAM, from, sym, sl.sym, h->stream)) return e;
-            if (const hipError_t e = launch_ns_product(a, NS_POLY, from, sym, sl.sym, h->stream)) return e;
-            return launch_ns_product(a, t + 1 < steps ? NS_STEP : NS_LAST, from, step, sl.step, h->stream);
+            if (const hipError_t e = launch_ns_product(a, NS_GRAM, t, sym, sl.sym, h->stream)) return e;
+            if (const hipError_t e = launch_ns_product(a, NS_POLY, t, sym, sl.sym, h->stream)) return e;
+            return launch_ns_product(a, t + 1 < steps ? NS_STEP : NS_LAST, t, step, sl.step, h->stream);
           }))
         return rc;
     }

@@ -2,6 +2,9 @@
 // pmlp_muon_step).  Declarations shared by the host library and k_newton.hip.
 #pragma once
 
+#include <algorithm>
+#include <cmath>
+
 #include "pmlp_internal.h"
 
 namespace pmlpk {
@@ -21,15 +24,17 @@ struct NsMat {
   int32_t rows, cols, ld, wld;
   int32_t r, c, rp, cp;
   int64_t xo, ao; // first entry of its X (of rp cp) and A (of rp rp) in a slice's workspace
+  int64_t ro, co; // .. of its rows' and columns' exponents in those of all
   int32_t piece0, pieces;  // its pieces
-  int32_t m, pad;
+  int32_t m;
+  int16_t root, grow;  // (ns_scales)
 };
 struct NsPiece {
   int32_t mat, row0, rows, pad;
 };
 // Tile (i, j) of a matrix, with all that a workgroup wants to know of it.
 struct NsItem {
-  int32_t mat, i, j, pad[9];
+  int32_t mat, i, j, pad[5];
   NsMat t;
 };
 static_assert(sizeof(NsItem) == 128, "NsItem layout");
@@ -43,6 +48,12 @@ struct NsArgs {
   float mu;
   int32_t nesterov;
   double* sums;         // [pieces] sums of squares
+  // exponents of X's rows and columns before and after a step, [2][nr] and [2][nc]; the rows'
+  // largest |U| [nr], the columns' largest |X / rows' scales| in turn [3][nc], as float bits
+  int8_t *rows, *cols;
+  int64_t nr, nc;
+  uint32_t *rmax, *cmax;
+  int32_t* uneven;      // [M] whether a column has a scale
   // a slice of the matrices: planes of the high and the low half of every entry
   _Float16 *X[2], *XT[2];  // [2][nx] each: X and its transpose, before and after a step
   _Float16 *A, *P;         // [2][na]
@@ -61,14 +72,30 @@ struct NsArgs {
 // mom_out = mu mom_in + G and the pieces' sums of squares of U (out null, W null), or,
 // with W set, W -= lr (decay W + U).
 hipError_t launch_ns_momentum(const NsArgs& a, int32_t piece0, int32_t pieces, bool apply, hipStream_t s);
-// X = U / |U|_F
+// Before it, what the scales of turned matrices' rows come from.
+hipError_t launch_ns_rows(const NsArgs& a, const NsItem* items, int32_t n, hipStream_t s);
+// X = U / |U|_F, with the scales of its rows and columns
 hipError_t launch_ns_load(const NsArgs& a, const NsItem* items, int32_t n, hipStream_t s);
 enum NsProduct { NS_GRAM = 0, NS_POLY = 1, NS_STEP = 2, NS_LAST = 3 };
-// From X[from], XT[from].  items: tiles of `tile` x `tile` (j <= i) of A and P, of `tile` x
+// Step `step`, from X[step % 2], XT[step % 2].  items: tiles of `tile` x `tile` (j <= i) of A and P, of `tile` x
 // ns_step_columns(tile) of the steps.
 inline int32_t ns_step_columns(int32_t tile) { return tile == 64 ? 64 : 256; }
-hipError_t launch_ns_product(const NsArgs& a, int what, int from, const NsItem* items, int32_t n,
+hipError_t launch_ns_product(const NsArgs& a, int what, int step, const NsItem* items, int32_t n,
                              hipStream_t s);
+
+// Exponents that the scales of an r x c X (newton_device.h) are derived with: of sqrt(c), which
+// bounds a row's norm by its largest entry, and of 4 (3.45 + 5.64 sqrt(r)), which bounds what a
+// step makes of a column's largest entry, but 2^10 at least: most matrices' columns then have scale
+// 1, and the largest entry of a column still keeps 2^-24 of itself.
+inline void ns_scales(NsMat* t) {
+  auto up = [](double v) {
+    int e = 0;
+    while (std::ldexp(1.0, e) < v) ++e;
+    return (int16_t)e;
+  };
+  t->root = up(std::sqrt((double)t->c));
+  t->grow = std::max<int16_t>(10, up(4 * (3.45 + 5.64 * std::sqrt((double)t->r))));
+}
 
 // Matrices that fit LDS, a workgroup each: classes 0 .. 7 (r of 1 .. 8 tiles of 16, c up to
 // 128), 8 (r up to 16 and c up to 512, or 32 and 256: output weights) and 9 .. 12 (wider, r up to
@@ -98,7 +125,7 @@ inline size_t ns_small_lds(int32_t r, int32_t c, int waves) {
   const int cp = (c + 31) / 32 * 32, rp = (r + 31) / 32 * 32, tr = (r + 15) / 16;
   const int split = ns_small_split(tr, waves);
   return (size_t)32 * tr * ((2 * cp + 16) + (2 * rp + 16)) +
-         (split > 1 ? (size_t)split * ns_strips(tr) * 2048 : 0);
+         (split > 1 ? (size_t)split * ns_strips(tr) * 2048 : 0) + 32 * tr + 2 * cp + 16;
 }
 // The class of an r x c matrix, or -1.
 inline int ns_small_class(int32_t r, int32_t c) {

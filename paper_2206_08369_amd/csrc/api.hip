@@ -1995,7 +1995,7 @@ RtLayout rt_layout(const pmlp* h, int64_t R, int32_t K, const RtShape& sh, bool 
   p.K = K;
   p.M = h->M;
   const int64_t groups = std::min<int64_t>(h->M, R);  // that have rows, at most
-  const int64_t P = R + (kRtPad - 1) * groups;
+  const int64_t P = rt_places(R, groups);
   p.P = (int32_t)P;
   p.chunk = (int32_t)((R + kRtChunks - 1) / kRtChunks + 63) / 64 * 64;
   p.nchunk = (int32_t)((R + p.chunk - 1) / p.chunk);
@@ -2144,7 +2144,7 @@ int gradients_routed(pmlp* h, const float* X, int32_t B, const int32_t* idx, con
   const int32_t parts = 2 * div_up(h->widest, l.p.t.uc);
   const int64_t whole = (R + kRtPad - 1) / kRtPad * kRtPad;
   const int32_t nparts = div_up(whole, l.p.t.part);
-  const size_t hidden = (size_t)h->widest * l.p.P, k = gated ? 2 : 1;
+  const size_t hidden = (size_t)rt_hidden(R, l.p.P, h->widest, h->N), k = gated ? 2 : 1;
   const size_t oD = l.c.take((size_t)R * parts), oZ = l.c.take(hidden), oH = l.c.take(hidden),
                oU = l.c.take(gated ? hidden : 0),
                oW = l.c.take(nparts > 1 ? nparts * k * h->N * h->F : 0),

@@ -19,6 +19,15 @@ constexpr int32_t kRtChunks = 256;  // runs of slots that are counted side by si
 constexpr int32_t kRtLdsModels = 16384;  // models whose counters lie in LDS
 constexpr int32_t kRtOneSlots = 4096, kRtOneModels = 512;  // that one workgroup groups, at most
 
+// Places of R slots on at most `groups` models, each padded.
+inline int64_t rt_places(int64_t R, int64_t groups) { return R + (kRtPad - 1) * groups; }
+// Values of a hidden layer of N units, `widest` in the widest model, on those P places: each place,
+// padding too, has the units of its own model.
+inline int64_t rt_hidden(int64_t R, int64_t P, int64_t widest, int64_t N) {
+  const int64_t own = widest * R + (kRtPad - 1) * N;
+  return own < widest * P ? own : widest * P;
+}
+
 // A work unit: row block `a` and unit chunk `b` of model m, or unit tile `a`, column tile `b`
 // and part `c` of its weight gradients; with what a workgroup wants to know of its model, so
 // that it starts after one load.

@@ -19,8 +19,11 @@ constexpr int32_t kRtChunks = 256;  // runs of slots that are counted side by si
 constexpr int32_t kRtLdsModels = 16384;  // models whose counters lie in LDS
 constexpr int32_t kRtOneSlots = 4096, kRtOneModels = 512;  // that one workgroup groups, at most
 
-// Places of R slots on at most `groups` models, each padded.
-inline int64_t rt_places(int64_t R, int64_t groups) { return R + (kRtPad - 1) * groups; }
+// Places of R slots on at most `groups` models, each padded: a multiple of kRtPad, so that rows of P
+// values are aligned as one model's places are.
+inline int64_t rt_places(int64_t R, int64_t groups) {
+  return (R + (kRtPad - 1) * groups + kRtPad - 1) / kRtPad * kRtPad;
+}
 // Values of a hidden layer of N units, `widest` in the widest model, on those P places: each place,
 // padding too, has the units of its own model.
 inline int64_t rt_hidden(int64_t R, int64_t P, int64_t widest, int64_t N) {

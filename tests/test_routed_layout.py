@@ -58,6 +58,12 @@ def test_places_and_hidden_values_suffice(sizes):
         assert places <= P and hidden <= H, row
 
 
+def test_rows_of_places_are_aligned(sizes):
+    """Output gradients by place are [O][P] floats, read four at a time."""
+    rows = [(R, g, 1, 1) for R in range(1, 200) for g in (1, 2, 3, 7, 64) if g <= R]
+    assert all(P % 32 == 0 for P, _ in sizes(rows))
+
+
 def test_one_wide_model_does_not_widen_the_others_padding(sizes):
     # 5,999 models of 1 to 9 units and one of 1,000, 32,768 slots
     N = sum(1 + m % 9 for m in range(5999)) + 1000

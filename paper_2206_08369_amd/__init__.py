@@ -535,8 +535,10 @@ class PackedMLP:
             pass
 
     def _stream(self) -> None:
-        # (the current stream's pointer, without an object for it: 1 us of a call's 9)
-        pmlp_set_stream(self.handle, self._torch._C._cuda_getCurrentRawStream(self.device.index))
+        # (where torch gives the current stream's pointer without an object for it: 1 us of a call's 9)
+        pointer = getattr(self._torch._C, "_cuda_getCurrentRawStream", None)
+        pmlp_set_stream(self.handle, pointer(self.device.index) if pointer
+                        else self._torch.cuda.current_stream(self.device).cuda_stream)
 
     def _x(self, X):
         t = self._torch

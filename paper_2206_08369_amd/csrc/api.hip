@@ -1964,17 +1964,24 @@ RtShape rt_weight_shape(const pmlp* h) {
 }
 
 // Whether every slot goes to its model on its own: while the weights they read, each its
-// model's, are 128 MB at most, with 1.5 KB for a slot and 0.4 for an output of it, or the
-// models have three rows each at most.  (us, slot by slot / grouped: 600 gated models of 1 to
+// model's, are 128 MB at most, with 1.5 KB for a slot, 0.4 for an output of it and 3 for each
+// workgroup that a model of average width leaves idle (there are as many for each slot as the widest
+// one needs), or the models have three rows each at most and 2^16 such workgroups.  (us, slot by slot / grouped: 600 gated models of 1 to
 // 100 units, 100 columns, 4,096 slots 35 / 40, 8,192 slots 59 / 42; 200 of 100 to 200 units, 200
 // columns, 1,024 slots 23 / 30, 2,048 slots 37 / 31; 60 of 1 to 10 units, ten columns, 32,768
 // slots 16 / 23, 131,072 slots 51 / 41; 300 of 20 to 60, 20 columns, 16 outputs, 8,192 slots 22 /
 // 26, 16,384 slots 36 / 27; 6,000 of 1 to 100, 100 columns, 16,384 slots 68 / 138, 131,072 slots
-// 474 / 157.)  A launch has fewer than 2^24 workgroups of 256.
+// 474 / 157.  600 of 1 to 50 and one of 1,000, 100 columns, 1,024 slots 16 / 32, 4,096 slots 45 /
+// 33; one of 10,000, 256 slots 34 / 28, 1,024 slots 70 / 30; 6,000 of 1 to 9 and one of 2,000, 1,024
+// slots 23 / 74, 4,096 slots 67 / 91, 16,384 slots 254 / 126; 200 of 1 to 100 and one of 3,000, 200
+// columns, 256 slots 16 / 22, 1,024 slots 30 / 31, 4,096 slots 93 / 35.)  A launch has fewer than 2^24 workgroups of 256.
 bool rt_few(const pmlp* h, int64_t R) {
-  if (R * div_up(h->widest, kRtFewUnits) >= (int64_t)1 << 24) return false;
+  const int32_t chunks = div_up(h->widest, kRtFewUnits);
+  if (R * chunks >= (int64_t)1 << 24) return false;
+  const int64_t idle = chunks - div_up(h->N / h->M, kRtFewUnits);
   const double weights = 4.0 * h->N / h->M * h->F4 * (h->block && h->block->gated ? 2 : 1);
-  return R * (weights + 1500 + 400 * h->O) <= (double)(128 << 20) || R <= 3 * (int64_t)h->M;
+  return R * (weights + 1500 + 400 * h->O + 3000 * idle) <= (double)(128 << 20) ||
+         (R <= 3 * (int64_t)h->M && R * idle <= 1 << 16);
 }
 
 // Where the parts of a routed call's workspace lie.

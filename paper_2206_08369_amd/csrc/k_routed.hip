@@ -490,10 +490,14 @@ __device__ __forceinline__ float few_output(const RtArgs& a, int64_t n0, int64_t
 
 }  // namespace
 
-// 64 units of a slot a workgroup
+// 64 units of a slot a workgroup.  A die takes a run of the slots: dies in turn, the workgroups with
+// something to do could all come to one, as every eighth does where one model is wide and the others
+// are not.  (600 models of 1 to 50 units and one of 1,000, 100 columns, 4,096 slots 102 us, 45 so.)
 template <bool GATED>
 __global__ __launch_bounds__(256) void k_rt_few(RtArgs a, RtFew f) {
-  const int s = blockIdx.x / f.chunks, chunk = blockIdx.x % f.chunks;
+  const int at = die_order(blockIdx.x, f.R * f.chunks);
+  if (at >= f.R * f.chunks) return;
+  const int s = at / f.chunks, chunk = at % f.chunks;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int m = f.idx[s];
   if (m < 0 || m >= a.M) {
@@ -521,7 +525,8 @@ __global__ __launch_bounds__(256) void k_rt_few(RtArgs a, RtFew f) {
 template <bool GATED>
 __global__ __launch_bounds__(256) void k_rt_few_waves(RtArgs a, RtFew f) {
   const int lane = threadIdx.x & 63;
-  const int64_t q = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int groups = (f.R * f.chunks + 3) / 4;
+  const int64_t q = (int64_t)die_order(blockIdx.x, groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (q >= (int64_t)f.R * f.chunks) return;
   const int s = (int)(q / f.chunks), chunk = (int)(q % f.chunks);
   const int m = f.idx[s];
@@ -577,10 +582,11 @@ hipError_t launch_rt_few(const RtArgs& a, const RtFew& f, hipStream_t s) {
   const bool waves = grid >= 1024 && a.F4 <= 64;
   note_variant(waves ? "k_rt_few_waves" : "k_rt_few", kArithNone);
   if (waves) {
-    if (a.V1) k_rt_few_waves<true><<<(grid + 3) / 4, 256, 0, s>>>(a, f);
-    else k_rt_few_waves<false><<<(grid + 3) / 4, 256, 0, s>>>(a, f);
-  } else if (a.V1) k_rt_few<true><<<grid, 256, 0, s>>>(a, f);
-  else k_rt_few<false><<<grid, 256, 0, s>>>(a, f);
+    const unsigned groups = ((grid + 3) / 4 + 7) / 8 * 8;  // (die_order)
+    if (a.V1) k_rt_few_waves<true><<<groups, 256, 0, s>>>(a, f);
+    else k_rt_few_waves<false><<<groups, 256, 0, s>>>(a, f);
+  } else if (a.V1) k_rt_few<true><<<(grid + 7) / 8 * 8, 256, 0, s>>>(a, f);
+  else k_rt_few<false><<<(grid + 7) / 8 * 8, 256, 0, s>>>(a, f);
   return hipGetLastError();
 }
 

@@ -1965,16 +1965,18 @@ RtShape rt_weight_shape(const pmlp* h) {
 
 // Whether every slot goes to its model on its own: while the weights they read, each its
 // model's, are 128 MB at most, with 1.5 KB for a slot, 0.4 for an output of it and 3 for each
-// workgroup that a model of average width leaves idle (there are as many for each slot as the widest
-// one needs), or the models have three rows each at most and 2^16 such workgroups.  (us, slot by slot / grouped: 600 gated models of 1 to
-// 100 units, 100 columns, 4,096 slots 35 / 40, 8,192 slots 59 / 42; 200 of 100 to 200 units, 200
-// columns, 1,024 slots 23 / 30, 2,048 slots 37 / 31; 60 of 1 to 10 units, ten columns, 32,768
-// slots 16 / 23, 131,072 slots 51 / 41; 300 of 20 to 60, 20 columns, 16 outputs, 8,192 slots 22 /
-// 26, 16,384 slots 36 / 27; 6,000 of 1 to 100, 100 columns, 16,384 slots 68 / 138, 131,072 slots
-// 474 / 157.  600 of 1 to 50 and one of 1,000, 100 columns, 1,024 slots 16 / 32, 4,096 slots 45 /
-// 33; one of 10,000, 256 slots 34 / 28, 1,024 slots 70 / 30; 6,000 of 1 to 9 and one of 2,000, 1,024
-// slots 23 / 74, 4,096 slots 67 / 91, 16,384 slots 254 / 126; 200 of 1 to 100 and one of 3,000, 200
-// columns, 256 slots 16 / 22, 1,024 slots 30 / 31, 4,096 slots 93 / 35.)  A launch has fewer than 2^24 workgroups of 256.
+// workgroup that a model of average width leaves idle (there are as many for each slot as the
+// widest one needs), or the models have three rows each at most and leave 2^16 idle at most.
+// (us, slot by slot / grouped, one choice a sample: 600 gated models of 1 to 100 units, 100
+// columns, 4,096 slots 29 / 42, 8,192 slots 51 / 43; 200 of 100 to 200 units, 200 columns, 1,024
+// slots 19 / 28, 2,048 slots 35 / 29; 60 of 1 to 10 units, ten columns, 16,384 slots 20 / 24, 65,536
+// slots 73 / 30, four choices 32,768 slots 16 / 26, 131,072 slots 54 / 46; 300 of 20 to 60, 20
+// columns, 16 outputs, 8,192 slots 20 / 27, 16,384 slots 36 / 29; 6,000 of 1 to 100, 100 columns,
+// 16,384 slots 56 / 145, 131,072 slots 399 / 164.  600 of 1 to 50 and one of 1,000, 100 columns, 1,024
+// slots 16 / 32, 4,096 slots 45 / 33; one of 10,000, 256 slots 34 / 28, 1,024 slots 70 / 30; 6,000 of 1
+// to 9 and one of 2,000, 1,024 slots 23 / 74, 4,096 slots 67 / 91, 16,384 slots 254 / 126; 200 of 1 to
+// 100 and one of 3,000, 200 columns, 256 slots 16 / 22, 1,024 slots 30 / 31, 4,096 slots 93 / 35.)
+// A launch has fewer than 2^24 workgroups of 256.
 bool rt_few(const pmlp* h, int64_t R) {
   const int32_t chunks = div_up(h->widest, kRtFewUnits);
   if (R * chunks >= (int64_t)1 << 24) return false;
@@ -2262,7 +2264,7 @@ int ensure_newton(pmlp* h, int32_t mat) {
     return it;
   };
   std::vector<int32_t> by_class[kNsClasses], large;
-  int32_t nsmall = 0;
+  int32_t nsmall = 0, tallest = 0;  // matrices in LDS, and the rows of the tallest
   int64_t tiles = 0, tiles64 = 0;  // of 128 and of 64, of a product of the large ones
   for (int32_t m = 0; m < h->M; ++m) {
     NsMat& t = mats[m];
@@ -2296,16 +2298,17 @@ int ensure_newton(pmlp* h, int32_t mat) {
     if (const int cls = ns_small_class(t.r, t.c); cls >= 0) {
       by_class[cls].push_back(m);
       ++nsmall;
+      tallest = std::max(tallest, t.r);
       continue;
     }
     large.push_back(m);
     tiles += (int64_t)div_up(t.rp, 128) * div_up(t.cp, 128);
     tiles64 += (int64_t)div_up(t.rp, 64) * div_up(t.cp, 64);
   }
-  // Tiles of 128 take 0.77 of the time of four of 64 (32 matrices of 1,000 x 1,000: 2,942
-  // against 3,841 us) where there are enough of them (4 such matrices, 256 tiles: 705 against
-  // 589; 8: 930 against 999) and the last ones are not too empty (300 of 300 x 300: 1,951
-  // against 1,729).
+  // Tiles of 128 take 0.77 of the time of four of 64 (32 matrices of 1,000 x 1,000: 3,051
+  // against 3,968 us) where there are enough of them (4 such matrices, 256 tiles: 740 against
+  // 583; 8: 951 against 995) and the last ones are not too empty (300 of 300 x 300: 2,113
+  // against 1,906).
   if (tiles < 512 || 16 * tiles > 5 * tiles64) q->tile = 64;
   for (int32_t m : large) {
     NsMat& t = mats[m];
@@ -2331,7 +2334,7 @@ int ensure_newton(pmlp* h, int32_t mat) {
   if (sl.nx) close();
   q->nlarge = (int32_t)pieces.size();
   std::vector<int32_t> list;
-  if (nsmall <= 2 * kNsOneLaunch) {
+  if (nsmall <= kNsOneLaunch || (nsmall <= 2 * kNsOneLaunch && tallest > 64)) {
     std::vector<int32_t> low, any;
     for (std::vector<int32_t>& v : by_class) {
       for (int32_t m : v) (ns_low(mats[m].r, mats[m].c) ? low : any).push_back(m);

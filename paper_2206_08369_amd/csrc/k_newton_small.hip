@@ -110,12 +110,13 @@ __device__ __forceinline__ void small_matrix(const NsArgs& a, const NsMat& t, in
   constexpr int NT = 64 * NW, RP = (TR + 1) / 2 * 32, TRB = RP / 32, NB = ns_strips(TR);
   constexpr int NG = NW == 16 ? (TR + 1) / 2 : TR <= 4 ? 1 : 2, RG = (TR + NG - 1) / NG;  // row tiles of a unit
   constexpr int KS = ns_small_split(TR, NW), PER = (NB + NW - 1) / NW;
+  constexpr int RS = TR == 1 ? 1 : 2;  // tiles of a strip
   constexpr int SP = 2 * RP + 16;
   const int C = t.cp, SX = 2 * C + 16, pairs = C / 32;
   const int xplane = 16 * TR * SX, pplane = 16 * TR * SP;
   char *X = lds, *A = lds + 2 * xplane;
-  f32x4* part = (f32x4*)(A + 2 * pplane);  // [KS][NB][2][64]
-  int8_t* const rows_at = (int8_t*)(part + (KS > 1 ? KS * NB * 128 : 0));  // exponents of D [2][16 TR],
+  f32x4* part = (f32x4*)(A + 2 * pplane);  // [KS][NB][RS][64]
+  int8_t* const rows_at = (int8_t*)(part + (KS > 1 ? KS * NB * RS * 64 : 0));  // exponents of D [2][16 TR],
   int8_t* const cols_at = rows_at + 32 * TR;                               // .. of E [2][C]
   int* const uneven = (int*)(cols_at + 2 * C);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -253,256 +254,263 @@ __device__ __forceinline__ void small_matrix(const NsArgs& a, const NsMat& t, in
   }
   __syncthreads();
 
-  f32x4 held[PER][2];  // this wave's strips of A'
-  for (int step = 0; step < steps; ++step) {
-    // (Places in LDS anew in each step: kept from the first one they would go to memory.)
-    const int lane = afresh(tid & 63), li = lane & 15, lk = lane >> 4;
-    // A tile of a symmetric matrix, rows 16 ti + 4 lk + e of column 16 tj + li, and mirrored: each
-    // value times the scale of the column of B or P' that it goes to
-    auto put_symmetric = [&](int ti, int tj, const f32x4& v, const f32x4& by_row, float by_column) __attribute__((always_inline)) {
-      f16x4 hi, lo;
-      halve(v * by_row, hi, lo);
-      char* to = A + (16 * tj + li) * SP + held_column(ti, lk);
-      *(f16x4*)to = hi;
-      *(f16x4*)(to + pplane) = lo;
-      if (ti == tj) return;
-      halve(v * by_column, hi, lo);
-      char* at = A + (16 * ti + 4 * lk) * SP + held_column(tj, li >> 2) + 2 * (li & 3);
+  // (Both ways compiled on their own: the scales of columns take registers.)
+  auto iterate = [&](auto all_even) __attribute__((always_inline)) {
+    constexpr bool even = decltype(all_even)::value;
+    f32x4 held[PER][RS];  // this wave's strips of A'
+    for (int step = 0; step < steps; ++step) {
+      // (Places in LDS anew in each step: kept from the first one they would go to memory.)
+      const int lane = afresh(tid & 63), li = lane & 15, lk = lane >> 4;
+      // A tile of a symmetric matrix, rows 16 ti + 4 lk + e of column 16 tj + li, and mirrored: each
+      // value times the scale of the column of B or P' that it goes to
+      auto put_symmetric = [&](int ti, int tj, const f32x4& v, const f32x4& by_row, float by_column) __attribute__((always_inline)) {
+        f16x4 hi, lo;
+        halve(v * by_row, hi, lo);
+        char* to = A + (16 * tj + li) * SP + held_column(ti, lk);
+        *(f16x4*)to = hi;
+        *(f16x4*)(to + pplane) = lo;
+        if (ti == tj) return;
+        halve(v * by_column, hi, lo);
+        char* at = A + (16 * ti + 4 * lk) * SP + held_column(tj, li >> 2) + 2 * (li & 3);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        *(_Float16*)(at + e * SP) = hi[e];
-        *(_Float16*)(at + e * SP + pplane) = lo[e];
-      }
-    };
-    // Tiles (ti, tj) and (ti, tj + 1) of S S^T over the 32-column steps k0 <= k < k1, with columns
-    // times 4^e where `scaled`.
-    auto strip_product = [&](const char* S, int stride, int plane, int ti, int tj, int k0, int k1,
-                             auto scaled, const int8_t* e, f32x4 (&acc)[2]) __attribute__((always_inline)) {
-      acc[0] = acc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
-      const char* x0 = S + (16 * ti + li) * stride + 16 * lk;
-      const char* y0 = S + (16 * tj + li) * stride + 16 * lk;
-      const int second = tj < ti ? 16 * stride : 0;
-      f16x8 x[2][2], y[2][2][2];  // [stage]
-      auto fetch = [&](int b, int k) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          x[b][h] = *(const f16x8*)(x0 + h * plane + 64 * k);
-          y[b][0][h] = *(const f16x8*)(y0 + h * plane + 64 * k);
-          y[b][1][h] = *(const f16x8*)(y0 + second + h * plane + 64 * k);
-        }
-        if constexpr (decltype(scaled)::value) {
-          const f16x8 by = pow2_8(*(const uint2*)(e + 32 * k + 8 * lk));
-#pragma unroll
-          for (int h = 0; h < 2; ++h) x[b][h] = scaled_twice(x[b][h], by);
+        for (int e = 0; e < 4; ++e) {
+          *(_Float16*)(at + e * SP) = hi[e];
+          *(_Float16*)(at + e * SP + pplane) = lo[e];
         }
       };
-      auto multiply = [&](int b) {
+      // Tiles (ti, tj) and (ti, tj + 1) of S S^T over the 32-column steps k0 <= k < k1, with columns
+      // times 4^e where `scaled`.
+      auto strip_product = [&](const char* S, int stride, int plane, int ti, int tj, int k0, int k1,
+                               auto scaled, const int8_t* e, f32x4 (&acc)[RS]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int h = 0; h < 3; ++h)  // (small products first, the tiles in turn)
+        for (int q = 0; q < RS; ++q) acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const char* x0 = S + (16 * ti + li) * stride + 16 * lk;
+        const char* y0 = S + (16 * tj + li) * stride + 16 * lk;
+        const int second = tj < ti ? 16 * stride : 0;
+        f16x8 x[2][2], y[2][RS][2];  // [stage]
+        auto fetch = [&](int b, int k) {
 #pragma unroll
-          for (int q = 0; q < 2; ++q)
-            acc[q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[b][h == 0], y[b][q][h == 1], acc[q], 0, 0, 0);
+          for (int h = 0; h < 2; ++h) {
+            x[b][h] = *(const f16x8*)(x0 + h * plane + 64 * k);
+            y[b][0][h] = *(const f16x8*)(y0 + h * plane + 64 * k);
+            if (RS > 1) y[b][RS - 1][h] = *(const f16x8*)(y0 + second + h * plane + 64 * k);
+          }
+          if constexpr (decltype(scaled)::value) {
+            const f16x8 by = pow2_8(*(const uint2*)(e + 32 * k + 8 * lk));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) x[b][h] = scaled_twice(x[b][h], by);
+          }
+        };
+        auto multiply = [&](int b) {
+#pragma unroll
+          for (int h = 0; h < 3; ++h)  // (small products first, the tiles in turn)
+#pragma unroll
+            for (int q = 0; q < RS; ++q)
+              acc[q] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[b][h == 0], y[b][q][h == 1], acc[q], 0, 0, 0);
+        };
+        // (past the last step that again: a branch around the loads would wait for all)
+        if (k0 < k1) fetch(0, k0);
+        for (int k = k0; k < k1; k += 2) {
+          fetch(1, k + 1 < k1 ? k + 1 : k1 - 1);
+          multiply(0);
+          if (k + 1 >= k1) break;
+          fetch(0, k + 2 < k1 ? k + 2 : k1 - 1);
+          multiply(1);
+        }
       };
-      // (past the last step that again: a branch around the loads would wait for all)
-      if (k0 < k1) fetch(0, k0);
-      for (int k = k0; k < k1; k += 2) {
-        fetch(1, k + 1 < k1 ? k + 1 : k1 - 1);
-        multiply(0);
-        if (k + 1 >= k1) break;
-        fetch(0, k + 2 < k1 ? k + 2 : k1 - 1);
-        multiply(1);
-      }
-    };
-    const int8_t* const rows = rows_at + (step & 1) * 16 * TR;
-    const int8_t* const cols = cols_at + (step & 1) * C;
-    int8_t* const next_rows = rows_at + (~step & 1) * 16 * TR;
-    int8_t* const next_cols = cols_at + (~step & 1) * C;
-    // exponents of the rows of a strip's tiles that a lane has, and of its columns
-    int of_rows[PER], of_column[PER][2];
-    // ---- A' -------------------------------------------------------------------------
-    if (!even)
-      for (int q = wave; q < C / 16; q += NW) {
-        const int j = 16 * q + li;
-        float m = 0.f;
+      const int8_t* const rows = rows_at + (step & 1) * 16 * TR;
+      const int8_t* const cols = cols_at + (step & 1) * C;
+      int8_t* const next_rows = rows_at + (~step & 1) * 16 * TR;
+      int8_t* const next_cols = cols_at + (~step & 1) * C;
+      // exponents of the rows of a strip's tiles that a lane has, and of its columns
+      int of_rows[PER], of_column[PER][RS];
+      // ---- A' -------------------------------------------------------------------------
+      if (!even)
+        for (int q = wave; q < C / 16; q += NW) {
+          const int j = 16 * q + li;
+          float m = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4 * TR; ++i)
-          m = fmaxf(m, fabsf((float)*(const _Float16*)(X + (4 * i + lk) * SX + 2 * j)));
-        m = ldexpf(column4_max(m), (int)cols[j] - kXBits);
-        if (lane < 16) next_cols[j] = (int8_t)column_exponent(t, m, cols[j]);
-      }
-    auto gram = [&](int b, int k0, int k1, f32x4 (&acc)[2]) __attribute__((always_inline)) {
-      int ti, tj;
-      strip_of(b, ti, tj);
-      if (even) strip_product(X, SX, xplane, ti, tj, k0, k1, std::false_type(), cols, acc);
-      else strip_product(X, SX, xplane, ti, tj, k0, k1, std::true_type(), cols, acc);
-    };
-    if (KS > 1) {
-      for (int q = wave; q < NB * KS; q += NW) {
-        const int b = q % NB, ks = q / NB;
-        f32x4 acc[2];
-        gram(b, ks * pairs / KS, (ks + 1) * pairs / KS, acc);
+          for (int i = 0; i < 4 * TR; ++i)
+            m = fmaxf(m, fabsf((float)*(const _Float16*)(X + (4 * i + lk) * SX + 2 * j)));
+          m = ldexpf(column4_max(m), (int)cols[j] - kXBits);
+          if (lane < 16) next_cols[j] = (int8_t)column_exponent(t, m, cols[j]);
+        }
+      auto gram = [&](int b, int k0, int k1, f32x4 (&acc)[RS]) __attribute__((always_inline)) {
+        int ti, tj;
+        strip_of(b, ti, tj);
+        if (even) strip_product(X, SX, xplane, ti, tj, k0, k1, std::false_type(), cols, acc);
+        else strip_product(X, SX, xplane, ti, tj, k0, k1, std::true_type(), cols, acc);
+      };
+      if (KS > 1) {
+        for (int q = wave; q < NB * KS; q += NW) {
+          const int b = q % NB, ks = q / NB;
+          f32x4 acc[RS];
+          gram(b, ks * pairs / KS, (ks + 1) * pairs / KS, acc);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) part[((ks * NB + b) * 2 + r) * 64 + lane] = acc[r];
+          for (int r = 0; r < RS; ++r) part[((ks * NB + b) * RS + r) * 64 + lane] = acc[r];
+        }
+        __syncthreads();
+      }
+#pragma unroll
+      for (int u = 0; u < PER; ++u) {
+        const int b = wave + u * NW;
+        if (b >= NB) continue;
+        int ti, tj;
+        strip_of(b, ti, tj);
+        of_rows[u] = *(const int*)(rows + 16 * ti + 4 * lk);
+#pragma unroll
+        for (int r = 0; r < RS; ++r) of_column[u][r] = rows[16 * (tj + r < ti ? tj + r : ti) + li];
+        if (KS == 1) gram(b, 0, pairs, held[u]);
+#pragma unroll
+        for (int r = 0; r < RS; ++r) {
+          if (tj + r > ti) continue;
+          if (KS > 1) {
+            held[u][r] = part[(RS * b + r) * 64 + lane];
+#pragma unroll
+            for (int k = 1; k < KS; ++k) held[u][r] += part[((k * NB + b) * RS + r) * 64 + lane];
+          }
+          held[u][r] *= kPow2Less<2 * kXBits>;
+          put_symmetric(ti, tj + r, held[u][r], pow2_4(of_rows[u], 1, kBBits),
+                        ldexpf(1.f, of_column[u][r] + kBBits));
+        }
       }
       __syncthreads();
-    }
+      // ---- P', over B -------------------------------------------------------------------
+      f32x4 poly[PER][RS];
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int b = wave + u * NW;
-      if (b >= NB) continue;
-      int ti, tj;
-      strip_of(b, ti, tj);
-      of_rows[u] = *(const int*)(rows + 16 * ti + 4 * lk);
+      for (int u = 0; u < PER; ++u) {
+        if (wave + u * NW >= NB) continue;
+        int ti, tj;
+        strip_of(wave + u * NW, ti, tj);
 #pragma unroll
-      for (int r = 0; r < 2; ++r) of_column[u][r] = rows[16 * (tj + r < ti ? tj + r : ti) + li];
-      if (KS == 1) gram(b, 0, pairs, held[u]);
+        for (int r = 0; r < RS; ++r)
+          if (tj + r == ti && lk == li >> 2) {
+            const f32x4& v = held[u][r];
+            const int q = li & 3;
+            const float square = q == 0 ? v[0] : q == 1 ? v[1] : q == 2 ? v[2] : v[3];
+            next_rows[16 * ti + li] = (int8_t)next_row_exponent(of_column[u][r], square);
+          }
+        strip_product(A, SP, pplane, ti, tj, 0, TRB, std::false_type(), nullptr, poly[u]);
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        if (tj + r > ti) continue;
-        if (KS > 1) {
-          held[u][r] = part[(2 * b + r) * 64 + lane];
-#pragma unroll
-          for (int k = 1; k < KS; ++k) held[u][r] += part[((k * NB + b) * 2 + r) * 64 + lane];
-        }
-        held[u][r] *= kPow2Less<2 * kXBits>;
-        put_symmetric(ti, tj + r, held[u][r], pow2_4(of_rows[u], 1, kBBits),
-                      ldexpf(1.f, of_column[u][r] + kBBits));
+        for (int r = 0; r < RS; ++r)
+          if (tj + r <= ti) poly[u][r] = kNsB * held[u][r] + (kNsC * kPow2Less<2 * kBBits>) * poly[u][r];
       }
-    }
-    __syncthreads();
-    // ---- P', over B -------------------------------------------------------------------
-    f32x4 poly[PER][2];
+      __syncthreads();
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      if (wave + u * NW >= NB) continue;
-      int ti, tj;
-      strip_of(wave + u * NW, ti, tj);
+      for (int u = 0; u < PER; ++u) {
+        if (wave + u * NW >= NB) continue;
+        int ti, tj;
+        strip_of(wave + u * NW, ti, tj);
 #pragma unroll
-      for (int r = 0; r < 2; ++r)
-        if (tj + r == ti && lk == li >> 2) {
-          const f32x4& v = held[u][r];
-          const int q = li & 3;
-          const float square = q == 0 ? v[0] : q == 1 ? v[1] : q == 2 ? v[2] : v[3];
-          next_rows[16 * ti + li] = (int8_t)next_row_exponent(of_column[u][r], square);
-        }
-      strip_product(A, SP, pplane, ti, tj, 0, TRB, std::false_type(), nullptr, poly[u]);
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-        if (tj + r <= ti) poly[u][r] = kNsB * held[u][r] + (kNsC * kPow2Less<2 * kBBits>) * poly[u][r];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      if (wave + u * NW >= NB) continue;
-      int ti, tj;
-      strip_of(wave + u * NW, ti, tj);
-#pragma unroll
-      for (int r = 0; r < 2; ++r)
-        if (tj + r <= ti)
-          put_symmetric(ti, tj + r, poly[u][r], pow2_4(of_rows[u], 2, kPBits),
-                        ldexpf(1.f, 2 * of_column[u][r] + kPBits));
-    }
-    __syncthreads();
-    // ---- X' --------------------------------------------------------------------------
-    f32x4 next[UMAX][2][RG];
-#pragma unroll
-    for (int u = 0; u < UMAX; ++u) {
-      const int unit = wave + u * NW;
-      if (unit >= pairs * NG) continue;
-      const int pair = unit % pairs, r0 = unit / pairs * RG;
-#pragma unroll
-      for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int r = 0; r < RG; ++r) next[u][p][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-      int by_row[RG];
-#pragma unroll
-      for (int r = 0; r < RG; ++r) {
-        const int row = 16 * (NG * RG > TR && r0 + r >= TR ? TR - 1 : r0 + r) + li;
-        by_row[r] = (int)rows[row] - (int)next_rows[row];
+        for (int r = 0; r < RS; ++r)
+          if (tj + r <= ti)
+            put_symmetric(ti, tj + r, poly[u][r], pow2_4(of_rows[u], 2, kPBits),
+                          ldexpf(1.f, 2 * of_column[u][r] + kPBits));
       }
-      const char* x0 = X + (4 * lk + (li >> 2)) * SX + 64 * pair + 8 * (li & 3);
-      const char* p0 = A + (16 * r0 + li) * SP + 16 * lk;
+      __syncthreads();
+      // ---- X' --------------------------------------------------------------------------
+      f32x4 next[UMAX][2][RG];
 #pragma unroll
-      for (int k = 0; k < TRB; ++k) {
-        f16x8 x[2][2];
+      for (int u = 0; u < UMAX; ++u) {
+        const int unit = wave + u * NW;
+        if (unit >= pairs * NG) continue;
+        const int pair = unit % pairs, r0 = unit / pairs * RG;
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-            // (16 rows are left of an odd number of tiles: their second reading meets the zeros
-            // in P's last 16 columns)
-            x[p][h] = columns(x0 + h * xplane + 32 * k * SX + 32 * p, 2 * k + 1 < TR ? 16 * SX : 0);
-        f16x8 y[RG][2];
+          for (int r = 0; r < RG; ++r) next[u][p][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+        int by_row[RG];
 #pragma unroll
-        for (int r = 0; r < RG; ++r)
+        for (int r = 0; r < RG; ++r) {
+          const int row = 16 * (NG * RG > TR && r0 + r >= TR ? TR - 1 : r0 + r) + li;
+          by_row[r] = (int)rows[row] - (int)next_rows[row];
+        }
+        const char* x0 = X + (4 * lk + (li >> 2)) * SX + 64 * pair + 8 * (li & 3);
+        const char* p0 = A + (16 * r0 + li) * SP + 16 * lk;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            // (a tile past the last one reads the last one again, and is not stored)
-            const int tile = NG * RG > TR && r0 + r >= TR ? r - 1 : r;
-            y[r][h] = *(const f16x8*)(p0 + h * pplane + 16 * tile * SP + 64 * k);
-          }
+        for (int k = 0; k < TRB; ++k) {
+          f16x8 x[2][2];
 #pragma unroll
-        for (int h = 0; h < 3; ++h)
+          for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              // (16 rows are left of an odd number of tiles: their second reading meets the zeros
+              // in P's last 16 columns)
+              x[p][h] = columns(x0 + h * xplane + 32 * k * SX + 32 * p, 2 * k + 1 < TR ? 16 * SX : 0);
+          f16x8 y[RG][2];
 #pragma unroll
           for (int r = 0; r < RG; ++r)
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
-              next[u][p][r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[p][h == 0], y[r][h == 1], next[u][p][r], 0, 0, 0);
-      }
+            for (int h = 0; h < 2; ++h) {
+              // (a tile past the last one reads the last one again, and is not stored)
+              const int tile = NG * RG > TR && r0 + r >= TR ? r - 1 : r;
+              y[r][h] = *(const f16x8*)(p0 + h * pplane + 16 * tile * SP + 64 * k);
+            }
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
+          for (int h = 0; h < 3; ++h)
+#pragma unroll
+            for (int r = 0; r < RG; ++r)
+#pragma unroll
+              for (int p = 0; p < 2; ++p)
+                next[u][p][r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[p][h == 0], y[r][h == 1], next[u][p][r], 0, 0, 0);
+        }
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int r = 0; r < RG; ++r) {
+            if (NG * RG > TR && r0 + r >= TR) continue;
+            next[u][p][r] = add4(kNsA, X + (16 * (r0 + r) + li) * SX + 2 * (32 * pair + 16 * p + 4 * lk),
+                                 xplane, kPow2Less<kPBits> * next[u][p][r]);
+          }
 #pragma unroll
         for (int r = 0; r < RG; ++r) {
-          if (NG * RG > TR && r0 + r >= TR) continue;
-          next[u][p][r] = add4(kNsA, X + (16 * (r0 + r) + li) * SX + 2 * (32 * pair + 16 * p + 4 * lk),
-                               xplane, kPow2Less<kPBits> * next[u][p][r]);
-        }
 #pragma unroll
-      for (int r = 0; r < RG; ++r) {
+          for (int p = 0; p < 2; ++p) {
+            next[u][p][r] *= ldexpf(1.f, by_row[r]);
+            if (even) continue;
+            const int col = 32 * pair + 16 * p + 4 * lk;
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          next[u][p][r] *= ldexpf(1.f, by_row[r]);
-          if (even) continue;
-          const int col = 32 * pair + 16 * p + 4 * lk;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            next[u][p][r][e] = ldexpf(next[u][p][r][e], (int)cols[col + e] - (int)next_cols[col + e]);
+            for (int e = 0; e < 4; ++e)
+              next[u][p][r][e] = ldexpf(next[u][p][r][e], (int)cols[col + e] - (int)next_cols[col + e]);
+          }
         }
       }
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < UMAX; ++u) {
+        const int unit = wave + u * NW;
+        if (unit >= pairs * NG) continue;
+        const int pair = unit % pairs, r0 = unit / pairs * RG;
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int r = 0; r < RG; ++r) {
+            if (NG * RG > TR && r0 + r >= TR) continue;
+            const int row = 16 * (r0 + r) + li, col = 32 * pair + 16 * p + 4 * lk;
+            if (step + 1 < steps) put4(X + row * SX + 2 * col, xplane, next[u][p][r]);
+            else *(f32x4*)(X + row * XF + 4 * col) = next[u][p][r];
+          }
+      }
+      __syncthreads();
     }
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < UMAX; ++u) {
-      const int unit = wave + u * NW;
-      if (unit >= pairs * NG) continue;
-      const int pair = unit % pairs, r0 = unit / pairs * RG;
-#pragma unroll
-      for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int r = 0; r < RG; ++r) {
-          if (NG * RG > TR && r0 + r >= TR) continue;
-          const int row = 16 * (r0 + r) + li, col = 32 * pair + 16 * p + 4 * lk;
-          if (step + 1 < steps) put4(X + row * SX + 2 * col, xplane, next[u][p][r]);
-          else *(f32x4*)(X + row * XF + 4 * col) = next[u][p][r];
-        }
-    }
-    __syncthreads();
-  }
 
-  // ---- the result ---------------------------------------------------------------------
-  const float gain = ns_gain(t);
-  const int8_t* const rows = rows_at + (steps & 1) * 16 * TR;
-  const int8_t* const cols = cols_at + (steps & 1) * C;
-  Walk<NT> w(tid, t);
+    // ---- the result ---------------------------------------------------------------------
+    const float gain = ns_gain(t);
+    const int8_t* const rows = rows_at + (steps & 1) * 16 * TR;
+    const int8_t* const cols = cols_at + (steps & 1) * C;
+    Walk<NT> w(tid, t);
 #pragma unroll 4
-  for (int e = tid; e < n; e += NT) {
-    const int i = turned ? w.j : w.i, j = turned ? w.i : w.j;
-    const float x = ldexpf(*(const float*)(X + i * XF + 4 * j), (int)rows[i] + (even ? 0 : (int)cols[j]) - kXBits);
-    if (a.W) apply(a, t, w.i, w.j, gain * x);
-    else a.out[t.src + w.at] = x;
-    w.next();
-  }
-  if (a.W && a.lrm && tid == 0 && !(fabsf(a.lrm[t.m]) < INFINITY)) a.flag[1] = 1;
+    for (int e = tid; e < n; e += NT) {
+      const int i = turned ? w.j : w.i, j = turned ? w.i : w.j;
+      const float x = ldexpf(*(const float*)(X + i * XF + 4 * j), (int)rows[i] + (even ? 0 : (int)cols[j]) - kXBits);
+      if (a.W) apply(a, t, w.i, w.j, gain * x);
+      else a.out[t.src + w.at] = x;
+      w.next();
+    }
+    if (a.W && a.lrm && tid == 0 && !(fabsf(a.lrm[t.m]) < INFINITY)) a.flag[1] = 1;
+  };
+  if (even) iterate(std::true_type());
+  else iterate(std::false_type());
 }
 
 }  // namespace
@@ -520,8 +528,7 @@ __global__ __launch_bounds__(64 * kNsWaves[TR - 1], OCC) void k_ns_small(NsArgs 
 }
 
 // Few rows and many columns, at four waves a SIMD (k_ns_small_any takes the registers of two, and
-// one workgroup a compute unit: 4,085 matrices of 10 x 6 to 219 took 127 us, 62 so; 600 of 10 x 1 to
-// 100 in one launch 39, 15 so).
+// one workgroup a compute unit: 600 matrices of 10 x 1 to 100 in one launch 48 us, 17 so).
 __global__ __launch_bounds__(64 * kNsWaves[kNsLow], 4) void k_ns_low(NsArgs a, const int32_t* list, int steps) {
   constexpr int NW = kNsWaves[kNsLow];
   extern __shared__ __align__(16) char lds[];

@@ -520,8 +520,8 @@ __global__ __launch_bounds__(256) void k_rt_few(RtArgs a, RtFew f) {
 }
 
 // .. and a wave, for up to 64 columns and 1,024 such chunks or more.  (130 models of 1 to 250
-// units, 37 columns, 2,048 slots 12.7 us against 18.0, 256 slots the same; 200 of 100 to 200, 200
-// columns, 1,024 slots 27.5 against 23.4.)
+// units, 2,048 slots with the join, 37 columns 14.5 us either way, 64 columns 14.0 against 14.4, 65
+// columns 17.7 either way, 100 columns 18.8 against 19.1; 256 slots of 37 columns 7.9 against 7.3.)
 template <bool GATED>
 __global__ __launch_bounds__(256) void k_rt_few_waves(RtArgs a, RtFew f) {
   const int lane = threadIdx.x & 63;

@@ -125,7 +125,7 @@ inline size_t ns_small_lds(int32_t r, int32_t c, int waves) {
   const int cp = (c + 31) / 32 * 32, rp = (r + 31) / 32 * 32, tr = (r + 15) / 16;
   const int split = ns_small_split(tr, waves);
   return (size_t)32 * tr * ((2 * cp + 16) + (2 * rp + 16)) +
-         (split > 1 ? (size_t)split * ns_strips(tr) * 2048 : 0) + 32 * tr + 2 * cp + 16;
+         (split > 1 ? (size_t)split * ns_strips(tr) * (tr == 1 ? 1024 : 2048) : 0) + 32 * tr + 2 * cp + 16;
 }
 // The class of an r x c matrix, or -1.
 inline int ns_small_class(int32_t r, int32_t c) {
@@ -138,10 +138,11 @@ inline int ns_small_class(int32_t r, int32_t c) {
   return kNsLow + 1 + k;
 }
 // Up to so many matrices go in one launch whatever their classes, and up to twice as many in two,
-// the low ones and the others: each launch ends with workgroups that wait for its longest.  Low
-// ones alone are one launch of theirs.  (us, one / two / by class: 300 matrices of 1 to 100 rows,
-// 100 columns 56 / 73 / 200, 1,000: 121 / 124 / 204, 2,000: 227 / 217 / 269; 6,000 by class 507;
-// 2,040 of 1 to 64 rows, 64 columns 145 / 111.)
+// the low ones and the others, if one of them has more than 64 rows: each launch ends with workgroups
+// that wait for its longest.  Low ones alone are one launch of theirs.  (us, one / two / by class:
+// 300 matrices of 1 to 100 rows, 100 columns 65 / 85 / 236, 1,000: 144 / 146 / 241, 2,000: 272 / 259 /
+// 313, 6,000: 790 / 692 / 512; 300 of 1 to 64 rows, 64 columns 39 / 49 / 85, 1,000: 97 / 77 / 90, 2,040:
+// 186 / 132 / 99.)
 constexpr int kNsOneLaunch = 1024;
 // From the gradient to the result, a workgroup for each matrix of the list; classes above
 // kNsLow: any of the classes.

@@ -3355,7 +3355,8 @@ int pmlp_muon_step(pmlp_t h, int32_t matrix, const float* G_dev, float* mom_dev,
     return fail(PMLP_EINVAL, "mu, lr and decay must be finite");
   if (steps < 0 || steps > kMaxSteps) return fail(PMLP_EINVAL, "steps must be in [0, 10]");
   const size_t n = matrix_bytes(h, matrix);
-  if (overlap({G_dev, n}, {mom_dev, n})) return fail(PMLP_EINVAL, "the buffers overlap");
+  if (overlap({G_dev, n}, {mom_dev, n}) || overlap({lr_dev, (size_t)h->M * sizeof(float)}, {mom_dev, n}))
+    return fail(PMLP_EINVAL, "the buffers overlap");
   NsArgs a{};
   a.G = G_dev;
   a.mom_in = mom_dev;

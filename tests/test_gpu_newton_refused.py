@@ -32,3 +32,17 @@ def test_a_refused_update_changes_nothing(pm):
     assert all(np.array_equal(a, b) for a, b in zip(net.get_params(), weights))
     net.muon_step(G, 0.1, momentum=mom)  # the pack as it was: one update, of every model
     assert torch.allclose(mom, 0.95 * held + G, rtol=1e-6, atol=1e-6)
+
+
+@pytest.mark.parametrize("steps", [0, 5])
+def test_rates_inside_the_momentum_are_refused(pm, steps):
+    """The momentum is written while models still read their rates."""
+    net = pm.PackedMLP(20, 2, [30, 9], [2, 2])
+    G, mom = randn(1, 39, 20).cuda(), randn(2, 39, 20).cuda()
+    weights, held = net.get_params(), mom.clone()
+    for rates in (mom.reshape(-1)[:2], mom.reshape(-1)[-2:]):
+        with pytest.raises(pm.PmlpError, match="overlap"):
+            net.muon_step(G, rates, momentum=mom, steps=steps)
+    torch.cuda.synchronize()
+    assert torch.equal(mom, held)
+    assert all(np.array_equal(a, b) for a, b in zip(net.get_params(), weights))

@@ -225,9 +225,10 @@ hipError_t launch_ns_load(const NsArgs& a, const NsItem* items, int32_t n, hipSt
 // LDS, where it is read by rows of either order, 16 bytes a lane.
 //
 // Bound by the matrix cores behind LDS and two barriers a stage, and by the stores of both
-// orders: 40 matrices of 500 to 1,000 x 1,000 119 us for A, 101 for P, 237 for a step (193, 181
-// and 194 TFLOP/s of the 355 that three fp16 products at a large library product's rate make;
-// MFMA busy 0.39, 0.39, 0.33).  Steps of 128 x 128 tiles took 254 us where these take 240.
+// orders: 40 matrices of 500 to 1,000 x 1,000 120 us for A, 108 for P, 247 for a step (191, 169
+// and 186 TFLOP/s of the 355 that three fp16 products at a large library product's rate make;
+// MFMA busy 0.38, 0.35, 0.31), 119, 101 and 237 without the scales.  Steps of 128 x 128 tiles
+// took 254 us where these took 240.
 // ---------------------------------------------------------------------------
 
 template <int WHAT, int T, int TJ>

@@ -14,8 +14,10 @@
 // banks.  The transposing loads read 32 bytes of each of eight rows, and a mirrored tile is stored
 // 2 bytes a lane and four rows apart: two ways on a bank.
 //
-// Bound by LDS and latency: a 2 x 4 block of tiles reads 12 fragments for its 24
-// matrix instructions, what one LDS feeds four SIMDs with.
+// Bound by LDS, vector work and latency: a 2 x 4 block of tiles reads 12 fragments for its 24
+// matrix instructions, what one LDS feeds four SIMDs with.  10,000 matrices of 1 to 100 x 100: 581
+// us; LDS busy 0.37 to 0.48 of the time and 0.42 of that with bank conflicts, VALU 0.43 to 0.57 with
+// halving and scaling, one to three workgroups a compute unit.  (507 us without the scales.)
 
 #include <algorithm>
 #include <type_traits>

@@ -1,7 +1,7 @@
 """Bounds of the Newton-Schulz steps for matrices whose rows and columns are of unlike size.
 
 A matrix is D M0 E with D and E diagonal and M0 of even size.  The steps commute with E
-(X <- (a + P) X) and treat a row of X as a whole, so what fp32 keeps is judged beside a row's
+(X <- (a + P) X) and treat a row of X as a whole, so what fp32 keeps is measured beside a row's
 and a column's own size, not beside the largest entry."""
 import torch
 

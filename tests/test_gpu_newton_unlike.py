@@ -74,6 +74,19 @@ def test_many_models(pm, F):
         check(got[at[m]:at[m + 1]], mats[m:m + 1], 5, "model %d" % m)
 
 
+@pytest.mark.parametrize("F,h,M", [(380, 250, 90), (250, 380, 90), (200, 256, 130)])
+def test_large_tiles(pm, F, h, M):
+    """512 tiles of 128 x 128 and more, with partly empty ones at their ends; turned and not."""
+    net = pm.PackedMLP(F, 2, [h] * M, [0] * M)
+    mats = [nb.unlike(h, F, nb.KINDS[m % 4], m) for m in range(M)]
+    G = torch.cat([A for A, _, _ in mats]).float().cuda()
+    got = net.orthogonalize(G)
+    assert net.kernel_variants()["hidden2"][0] == "k_ns_product"
+    for m in (0, 1, 2, 3, M - 4, M - 3, M - 2, M - 1):
+        check(got[h * m:h * (m + 1)], mats[m:m + 1], 5, "model %d" % m)
+    assert torch.equal(got, net.orthogonalize(G))
+
+
 @pytest.mark.parametrize("F,hs", [(50, [8, 40]), (200, [150, 9])])
 def test_tiny_rows_do_not_vanish(pm, F, hs):
     """Rows of 1e-20 of the others grow by 3.4445 in each of five steps, as they do in fp32."""
